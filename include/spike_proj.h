@@ -25,7 +25,11 @@
  * a spike producer (spike_proj_lif, and spike_proj_group_decode_lif with the
  * producer inside the decode launch), and the vocabulary head with INT8
  * activations and FP32 recomputation of the top candidates (spike_proj_head,
- * Section 5).  Each is documented at its declaration below.
+ * Section 5).  For decode steps of drafted tokens it has the operators around
+ * a KV cache: attention of a batch that shares a long prefix
+ * (spike_proj_cache_attend), eviction by accumulated attention weight
+ * (spike_proj_cache_evict) and verification of the drafts
+ * (spike_proj_verify).  Each is documented at its declaration below.
  *
  * Conventions for every call
  *   - Pointers named d_* or documented as "device" are CUDA device pointers
@@ -61,10 +65,18 @@ extern "C" {
 #define SPIKE_PROJ_HEAD_MAX_CAND 64    /* largest k_sel of spike_proj_head */
 #define SPIKE_PROJ_HEAD_MAX_K 8192     /* largest hidden width of a head */
 #define SPIKE_PROJ_HEAD_MAX_V (1 << 26) /* largest vocabulary of a head */
+#define SPIKE_PROJ_CACHE_MAX_B 1024    /* sequences of a cache */
+#define SPIKE_PROJ_CACHE_MAX_T 32      /* query tokens per sequence and attend call */
+#define SPIKE_PROJ_CACHE_MAX_HEADS 512 /* query heads of a cache */
+#define SPIKE_PROJ_CACHE_MAX_D 128     /* largest head width of a cache */
+#define SPIKE_PROJ_CACHE_MAX_LEN (1 << 24) /* longest prefix, largest capacity */
+#define SPIKE_PROJ_VERIFY_MAX_T 64     /* drafted tokens per sequence */
+#define SPIKE_PROJ_VERIFY_MAX_V (1 << 24) /* largest vocabulary of a verification */
 
 typedef struct sp_plan_s *sp_plan_t;
 typedef struct sp_group_s *sp_group_t;
 typedef struct sp_head_s *sp_head_t;
+typedef struct sp_cache_s *sp_cache_t;
 typedef void *sp_stream_t;             /* a cudaStream_t */
 
 typedef enum sp_status {
@@ -503,6 +515,193 @@ sp_status spike_proj_head(sp_head_t head, const float *h, int64_t ldh, int32_t B
                           float tau, int32_t k_sel, int32_t *token,
                           int32_t *verified, float *gap, int32_t *cand, float *r,
                           float *z, int64_t ld_z, sp_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over a KV cache whose sequences share a prefix, and the upkeep of
+ * the sequences' own caches (the block's attention path keeps a KV cache,
+ * Section 2.1; the paper does not describe its layout, so the layout here is
+ * this library's).
+ *
+ * Every sequence b sees the same prefix of P entries and an own cache of up to
+ * `capacity` entries, of which the first lens[b] are in use.  An entry is one
+ * key and one value of D elements per K/V head; Hq query heads share Hkv K/V
+ * heads, query head i reading K/V head i / (Hq / Hkv).  K, V, q and out have
+ * one 16-bit type (sp_dtype).  Tensors are strided: strides are counted in
+ * elements, the D elements of a row are contiguous.
+ *
+ * spike_proj_cache_create: the handle owns workspace for calls of up to
+ *   max_batch sequences and max_T query tokens each, and no entry of any
+ *   cache.  1 <= max_batch <= SPIKE_PROJ_CACHE_MAX_B, 1 <= max_T <=
+ *   SPIKE_PROJ_CACHE_MAX_T, 1 <= Hq <= SPIKE_PROJ_CACHE_MAX_HEADS,
+ *   8 <= D <= SPIKE_PROJ_CACHE_MAX_D, 1 <= capacity <=
+ *   SPIKE_PROJ_CACHE_MAX_LEN (else SP_ERANGE); Hq % Hkv == 0 (SP_EINVAL);
+ *   D % 8 == 0 (SP_EALIGN).  flags: SP_CACHE_WEIGHTS, needed for attend calls
+ *   that accumulate weights (workspace of 4 bytes per K/V head, query row and
+ *   own entry).  A handle serves one stream at a time, on the device that was
+ *   current when it was made (SP_EDEVICE on another).
+ * ------------------------------------------------------------------------- */
+typedef enum sp_dtype {
+    SP_BF16 = 0,
+    SP_FP16 = 1
+} sp_dtype;
+
+#define SP_CACHE_WEIGHTS 0x1u
+
+sp_status spike_proj_cache_create(sp_cache_t *cache, int32_t max_batch,
+                                  int32_t max_T, int32_t Hq, int32_t Hkv,
+                                  int32_t D, int32_t capacity, int32_t dtype,
+                                  uint32_t flags, sp_stream_t stream);
+sp_status spike_proj_cache_destroy(sp_cache_t cache);
+
+/* Synchronises the stream and returns SP_EKERNEL, once, when a kernel of the
+ * handle gave up on a wait since the last call. */
+sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream);
+
+/* spike_proj_cache_attend: T query tokens of each of B sequences.  The own
+ * cache already holds the entries of these T tokens as its last ones; query t
+ * sees the whole prefix and the own entries j < lens[b] - (T - 1 - t):
+ *
+ *     s_j  = scale * sum_d q_d k_jd            FP32
+ *     lse  = ln sum_j exp(s_j)
+ *     out  = sum_j exp(s_j - lse) v_j          rounded once to the type
+ *     weights[b][h][j] += sum over query tokens t and the query heads of K/V
+ *                         head h of exp(s_j - lse)      (own entries, FP32)
+ *
+ * A row that sees no entry (or scores of minus infinity alone) gives out = 0,
+ * lse = -infinity and no weight.  Entries that no row sees are never used,
+ * whatever they hold; a NaN that a row sees makes that row NaN.  The
+ * probabilities are rounded to the type before they meet V (relative error
+ * 2^-9 or 2^-12 each); scores, the running maximum and sum, and the sums over
+ * V are FP32.  Results do not depend on the order in which blocks run.
+ *
+ *   lens       device int32 [B]; values outside 0 .. capacity are taken as
+ *              the nearest end.
+ *   lse        FP32 [B][T][Hq] contiguous, or NULL.
+ *   weights    FP32, entry j of (b, h) at b*weights_batch + h*weights_head + j,
+ *              read and written for j < lens[b]; NULL for none (a handle
+ *              without SP_CACHE_WEIGHTS: SP_EUNSUPPORTED).
+ *   scale      finite and > 0 (SP_EINVAL).
+ * prefix_k / prefix_v may be NULL when prefix_len is 0.  q, out, K and V:
+ * 16-byte aligned, strides of dimensions longer than 1 multiples of 8 (and
+ * positive for K and V, |stride| >= D for out), else SP_EALIGN.  A B above
+ * max_batch, a T above max_T, a prefix above SPIKE_PROJ_CACHE_MAX_LEN or a
+ * call of 2^30 tiles of 128 entries and more: SP_ERANGE. */
+typedef struct sp_attend {
+    const void *q;                        /* [B][T][Hq][D] */
+    int64_t q_batch, q_token, q_head;
+    const void *prefix_k, *prefix_v;      /* [prefix_len][Hkv][D] */
+    int64_t pk_entry, pk_head, pv_entry, pv_head;
+    const void *k, *v;                    /* [B][capacity][Hkv][D] */
+    int64_t k_batch, k_entry, k_head, v_batch, v_entry, v_head;
+    const int32_t *lens;
+    void *out;                            /* [B][T][Hq][D] */
+    int64_t out_batch, out_token, out_head;
+    float *lse;
+    float *weights;                       /* [B][Hkv][capacity] */
+    int64_t weights_batch, weights_head;
+    int32_t B, T, prefix_len;
+    float scale;
+} sp_attend;
+
+sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend *call,
+                                  sp_stream_t stream);
+
+/* spike_proj_cache_evict: brings the own cache of each of B sequences down to
+ * `budget` entries per K/V head, each head on its own.  With n = lens[b]
+ * (taken into 0 .. capacity):
+ *
+ *   n <= budget: every entry stays where it is.
+ *   n > budget:  the entries are ordered: those with pos >= now[b] - recent
+ *                first, then by weight descending (NaN above all, -0 as +0),
+ *                equal ones by lower slot; the first `budget` are kept.  A
+ *                kept entry below slot `budget` stays.  Each slot below
+ *                `budget` whose entry goes, in ascending order, receives the
+ *                next kept entry from slot `budget` on, in ascending order.
+ *
+ * So the order of arrival is not the order of slots afterwards; pos keeps it
+ * (attention itself does not depend on it).  K and V move in place, reading
+ * slots >= budget and writing slots < budget only; weight and pos of slot j of
+ * the result go to weights_out and pos_out (j < min(n, budget); the rest of
+ * them is left alone), min(n, budget) to lens_out[b].  The outputs must not
+ * overlap the inputs (SP_EINVAL where the pointers are equal).
+ *
+ *   weights, pos           FP32 / int32, entry j of (b, h) at
+ *                          b*in_batch + h*in_head + j
+ *   weights_out, pos_out   likewise with out_batch, out_head (out_head >=
+ *                          min(budget, capacity) and so on: slots must not
+ *                          overlap); may be NULL when budget is 0
+ *   lens, now, lens_out    device int32 [B]
+ *   0 <= recent <= budget (SP_EINVAL).  K and V: as for attend (positive
+ *   strides; the whole of a row is copied).
+ * Errors: SP_EINVAL, SP_EALIGN, SP_ERANGE (B above max_batch), SP_EDEVICE,
+ * SP_ECUDA. */
+typedef struct sp_evict {
+    void *k, *v;                          /* [B][capacity][Hkv][D] */
+    int64_t k_batch, k_entry, k_head, v_batch, v_entry, v_head;
+    const float *weights;                 /* [B][Hkv][capacity] */
+    const int32_t *pos;
+    int64_t in_batch, in_head;
+    float *weights_out;                   /* [B][Hkv][>= min(budget, capacity)] */
+    int32_t *pos_out;
+    int64_t out_batch, out_head;
+    const int32_t *lens, *now;
+    int32_t *lens_out;
+    int32_t B, budget, recent;
+} sp_evict;
+
+sp_status spike_proj_cache_evict(sp_cache_t cache, const sp_evict *call,
+                                 sp_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * spike_proj_verify: how many drafted tokens of each sequence the target model
+ * keeps, and the token that follows them, from given random numbers.  For
+ * sequence b with n_draft[b] drafts x_0 .. (0 .. T; NULL: T each):
+ *
+ *   draft t is kept when u[b][t] * q[b][t][x_t] < p[b][t][x_t] (one FP32
+ *   multiply; an x_t outside 0 .. V-1, or a NaN, is not kept); n = the drafts
+ *   kept before the first that is not (or before n_draft[b])
+ *   r_v = p[b][n][v] - q[b][n][v] (n < n_draft[b]), else p[b][n][v]     FP32
+ *   w_v = rint(min(r_v, 1) * 2^36) where r_v > 0, else 0       whole numbers
+ *   S   = sum_v w_v,  c = floor(floor(u_sample[b] * 2^24) * S / 2^24)
+ *   the token is the first v with w_0 + .. + w_v > c.  S = 0: the same with
+ *   r_v = p[b][n][v]; S = 0 again: -1.
+ *
+ * The sums are whole numbers, so that no order of summation changes the token.
+ * u and u_sample are taken into [0, 1 - 2^-24] (NaN as 0).
+ *
+ *   p          FP32, row t of sequence b at p + b*p_batch + t*p_row, T+1 rows
+ *              of V: the target's probabilities after 0 .. T drafts
+ *   q          FP32, likewise, T rows: the drafting model's (NULL when T is 0)
+ *   draft      int32 [B], row stride ld_draft >= T (NULL when T is 0)
+ *   u          FP32 [B], row stride ld_u >= T (NULL when T is 0)
+ *   u_sample   FP32 [B]
+ *   n_accept   int32 [B]: n
+ *   tokens     int32 [B], row stride ld_tokens >= T+1: the n kept drafts, the
+ *              token after them, -1 from there on
+ *   0 <= T <= SPIKE_PROJ_VERIFY_MAX_T, 1 <= V <= SPIKE_PROJ_VERIFY_MAX_V,
+ *   1 <= B <= 65535 (SP_ERANGE); 4-byte aligned pointers (SP_EALIGN).
+ * Of p and q only the entries at the drafts and the one row of each that the
+ * token is drawn from are read.
+ * Errors: SP_EINVAL, SP_EALIGN, SP_ERANGE, SP_EDEVICE, SP_ECUDA.
+ * ------------------------------------------------------------------------- */
+typedef struct sp_verify {
+    const float *p;
+    int64_t p_batch, p_row;
+    const float *q;
+    int64_t q_batch, q_row;
+    const int32_t *draft;
+    int64_t ld_draft;
+    const int32_t *n_draft;
+    const float *u;
+    int64_t ld_u;
+    const float *u_sample;
+    int32_t *n_accept;
+    int32_t *tokens;
+    int64_t ld_tokens;
+    int32_t B, T, V;
+} sp_verify;
+
+sp_status spike_proj_verify(const sp_verify *call, sp_stream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Test faults -- FOR TESTS OF THE ERROR PATH ONLY (the paper has no

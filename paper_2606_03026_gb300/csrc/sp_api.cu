@@ -5,11 +5,13 @@
 #include <cstdlib>
 #include <algorithm>
 #include <chrono>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 #include <new>
 #include <thread>
 
+#include "sp_cache.h"
 #include "sp_gemm.h"
 #include "sp_internal.h"
 
@@ -78,6 +80,13 @@ struct sp_head_s {
   uint8_t* ws = nullptr;          // head_workspace_bytes()
 };
 
+struct sp_cache_s {
+  int device = 0;
+  CacheShape shape;
+  uint8_t* ws = nullptr;          // cache_workspace(shape).bytes
+  int* err = nullptr;             // device error word
+};
+
 struct sp_group_s {
   int32_t count = 0;
   int32_t maxN = 0, maxK = 0;
@@ -140,6 +149,13 @@ sp_status check_device(int* dev_out) {
   if (major != 10 || minor != 3) return SP_EDEVICE;
   *dev_out = dev;
   return SP_OK;
+}
+
+// Whether the current device is the one a handle was made on.
+sp_status on_device(int device) {
+  int dev = 0;
+  SP_CUDA(cudaGetDevice(&dev));
+  return dev == device ? SP_OK : SP_EDEVICE;
 }
 
 template <typename T>
@@ -1154,12 +1170,144 @@ sp_status spike_proj_head(sp_head_t hd, const float* h, int64_t ldh, int32_t B, 
   return SP_OK;
 }
 
+sp_status spike_proj_cache_create(sp_cache_t* cache, int32_t max_batch, int32_t max_T, int32_t Hq,
+                                  int32_t Hkv, int32_t D, int32_t capacity, int32_t dtype,
+                                  uint32_t flags, sp_stream_t stream) {
+  if (!cache || (dtype != SP_BF16 && dtype != SP_FP16) || (flags & ~SP_CACHE_WEIGHTS)) return SP_EINVAL;
+  if (max_batch < 1 || max_batch > SPIKE_PROJ_CACHE_MAX_B || max_T < 1 || max_T > SPIKE_PROJ_CACHE_MAX_T ||
+      Hq < 1 || Hq > SPIKE_PROJ_CACHE_MAX_HEADS || D < 8 || D > SPIKE_PROJ_CACHE_MAX_D || capacity < 1 ||
+      capacity > SPIKE_PROJ_CACHE_MAX_LEN)
+    return SP_ERANGE;
+  if (Hkv < 1 || Hq % Hkv != 0) return SP_EINVAL;
+  if (D % 8 != 0) return SP_EALIGN;
+  int dev = 0, sms = 0;
+  sp_status st = check_device(&dev);
+  if (st != SP_OK) return st;
+  SP_CUDA(current_device(&dev, &sms));
+  sp_cache_s* ca = new (std::nothrow) sp_cache_s();
+  if (!ca) return SP_ENOMEM;
+  ca->device = dev;
+  ca->shape = CacheShape{max_batch, max_T, Hq, Hkv, D, capacity, dtype, (flags & SP_CACHE_WEIGHTS) != 0};
+  cudaStream_t s = as_stream(stream);
+  // (the workspace needs no clearing: every call writes what it reads)
+  cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&ca->ws), cache_workspace(ca->shape, sms).bytes);
+  if (e != cudaSuccess) {
+    ca->ws = nullptr;
+    (void)cudaGetLastError();
+    g_last_cuda_error = (int)e;
+    st = e == cudaErrorMemoryAllocation ? SP_ENOMEM : SP_ECUDA;
+  }
+  if (st == SP_OK) st = dev_alloc_zero(&ca->err, 1, s);
+  if (st == SP_OK && (e = cudaStreamSynchronize(s)) != cudaSuccess) st = cuda_fail(e);
+  if (st != SP_OK) {
+    cudaFree(ca->ws);
+    cudaFree(ca->err);
+    delete ca;
+    return st;
+  }
+  *cache = ca;
+  return SP_OK;
+}
+
+sp_status spike_proj_cache_destroy(sp_cache_t cache) {
+  if (!cache) return SP_OK;
+  cudaError_t e = cudaDeviceSynchronize();
+  cudaFree(cache->ws);
+  cudaFree(cache->err);
+  delete cache;
+  return e == cudaSuccess ? SP_OK : cuda_fail(e);
+}
+
+sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream) {
+  if (!cache) return SP_EINVAL;
+  cudaStream_t s = as_stream(stream);
+  int err = 0;
+  SP_CUDA(cudaMemcpyAsync(&err, cache->err, sizeof(err), cudaMemcpyDeviceToHost, s));
+  SP_CUDA(cudaStreamSynchronize(s));
+  if (err == 0) return SP_OK;
+  SP_CUDA(cudaMemsetAsync(cache->err, 0, sizeof(err), s));
+  SP_CUDA(cudaStreamSynchronize(s));
+  return SP_EKERNEL;
+}
+
+sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend* c, sp_stream_t stream) {
+  if (!cache || !c || !c->q || !c->k || !c->v || !c->lens || !c->out) return SP_EINVAL;
+  const CacheShape& sh = cache->shape;
+  if (c->B < 1 || c->T < 1 || c->prefix_len < 0 || !(c->scale > 0.f) || !std::isfinite(c->scale)) return SP_EINVAL;
+  if (c->prefix_len > 0 && (!c->prefix_k || !c->prefix_v)) return SP_EINVAL;
+  if (c->B > sh.max_batch || c->T > sh.max_T || c->prefix_len > SPIKE_PROJ_CACHE_MAX_LEN) return SP_ERANGE;
+  if (c->weights && !sh.weights) return SP_EUNSUPPORTED;
+  // tiles of 128 entries that the launch counts in 32 bits
+  const int64_t rows = (int64_t)c->T * (sh.Hq / sh.Hkv);
+  const int64_t tiles = (c->B * rows + 127) / 128 * ((c->prefix_len + 127) / 128) +
+                        c->B * ((rows + 127) / 128) * (((int64_t)sh.capacity + 127) / 128);
+  if (tiles * sh.Hkv >= (int64_t)1 << 30) return SP_ERANGE;
+  const auto any = [](int64_t n, int64_t stride) { return n == 1 || stride % 8 == 0; };
+  const auto kv = [&](int64_t n, int64_t stride) { return n <= 1 || (stride % 8 == 0 && stride > 0); };
+  const auto out = [&](int64_t n, int64_t stride) {
+    return n == 1 || (stride % 8 == 0 && (stride >= sh.D || stride <= -sh.D));
+  };
+  if (!aligned(c->q, 16) || !aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->out, 16) ||
+      !aligned(c->lens, 4) || (c->lse && !aligned(c->lse, 4)) || (c->weights && !aligned(c->weights, 4)) ||
+      !any(c->B, c->q_batch) || !any(c->T, c->q_token) || !any(sh.Hq, c->q_head) || !out(c->B, c->out_batch) ||
+      !out(c->T, c->out_token) || !out(sh.Hq, c->out_head) || !kv(c->B, c->k_batch) ||
+      !kv(sh.capacity, c->k_entry) || !kv(sh.Hkv, c->k_head) || !kv(c->B, c->v_batch) ||
+      !kv(sh.capacity, c->v_entry) || !kv(sh.Hkv, c->v_head))
+    return SP_EALIGN;
+  if (c->prefix_len > 0 &&
+      (!aligned(c->prefix_k, 16) || !aligned(c->prefix_v, 16) || !kv(c->prefix_len, c->pk_entry) ||
+       !kv(sh.Hkv, c->pk_head) || !kv(c->prefix_len, c->pv_entry) || !kv(sh.Hkv, c->pv_head)))
+    return SP_EALIGN;
+  const sp_status st = on_device(cache->device);
+  if (st != SP_OK) return st;
+  SP_CUDA(launch_attend(sh, *c, cache->ws, cache->err, as_stream(stream)));
+  return SP_OK;
+}
+
+sp_status spike_proj_cache_evict(sp_cache_t cache, const sp_evict* c, sp_stream_t stream) {
+  if (!cache || !c || !c->k || !c->v || !c->weights || !c->pos || !c->lens || !c->now || !c->lens_out)
+    return SP_EINVAL;
+  const CacheShape& sh = cache->shape;
+  if (c->budget != 0 && (!c->weights_out || !c->pos_out)) return SP_EINVAL;
+  if (c->B < 1 || c->budget < 0 || c->recent < 0 || c->recent > c->budget) return SP_EINVAL;
+  if (c->weights == c->weights_out || c->pos == c->pos_out || c->lens == c->lens_out) return SP_EINVAL;
+  if (c->B > sh.max_batch) return SP_ERANGE;
+  const auto kv = [](int64_t n, int64_t stride) { return n == 1 || (stride % 8 == 0 && stride > 0); };
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !kv(c->B, c->k_batch) || !kv(sh.capacity, c->k_entry) ||
+      !kv(sh.Hkv, c->k_head) || !kv(c->B, c->v_batch) || !kv(sh.capacity, c->v_entry) || !kv(sh.Hkv, c->v_head))
+    return SP_EALIGN;
+  for (const void* x : {(const void*)c->weights, (const void*)c->pos, (const void*)c->weights_out,
+                        (const void*)c->pos_out, (const void*)c->lens, (const void*)c->now, (const void*)c->lens_out})
+    if (!aligned(x, 4)) return SP_EALIGN;
+  const sp_status st = on_device(cache->device);
+  if (st != SP_OK) return st;
+  SP_CUDA(launch_evict(sh, *c, cache->ws, as_stream(stream)));
+  return SP_OK;
+}
+
+sp_status spike_proj_verify(const sp_verify* c, sp_stream_t stream) {
+  if (!c || !c->p || !c->u_sample || !c->n_accept || !c->tokens) return SP_EINVAL;
+  if (c->T < 0 || c->T > SPIKE_PROJ_VERIFY_MAX_T || c->V < 1 || c->V > SPIKE_PROJ_VERIFY_MAX_V || c->B < 1 ||
+      c->B > 65535)
+    return SP_ERANGE;
+  if (c->T > 0 && (!c->q || !c->draft || !c->u || c->ld_draft < c->T || c->ld_u < c->T)) return SP_EINVAL;
+  if (c->ld_tokens < c->T + 1) return SP_EINVAL;
+  for (const void* x : {(const void*)c->p, (const void*)c->q, (const void*)c->draft, (const void*)c->n_draft,
+                        (const void*)c->u, (const void*)c->u_sample, (const void*)c->n_accept, (const void*)c->tokens})
+    if (!aligned(x, 4)) return SP_EALIGN;
+  int dev = 0;
+  const sp_status st = check_device(&dev);
+  if (st != SP_OK) return st;
+  SP_CUDA(launch_verify(*c, as_stream(stream)));
+  return SP_OK;
+}
+
 const char* spike_proj_strerror(sp_status status) {
   switch (status) {
     case SP_OK: return "success";
     case SP_EINVAL: return "invalid argument";
     case SP_EALIGN: return "alignment or leading-dimension rule violated";
-    case SP_EDEVICE: return "current device is not compute capability 10.3 (GB300)";
+    case SP_EDEVICE: return "current device is not compute capability 10.3 (GB300), or not the handle's";
     case SP_ECUDA: return "CUDA runtime error (see spike_proj_last_cuda_error)";
     case SP_ENOMEM: return "device memory allocation failed";
     case SP_ERANGE: return "size out of range (K above 131072 or batch above the plan's maximum)";

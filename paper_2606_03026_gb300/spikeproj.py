@@ -22,14 +22,25 @@ SP_AUTO, SP_GATHER, SP_UNION, SP_GEMM = 0, 1, 2, 3
 # sp_fault (tests of the error path only)
 SP_FAULT_NONE, SP_FAULT_ABORT, SP_FAULT_STALL = 0, 1, 2
 SP_PLAN_GEMM = 0x1
+# sp_dtype
+SP_BF16, SP_FP16 = 0, 1
+SP_CACHE_WEIGHTS = 0x1
 SPIKE_PROJ_MAX_K = 131072
 SPIKE_PROJ_MAX_GROUP = 64
 SPIKE_PROJ_NOALLOC_MAX_N = 32768
 SPIKE_PROJ_DENSE_MAX_B = 4
 SPIKE_PROJ_DENSE_MAX_GROUP = 128
+SPIKE_PROJ_CACHE_MAX_B = 1024
+SPIKE_PROJ_CACHE_MAX_T = 32
+SPIKE_PROJ_CACHE_MAX_HEADS = 512
+SPIKE_PROJ_CACHE_MAX_D = 128
+SPIKE_PROJ_CACHE_MAX_LEN = 1 << 24
+SPIKE_PROJ_VERIFY_MAX_T = 64
+SPIKE_PROJ_VERIFY_MAX_V = 1 << 24
 
 FMTS = {"bits": SP_SPIKES_BITS32, "u8": SP_SPIKES_U8, "bool8": SP_SPIKES_BOOL8}
 KERNELS = {"auto": SP_AUTO, "gather": SP_GATHER, "union": SP_UNION, "gemm": SP_GEMM}
+DTYPES = {"bf16": SP_BF16, "fp16": SP_FP16}
 KERNEL_NAMES = {v: k for k, v in KERNELS.items()}
 
 # every entry point of the C ABI with its ctypes signature
@@ -61,6 +72,13 @@ _SIGNATURES = {
     "spike_proj_head_destroy": ([_P], ctypes.c_int),
     "spike_proj_head": ([_P, _P, _I64, _I32, ctypes.c_float, _I32, _P, _P, _P, _P, _P, _P, _I64,
                          _P], ctypes.c_int),
+    "spike_proj_cache_create": ([_P, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _U32, _P],
+                                ctypes.c_int),
+    "spike_proj_cache_destroy": ([_P], ctypes.c_int),
+    "spike_proj_cache_status": ([_P, _P], ctypes.c_int),
+    "spike_proj_cache_attend": ([_P, _P, _P], ctypes.c_int),
+    "spike_proj_cache_evict": ([_P, _P, _P], ctypes.c_int),
+    "spike_proj_verify": ([_P, _P], ctypes.c_int),
     "spike_proj_probe_gather": ([_P, _P, _I32, _I32, _P, _P], ctypes.c_int),
     "spike_proj_plan_inject_fault": ([_P, _I32], ctypes.c_int),
     "spike_proj_group_inject_fault": ([_P, _I32], ctypes.c_int),
@@ -466,3 +484,197 @@ class Head:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------------------
+# a KV cache with a shared prefix, and the verification of drafted tokens
+# ---------------------------------------------------------------------------
+class SpAttend(ctypes.Structure):
+    """struct sp_attend of spike_proj.h."""
+    _fields_ = [("q", _P), ("q_batch", _I64), ("q_token", _I64), ("q_head", _I64),
+                ("prefix_k", _P), ("prefix_v", _P),
+                ("pk_entry", _I64), ("pk_head", _I64), ("pv_entry", _I64), ("pv_head", _I64),
+                ("k", _P), ("v", _P), ("k_batch", _I64), ("k_entry", _I64), ("k_head", _I64),
+                ("v_batch", _I64), ("v_entry", _I64), ("v_head", _I64),
+                ("lens", _P), ("out", _P), ("out_batch", _I64), ("out_token", _I64),
+                ("out_head", _I64), ("lse", _P), ("weights", _P), ("weights_batch", _I64),
+                ("weights_head", _I64), ("B", _I32), ("T", _I32), ("prefix_len", _I32),
+                ("scale", ctypes.c_float)]
+
+
+class SpEvict(ctypes.Structure):
+    """struct sp_evict of spike_proj.h."""
+    _fields_ = [("k", _P), ("v", _P), ("k_batch", _I64), ("k_entry", _I64), ("k_head", _I64),
+                ("v_batch", _I64), ("v_entry", _I64), ("v_head", _I64),
+                ("weights", _P), ("pos", _P), ("in_batch", _I64), ("in_head", _I64),
+                ("weights_out", _P), ("pos_out", _P), ("out_batch", _I64), ("out_head", _I64),
+                ("lens", _P), ("now", _P), ("lens_out", _P),
+                ("B", _I32), ("budget", _I32), ("recent", _I32)]
+
+
+class SpVerify(ctypes.Structure):
+    """struct sp_verify of spike_proj.h."""
+    _fields_ = [("p", _P), ("p_batch", _I64), ("p_row", _I64),
+                ("q", _P), ("q_batch", _I64), ("q_row", _I64),
+                ("draft", _P), ("ld_draft", _I64), ("n_draft", _P), ("u", _P), ("ld_u", _I64),
+                ("u_sample", _P), ("n_accept", _P), ("tokens", _P), ("ld_tokens", _I64),
+                ("B", _I32), ("T", _I32), ("V", _I32)]
+
+
+def spike_proj_cache_create(max_batch, max_T, Hq, Hkv, D, capacity, dtype, flags=0,
+                            stream=None) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().spike_proj_cache_create(ctypes.byref(h), max_batch, max_T, Hq, Hkv, D, capacity,
+                                         DTYPES[dtype] if isinstance(dtype, str) else int(dtype),
+                                         flags, _stream(stream)), "spike_proj_cache_create")
+    return h.value
+
+
+def spike_proj_cache_destroy(cache):
+    _check(lib().spike_proj_cache_destroy(cache), "spike_proj_cache_destroy")
+
+
+def spike_proj_cache_status(cache, stream=None) -> int:
+    return lib().spike_proj_cache_status(cache, _stream(stream))
+
+
+def spike_proj_cache_attend(cache, call, stream=None):
+    """call: an SpAttend."""
+    _check(lib().spike_proj_cache_attend(cache, ctypes.addressof(call), _stream(stream)),
+           "spike_proj_cache_attend")
+
+
+def spike_proj_cache_evict(cache, call, stream=None):
+    """call: an SpEvict."""
+    _check(lib().spike_proj_cache_evict(cache, ctypes.addressof(call), _stream(stream)),
+           "spike_proj_cache_evict")
+
+
+def spike_proj_verify(call, stream=None):
+    """call: an SpVerify."""
+    _check(lib().spike_proj_verify(ctypes.addressof(call), _stream(stream)), "spike_proj_verify")
+
+
+def _want(x, name, shape, dtype, inner=True):
+    """A tensor of the shape and type that a call needs, rows contiguous."""
+    if tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(x.shape)}, expected {tuple(shape)}")
+    if str(x.dtype) != "torch." + dtype:
+        raise ValueError(f"{name}: {x.dtype}, expected torch.{dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{name}: not a CUDA tensor")
+    if inner and x.shape and x.shape[-1] > 1 and x.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension is not contiguous")
+
+
+class Cache:
+    """Attention over own caches [B, capacity, Hkv, D] of sequences that share a
+    prefix [P, Hkv, D], and eviction from the own caches.  Owns workspace for
+    max_batch sequences of max_T query tokens; the tensors are the caller's."""
+
+    def __init__(self, max_batch, Hq, Hkv, D, capacity, max_T=1, dtype="bf16", weights=False,
+                 stream=None):
+        self.Hq, self.Hkv, self.D, self.capacity, self.max_T = Hq, Hkv, D, capacity, max_T
+        self.dtype = {"bf16": "bfloat16", "fp16": "float16"}[dtype]
+        self.handle = spike_proj_cache_create(max_batch, max_T, Hq, Hkv, D, capacity, dtype,
+                                              SP_CACHE_WEIGHTS if weights else 0, stream)
+
+    def attend(self, q, k, v, lens, out, prefix_k=None, prefix_v=None, weights=None, lse=None,
+               scale=None, stream=None):
+        """T query tokens per sequence, q [B, T, Hq, D] -> out [B, T, Hq, D]; the
+        own caches already hold the T tokens' entries, which lens (int32 [B])
+        counts.  weights (float32 [B, Hkv, capacity]) gains the attention that
+        the own entries get; lse (float32 [B, T, Hq]) is optional."""
+        B, T, P = q.shape[0], q.shape[1], 0 if prefix_k is None else prefix_k.shape[0]
+        own = (B, self.capacity, self.Hkv, self.D)
+        for x, name, shape in ((q, "q", (B, T, self.Hq, self.D)), (out, "out", q.shape),
+                               (k, "k", own), (v, "v", own)):
+            _want(x, name, shape, self.dtype)
+        _want(lens, "lens", (B,), "int32")
+        pk, pv = (0, 0), (0, 0)
+        if P:
+            for x, name in ((prefix_k, "prefix_k"), (prefix_v, "prefix_v")):
+                _want(x, name, (P, self.Hkv, self.D), self.dtype)
+            pk, pv = prefix_k.stride()[:2], prefix_v.stride()[:2]
+        ws = (0, 0)
+        if weights is not None:
+            _want(weights, "weights", (B, self.Hkv, self.capacity), "float32")
+            ws = weights.stride()[:2]
+        if lse is not None:
+            _want(lse, "lse", (B, T, self.Hq), "float32")
+            if not lse.is_contiguous():
+                raise ValueError("lse: not contiguous")
+        call = SpAttend(_addr(q), *q.stride()[:3], _addr(prefix_k) if P else None,
+                        _addr(prefix_v) if P else None, *pk, *pv, _addr(k), _addr(v),
+                        *k.stride()[:3], *v.stride()[:3], _addr(lens), _addr(out),
+                        *out.stride()[:3], _addr(lse), _addr(weights), *ws, B, T, P,
+                        self.D ** -0.5 if scale is None else scale)
+        spike_proj_cache_attend(self.handle, call, stream)
+
+    def evict(self, k, v, weights, pos, lens, now, budget, recent, weights_out, pos_out, lens_out,
+              stream=None):
+        """Keeps `budget` entries of every own cache, the `recent` newest (pos >=
+        now - recent) and then those of the most weight; K and V [B, capacity,
+        Hkv, D] in place, weights and pos [B, Hkv, capacity] into weights_out
+        and pos_out [B, Hkv, >= min(budget, capacity)]."""
+        B = k.shape[0]
+        own = (B, self.capacity, self.Hkv, self.D)
+        _want(k, "k", own, self.dtype)
+        _want(v, "v", own, self.dtype)
+        _want(weights, "weights", (B, self.Hkv, self.capacity), "float32")
+        _want(pos, "pos", weights.shape, "int32")
+        room = weights_out.shape[2] if weights_out.dim() == 3 else -1
+        if room < min(budget, self.capacity):
+            raise ValueError("weights_out: no room for the budget")
+        _want(weights_out, "weights_out", (B, self.Hkv, room), "float32")
+        _want(pos_out, "pos_out", weights_out.shape, "int32")
+        if pos.stride()[:2] != weights.stride()[:2] or pos_out.stride()[:2] != weights_out.stride()[:2]:
+            raise ValueError("pos: other strides than weights")
+        for x, name in ((lens, "lens"), (now, "now"), (lens_out, "lens_out")):
+            _want(x, name, (B,), "int32")
+        call = SpEvict(_addr(k), _addr(v), *k.stride()[:3], *v.stride()[:3], _addr(weights),
+                       _addr(pos), *weights.stride()[:2], _addr(weights_out), _addr(pos_out),
+                       *weights_out.stride()[:2], _addr(lens), _addr(now), _addr(lens_out), B,
+                       budget, recent)
+        spike_proj_cache_evict(self.handle, call, stream)
+
+    def status(self, stream=None) -> int:
+        return spike_proj_cache_status(self.handle, stream)
+
+    def close(self):
+        if self.handle:
+            spike_proj_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def verify(p, q, draft, u, u_sample, n_accept, tokens, n_draft=None, stream=None):
+    """How many of the drafts [B, T] the target keeps and the token after them:
+    p [B, T+1, V] and q [B, T, V] float32 probabilities (q, draft and u may be
+    None when T is 0), u [B, T] and u_sample [B] uniform float32 in [0, 1),
+    n_draft int32 [B] or None; n_accept int32 [B], tokens int32 [B, T+1]."""
+    B, T, V = p.shape[0], p.shape[1] - 1, p.shape[2]
+    _want(p, "p", (B, T + 1, V), "float32")
+    qs, ld_draft, ld_u = (0, 0), 0, 0
+    if T:
+        _want(q, "q", (B, T, V), "float32")
+        _want(draft, "draft", (B, T), "int32")
+        _want(u, "u", (B, T), "float32")
+        qs, ld_draft, ld_u = q.stride()[:2], draft.stride(0), u.stride(0)
+    _want(u_sample, "u_sample", (B,), "float32")
+    _want(n_accept, "n_accept", (B,), "int32")
+    _want(tokens, "tokens", (B, T + 1), "int32")
+    if n_draft is not None:
+        _want(n_draft, "n_draft", (B,), "int32")
+    # the row strides of one row do not count
+    call = SpVerify(_addr(p), *p.stride()[:2], _addr(q) if T else None, *qs,
+                    _addr(draft) if T else None, max(ld_draft, T) if B == 1 else ld_draft,
+                    _addr(n_draft), _addr(u) if T else None, max(ld_u, T) if B == 1 else ld_u,
+                    _addr(u_sample), _addr(n_accept), _addr(tokens),
+                    max(tokens.stride(0), T + 1) if B == 1 else tokens.stride(0), B, T, V)
+    spike_proj_verify(call, stream)
