@@ -570,9 +570,10 @@ sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream);
  * A row that sees no entry (or scores of minus infinity alone) gives out = 0,
  * lse = -infinity and no weight.  Entries that no row sees are never used,
  * whatever they hold; a NaN that a row sees makes that row NaN.  The
- * probabilities are rounded to the type before they meet V (relative error
- * 2^-9 or 2^-12 each); scores, the running maximum and sum, and the sums over
- * V are FP32.  Results do not depend on the order in which blocks run.
+ * probabilities are rounded to the type before they meet V, and out is divided
+ * by the sum of the rounded ones; lse and weights take them unrounded.  Scores,
+ * the running maximum and sums, and the sums over V are FP32.  Results do not
+ * depend on the order in which blocks run.
  *
  *   lens       device int32 [B]; values outside 0 .. capacity are taken as
  *              the nearest end.
