@@ -1237,26 +1237,21 @@ sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend* c, sp_strea
   if (c->prefix_len > 0 && (!c->prefix_k || !c->prefix_v)) return SP_EINVAL;
   if (c->B > sh.max_batch || c->T > sh.max_T || c->prefix_len > SPIKE_PROJ_CACHE_MAX_LEN) return SP_ERANGE;
   if (c->weights && !sh.weights) return SP_EUNSUPPORTED;
-  // tiles of 128 entries that the launch counts in 32 bits
-  const int64_t rows = (int64_t)c->T * (sh.Hq / sh.Hkv);
-  const int64_t tiles = (c->B * rows + 127) / 128 * ((c->prefix_len + 127) / 128) +
-                        c->B * ((rows + 127) / 128) * (((int64_t)sh.capacity + 127) / 128);
-  if (tiles * sh.Hkv >= (int64_t)1 << 30) return SP_ERANGE;
-  const auto any = [](int64_t n, int64_t stride) { return n == 1 || stride % 8 == 0; };
-  const auto kv = [&](int64_t n, int64_t stride) { return n <= 1 || (stride % 8 == 0 && stride > 0); };
+  if (attend_tiles(sh, *c) >= (int64_t)1 << 30) return SP_ERANGE;
+  const auto in = [&](int64_t n, int64_t stride) { return n <= 1 || (stride % 8 == 0 && stride > 0); };
   const auto out = [&](int64_t n, int64_t stride) {
     return n == 1 || (stride % 8 == 0 && (stride >= sh.D || stride <= -sh.D));
   };
   if (!aligned(c->q, 16) || !aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->out, 16) ||
       !aligned(c->lens, 4) || (c->lse && !aligned(c->lse, 4)) || (c->weights && !aligned(c->weights, 4)) ||
-      !any(c->B, c->q_batch) || !any(c->T, c->q_token) || !any(sh.Hq, c->q_head) || !out(c->B, c->out_batch) ||
-      !out(c->T, c->out_token) || !out(sh.Hq, c->out_head) || !kv(c->B, c->k_batch) ||
-      !kv(sh.capacity, c->k_entry) || !kv(sh.Hkv, c->k_head) || !kv(c->B, c->v_batch) ||
-      !kv(sh.capacity, c->v_entry) || !kv(sh.Hkv, c->v_head))
+      !in(c->B, c->q_batch) || !in(c->T, c->q_token) || !in(sh.Hq, c->q_head) || !out(c->B, c->out_batch) ||
+      !out(c->T, c->out_token) || !out(sh.Hq, c->out_head) || !in(c->B, c->k_batch) ||
+      !in(sh.capacity, c->k_entry) || !in(sh.Hkv, c->k_head) || !in(c->B, c->v_batch) ||
+      !in(sh.capacity, c->v_entry) || !in(sh.Hkv, c->v_head))
     return SP_EALIGN;
   if (c->prefix_len > 0 &&
-      (!aligned(c->prefix_k, 16) || !aligned(c->prefix_v, 16) || !kv(c->prefix_len, c->pk_entry) ||
-       !kv(sh.Hkv, c->pk_head) || !kv(c->prefix_len, c->pv_entry) || !kv(sh.Hkv, c->pv_head)))
+      (!aligned(c->prefix_k, 16) || !aligned(c->prefix_v, 16) || !in(c->prefix_len, c->pk_entry) ||
+       !in(sh.Hkv, c->pk_head) || !in(c->prefix_len, c->pv_entry) || !in(sh.Hkv, c->pv_head)))
     return SP_EALIGN;
   const sp_status st = on_device(cache->device);
   if (st != SP_OK) return st;

@@ -9,20 +9,25 @@
 // one sequence, R in all; for the prefix the rows of every sequence together,
 // so that its entries are read once for 128 of them.
 //
-// attend_kernel: units of (128 rows, K/V head) x all their entries, cut into
-// tiles of 128 entries.  The tiles of all units, the prefix's first, are one
-// line that two CTAs per SM share out evenly, whatever the lengths (which only
-// the device knows); a CTA's run of tiles within a unit is a segment, which
-// leaves its sum over V, its maximum and its sum of exponentials in a slot of
-// the workspace.  Per CTA (192 threads):
-//   warps 0-3   the softmax, thread = row = tensor-memory lane: they write the
-//               segment's query rows to shared memory in the 128-byte swizzle
-//               that the MMA reads, and per tile read the 128 scores of their
-//               row, keep the running maximum and sum, and put the
-//               probabilities, rounded to the type, back over the scores.
-//   warp 4      TMA: K and V tiles into a ring.
-//   warp 5      one thread issues S = Q K^T and O += P V (tcgen05, M = 128, P
-//               from tensor memory, V as an N-major operand).
+// attend_kernel: units of (up to 128 rows, K/V head) x all their entries, cut
+// into tiles of 64 entries.  The tiles of all units, the prefix's first, are one
+// line that two CTAs per SM share out evenly by cost, whatever the lengths
+// (which only the device knows); a CTA's run of tiles within a unit is a
+// segment, which leaves its sum over V, its maximum and its sums of
+// exponentials in a slot of the workspace.  Per CTA (192 threads):
+//   warp 4      TMA: the query rows of a segment (a box of G heads x T tokens,
+//               for the prefix x as many sequences as 128 rows hold), K and V
+//               tiles into a ring.
+//   warp 5      one thread issues S = Q K^T one tile ahead of O += P V (tcgen05,
+//               M = 128, P from tensor memory, V as an N-major operand).
+//   warps 0-3   the softmax, thread = row = tensor-memory lane: per tile they
+//               read the 64 scores of their row, keep the running maximum and
+//               sums, and put the probabilities, rounded to the type, back over
+//               the scores.
+// A unit of at most 32 (64) rows has them four times (twice) in the MMA's 128,
+// and each copy's warps take a quarter (half) of a tile's entries, with
+// probabilities of 0 for the others: a tile's softmax takes a warp a quarter of
+// the time, and every copy is a partial result of its own.
 // Exponentials are powers of two of (s scale log2 e - reference).  The
 // reference follows the running maximum only when that has grown by more than
 // 2^kLag, so that O is rescaled seldom; half precision is offset by 2^10 so that
@@ -34,7 +39,7 @@
 // entries, of which the query tokens see 0, 1, .. T - 1, are left to
 // combine_kernel, so that no masked probability ever meets a value.
 //
-// combine_kernel: one or four warps per query row merge its segments' slots and
+// combine_kernel: one or four warps per query row merge its partial results and
 // these last entries.  weights_kernel: the weights, from the scores of the own
 // entries that attend_kernel left in the workspace and the rows' lse.
 #include <cuda.h>
@@ -50,28 +55,47 @@
 namespace sp {
 namespace {
 
-constexpr int kTile = 128;                 // entries of a tile, rows of a unit
+constexpr int kTile = 64;                  // entries of a tile
+constexpr int kRows = 128;                 // rows of the MMA
 constexpr int kAttThreads = 192;
-constexpr int kTmemCols = 256;             // S and P: 0 .. 127, O: 128 .. 255
+constexpr int kTmemCols = 256;             // S and P: 0 .. 63 and 64 .. 127, O: 128 .. 255
 constexpr uint32_t kTmemO = 128;
-constexpr int kBlockBytes = kTile * 128;   // 64 elements of 128 entries
+constexpr int kQBlock = kRows * 128;       // 64 elements of 128 rows
+constexpr int kBlock = kTile * 128;        // 64 elements of a tile's entries
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-template <int DK> constexpr int kStages = DK == 64 ? 2 : 1;
-template <int DK> constexpr int kTileBytes = DK / 64 * kBlockBytes;
+template <int DK> constexpr int kStages = 256 / DK;       // 64 KB of K and V
+template <int DK> constexpr int kQBytes = DK / 64 * kQBlock;
+template <int DK> constexpr int kTileBytes = DK / 64 * kBlock;
+
+// The rows of units.  Of one sequence: `per_seq` tiles of `tokens` query tokens
+// x `heads` query heads (all G of them, or 128 at a time).  A prefix unit has
+// those of `seqs` sequences, which is 1 unless all rows of a sequence fit.
+struct Rows {
+  int32_t heads, tokens, seqs;
+  int32_t head_tiles, per_seq;             // tiles that share a token; tiles of a sequence
+  int32_t prefix_units, own_units;         // per K/V head; per sequence and K/V head
+  int32_t prefix_rows, own_rows;           // of a whole unit
+  int32_t prefix_copies, own_copies;       // of the rows in the MMA's 128
+};
+
+struct AttnMaps {
+  CUtensorMap pq, pk, pv, q, k, v;         // of the prefix units, of the own units
+};
 
 struct AttnParams {
   sp_attend c;
-  int32_t Hq, Hkv, G, D, capacity;
-  int32_t R, Rm, mt_own, mt_prefix, nt_prefix, nt_cap;   // Rm: rows of an own slot
+  int32_t Hq, Hkv, G, D, capacity, R;      // R = T G: query rows of a sequence and K/V head
+  Rows rows;
+  int32_t nt_prefix, nt_cap;               // tiles of the prefix, of the capacity
   float c2;                 // scale * log2 e
   int* err;
   int32_t* sched;           // [B + 1]: own tiles before each sequence; [B] all of them
   float4* p_ml;             // prefix slots: [slot][128] reference, sum, sum of the rounded
   float* p_o;               //               [slot][128][DK]
-  float4* o_ml;             // own slots: [slot][Rm], [slot][Rm][DK]
+  float4* o_ml;             // own slots: [slot][own_rows own_copies], the same [DK]
   float* o_o;
-  float* scores;            // [B][Hkv][nt_cap][R][128], or null
+  float* scores;            // [B][Hkv][nt_cap][R][64], or null
   float* lse2;              // [B][Hkv][R], base 2; +infinity where a row sees nothing
 };
 
@@ -79,67 +103,82 @@ struct AttnParams {
 __device__ __forceinline__ int used(const AttnParams& p, int b) {
   return min(max(__ldg(p.c.lens + b), 0), p.capacity);
 }
-// Own entries of a sequence that every query token sees, and their tiles.
+// Own entries of a sequence that every query token sees.
 __device__ __forceinline__ int seen_by_all(const AttnParams& p, int b) { return max(0, used(p, b) - (p.c.T - 1)); }
+
+// Costs of a tile.
+constexpr int kCostPrefix = 1, kCostOwn = 1, kCostMost = 1;
 
 struct Line {
   int prefix;               // tiles of the prefix units
-  int64_t all;              // tiles
+  int64_t cost;             // of all tiles
   int ctas;                 // that have any
-  // CTA c has tiles first(c) .. first(c + 1)
-  __device__ __forceinline__ int64_t first(int c) const { return c * all / ctas; }
+  // CTA c has tiles first(c) .. first(c + 1); every one of them has at least one
+  __device__ __forceinline__ int64_t first(int c) const {
+    const int64_t x = c * cost / ctas, px = (int64_t)prefix * kCostPrefix;
+    return x < px ? x / kCostPrefix : prefix + (x - px) / kCostOwn;
+  }
   // the CTA of a tile
-  __device__ __forceinline__ int cta(int64_t tile) const { return (int)(((tile + 1) * ctas - 1) / all); }
+  __device__ __forceinline__ int cta(int64_t tile) const {
+    const int64_t end = tile < prefix ? (tile + 1) * kCostPrefix
+                                      : (int64_t)prefix * kCostPrefix + (tile + 1 - prefix) * kCostOwn;
+    return (int)((end * ctas - 1) / cost);
+  }
 };
 __device__ __forceinline__ Line line_of(const AttnParams& p, int own_tiles, int grid) {
   Line l;
-  l.prefix = p.Hkv * p.mt_prefix * p.nt_prefix;
-  l.all = (int64_t)l.prefix + own_tiles;
-  l.ctas = (int)min((int64_t)grid, l.all);
+  l.prefix = p.Hkv * p.rows.prefix_units * p.nt_prefix;
+  l.cost = (int64_t)l.prefix * kCostPrefix + (int64_t)own_tiles * kCostOwn;
+  l.ctas = l.cost == 0 ? 0 : (int)min((int64_t)grid, max((int64_t)1, l.cost / kCostMost));
   return l;
 }
 
 struct Segment {
   bool prefix;
-  int b, h, m;              // sequence (own), head, row tile
+  int b, h, m;              // first sequence, head, row tile of the sequence
   int j0, count;            // tiles
   int seen;                 // entries of the unit
-  int rows;                 // of the unit
+  int rows, copies;
   int64_t slot;
 };
 // The segment at tile x of a CTA whose tiles end at `end`.
 __device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l, const int* off, int64_t x,
                                               int64_t end, int cta) {
+  const Rows& r = p.rows;
   Segment s;
   s.prefix = x < l.prefix;
   if (s.prefix) {
     const int u = (int)x / p.nt_prefix;
     s.j0 = (int)x - u * p.nt_prefix;
     s.count = (int)min((int64_t)(p.nt_prefix - s.j0), end - x);
-    s.b = 0;
-    s.h = u / p.mt_prefix;
-    s.m = u - s.h * p.mt_prefix;
+    s.h = u / r.prefix_units;
+    const int i = u - s.h * r.prefix_units;
+    s.b = i / r.per_seq * r.seqs;
+    s.m = i % r.per_seq;
     s.seen = p.c.prefix_len;
-    s.rows = min(kTile, p.c.B * p.R - s.m * kTile);
+    s.copies = r.prefix_copies;
     s.slot = cta + u;
-    return s;
+  } else {
+    const int y = (int)(x - l.prefix);
+    int lo = 0, hi = p.c.B;                // off[lo] <= y < off[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (off[mid] <= y) lo = mid; else hi = mid;
+    }
+    s.b = lo;
+    const int nt = (off[lo + 1] - off[lo]) / (p.Hkv * r.own_units);
+    const int u = (y - off[lo]) / nt;
+    s.j0 = y - off[lo] - u * nt;
+    s.count = (int)min((int64_t)(nt - s.j0), end - x);
+    s.h = u / r.own_units;
+    s.m = u - s.h * r.own_units;
+    s.seen = seen_by_all(p, lo);
+    s.copies = r.own_copies;
+    s.slot = cta + (int64_t)lo * p.Hkv * r.own_units + u;
   }
-  const int y = (int)(x - l.prefix);
-  int lo = 0, hi = p.c.B;                  // off[lo] <= y < off[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (off[mid] <= y) lo = mid; else hi = mid;
-  }
-  s.b = lo;
-  const int nt = (off[lo + 1] - off[lo]) / (p.Hkv * p.mt_own);
-  const int u = (y - off[lo]) / nt;
-  s.j0 = y - off[lo] - u * nt;
-  s.count = (int)min((int64_t)(nt - s.j0), end - x);
-  s.h = u / p.mt_own;
-  s.m = u - s.h * p.mt_own;
-  s.seen = seen_by_all(p, lo);
-  s.rows = min(kTile, p.R - s.m * kTile);
-  s.slot = cta + (int64_t)lo * p.Hkv * p.mt_own + u;
+  s.rows = r.head_tiles > 1 ? min(r.heads, p.G - s.m % r.head_tiles * r.heads)
+                            : min(r.tokens, p.c.T - s.m * r.tokens) * p.G;
+  if (s.prefix) s.rows *= min(r.seqs, p.c.B - s.b);
   return s;
 }
 
@@ -189,32 +228,133 @@ __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy
 
 // An operand whose rows run along the MMA's N: 64 elements (128 bytes,
 // swizzled) per row of K, 8 rows of K 1024 bytes apart, the next 64 elements
-// of N kBlockBytes on.
+// of N kBlock on.
 __device__ __forceinline__ uint64_t n_major_desc(const void* p) {
   uint64_t d = smem_desc(p, 1024, kSwizzle128);
   d &= ~((uint64_t)0x3FFF << 16);
-  return d | (uint64_t)(kBlockBytes >> 4) << 16;
+  return d | (uint64_t)(kBlock >> 4) << 16;
+}
+
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+  return mbar_try_wait(bar, parity) || mbar_wait(bar, parity);
+}
+
+// What a softmax thread keeps of its row.
+struct RowState {
+  float m, ref, l, rl;      // maximum that the reference follows, reference, sums
+};
+
+template <int NC> __device__ __forceinline__ void tmem_ld_issue(uint32_t at, uint32_t (&v)[NC]) {
+  if constexpr (NC == 16) tmem_ld16_issue(at, v);
+  else if constexpr (NC == 32) tmem_ld32_issue(at, v);
+}
+template <int NC> __device__ __forceinline__ void tmem_st_issue(uint32_t at, const uint32_t (&v)[NC]) {
+  if constexpr (NC == 8) tmem_st8_issue(at, v);
+  else if constexpr (NC == 16) tmem_st16_issue(at, v);
+  else tmem_st32_issue(at, v);
+}
+
+// One tile for a warp whose rows' copy has NC of the tile's entries, from entry
+// c0 on.  s_buf: this warp's lanes of the tile's scores.  pv: the barrier (and
+// its parity) that says the product before this tile's is complete.
+template <int DK, bool BF16, int NC>
+__device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, uint32_t s_buf, uint32_t o_buf, int c0,
+                                             int nv, bool first, uint64_t* pv, uint32_t pv_parity, float* scores) {
+  constexpr float kLag = BF16 ? 8.f : 4.f, kLift = BF16 ? 0.f : 10.f;
+  constexpr int NL = NC < 32 ? NC : 32;
+  uint32_t v[NC / NL][NL];
+#pragma unroll
+  for (int i = 0; i < NC / NL; ++i) tmem_ld_issue<NL>(s_buf + c0 + NL * i, v[i]);
+  tmem_ld_wait();
+#pragma unroll
+  for (int i = 0; i < NC / NL; ++i) reg_pin(v[i]);
+  if (scores) {
+#pragma unroll
+    for (int i = 0; i < NC / 4; ++i)
+      reinterpret_cast<uint4*>(scores + c0)[i] =
+          make_uint4(v[4 * i / NL][4 * i % NL], v[4 * i / NL][4 * i % NL + 1], v[4 * i / NL][4 * i % NL + 2],
+                     v[4 * i / NL][4 * i % NL + 3]);
+  }
+  if (nv < kTile) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (c0 + i >= nv) v[i / NL][i % NL] = 0xff800000u;
+  }
+  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < NC; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(v[i / NL][i % NL]));
+  const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.c2;
+  const bool grow = top > r.m + kLag;
+  if (__any_sync(0xffffffffu, grow)) {
+    float a = 1.f;
+    if (grow) {
+      a = ex2(r.m - top);                  // 0 at the first
+      r.m = top;
+      r.ref = top - kLift;
+    }
+    r.l *= a;
+    r.rl *= a;
+    if (!first) {
+      if (!__all_sync(0xffffffffu, wait(pv, pv_parity))) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int i = 0; i < DK / 16; ++i) {
+        uint32_t o[16];
+        tmem_ld16_issue(o_buf + 16 * i, o);
+        tmem_ld_wait();
+        reg_pin(o);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
+        tmem_st16_issue(o_buf + 16 * i, o);
+      }
+    }
+  }
+  f32x2 sum[2] = {}, rsum[2] = {};
+  const f32x2 c2 = pair(p.c2, p.c2), base = pair(-r.ref, -r.ref);
+  uint32_t pk[NC / 2];
+#pragma unroll
+  for (int i = 0; i < NC / 2; ++i) {
+    const float2 x = halves(
+        fma2(pair(__uint_as_float(v[2 * i / NL][2 * i % NL]), __uint_as_float(v[2 * i / NL][2 * i % NL + 1])), c2, base));
+    const float2 y = make_float2(ex2(x.x), ex2(x.y));
+    pk[i] = pack2<BF16>(y.x, y.y);
+    const float2 q = unpack2<BF16>(pk[i]);
+    sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
+    rsum[i % 2] = add2(rsum[i % 2], pair(q.x, q.y));
+  }
+  const float2 ls = halves(add2(sum[0], sum[1])), lr = halves(add2(rsum[0], rsum[1]));
+  r.l += ls.x + ls.y;
+  r.rl += lr.x + lr.y;
+  if constexpr (NC == kTile) {
+    tmem_st_issue<NC / 2>(s_buf, pk);
+  } else {                                 // the other copies' entries: 0
+    const uint32_t zero[NC / 2] = {};
+#pragma unroll
+    for (int i = 0; i < kTile / NC; ++i) {
+      if (i * NC == c0) tmem_st_issue<NC / 2>(s_buf + i * (NC / 2), pk);
+      else tmem_st_issue<NC / 2>(s_buf + i * (NC / 2), zero);
+    }
+  }
+  tmem_st_wait();
+  return true;
 }
 
 template <int DK, bool BF16>
 __global__ void __launch_bounds__(kAttThreads, 2)
-attend_kernel(const __grid_constant__ CUtensorMap map_pk, const __grid_constant__ CUtensorMap map_pv,
-              const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-              const __grid_constant__ AttnParams p) {
+attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnParams p) {
   constexpr int NS = kStages<DK>, kBytes = kTileBytes<DK>;
   constexpr uint32_t kType = BF16 ? 1u << 7 | 1u << 10 : 0u;
-  constexpr uint32_t kIdescS = 1u << 4 | kType | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
-  constexpr uint32_t kIdescO = 1u << 4 | kType | 1u << 16 | (uint32_t)(DK >> 3) << 17 | (uint32_t)(kTile >> 4) << 24;
-  constexpr float kLag = BF16 ? 8.f : 4.f, kLift = BF16 ? 0.f : 10.f;
+  constexpr uint32_t kIdescS = 1u << 4 | kType | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+  constexpr uint32_t kIdescO = 1u << 4 | kType | 1u << 16 | (uint32_t)(DK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint8_t* sQ = smem;
-  uint8_t* sK = sQ + kBytes;
+  uint8_t* sK = sQ + kQBytes<DK>;
   uint8_t* sV = sK + NS * kBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sV + NS * kBytes);
   uint64_t *k_full = bars, *k_empty = bars + NS, *v_full = bars + 2 * NS, *v_empty = bars + 3 * NS;
-  uint64_t *q_full = bars + 4 * NS, *s_full = q_full + 1, *p_full = q_full + 2, *o_full = q_full + 3,
-           *o_empty = q_full + 4, *done = q_full + 5;
+  uint64_t *s_full = bars + 4 * NS, *p_full = s_full + 2;  // [2]: by score buffer
+  uint64_t *q_full = p_full + 2, *q_empty = q_full + 1, *o_full = q_full + 2, *o_empty = q_full + 3, *done = q_full + 4;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_sum = reinterpret_cast<int*>(s_tmem + 2);         // [8]
@@ -228,18 +368,23 @@ attend_kernel(const __grid_constant__ CUtensorMap map_pk, const __grid_constant_
       mbar_init(&v_full[i], 1);
       mbar_init(&v_empty[i], 1);
     }
-    mbar_init(q_full, 4);
-    mbar_init(s_full, 1);
-    mbar_init(p_full, 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 4);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     mbar_init(o_full, 1);
     mbar_init(o_empty, 4);
     mbar_init(done, 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    tma_prefetch_desc(&map_pk);
-    tma_prefetch_desc(&map_pv);
-    tma_prefetch_desc(&map_k);
-    tma_prefetch_desc(&map_v);
+    tma_prefetch_desc(&maps.pq);
+    tma_prefetch_desc(&maps.pk);
+    tma_prefetch_desc(&maps.pv);
+    tma_prefetch_desc(&maps.q);
+    tma_prefetch_desc(&maps.k);
+    tma_prefetch_desc(&maps.v);
   }
   if (warp == 5) tmem_alloc(s_tmem, kTmemCols);
   pdl_launch_dependents();
@@ -248,8 +393,9 @@ attend_kernel(const __grid_constant__ CUtensorMap map_pk, const __grid_constant_
   // own tiles before each sequence: every CTA adds them up for itself
   {
     const int per = ceil_div(p.c.B, kAttThreads), b0 = threadIdx.x * per, b1 = min(b0 + per, p.c.B);
+    const int units = p.Hkv * p.rows.own_units;
     int sum = 0;
-    for (int b = b0; b < b1; ++b) sum += ceil_div(seen_by_all(p, b), kTile) * p.Hkv * p.mt_own;
+    for (int b = b0; b < b1; ++b) sum += ceil_div(seen_by_all(p, b), kTile) * units;
     int incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -265,7 +411,7 @@ attend_kernel(const __grid_constant__ CUtensorMap map_pk, const __grid_constant_
     for (int b = b0; b < b1; ++b) {
       s_off[b] = at;
       if (blockIdx.x == 0) p.sched[b] = at;
-      at += ceil_div(seen_by_all(p, b), kTile) * p.Hkv * p.mt_own;
+      at += ceil_div(seen_by_all(p, b), kTile) * units;
     }
     if (b0 < p.c.B && b1 == p.c.B) {
       s_off[p.c.B] = at;
@@ -281,72 +427,92 @@ attend_kernel(const __grid_constant__ CUtensorMap map_pk, const __grid_constant_
   if (warp == 4) {
     // ------------------------------ TMA -----------------------------------------
     if (lane == 0) {
-      int it = 0;
-      for (int64_t x = x0; x < x1 && !*s_abort;) {
+      int it = 0, seg = 0;
+      bool ok = true;
+      for (int64_t x = x0; x < x1 && ok; ++seg) {
         const Segment s = segment_at(p, line, s_off, x, x1, cta);
-        const CUtensorMap* mk = s.prefix ? &map_pk : &map_k;
-        const CUtensorMap* mv = s.prefix ? &map_pv : &map_v;
-        for (int j = 0; j < s.count && !*s_abort; ++j, ++it) {
+        const CUtensorMap* mk = s.prefix ? &maps.pk : &maps.k;
+        const CUtensorMap* mv = s.prefix ? &maps.pv : &maps.v;
+        const int kb = s.prefix ? 0 : s.b;
+        for (int j = 0; j < s.count; ++j, ++it) {
           const int st = it % NS;
           const uint32_t ph = (it / NS) & 1;
-          bool ok = mbar_wait_sleep(&k_empty[st], ph ^ 1u);
-          if (ok) {
-            mbar_arrive_expect_tx(&k_full[st], kBytes);
-            for (int i = 0; i < DK / 64; ++i)
-              tma_load_4d(sK + st * kBytes + i * kBlockBytes, mk, &k_full[st], 64 * i, (s.j0 + j) * kTile, s.h, s.b);
-            ok = mbar_wait_sleep(&v_empty[st], ph ^ 1u);
+          ok = mbar_wait_sleep(&k_empty[st], ph ^ 1u) && !*s_abort;
+          if (!ok) break;
+          mbar_arrive_expect_tx(&k_full[st], kBytes);
+          for (int i = 0; i < DK / 64; ++i)
+            tma_load_4d(sK + st * kBytes + i * kBlock, mk, &k_full[st], 64 * i, (s.j0 + j) * kTile, s.h, kb);
+          if (j == 0) {
+            ok = mbar_wait_sleep(q_empty, (seg & 1) ^ 1u) && !*s_abort;
             if (ok) {
-              mbar_arrive_expect_tx(&v_full[st], kBytes);
-              for (int i = 0; i < DK / 64; ++i)
-                tma_load_4d(sV + st * kBytes + i * kBlockBytes, mv, &v_full[st], 64 * i, (s.j0 + j) * kTile, s.h, s.b);
-            } else {
-              mbar_wait(&k_full[st], ph);  // no copy is in flight at the end
+              const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows;
+              const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
+              const int token = s.m / p.rows.head_tiles * p.rows.tokens;
+              mbar_arrive_expect_tx(q_full, DK / 64 * 128 * box * s.copies);
+              for (int c = 0; c < s.copies; ++c)
+                for (int i = 0; i < DK / 64; ++i)
+                  tma_load_4d(sQ + i * kQBlock + c * (kQBlock / s.copies), s.prefix ? &maps.pq : &maps.q, q_full, 64 * i,
+                              head, token, s.b);
             }
           }
+          ok = ok && mbar_wait_sleep(&v_empty[st], ph ^ 1u) && !*s_abort;
           if (!ok) {
-            *s_abort = 1;
-            atomicExch(p.err, kErrMbarTimeout);
+            wait(&k_full[st], ph);         // no copy is in flight at the end
             break;
           }
+          mbar_arrive_expect_tx(&v_full[st], kBytes);
+          for (int i = 0; i < DK / 64; ++i)
+            tma_load_4d(sV + st * kBytes + i * kBlock, mv, &v_full[st], 64 * i, (s.j0 + j) * kTile, s.h, kb);
         }
         x += s.count;
       }
+      if (!ok) {
+        *s_abort = 1;
+        atomicExch(p.err, kErrMbarTimeout);
+        if (seg > 0) wait(q_full, (seg - 1) & 1);
+      }
       // the last copies have landed
       for (int i = max(0, it - NS); i < it; ++i) {
-        mbar_wait(&k_full[i % NS], (i / NS) & 1);
-        mbar_wait(&v_full[i % NS], (i / NS) & 1);
+        wait(&k_full[i % NS], (i / NS) & 1);
+        wait(&v_full[i % NS], (i / NS) & 1);
       }
     }
   } else if (warp == 5) {
     // ------------------------------ MMA -----------------------------------------
     if (lane == 0) {
-      int it = 0, seg = 0;
+      int it = 0, seg = 0;                 // it: tiles whose product with V is issued
       bool ok = true;
       const uint64_t qd = smem_desc(sQ, 1024, kSwizzle128);
+      const auto scores = [&](int i, bool last) {
+        const int st = i % NS;
+        if (!wait(&k_full[st], (i / NS) & 1) || *s_abort) return false;
+        tc_fence_after();
+        const uint64_t kd = smem_desc(sK + st * kBytes, 1024, kSwizzle128);
+#pragma unroll
+        for (int k = 0; k < DK / 16; ++k)
+          mma_f16(tmem + (i & 1) * kTile, qd + (k / 4) * (kQBlock >> 4) + (k % 4) * 2,
+                  kd + (k / 4) * (kBlock >> 4) + (k % 4) * 2, kIdescS, k > 0);
+        mma_commit(&s_full[i & 1]);
+        mma_commit(&k_empty[st]);
+        if (last) mma_commit(q_empty);
+        return true;
+      };
       for (int64_t x = x0; x < x1 && ok; ++seg) {
         const Segment s = segment_at(p, line, s_off, x, x1, cta);
-        ok = mbar_wait(q_full, seg & 1);
+        // (the buffer of tile i + 1 is that of tile i - 1, whose product with V,
+        // issued before, reads the probabilities there first)
+        ok = wait(q_full, seg & 1) && scores(it, s.count == 1);
         for (int j = 0; j < s.count && ok; ++j, ++it) {
           const int st = it % NS;
-          const uint32_t ph = (it / NS) & 1;
-          ok = mbar_wait(&k_full[st], ph) && !*s_abort;
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t kd = smem_desc(sK + st * kBytes, 1024, kSwizzle128);
-#pragma unroll
-          for (int k = 0; k < DK / 16; ++k)
-            mma_f16(tmem, qd + (k / 4) * (kBlockBytes >> 4) + (k % 4) * 2, kd + (k / 4) * (kBlockBytes >> 4) + (k % 4) * 2,
-                    kIdescS, k > 0);
-          mma_commit(s_full);
-          mma_commit(&k_empty[st]);
-          ok = mbar_wait(p_full, it & 1) && mbar_wait(&v_full[st], ph) && (j > 0 || mbar_wait(o_empty, (seg & 1) ^ 1u)) &&
-               !*s_abort;
+          if (j + 1 < s.count) ok = scores(it + 1, j + 2 == s.count);
+          ok = ok && wait(&v_full[st], (it / NS) & 1) && (j > 0 || wait(o_empty, (seg & 1) ^ 1u)) &&
+               wait(&p_full[it & 1], (it >> 1) & 1) && !*s_abort;
           if (!ok) break;
           tc_fence_after();
           const uint64_t vd = n_major_desc(sV + st * kBytes);
 #pragma unroll
           for (int k = 0; k < kTile / 16; ++k)
-            mma_f16_ta(tmem + kTmemO, tmem + 8 * k, vd + k * (2048 >> 4), kIdescO, j > 0 || k > 0);
+            mma_f16_ta(tmem + kTmemO, tmem + (it & 1) * kTile + 8 * k, vd + k * (2048 >> 4), kIdescO, j > 0 || k > 0);
           mma_commit(&v_empty[st]);
         }
         if (ok) mma_commit(o_full);
@@ -357,148 +523,68 @@ attend_kernel(const __grid_constant__ CUtensorMap map_pk, const __grid_constant_
         atomicExch(p.err, kErrMbarTimeout);
       }
       mma_commit(done);                    // every MMA has retired
-      mbar_wait(done, 0);
+      wait(done, 0);
     }
   } else {
     // ------------------------------ softmax -------------------------------------
-    const int row = threadIdx.x;
-    const uint32_t t_row = tmem + ((uint32_t)(warp * 32) << 16);
+    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
     int it = 0, seg = 0;
     bool ok = true;
     for (int64_t x = x0; x < x1 && ok; ++seg) {
       const Segment s = segment_at(p, line, s_off, x, x1, cta);
-      const bool work = warp * 32 < s.rows, mine = row < s.rows;
-      // the segment's query rows (the tile's other rows hold what they hold)
-      int b = s.b, rr = s.m * kTile + row;
-      if (s.prefix) {
-        b = rr / p.R;
-        rr -= b * p.R;
-      }
-      {
-        const int t = rr / p.G;
-        const int64_t at = mine ? b * p.c.q_batch + t * p.c.q_token + (int64_t)(s.h * p.G + rr - t * p.G) * p.c.q_head : 0;
-        constexpr int kPieces = DK / 8, kRows = 32 / kPieces;
-        const int piece = lane % kPieces;
-        const bool real = piece * 8 < p.D;
-#pragma unroll 4
-        for (int r = lane / kPieces; r < 32; r += kRows) {
-          const int64_t from = __shfl_sync(0xffffffffu, at, r);
-          const int tr = warp * 32 + r;
-          if (tr < s.rows) {
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (real) v = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.c.q) + from) + piece);
-            *reinterpret_cast<uint4*>(sQ + (piece / 8) * kBlockBytes + tr * 128 + (((piece % 8) ^ (tr & 7)) << 4)) = v;
-          }
-        }
-        fence_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_full);
-      }
-      float m = -INFINITY, ref = 0.f, l = 0.f, rl = 0.f;
+      const int per_copy = kRows / s.copies, copy = threadIdx.x / per_copy, row = threadIdx.x % per_copy;
+      const bool work = warp * 32 % per_copy < s.rows, mine = row < s.rows;
+      const int c0 = copy * (kTile / s.copies);
+      const int rr = s.m / p.rows.head_tiles * p.rows.tokens * p.G + s.m % p.rows.head_tiles * p.rows.heads + row;
+      RowState r = {-INFINITY, 0.f, 0.f, 0.f};
       for (int j = 0; j < s.count; ++j, ++it) {
         const int nv = min(kTile, s.seen - (s.j0 + j) * kTile);
-        ok = __all_sync(0xffffffffu, mbar_wait(s_full, it & 1) && !*s_abort);
+        ok = __all_sync(0xffffffffu, wait(&s_full[it & 1], (it >> 1) & 1) && !*s_abort);
         if (!ok) break;
         tc_fence_after();
         if (work) {
-          uint32_t v[4][32];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld32_issue(t_row + 32 * i, v[i]);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 4; ++i) reg_pin(v[i]);
-          if (!s.prefix && p.scores && mine) {
-            float4* dst = reinterpret_cast<float4*>(
-                p.scores + ((((int64_t)s.b * p.Hkv + s.h) * p.nt_cap + s.j0 + j) * p.R + rr) * kTile);
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              dst[i] = make_float4(__uint_as_float(v[i / 8][i % 8 * 4]), __uint_as_float(v[i / 8][i % 8 * 4 + 1]),
-                                   __uint_as_float(v[i / 8][i % 8 * 4 + 2]), __uint_as_float(v[i / 8][i % 8 * 4 + 3]));
-          }
-          if (nv < kTile) {
-#pragma unroll
-            for (int i = 0; i < 128; ++i)
-              if (i >= nv) v[i / 32][i % 32] = 0xff800000u;
-          }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int i = 0; i < 128; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(v[i / 32][i % 32]));
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.c2;
-          const bool grow = top > m + kLag;
-          if (__any_sync(0xffffffffu, grow)) {
-            float a = 1.f;
-            if (grow) {
-              a = ex2(m - top);            // 0 at the first
-              m = top;
-              ref = top - kLift;
-            }
-            l *= a;
-            rl *= a;
-            if (j > 0) {
-#pragma unroll
-              for (int i = 0; i < DK / 16; ++i) {
-                uint32_t o[16];
-                tmem_ld16(t_row + kTmemO + 16 * i, o);
-                reg_pin(o);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * a);
-                tmem_st16_issue(t_row + kTmemO + 16 * i, o);
-              }
-            }
-          }
-          f32x2 sum[2] = {}, rsum[2] = {};
-          const f32x2 c2 = pair(p.c2, p.c2), base = pair(-ref, -ref);
-#pragma unroll
-          for (int h2 = 0; h2 < 2; ++h2) {
-            uint32_t pk[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const int e = 64 * h2 + 2 * i;
-              const float2 x = halves(fma2(
-                  pair(__uint_as_float(v[e / 32][e % 32]), __uint_as_float(v[e / 32][e % 32 + 1])), c2, base));
-              const float2 y = make_float2(ex2(x.x), ex2(x.y));
-              pk[i] = pack2<BF16>(y.x, y.y);
-              const float2 r = unpack2<BF16>(pk[i]);
-              sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
-              rsum[i % 2] = add2(rsum[i % 2], pair(r.x, r.y));
-            }
-            tmem_st32_issue(t_row + 32 * h2, pk);
-          }
-          const float2 ls = halves(add2(sum[0], sum[1])), lr = halves(add2(rsum[0], rsum[1]));
-          l += ls.x + ls.y;
-          rl += lr.x + lr.y;
-          tmem_st_wait();
+          float* sc = !s.prefix && p.scores && mine
+                          ? p.scores + ((((int64_t)s.b * p.Hkv + s.h) * p.nt_cap + s.j0 + j) * p.R + rr) * kTile
+                          : nullptr;
+          uint64_t* pv = &v_empty[(it + NS - 1) % NS];
+          const uint32_t pvp = ((it + NS - 1) / NS - 1) & 1, sb = lanes + (it & 1) * kTile, ob = lanes + kTmemO;
+          if (s.copies == 1) ok = softmax_tile<DK, BF16, 64>(p, r, sb, ob, 0, nv, j == 0, pv, pvp, sc);
+          else if (s.copies == 2) ok = softmax_tile<DK, BF16, 32>(p, r, sb, ob, c0, nv, j == 0, pv, pvp, sc);
+          else ok = softmax_tile<DK, BF16, 16>(p, r, sb, ob, c0, nv, j == 0, pv, pvp, sc);
+          if (!ok) break;
         }
         if (!s.prefix && nv < kTile) {
           // entries past those in use hold anything: their values become 0
           const int st = it % NS;
-          ok = __all_sync(0xffffffffu, mbar_wait(&v_full[st], (it / NS) & 1));
+          ok = __all_sync(0xffffffffu, wait(&v_full[st], (it / NS) & 1));
           if (!ok) break;
-          if (row >= nv) {
+          if (threadIdx.x >= nv && threadIdx.x < kTile) {
 #pragma unroll
             for (int i = 0; i < DK / 64; ++i)
 #pragma unroll
               for (int e = 0; e < 8; ++e)
-                *reinterpret_cast<uint4*>(sV + st * kBytes + i * kBlockBytes + row * 128 + 16 * e) =
+                *reinterpret_cast<uint4*>(sV + st * kBytes + i * kBlock + threadIdx.x * 128 + 16 * e) =
                     make_uint4(0u, 0u, 0u, 0u);
           }
           fence_async_shared();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full);
+        if (lane == 0) mbar_arrive(&p_full[it & 1]);
       }
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, mbar_wait(o_full, seg & 1) && !*s_abort);
+      ok = __all_sync(0xffffffffu, wait(o_full, seg & 1) && !*s_abort);
       if (!ok) break;
       tc_fence_after();
       if (work) {
-        float* o = s.prefix ? p.p_o + (s.slot * kTile + row) * DK : p.o_o + (s.slot * p.Rm + row) * DK;
-        if (mine) (s.prefix ? p.p_ml + s.slot * kTile : p.o_ml + s.slot * p.Rm)[row] = make_float4(ref, l, rl, 0.f);
+        const int64_t at = s.prefix ? s.slot * kRows + copy * p.rows.prefix_rows + row
+                                    : (s.slot * s.copies + copy) * p.rows.own_rows + row;
+        float* o = (s.prefix ? p.p_o : p.o_o) + at * DK;
+        if (mine) (s.prefix ? p.p_ml : p.o_ml)[at] = make_float4(r.ref, r.l, r.rl, 0.f);
 #pragma unroll
         for (int i = 0; i < DK / 32; ++i) {
           uint32_t v[32];
-          tmem_ld32(t_row + kTmemO + 32 * i, v);
+          tmem_ld32(lanes + kTmemO + 32 * i, v);
           reg_pin(v);
           if (mine) {
 #pragma unroll
@@ -585,33 +671,38 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
     h = (int)(id / p.R % p.Hkv);
     b = (int)(id / p.R / p.Hkv);
     const Line line = line_of(p, __ldg(p.sched + p.c.B), grid);
-    // slots of the row: those of the prefix unit, then those of the own unit
+    // partial results of the row: np of its prefix unit, no of its own one, a
+    // result's copies one after the other
+    const Rows& rw = p.rows;
+    const int t = rr / p.G, g = rr % p.G;
+    const int m = t / rw.tokens * rw.head_tiles + g / rw.heads;              // tile of the sequence
+    const int ro = (t % rw.tokens) * p.G + g % rw.heads;                     // row of the tile
     int np = 0, no = 0;
-    int64_t sp0 = 0, so0 = 0;
-    int rp = 0, ro = 0;
+    int64_t at_p = 0, at_o = 0;
     if (p.nt_prefix > 0) {
-      const int64_t at = (int64_t)b * p.R + rr;
-      const int m = (int)(at / kTile), u = h * p.mt_prefix + m;
-      rp = (int)(at % kTile);
+      const int u = h * rw.prefix_units + b / rw.seqs * rw.per_seq + m;
       const int64_t t0 = (int64_t)u * p.nt_prefix;
       const int c0 = line.cta(t0), c1 = line.cta(t0 + p.nt_prefix - 1);
-      sp0 = c0 + u;
-      np = c1 - c0 + 1;
+      np = (c1 - c0 + 1) * rw.prefix_copies;
+      at_p = (int64_t)(c0 + u) * kRows + b % rw.seqs * p.R + ro;
     }
-    const int own0 = __ldg(p.sched + b), nt = (__ldg(p.sched + b + 1) - own0) / (p.Hkv * p.mt_own);
+    const int own0 = __ldg(p.sched + b), nt = (__ldg(p.sched + b + 1) - own0) / (p.Hkv * rw.own_units);
     if (nt > 0) {
-      const int u = h * p.mt_own + rr / kTile;
-      ro = rr % kTile;
+      const int u = h * rw.own_units + m;
       const int64_t t0 = line.prefix + own0 + (int64_t)u * nt;
       const int c0 = line.cta(t0), c1 = line.cta(t0 + nt - 1);
-      so0 = c0 + (int64_t)b * p.Hkv * p.mt_own + u;
-      no = c1 - c0 + 1;
+      no = (c1 - c0 + 1) * rw.own_copies;
+      at_o = (c0 + (int64_t)b * p.Hkv * rw.own_units + u) * rw.own_copies * rw.own_rows + ro;
     }
+    const auto row_of = [&](int i) -> int64_t {            // of result i
+      if (i >= np) return at_o + (int64_t)(i - np) * rw.own_rows;
+      const int c = i / rw.prefix_copies;
+      return at_p + (int64_t)c * kRows + (i - c * rw.prefix_copies) * rw.prefix_rows;
+    };
     for (int s0 = 32 * sub; s0 < np + no; s0 += 32 * WPR) {
       const int s = s0 + lane;
       float4 ml = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (s < np) ml = __ldcg(p.p_ml + (sp0 + s) * kTile + rp);
-      else if (s < np + no) ml = __ldcg(p.o_ml + (so0 + s - np) * p.Rm + ro);
+      if (s < np + no) ml = __ldcg((s < np ? p.p_ml : p.o_ml) + row_of(s));
       float m = ml.y == 0.f ? -INFINITY : ml.x;             // (a NaN sum stays in)
       float top = m;
 #pragma unroll
@@ -632,7 +723,7 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
       for (int i = 0; i < n; ++i) {
         const float wi = __shfl_sync(0xffffffffu, w, i);
         const int si = s0 + i;
-        const float* src = si < np ? p.p_o + ((sp0 + si) * kTile + rp) * DK : p.o_o + ((so0 + si - np) * p.Rm + ro) * DK;
+        const float* src = (si < np ? p.p_o : p.o_o) + row_of(si) * DK;
         float o[E];
         if constexpr (E == 4) {
           const float4 f = __ldcg(reinterpret_cast<const float4*>(src) + lane);
@@ -649,7 +740,7 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
     }
     // the last T - 1 own entries, of which this row sees the first few
     if (sub == 0 && p.c.T > 1) {
-      const int t = rr / p.G, hq = h * p.G + rr % p.G, n = used(p, b), j0 = max(0, n - (p.c.T - 1));
+      const int hq = h * p.G + g, n = used(p, b), j0 = max(0, n - (p.c.T - 1));
       const int far = n - (p.c.T - 1 - t);
       float q[E];
       load_row<DK, BF16>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, lane, q);
@@ -721,16 +812,14 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
   }
 }
 
-// One warp per 32 entries of a tile: the rows' scores of an entry, added up.
-__global__ void __launch_bounds__(kTile) weights_kernel(const __grid_constant__ AttnParams p) {
+// Two tiles per CTA, one thread per entry: the scores of its rows, added up.
+__global__ void __launch_bounds__(2 * kTile) weights_kernel(const __grid_constant__ AttnParams p) {
   pdl_launch_dependents();
   pdl_wait();
   const int b = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, n = used(p, b);
   const float* lse2 = p.lse2 + (int64_t)blockIdx.y * p.R;
-  for (int tile = blockIdx.x; tile * kTile < n; tile += gridDim.x) {
-    const int j = tile * kTile + threadIdx.x;
-    if (j >= n) return;
-    const float* s = p.scores + ((int64_t)blockIdx.y * p.nt_cap + tile) * p.R * kTile + threadIdx.x;
+  for (int j = blockIdx.x * 2 * kTile + threadIdx.x; j < n; j += gridDim.x * 2 * kTile) {
+    const float* s = p.scores + ((int64_t)blockIdx.y * p.nt_cap + j / kTile) * p.R * kTile + j % kTile;
     float* w = p.c.weights + b * p.c.weights_batch + h * p.c.weights_head + j;
     float sum = 0.f;
 #pragma unroll 4
@@ -755,37 +844,40 @@ PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
   return fn;
 }
 
-// [batch][entry][head][D] of 16-bit elements in boxes of 64 elements x 128
-// entries, zero past the extents.  A dimension of size 1 has no stride.
-bool encode_kv(CUtensorMap* map, bool bf16, const void* base, int D, int64_t entries, int64_t heads, int64_t batch,
-               int64_t s_entry, int64_t s_head, int64_t s_batch) {
+// Rows of D 16-bit elements over three outer dimensions, in boxes of 64 elements
+// x `box`, zero past the extents.  A dimension of size 1 has no stride.
+bool encode(CUtensorMap* map, bool bf16, const void* base, int D, const int64_t (&n)[3], const int64_t (&stride)[3],
+            const int (&box)[3]) {
   const auto enc = get_encode();
   if (!enc) return false;
-  const auto bytes = [&](int64_t n, int64_t stride) { return (cuuint64_t)(n > 1 ? 2 * stride : 2 * (int64_t)D); };
-  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)entries, (cuuint64_t)heads, (cuuint64_t)batch};
-  const cuuint64_t strides[3] = {bytes(entries, s_entry), bytes(heads, s_head), bytes(batch, s_batch)};
-  const cuuint32_t box[4] = {64, kTile, 1, 1}, ones[4] = {1, 1, 1, 1};
+  cuuint64_t dims[4] = {(cuuint64_t)D}, bytes[3];
+  cuuint32_t boxes[4] = {64}, ones[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) {
+    dims[i + 1] = (cuuint64_t)n[i];
+    bytes[i] = (cuuint64_t)(n[i] > 1 ? 2 * stride[i] : 2 * (int64_t)D);
+    boxes[i + 1] = (cuuint32_t)box[i];
+  }
   return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
-             const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             const_cast<void*>(base), dims, bytes, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DK>
 size_t attend_smem(int B) {
-  return 1024 + (size_t)(1 + 2 * kStages<DK>) * kTileBytes<DK> + (4 * kStages<DK> + 6) * 8 + 8 + 32 + (size_t)(B + 1) * 4;
+  return 1024 + kQBytes<DK> + (size_t)2 * kStages<DK> * kTileBytes<DK> + (4 * kStages<DK> + 9) * 8 + 8 + 32 +
+         (size_t)(B + 1) * 4;
 }
 
 template <int DK, bool BF16>
-cudaError_t launch_attend_t(const AttnParams& p, const CUtensorMap (&maps)[4], int dev, int grid, cudaStream_t s) {
+cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, int grid, cudaStream_t s) {
   static PerDevice attr;
   cudaError_t e = attr.once(dev, []() {
     return cudaFuncSetAttribute(attend_kernel<DK, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)attend_smem<DK>(SPIKE_PROJ_CACHE_MAX_B));
   });
   if (e != cudaSuccess) return e;
-  e = launch_pdl(attend_kernel<DK, BF16>, dim3(grid), dim3(kAttThreads), attend_smem<DK>(p.c.B), s, maps[0], maps[1],
-                 maps[2], maps[3], p);
+  e = launch_pdl(attend_kernel<DK, BF16>, dim3(grid), dim3(kAttThreads), attend_smem<DK>(p.c.B), s, maps, p);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
   if (rows <= 2048)
@@ -793,7 +885,27 @@ cudaError_t launch_attend_t(const AttnParams& p, const CUtensorMap (&maps)[4], i
   else
     e = launch_pdl(combine_kernel<DK, BF16, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(32 * kCombWarps), 0, s, p, grid);
   if (e != cudaSuccess || !p.c.weights) return e;
-  return launch_pdl(weights_kernel, dim3((unsigned)min(p.nt_cap, 65535), (unsigned)(p.c.B * p.Hkv)), dim3(kTile), 0, s, p);
+  return launch_pdl(weights_kernel, dim3((unsigned)min(ceil_div(p.nt_cap, 2), 65535), (unsigned)(p.c.B * p.Hkv)),
+                    dim3(2 * kTile), 0, s, p);
+}
+
+// Copies of a unit's rows in the MMA's 128.
+int copies_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
+
+Rows rows_of(int B, int T, int G) {
+  Rows r;
+  r.heads = min(G, kRows);
+  r.head_tiles = ceil_div(G, kRows);
+  r.tokens = r.head_tiles > 1 ? 1 : min(T, kRows / G);
+  r.per_seq = ceil_div(T, r.tokens) * r.head_tiles;
+  r.seqs = r.per_seq > 1 ? 1 : min(B, kRows / (T * G));
+  r.own_units = r.per_seq;
+  r.prefix_units = ceil_div(B, r.seqs) * r.per_seq;
+  r.own_rows = r.heads * r.tokens;
+  r.prefix_rows = r.own_rows * r.seqs;
+  r.own_copies = copies_of(r.own_rows);
+  r.prefix_copies = copies_of(r.prefix_rows);
+  return r;
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -803,17 +915,18 @@ struct Parts {
   size_t sched, lse2, p_ml, p_o, o_ml, o_o, scores, end;
 };
 Parts parts_of(const CacheShape& s, int B, int T, int grid) {
-  const int R = T * (s.Hq / s.Hkv), Rm = min(R, kTile), DK = s.D <= 64 ? 64 : 128;
-  const size_t p_slots = (size_t)grid + (size_t)s.Hkv * ceil_div(B * R, kTile);
-  const size_t o_slots = (size_t)grid + (size_t)B * s.Hkv * ceil_div(R, kTile);
+  const int G = s.Hq / s.Hkv, R = T * G, DK = s.D <= 64 ? 64 : 128;
+  const Rows r = rows_of(B, T, G);
+  const size_t p_slots = (size_t)grid + (size_t)s.Hkv * r.prefix_units;
+  const size_t o_rows = ((size_t)grid + (size_t)B * s.Hkv * r.own_units) * r.own_rows * r.own_copies;
   Parts w;
   w.sched = 0;
   w.lse2 = round256((size_t)(B + 1) * 4);
   w.p_ml = w.lse2 + round256((size_t)B * s.Hkv * R * 4);
-  w.p_o = w.p_ml + p_slots * kTile * 16;
-  w.o_ml = w.p_o + p_slots * kTile * DK * 4;
-  w.o_o = w.o_ml + round256(o_slots * Rm * 16);
-  w.scores = w.o_o + round256(o_slots * Rm * DK * 4);
+  w.p_o = w.p_ml + p_slots * kRows * 16;
+  w.o_ml = w.p_o + p_slots * kRows * DK * 4;
+  w.o_o = w.o_ml + round256(o_rows * 16);
+  w.scores = w.o_o + round256(o_rows * DK * 4);
   w.end = w.scores + (s.weights ? (size_t)B * s.Hkv * ceil_div(s.capacity, kTile) * R * kTile * 4 : 0);
   return w;
 }
@@ -822,9 +935,18 @@ Parts parts_of(const CacheShape& s, int B, int T, int grid) {
 
 CacheWorkspace cache_workspace(const CacheShape& s, int sms) {
   CacheWorkspace w;
-  w.moves = round256(parts_of(s, s.max_batch, s.max_T, 2 * sms).end);
+  // (the rows of a unit, and with them its parts, do not only grow with T)
+  size_t most = 0;
+  for (int T = 1; T <= s.max_T; ++T) most = max(most, parts_of(s, s.max_batch, T, 2 * sms).end);
+  w.moves = round256(most);
   w.bytes = w.moves + (size_t)s.max_batch * s.Hkv * (s.capacity / 2 + 1) * 8;
   return w;
+}
+
+int64_t attend_tiles(const CacheShape& s, const sp_attend& c) {
+  const Rows r = rows_of(c.B, c.T, s.Hq / s.Hkv);
+  return s.Hkv * ((int64_t)r.prefix_units * ceil_div(c.prefix_len, kTile) +
+                  (int64_t)c.B * r.own_units * ceil_div(s.capacity, kTile));
 }
 
 cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err, cudaStream_t stream) {
@@ -839,9 +961,7 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.D = s.D;
   p.capacity = s.capacity;
   p.R = c.T * p.G;
-  p.Rm = min(p.R, kTile);
-  p.mt_own = ceil_div(p.R, kTile);
-  p.mt_prefix = ceil_div(c.B * p.R, kTile);
+  p.rows = rows_of(c.B, c.T, p.G);
   p.nt_prefix = ceil_div(c.prefix_len, kTile);
   p.nt_cap = ceil_div(s.capacity, kTile);
   p.c2 = c.scale * kLog2e;
@@ -856,16 +976,23 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.o_o = reinterpret_cast<float*>(ws + w.o_o);
   p.scores = c.weights ? reinterpret_cast<float*>(ws + w.scores) : nullptr;
   const bool bf16 = s.dtype == SP_BF16;
-  CUtensorMap maps[4];
-  if (!encode_kv(&maps[2], bf16, c.k, s.D, s.capacity, s.Hkv, c.B, c.k_entry, c.k_head, c.k_batch) ||
-      !encode_kv(&maps[3], bf16, c.v, s.D, s.capacity, s.Hkv, c.B, c.v_entry, c.v_head, c.v_batch))
+  const Rows& r = p.rows;
+  AttnMaps maps;
+  const int64_t nq[3] = {s.Hq, c.T, c.B}, sq[3] = {c.q_head, c.q_token, c.q_batch};
+  const int64_t nk[3] = {s.capacity, s.Hkv, c.B};
+  if (!encode(&maps.q, bf16, c.q, s.D, nq, sq, {r.heads, r.tokens, 1}) ||
+      !encode(&maps.pq, bf16, c.q, s.D, nq, sq, {r.heads, r.tokens, r.seqs}) ||
+      !encode(&maps.k, bf16, c.k, s.D, nk, {c.k_entry, c.k_head, c.k_batch}, {kTile, 1, 1}) ||
+      !encode(&maps.v, bf16, c.v, s.D, nk, {c.v_entry, c.v_head, c.v_batch}, {kTile, 1, 1}))
     return cudaErrorInvalidValue;
   if (c.prefix_len == 0) {
-    maps[0] = maps[2];                     // (read by nothing)
-    maps[1] = maps[3];
-  } else if (!encode_kv(&maps[0], bf16, c.prefix_k, s.D, c.prefix_len, s.Hkv, 1, c.pk_entry, c.pk_head, 0) ||
-             !encode_kv(&maps[1], bf16, c.prefix_v, s.D, c.prefix_len, s.Hkv, 1, c.pv_entry, c.pv_head, 0)) {
-    return cudaErrorInvalidValue;
+    maps.pk = maps.k;                      // (read by nothing)
+    maps.pv = maps.v;
+  } else {
+    const int64_t np[3] = {c.prefix_len, s.Hkv, 1};
+    if (!encode(&maps.pk, bf16, c.prefix_k, s.D, np, {c.pk_entry, c.pk_head, 0}, {kTile, 1, 1}) ||
+        !encode(&maps.pv, bf16, c.prefix_v, s.D, np, {c.pv_entry, c.pv_head, 0}, {kTile, 1, 1}))
+      return cudaErrorInvalidValue;
   }
   if (s.D <= 64)
     return bf16 ? launch_attend_t<64, true>(p, maps, dev, grid, stream)

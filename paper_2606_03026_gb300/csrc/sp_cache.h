@@ -18,10 +18,12 @@ struct CacheShape {
 // Workspace of a handle (bytes from the start of one allocation).
 struct CacheWorkspace {
   size_t bytes;
-  size_t lse, moves;
+  size_t moves;
 };
 CacheWorkspace cache_workspace(const CacheShape& s, int sms);
 
+// Tiles of entries that a call has at most (its launch counts them in 32 bits).
+int64_t attend_tiles(const CacheShape& s, const sp_attend& c);
 cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err,
                           cudaStream_t stream);
 cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cudaStream_t stream);
