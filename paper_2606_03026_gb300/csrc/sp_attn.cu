@@ -39,7 +39,7 @@
 // entries, of which the query tokens see 0, 1, .. T - 1, are left to
 // combine_kernel, so that no masked probability ever meets a value.
 //
-// combine_kernel: one or four warps per query row merge its partial results and
+// combine_kernel: one or eight warps per query row merge its partial results and
 // these last entries.  weights_kernel: the weights, from the scores of the own
 // entries that attend_kernel left in the workspace and the rows' lse.
 #include <cuda.h>
@@ -650,31 +650,35 @@ template <int E> struct Part {
   }
 };
 
-constexpr int kCombWarps = 4;
+constexpr int kCombBatch = 8;              // results that a warp has on their way
 
-template <int DK, bool BF16, int WPR>      // WPR warps per query row
-__global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_constant__ AttnParams p, int grid) {
+// WPR warps of a CTA of W per query row, each with its share of the row's
+// partial results and of its last entries.
+template <int DK, bool BF16, int W, int WPR>
+__global__ void __launch_bounds__(32 * W) combine_kernel(const __grid_constant__ AttnParams p, int grid) {
   constexpr int E = DK / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
   pdl_launch_dependents();
   pdl_wait();
-  const int64_t id = (int64_t)blockIdx.x * (kCombWarps / WPR) + warp / WPR;     // (b, h, row)
+  const int64_t id = (int64_t)blockIdx.x * (W / WPR) + warp / WPR;     // (b, h, row)
   const bool real = id < (int64_t)p.c.B * p.Hkv * p.R;
   Part<E> a;
   a.m = -INFINITY;
   a.l = a.r = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) a.o[i] = 0.f;
-  int b = 0, h = 0, rr = 0;
+  int b = 0, h = 0, t = 0, hq = 0;
   if (real) {
-    rr = (int)(id % p.R);
-    h = (int)(id / p.R % p.Hkv);
-    b = (int)(id / p.R / p.Hkv);
+    const int rr = (int)(id % p.R), bh = (int)(id / p.R);
+    h = bh % p.Hkv;
+    b = bh / p.Hkv;
+    t = rr / p.G;
+    const int g = rr - t * p.G;
+    hq = h * p.G + g;
     const Line line = line_of(p, __ldg(p.sched + p.c.B), grid);
     // partial results of the row: np of its prefix unit, no of its own one, a
-    // result's copies one after the other
+    // segment's copies one after the other
     const Rows& rw = p.rows;
-    const int t = rr / p.G, g = rr % p.G;
     const int m = t / rw.tokens * rw.head_tiles + g / rw.heads;              // tile of the sequence
     const int ro = (t % rw.tokens) * p.G + g % rw.heads;                     // row of the tile
     int np = 0, no = 0;
@@ -694,16 +698,20 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
       no = (c1 - c0 + 1) * rw.own_copies;
       at_o = (c0 + (int64_t)b * p.Hkv * rw.own_units + u) * rw.own_copies * rw.own_rows + ro;
     }
-    const auto row_of = [&](int i) -> int64_t {            // of result i
-      if (i >= np) return at_o + (int64_t)(i - np) * rw.own_rows;
-      const int c = i / rw.prefix_copies;
-      return at_p + (int64_t)c * kRows + (i - c * rw.prefix_copies) * rw.prefix_rows;
-    };
-    for (int s0 = 32 * sub; s0 < np + no; s0 += 32 * WPR) {
-      const int s = s0 + lane;
+    const int share = (np + no + WPR - 1) / WPR, end = min((sub + 1) * share, np + no);
+    for (int s0 = sub * share; s0 < end; s0 += 32) {
+      const int s = s0 + lane, n = min(32, end - s0);
       float4 ml = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (s < np + no) ml = __ldcg((s < np ? p.p_ml : p.o_ml) + row_of(s));
-      float m = ml.y == 0.f ? -INFINITY : ml.x;             // (a NaN sum stays in)
+      const float* src = p.p_o;
+      if (lane < n) {
+        const bool own = s >= np;
+        const int c = s / rw.prefix_copies;
+        const int64_t at = own ? at_o + (int64_t)(s - np) * rw.own_rows
+                               : at_p + (int64_t)c * kRows + (s - c * rw.prefix_copies) * rw.prefix_rows;
+        ml = __ldcg((own ? p.o_ml : p.p_ml) + at);
+        src = (own ? p.o_o : p.p_o) + at * DK;
+      }
+      const float m = ml.y == 0.f ? -INFINITY : ml.x;       // (a NaN sum stays in)
       float top = m;
 #pragma unroll
       for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -718,33 +726,38 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
       }
       a.l += l;
       a.r += r;
-      const int n = min(32, np + no - s0);
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) {
-        const float wi = __shfl_sync(0xffffffffu, w, i);
-        const int si = s0 + i;
-        const float* src = (si < np ? p.p_o : p.o_o) + row_of(si) * DK;
-        float o[E];
-        if constexpr (E == 4) {
-          const float4 f = __ldcg(reinterpret_cast<const float4*>(src) + lane);
-          o[0] = f.x, o[1] = f.y, o[2] = f.z, o[3] = f.w;
-        } else {
-          const float2 f = __ldcg(reinterpret_cast<const float2*>(src) + lane);
-          o[0] = f.x, o[1] = f.y;
-        }
-        if (wi != 0.f) {
+      for (int i0 = 0; i0 < n; i0 += kCombBatch) {
+        float o[kCombBatch][E];
 #pragma unroll
-          for (int e = 0; e < E; ++e) a.o[e] = fmaf(wi, o[e], a.o[e]);
+        for (int i = 0; i < kCombBatch; ++i) {
+          const float* from =
+              reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), i0 + i));
+          if (i0 + i < n) {
+            if constexpr (E == 4) {
+              const float4 f = __ldcg(reinterpret_cast<const float4*>(from) + lane);
+              o[i][0] = f.x, o[i][1] = f.y, o[i][2] = f.z, o[i][3] = f.w;
+            } else {
+              const float2 f = __ldcg(reinterpret_cast<const float2*>(from) + lane);
+              o[i][0] = f.x, o[i][1] = f.y;
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kCombBatch; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
+          if (i0 + i < n && wi != 0.f) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) a.o[e] = fmaf(wi, o[i][e], a.o[e]);
+          }
         }
       }
     }
     // the last T - 1 own entries, of which this row sees the first few
-    if (sub == 0 && p.c.T > 1) {
-      const int hq = h * p.G + g, n = used(p, b), j0 = max(0, n - (p.c.T - 1));
-      const int far = n - (p.c.T - 1 - t);
+    if (p.c.T > 1) {
+      const int n = used(p, b), far = n - (p.c.T - 1 - t);
       float q[E];
       load_row<DK, BF16>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, lane, q);
-      for (int j = j0; j < n; ++j) {
+      for (int j = max(0, n - (p.c.T - 1)) + sub; j < n; j += WPR) {
         float s = -INFINITY;
         if (j < far) {
           float k[E], v[E];
@@ -770,7 +783,7 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
     }
   }
   if constexpr (WPR > 1) {
-    __shared__ float s_ml[kCombWarps][3], s_o[kCombWarps][DK];
+    __shared__ float s_ml[W][3], s_o[W][DK];
 #pragma unroll
     for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = a.o[e];
     if (lane == 0) {
@@ -780,7 +793,6 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
     }
     __syncthreads();
     if (sub != 0) return;
-#pragma unroll
     for (int w = 1; w < WPR; ++w) {
       const float m = s_ml[warp + w][0];
       if (m == -INFINITY) continue;
@@ -793,7 +805,6 @@ __global__ void __launch_bounds__(32 * kCombWarps) combine_kernel(const __grid_c
     }
   }
   if (!real) return;
-  const int t = rr / p.G, hq = h * p.G + rr % p.G;
   const bool empty = a.l == 0.f;
   const float inv = empty ? 0.f : 1.f / a.r;
   if (lane * E < p.D) {
@@ -881,9 +892,9 @@ cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, 
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
   if (rows <= 2048)
-    e = launch_pdl(combine_kernel<DK, BF16, 4>, dim3((unsigned)rows), dim3(32 * kCombWarps), 0, s, p, grid);
+    e = launch_pdl(combine_kernel<DK, BF16, 8, 8>, dim3((unsigned)rows), dim3(256), 0, s, p, grid);
   else
-    e = launch_pdl(combine_kernel<DK, BF16, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(32 * kCombWarps), 0, s, p, grid);
+    e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, p, grid);
   if (e != cudaSuccess || !p.c.weights) return e;
   return launch_pdl(weights_kernel, dim3((unsigned)min(ceil_div(p.nt_cap, 2), 65535), (unsigned)(p.c.B * p.Hkv)),
                     dim3(2 * kTile), 0, s, p);
