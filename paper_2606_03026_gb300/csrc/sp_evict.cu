@@ -9,9 +9,12 @@
 // ranges of slots, their warps contiguous spans.  The order's place of each
 // entry is one 32-bit key: the weight's bits made monotone, above them NaN,
 // above all the newest entries.  The budget-th largest key is found by digits,
-// high ones first, from histograms that the CTAs of the cluster add up; ties at
-// it go by slot.  Then counts and ranks of the slots that are left and of the
-// entries that move make a list of moves, and the cluster's warps share it.
+// of 11, 11 and 10 bits, high ones first, from histograms that the CTAs of the
+// cluster add up (the first one while the keys are made), and ends where every
+// entry that shares the digits found is kept; ties at a whole key go by slot.
+// Then counts and ranks of the slots that are left and of the entries that move
+// make a list of moves, and the cluster's threads copy its rows in pieces of 16
+// bytes, kCopies of them on their way per thread.
 #include <math.h>
 
 #include "sp_cache.h"
@@ -20,16 +23,18 @@
 namespace sp {
 namespace {
 
-constexpr int kEvThreads = 512;
+constexpr int kEvThreads = 256;
 constexpr int kEvWarps = kEvThreads / 32;
-constexpr int kEvBits = 8;
-constexpr int kEvBins = 1 << kEvBits;
+constexpr int kEvBins = 2048;
+constexpr int kEvPer = kEvBins / kEvThreads;       // bins of a thread
+constexpr int kCopies = 8;
 constexpr int kEvMaxCluster = 8;
-constexpr int kEvCached = 20 * 1024;       // keys of a CTA held in shared memory
+constexpr int kEvCached = 16 * 1024;       // keys of a CTA held in shared memory
 
 struct EvictParams {
   sp_evict c;
-  int32_t Hkv, capacity, row16, cached;    // 16-byte pieces of a K or V row; keys that fit in shared memory
+  int32_t Hkv, capacity, cached;           // keys that fit in shared memory
+  int32_t row16, row16_log2;               // 16-byte pieces of a K or V row; its logarithm, -1 if it is none
   int2* moves;                             // [B][Hkv][capacity / 2 + 1]
 };
 
@@ -46,13 +51,23 @@ __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
   return v;
 }
 
+__device__ __forceinline__ uint4 ld_cluster4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(addr)
+               : "memory");
+  return v;
+}
+
 struct Counts {                            // of one CTA, read by its cluster
   uint32_t ties, holes, moved;
 };
 
 __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant__ EvictParams p) {
   extern __shared__ uint32_t s_keys[];
-  __shared__ uint32_t s_hist[2][kEvBins], s_warp[3][kEvWarps], s_pick[3];
+  __shared__ __align__(16) uint32_t s_hist[2][kEvBins];
+  __shared__ uint32_t s_warp[3][kEvWarps], s_pick[3];
   __shared__ Counts s_counts;
   const sp_evict& c = p.c;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -60,6 +75,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
   const int bh = blockIdx.x / ranks, b = bh / p.Hkv, h = bh % p.Hkv;
+  for (int i = t; i < kEvBins; i += kEvThreads) s_hist[0][i] = 0;
   pdl_launch_dependents();
   pdl_wait();
   const int n = min(max(__ldg(c.lens + b), 0), p.capacity);
@@ -81,58 +97,86 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   const int per = ceil_div(n, (int)ranks), j0 = min((int)rank * per, n), j1 = min(j0 + per, n);
   const int span = ceil_div(ceil_div(per, kEvWarps), 32) * 32;
   const int w0 = min(j0 + warp * span, j1), w1 = min(w0 + span, j1);
-  for (int i = t; i < min(j1 - j0, p.cached); i += kEvThreads) s_keys[i] = key_of(__ldg(wt + j0 + i), __ldg(ps + j0 + i), newest);
   const auto key = [&](int j) {
     return j - j0 < p.cached ? s_keys[j - j0] : key_of(__ldg(wt + j), __ldg(ps + j), newest);
   };
+  __syncthreads();                         // (the histogram is zero)
+  for (int i = w0 + lane; i < w1; i += 32 * 4) {
+    float w[4];
+    int q[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + 32 * e < w1) {
+        w[e] = __ldg(wt + i + 32 * e);
+        q[e] = __ldg(ps + i + 32 * e);
+      }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + 32 * e < w1) {
+        const uint32_t k = key_of(w[e], q[e], newest);
+        if (i + 32 * e - j0 < p.cached) s_keys[i + 32 * e - j0] = k;
+        atomicAdd(&s_hist[0][k >> 21], 1u);
+      }
+  }
 
   // The budget-th largest key: `top` its digits found so far, `need` how many
   // of the entries with these digits are kept.
   uint32_t top = 0, need = c.budget;
-  int shift = 32, pass = 0;
+  int shift = 21;
   bool ties = true;
-  while (shift > 0) {
-    shift -= kEvBits;
-    uint32_t* hist = s_hist[pass & 1];
-    for (int i = t; i < kEvBins; i += kEvThreads) hist[i] = 0;
+  for (int pass = 0;; ++pass) {
+    const uint32_t* hist = s_hist[pass & 1];
+    if (ranks > 1) cluster_sync(); else __syncthreads();
+    // thread i has the kEvPer bins below kEvBins - kEvPer i: entries in them
+    // and in higher bins
+    const int bin = kEvBins - kEvPer * (t + 1);
+    uint32_t in[kEvPer] = {}, mine = 0;
+    for (uint32_t r = 0; r < ranks; ++r) {
+#pragma unroll
+      for (int i = 0; i < kEvPer / 4; ++i) {
+        const uint4 g = ranks > 1 ? ld_cluster4(cluster_addr(&hist[bin + 4 * i], r))
+                                  : *reinterpret_cast<const uint4*>(&hist[bin + 4 * i]);
+        in[4 * i] += g.x, in[4 * i + 1] += g.y, in[4 * i + 2] += g.z, in[4 * i + 3] += g.w;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kEvPer; ++i) mine += in[i];
+    uint32_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += y;
+    }
+    if (lane == 31) s_warp[0][warp] = incl;
+    // the next pass's histogram (that of two passes ago, which every CTA has read)
+    for (int i = t; i < kEvBins; i += kEvThreads) s_hist[(pass + 1) & 1][i] = 0;
     __syncthreads();
+    for (int w = 0; w < warp; ++w) incl += s_warp[0][w];
+    if (incl >= need && incl - mine < need) {
+      uint32_t over = incl - mine;         // entries in higher bins
+      bool found = false;
+#pragma unroll
+      for (int i = kEvPer - 1; i >= 0; --i) {
+        if (!found && over + in[i] >= need) {
+          found = true;
+          s_pick[0] = bin + i;
+          s_pick[1] = need - over;
+          s_pick[2] = in[i];
+        }
+        over += in[i];
+      }
+    }
+    __syncthreads();
+    top = (pass == 0 ? 0u : top << (pass == 1 ? 11 : 10)) | s_pick[0];
+    need = s_pick[1];
+    ties = need != s_pick[2];              // else every entry with these digits is kept
+    if (!ties || pass == 2) break;
+    const int next = pass == 0 ? 10 : 0;
     for (int i = w0 + lane; i < w1; i += 32) {
       const uint32_t k = key(i);
-      if (pass == 0 || (k >> (shift + kEvBits)) == top) atomicAdd(&hist[(k >> shift) & (kEvBins - 1)], 1u);
+      if (k >> shift == top) atomicAdd(&s_hist[(pass + 1) & 1][(k >> next) & (pass == 0 ? 2047u : 1023u)], 1u);
     }
-    if (ranks > 1) cluster_sync(); else __syncthreads();
-    // thread i has bin kEvBins - 1 - i: entries in it and in higher bins
-    uint32_t mine = 0, incl = 0;
-    if (t < kEvBins) {
-      if (ranks > 1)
-        for (uint32_t r = 0; r < ranks; ++r) mine += ld_cluster(cluster_addr(&hist[kEvBins - 1 - t], r));
-      else
-        mine = hist[kEvBins - 1 - t];
-      incl = mine;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += y;
-      }
-      if (lane == 31) s_warp[0][warp] = incl;
-    }
-    __syncthreads();
-    if (t < kEvBins) {
-      for (int w = 0; w < warp; ++w) incl += s_warp[0][w];
-      if (incl >= need && incl - mine < need) {
-        s_pick[0] = kEvBins - 1 - t;
-        s_pick[1] = need - (incl - mine);
-        s_pick[2] = mine;
-      }
-    }
-    __syncthreads();
-    top = top << kEvBits | s_pick[0];
-    need = s_pick[1];
-    ++pass;
-    if (need == s_pick[2]) {               // every entry with these digits is kept
-      ties = false;
-      break;
-    }
+    shift = next;
   }
 
   // Ties at the key go by slot: those before this warp's span.
@@ -155,7 +199,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   }
   const auto kept_of = [&](int j, uint32_t& tie) {     // (every lane of the warp together)
     const bool in = j < w1;
-    const uint32_t k = in ? key(j) : 0u, d = shift < 32 ? k >> shift : 0u;
+    const uint32_t d = in ? key(j) >> shift : 0u;
     bool kept = in && d > top;
     if (!ties) return kept || (in && d == top);
     const uint32_t eq = __ballot_sync(0xffffffffu, in && d == top);
@@ -224,19 +268,36 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   const int64_t kb = b * c.k_batch + h * c.k_head, vb = b * c.v_batch + h * c.v_head;
   uint16_t* K = static_cast<uint16_t*>(c.k) + kb;
   uint16_t* V = static_cast<uint16_t*>(c.v) + vb;
-  for (uint32_t i = rank * kEvWarps + warp; i < total; i += ranks * kEvWarps) {
+  const uint32_t stride = ranks * kEvThreads, at = rank * kEvThreads + t;
+  for (uint32_t i = at; i < total; i += stride) {
     const int2 m = __ldcg(moves + i);
-    for (int e = lane; e < 2 * p.row16; e += 32) {
-      const bool is_v = e >= p.row16;
-      const int at = 8 * (is_v ? e - p.row16 : e);
-      uint16_t* X = is_v ? V : K;
-      const int64_t ent = is_v ? c.v_entry : c.k_entry;
-      *reinterpret_cast<uint4*>(X + m.y * ent + at) = __ldcg(reinterpret_cast<const uint4*>(X + m.x * ent + at));
+    wt_out[m.y] = __ldg(wt + m.x);
+    ps_out[m.y] = __ldg(ps + m.x);
+  }
+  // (move, piece) pairs: the K row's pieces, then the V row's
+  const uint32_t pieces = 2 * p.row16;
+  for (uint64_t e0 = at; e0 < (uint64_t)total * pieces; e0 += (uint64_t)kCopies * stride) {
+    uint4 x[kCopies];
+    uint16_t* to[kCopies];
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const uint64_t e = e0 + (uint64_t)i * stride;
+      to[i] = nullptr;
+      if (e < (uint64_t)total * pieces) {
+        const uint32_t mv = p.row16_log2 >= 0 ? (uint32_t)(e >> (p.row16_log2 + 1)) : (uint32_t)(e / pieces);
+        uint32_t piece = (uint32_t)(e - (uint64_t)mv * pieces);
+        const bool is_v = piece >= (uint32_t)p.row16;
+        if (is_v) piece -= p.row16;
+        const int2 m = __ldcg(moves + mv);
+        uint16_t* X = (is_v ? V : K) + 8 * piece;
+        const int64_t ent = is_v ? c.v_entry : c.k_entry;
+        x[i] = __ldcg(reinterpret_cast<const uint4*>(X + m.x * ent));
+        to[i] = X + m.y * ent;
+      }
     }
-    if (lane == 0) {
-      wt_out[m.y] = __ldg(wt + m.x);
-      ps_out[m.y] = __ldg(ps + m.x);
-    }
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i)
+      if (to[i]) *reinterpret_cast<uint4*>(to[i]) = x[i];
   }
   if (ranks > 1) cluster_sync();           // no CTA leaves while its counts may be read
 }
@@ -253,12 +314,15 @@ cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cu
   });
   if (e != cudaSuccess) return e;
   int cluster = kEvMaxCluster;
-  while (cluster > 1 && (c.B * s.Hkv * cluster > 2 * sms || s.capacity < 2048 * cluster)) cluster /= 2;
+  while (cluster > 1 && (c.B * s.Hkv * cluster > 4 * sms || s.capacity < 2048 * cluster)) cluster /= 2;
   EvictParams p;
   p.c = c;
   p.Hkv = s.Hkv;
   p.capacity = s.capacity;
   p.row16 = s.D / 8;
+  p.row16_log2 = -1;
+  for (int i = 0; i < 8; ++i)
+    if (p.row16 == 1 << i) p.row16_log2 = i;
   p.cached = min(ceil_div(s.capacity, cluster), kEvCached);
   p.moves = reinterpret_cast<int2*>(ws + cache_workspace(s, sms).moves);
   cudaLaunchConfig_t cfg = {};

@@ -7,9 +7,13 @@
 //
 // The sums are whole numbers in 64 bits, so that they may be split anywhere.
 // One thread-block cluster per sequence: its CTAs take contiguous slices of the
-// row, their warps contiguous spans of the slice.  The spans' sums meet in
-// shared memory, the slices' in every CTA's (distributed shared memory), and
-// the one warp whose span the running sum passes c in reads that span again.
+// row, their warps contiguous spans of the slice.  A warp streams its span of
+// both rows through a ring in shared memory of its own, in pieces of 512 entries
+// (bulk copies: all that the ring holds is on its way, 96 KB per CTA), and keeps
+// the sums of up to kGroups groups of pieces.  The spans' sums meet in shared
+// memory, the slices' in every CTA's (distributed shared memory).  The CTA whose
+// slice the running sum passes c in reads the one group where it does again,
+// every thread a few entries of it.
 #include <math.h>
 
 #include "sp_cache.h"
@@ -18,13 +22,20 @@
 namespace sp {
 namespace {
 
-constexpr int kVerThreads = 512;
+constexpr int kVerThreads = 256;
 constexpr int kVerWarps = kVerThreads / 32;
 constexpr int kVerMaxCluster = 16;
+constexpr int kVerPerSm = 2;               // CTAs that an SM holds
+constexpr int kPiece = 512;                // entries of a bulk copy
+constexpr int kPieceBytes = 4 * kPiece + 32;   // and what lies around them in its 16-byte pieces
+constexpr int kRing = 3;                   // pieces of each row per warp
+constexpr int kGroups = 64;
+constexpr size_t kVerSmem = (size_t)kVerWarps * kRing * 2 * kPieceBytes;
 
 struct VerifyParams {
   sp_verify c;
   int32_t slice, span;      // entries of a CTA and of a warp
+  int32_t per_group;        // pieces of a group
 };
 
 __device__ __forceinline__ float unit(float u) { return fminf(fmaxf(u, 0.f), 0x1.fffffep-1f); }
@@ -32,29 +43,112 @@ __device__ __forceinline__ unsigned long long whole(float r) {
   return r > 0.f ? __float2ull_rn(fminf(r, 1.f) * 0x1p36f) : 0ull;
 }
 
-__global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_constant__ VerifyParams p) {
+// `count` entries of a row, in the 16-byte pieces that hold them.
+__device__ __forceinline__ uint32_t piece_bytes(const float* from, int count) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(from);
+  return (uint32_t)(((a + 4 * (uintptr_t)count + 15) & ~(uintptr_t)15) - (a & ~(uintptr_t)15));
+}
+__device__ __forceinline__ const float* piece_base(const float* from) {
+  return reinterpret_cast<const float*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15);
+}
+__device__ __forceinline__ int piece_skip(const float* from) {
+  return (int)(reinterpret_cast<uintptr_t>(from) & 15) / 4;
+}
+
+// Sum of the whole numbers of entries v0 .. v1 of a warp, the groups' into
+// `groups`.  it: pieces that have gone through the ring before.
+__device__ __forceinline__ unsigned long long sum_span(const float* pr, const float* qr, int v0, int v1, int per_group,
+                                                       uint8_t* ring, uint64_t* full, int& it,
+                                                       unsigned long long* groups) {
+  const int lane = threadIdx.x & 31;
+  const int pieces = ceil_div(max(v1 - v0, 0), kPiece);
+  const int it0 = it;
+  const auto fetch = [&](int i) {
+    const int st = (it0 + i) % kRing, v = v0 + i * kPiece, n = min(kPiece, v1 - v);
+    uint8_t* to = ring + st * 2 * kPieceBytes;
+    mbar_arrive_expect_tx(&full[st], piece_bytes(pr + v, n) + (qr ? piece_bytes(qr + v, n) : 0u));
+    bulk_load(to, piece_base(pr + v), piece_bytes(pr + v, n), &full[st]);
+    if (qr) bulk_load(to + kPieceBytes, piece_base(qr + v), piece_bytes(qr + v, n), &full[st]);
+  };
+  if (lane == 0)
+    for (int i = 0; i < min(kRing, pieces); ++i) fetch(i);
+  unsigned long long all = 0, group = 0;
+  for (int i = 0; i < pieces; ++i, ++it) {
+    const int st = it % kRing, v = v0 + i * kPiece, n = min(kPiece, v1 - v);
+    const float* x = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes) + piece_skip(pr + v);
+    const float* y = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes + kPieceBytes) + (qr ? piece_skip(qr + v) : 0);
+    // (a copy that never arrives is read from its source instead)
+    const uint32_t parity = it / kRing & 1;
+    const bool here = __all_sync(0xffffffffu, mbar_try_wait(&full[st], parity) || mbar_wait(&full[st], parity));
+    if (!here) {
+      x = pr + v;
+      y = qr + v;
+    }
+    // nearly every number fits 32 bits, whose conversion is several times faster
+    unsigned long long sum = 0;
+    float most = 0.f;
+    if (n == kPiece) {
+#pragma unroll
+      for (int e = 0; e < kPiece / 32; ++e) {
+        const float r = fmaxf(x[lane + 32 * e] - (qr ? y[lane + 32 * e] : 0.f), 0.f) * 0x1p36f;
+        most = fmaxf(most, r);
+        sum += __float2uint_rn(r);
+      }
+    } else {
+      most = INFINITY;
+    }
+    if (most >= 0x1p31f) {
+      sum = 0;
+      for (int e = lane; e < n; e += 32) sum += whole(x[e] - (qr ? y[e] : 0.f));
+    }
+    __syncwarp();
+    if (lane == 0 && i + kRing < pieces && here) fetch(i + kRing);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    all += sum;
+    group += sum;
+    if (i % per_group == per_group - 1 || i == pieces - 1) {
+      if (lane == 0) groups[i / per_group] = group;
+      group = 0;
+    }
+  }
+  return all;
+}
+
+__global__ void __launch_bounds__(kVerThreads, kVerPerSm) verify_kernel(const __grid_constant__ VerifyParams p) {
+  extern __shared__ __align__(128) uint8_t s_ring[];
+  __shared__ __align__(8) uint64_t s_full[kVerWarps][kRing];
   __shared__ int s_bad[2];
-  __shared__ unsigned long long s_warp[kVerWarps], s_cta[2][kVerMaxCluster];
+  __shared__ unsigned long long s_warp[kVerWarps], s_cta[2][kVerMaxCluster], s_scan[kVerWarps];
+  __shared__ unsigned long long s_group[kVerWarps][kGroups];
   const sp_verify& c = p.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t rank, ranks;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
   const int b = blockIdx.x / ranks;
+  if (lane == 0) {
+    for (int i = 0; i < kRing; ++i) mbar_init(&s_full[warp][i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  int it = 0;
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   pdl_launch_dependents();
   pdl_wait();
 
   // the first draft that is not kept
+  const float us = unit(__ldg(c.u_sample + b));
   const int nd = c.n_draft ? min(max(__ldg(c.n_draft + b), 0), c.T) : c.T;
   if (warp < 2) {
     const int t = threadIdx.x;
     bool ok = false;
-    if (t < nd) {
+    if (t < c.T) {
       const int x = __ldg(c.draft + b * c.ld_draft + t);
+      const float u = unit(__ldg(c.u + b * c.ld_u + t));
       if (x >= 0 && x < c.V)
-        ok = __fmul_rn(unit(__ldg(c.u + b * c.ld_u + t)), __ldg(c.q + b * c.q_batch + t * c.q_row + x)) <
-             __ldg(c.p + b * c.p_batch + t * c.p_row + x);
+        ok = __fmul_rn(u, __ldg(c.q + b * c.q_batch + t * c.q_row + x)) < __ldg(c.p + b * c.p_batch + t * c.p_row + x);
+      if (rank == 0) c.tokens[b * c.ld_tokens + t] = x;     // (those that are not kept go below)
     }
     const uint32_t bad = __ballot_sync(0xffffffffu, !ok);
     if (lane == 0) s_bad[warp] = bad ? 32 * warp + __ffs(bad) - 1 : 64;
@@ -62,10 +156,8 @@ __global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_consta
   __syncthreads();
   const int n = min(min(s_bad[0], s_bad[1]), nd);
   if (rank == 0 && threadIdx.x <= c.T) {
-    const int t = threadIdx.x;
-    if (t < n) c.tokens[b * c.ld_tokens + t] = __ldg(c.draft + b * c.ld_draft + t);
-    if (t > n) c.tokens[b * c.ld_tokens + t] = -1;
-    if (t == 0) c.n_accept[b] = n;
+    if (threadIdx.x > n) c.tokens[b * c.ld_tokens + threadIdx.x] = -1;
+    if (threadIdx.x == 0) c.n_accept[b] = n;
   }
 
   const float* pr = c.p + b * c.p_batch + n * c.p_row;
@@ -74,10 +166,8 @@ __global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_consta
   const int v1 = min(min(v0 + p.span, (int)(rank + 1) * p.slice), c.V);
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // every CTA of the cluster is running
   for (int pass = 0;; ++pass) {
-    unsigned long long sum = 0;
-    for (int v = v0 + lane; v < v1; v += 32) sum += whole(qr ? __ldg(pr + v) - __ldg(qr + v) : __ldg(pr + v));
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const unsigned long long sum =
+        sum_span(pr, qr, v0, v1, p.per_group, s_ring + (size_t)warp * kRing * 2 * kPieceBytes, s_full[warp], it, s_group[warp]);
     if (lane == 0) s_warp[warp] = sum;
     __syncthreads();
     if (threadIdx.x < ranks) {
@@ -100,23 +190,36 @@ __global__ void __launch_bounds__(kVerThreads) verify_kernel(const __grid_consta
       if (rank == 0 && threadIdx.x == 0) c.tokens[b * c.ld_tokens + n] = -1;
       return;
     }
-    const unsigned long long at = __umul64hi((unsigned long long)(unit(__ldg(c.u_sample + b)) * 0x1p24f) << 40, S);
-    for (int w = 0; w < warp; ++w) before += s_warp[w];
-    if (at < before || at - before >= s_warp[warp]) return;
-    for (int v = v0; v < v1; v += 32) {
-      const int i = v + lane;
-      unsigned long long x = i < v1 ? whole(qr ? __ldg(pr + i) - __ldg(qr + i) : __ldg(pr + i)) : 0ull;
+    const unsigned long long at = __umul64hi((unsigned long long)(us * 0x1p24f) << 40, S);
+    if (at < before || at - before >= s_cta[pass][rank]) return;
+    // the group of pieces in which the running sum passes c (the whole CTA is here)
+    int w = 0, g = 0;
+    while (at - before >= s_warp[w]) before += s_warp[w++];
+    while (at - before >= s_group[w][g]) before += s_group[w][g++];
+    const int w0 = (int)rank * p.slice + w * p.span + g * p.per_group * kPiece;
+    const int w1 = min(min(w0 + p.per_group * kPiece, (int)rank * p.slice + (w + 1) * p.span), min((int)(rank + 1) * p.slice, c.V));
+    const int each = p.per_group * kPiece / kVerThreads, i0 = w0 + (int)threadIdx.x * each, i1 = min(i0 + each, w1);
+    unsigned long long mine = 0;
+    for (int i = i0; i < i1; ++i) mine += whole(qr ? __ldg(pr + i) - __ldg(qr + i) : __ldg(pr + i));
+    unsigned long long run = mine;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const unsigned long long y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned long long y = __shfl_up_sync(0xffffffffu, run, d);
+      if (lane >= d) run += y;
+    }
+    if (lane == 31) s_scan[warp] = run;
+    __syncthreads();
+    run += before - mine;                  // sum of all entries before this thread's
+    for (int i = 0; i < warp; ++i) run += s_scan[i];
+    if (run <= at && at - run < mine) {
+      for (int i = i0;; ++i) {
+        const unsigned long long x = whole(qr ? __ldg(pr + i) - __ldg(qr + i) : __ldg(pr + i));
+        if (at - run < x) {
+          c.tokens[b * c.ld_tokens + n] = i;
+          break;
+        }
+        run += x;
       }
-      const uint32_t past = __ballot_sync(0xffffffffu, before + x > at);
-      if (past) {
-        if (lane == 0) c.tokens[b * c.ld_tokens + n] = v + __ffs(past) - 1;
-        return;
-      }
-      before += __shfl_sync(0xffffffffu, x, 31);
     }
     return;
   }
@@ -128,15 +231,23 @@ cudaError_t launch_verify(const sp_verify& c, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = current_device(&dev, &sms);
   if (e != cudaSuccess) return e;
-  int cluster = 8;
-  while (cluster > 1 && (c.B * cluster > 2 * sms || c.V < 1024 * cluster)) cluster /= 2;
+  static PerDevice set;
+  e = set.once(dev, []() {
+    const cudaError_t e = cudaFuncSetAttribute(verify_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(verify_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kVerSmem);
+  });
+  if (e != cudaSuccess) return e;
+  int cluster = kVerMaxCluster;
+  while (cluster > 1 && (c.B * cluster > kVerPerSm * sms || c.V < 1024 * cluster)) cluster /= 2;
   VerifyParams p;
   p.c = c;
   p.slice = ceil_div(c.V, cluster);
-  p.span = ceil_div(ceil_div(p.slice, kVerWarps), 32) * 32;
+  p.span = ceil_div(ceil_div(p.slice, kVerWarps), 64) * 64;
+  p.per_group = ceil_div(ceil_div(p.span, kPiece), kGroups);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(c.B * cluster), 1, 1);
   cfg.blockDim = dim3(kVerThreads, 1, 1);
+  cfg.dynamicSmemBytes = kVerSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
