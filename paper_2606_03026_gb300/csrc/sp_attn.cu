@@ -950,7 +950,8 @@ CacheWorkspace cache_workspace(const CacheShape& s, int sms) {
   size_t most = 0;
   for (int T = 1; T <= s.max_T; ++T) most = max(most, parts_of(s, s.max_batch, T, 2 * sms).end);
   w.moves = round256(most);
-  w.bytes = w.moves + (size_t)s.max_batch * s.Hkv * (s.capacity / 2 + 1) * 8;
+  w.counts = w.moves + round256((size_t)s.max_batch * s.Hkv * (s.capacity / 2) * 8);
+  w.bytes = w.counts + (size_t)s.max_batch * s.Hkv * 4;
   return w;
 }
 

@@ -18,7 +18,7 @@ struct CacheShape {
 // Workspace of a handle (bytes from the start of one allocation).
 struct CacheWorkspace {
   size_t bytes;
-  size_t moves;
+  size_t moves, counts;                    // of evictions: lists of slot pairs per head, their lengths
 };
 CacheWorkspace cache_workspace(const CacheShape& s, int sms);
 

@@ -5,16 +5,19 @@
 // move into the slots below it that others leave, so that no row is read and
 // written in one call and nothing moves that can stay.
 //
-// One thread-block cluster per (sequence, head); its CTAs take contiguous
-// ranges of slots, their warps contiguous spans.  The order's place of each
-// entry is one 32-bit key: the weight's bits made monotone, above them NaN,
-// above all the newest entries.  The budget-th largest key is found by digits,
-// of 11, 11 and 10 bits, high ones first, from histograms that the CTAs of the
-// cluster add up (the first one while the keys are made), and ends where every
-// entry that shares the digits found is kept; ties at a whole key go by slot.
-// Then counts and ranks of the slots that are left and of the entries that move
-// make a list of moves, and the cluster's threads copy its rows in pieces of 16
-// bytes, kCopies of them on their way per thread.
+// One CTA per (sequence, head), or a thread-block cluster where there are few of
+// them and their caches are long; its CTAs take contiguous ranges of slots, their
+// warps contiguous spans.  The order's place of each entry is one 32-bit key:
+// the weight's bits made monotone, above them NaN, above all the newest entries.
+// The budget-th largest key is found by digits of 11, 11 and 10 bits, high ones
+// first, from histograms that the CTAs of the cluster add up (the first one
+// while the keys are made), and ends where every entry that shares the digits
+// found is kept; ties at a whole key go by slot.  A CTA that is alone ranks the
+// entries of the first digit found one against another instead, when they are
+// few.  Then each warp turns its span into words of kept entries, and counts and
+// ranks of the slots that are left and of the entries that move make a list of
+// moves.  Few moves are made at once, in pieces of 16 bytes; many by a second
+// kernel, whose CTAs take 128 moves each, whatever head they are of.
 #include <math.h>
 
 #include "sp_cache.h"
@@ -23,11 +26,12 @@
 namespace sp {
 namespace {
 
-constexpr int kEvThreads = 256;
-constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBins = 2048;
-constexpr int kEvPer = kEvBins / kEvThreads;       // bins of a thread
-constexpr int kCopies = 8;
+constexpr int kCopies = 8;                 // pieces that a thread has on their way
+constexpr int kFewMoves = 64;              // of a head, made by the kernel that finds them
+constexpr int kMoveBlock = 128;            // of a CTA of the other kernel
+constexpr int kMoveThreads = 256;
+constexpr int kRanked = kEvBins / 2;       // entries ranked one against another (in a histogram's place)
 constexpr int kEvMaxCluster = 8;
 constexpr int kEvCached = 16 * 1024;       // keys of a CTA held in shared memory
 
@@ -35,7 +39,9 @@ struct EvictParams {
   sp_evict c;
   int32_t Hkv, capacity, cached;           // keys that fit in shared memory
   int32_t row16, row16_log2;               // 16-byte pieces of a K or V row; its logarithm, -1 if it is none
-  int2* moves;                             // [B][Hkv][capacity / 2 + 1]
+  int2* moves;                             // [B][Hkv][most_moves]
+  int32_t* counts;                         // [B][Hkv], where a second kernel makes the moves; else null
+  int32_t most_moves;                      // that a head can have
 };
 
 __device__ __forceinline__ uint32_t key_of(float w, int pos, int64_t newest) {
@@ -51,12 +57,9 @@ __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
   return v;
 }
 
-__device__ __forceinline__ uint4 ld_cluster4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(addr)
-               : "memory");
+__device__ __forceinline__ uint2 ld_cluster2(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
   return v;
 }
 
@@ -64,10 +67,57 @@ struct Counts {                            // of one CTA, read by its cluster
   uint32_t ties, holes, moved;
 };
 
-__global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant__ EvictParams p) {
+// What a move takes along: weight and pos of `count` moves, then the pieces of
+// their K and V rows; thread `at` of `stride`, COPIES pieces on their way each.
+template <int COPIES, typename Move>
+__device__ __forceinline__ void make_moves(const EvictParams& p, int b, int h, uint32_t count, uint32_t at, uint32_t stride,
+                                           Move move) {
+  const sp_evict& c = p.c;
+  const float* wt = c.weights + b * c.in_batch + h * c.in_head;
+  const int* ps = c.pos + b * c.in_batch + h * c.in_head;
+  float* wt_out = c.weights_out + b * c.out_batch + h * c.out_head;
+  int* ps_out = c.pos_out + b * c.out_batch + h * c.out_head;
+  uint16_t* K = static_cast<uint16_t*>(c.k) + b * c.k_batch + h * c.k_head;
+  uint16_t* V = static_cast<uint16_t*>(c.v) + b * c.v_batch + h * c.v_head;
+  for (uint32_t i = at; i < count; i += stride) {
+    const int2 m = move(i);
+    wt_out[m.y] = __ldg(wt + m.x);
+    ps_out[m.y] = __ldg(ps + m.x);
+  }
+  // (a head has fewer than 2^23 moves of at most 32 pieces)
+  const uint32_t pieces = 2 * p.row16, total = count * pieces;
+  for (uint32_t e0 = at; e0 < total; e0 += COPIES * stride) {
+    uint4 x[COPIES];
+    uint16_t* to[COPIES];
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+      const uint32_t e = e0 + i * stride;
+      to[i] = nullptr;
+      if (e < total) {
+        const uint32_t mv = p.row16_log2 >= 0 ? e >> (p.row16_log2 + 1) : e / pieces;
+        uint32_t piece = e - mv * pieces;
+        const bool is_v = piece >= (uint32_t)p.row16;
+        if (is_v) piece -= p.row16;
+        const int2 m = move(mv);
+        uint16_t* X = (is_v ? V : K) + 8 * piece;
+        const int64_t ent = is_v ? c.v_entry : c.k_entry;
+        x[i] = __ldcg(reinterpret_cast<const uint4*>(X + m.x * ent));
+        to[i] = X + m.y * ent;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i)
+      if (to[i]) *reinterpret_cast<uint4*>(to[i]) = x[i];
+  }
+}
+
+// NT threads, 1024 / NT CTAs per SM.
+template <int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_constant__ EvictParams p) {
+  constexpr int kWarps = NT / 32, kPer = kEvBins / NT;     // bins of a thread
   extern __shared__ uint32_t s_keys[];
   __shared__ __align__(16) uint32_t s_hist[2][kEvBins];
-  __shared__ uint32_t s_warp[3][kEvWarps], s_pick[3];
+  __shared__ uint32_t s_warp[3][kWarps], s_pick[3], s_ranked;
   __shared__ Counts s_counts;
   const sp_evict& c = p.c;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -75,32 +125,26 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
   const int bh = blockIdx.x / ranks, b = bh / p.Hkv, h = bh % p.Hkv;
-  for (int i = t; i < kEvBins; i += kEvThreads) s_hist[0][i] = 0;
+  for (int i = t; i < kEvBins; i += NT) s_hist[0][i] = 0;
+  if (t == 0) s_ranked = 0;
   pdl_launch_dependents();
   pdl_wait();
   const int n = min(max(__ldg(c.lens + b), 0), p.capacity);
+  const int64_t newest = (int64_t)__ldg(c.now + b) - c.recent;
   const float* wt = c.weights + b * c.in_batch + h * c.in_head;
   const int* ps = c.pos + b * c.in_batch + h * c.in_head;
   float* wt_out = c.weights_out + b * c.out_batch + h * c.out_head;
   int* ps_out = c.pos_out + b * c.out_batch + h * c.out_head;
   if (h == 0 && rank == 0 && t == 0) c.lens_out[b] = min(n, c.budget);
-  if (n <= c.budget) {
-    for (int j = rank * kEvThreads + t; j < n; j += ranks * kEvThreads) {
-      wt_out[j] = __ldg(wt + j);
-      ps_out[j] = __ldg(ps + j);
-    }
-    return;
-  }
+  const bool stay = n <= c.budget || c.budget == 0;        // nothing moves
+  if (p.counts && rank == 0 && t == 0 && stay) p.counts[bh] = 0;
   if (c.budget == 0) return;
-
-  const int64_t newest = (int64_t)__ldg(c.now + b) - c.recent;
   const int per = ceil_div(n, (int)ranks), j0 = min((int)rank * per, n), j1 = min(j0 + per, n);
-  const int span = ceil_div(ceil_div(per, kEvWarps), 32) * 32;
+  const int span = ceil_div(ceil_div(per, kWarps), 32) * 32;
   const int w0 = min(j0 + warp * span, j1), w1 = min(w0 + span, j1);
-  const auto key = [&](int j) {
-    return j - j0 < p.cached ? s_keys[j - j0] : key_of(__ldg(wt + j), __ldg(ps + j), newest);
-  };
   __syncthreads();                         // (the histogram is zero)
+  // Weight and pos below the budget go out as they are (those of slots that
+  // are left are written again with the moves); all of them make keys.
   for (int i = w0 + lane; i < w1; i += 32 * 4) {
     float w[4];
     int q[4];
@@ -111,13 +155,25 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
         q[e] = __ldg(ps + i + 32 * e);
       }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (i + 32 * e < w1) {
+    for (int e = 0; e < 4; ++e) {
+      const int j = i + 32 * e;
+      if (j < w1) {
         const uint32_t k = key_of(w[e], q[e], newest);
-        if (i + 32 * e - j0 < p.cached) s_keys[i + 32 * e - j0] = k;
-        atomicAdd(&s_hist[0][k >> 21], 1u);
+        if (j < c.budget) {
+          wt_out[j] = w[e];
+          ps_out[j] = q[e];
+        }
+        if (!stay) {
+          if (j - j0 < p.cached) s_keys[j - j0] = k;
+          atomicAdd(&s_hist[0][k >> 21], 1u);
+        }
       }
+    }
   }
+  if (stay) return;
+  const auto key = [&](int j) {
+    return j - j0 < p.cached ? s_keys[j - j0] : key_of(__ldg(wt + j), __ldg(ps + j), newest);
+  };
 
   // The budget-th largest key: `top` its digits found so far, `need` how many
   // of the entries with these digits are kept.
@@ -127,20 +183,25 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
   for (int pass = 0;; ++pass) {
     const uint32_t* hist = s_hist[pass & 1];
     if (ranks > 1) cluster_sync(); else __syncthreads();
-    // thread i has the kEvPer bins below kEvBins - kEvPer i: entries in them
-    // and in higher bins
-    const int bin = kEvBins - kEvPer * (t + 1);
-    uint32_t in[kEvPer] = {}, mine = 0;
-    for (uint32_t r = 0; r < ranks; ++r) {
+    // thread i has the kPer bins below kEvBins - kPer i: entries in them and in
+    // higher bins
+    const int bin = kEvBins - kPer * (t + 1);
+    uint32_t in[kPer] = {}, mine = 0;
+    if (ranks > 1) {
 #pragma unroll
-      for (int i = 0; i < kEvPer / 4; ++i) {
-        const uint4 g = ranks > 1 ? ld_cluster4(cluster_addr(&hist[bin + 4 * i], r))
-                                  : *reinterpret_cast<const uint4*>(&hist[bin + 4 * i]);
-        in[4 * i] += g.x, in[4 * i + 1] += g.y, in[4 * i + 2] += g.z, in[4 * i + 3] += g.w;
-      }
+      for (uint32_t r = 0; r < kEvMaxCluster; ++r)
+#pragma unroll
+        for (int i = 0; i < kPer / 2; ++i)
+          if (r < ranks) {
+            const uint2 g = ld_cluster2(cluster_addr(&hist[bin + 2 * i], r));
+            in[2 * i] += g.x, in[2 * i + 1] += g.y;
+          }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) in[i] = hist[bin + i];
     }
 #pragma unroll
-    for (int i = 0; i < kEvPer; ++i) mine += in[i];
+    for (int i = 0; i < kPer; ++i) mine += in[i];
     uint32_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -149,14 +210,14 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     }
     if (lane == 31) s_warp[0][warp] = incl;
     // the next pass's histogram (that of two passes ago, which every CTA has read)
-    for (int i = t; i < kEvBins; i += kEvThreads) s_hist[(pass + 1) & 1][i] = 0;
+    for (int i = t; i < kEvBins; i += NT) s_hist[(pass + 1) & 1][i] = 0;
     __syncthreads();
     for (int w = 0; w < warp; ++w) incl += s_warp[0][w];
     if (incl >= need && incl - mine < need) {
       uint32_t over = incl - mine;         // entries in higher bins
       bool found = false;
 #pragma unroll
-      for (int i = kEvPer - 1; i >= 0; --i) {
+      for (int i = kPer - 1; i >= 0; --i) {
         if (!found && over + in[i] >= need) {
           found = true;
           s_pick[0] = bin + i;
@@ -169,8 +230,28 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     __syncthreads();
     top = (pass == 0 ? 0u : top << (pass == 1 ? 11 : 10)) | s_pick[0];
     need = s_pick[1];
-    ties = need != s_pick[2];              // else every entry with these digits is kept
+    const uint32_t share = s_pick[2];      // entries with these digits
+    ties = need != share;                  // else all of them are kept
     if (!ties || pass == 2) break;
+    if (pass == 0 && ranks == 1 && share <= kRanked && n <= p.cached && top < kEvBins - 1) {
+      // few: by key, then slot; the kept ones get a key above the digit, the others 0
+      unsigned long long* few = reinterpret_cast<unsigned long long*>(s_hist[1]);
+      for (int i = w0 + lane; i < w1; i += 32) {
+        const uint32_t k = s_keys[i];
+        if (k >> 21 == top) few[atomicAdd(&s_ranked, 1u)] = (unsigned long long)k << 32 | (uint32_t)~i;
+      }
+      __syncthreads();
+      for (uint32_t i = t; i < share; i += NT) {
+        const unsigned long long x = few[i];
+        uint32_t above = 0;
+#pragma unroll 4
+        for (uint32_t e = 0; e < share; ++e) above += few[e] > x;
+        s_keys[~(uint32_t)x] = above < need ? (top + 1) << 21 : 0u;
+      }
+      __syncthreads();
+      ties = false;
+      break;
+    }
     const int next = pass == 0 ? 10 : 0;
     for (int i = w0 + lane; i < w1; i += 32) {
       const uint32_t k = key(i);
@@ -187,7 +268,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
     if (lane == 0) s_warp[0][warp] = cnt;
     __syncthreads();
     uint32_t all = 0;
-    for (int w = 0; w < kEvWarps; ++w) {
+    for (int w = 0; w < kWarps; ++w) {
       if (w < warp) tie_at += s_warp[0][w];
       all += s_warp[0][w];
     }
@@ -197,31 +278,48 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
       for (uint32_t r = 0; r < rank; ++r) tie_at += ld_cluster(cluster_addr(&s_counts.ties, r));
     }
   }
-  const auto kept_of = [&](int j, uint32_t& tie) {     // (every lane of the warp together)
-    const bool in = j < w1;
-    const uint32_t d = in ? key(j) >> shift : 0u;
-    bool kept = in && d > top;
-    if (!ties) return kept || (in && d == top);
-    const uint32_t eq = __ballot_sync(0xffffffffu, in && d == top);
-    if (in && d == top) kept = tie + __popc(eq & ((1u << lane) - 1u)) < need;
-    tie += __popc(eq);
-    return kept;
+  // 32 words of the span: lane i's has a bit for each of the entries from
+  // base + 32 i on that are kept.
+  const auto kept_words = [&](int base, uint32_t& tie) {
+    uint32_t mine = 0;
+    for (int i = 0; i < 32 && base + 32 * i < w1; ++i) {
+      const int j = base + 32 * i + lane;
+      const bool in = j < w1;
+      const uint32_t d = in ? key(j) >> shift : 0u;
+      uint32_t kept = __ballot_sync(0xffffffffu, in && (d > top || (!ties && d == top)));
+      if (ties) {
+        uint32_t eq = __ballot_sync(0xffffffffu, in && d == top);
+        tie += __popc(eq);
+        for (uint32_t cut = tie > need ? tie - need : 0u; cut > 0 && eq; --cut) eq &= ~(0x80000000u >> __clz(eq));
+        kept |= eq;
+      }
+      if (lane == i) mine = kept;
+    }
+    return mine;
   };
+  const auto low = [](int bits) { return bits >= 32 ? 0xffffffffu : bits <= 0 ? 0u : (1u << bits) - 1u; };
   // Slots below the budget that are left, and kept entries behind it.
-  uint32_t holes = 0, moved = 0, tie = tie_at;
-  for (int i = w0; i < w1; i += 32) {
-    const int j = i + lane;
-    const bool kept = kept_of(j, tie);
-    holes += __popc(__ballot_sync(0xffffffffu, j < w1 && j < c.budget && !kept));
-    moved += __popc(__ballot_sync(0xffffffffu, j < w1 && j >= c.budget && kept));
+  uint32_t holes = 0, moved = 0, tie = tie_at, word = 0;
+  for (int base = w0; base < w1; base += 1024) {
+    word = kept_words(base, tie);
+    const int at = base + 32 * lane;
+    const uint32_t there = low(w1 - at), below = low(c.budget - at);
+    holes += __popc(~word & there & below);
+    moved += __popc(word & there & ~below);
   }
-  if (lane == 0) {
-    s_warp[1][warp] = holes;
-    s_warp[2][warp] = moved;
+  uint32_t holes_in = holes, moved_in = moved;             // with the lanes before
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, holes_in, d), y = __shfl_up_sync(0xffffffffu, moved_in, d);
+    if (lane >= d) holes_in += x, moved_in += y;
+  }
+  if (lane == 31) {
+    s_warp[1][warp] = holes_in;
+    s_warp[2][warp] = moved_in;
   }
   __syncthreads();
   uint32_t hole_at = 0, moved_at = 0, all_moved = 0, all_holes = 0;
-  for (int w = 0; w < kEvWarps; ++w) {
+  for (int w = 0; w < kWarps; ++w) {
     if (w < warp) {
       hole_at += s_warp[1][w];
       moved_at += s_warp[2][w];
@@ -246,88 +344,64 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const __grid_constant
       total += m;
     }
   }
-  // The list of moves (from, to), and what stays in place.
-  int2* moves = p.moves + (int64_t)bh * (p.capacity / 2 + 1);
+  // The list of moves (from, to).
+  int2* moves = p.moves + (int64_t)bh * p.most_moves;
+  const bool whole = w1 - w0 <= 1024;      // `word` is still the span's
   tie = tie_at;
-  for (int i = w0; i < w1; i += 32) {
-    const int j = i + lane;
-    const bool kept = kept_of(j, tie), in = j < w1, below = j < c.budget;
-    const uint32_t mh = __ballot_sync(0xffffffffu, in && below && !kept);
-    const uint32_t mm = __ballot_sync(0xffffffffu, in && !below && kept);
-    const uint32_t lower = (1u << lane) - 1u;
-    if (in && below && !kept) moves[hole_at + __popc(mh & lower)].y = j;
-    if (in && !below && kept) moves[moved_at + __popc(mm & lower)].x = j;
-    if (in && below && kept) {
-      wt_out[j] = __ldg(wt + j);
-      ps_out[j] = __ldg(ps + j);
+  for (int base = w0; base < w1; base += 1024) {
+    if (!whole) {
+      word = kept_words(base, tie);
     }
-    hole_at += __popc(mh);
-    moved_at += __popc(mm);
+    const int at = base + 32 * lane;
+    const uint32_t there = low(w1 - at), below = low(c.budget - at);
+    uint32_t hole = ~word & there & below, move = word & there & ~below;
+    uint32_t hi = __popc(hole), mi = __popc(move);
+    const uint32_t nh = hi, nm = mi;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const uint32_t x = __shfl_up_sync(0xffffffffu, hi, d), y = __shfl_up_sync(0xffffffffu, mi, d);
+      if (lane >= d) hi += x, mi += y;
+    }
+    uint32_t to = hole_at + hi - nh, from = moved_at + mi - nm;
+    for (; hole; hole &= hole - 1) moves[to++].y = at + __ffs(hole) - 1;
+    for (; move; move &= move - 1) moves[from++].x = at + __ffs(move) - 1;
+    hole_at += __shfl_sync(0xffffffffu, hi, 31);
+    moved_at += __shfl_sync(0xffffffffu, mi, 31);
+  }
+  if (p.counts) {
+    if (rank == 0 && t == 0) p.counts[bh] = total;
+    if (ranks > 1) cluster_sync();         // no CTA leaves while its counts may be read
+    return;
   }
   if (ranks > 1) cluster_sync(); else __syncthreads();
-  const int64_t kb = b * c.k_batch + h * c.k_head, vb = b * c.v_batch + h * c.v_head;
-  uint16_t* K = static_cast<uint16_t*>(c.k) + kb;
-  uint16_t* V = static_cast<uint16_t*>(c.v) + vb;
-  const uint32_t stride = ranks * kEvThreads, at = rank * kEvThreads + t;
-  for (uint32_t i = at; i < total; i += stride) {
-    const int2 m = __ldcg(moves + i);
-    wt_out[m.y] = __ldg(wt + m.x);
-    ps_out[m.y] = __ldg(ps + m.x);
-  }
-  // (move, piece) pairs: the K row's pieces, then the V row's
-  const uint32_t pieces = 2 * p.row16;
-  for (uint64_t e0 = at; e0 < (uint64_t)total * pieces; e0 += (uint64_t)kCopies * stride) {
-    uint4 x[kCopies];
-    uint16_t* to[kCopies];
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i) {
-      const uint64_t e = e0 + (uint64_t)i * stride;
-      to[i] = nullptr;
-      if (e < (uint64_t)total * pieces) {
-        const uint32_t mv = p.row16_log2 >= 0 ? (uint32_t)(e >> (p.row16_log2 + 1)) : (uint32_t)(e / pieces);
-        uint32_t piece = (uint32_t)(e - (uint64_t)mv * pieces);
-        const bool is_v = piece >= (uint32_t)p.row16;
-        if (is_v) piece -= p.row16;
-        const int2 m = __ldcg(moves + mv);
-        uint16_t* X = (is_v ? V : K) + 8 * piece;
-        const int64_t ent = is_v ? c.v_entry : c.k_entry;
-        x[i] = __ldcg(reinterpret_cast<const uint4*>(X + m.x * ent));
-        to[i] = X + m.y * ent;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kCopies; ++i)
-      if (to[i]) *reinterpret_cast<uint4*>(to[i]) = x[i];
-  }
-  if (ranks > 1) cluster_sync();           // no CTA leaves while its counts may be read
+  make_moves<kCopies>(p, b, h, total, rank * NT + t, ranks * NT, [&](uint32_t i) { return __ldcg(moves + i); });
 }
 
-}  // namespace
+// CTA (i, bh): moves kMoveBlock i .. of the list of head bh.
+__global__ void __launch_bounds__(kMoveThreads, 5) move_kernel(const __grid_constant__ EvictParams p) {
+  __shared__ int2 s_moves[kMoveBlock];
+  pdl_launch_dependents();
+  pdl_wait();
+  const uint32_t heads = p.c.B * p.Hkv, bh = blockIdx.x % heads, first = blockIdx.x / heads * kMoveBlock;
+  const uint32_t total = __ldcg(p.counts + bh);
+  if (first >= total) return;
+  const uint32_t count = min((uint32_t)kMoveBlock, total - first);
+  if (threadIdx.x < count) s_moves[threadIdx.x] = __ldcg(p.moves + (int64_t)bh * p.most_moves + first + threadIdx.x);
+  __syncthreads();
+  make_moves<4>(p, bh / p.Hkv, bh % p.Hkv, count, threadIdx.x, kMoveThreads, [&](uint32_t i) { return s_moves[i]; });
+}
 
-cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cudaStream_t stream) {
-  static PerDevice attr_set;
-  int dev = 0, sms = 0;
-  cudaError_t e = current_device(&dev, &sms);
-  if (e != cudaSuccess) return e;
-  e = attr_set.once(dev, []() {
-    return cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvCached * 4);
+template <int NT>
+cudaError_t launch_evict_t(EvictParams p, int dev, int cluster, cudaStream_t stream) {
+  static PerDevice set;
+  const cudaError_t e = set.once(dev, []() {
+    return cudaFuncSetAttribute(evict_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvCached * 4);
   });
   if (e != cudaSuccess) return e;
-  int cluster = kEvMaxCluster;
-  while (cluster > 1 && (c.B * s.Hkv * cluster > 4 * sms || s.capacity < 2048 * cluster)) cluster /= 2;
-  EvictParams p;
-  p.c = c;
-  p.Hkv = s.Hkv;
-  p.capacity = s.capacity;
-  p.row16 = s.D / 8;
-  p.row16_log2 = -1;
-  for (int i = 0; i < 8; ++i)
-    if (p.row16 == 1 << i) p.row16_log2 = i;
-  p.cached = min(ceil_div(s.capacity, cluster), kEvCached);
-  p.moves = reinterpret_cast<int2*>(ws + cache_workspace(s, sms).moves);
+  p.cached = min(ceil_div(p.capacity, cluster), kEvCached);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(c.B * s.Hkv * cluster), 1, 1);
-  cfg.blockDim = dim3(kEvThreads, 1, 1);
+  cfg.gridDim = dim3((unsigned)(p.c.B * p.Hkv * cluster), 1, 1);
+  cfg.blockDim = dim3(NT, 1, 1);
   cfg.dynamicSmemBytes = (size_t)p.cached * 4;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -339,7 +413,44 @@ cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cu
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, evict_kernel, p);
+  return cudaLaunchKernelEx(&cfg, evict_kernel<NT>, p);
+}
+
+}  // namespace
+
+cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cudaStream_t stream) {
+  int dev = 0, sms = 0;
+  const cudaError_t e = current_device(&dev, &sms);
+  if (e != cudaSuccess) return e;
+  EvictParams p;
+  p.c = c;
+  p.Hkv = s.Hkv;
+  p.capacity = s.capacity;
+  p.row16 = s.D / 8;
+  p.row16_log2 = -1;
+  for (int i = 0; i < 8; ++i)
+    if (p.row16 == 1 << i) p.row16_log2 = i;
+  p.moves = reinterpret_cast<int2*>(ws + cache_workspace(s, sms).moves);
+  const int heads = c.B * s.Hkv;
+  // (n - budget entries go, budget stay: no more moves than the fewer of them)
+  p.most_moves = max(0, min(c.budget, s.capacity - c.budget));
+  p.counts = p.most_moves > kFewMoves ? reinterpret_cast<int32_t*>(ws + cache_workspace(s, sms).counts) : nullptr;
+  // Clusters where four CTAs would find an SM each per head, and 8192 entries:
+  // us a call with 1 / 2 / 4 / 8 CTAs of 1024 threads: 1 head of 40000 entries
+  // 72 / 40 / 23.6 / 22.8, 16 heads of 20000 58 / 46 / 43 / 57; beyond, the adding up
+  // of histograms costs more than it saves (64 heads of 10000 23.3 / 25.5 / 35 / 79).
+  // Threads by what fits the SMs in one wave, no more than the entries need: 512 /
+  // 1024 threads: 4 heads of 1029 entries 6.0 / 7.5, 256 heads of 2056 9.3 / 16.5,
+  // 128 heads of 16384 88 / 75; 256 / 512: 1024 heads of 2000 23 / 32.
+  int cluster = 1;
+  while (cluster < kEvMaxCluster && 4 * cluster * heads <= sms && s.capacity >= 8192 * cluster) cluster *= 2;
+  int nt = heads * cluster > 2 * sms ? 256 : heads * cluster > sms || s.capacity <= 4096 * cluster ? 512 : 1024;
+  const cudaError_t r = nt == 1024 ? launch_evict_t<1024>(p, dev, cluster, stream)
+                        : nt == 512 ? launch_evict_t<512>(p, dev, cluster, stream)
+                                    : launch_evict_t<256>(p, dev, cluster, stream);
+  if (r != cudaSuccess || !p.counts) return r;
+  const int64_t blocks = (int64_t)heads * ceil_div(p.most_moves, kMoveBlock);
+  return launch_pdl(move_kernel, dim3((unsigned)blocks), dim3(kMoveThreads), 0, stream, p);
 }
 
 }  // namespace sp
