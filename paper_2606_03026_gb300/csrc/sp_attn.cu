@@ -15,9 +15,9 @@
 // (which only the device knows); a CTA's run of tiles within a unit is a
 // segment, which leaves its sum over V, its maximum and its sums of
 // exponentials in a slot of the workspace.  Per CTA (192 threads):
-//   warp 4      TMA: the query rows of a segment (a box of G heads x T tokens,
-//               for the prefix x as many sequences as 128 rows hold), K and V
-//               tiles into a ring.
+//   warp 4      one thread issues copies (TMA): the query rows of a segment (a box of G heads x T tokens,
+//               for the prefix x as many sequences as 128 rows hold), K tiles and V
+//               tiles into rings, each as soon as its place is free.
 //   warp 5      one thread issues S = Q K^T one tile ahead of O += P V (tcgen05,
 //               M = 128, P from tensor memory, V as an N-major operand).
 //   warps 0-3   the softmax, thread = row = tensor-memory lane: per tile they
@@ -48,6 +48,8 @@
 #include <cudaTypedefs.h>
 
 #include <math.h>
+#include <stdio.h>
+#include <stdlib.h>
 
 #include "sp_cache.h"
 #include "sp_ptx.cuh"
@@ -79,6 +81,10 @@ struct Rows {
   int32_t prefix_copies, own_copies;       // of the rows in the MMA's 128
 };
 
+struct Costs {
+  int32_t prefix_start, prefix_tile, own_start, own_tile;
+};
+
 struct AttnMaps {
   CUtensorMap pq, pk, pv, q, k, v;         // of the prefix units, of the own units
 };
@@ -87,10 +93,12 @@ struct AttnParams {
   sp_attend c;
   int32_t Hq, Hkv, G, D, capacity, R;      // R = T G: query rows of a sequence and K/V head
   Rows rows;
+  Costs costs;
   int32_t nt_prefix, nt_cap;               // tiles of the prefix, of the capacity
+  bool whole_rows;          // D is DK = 128: a tile of K or V is one copy
   float c2;                 // scale * log2 e
   int* err;
-  int32_t* sched;           // [B + 1]: own tiles before each sequence; [B] all of them
+  int32_t* sched;           // [B + 1]: cost of the own units before each sequence; [B] of all
   float4* p_ml;             // prefix slots: [slot][128] reference, sum, sum of the rounded
   float* p_o;               //               [slot][128][DK]
   float4* o_ml;             // own slots: [slot][own_rows own_copies], the same [DK]
@@ -106,31 +114,29 @@ __device__ __forceinline__ int used(const AttnParams& p, int b) {
 // Own entries of a sequence that every query token sees.
 __device__ __forceinline__ int seen_by_all(const AttnParams& p, int b) { return max(0, used(p, b) - (p.c.T - 1)); }
 
-// Costs of a tile.
-constexpr int kCostPrefix = 1, kCostOwn = 1, kCostMost = 1;
-
+// The line is measured in cost: a unit costs `start` and then each of its tiles.
 struct Line {
-  int prefix;               // tiles of the prefix units
-  int64_t cost;             // of all tiles
-  int ctas;                 // that have any
-  // CTA c has tiles first(c) .. first(c + 1); every one of them has at least one
-  __device__ __forceinline__ int64_t first(int c) const {
-    const int64_t x = c * cost / ctas, px = (int64_t)prefix * kCostPrefix;
-    return x < px ? x / kCostPrefix : prefix + (x - px) / kCostOwn;
-  }
-  // the CTA of a tile
-  __device__ __forceinline__ int cta(int64_t tile) const {
-    const int64_t end = tile < prefix ? (tile + 1) * kCostPrefix
-                                      : (int64_t)prefix * kCostPrefix + (tile + 1 - prefix) * kCostOwn;
-    return (int)((end * ctas - 1) / cost);
-  }
+  int64_t prefix, all;      // cost of the prefix units; of all
+  int32_t prefix_unit;      // of one
+  int ctas;                 // that share it
+  // CTA c has the tiles that end past first(c), up to first(c + 1)
+  __device__ __forceinline__ int64_t first(int c) const { return c * all / ctas; }
+  __device__ __forceinline__ int cta(int64_t tile_end) const { return (int)((tile_end * ctas - 1) / all); }
 };
-__device__ __forceinline__ Line line_of(const AttnParams& p, int own_tiles, int grid) {
+__device__ __forceinline__ Line line_of(const AttnParams& p, int own_cost, int grid) {
+  const Costs& k = p.costs;
   Line l;
-  l.prefix = p.Hkv * p.rows.prefix_units * p.nt_prefix;
-  l.cost = (int64_t)l.prefix * kCostPrefix + (int64_t)own_tiles * kCostOwn;
-  l.ctas = l.cost == 0 ? 0 : (int)min((int64_t)grid, max((int64_t)1, l.cost / kCostMost));
+  l.prefix_unit = k.prefix_start + p.nt_prefix * k.prefix_tile;
+  l.prefix = p.nt_prefix == 0 ? 0 : (int64_t)p.Hkv * p.rows.prefix_units * l.prefix_unit;
+  l.all = l.prefix + own_cost;
+  // (as much for every CTA as a tile costs at most: a unit's tiles are of
+  // CTAs without a gap)
+  l.ctas = (int)min((int64_t)grid, max((int64_t)1, l.all / max(k.prefix_tile, k.own_tile)));
   return l;
+}
+__device__ __forceinline__ int own_cost(const AttnParams& p, int b) {
+  const int nt = ceil_div(seen_by_all(p, b), kTile);
+  return nt == 0 ? 0 : p.Hkv * p.rows.own_units * (p.costs.own_start + nt * p.costs.own_tile);
 }
 
 struct Segment {
@@ -139,18 +145,24 @@ struct Segment {
   int j0, count;            // tiles
   int seen;                 // entries of the unit
   int rows, copies;
-  int64_t slot;
+  int64_t slot, next;       // next: where the following unit begins on the line
 };
-// The segment at tile x of a CTA whose tiles end at `end`.
+// The segment at point x of a CTA whose tiles end at `end`; of no tiles where
+// the first one past x ends past `end`.
 __device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l, const int* off, int64_t x,
                                               int64_t end, int cta) {
   const Rows& r = p.rows;
   Segment s;
   s.prefix = x < l.prefix;
+  int nt, start, tile;
+  int64_t at;                              // where the unit begins
   if (s.prefix) {
-    const int u = (int)x / p.nt_prefix;
-    s.j0 = (int)x - u * p.nt_prefix;
-    s.count = (int)min((int64_t)(p.nt_prefix - s.j0), end - x);
+    const int u = (int)(x / l.prefix_unit);
+    at = (int64_t)u * l.prefix_unit;
+    s.next = at + l.prefix_unit;
+    nt = p.nt_prefix;
+    start = p.costs.prefix_start;
+    tile = p.costs.prefix_tile;
     s.h = u / r.prefix_units;
     const int i = u - s.h * r.prefix_units;
     s.b = i / r.per_seq * r.seqs;
@@ -166,16 +178,22 @@ __device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l
       if (off[mid] <= y) lo = mid; else hi = mid;
     }
     s.b = lo;
-    const int nt = (off[lo + 1] - off[lo]) / (p.Hkv * r.own_units);
-    const int u = (y - off[lo]) / nt;
-    s.j0 = y - off[lo] - u * nt;
-    s.count = (int)min((int64_t)(nt - s.j0), end - x);
+    const int unit = (off[lo + 1] - off[lo]) / (p.Hkv * r.own_units);
+    const int u = (y - off[lo]) / unit;
+    at = l.prefix + off[lo] + u * unit;
+    s.next = at + unit;
+    start = p.costs.own_start;
+    tile = p.costs.own_tile;
+    s.seen = seen_by_all(p, lo);
+    nt = ceil_div(s.seen, kTile);
     s.h = u / r.own_units;
     s.m = u - s.h * r.own_units;
-    s.seen = seen_by_all(p, lo);
     s.copies = r.own_copies;
     s.slot = cta + (int64_t)lo * p.Hkv * r.own_units + u;
   }
+  // tile j ends at `at + start + (j + 1) tile`
+  s.j0 = max(0, (int)(x - at) - start) / tile;
+  s.count = min(nt, (int)max((int64_t)0, min(end, s.next) - at - start) / tile) - s.j0;
   s.rows = r.head_tiles > 1 ? min(r.heads, p.G - s.m % r.head_tiles * r.heads)
                             : min(r.tokens, p.c.T - s.m * r.tokens) * p.G;
   if (s.prefix) s.rows *= min(r.seqs, p.c.B - s.b);
@@ -235,8 +253,14 @@ __device__ __forceinline__ uint64_t n_major_desc(const void* p) {
   return d | (uint64_t)(kBlock >> 4) << 16;
 }
 
+// Bounded wait, inline: a call would cost the softmax's loop its registers.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
-  return mbar_try_wait(bar, parity) || mbar_wait(bar, parity);
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  do {
+    if (mbar_try_wait(bar, parity)) return true;
+  } while (clock64() - t0 < kWaitLimitCycles);
+  return false;
 }
 
 // What a softmax thread keeps of its row.
@@ -311,32 +335,47 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
   }
   f32x2 sum[2] = {}, rsum[2] = {};
   const f32x2 c2 = pair(p.c2, p.c2), base = pair(-r.ref, -r.ref);
-  uint32_t pk[NC / 2];
 #pragma unroll
-  for (int i = 0; i < NC / 2; ++i) {
-    const float2 x = halves(
-        fma2(pair(__uint_as_float(v[2 * i / NL][2 * i % NL]), __uint_as_float(v[2 * i / NL][2 * i % NL + 1])), c2, base));
-    const float2 y = make_float2(ex2(x.x), ex2(x.y));
-    pk[i] = pack2<BF16>(y.x, y.y);
-    const float2 q = unpack2<BF16>(pk[i]);
-    sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
-    rsum[i % 2] = add2(rsum[i % 2], pair(q.x, q.y));
+  for (int g = 0; g < NC / NL; ++g) {
+    uint32_t pk[NL / 2];
+#pragma unroll
+    for (int i = 0; i < NL / 2; ++i) {
+      const float2 x = halves(fma2(pair(__uint_as_float(v[g][2 * i]), __uint_as_float(v[g][2 * i + 1])), c2, base));
+      const float2 y = make_float2(ex2(x.x), ex2(x.y));
+      pk[i] = pack2<BF16>(y.x, y.y);
+      const float2 q = unpack2<BF16>(pk[i]);
+      sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
+      rsum[i % 2] = add2(rsum[i % 2], pair(q.x, q.y));
+    }
+    if constexpr (NC == kTile) {
+      tmem_st_issue<NL / 2>(s_buf + g * (NL / 2), pk);
+    } else {                               // the other copies' entries: 0
+      const uint32_t zero[NL / 2] = {};
+#pragma unroll
+      for (int i = 0; i < kTile / NC; ++i) {
+        if (i * NC == c0) tmem_st_issue<NL / 2>(s_buf + i * (NL / 2), pk);
+        else tmem_st_issue<NL / 2>(s_buf + i * (NL / 2), zero);
+      }
+    }
   }
   const float2 ls = halves(add2(sum[0], sum[1])), lr = halves(add2(rsum[0], rsum[1]));
   r.l += ls.x + ls.y;
   r.rl += lr.x + lr.y;
-  if constexpr (NC == kTile) {
-    tmem_st_issue<NC / 2>(s_buf, pk);
-  } else {                                 // the other copies' entries: 0
-    const uint32_t zero[NC / 2] = {};
-#pragma unroll
-    for (int i = 0; i < kTile / NC; ++i) {
-      if (i * NC == c0) tmem_st_issue<NC / 2>(s_buf + i * (NC / 2), pk);
-      else tmem_st_issue<NC / 2>(s_buf + i * (NC / 2), zero);
-    }
-  }
   tmem_st_wait();
   return true;
+}
+
+// One tile of entries into shared memory, 64 elements of all of them after 64
+// elements (`block` bytes on): in one copy where rows are made of whole blocks.
+template <int DK>
+__device__ __forceinline__ void load_tile(uint8_t* to, int block, const CUtensorMap* map, uint64_t* full, bool whole, int entry,
+                                          int head, int batch) {
+  if (DK == 64 || !whole) {
+#pragma unroll
+    for (int i = 0; i < DK / 64; ++i) tma_load_4d(to + i * block, map, full, 64 * i, entry, head, batch);
+  } else {
+    tma_load_5d(to, map, full, 0, entry, 0, head, batch);
+  }
 }
 
 template <int DK, bool BF16>
@@ -390,12 +429,11 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   pdl_launch_dependents();
   pdl_wait();
 
-  // own tiles before each sequence: every CTA adds them up for itself
+  // the own units before each sequence: every CTA adds their costs up for itself
   {
     const int per = ceil_div(p.c.B, kAttThreads), b0 = threadIdx.x * per, b1 = min(b0 + per, p.c.B);
-    const int units = p.Hkv * p.rows.own_units;
     int sum = 0;
-    for (int b = b0; b < b1; ++b) sum += ceil_div(seen_by_all(p, b), kTile) * units;
+    for (int b = b0; b < b1; ++b) sum += own_cost(p, b);
     int incl = sum;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -411,7 +449,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     for (int b = b0; b < b1; ++b) {
       s_off[b] = at;
       if (blockIdx.x == 0) p.sched[b] = at;
-      at += ceil_div(seen_by_all(p, b), kTile) * units;
+      at += own_cost(p, b);
     }
     if (b0 < p.c.B && b1 == p.c.B) {
       s_off[p.c.B] = at;
@@ -427,44 +465,69 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   if (warp == 4) {
     // ------------------------------ TMA -----------------------------------------
     if (lane == 0) {
-      int it = 0, seg = 0;
+      // where the keys and where the values are: a tile of a segment
+      struct Cursor {
+        Segment s;
+        int64_t x;
+        int j, it;
+      };
+      Cursor k, v;
+      const auto enter = [&](Cursor& c, int64_t x) {
+        c.x = x;
+        c.j = 0;
+        c.s.count = 0;
+        if (x < x1) c.s = segment_at(p, line, s_off, x, x1, cta);
+      };
+      enter(k, x0);
+      enter(v, x0);
+      k.it = v.it = 0;
+      int seg = 0;                         // segments whose query rows are on their way
+      bool rows = k.s.count > 0;           // those of the keys' segment are to come
       bool ok = true;
-      for (int64_t x = x0; x < x1 && ok; ++seg) {
-        const Segment s = segment_at(p, line, s_off, x, x1, cta);
-        const CUtensorMap* mk = s.prefix ? &maps.pk : &maps.k;
-        const CUtensorMap* mv = s.prefix ? &maps.pv : &maps.v;
-        const int kb = s.prefix ? 0 : s.b;
-        for (int j = 0; j < s.count; ++j, ++it) {
-          const int st = it % NS;
-          const uint32_t ph = (it / NS) & 1;
-          ok = mbar_wait_sleep(&k_empty[st], ph ^ 1u) && !*s_abort;
-          if (!ok) break;
-          mbar_arrive_expect_tx(&k_full[st], kBytes);
-          for (int i = 0; i < DK / 64; ++i)
-            tma_load_4d(sK + st * kBytes + i * kBlock, mk, &k_full[st], 64 * i, (s.j0 + j) * kTile, s.h, kb);
-          if (j == 0) {
-            ok = mbar_wait_sleep(q_empty, (seg & 1) ^ 1u) && !*s_abort;
-            if (ok) {
-              const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows;
-              const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
-              const int token = s.m / p.rows.head_tiles * p.rows.tokens;
-              mbar_arrive_expect_tx(q_full, DK / 64 * 128 * box * s.copies);
-              for (int c = 0; c < s.copies; ++c)
-                for (int i = 0; i < DK / 64; ++i)
-                  tma_load_4d(sQ + i * kQBlock + c * (kQBlock / s.copies), s.prefix ? &maps.pq : &maps.q, q_full, 64 * i,
-                              head, token, s.b);
-            }
-          }
-          ok = ok && mbar_wait_sleep(&v_empty[st], ph ^ 1u) && !*s_abort;
-          if (!ok) {
-            wait(&k_full[st], ph);         // no copy is in flight at the end
-            break;
-          }
-          mbar_arrive_expect_tx(&v_full[st], kBytes);
-          for (int i = 0; i < DK / 64; ++i)
-            tma_load_4d(sV + st * kBytes + i * kBlock, mv, &v_full[st], 64 * i, (s.j0 + j) * kTile, s.h, kb);
+      const auto issue = [&](Cursor& c, uint8_t* ring, uint64_t* full, uint64_t* empty, const CUtensorMap* prefix,
+                             const CUtensorMap* own) {
+        const int st = c.it % NS;
+        if (c.s.count <= 0 || !mbar_test(&empty[st], (c.it / NS & 1) ^ 1)) return false;
+        mbar_arrive_expect_tx(&full[st], kBytes);
+        load_tile<DK>(ring + st * kBytes, kBlock, c.s.prefix ? prefix : own, &full[st], p.whole_rows,
+                      (c.s.j0 + c.j) * kTile, c.s.h, c.s.prefix ? 0 : c.s.b);
+        ++c.it;
+        ++c.j;
+        return true;
+      };
+      long long since = clock64();
+      while (k.s.count > 0 || v.s.count > 0) {
+        bool moved = false;
+        // (a segment's keys may go ahead of its query rows, the next one's not)
+        if (k.j < k.s.count) moved = issue(k, sK, k_full, k_empty, &maps.pk, &maps.k);
+        if (rows && mbar_test(q_empty, (seg & 1) ^ 1)) {
+          const Segment& s = k.s;
+          const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows;
+          const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
+          const int token = s.m / p.rows.head_tiles * p.rows.tokens;
+          mbar_arrive_expect_tx(q_full, DK / 64 * 128 * box * s.copies);
+          for (int c = 0; c < s.copies; ++c)
+            for (int i = 0; i < DK / 64; ++i)
+              tma_load_4d(sQ + i * kQBlock + c * (kQBlock / s.copies), s.prefix ? &maps.pq : &maps.q, q_full, 64 * i, head,
+                          token, s.b);
+          ++seg;
+          rows = false;
+          moved = true;
         }
-        x += s.count;
+        if (k.j == k.s.count && k.s.count > 0 && !rows) {
+          enter(k, k.s.next);
+          rows = k.s.count > 0;
+        }
+        if (issue(v, sV, v_full, v_empty, &maps.pv, &maps.v)) {
+          moved = true;
+          if (v.j == v.s.count) enter(v, v.s.next);
+        }
+        if (moved) {
+          since = clock64();
+        } else if (*s_abort || clock64() - since > kWaitLimitCycles) {
+          ok = false;
+          break;
+        }
       }
       if (!ok) {
         *s_abort = 1;
@@ -472,10 +535,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (seg > 0) wait(q_full, (seg - 1) & 1);
       }
       // the last copies have landed
-      for (int i = max(0, it - NS); i < it; ++i) {
-        wait(&k_full[i % NS], (i / NS) & 1);
-        wait(&v_full[i % NS], (i / NS) & 1);
-      }
+      for (int i = max(0, k.it - NS); i < k.it; ++i) wait(&k_full[i % NS], i / NS & 1);
+      for (int i = max(0, v.it - NS); i < v.it; ++i) wait(&v_full[i % NS], i / NS & 1);
     }
   } else if (warp == 5) {
     // ------------------------------ MMA -----------------------------------------
@@ -499,6 +560,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       };
       for (int64_t x = x0; x < x1 && ok; ++seg) {
         const Segment s = segment_at(p, line, s_off, x, x1, cta);
+        if (s.count <= 0) break;
         // (the buffer of tile i + 1 is that of tile i - 1, whose product with V,
         // issued before, reads the probabilities there first)
         ok = wait(q_full, seg & 1) && scores(it, s.count == 1);
@@ -516,7 +578,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
           mma_commit(&v_empty[st]);
         }
         if (ok) mma_commit(o_full);
-        x += s.count;
+        x = s.next;
       }
       if (!ok) {
         *s_abort = 1;
@@ -532,6 +594,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     bool ok = true;
     for (int64_t x = x0; x < x1 && ok; ++seg) {
       const Segment s = segment_at(p, line, s_off, x, x1, cta);
+      if (s.count <= 0) break;
       const int per_copy = kRows / s.copies, copy = threadIdx.x / per_copy, row = threadIdx.x % per_copy;
       const bool work = warp * 32 % per_copy < s.rows, mine = row < s.rows;
       const int c0 = copy * (kTile / s.copies);
@@ -596,7 +659,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(o_empty);
-      x += s.count;
+      x = s.next;
     }
     if (!ok) {
       *s_abort = 1;
@@ -611,27 +674,19 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
 
 // ---- merging ------------------------------------------------------------------
 // A lane has DK / 32 elements of a row: lane * DK / 32 ...
-template <int DK, bool BF16>
-__device__ __forceinline__ void load_row(const void* base, int64_t at, int D, int lane, float (&x)[DK / 32]) {
-  constexpr int E = DK / 32;
-  const uint16_t* p = static_cast<const uint16_t*>(base) + at + lane * E;
-  uint32_t w[E / 2];
+template <int DK>
+__device__ __forceinline__ void load_raw(const void* base, int64_t at, int D, int lane, uint32_t (&w)[DK / 64]) {
+  const uint16_t* p = static_cast<const uint16_t*>(base) + at + lane * (DK / 32);
 #pragma unroll
-  for (int i = 0; i < E / 2; ++i) w[i] = 0u;
-  if (lane * E < D) {                      // (D is a multiple of 8)
-    if constexpr (E == 4) {
+  for (int i = 0; i < DK / 64; ++i) w[i] = 0u;
+  if (lane * (DK / 32) < D) {              // (D is a multiple of 8)
+    if constexpr (DK == 128) {
       const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
       w[0] = u.x;
       w[1] = u.y;
     } else {
       w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
     }
-  }
-#pragma unroll
-  for (int i = 0; i < E / 2; ++i) {
-    const float2 f = unpack2<BF16>(w[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
   }
 }
 
@@ -650,13 +705,13 @@ template <int E> struct Part {
   }
 };
 
-constexpr int kCombBatch = 8;              // results that a warp has on their way
+constexpr int kLast = 4;                   // last entries that a warp has on their way
 
 // WPR warps of a CTA of W per query row, each with its share of the row's
 // partial results and of its last entries.
 template <int DK, bool BF16, int W, int WPR>
-__global__ void __launch_bounds__(32 * W) combine_kernel(const __grid_constant__ AttnParams p, int grid) {
-  constexpr int E = DK / 32;
+__global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 7) combine_kernel(const __grid_constant__ AttnParams p, int grid) {
+  constexpr int E = DK / 32, kCombBatch = WPR > 1 ? 8 : 4;                // results on their way
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
   pdl_launch_dependents();
   pdl_wait();
@@ -685,25 +740,43 @@ __global__ void __launch_bounds__(32 * W) combine_kernel(const __grid_constant__
     int64_t at_p = 0, at_o = 0;
     if (p.nt_prefix > 0) {
       const int u = h * rw.prefix_units + b / rw.seqs * rw.per_seq + m;
-      const int64_t t0 = (int64_t)u * p.nt_prefix;
-      const int c0 = line.cta(t0), c1 = line.cta(t0 + p.nt_prefix - 1);
+      const int64_t end = (int64_t)(u + 1) * line.prefix_unit;
+      const int c0 = line.cta(end - (int64_t)(p.nt_prefix - 1) * p.costs.prefix_tile), c1 = line.cta(end);
       np = (c1 - c0 + 1) * rw.prefix_copies;
       at_p = (int64_t)(c0 + u) * kRows + b % rw.seqs * p.R + ro;
     }
-    const int own0 = __ldg(p.sched + b), nt = (__ldg(p.sched + b + 1) - own0) / (p.Hkv * rw.own_units);
-    if (nt > 0) {
+    const int own0 = __ldg(p.sched + b), unit = (__ldg(p.sched + b + 1) - own0) / (p.Hkv * rw.own_units);
+    if (unit > 0) {
       const int u = h * rw.own_units + m;
-      const int64_t t0 = line.prefix + own0 + (int64_t)u * nt;
-      const int c0 = line.cta(t0), c1 = line.cta(t0 + nt - 1);
+      const int64_t end = line.prefix + own0 + (int64_t)(u + 1) * unit;
+      const int c0 = line.cta(end - unit + p.costs.own_start + p.costs.own_tile), c1 = line.cta(end);
       no = (c1 - c0 + 1) * rw.own_copies;
       at_o = (c0 + (int64_t)b * p.Hkv * rw.own_units + u) * rw.own_copies * rw.own_rows + ro;
     }
+    // the last T - 1 own entries, of which this row sees the first few: j_first
+    // on, this warp every WPR-th, the first kLast on their way from here
+    const int n = p.c.T > 1 ? used(p, b) : 0, far = n - (p.c.T - 1 - t), j_first = max(0, n - (p.c.T - 1)) + sub;
+    uint32_t qw[DK / 64], kw[kLast][DK / 64], vw[kLast][DK / 64];
+    const auto fetch = [&](int j0) {
+#pragma unroll
+      for (int i = 0; i < kLast; ++i) {
+        const int64_t j = j0 + i * WPR;
+        if (j < far) {
+          load_raw<DK>(p.c.k, b * p.c.k_batch + j * p.c.k_entry + h * p.c.k_head, p.D, lane, kw[i]);
+          load_raw<DK>(p.c.v, b * p.c.v_batch + j * p.c.v_entry + h * p.c.v_head, p.D, lane, vw[i]);
+        }
+      }
+    };
+    if (j_first < n) {
+      load_raw<DK>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, lane, qw);
+      fetch(j_first);
+    }
     const int share = (np + no + WPR - 1) / WPR, end = min((sub + 1) * share, np + no);
     for (int s0 = sub * share; s0 < end; s0 += 32) {
-      const int s = s0 + lane, n = min(32, end - s0);
+      const int s = s0 + lane, some = min(32, end - s0);
       float4 ml = make_float4(0.f, 0.f, 0.f, 0.f);
       const float* src = p.p_o;
-      if (lane < n) {
+      if (lane < some) {
         const bool own = s >= np;
         const int c = s / rw.prefix_copies;
         const int64_t at = own ? at_o + (int64_t)(s - np) * rw.own_rows
@@ -726,13 +799,13 @@ __global__ void __launch_bounds__(32 * W) combine_kernel(const __grid_constant__
       }
       a.l += l;
       a.r += r;
-      for (int i0 = 0; i0 < n; i0 += kCombBatch) {
+      for (int i0 = 0; i0 < some; i0 += kCombBatch) {
         float o[kCombBatch][E];
 #pragma unroll
         for (int i = 0; i < kCombBatch; ++i) {
           const float* from =
               reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), i0 + i));
-          if (i0 + i < n) {
+          if (i0 + i < some) {
             if constexpr (E == 4) {
               const float4 f = __ldcg(reinterpret_cast<const float4*>(from) + lane);
               o[i][0] = f.x, o[i][1] = f.y, o[i][2] = f.z, o[i][3] = f.w;
@@ -745,27 +818,27 @@ __global__ void __launch_bounds__(32 * W) combine_kernel(const __grid_constant__
 #pragma unroll
         for (int i = 0; i < kCombBatch; ++i) {
           const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
-          if (i0 + i < n && wi != 0.f) {
+          if (i0 + i < some && wi != 0.f) {
 #pragma unroll
             for (int e = 0; e < E; ++e) a.o[e] = fmaf(wi, o[i][e], a.o[e]);
           }
         }
       }
     }
-    // the last T - 1 own entries, of which this row sees the first few
-    if (p.c.T > 1) {
-      const int n = used(p, b), far = n - (p.c.T - 1 - t);
-      float q[E];
-      load_row<DK, BF16>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, lane, q);
-      for (int j = max(0, n - (p.c.T - 1)) + sub; j < n; j += WPR) {
+    for (int j0 = j_first; j0 < n; j0 += kLast * WPR) {
+      if (j0 > j_first) fetch(j0);
+#pragma unroll
+      for (int i = 0; i < kLast; ++i) {
+        const int j = j0 + i * WPR;
+        if (j >= n) break;
         float s = -INFINITY;
         if (j < far) {
-          float k[E], v[E];
-          load_row<DK, BF16>(p.c.k, b * p.c.k_batch + j * p.c.k_entry + h * p.c.k_head, p.D, lane, k);
-          load_row<DK, BF16>(p.c.v, b * p.c.v_batch + j * p.c.v_entry + h * p.c.v_head, p.D, lane, v);
           s = 0.f;
 #pragma unroll
-          for (int e = 0; e < E; ++e) s = fmaf(q[e], k[e], s);
+          for (int e = 0; e < E / 2; ++e) {
+            const float2 x = unpack2<BF16>(qw[e]), y = unpack2<BF16>(kw[i][e]);
+            s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
+          }
 #pragma unroll
           for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
           const float x = s * p.c2;
@@ -774,7 +847,11 @@ __global__ void __launch_bounds__(32 * W) combine_kernel(const __grid_constant__
           a.l += w;
           a.r += w;
 #pragma unroll
-          for (int e = 0; e < E; ++e) a.o[e] = fmaf(w, v[e], a.o[e]);
+          for (int e = 0; e < E / 2; ++e) {
+            const float2 v = unpack2<BF16>(vw[i][e]);
+            a.o[2 * e] = fmaf(w, v.x, a.o[2 * e]);
+            a.o[2 * e + 1] = fmaf(w, v.y, a.o[2 * e + 1]);
+          }
           if (a.m == -INFINITY && w != 0.f) a.m = 0.f;      // (a NaN score)
         }
         if (p.scores && lane == 0)
@@ -870,6 +947,23 @@ bool encode(CUtensorMap* map, bool bf16, const void* base, int D, const int64_t 
   }
   return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
              const_cast<void*>(base), dims, bytes, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The same for a cache [batch][entry][head][D], in boxes of a tile of entries;
+// with rows of two whole blocks of 64 elements the block is a dimension (after
+// the entries), and a box has both.
+bool encode_kv(CUtensorMap* map, bool bf16, const void* base, int D, const int64_t (&n)[3], const int64_t (&stride)[3]) {
+  if (D != 128) return encode(map, bf16, base, D, n, stride, {kTile, 1, 1});
+  const auto enc = get_encode();
+  if (!enc) return false;
+  const auto bytes = [&](int i) { return (cuuint64_t)(n[i] > 1 ? 2 * stride[i] : 2 * (int64_t)D); };
+  const cuuint64_t dims[5] = {64, (cuuint64_t)n[0], 2, (cuuint64_t)n[1], (cuuint64_t)n[2]};
+  const cuuint64_t strides[4] = {bytes(0), 128, bytes(1), bytes(2)};
+  const cuuint32_t box[5] = {64, kTile, 2, 1, 1}, ones[5] = {1, 1, 1, 1, 1};
+  return enc(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5,
+             const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -974,9 +1068,12 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.capacity = s.capacity;
   p.R = c.T * p.G;
   p.rows = rows_of(c.B, c.T, p.G);
+  p.costs = Costs{8, 6, 8, 7};
+  if (const char* f = getenv("AT_COST")) sscanf(f, "%d,%d,%d,%d", &p.costs.prefix_start, &p.costs.prefix_tile, &p.costs.own_start, &p.costs.own_tile);
   p.nt_prefix = ceil_div(c.prefix_len, kTile);
   p.nt_cap = ceil_div(s.capacity, kTile);
   p.c2 = c.scale * kLog2e;
+  p.whole_rows = s.D == 128;
   p.err = err;
   const int grid = 2 * sms;
   const Parts w = parts_of(s, c.B, c.T, grid);
@@ -994,16 +1091,16 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   const int64_t nk[3] = {s.capacity, s.Hkv, c.B};
   if (!encode(&maps.q, bf16, c.q, s.D, nq, sq, {r.heads, r.tokens, 1}) ||
       !encode(&maps.pq, bf16, c.q, s.D, nq, sq, {r.heads, r.tokens, r.seqs}) ||
-      !encode(&maps.k, bf16, c.k, s.D, nk, {c.k_entry, c.k_head, c.k_batch}, {kTile, 1, 1}) ||
-      !encode(&maps.v, bf16, c.v, s.D, nk, {c.v_entry, c.v_head, c.v_batch}, {kTile, 1, 1}))
+      !encode_kv(&maps.k, bf16, c.k, s.D, nk, {c.k_entry, c.k_head, c.k_batch}) ||
+      !encode_kv(&maps.v, bf16, c.v, s.D, nk, {c.v_entry, c.v_head, c.v_batch}))
     return cudaErrorInvalidValue;
   if (c.prefix_len == 0) {
     maps.pk = maps.k;                      // (read by nothing)
     maps.pv = maps.v;
   } else {
     const int64_t np[3] = {c.prefix_len, s.Hkv, 1};
-    if (!encode(&maps.pk, bf16, c.prefix_k, s.D, np, {c.pk_entry, c.pk_head, 0}, {kTile, 1, 1}) ||
-        !encode(&maps.pv, bf16, c.prefix_v, s.D, np, {c.pv_entry, c.pv_head, 0}, {kTile, 1, 1}))
+    if (!encode_kv(&maps.pk, bf16, c.prefix_k, s.D, np, {c.pk_entry, c.pk_head, 0}) ||
+        !encode_kv(&maps.pv, bf16, c.prefix_v, s.D, np, {c.pv_entry, c.pv_head, 0}))
       return cudaErrorInvalidValue;
   }
   if (s.D <= 64)
