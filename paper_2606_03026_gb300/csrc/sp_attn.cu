@@ -24,10 +24,6 @@
 //               read the 64 scores of their row, keep the running maximum and
 //               sums, and put the probabilities, rounded to the type, back over
 //               the scores.
-// A unit of at most 32 (64) rows has them four times (twice) in the MMA's 128,
-// and each copy's warps take a quarter (half) of a tile's entries, with
-// probabilities of 0 for the others: a tile's softmax takes a warp a quarter of
-// the time, and every copy is a partial result of its own.
 // Exponentials are powers of two of (s scale log2 e - reference).  The
 // reference follows the running maximum only when that has grown by more than
 // 2^kLag, so that O is rescaled seldom; half precision is offset by 2^10 so that
@@ -48,8 +44,6 @@
 #include <cudaTypedefs.h>
 
 #include <math.h>
-#include <stdio.h>
-#include <stdlib.h>
 
 #include "sp_cache.h"
 #include "sp_ptx.cuh"
@@ -60,13 +54,16 @@ namespace {
 constexpr int kTile = 64;                  // entries of a tile
 constexpr int kRows = 128;                 // rows of the MMA
 constexpr int kAttThreads = 192;
+constexpr int kGroups = kAttThreads;
 constexpr int kTmemCols = 256;             // S and P: 0 .. 63 and 64 .. 127, O: 128 .. 255
 constexpr uint32_t kTmemO = 128;
 constexpr int kQBlock = kRows * 128;       // 64 elements of 128 rows
 constexpr int kBlock = kTile * 128;        // 64 elements of a tile's entries
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-template <int DK> constexpr int kStages = 256 / DK;       // 64 KB of K and V
+// Tiles of K and of V on their way: what two CTAs of an SM have room for.
+template <int DK> constexpr int kStagesK = DK == 64 ? 5 : 3;
+template <int DK> constexpr int kStagesV = DK == 64 ? 5 : 2;
 template <int DK> constexpr int kQBytes = DK / 64 * kQBlock;
 template <int DK> constexpr int kTileBytes = DK / 64 * kBlock;
 
@@ -78,7 +75,6 @@ struct Rows {
   int32_t head_tiles, per_seq;             // tiles that share a token; tiles of a sequence
   int32_t prefix_units, own_units;         // per K/V head; per sequence and K/V head
   int32_t prefix_rows, own_rows;           // of a whole unit
-  int32_t prefix_copies, own_copies;       // of the rows in the MMA's 128
 };
 
 struct Costs {
@@ -98,10 +94,10 @@ struct AttnParams {
   bool whole_rows;          // D is DK = 128: a tile of K or V is one copy
   float c2;                 // scale * log2 e
   int* err;
-  int32_t* sched;           // [B + 1]: cost of the own units before each sequence; [B] of all
+  int2* unit_ctas;          // first and last CTA of each prefix unit, of each own unit that has tiles
   float4* p_ml;             // prefix slots: [slot][128] reference, sum, sum of the rounded
   float* p_o;               //               [slot][128][DK]
-  float4* o_ml;             // own slots: [slot][own_rows own_copies], the same [DK]
+  float4* o_ml;             // own slots: [slot][own_rows], the same [DK]
   float* o_o;
   float* scores;            // [B][Hkv][nt_cap][R][64], or null
   float* lse2;              // [B][Hkv][R], base 2; +infinity where a row sees nothing
@@ -121,7 +117,6 @@ struct Line {
   int ctas;                 // that share it
   // CTA c has the tiles that end past first(c), up to first(c + 1)
   __device__ __forceinline__ int64_t first(int c) const { return c * all / ctas; }
-  __device__ __forceinline__ int cta(int64_t tile_end) const { return (int)((tile_end * ctas - 1) / all); }
 };
 __device__ __forceinline__ Line line_of(const AttnParams& p, int own_cost, int grid) {
   const Costs& k = p.costs;
@@ -131,7 +126,8 @@ __device__ __forceinline__ Line line_of(const AttnParams& p, int own_cost, int g
   l.all = l.prefix + own_cost;
   // (as much for every CTA as a tile costs at most: a unit's tiles are of
   // CTAs without a gap)
-  l.ctas = (int)min((int64_t)grid, max((int64_t)1, l.all / max(k.prefix_tile, k.own_tile)));
+  const int most = max(k.prefix_tile, k.own_tile);
+  l.ctas = l.all >= (int64_t)grid * most ? grid : max(1, (int)l.all / most);
   return l;
 }
 __device__ __forceinline__ int own_cost(const AttnParams& p, int b) {
@@ -142,25 +138,26 @@ __device__ __forceinline__ int own_cost(const AttnParams& p, int b) {
 struct Segment {
   bool prefix;
   int b, h, m;              // first sequence, head, row tile of the sequence
-  int j0, count;            // tiles
+  int j0, count, nt;        // tiles, of nt that the unit has
   int seen;                 // entries of the unit
-  int rows, copies;
+  int rows;
   int64_t slot, next;       // next: where the following unit begins on the line
 };
-// The segment at point x of a CTA whose tiles end at `end`; of no tiles where
+// off: cost of the own units before each of the groups of sequences that
+// attend_kernel's threads add up.  The segment at point x of a CTA whose tiles end at `end`; of no tiles where
 // the first one past x ends past `end`.
 __device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l, const int* off, int64_t x,
                                               int64_t end, int cta) {
   const Rows& r = p.rows;
   Segment s;
   s.prefix = x < l.prefix;
-  int nt, start, tile;
+  int start, tile;
   int64_t at;                              // where the unit begins
   if (s.prefix) {
     const int u = (int)(x / l.prefix_unit);
     at = (int64_t)u * l.prefix_unit;
     s.next = at + l.prefix_unit;
-    nt = p.nt_prefix;
+    s.nt = p.nt_prefix;
     start = p.costs.prefix_start;
     tile = p.costs.prefix_tile;
     s.h = u / r.prefix_units;
@@ -168,32 +165,38 @@ __device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l
     s.b = i / r.per_seq * r.seqs;
     s.m = i % r.per_seq;
     s.seen = p.c.prefix_len;
-    s.copies = r.prefix_copies;
     s.slot = cta + u;
   } else {
     const int y = (int)(x - l.prefix);
-    int lo = 0, hi = p.c.B;                // off[lo] <= y < off[hi]
+    int lo = 0, hi = kGroups;              // off[lo] <= y < off[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (off[mid] <= y) lo = mid; else hi = mid;
     }
+    int before = off[lo], cost = off[lo + 1] - before;
+    const int per = ceil_div(p.c.B, kGroups);
+    lo *= per;
+    if (per > 1)
+      while (cost = own_cost(p, lo), before + cost <= y) {
+        before += cost;
+        ++lo;
+      }
     s.b = lo;
-    const int unit = (off[lo + 1] - off[lo]) / (p.Hkv * r.own_units);
-    const int u = (y - off[lo]) / unit;
-    at = l.prefix + off[lo] + u * unit;
+    const int unit = cost / (p.Hkv * r.own_units);
+    const int u = (y - before) / unit;
+    at = l.prefix + before + u * unit;
     s.next = at + unit;
     start = p.costs.own_start;
     tile = p.costs.own_tile;
     s.seen = seen_by_all(p, lo);
-    nt = ceil_div(s.seen, kTile);
+    s.nt = ceil_div(s.seen, kTile);
     s.h = u / r.own_units;
     s.m = u - s.h * r.own_units;
-    s.copies = r.own_copies;
     s.slot = cta + (int64_t)lo * p.Hkv * r.own_units + u;
   }
   // tile j ends at `at + start + (j + 1) tile`
   s.j0 = max(0, (int)(x - at) - start) / tile;
-  s.count = min(nt, (int)max((int64_t)0, min(end, s.next) - at - start) / tile) - s.j0;
+  s.count = min(s.nt, (int)max((int64_t)0, min(end, s.next) - at - start) / tile) - s.j0;
   s.rows = r.head_tiles > 1 ? min(r.heads, p.G - s.m % r.head_tiles * r.heads)
                             : min(r.tokens, p.c.T - s.m * r.tokens) * p.G;
   if (s.prefix) s.rows *= min(r.seqs, p.c.B - s.b);
@@ -268,45 +271,32 @@ struct RowState {
   float m, ref, l, rl;      // maximum that the reference follows, reference, sums
 };
 
-template <int NC> __device__ __forceinline__ void tmem_ld_issue(uint32_t at, uint32_t (&v)[NC]) {
-  if constexpr (NC == 16) tmem_ld16_issue(at, v);
-  else if constexpr (NC == 32) tmem_ld32_issue(at, v);
-}
-template <int NC> __device__ __forceinline__ void tmem_st_issue(uint32_t at, const uint32_t (&v)[NC]) {
-  if constexpr (NC == 8) tmem_st8_issue(at, v);
-  else if constexpr (NC == 16) tmem_st16_issue(at, v);
-  else tmem_st32_issue(at, v);
-}
-
-// One tile for a warp whose rows' copy has NC of the tile's entries, from entry
-// c0 on.  s_buf: this warp's lanes of the tile's scores.  pv: the barrier (and
-// its parity) that says the product before this tile's is complete.
-template <int DK, bool BF16, int NC>
-__device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, uint32_t s_buf, uint32_t o_buf, int c0,
-                                             int nv, bool first, uint64_t* pv, uint32_t pv_parity, float* scores) {
+// One tile: the row's scores at s_buf become its probabilities.  pv: the barrier
+// (and its parity) that says that the product before this tile's is complete.
+template <int DK, bool BF16>
+__device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, uint32_t s_buf, uint32_t o_buf, int nv,
+                                             bool first, uint64_t* pv, uint32_t pv_parity, float* scores) {
   constexpr float kLag = BF16 ? 8.f : 4.f, kLift = BF16 ? 0.f : 10.f;
-  constexpr int NL = NC < 32 ? NC : 32;
-  uint32_t v[NC / NL][NL];
-#pragma unroll
-  for (int i = 0; i < NC / NL; ++i) tmem_ld_issue<NL>(s_buf + c0 + NL * i, v[i]);
+  uint32_t v[2][32];
+  tmem_ld32_issue(s_buf, v[0]);
+  tmem_ld32_issue(s_buf + 32, v[1]);
   tmem_ld_wait();
-#pragma unroll
-  for (int i = 0; i < NC / NL; ++i) reg_pin(v[i]);
+  reg_pin(v[0]);
+  reg_pin(v[1]);
   if (scores) {
 #pragma unroll
-    for (int i = 0; i < NC / 4; ++i)
-      reinterpret_cast<uint4*>(scores + c0)[i] =
-          make_uint4(v[4 * i / NL][4 * i % NL], v[4 * i / NL][4 * i % NL + 1], v[4 * i / NL][4 * i % NL + 2],
-                     v[4 * i / NL][4 * i % NL + 3]);
+    for (int i = 0; i < kTile / 4; ++i)
+      reinterpret_cast<uint4*>(scores)[i] =
+          make_uint4(v[i / 8][i % 8 * 4], v[i / 8][i % 8 * 4 + 1], v[i / 8][i % 8 * 4 + 2], v[i / 8][i % 8 * 4 + 3]);
   }
   if (nv < kTile) {
 #pragma unroll
-    for (int i = 0; i < NC; ++i)
-      if (c0 + i >= nv) v[i / NL][i % NL] = 0xff800000u;
+    for (int i = 0; i < kTile; ++i)
+      if (i >= nv) v[i / 32][i % 32] = 0xff800000u;
   }
   float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-  for (int i = 0; i < NC; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(v[i / NL][i % NL]));
+  for (int i = 0; i < kTile; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(v[i / 32][i % 32]));
   const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.c2;
   const bool grow = top > r.m + kLag;
   if (__any_sync(0xffffffffu, grow)) {
@@ -336,10 +326,10 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
   f32x2 sum[2] = {}, rsum[2] = {};
   const f32x2 c2 = pair(p.c2, p.c2), base = pair(-r.ref, -r.ref);
 #pragma unroll
-  for (int g = 0; g < NC / NL; ++g) {
-    uint32_t pk[NL / 2];
+  for (int g = 0; g < 2; ++g) {
+    uint32_t pk[16];
 #pragma unroll
-    for (int i = 0; i < NL / 2; ++i) {
+    for (int i = 0; i < 16; ++i) {
       const float2 x = halves(fma2(pair(__uint_as_float(v[g][2 * i]), __uint_as_float(v[g][2 * i + 1])), c2, base));
       const float2 y = make_float2(ex2(x.x), ex2(x.y));
       pk[i] = pack2<BF16>(y.x, y.y);
@@ -347,16 +337,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
       sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
       rsum[i % 2] = add2(rsum[i % 2], pair(q.x, q.y));
     }
-    if constexpr (NC == kTile) {
-      tmem_st_issue<NL / 2>(s_buf + g * (NL / 2), pk);
-    } else {                               // the other copies' entries: 0
-      const uint32_t zero[NL / 2] = {};
-#pragma unroll
-      for (int i = 0; i < kTile / NC; ++i) {
-        if (i * NC == c0) tmem_st_issue<NL / 2>(s_buf + i * (NL / 2), pk);
-        else tmem_st_issue<NL / 2>(s_buf + i * (NL / 2), zero);
-      }
-    }
+    tmem_st16_issue(s_buf + 16 * g, pk);
   }
   const float2 ls = halves(add2(sum[0], sum[1])), lr = halves(add2(rsum[0], rsum[1]));
   r.l += ls.x + ls.y;
@@ -381,29 +362,30 @@ __device__ __forceinline__ void load_tile(uint8_t* to, int block, const CUtensor
 template <int DK, bool BF16>
 __global__ void __launch_bounds__(kAttThreads, 2)
 attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnParams p) {
-  constexpr int NS = kStages<DK>, kBytes = kTileBytes<DK>;
+  constexpr int NK = kStagesK<DK>, NV = kStagesV<DK>, kBytes = kTileBytes<DK>;
   constexpr uint32_t kType = BF16 ? 1u << 7 | 1u << 10 : 0u;
   constexpr uint32_t kIdescS = 1u << 4 | kType | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
   constexpr uint32_t kIdescO = 1u << 4 | kType | 1u << 16 | (uint32_t)(DK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sQ = smem;
   uint8_t* sK = sQ + kQBytes<DK>;
-  uint8_t* sV = sK + NS * kBytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sV + NS * kBytes);
-  uint64_t *k_full = bars, *k_empty = bars + NS, *v_full = bars + 2 * NS, *v_empty = bars + 3 * NS;
-  uint64_t *s_full = bars + 4 * NS, *p_full = s_full + 2;  // [2]: by score buffer
+  uint8_t* sV = sK + NK * kBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sV + NV * kBytes);
+  uint64_t *k_full = bars, *k_empty = bars + NK, *v_full = bars + 2 * NK, *v_empty = v_full + NV;
+  uint64_t *s_full = v_empty + NV, *p_full = s_full + 2;   // [2]: by score buffer
   uint64_t *q_full = p_full + 2, *q_empty = q_full + 1, *o_full = q_full + 2, *o_empty = q_full + 3, *done = q_full + 4;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_sum = reinterpret_cast<int*>(s_tmem + 2);         // [8]
-  int* s_off = s_sum + 8;                                  // [B + 1]
+  int* s_off = s_sum + 8;                                  // [kGroups + 1]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NS; ++i) {
+    for (int i = 0; i < NK; ++i) {
       mbar_init(&k_full[i], 1);
       mbar_init(&k_empty[i], 1);
+    }
+    for (int i = 0; i < NV; ++i) {
       mbar_init(&v_full[i], 1);
       mbar_init(&v_empty[i], 1);
     }
@@ -431,7 +413,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
 
   // the own units before each sequence: every CTA adds their costs up for itself
   {
-    const int per = ceil_div(p.c.B, kAttThreads), b0 = threadIdx.x * per, b1 = min(b0 + per, p.c.B);
+    const int per = ceil_div(p.c.B, kGroups), b0 = threadIdx.x * per, b1 = min(b0 + per, p.c.B);
     int sum = 0;
     for (int b = b0; b < b1; ++b) sum += own_cost(p, b);
     int incl = sum;
@@ -446,19 +428,12 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     tc_fence_after();
     int at = incl - sum;
     for (int w = 0; w < warp; ++w) at += s_sum[w];
-    for (int b = b0; b < b1; ++b) {
-      s_off[b] = at;
-      if (blockIdx.x == 0) p.sched[b] = at;
-      at += own_cost(p, b);
-    }
-    if (b0 < p.c.B && b1 == p.c.B) {
-      s_off[p.c.B] = at;
-      if (blockIdx.x == 0) p.sched[p.c.B] = at;
-    }
+    s_off[threadIdx.x] = at;
+    if (threadIdx.x == kGroups - 1) s_off[kGroups] = at + sum;
     __syncthreads();
   }
   const uint32_t tmem = *s_tmem;
-  const Line line = line_of(p, s_off[p.c.B], gridDim.x);
+  const Line line = line_of(p, s_off[kGroups], gridDim.x);
   const int cta = blockIdx.x;
   const int64_t x0 = cta < line.ctas ? line.first(cta) : 0, x1 = cta < line.ctas ? line.first(cta + 1) : 0;
 
@@ -484,10 +459,10 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       int seg = 0;                         // segments whose query rows are on their way
       bool rows = k.s.count > 0;           // those of the keys' segment are to come
       bool ok = true;
-      const auto issue = [&](Cursor& c, uint8_t* ring, uint64_t* full, uint64_t* empty, const CUtensorMap* prefix,
+      const auto issue = [&](Cursor& c, int n, uint8_t* ring, uint64_t* full, uint64_t* empty, const CUtensorMap* prefix,
                              const CUtensorMap* own) {
-        const int st = c.it % NS;
-        if (c.s.count <= 0 || !mbar_test(&empty[st], (c.it / NS & 1) ^ 1)) return false;
+        const int st = c.it % n;
+        if (c.s.count <= 0 || !mbar_test(&empty[st], (c.it / n & 1) ^ 1)) return false;
         mbar_arrive_expect_tx(&full[st], kBytes);
         load_tile<DK>(ring + st * kBytes, kBlock, c.s.prefix ? prefix : own, &full[st], p.whole_rows,
                       (c.s.j0 + c.j) * kTile, c.s.h, c.s.prefix ? 0 : c.s.b);
@@ -499,17 +474,15 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       while (k.s.count > 0 || v.s.count > 0) {
         bool moved = false;
         // (a segment's keys may go ahead of its query rows, the next one's not)
-        if (k.j < k.s.count) moved = issue(k, sK, k_full, k_empty, &maps.pk, &maps.k);
+        if (k.j < k.s.count) moved = issue(k, NK, sK, k_full, k_empty, &maps.pk, &maps.k);
         if (rows && mbar_test(q_empty, (seg & 1) ^ 1)) {
           const Segment& s = k.s;
           const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows;
           const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
           const int token = s.m / p.rows.head_tiles * p.rows.tokens;
-          mbar_arrive_expect_tx(q_full, DK / 64 * 128 * box * s.copies);
-          for (int c = 0; c < s.copies; ++c)
-            for (int i = 0; i < DK / 64; ++i)
-              tma_load_4d(sQ + i * kQBlock + c * (kQBlock / s.copies), s.prefix ? &maps.pq : &maps.q, q_full, 64 * i, head,
-                          token, s.b);
+          mbar_arrive_expect_tx(q_full, DK / 64 * 128 * box);
+          for (int i = 0; i < DK / 64; ++i)
+            tma_load_4d(sQ + i * kQBlock, s.prefix ? &maps.pq : &maps.q, q_full, 64 * i, head, token, s.b);
           ++seg;
           rows = false;
           moved = true;
@@ -518,7 +491,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
           enter(k, k.s.next);
           rows = k.s.count > 0;
         }
-        if (issue(v, sV, v_full, v_empty, &maps.pv, &maps.v)) {
+        if (issue(v, NV, sV, v_full, v_empty, &maps.pv, &maps.v)) {
           moved = true;
           if (v.j == v.s.count) enter(v, v.s.next);
         }
@@ -535,58 +508,63 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (seg > 0) wait(q_full, (seg - 1) & 1);
       }
       // the last copies have landed
-      for (int i = max(0, k.it - NS); i < k.it; ++i) wait(&k_full[i % NS], i / NS & 1);
-      for (int i = max(0, v.it - NS); i < v.it; ++i) wait(&v_full[i % NS], i / NS & 1);
+      for (int i = max(0, k.it - NK); i < k.it; ++i) wait(&k_full[i % NK], i / NK & 1);
+      for (int i = max(0, v.it - NV); i < v.it; ++i) wait(&v_full[i % NV], i / NV & 1);
     }
   } else if (warp == 5) {
     // ------------------------------ MMA -----------------------------------------
-    if (lane == 0) {
-      int it = 0, seg = 0;                 // it: tiles whose product with V is issued
-      bool ok = true;
-      const uint64_t qd = smem_desc(sQ, 1024, kSwizzle128);
-      const auto scores = [&](int i, bool last) {
-        const int st = i % NS;
-        if (!wait(&k_full[st], (i / NS) & 1) || *s_abort) return false;
+    // The whole warp walks the tiles and one lane issues, by predicate: operands
+    // stay in uniform registers (by a branch of lane 0, each instruction took
+    // about 70 cycles to issue).
+    const uint32_t one = elect_one();
+    int it = 0, seg = 0;                   // it: tiles whose product with V is issued
+    bool ok = true;
+    const uint64_t qd = smem_desc(sQ, 1024, kSwizzle128);
+    const auto all = [](bool x) { return __all_sync(0xffffffffu, x) != 0; };
+    const auto scores = [&](int i, bool last) {
+      const int st = i % NK;
+      if (!all(wait(&k_full[st], (i / NK) & 1) && !*s_abort)) return false;
+      tc_fence_after();
+      const uint64_t kd = smem_desc(sK + st * kBytes, 1024, kSwizzle128);
+#pragma unroll
+      for (int k = 0; k < DK / 16; ++k)
+        mma_f16_if(one, tmem + (i & 1) * kTile, qd + (k / 4) * (kQBlock >> 4) + (k % 4) * 2,
+                   kd + (k / 4) * (kBlock >> 4) + (k % 4) * 2, kIdescS, k > 0);
+      mma_commit_if(one, &s_full[i & 1]);
+      mma_commit_if(one, &k_empty[st]);
+      if (last) mma_commit_if(one, q_empty);
+      return true;
+    };
+    for (int64_t x = x0; x < x1 && ok; ++seg) {
+      const Segment s = segment_at(p, line, s_off, x, x1, cta);
+      if (s.count <= 0) break;
+      const int count = __shfl_sync(0xffffffffu, s.count, 0);
+      // (the buffer of tile i + 1 is that of tile i - 1, whose product with V,
+      // issued before, reads the probabilities there first)
+      ok = all(wait(q_full, seg & 1)) && scores(it, count == 1);
+      for (int j = 0; j < count && ok; ++j, ++it) {
+        const int st = it % NV;
+        if (j + 1 < count) ok = scores(it + 1, j + 2 == count);
+        if (ok)
+          ok = all(wait(&v_full[st], (it / NV) & 1) && (j > 0 || wait(o_empty, (seg & 1) ^ 1u)) &&
+                   wait(&p_full[it & 1], (it >> 1) & 1) && !*s_abort);
+        if (!ok) break;
         tc_fence_after();
-        const uint64_t kd = smem_desc(sK + st * kBytes, 1024, kSwizzle128);
+        const uint64_t vd = n_major_desc(sV + st * kBytes);
 #pragma unroll
-        for (int k = 0; k < DK / 16; ++k)
-          mma_f16(tmem + (i & 1) * kTile, qd + (k / 4) * (kQBlock >> 4) + (k % 4) * 2,
-                  kd + (k / 4) * (kBlock >> 4) + (k % 4) * 2, kIdescS, k > 0);
-        mma_commit(&s_full[i & 1]);
-        mma_commit(&k_empty[st]);
-        if (last) mma_commit(q_empty);
-        return true;
-      };
-      for (int64_t x = x0; x < x1 && ok; ++seg) {
-        const Segment s = segment_at(p, line, s_off, x, x1, cta);
-        if (s.count <= 0) break;
-        // (the buffer of tile i + 1 is that of tile i - 1, whose product with V,
-        // issued before, reads the probabilities there first)
-        ok = wait(q_full, seg & 1) && scores(it, s.count == 1);
-        for (int j = 0; j < s.count && ok; ++j, ++it) {
-          const int st = it % NS;
-          if (j + 1 < s.count) ok = scores(it + 1, j + 2 == s.count);
-          ok = ok && wait(&v_full[st], (it / NS) & 1) && (j > 0 || wait(o_empty, (seg & 1) ^ 1u)) &&
-               wait(&p_full[it & 1], (it >> 1) & 1) && !*s_abort;
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t vd = n_major_desc(sV + st * kBytes);
-#pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)
-            mma_f16_ta(tmem + kTmemO, tmem + (it & 1) * kTile + 8 * k, vd + k * (2048 >> 4), kIdescO, j > 0 || k > 0);
-          mma_commit(&v_empty[st]);
-        }
-        if (ok) mma_commit(o_full);
-        x = s.next;
+        for (int k = 0; k < kTile / 16; ++k)
+          mma_f16_ta_if(one, tmem + kTmemO, tmem + (it & 1) * kTile + 8 * k, vd + k * (2048 >> 4), kIdescO, j > 0 || k > 0);
+        mma_commit_if(one, &v_empty[st]);
       }
-      if (!ok) {
-        *s_abort = 1;
-        atomicExch(p.err, kErrMbarTimeout);
-      }
-      mma_commit(done);                    // every MMA has retired
-      wait(done, 0);
+      if (ok) mma_commit_if(one, o_full);
+      x = s.next;
     }
+    if (!ok) {
+      *s_abort = 1;
+      atomicExch(p.err, kErrMbarTimeout);
+    }
+    mma_commit_if(one, done);              // every MMA has retired
+    wait(done, 0);
   } else {
     // ------------------------------ softmax -------------------------------------
     const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
@@ -595,9 +573,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     for (int64_t x = x0; x < x1 && ok; ++seg) {
       const Segment s = segment_at(p, line, s_off, x, x1, cta);
       if (s.count <= 0) break;
-      const int per_copy = kRows / s.copies, copy = threadIdx.x / per_copy, row = threadIdx.x % per_copy;
-      const bool work = warp * 32 % per_copy < s.rows, mine = row < s.rows;
-      const int c0 = copy * (kTile / s.copies);
+      const int row = threadIdx.x;
+      const bool work = warp * 32 < s.rows, mine = row < s.rows;
       const int rr = s.m / p.rows.head_tiles * p.rows.tokens * p.G + s.m % p.rows.head_tiles * p.rows.heads + row;
       RowState r = {-INFINITY, 0.f, 0.f, 0.f};
       for (int j = 0; j < s.count; ++j, ++it) {
@@ -609,17 +586,15 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
           float* sc = !s.prefix && p.scores && mine
                           ? p.scores + ((((int64_t)s.b * p.Hkv + s.h) * p.nt_cap + s.j0 + j) * p.R + rr) * kTile
                           : nullptr;
-          uint64_t* pv = &v_empty[(it + NS - 1) % NS];
-          const uint32_t pvp = ((it + NS - 1) / NS - 1) & 1, sb = lanes + (it & 1) * kTile, ob = lanes + kTmemO;
-          if (s.copies == 1) ok = softmax_tile<DK, BF16, 64>(p, r, sb, ob, 0, nv, j == 0, pv, pvp, sc);
-          else if (s.copies == 2) ok = softmax_tile<DK, BF16, 32>(p, r, sb, ob, c0, nv, j == 0, pv, pvp, sc);
-          else ok = softmax_tile<DK, BF16, 16>(p, r, sb, ob, c0, nv, j == 0, pv, pvp, sc);
+          uint64_t* pv = &v_empty[(it + NV - 1) % NV];
+          const uint32_t pvp = ((it + NV - 1) / NV - 1) & 1, sb = lanes + (it & 1) * kTile, ob = lanes + kTmemO;
+          ok = softmax_tile<DK, BF16>(p, r, sb, ob, nv, j == 0, pv, pvp, sc);
           if (!ok) break;
         }
         if (!s.prefix && nv < kTile) {
           // entries past those in use hold anything: their values become 0
-          const int st = it % NS;
-          ok = __all_sync(0xffffffffu, wait(&v_full[st], (it / NS) & 1));
+          const int st = it % NV;
+          ok = __all_sync(0xffffffffu, wait(&v_full[st], (it / NV) & 1));
           if (!ok) break;
           if (threadIdx.x >= nv && threadIdx.x < kTile) {
 #pragma unroll
@@ -640,8 +615,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       if (!ok) break;
       tc_fence_after();
       if (work) {
-        const int64_t at = s.prefix ? s.slot * kRows + copy * p.rows.prefix_rows + row
-                                    : (s.slot * s.copies + copy) * p.rows.own_rows + row;
+        const int64_t at = s.slot * (s.prefix ? kRows : p.rows.own_rows) + row;
         float* o = (s.prefix ? p.p_o : p.o_o) + at * DK;
         if (mine) (s.prefix ? p.p_ml : p.o_ml)[at] = make_float4(r.ref, r.l, r.rl, 0.f);
 #pragma unroll
@@ -659,6 +633,12 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(o_empty);
+      if (threadIdx.x == 0) {
+        // (the unit: prefix units are numbered first)
+        const int64_t u = s.slot - cta + (s.prefix ? 0 : p.Hkv * p.rows.prefix_units);
+        if (s.j0 == 0) p.unit_ctas[u].x = cta;
+        if (s.j0 + s.count == s.nt) p.unit_ctas[u].y = cta;
+      }
       x = s.next;
     }
     if (!ok) {
@@ -708,15 +688,16 @@ template <int E> struct Part {
 constexpr int kLast = 4;                   // last entries that a warp has on their way
 
 // WPR warps of a CTA of W per query row, each with its share of the row's
-// partial results and of its last entries.
+// partial results and of its last entries.  Two rounds of loads: what the shares
+// are, and what they hold.
 template <int DK, bool BF16, int W, int WPR>
-__global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 7) combine_kernel(const __grid_constant__ AttnParams p, int grid) {
-  constexpr int E = DK / 32, kCombBatch = WPR > 1 ? 8 : 4;                // results on their way
+__global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const __grid_constant__ AttnParams p) {
+  constexpr int E = DK / 32, kBatch = WPR > 1 ? 8 : 4;     // results on their way
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
   pdl_launch_dependents();
   pdl_wait();
-  const int64_t id = (int64_t)blockIdx.x * (W / WPR) + warp / WPR;     // (b, h, row)
-  const bool real = id < (int64_t)p.c.B * p.Hkv * p.R;
+  const uint32_t id = blockIdx.x * (W / WPR) + warp / WPR;     // (b, h, row)
+  const bool real = id < (uint32_t)(p.c.B * p.Hkv * p.R);
   Part<E> a;
   a.m = -INFINITY;
   a.l = a.r = 0.f;
@@ -724,38 +705,33 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 7) combine_kernel(const 
   for (int i = 0; i < E; ++i) a.o[i] = 0.f;
   int b = 0, h = 0, t = 0, hq = 0;
   if (real) {
-    const int rr = (int)(id % p.R), bh = (int)(id / p.R);
-    h = bh % p.Hkv;
-    b = bh / p.Hkv;
-    t = rr / p.G;
+    const uint32_t bh = id / (uint32_t)p.R;
+    const int rr = id - bh * p.R;
+    b = bh / (uint32_t)p.Hkv;
+    h = bh - b * p.Hkv;
+    t = (uint32_t)rr / (uint32_t)p.G;
     const int g = rr - t * p.G;
     hq = h * p.G + g;
-    const Line line = line_of(p, __ldg(p.sched + p.c.B), grid);
-    // partial results of the row: np of its prefix unit, no of its own one, a
-    // segment's copies one after the other
     const Rows& rw = p.rows;
-    const int m = t / rw.tokens * rw.head_tiles + g / rw.heads;              // tile of the sequence
-    const int ro = (t % rw.tokens) * p.G + g % rw.heads;                     // row of the tile
-    int np = 0, no = 0;
-    int64_t at_p = 0, at_o = 0;
-    if (p.nt_prefix > 0) {
-      const int u = h * rw.prefix_units + b / rw.seqs * rw.per_seq + m;
-      const int64_t end = (int64_t)(u + 1) * line.prefix_unit;
-      const int c0 = line.cta(end - (int64_t)(p.nt_prefix - 1) * p.costs.prefix_tile), c1 = line.cta(end);
-      np = (c1 - c0 + 1) * rw.prefix_copies;
-      at_p = (int64_t)(c0 + u) * kRows + b % rw.seqs * p.R + ro;
+    int m = 0, ro = rr;                                        // tile of the sequence, row of the tile
+    if (rw.per_seq > 1) {
+      m = t / rw.tokens * rw.head_tiles + g / rw.heads;
+      ro = (t % rw.tokens) * p.G + g % rw.heads;
     }
-    const int own0 = __ldg(p.sched + b), unit = (__ldg(p.sched + b + 1) - own0) / (p.Hkv * rw.own_units);
-    if (unit > 0) {
-      const int u = h * rw.own_units + m;
-      const int64_t end = line.prefix + own0 + (int64_t)(u + 1) * unit;
-      const int c0 = line.cta(end - unit + p.costs.own_start + p.costs.own_tile), c1 = line.cta(end);
-      no = (c1 - c0 + 1) * rw.own_copies;
-      at_o = (c0 + (int64_t)b * p.Hkv * rw.own_units + u) * rw.own_copies * rw.own_rows + ro;
-    }
+    const int group = (uint32_t)b / (uint32_t)rw.seqs;
+    const int up = h * rw.prefix_units + group * rw.per_seq + m, prefix_units = p.Hkv * rw.prefix_units;
+    const int64_t uo = (int64_t)(b * p.Hkv + h) * rw.own_units + m;
+    const int n = used(p, b);
+    int2 cp = make_int2(0, -1), co = make_int2(0, -1);         // CTAs of the row's prefix unit, of its own one
+    if (p.nt_prefix > 0) cp = __ldcg(p.unit_ctas + up);
+    if (n > p.c.T - 1) co = __ldcg(p.unit_ctas + prefix_units + uo);
+    // partial results: np of the prefix unit, no of the own one
+    const int np = cp.y - cp.x + 1, no = co.y - co.x + 1;
+    const int64_t at_p = (int64_t)(cp.x + up) * kRows + (b - group * rw.seqs) * p.R + ro;
+    const int64_t at_o = (co.x + uo) * rw.own_rows + ro;
     // the last T - 1 own entries, of which this row sees the first few: j_first
     // on, this warp every WPR-th, the first kLast on their way from here
-    const int n = p.c.T > 1 ? used(p, b) : 0, far = n - (p.c.T - 1 - t), j_first = max(0, n - (p.c.T - 1)) + sub;
+    const int far = n - (p.c.T - 1 - t), j_first = p.c.T > 1 ? max(0, n - (p.c.T - 1)) + sub : n;
     uint32_t qw[DK / 64], kw[kLast][DK / 64], vw[kLast][DK / 64];
     const auto fetch = [&](int j0) {
 #pragma unroll
@@ -771,41 +747,21 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 7) combine_kernel(const 
       load_raw<DK>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, lane, qw);
       fetch(j_first);
     }
-    const int share = (np + no + WPR - 1) / WPR, end = min((sub + 1) * share, np + no);
+    const int share = (uint32_t)(np + no + WPR - 1) / (uint32_t)WPR, end = min((sub + 1) * share, np + no);
     for (int s0 = sub * share; s0 < end; s0 += 32) {
       const int s = s0 + lane, some = min(32, end - s0);
+      const auto row_of = [&](int i) {                         // of result i
+        return i < np ? at_p + (int64_t)i * kRows : at_o + (int64_t)(i - np) * rw.own_rows;
+      };
       float4 ml = make_float4(0.f, 0.f, 0.f, 0.f);
-      const float* src = p.p_o;
-      if (lane < some) {
-        const bool own = s >= np;
-        const int c = s / rw.prefix_copies;
-        const int64_t at = own ? at_o + (int64_t)(s - np) * rw.own_rows
-                               : at_p + (int64_t)c * kRows + (s - c * rw.prefix_copies) * rw.prefix_rows;
-        ml = __ldcg((own ? p.o_ml : p.p_ml) + at);
-        src = (own ? p.o_o : p.p_o) + at * DK;
-      }
-      const float m = ml.y == 0.f ? -INFINITY : ml.x;       // (a NaN sum stays in)
-      float top = m;
+      if (lane < some) ml = __ldcg((s < np ? p.p_ml : p.o_ml) + row_of(s));
+      float o[kBatch][E];
+      const auto load = [&](int i0) {
 #pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      if (top == -INFINITY) continue;
-      if (top > a.m) a.rebase(top);
-      const float w = m == -INFINITY ? 0.f : ex2(m - a.m);
-      float l = m == -INFINITY ? 0.f : w * ml.y, r = m == -INFINITY ? 0.f : w * ml.z;
-#pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) {
-        l += __shfl_xor_sync(0xffffffffu, l, d);
-        r += __shfl_xor_sync(0xffffffffu, r, d);
-      }
-      a.l += l;
-      a.r += r;
-      for (int i0 = 0; i0 < some; i0 += kCombBatch) {
-        float o[kCombBatch][E];
-#pragma unroll
-        for (int i = 0; i < kCombBatch; ++i) {
-          const float* from =
-              reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), i0 + i));
+        for (int i = 0; i < kBatch; ++i)
           if (i0 + i < some) {
+            const int si = s0 + i0 + i;
+            const float* from = (si < np ? p.p_o : p.o_o) + row_of(si) * DK;
             if constexpr (E == 4) {
               const float4 f = __ldcg(reinterpret_cast<const float4*>(from) + lane);
               o[i][0] = f.x, o[i][1] = f.y, o[i][2] = f.z, o[i][3] = f.w;
@@ -814,9 +770,27 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 7) combine_kernel(const 
               o[i][0] = f.x, o[i][1] = f.y;
             }
           }
-        }
+      };
+      load(0);
+      const float mi = ml.y == 0.f ? -INFINITY : ml.x;         // (a NaN sum stays in)
+      float top = mi;
 #pragma unroll
-        for (int i = 0; i < kCombBatch; ++i) {
+      for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      if (top == -INFINITY) continue;
+      if (top > a.m) a.rebase(top);
+      const float w = mi == -INFINITY ? 0.f : ex2(mi - a.m);
+      float l = mi == -INFINITY ? 0.f : w * ml.y, r = mi == -INFINITY ? 0.f : w * ml.z;
+#pragma unroll
+      for (int d = 16; d >= 1; d >>= 1) {
+        l += __shfl_xor_sync(0xffffffffu, l, d);
+        r += __shfl_xor_sync(0xffffffffu, r, d);
+      }
+      a.l += l;
+      a.r += r;
+      for (int i0 = 0; i0 < some; i0 += kBatch) {
+        if (i0 > 0) load(i0);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
           const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
           if (i0 + i < some && wi != 0.f) {
 #pragma unroll
@@ -969,33 +943,32 @@ bool encode_kv(CUtensorMap* map, bool bf16, const void* base, int D, const int64
 }
 
 template <int DK>
-size_t attend_smem(int B) {
-  return 1024 + kQBytes<DK> + (size_t)2 * kStages<DK> * kTileBytes<DK> + (4 * kStages<DK> + 9) * 8 + 8 + 32 +
-         (size_t)(B + 1) * 4;
+constexpr size_t attend_smem() {
+  return kQBytes<DK> + (size_t)(kStagesK<DK> + kStagesV<DK>) * kTileBytes<DK> +
+         (2 * kStagesK<DK> + 2 * kStagesV<DK> + 9) * 8 + 8 + 32 + (kGroups + 1) * 4;
 }
+
+static_assert(2 * (attend_smem<128>() + 1024) <= 228 * 1024 && 2 * (attend_smem<64>() + 1024) <= 228 * 1024, "two CTAs per SM");
 
 template <int DK, bool BF16>
 cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, int grid, cudaStream_t s) {
   static PerDevice attr;
   cudaError_t e = attr.once(dev, []() {
     return cudaFuncSetAttribute(attend_kernel<DK, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)attend_smem<DK>(SPIKE_PROJ_CACHE_MAX_B));
+                                (int)attend_smem<DK>());
   });
   if (e != cudaSuccess) return e;
-  e = launch_pdl(attend_kernel<DK, BF16>, dim3(grid), dim3(kAttThreads), attend_smem<DK>(p.c.B), s, maps, p);
+  e = launch_pdl(attend_kernel<DK, BF16>, dim3(grid), dim3(kAttThreads), attend_smem<DK>(), s, maps, p);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
   if (rows <= 2048)
-    e = launch_pdl(combine_kernel<DK, BF16, 8, 8>, dim3((unsigned)rows), dim3(256), 0, s, p, grid);
+    e = launch_pdl(combine_kernel<DK, BF16, 8, 8>, dim3((unsigned)rows), dim3(256), 0, s, p);
   else
-    e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, p, grid);
+    e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, p);
   if (e != cudaSuccess || !p.c.weights) return e;
   return launch_pdl(weights_kernel, dim3((unsigned)min(ceil_div(p.nt_cap, 2), 65535), (unsigned)(p.c.B * p.Hkv)),
                     dim3(2 * kTile), 0, s, p);
 }
-
-// Copies of a unit's rows in the MMA's 128.
-int copies_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
 
 Rows rows_of(int B, int T, int G) {
   Rows r;
@@ -1008,8 +981,6 @@ Rows rows_of(int B, int T, int G) {
   r.prefix_units = ceil_div(B, r.seqs) * r.per_seq;
   r.own_rows = r.heads * r.tokens;
   r.prefix_rows = r.own_rows * r.seqs;
-  r.own_copies = copies_of(r.own_rows);
-  r.prefix_copies = copies_of(r.prefix_rows);
   return r;
 }
 
@@ -1017,16 +988,16 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 // The workspace's parts, for calls of B sequences and T query tokens.
 struct Parts {
-  size_t sched, lse2, p_ml, p_o, o_ml, o_o, scores, end;
+  size_t units, lse2, p_ml, p_o, o_ml, o_o, scores, end;
 };
 Parts parts_of(const CacheShape& s, int B, int T, int grid) {
   const int G = s.Hq / s.Hkv, R = T * G, DK = s.D <= 64 ? 64 : 128;
   const Rows r = rows_of(B, T, G);
   const size_t p_slots = (size_t)grid + (size_t)s.Hkv * r.prefix_units;
-  const size_t o_rows = ((size_t)grid + (size_t)B * s.Hkv * r.own_units) * r.own_rows * r.own_copies;
+  const size_t o_rows = ((size_t)grid + (size_t)B * s.Hkv * r.own_units) * r.own_rows;
   Parts w;
-  w.sched = 0;
-  w.lse2 = round256((size_t)(B + 1) * 4);
+  w.units = 0;
+  w.lse2 = round256(((size_t)s.Hkv * r.prefix_units + (size_t)B * s.Hkv * r.own_units) * 8);
   w.p_ml = w.lse2 + round256((size_t)B * s.Hkv * R * 4);
   w.p_o = w.p_ml + p_slots * kRows * 16;
   w.o_ml = w.p_o + p_slots * kRows * DK * 4;
@@ -1068,8 +1039,11 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.capacity = s.capacity;
   p.R = c.T * p.G;
   p.rows = rows_of(c.B, c.T, p.G);
+  // A unit costs its row's copy and its result about what a tile does, and own
+  // tiles come from memory where the prefix's are found in L2.  us a call with
+  // all tiles alike / like this: 128 drafting sequences on 16384 entries 221 / 202,
+  // 64 chats 48 / 43.5, 16 on a document of 131072 70 / 64.
   p.costs = Costs{8, 6, 8, 7};
-  if (const char* f = getenv("AT_COST")) sscanf(f, "%d,%d,%d,%d", &p.costs.prefix_start, &p.costs.prefix_tile, &p.costs.own_start, &p.costs.own_tile);
   p.nt_prefix = ceil_div(c.prefix_len, kTile);
   p.nt_cap = ceil_div(s.capacity, kTile);
   p.c2 = c.scale * kLog2e;
@@ -1077,7 +1051,7 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.err = err;
   const int grid = 2 * sms;
   const Parts w = parts_of(s, c.B, c.T, grid);
-  p.sched = reinterpret_cast<int32_t*>(ws + w.sched);
+  p.unit_ctas = reinterpret_cast<int2*>(ws + w.units);
   p.lse2 = reinterpret_cast<float*>(ws + w.lse2);
   p.p_ml = reinterpret_cast<float4*>(ws + w.p_ml);
   p.p_o = reinterpret_cast<float*>(ws + w.p_o);
