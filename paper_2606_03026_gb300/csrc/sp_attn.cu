@@ -112,22 +112,22 @@ __device__ __forceinline__ int seen_by_all(const AttnParams& p, int b) { return 
 
 // The line is measured in cost: a unit costs `start` and then each of its tiles.
 struct Line {
-  int64_t prefix, all;      // cost of the prefix units; of all
+  int prefix, all;          // cost of the prefix units; of all (a call has fewer than 2^27 tiles)
   int32_t prefix_unit;      // of one
   int ctas;                 // that share it
   // CTA c has the tiles that end past first(c), up to first(c + 1)
-  __device__ __forceinline__ int64_t first(int c) const { return c * all / ctas; }
+  __device__ __forceinline__ int first(int c) const { return (int)((int64_t)c * all / ctas); }
 };
 __device__ __forceinline__ Line line_of(const AttnParams& p, int own_cost, int grid) {
   const Costs& k = p.costs;
   Line l;
   l.prefix_unit = k.prefix_start + p.nt_prefix * k.prefix_tile;
-  l.prefix = p.nt_prefix == 0 ? 0 : (int64_t)p.Hkv * p.rows.prefix_units * l.prefix_unit;
+  l.prefix = p.nt_prefix == 0 ? 0 : p.Hkv * p.rows.prefix_units * l.prefix_unit;
   l.all = l.prefix + own_cost;
   // (as much for every CTA as a tile costs at most: a unit's tiles are of
   // CTAs without a gap)
   const int most = max(k.prefix_tile, k.own_tile);
-  l.ctas = l.all >= (int64_t)grid * most ? grid : max(1, (int)l.all / most);
+  l.ctas = l.all / most >= grid ? grid : max(1, l.all / most);
   return l;
 }
 __device__ __forceinline__ int own_cost(const AttnParams& p, int b) {
@@ -141,62 +141,67 @@ struct Segment {
   int j0, count, nt;        // tiles, of nt that the unit has
   int seen;                 // entries of the unit
   int rows;
-  int64_t slot, next;       // next: where the following unit begins on the line
+  int next;                 // where the following unit begins on the line
+  int64_t slot;
 };
 // off: cost of the own units before each of the groups of sequences that
 // attend_kernel's threads add up.  The segment at point x of a CTA whose tiles end at `end`; of no tiles where
 // the first one past x ends past `end`.
-__device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l, const int* off, int64_t x,
-                                              int64_t end, int cta) {
+__device__ __forceinline__ Segment segment_at(const AttnParams& p, const Line& l, const int* off, int x, int end,
+                                              int cta) {
   const Rows& r = p.rows;
   Segment s;
   s.prefix = x < l.prefix;
-  int start, tile;
-  int64_t at;                              // where the unit begins
+  int start, tile, at;                     // at: where the unit begins
   if (s.prefix) {
-    const int u = (int)(x / l.prefix_unit);
-    at = (int64_t)u * l.prefix_unit;
+    const int u = (uint32_t)x / (uint32_t)l.prefix_unit;
+    at = u * l.prefix_unit;
     s.next = at + l.prefix_unit;
     s.nt = p.nt_prefix;
     start = p.costs.prefix_start;
     tile = p.costs.prefix_tile;
-    s.h = u / r.prefix_units;
+    s.h = (uint32_t)u / (uint32_t)r.prefix_units;
     const int i = u - s.h * r.prefix_units;
-    s.b = i / r.per_seq * r.seqs;
-    s.m = i % r.per_seq;
+    s.b = i * r.seqs;
+    s.m = 0;
+    if (r.per_seq > 1) {                   // (then seqs is 1)
+      s.b = i / r.per_seq;
+      s.m = i - s.b * r.per_seq;
+    }
     s.seen = p.c.prefix_len;
     s.slot = cta + u;
   } else {
-    const int y = (int)(x - l.prefix);
+    const int y = x - l.prefix;
     int lo = 0, hi = kGroups;              // off[lo] <= y < off[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (off[mid] <= y) lo = mid; else hi = mid;
     }
-    int before = off[lo], cost = off[lo + 1] - before;
+    int before = off[lo];
     const int per = ceil_div(p.c.B, kGroups);
     lo *= per;
     if (per > 1)
-      while (cost = own_cost(p, lo), before + cost <= y) {
-        before += cost;
-        ++lo;
-      }
+      for (int cost; before + (cost = own_cost(p, lo)) <= y; ++lo) before += cost;
     s.b = lo;
-    const int unit = cost / (p.Hkv * r.own_units);
-    const int u = (y - before) / unit;
+    s.seen = seen_by_all(p, lo);
+    s.nt = ceil_div(s.seen, kTile);
+    const int unit = p.costs.own_start + s.nt * p.costs.own_tile;
+    const int u = (uint32_t)(y - before) / (uint32_t)unit;
     at = l.prefix + before + u * unit;
     s.next = at + unit;
     start = p.costs.own_start;
     tile = p.costs.own_tile;
-    s.seen = seen_by_all(p, lo);
-    s.nt = ceil_div(s.seen, kTile);
-    s.h = u / r.own_units;
-    s.m = u - s.h * r.own_units;
+    s.h = u;
+    s.m = 0;
+    if (r.own_units > 1) {
+      s.h = u / r.own_units;
+      s.m = u - s.h * r.own_units;
+    }
     s.slot = cta + (int64_t)lo * p.Hkv * r.own_units + u;
   }
   // tile j ends at `at + start + (j + 1) tile`
-  s.j0 = max(0, (int)(x - at) - start) / tile;
-  s.count = min(s.nt, (int)max((int64_t)0, min(end, s.next) - at - start) / tile) - s.j0;
+  s.j0 = max(0, x - at - start) / tile;
+  s.count = min(s.nt, max(0, min(end, s.next) - at - start) / tile) - s.j0;
   s.rows = r.head_tiles > 1 ? min(r.heads, p.G - s.m % r.head_tiles * r.heads)
                             : min(r.tokens, p.c.T - s.m * r.tokens) * p.G;
   if (s.prefix) s.rows *= min(r.seqs, p.c.B - s.b);
@@ -256,15 +261,29 @@ __device__ __forceinline__ uint64_t n_major_desc(const void* p) {
   return d | (uint64_t)(kBlock >> 4) << 16;
 }
 
-// Bounded wait, inline: a call would cost the softmax's loop its registers.
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity) {
+// Bounded wait, inline (a call would cost the softmax's loop its registers);
+// false too when another warp of the CTA has given up (`stop`, where given).
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, const volatile int* stop = nullptr) {
   if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   do {
     if (mbar_try_wait(bar, parity)) return true;
-  } while (clock64() - t0 < kWaitLimitCycles);
+  } while (!(stop && *stop) && clock64() - t0 < kWaitLimitCycles);
   return false;
 }
+
+// The place of the query rows in shared memory: segments of up to 64 rows have
+// half of it in turn (64 rows of every block of 64 elements), so that the next
+// one's rows are there in time; others the whole.  used: the parity of the times
+// that each half was taken.
+struct RowPlaces {
+  int next = 0, used = 0;
+  __device__ __forceinline__ int of(int rows) const { return rows > kRows / 2 ? 3 : 1 << next; }
+  __device__ __forceinline__ void take(int halves) {
+    if (halves != 3) next ^= 1;
+    used ^= halves;
+  }
+};
 
 // What a softmax thread keeps of its row.
 struct RowState {
@@ -373,7 +392,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   uint64_t* bars = reinterpret_cast<uint64_t*>(sV + NV * kBytes);
   uint64_t *k_full = bars, *k_empty = bars + NK, *v_full = bars + 2 * NK, *v_empty = v_full + NV;
   uint64_t *s_full = v_empty + NV, *p_full = s_full + 2;   // [2]: by score buffer
-  uint64_t *q_full = p_full + 2, *q_empty = q_full + 1, *o_full = q_full + 2, *o_empty = q_full + 3, *done = q_full + 4;
+  uint64_t *q_full = p_full + 2, *q_empty = q_full + 2,     // [2]: by half of the rows' place
+           *o_full = q_full + 4, *o_empty = q_full + 5, *done = q_full + 6;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* s_abort = reinterpret_cast<volatile int*>(s_tmem + 1);
   int* s_sum = reinterpret_cast<int*>(s_tmem + 2);         // [8]
@@ -393,8 +413,10 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[i], 4);
     }
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 1);
+      mbar_init(&q_empty[i], 1);
+    }
     mbar_init(o_full, 1);
     mbar_init(o_empty, 4);
     mbar_init(done, 1);
@@ -435,7 +457,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   const uint32_t tmem = *s_tmem;
   const Line line = line_of(p, s_off[kGroups], gridDim.x);
   const int cta = blockIdx.x;
-  const int64_t x0 = cta < line.ctas ? line.first(cta) : 0, x1 = cta < line.ctas ? line.first(cta + 1) : 0;
+  const int x0 = cta < line.ctas ? line.first(cta) : 0, x1 = cta < line.ctas ? line.first(cta + 1) : 0;
 
   if (warp == 4) {
     // ------------------------------ TMA -----------------------------------------
@@ -443,12 +465,10 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       // where the keys and where the values are: a tile of a segment
       struct Cursor {
         Segment s;
-        int64_t x;
         int j, it;
       };
       Cursor k, v;
-      const auto enter = [&](Cursor& c, int64_t x) {
-        c.x = x;
+      const auto enter = [&](Cursor& c, int x) {
         c.j = 0;
         c.s.count = 0;
         if (x < x1) c.s = segment_at(p, line, s_off, x, x1, cta);
@@ -456,8 +476,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       enter(k, x0);
       enter(v, x0);
       k.it = v.it = 0;
-      int seg = 0;                         // segments whose query rows are on their way
-      bool rows = k.s.count > 0;           // those of the keys' segment are to come
+      RowPlaces places;
+      bool rows = k.s.count > 0;           // the query rows of the keys' segment are to come
       bool ok = true;
       const auto issue = [&](Cursor& c, int n, uint8_t* ring, uint64_t* full, uint64_t* empty, const CUtensorMap* prefix,
                              const CUtensorMap* own) {
@@ -475,17 +495,23 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         bool moved = false;
         // (a segment's keys may go ahead of its query rows, the next one's not)
         if (k.j < k.s.count) moved = issue(k, NK, sK, k_full, k_empty, &maps.pk, &maps.k);
-        if (rows && mbar_test(q_empty, (seg & 1) ^ 1)) {
+        if (rows) {
           const Segment& s = k.s;
-          const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows;
-          const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
-          const int token = s.m / p.rows.head_tiles * p.rows.tokens;
-          mbar_arrive_expect_tx(q_full, DK / 64 * 128 * box);
-          for (int i = 0; i < DK / 64; ++i)
-            tma_load_4d(sQ + i * kQBlock, s.prefix ? &maps.pq : &maps.q, q_full, 64 * i, head, token, s.b);
-          ++seg;
-          rows = false;
-          moved = true;
+          const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows, halves = places.of(box);
+          if (((halves & 1) == 0 || mbar_test(&q_empty[0], places.used & 1 ^ 1)) &&
+              ((halves & 2) == 0 || mbar_test(&q_empty[1], places.used >> 1 ^ 1))) {
+            const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
+            const int token = s.m / p.rows.head_tiles * p.rows.tokens;
+            uint64_t* full = &q_full[halves == 2];
+            mbar_arrive_expect_tx(full, DK / 64 * 128 * box);
+            if (halves == 3) mbar_arrive(&q_full[1]);
+            for (int i = 0; i < DK / 64; ++i)
+              tma_load_4d(sQ + i * kQBlock + (halves == 2 ? kQBlock / 2 : 0), s.prefix ? &maps.pq : &maps.q, full, 64 * i,
+                          head, token, s.b);
+            places.take(halves);
+            rows = false;
+            moved = true;
+          }
         }
         if (k.j == k.s.count && k.s.count > 0 && !rows) {
           enter(k, k.s.next);
@@ -505,7 +531,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       if (!ok) {
         *s_abort = 1;
         atomicExch(p.err, kErrMbarTimeout);
-        if (seg > 0) wait(q_full, (seg - 1) & 1);
+        for (int i = 0; i < 2; ++i) wait(&q_full[i], places.used >> i & 1 ^ 1);
       }
       // the last copies have landed
       for (int i = max(0, k.it - NK); i < k.it; ++i) wait(&k_full[i % NK], i / NK & 1);
@@ -519,12 +545,14 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     const uint32_t one = elect_one();
     int it = 0, seg = 0;                   // it: tiles whose product with V is issued
     bool ok = true;
-    const uint64_t qd = smem_desc(sQ, 1024, kSwizzle128);
+    RowPlaces places;
     const auto all = [](bool x) { return __all_sync(0xffffffffu, x) != 0; };
-    const auto scores = [&](int i, bool last) {
+    const auto scores = [&](int i, int halves, bool last) {
       const int st = i % NK;
-      if (!all(wait(&k_full[st], (i / NK) & 1) && !*s_abort)) return false;
+      if (!all(wait(&k_full[st], (i / NK) & 1, s_abort))) return false;
       tc_fence_after();
+      // (half a place on the MMA's later rows read what is there: nobody reads theirs)
+      const uint64_t qd = smem_desc(sQ + (halves == 2 ? kQBlock / 2 : 0), 1024, kSwizzle128);
       const uint64_t kd = smem_desc(sK + st * kBytes, 1024, kSwizzle128);
 #pragma unroll
       for (int k = 0; k < DK / 16; ++k)
@@ -532,22 +560,31 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
                    kd + (k / 4) * (kBlock >> 4) + (k % 4) * 2, kIdescS, k > 0);
       mma_commit_if(one, &s_full[i & 1]);
       mma_commit_if(one, &k_empty[st]);
-      if (last) mma_commit_if(one, q_empty);
+      if (last && (halves & 1)) mma_commit_if(one, &q_empty[0]);
+      if (last && (halves & 2)) mma_commit_if(one, &q_empty[1]);
       return true;
     };
-    for (int64_t x = x0; x < x1 && ok; ++seg) {
-      const Segment s = segment_at(p, line, s_off, x, x1, cta);
-      if (s.count <= 0) break;
-      const int count = __shfl_sync(0xffffffffu, s.count, 0);
+    Segment next;
+    next.count = 0;
+    if (x0 < x1) next = segment_at(p, line, s_off, x0, x1, cta);
+    for (; ok && next.count > 0; ++seg) {
+      const int count = __shfl_sync(0xffffffffu, next.count, 0);
+      const int halves = __shfl_sync(0xffffffffu, places.of(next.prefix ? p.rows.prefix_rows : p.rows.own_rows), 0);
       // (the buffer of tile i + 1 is that of tile i - 1, whose product with V,
       // issued before, reads the probabilities there first)
-      ok = all(wait(q_full, seg & 1)) && scores(it, count == 1);
+      ok = all(((halves & 1) == 0 || wait(&q_full[0], places.used & 1, s_abort)) &&
+               ((halves & 2) == 0 || wait(&q_full[1], places.used >> 1, s_abort))) &&
+           scores(it, halves, count == 1);
+      places.take(halves);
+      const int x = next.next;             // (the next segment, while the first softmax runs)
+      next.count = 0;
+      if (x < x1) next = segment_at(p, line, s_off, x, x1, cta);
       for (int j = 0; j < count && ok; ++j, ++it) {
         const int st = it % NV;
-        if (j + 1 < count) ok = scores(it + 1, j + 2 == count);
+        if (j + 1 < count) ok = scores(it + 1, halves, j + 2 == count);
         if (ok)
-          ok = all(wait(&v_full[st], (it / NV) & 1) && (j > 0 || wait(o_empty, (seg & 1) ^ 1u)) &&
-                   wait(&p_full[it & 1], (it >> 1) & 1) && !*s_abort);
+          ok = all(wait(&v_full[st], (it / NV) & 1, s_abort) && (j > 0 || wait(o_empty, (seg & 1) ^ 1u, s_abort)) &&
+                   wait(&p_full[it & 1], (it >> 1) & 1, s_abort));
         if (!ok) break;
         tc_fence_after();
         const uint64_t vd = n_major_desc(sV + st * kBytes);
@@ -557,7 +594,6 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         mma_commit_if(one, &v_empty[st]);
       }
       if (ok) mma_commit_if(one, o_full);
-      x = s.next;
     }
     if (!ok) {
       *s_abort = 1;
@@ -570,16 +606,18 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
     int it = 0, seg = 0;
     bool ok = true;
-    for (int64_t x = x0; x < x1 && ok; ++seg) {
-      const Segment s = segment_at(p, line, s_off, x, x1, cta);
-      if (s.count <= 0) break;
+    Segment next;
+    next.count = 0;
+    if (x0 < x1) next = segment_at(p, line, s_off, x0, x1, cta);
+    for (; ok && next.count > 0; ++seg) {
+      const Segment s = next;
       const int row = threadIdx.x;
       const bool work = warp * 32 < s.rows, mine = row < s.rows;
       const int rr = s.m / p.rows.head_tiles * p.rows.tokens * p.G + s.m % p.rows.head_tiles * p.rows.heads + row;
       RowState r = {-INFINITY, 0.f, 0.f, 0.f};
       for (int j = 0; j < s.count; ++j, ++it) {
         const int nv = min(kTile, s.seen - (s.j0 + j) * kTile);
-        ok = __all_sync(0xffffffffu, wait(&s_full[it & 1], (it >> 1) & 1) && !*s_abort);
+        ok = __all_sync(0xffffffffu, wait(&s_full[it & 1], (it >> 1) & 1, s_abort));
         if (!ok) break;
         tc_fence_after();
         if (work) {
@@ -594,7 +632,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (!s.prefix && nv < kTile) {
           // entries past those in use hold anything: their values become 0
           const int st = it % NV;
-          ok = __all_sync(0xffffffffu, wait(&v_full[st], (it / NV) & 1));
+          ok = __all_sync(0xffffffffu, wait(&v_full[st], (it / NV) & 1, s_abort));
           if (!ok) break;
           if (threadIdx.x >= nv && threadIdx.x < kTile) {
 #pragma unroll
@@ -611,7 +649,9 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (lane == 0) mbar_arrive(&p_full[it & 1]);
       }
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, wait(o_full, seg & 1) && !*s_abort);
+      next.count = 0;                      // (the next segment, while the last product is computed)
+      if (s.next < x1) next = segment_at(p, line, s_off, s.next, x1, cta);
+      ok = __all_sync(0xffffffffu, wait(o_full, seg & 1, s_abort));
       if (!ok) break;
       tc_fence_after();
       if (work) {
@@ -639,7 +679,6 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (s.j0 == 0) p.unit_ctas[u].x = cta;
         if (s.j0 + s.count == s.nt) p.unit_ctas[u].y = cta;
       }
-      x = s.next;
     }
     if (!ok) {
       *s_abort = 1;
@@ -945,7 +984,7 @@ bool encode_kv(CUtensorMap* map, bool bf16, const void* base, int D, const int64
 template <int DK>
 constexpr size_t attend_smem() {
   return kQBytes<DK> + (size_t)(kStagesK<DK> + kStagesV<DK>) * kTileBytes<DK> +
-         (2 * kStagesK<DK> + 2 * kStagesV<DK> + 9) * 8 + 8 + 32 + (kGroups + 1) * 4;
+         (2 * kStagesK<DK> + 2 * kStagesV<DK> + 11) * 8 + 8 + 32 + (kGroups + 1) * 4;
 }
 
 static_assert(2 * (attend_smem<128>() + 1024) <= 228 * 1024 && 2 * (attend_smem<64>() + 1024) <= 228 * 1024, "two CTAs per SM");
