@@ -285,29 +285,30 @@ struct RowPlaces {
   }
 };
 
+// 32 bytes, a whole sector of memory.
+__device__ __forceinline__ void store8(float* to, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
 // What a softmax thread keeps of its row.
 struct RowState {
   float m, ref, l, rl;      // maximum that the reference follows, reference, sums
 };
 
-// One tile: the row's scores at s_buf become its probabilities.  pv: the barrier
+// One tile: the row's scores at s_buf (left in v, -infinity past nv) become its
+// probabilities.  pv: the barrier
 // (and its parity) that says that the product before this tile's is complete.
 template <int DK, bool BF16>
-__device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, uint32_t s_buf, uint32_t o_buf, int nv,
-                                             bool first, uint64_t* pv, uint32_t pv_parity, float* scores) {
+__device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, uint32_t (&v)[2][32], uint32_t s_buf,
+                                             uint32_t o_buf, int nv, bool first, uint64_t* pv, uint32_t pv_parity) {
   constexpr float kLag = BF16 ? 8.f : 4.f, kLift = BF16 ? 0.f : 10.f;
-  uint32_t v[2][32];
   tmem_ld32_issue(s_buf, v[0]);
   tmem_ld32_issue(s_buf + 32, v[1]);
   tmem_ld_wait();
   reg_pin(v[0]);
   reg_pin(v[1]);
-  if (scores) {
-#pragma unroll
-    for (int i = 0; i < kTile / 4; ++i)
-      reinterpret_cast<uint4*>(scores)[i] =
-          make_uint4(v[i / 8][i % 8 * 4], v[i / 8][i % 8 * 4 + 1], v[i / 8][i % 8 * 4 + 2], v[i / 8][i % 8 * 4 + 3]);
-  }
   if (nv < kTile) {
 #pragma unroll
     for (int i = 0; i < kTile; ++i)
@@ -330,7 +331,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
     if (!first) {
       if (!__all_sync(0xffffffffu, wait(pv, pv_parity))) return false;
       tc_fence_after();
-#pragma unroll
+#pragma unroll 1                           // (rare, and registers are short)
       for (int i = 0; i < DK / 16; ++i) {
         uint32_t o[16];
         tmem_ld16_issue(o_buf + 16 * i, o);
@@ -620,13 +621,11 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         ok = __all_sync(0xffffffffu, wait(&s_full[it & 1], (it >> 1) & 1, s_abort));
         if (!ok) break;
         tc_fence_after();
+        uint32_t v[2][32];
         if (work) {
-          float* sc = !s.prefix && p.scores && mine
-                          ? p.scores + ((((int64_t)s.b * p.Hkv + s.h) * p.nt_cap + s.j0 + j) * p.R + rr) * kTile
-                          : nullptr;
           uint64_t* pv = &v_empty[(it + NV - 1) % NV];
           const uint32_t pvp = ((it + NV - 1) / NV - 1) & 1, sb = lanes + (it & 1) * kTile, ob = lanes + kTmemO;
-          ok = softmax_tile<DK, BF16>(p, r, sb, ob, nv, j == 0, pv, pvp, sc);
+          ok = softmax_tile<DK, BF16>(p, r, v, sb, ob, nv, j == 0, pv, pvp);
           if (!ok) break;
         }
         if (!s.prefix && nv < kTile) {
@@ -647,6 +646,12 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_full[it & 1]);
+        if (!s.prefix && p.scores && mine) {
+          // (after the probabilities are on their way: the stores hold a warp up)
+          float* sc = p.scores + ((((int64_t)s.b * p.Hkv + s.h) * p.nt_cap + s.j0 + j) * p.R + rr) * kTile;
+#pragma unroll
+          for (int i = 0; i < kTile / 8; ++i) store8(sc + 8 * i, &v[i / 4][i % 4 * 8]);
+        }
       }
       if (!ok) break;
       next.count = 0;                      // (the next segment, while the last product is computed)
@@ -658,15 +663,14 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         const int64_t at = s.slot * (s.prefix ? kRows : p.rows.own_rows) + row;
         float* o = (s.prefix ? p.p_o : p.o_o) + at * DK;
         if (mine) (s.prefix ? p.p_ml : p.o_ml)[at] = make_float4(r.ref, r.l, r.rl, 0.f);
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < DK / 32; ++i) {
           uint32_t v[32];
           tmem_ld32(lanes + kTmemO + 32 * i, v);
           reg_pin(v);
           if (mine) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              reinterpret_cast<uint4*>(o)[8 * i + e] = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+            for (int e = 0; e < 4; ++e) store8(o + 32 * i + 8 * e, &v[8 * e]);
           }
         }
       }
