@@ -586,7 +586,7 @@ sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream);
  * 16-byte aligned, strides of dimensions longer than 1 multiples of 8 (and
  * positive for q, K and V, |stride| >= D for out), else SP_EALIGN.  A B above
  * max_batch, a T above max_T, a prefix above SPIKE_PROJ_CACHE_MAX_LEN or a call
- * of 2^27 tiles (64 entries for the query rows of one K/V head) and more:
+ * of 2^25 tiles (64 entries for the query rows of one K/V head) and more:
  * SP_ERANGE. */
 typedef struct sp_attend {
     const void *q;                        /* [B][T][Hq][D] */

@@ -1237,7 +1237,7 @@ sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend* c, sp_strea
   if (c->prefix_len > 0 && (!c->prefix_k || !c->prefix_v)) return SP_EINVAL;
   if (c->B > sh.max_batch || c->T > sh.max_T || c->prefix_len > SPIKE_PROJ_CACHE_MAX_LEN) return SP_ERANGE;
   if (c->weights && !sh.weights) return SP_EUNSUPPORTED;
-  if (attend_tiles(sh, *c) >= (int64_t)1 << 27) return SP_ERANGE;
+  if (attend_tiles(sh, *c) >= (int64_t)1 << 25) return SP_ERANGE;
   const auto in = [&](int64_t n, int64_t stride) { return n <= 1 || (stride % 8 == 0 && stride > 0); };
   const auto out = [&](int64_t n, int64_t stride) {
     return n == 1 || (stride % 8 == 0 && (stride >= sh.D || stride <= -sh.D));

@@ -112,7 +112,7 @@ __device__ __forceinline__ int seen_by_all(const AttnParams& p, int b) { return 
 
 // The line is measured in cost: a unit costs `start` and then each of its tiles.
 struct Line {
-  int prefix, all;          // cost of the prefix units; of all (a call has fewer than 2^27 tiles)
+  int prefix, all;          // cost of the prefix units; of all (a call has fewer than 2^25 tiles)
   int32_t prefix_unit;      // of one
   int ctas;                 // that share it
   // CTA c has the tiles that end past first(c), up to first(c + 1)
@@ -1082,11 +1082,12 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.capacity = s.capacity;
   p.R = c.T * p.G;
   p.rows = rows_of(c.B, c.T, p.G);
-  // A unit costs its row's copy and its result about what a tile does, and own
-  // tiles come from memory where the prefix's are found in L2.  us a call with
-  // all tiles alike / like this: 128 drafting sequences on 16384 entries 221 / 202,
-  // 64 chats 48 / 43.5, 16 on a document of 131072 70 / 64.
-  p.costs = Costs{8, 6, 8, 7};
+  // A unit costs its rows' copy and its result about what three or four tiles do,
+  // and own tiles come from memory where the prefix's are found in L2.  us a call
+  // with (4, 6, 4, 6) / (8, 6, 8, 7) / these: 128 drafting sequences on 16384 entries
+  // 158 / 150 / 146, 32 with 64-wide heads 56 / 52 / 50, 64 chats 39 / 36 / 35, 34
+  // sequences of 18 to 54 entries on 73566 42 / 35 / 30.
+  p.costs = Costs{24, 6, 20, 7};
   p.nt_prefix = ceil_div(c.prefix_len, kTile);
   p.nt_cap = ceil_div(s.capacity, kTile);
   p.c2 = c.scale * kLog2e;
