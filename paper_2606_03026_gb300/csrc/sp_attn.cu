@@ -39,7 +39,6 @@
 // these last entries.  weights_kernel: the weights, from the scores of the own
 // entries that attend_kernel left in the workspace and the rows' lse.
 #include <cuda.h>
-#include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cudaTypedefs.h>
 
@@ -91,6 +90,7 @@ struct AttnParams {
   Rows rows;
   Costs costs;
   int32_t nt_prefix, nt_cap;               // tiles of the prefix, of the capacity
+  int32_t grid;                            // CTAs of attend_kernel
   bool whole_rows;          // D is DK = 128: a tile of K or V is one copy
   float c2;                 // scale * log2 e
   int* err;
@@ -766,8 +766,12 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
     const int64_t uo = (int64_t)(b * p.Hkv + h) * rw.own_units + m;
     const int n = used(p, b);
     int2 cp = make_int2(0, -1), co = make_int2(0, -1);         // CTAs of the row's prefix unit, of its own one
-    if (p.nt_prefix > 0) cp = __ldcg(p.unit_ctas + up);
-    if (n > p.c.T - 1) co = __ldcg(p.unit_ctas + prefix_units + uo);
+    const auto ctas = [&](int64_t unit) {                      // (in range also where attend_kernel gave up)
+      const int2 x = __ldcg(p.unit_ctas + unit);
+      return make_int2(max(x.x, 0), min(x.y, p.grid - 1));
+    };
+    if (p.nt_prefix > 0) cp = ctas(up);
+    if (n > p.c.T - 1) co = ctas(prefix_units + uo);
     // partial results: np of the prefix unit, no of the own one
     const int np = cp.y - cp.x + 1, no = co.y - co.x + 1;
     const int64_t at_p = (int64_t)(cp.x + up) * kRows + (b - group * rw.seqs) * p.R + ro;
@@ -921,18 +925,20 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
 __global__ void __launch_bounds__(2 * kTile) weights_kernel(const __grid_constant__ AttnParams p) {
   pdl_launch_dependents();
   pdl_wait();
-  const int b = blockIdx.y / p.Hkv, h = blockIdx.y % p.Hkv, n = used(p, b);
-  const float* lse2 = p.lse2 + (int64_t)blockIdx.y * p.R;
-  for (int j = blockIdx.x * 2 * kTile + threadIdx.x; j < n; j += gridDim.x * 2 * kTile) {
-    const float* s = p.scores + ((int64_t)blockIdx.y * p.nt_cap + j / kTile) * p.R * kTile + j % kTile;
-    float* w = p.c.weights + b * p.c.weights_batch + h * p.c.weights_head + j;
-    float sum = 0.f;
+  for (int bh = blockIdx.y; bh < p.c.B * p.Hkv; bh += gridDim.y) {   // (more than 65535 heads)
+    const int b = bh / p.Hkv, h = bh - b * p.Hkv, n = used(p, b);
+    const float* lse2 = p.lse2 + (int64_t)bh * p.R;
+    for (int j = blockIdx.x * 2 * kTile + threadIdx.x; j < n; j += gridDim.x * 2 * kTile) {
+      const float* s = p.scores + ((int64_t)bh * p.nt_cap + j / kTile) * p.R * kTile + j % kTile;
+      float* w = p.c.weights + b * p.c.weights_batch + h * p.c.weights_head + j;
+      float sum = 0.f;
 #pragma unroll 4
-    for (int r = 0; r < p.R; ++r) {
-      const float x = __ldcg(s + (int64_t)r * kTile);
-      if (x != -INFINITY) sum += ex2(fmaf(x, p.c2, -__ldcg(lse2 + r)));
+      for (int r = 0; r < p.R; ++r) {
+        const float x = __ldcg(s + (int64_t)r * kTile);
+        if (x != -INFINITY) sum += ex2(fmaf(x, p.c2, -__ldcg(lse2 + r)));
+      }
+      *w += sum;
     }
-    *w += sum;
   }
 }
 
@@ -994,14 +1000,14 @@ constexpr size_t attend_smem() {
 static_assert(2 * (attend_smem<128>() + 1024) <= 228 * 1024 && 2 * (attend_smem<64>() + 1024) <= 228 * 1024, "two CTAs per SM");
 
 template <int DK, bool BF16>
-cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, int grid, cudaStream_t s) {
+cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, cudaStream_t s) {
   static PerDevice attr;
   cudaError_t e = attr.once(dev, []() {
     return cudaFuncSetAttribute(attend_kernel<DK, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)attend_smem<DK>());
   });
   if (e != cudaSuccess) return e;
-  e = launch_pdl(attend_kernel<DK, BF16>, dim3(grid), dim3(kAttThreads), attend_smem<DK>(), s, maps, p);
+  e = launch_pdl(attend_kernel<DK, BF16>, dim3((unsigned)p.grid), dim3(kAttThreads), attend_smem<DK>(), s, maps, p);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
   if (rows <= 2048)
@@ -1009,7 +1015,7 @@ cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, 
   else
     e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, p);
   if (e != cudaSuccess || !p.c.weights) return e;
-  return launch_pdl(weights_kernel, dim3((unsigned)min(ceil_div(p.nt_cap, 2), 65535), (unsigned)(p.c.B * p.Hkv)),
+  return launch_pdl(weights_kernel, dim3((unsigned)min(ceil_div(p.nt_cap, 2), 65535), (unsigned)min(p.c.B * p.Hkv, 65535)),
                     dim3(2 * kTile), 0, s, p);
 }
 
@@ -1093,8 +1099,8 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.c2 = c.scale * kLog2e;
   p.whole_rows = s.D == 128;
   p.err = err;
-  const int grid = 2 * sms;
-  const Parts w = parts_of(s, c.B, c.T, grid);
+  p.grid = 2 * sms;
+  const Parts w = parts_of(s, c.B, c.T, p.grid);
   p.unit_ctas = reinterpret_cast<int2*>(ws + w.units);
   p.lse2 = reinterpret_cast<float*>(ws + w.lse2);
   p.p_ml = reinterpret_cast<float4*>(ws + w.p_ml);
@@ -1122,10 +1128,10 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
       return cudaErrorInvalidValue;
   }
   if (s.D <= 64)
-    return bf16 ? launch_attend_t<64, true>(p, maps, dev, grid, stream)
-                : launch_attend_t<64, false>(p, maps, dev, grid, stream);
-  return bf16 ? launch_attend_t<128, true>(p, maps, dev, grid, stream)
-              : launch_attend_t<128, false>(p, maps, dev, grid, stream);
+    return bf16 ? launch_attend_t<64, true>(p, maps, dev, stream)
+                : launch_attend_t<64, false>(p, maps, dev, stream);
+  return bf16 ? launch_attend_t<128, true>(p, maps, dev, stream)
+              : launch_attend_t<128, false>(p, maps, dev, stream);
 }
 
 }  // namespace sp

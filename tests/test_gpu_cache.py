@@ -231,6 +231,20 @@ def test_attend_in_a_graph():
     cache.close()
 
 
+def test_attend_more_heads_than_a_grid_is_high():
+    """1024 sequences x 65 K/V heads, one own entry each: it has all of the weight."""
+    B, H, D = 1024, 65, 8
+    g = torch.Generator().manual_seed(31)
+    q, k, v = (torch.randn(B, 1, H, D, generator=g).bfloat16().to(DEV) for _ in range(3))
+    cache = sp.Cache(B, H, H, D, 1, weights=True)
+    out, w = torch.empty_like(q), torch.zeros(B, H, 1, device=DEV)
+    cache.attend(q, k, v, torch.ones(B, dtype=torch.int32, device=DEV), out, weights=w)
+    torch.cuda.synchronize()
+    assert cache.status() == sp.SP_OK
+    assert torch.equal(out, v) and ((w - 1).abs() <= 2.0 ** -20).all()
+    cache.close()
+
+
 # ---------------------------------------------------------------------------
 def evict_case(seed, B, Hkv, D, C, lens, budget, recent, kind, dtype="bf16", layout="entries"):
     g = torch.Generator().manual_seed(seed)
