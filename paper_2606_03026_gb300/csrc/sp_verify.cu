@@ -56,9 +56,10 @@ __device__ __forceinline__ int piece_skip(const float* from) {
 }
 
 // Sum of the whole numbers of entries v0 .. v1 of a warp, the groups' into
-// `groups`.  it: pieces that have gone through the ring before.
+// `groups`.  it: pieces that have gone through the ring before; copies: every
+// copy so far has arrived.
 __device__ __forceinline__ unsigned long long sum_span(const float* pr, const float* qr, int v0, int v1, int per_group,
-                                                       uint8_t* ring, uint64_t* full, int& it,
+                                                       uint8_t* ring, uint64_t* full, int& it, bool& copies,
                                                        unsigned long long* groups) {
   const int lane = threadIdx.x & 31;
   const int pieces = ceil_div(max(v1 - v0, 0), kPiece);
@@ -70,17 +71,17 @@ __device__ __forceinline__ unsigned long long sum_span(const float* pr, const fl
     bulk_load(to, piece_base(pr + v), piece_bytes(pr + v, n), &full[st]);
     if (qr) bulk_load(to + kPieceBytes, piece_base(qr + v), piece_bytes(qr + v, n), &full[st]);
   };
-  if (lane == 0)
+  if (lane == 0 && copies)
     for (int i = 0; i < min(kRing, pieces); ++i) fetch(i);
   unsigned long long all = 0, group = 0;
   for (int i = 0; i < pieces; ++i, ++it) {
     const int st = it % kRing, v = v0 + i * kPiece, n = min(kPiece, v1 - v);
     const float* x = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes) + piece_skip(pr + v);
     const float* y = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes + kPieceBytes) + (qr ? piece_skip(qr + v) : 0);
-    // (a copy that never arrives is read from its source instead)
+    // (once a copy has not arrived in time, the rows are read themselves)
     const uint32_t parity = it / kRing & 1;
-    const bool here = __all_sync(0xffffffffu, mbar_try_wait(&full[st], parity) || mbar_wait(&full[st], parity));
-    if (!here) {
+    copies = copies && __all_sync(0xffffffffu, mbar_try_wait(&full[st], parity) || mbar_wait(&full[st], parity));
+    if (!copies) {
       x = pr + v;
       y = qr + v;
     }
@@ -102,7 +103,7 @@ __device__ __forceinline__ unsigned long long sum_span(const float* pr, const fl
       for (int e = lane; e < n; e += 32) sum += whole(x[e] - (qr ? y[e] : 0.f));
     }
     __syncwarp();
-    if (lane == 0 && i + kRing < pieces && here) fetch(i + kRing);
+    if (lane == 0 && i + kRing < pieces && copies) fetch(i + kRing);
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     all += sum;
@@ -133,6 +134,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerPerSm) verify_kernel(const __
   }
   __syncwarp();
   int it = 0;
+  bool copies = true;
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   pdl_launch_dependents();
   pdl_wait();
@@ -167,7 +169,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerPerSm) verify_kernel(const __
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // every CTA of the cluster is running
   for (int pass = 0;; ++pass) {
     const unsigned long long sum =
-        sum_span(pr, qr, v0, v1, p.per_group, s_ring + (size_t)warp * kRing * 2 * kPieceBytes, s_full[warp], it, s_group[warp]);
+        sum_span(pr, qr, v0, v1, p.per_group, s_ring + (size_t)warp * kRing * 2 * kPieceBytes, s_full[warp], it, copies,
+                 s_group[warp]);
     if (lane == 0) s_warp[warp] = sum;
     __syncthreads();
     if (threadIdx.x < ranks) {
