@@ -6,7 +6,10 @@ import math
 import numpy as np
 import torch
 
-ROUND = {torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -12}   # unit roundoff of the types
+# Half the unit roundoff of the types: what a rounding is off by on average.  (The
+# largest is twice that; what the probabilities' errors have in common cancels
+# in the division by the sum of the rounded ones.)
+ROUND = {torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -12}
 
 
 def attend(q, k, v, lens, prefix_k=None, prefix_v=None, scale=None):
