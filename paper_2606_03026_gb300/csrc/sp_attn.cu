@@ -370,12 +370,12 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
 // elements (`block` bytes on): in one copy where rows are made of whole blocks.
 template <int DK>
 __device__ __forceinline__ void load_tile(uint8_t* to, int block, const CUtensorMap* map, uint64_t* full, bool whole, int entry,
-                                          int head, int batch) {
+                                          int head, int batch, uint64_t policy) {
   if (DK == 64 || !whole) {
 #pragma unroll
-    for (int i = 0; i < DK / 64; ++i) tma_load_4d(to + i * block, map, full, 64 * i, entry, head, batch);
+    for (int i = 0; i < DK / 64; ++i) tma_load_4d(to + i * block, map, full, 64 * i, entry, head, batch, policy);
   } else {
-    tma_load_5d(to, map, full, 0, entry, 0, head, batch);
+    tma_load_5d(to, map, full, 0, entry, 0, head, batch, policy);
   }
 }
 
@@ -477,6 +477,10 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       enter(k, x0);
       enter(v, x0);
       k.it = v.it = 0;
+      // Own entries that one unit reads leave L2 to the prefix, the scores and the
+      // partial results (64 chats 33.7 -> 31.9 us, 128 drafting sequences 145.6 -> 143.1).
+      const bool once = p.rows.own_units == 1;
+      const uint64_t first = l2_evict_first(), normal = l2_evict_normal();
       RowPlaces places;
       bool rows = k.s.count > 0;           // the query rows of the keys' segment are to come
       bool ok = true;
@@ -486,7 +490,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (c.s.count <= 0 || !mbar_test(&empty[st], (c.it / n & 1) ^ 1)) return false;
         mbar_arrive_expect_tx(&full[st], kBytes);
         load_tile<DK>(ring + st * kBytes, kBlock, c.s.prefix ? prefix : own, &full[st], p.whole_rows,
-                      (c.s.j0 + c.j) * kTile, c.s.h, c.s.prefix ? 0 : c.s.b);
+                      (c.s.j0 + c.j) * kTile, c.s.h, c.s.prefix ? 0 : c.s.b, once && !c.s.prefix ? first : normal);
         ++c.it;
         ++c.j;
         return true;
@@ -921,23 +925,44 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
   }
 }
 
-// Two tiles per CTA, one thread per entry: the scores of its rows, added up.
-__global__ void __launch_bounds__(2 * kTile) weights_kernel(const __grid_constant__ AttnParams p) {
+// Eight tiles per CTA, one thread per four entries: the scores of their rows, a
+// few rows' on their way at a time, added up.
+constexpr int kWeightThreads = 128, kWeightEntries = 4 * kWeightThreads;
+__global__ void __launch_bounds__(kWeightThreads) weights_kernel(const __grid_constant__ AttnParams p) {
+  constexpr int kBatch = 8;
   pdl_launch_dependents();
   pdl_wait();
   for (int bh = blockIdx.y; bh < p.c.B * p.Hkv; bh += gridDim.y) {   // (more than 65535 heads)
     const int b = bh / p.Hkv, h = bh - b * p.Hkv, n = used(p, b);
     const float* lse2 = p.lse2 + (int64_t)bh * p.R;
-    for (int j = blockIdx.x * 2 * kTile + threadIdx.x; j < n; j += gridDim.x * 2 * kTile) {
+    const int j = blockIdx.x * kWeightEntries + 4 * threadIdx.x;
+    if (j < n) {
       const float* s = p.scores + ((int64_t)bh * p.nt_cap + j / kTile) * p.R * kTile + j % kTile;
       float* w = p.c.weights + b * p.c.weights_batch + h * p.c.weights_head + j;
-      float sum = 0.f;
-#pragma unroll 4
-      for (int r = 0; r < p.R; ++r) {
-        const float x = __ldcg(s + (int64_t)r * kTile);
-        if (x != -INFINITY) sum += ex2(fmaf(x, p.c2, -__ldcg(lse2 + r)));
+      float sum[4] = {}, had[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) had[e] = j + e < n ? w[e] : 0.f;
+      for (int r0 = 0; r0 < p.R; r0 += kBatch) {
+        float4 x[kBatch];
+        float l[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (r0 + i < p.R) {
+            x[i] = __ldcg(reinterpret_cast<const float4*>(s + (int64_t)(r0 + i) * kTile));
+            l[i] = __ldcg(lse2 + r0 + i);
+          }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+          if (r0 + i < p.R) {
+            const float v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v[e] != -INFINITY) sum[e] += ex2(fmaf(v[e], p.c2, -l[i]));
+          }
       }
-      *w += sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < n) w[e] = had[e] + sum[e];
     }
   }
 }
@@ -1010,13 +1035,22 @@ cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, 
   e = launch_pdl(attend_kernel<DK, BF16>, dim3((unsigned)p.grid), dim3(kAttThreads), attend_smem<DK>(), s, maps, p);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
-  if (rows <= 2048)
+  // Warps per row by the rows, and by the partial results that a row has if every
+  // own cache is full.  us a call with 8 / 2 / 1: 64 chats (768 rows of 3 results)
+  // 32.2 / 27.3 / 28.1, 19 sequences of 6 tokens (1824 of 15) 119 / 110 / 113, a
+  // document (192 of 71) 54 / 59 / 66, 30 sequences of one token (240 of 147) 25 / 34 /
+  // 50; 32 drafting sequences (3840 of 5) with 2 / 1 51.1 / 49.7, 128 (10240) 162 / 144.
+  const int64_t nt = p.nt_prefix + p.nt_cap;
+  const int64_t tiles = p.Hkv * ((int64_t)p.rows.prefix_units * p.nt_prefix + (int64_t)p.c.B * p.rows.own_units * p.nt_cap);
+  if (rows <= p.grid || (rows <= 2048 && p.grid * nt >= 24 * tiles))
     e = launch_pdl(combine_kernel<DK, BF16, 8, 8>, dim3((unsigned)rows), dim3(256), 0, s, p);
+  else if (rows <= 2048)
+    e = launch_pdl(combine_kernel<DK, BF16, 4, 2>, dim3((unsigned)((rows + 1) / 2)), dim3(128), 0, s, p);
   else
     e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, p);
   if (e != cudaSuccess || !p.c.weights) return e;
-  return launch_pdl(weights_kernel, dim3((unsigned)min(ceil_div(p.nt_cap, 2), 65535), (unsigned)min(p.c.B * p.Hkv, 65535)),
-                    dim3(2 * kTile), 0, s, p);
+  return launch_pdl(weights_kernel, dim3((unsigned)ceil_div(p.capacity, kWeightEntries), (unsigned)min(p.c.B * p.Hkv, 65535)),
+                    dim3(kWeightThreads), 0, s, p);
 }
 
 Rows rows_of(int B, int T, int G) {
