@@ -13,11 +13,18 @@
 // first, from histograms that the CTAs of the cluster add up (the first one
 // while the keys are made), and ends where every entry that shares the digits
 // found is kept; ties at a whole key go by slot.  A CTA that is alone ranks the
-// entries of the first digit found one against another instead, when they are
-// few.  Then each warp turns its span into words of kept entries, and counts and
+// entries of the digits found one against another instead, once they are few.
+// Then each warp turns its span into words of kept entries, and counts and
 // ranks of the slots that are left and of the entries that move make a list of
 // moves.  Few moves are made at once, in pieces of 16 bytes; many by a second
-// kernel, whose CTAs take 128 moves each, whatever head they are of.
+// kernel, whose CTAs take 64 moves each, whatever head they are of.
+//
+// Weights and pos have to be read once (8 bytes an entry), and what moves copied
+// once.  Cutting 16 prompts of 3000 to 16384 entries, 8 heads each, to 4096 moves
+// 75 MB in 41.6 us: about 24 us in move_kernel, at what a copy of scattered rows of
+// 128 bytes gets from memory, before it the selection, in a CTA a chain of
+// latencies (keys 5 us, digits 3.5, kept words and list 4).  64 sequences of 2048 to
+// 2056 entries take 7.3 us, one of 1029 4.8: start, keys, one digit, one ranking.
 #include <math.h>
 
 #include "sp_cache.h"
@@ -29,9 +36,13 @@ namespace {
 constexpr int kEvBins = 2048;
 constexpr int kCopies = 8;                 // pieces that a thread has on their way
 constexpr int kFewMoves = 64;              // of a head, made by the kernel that finds them
-constexpr int kMoveBlock = 128;            // of a CTA of the other kernel
+constexpr int kMoveBlock = 64;             // of a CTA of the other kernel
 constexpr int kMoveThreads = 256;
-constexpr int kRanked = kEvBins / 2;       // entries ranked one against another (in a histogram's place)
+// Entries ranked one against another at most, in a histogram's place (64 / 256 / 1024:
+// 16 prompts of up to 16384 cut to 4096 41.0 / 40.9 / 49.1 us a call, 64 heads of
+// 10000 entries 23.2 / 21.3 / 21.3).
+constexpr int kRanked = 256;
+constexpr int kKeysAhead = 8;              // weights and pos of a thread on their way
 constexpr int kEvMaxCluster = 8;
 constexpr int kEvCached = 16 * 1024;       // keys of a CTA held in shared memory
 
@@ -39,7 +50,7 @@ struct EvictParams {
   sp_evict c;
   int32_t Hkv, capacity, cached;           // keys that fit in shared memory
   int32_t row16, row16_log2;               // 16-byte pieces of a K or V row; its logarithm, -1 if it is none
-  int2* moves;                             // [B][Hkv][most_moves]
+  int32_t* moves;                          // [B][Hkv][2][most_moves]: from, to
   int32_t* counts;                         // [B][Hkv], where a second kernel makes the moves; else null
   int32_t most_moves;                      // that a head can have
 };
@@ -61,6 +72,13 @@ __device__ __forceinline__ uint2 ld_cluster2(uint32_t addr) {
   uint2 v;
   asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
   return v;
+}
+
+// Of what every warp has left in its element of `of`: the sum over the warps before this one
+// and that over all of them.
+template <int WARPS> __device__ __forceinline__ uint2 over_warps(const uint32_t* of, int warp, int lane) {
+  const uint32_t v = lane < WARPS ? of[lane] : 0u;
+  return make_uint2(__reduce_add_sync(0xffffffffu, lane < warp ? v : 0u), __reduce_add_sync(0xffffffffu, v));
 }
 
 struct Counts {                            // of one CTA, read by its cluster
@@ -145,17 +163,17 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
   __syncthreads();                         // (the histogram is zero)
   // Weight and pos below the budget go out as they are (those of slots that
   // are left are written again with the moves); all of them make keys.
-  for (int i = w0 + lane; i < w1; i += 32 * 4) {
-    float w[4];
-    int q[4];
+  for (int i = w0 + lane; i < w1; i += 32 * kKeysAhead) {
+    float w[kKeysAhead];
+    int q[kKeysAhead];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < kKeysAhead; ++e)
       if (i + 32 * e < w1) {
         w[e] = __ldg(wt + i + 32 * e);
         q[e] = __ldg(ps + i + 32 * e);
       }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < kKeysAhead; ++e) {
       const int j = i + 32 * e;
       if (j < w1) {
         const uint32_t k = key_of(w[e], q[e], newest);
@@ -212,7 +230,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
     // the next pass's histogram (that of two passes ago, which every CTA has read)
     for (int i = t; i < kEvBins; i += NT) s_hist[(pass + 1) & 1][i] = 0;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) incl += s_warp[0][w];
+    incl += over_warps<kWarps>(s_warp[0], warp, lane).x;
     if (incl >= need && incl - mine < need) {
       uint32_t over = incl - mine;         // entries in higher bins
       bool found = false;
@@ -233,12 +251,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
     const uint32_t share = s_pick[2];      // entries with these digits
     ties = need != share;                  // else all of them are kept
     if (!ties || pass == 2) break;
-    if (pass == 0 && ranks == 1 && share <= kRanked && n <= p.cached && top < kEvBins - 1) {
-      // few: by key, then slot; the kept ones get a key above the digit, the others 0
-      unsigned long long* few = reinterpret_cast<unsigned long long*>(s_hist[1]);
+    if (ranks == 1 && share <= kRanked && n <= p.cached && top < 0xffffffffu >> shift) {
+      // few: by key, then slot; the kept ones get a key above the digits, the others 0
+      unsigned long long* few = reinterpret_cast<unsigned long long*>(s_hist[(pass + 1) & 1]);
       for (int i = w0 + lane; i < w1; i += 32) {
         const uint32_t k = s_keys[i];
-        if (k >> 21 == top) few[atomicAdd(&s_ranked, 1u)] = (unsigned long long)k << 32 | (uint32_t)~i;
+        if (k >> shift == top) few[atomicAdd(&s_ranked, 1u)] = (unsigned long long)k << 32 | (uint32_t)~i;
       }
       __syncthreads();
       for (uint32_t i = t; i < share; i += NT) {
@@ -246,7 +264,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
         uint32_t above = 0;
 #pragma unroll 4
         for (uint32_t e = 0; e < share; ++e) above += few[e] > x;
-        s_keys[~(uint32_t)x] = above < need ? (top + 1) << 21 : 0u;
+        s_keys[~(uint32_t)x] = above < need ? (top + 1) << shift : 0u;
       }
       __syncthreads();
       ties = false;
@@ -267,13 +285,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
     for (int i = w0; i < w1; i += 32) cnt += __popc(__ballot_sync(0xffffffffu, i + lane < w1 && key(i + lane) == top));
     if (lane == 0) s_warp[0][warp] = cnt;
     __syncthreads();
-    uint32_t all = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) tie_at += s_warp[0][w];
-      all += s_warp[0][w];
-    }
+    const uint2 warps = over_warps<kWarps>(s_warp[0], warp, lane);
+    tie_at = warps.x;
     if (ranks > 1) {
-      if (t == 0) s_counts.ties = all;
+      if (t == 0) s_counts.ties = warps.y;
       cluster_sync();
       for (uint32_t r = 0; r < rank; ++r) tie_at += ld_cluster(cluster_addr(&s_counts.ties, r));
     }
@@ -282,7 +297,17 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
   // base + 32 i on that are kept.
   const auto kept_words = [&](int base, uint32_t& tie) {
     uint32_t mine = 0;
-    for (int i = 0; i < 32 && base + 32 * i < w1; ++i) {
+    const int words = min(32, ceil_div(w1 - base, 32));
+    if (!ties && w1 - j0 <= p.cached) {
+#pragma unroll 4
+      for (int i = 0; i < words; ++i) {
+        const int j = base + 32 * i + lane;
+        const uint32_t kept = __ballot_sync(0xffffffffu, j < w1 && s_keys[j - j0] >> shift >= top);
+        if (lane == i) mine = kept;
+      }
+      return mine;
+    }
+    for (int i = 0; i < words; ++i) {
       const int j = base + 32 * i + lane;
       const bool in = j < w1;
       const uint32_t d = in ? key(j) >> shift : 0u;
@@ -307,31 +332,20 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
     holes += __popc(~word & there & below);
     moved += __popc(word & there & ~below);
   }
-  uint32_t holes_in = holes, moved_in = moved;             // with the lanes before
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, holes_in, d), y = __shfl_up_sync(0xffffffffu, moved_in, d);
-    if (lane >= d) holes_in += x, moved_in += y;
-  }
-  if (lane == 31) {
-    s_warp[1][warp] = holes_in;
-    s_warp[2][warp] = moved_in;
+  holes = __reduce_add_sync(0xffffffffu, holes);
+  moved = __reduce_add_sync(0xffffffffu, moved);
+  if (lane == 0) {
+    s_warp[1][warp] = holes;
+    s_warp[2][warp] = moved;
   }
   __syncthreads();
-  uint32_t hole_at = 0, moved_at = 0, all_moved = 0, all_holes = 0;
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) {
-      hole_at += s_warp[1][w];
-      moved_at += s_warp[2][w];
-    }
-    all_holes += s_warp[1][w];
-    all_moved += s_warp[2][w];
-  }
-  uint32_t total = all_moved;
+  const uint2 warp_holes = over_warps<kWarps>(s_warp[1], warp, lane), warp_moved = over_warps<kWarps>(s_warp[2], warp, lane);
+  uint32_t hole_at = warp_holes.x, moved_at = warp_moved.x;
+  uint32_t total = warp_moved.y;
   if (ranks > 1) {
     if (t == 0) {
-      s_counts.holes = all_holes;
-      s_counts.moved = all_moved;
+      s_counts.holes = warp_holes.y;
+      s_counts.moved = warp_moved.y;
     }
     cluster_sync();
     total = 0;
@@ -344,8 +358,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
       total += m;
     }
   }
-  // The list of moves (from, to).
-  int2* moves = p.moves + (int64_t)bh * p.most_moves;
+  // The list of moves: in shared memory where this CTA makes them itself, alone.
+  const bool here = ranks == 1 && !p.counts;
+  int32_t* from = here ? reinterpret_cast<int32_t*>(s_hist[0]) : p.moves + (int64_t)bh * 2 * p.most_moves;
+  int32_t* to = from + (here ? kFewMoves : p.most_moves);
   const bool whole = w1 - w0 <= 1024;      // `word` is still the span's
   tie = tie_at;
   for (int base = w0; base < w1; base += 1024) {
@@ -354,27 +370,32 @@ __global__ void __launch_bounds__(NT, 1024 / NT) evict_kernel(const __grid_const
     }
     const int at = base + 32 * lane;
     const uint32_t there = low(w1 - at), below = low(c.budget - at);
-    uint32_t hole = ~word & there & below, move = word & there & ~below;
-    uint32_t hi = __popc(hole), mi = __popc(move);
-    const uint32_t nh = hi, nm = mi;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, hi, d), y = __shfl_up_sync(0xffffffffu, mi, d);
-      if (lane >= d) hi += x, mi += y;
+    const uint32_t hole = ~word & there & below, move = word & there & ~below, before = (1u << lane) - 1u;
+    const int words = min(32, ceil_div(w1 - base, 32));
+#pragma unroll 4
+    for (int i = 0; i < words; ++i) {
+      const uint32_t hi = __shfl_sync(0xffffffffu, hole, i), mi = __shfl_sync(0xffffffffu, move, i);
+      const int j = base + 32 * i + lane;
+      if (hi >> lane & 1u) to[hole_at + __popc(hi & before)] = j;
+      if (mi >> lane & 1u) from[moved_at + __popc(mi & before)] = j;
+      hole_at += __popc(hi);
+      moved_at += __popc(mi);
     }
-    uint32_t to = hole_at + hi - nh, from = moved_at + mi - nm;
-    for (; hole; hole &= hole - 1) moves[to++].y = at + __ffs(hole) - 1;
-    for (; move; move &= move - 1) moves[from++].x = at + __ffs(move) - 1;
-    hole_at += __shfl_sync(0xffffffffu, hi, 31);
-    moved_at += __shfl_sync(0xffffffffu, mi, 31);
   }
   if (p.counts) {
     if (rank == 0 && t == 0) p.counts[bh] = total;
     if (ranks > 1) cluster_sync();         // no CTA leaves while its counts may be read
     return;
   }
-  if (ranks > 1) cluster_sync(); else __syncthreads();
-  make_moves<kCopies>(p, b, h, total, rank * NT + t, ranks * NT, [&](uint32_t i) { return __ldcg(moves + i); });
+  if (here) {
+    const int32_t* list = reinterpret_cast<const int32_t*>(s_hist[0]);
+    __syncthreads();
+    make_moves<kCopies>(p, b, h, total, t, NT, [&](uint32_t i) { return make_int2(list[i], list[kFewMoves + i]); });
+  } else {
+    cluster_sync();
+    make_moves<kCopies>(p, b, h, total, rank * NT + t, ranks * NT,
+                        [&](uint32_t i) { return make_int2(__ldcg(from + i), __ldcg(to + i)); });
+  }
 }
 
 // CTA (i, bh): moves kMoveBlock i .. of the list of head bh.
@@ -386,7 +407,10 @@ __global__ void __launch_bounds__(kMoveThreads, 5) move_kernel(const __grid_cons
   const uint32_t total = __ldcg(p.counts + bh);
   if (first >= total) return;
   const uint32_t count = min((uint32_t)kMoveBlock, total - first);
-  if (threadIdx.x < count) s_moves[threadIdx.x] = __ldcg(p.moves + (int64_t)bh * p.most_moves + first + threadIdx.x);
+  if (threadIdx.x < count) {
+    const int32_t* from = p.moves + (int64_t)bh * 2 * p.most_moves + first + threadIdx.x;
+    s_moves[threadIdx.x] = make_int2(__ldcg(from), __ldcg(from + p.most_moves));
+  }
   __syncthreads();
   make_moves<4>(p, bh / p.Hkv, bh % p.Hkv, count, threadIdx.x, kMoveThreads, [&](uint32_t i) { return s_moves[i]; });
 }
@@ -430,18 +454,18 @@ cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cu
   p.row16_log2 = -1;
   for (int i = 0; i < 8; ++i)
     if (p.row16 == 1 << i) p.row16_log2 = i;
-  p.moves = reinterpret_cast<int2*>(ws + cache_workspace(s, sms).moves);
+  p.moves = reinterpret_cast<int32_t*>(ws + cache_workspace(s, sms).moves);
   const int heads = c.B * s.Hkv;
   // (n - budget entries go, budget stay: no more moves than the fewer of them)
   p.most_moves = max(0, min(c.budget, s.capacity - c.budget));
   p.counts = p.most_moves > kFewMoves ? reinterpret_cast<int32_t*>(ws + cache_workspace(s, sms).counts) : nullptr;
   // Clusters where four CTAs would find an SM each per head, and 8192 entries:
-  // us a call with 1 / 2 / 4 / 8 CTAs of 1024 threads: 1 head of 40000 entries
-  // 72 / 40 / 23.6 / 22.8, 16 heads of 20000 58 / 46 / 43 / 57; beyond, the adding up
-  // of histograms costs more than it saves (64 heads of 10000 23.3 / 25.5 / 35 / 79).
-  // Threads by what fits the SMs in one wave, no more than the entries need: 512 /
-  // 1024 threads: 4 heads of 1029 entries 6.0 / 7.5, 256 heads of 2056 9.3 / 16.5,
-  // 128 heads of 16384 88 / 75; 256 / 512: 1024 heads of 2000 23 / 32.
+  // us a call with 1 / 2 / 4 / 8 CTAs: 1 head of 40000 entries 64 / 32 / 15.1 / 15.7,
+  // 16 heads of 20000 40 / 29 / 27.8 / 46; beyond, the adding up of histograms costs
+  // more than it saves (64 heads of 10000 18.1 / 19.4 / 28).
+  // Threads by what fits the SMs in one wave, no more than the entries need: 256 / 512 /
+  // 1024: 4 heads of 1029 entries 5.0 / 5.0 / 5.4, 256 heads of 2056 8.9 / 7.3 / 12, 128
+  // heads of 16384 54 / 44 / 41.7, 1024 heads of 2000 17.7 / 26 / 44.
   int cluster = 1;
   while (cluster < kEvMaxCluster && 4 * cluster * heads <= sms && s.capacity >= 8192 * cluster) cluster *= 2;
   int nt = heads * cluster > 2 * sms ? 256 : heads * cluster > sms || s.capacity <= 4096 * cluster ? 512 : 1024;
