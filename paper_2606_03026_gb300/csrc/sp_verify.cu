@@ -9,7 +9,7 @@
 // One thread-block cluster per sequence: its CTAs take contiguous slices of the
 // row, their warps contiguous spans of the slice.  A warp streams its span of
 // both rows through a ring in shared memory of its own, in pieces of 512 entries
-// (bulk copies: all that the ring holds is on its way, 96 KB per CTA), and keeps
+// (bulk copies: all that the ring holds is on its way, 64 KB per CTA), and keeps
 // the sums of up to kGroups groups of pieces.  The spans' sums meet in shared
 // memory, the slices' in every CTA's (distributed shared memory).  The CTA whose
 // slice the running sum passes c in reads the one group where it does again,
@@ -28,7 +28,7 @@ constexpr int kVerMaxCluster = 16;
 constexpr int kVerPerSm = 2;               // CTAs that an SM holds
 constexpr int kPiece = 512;                // entries of a bulk copy
 constexpr int kPieceBytes = 4 * kPiece + 32;   // and what lies around them in its 16-byte pieces
-constexpr int kRing = 3;                   // pieces of each row per warp
+constexpr int kRing = 2;                   // pieces of each row per warp
 constexpr int kGroups = 64;
 constexpr size_t kVerSmem = (size_t)kVerWarps * kRing * 2 * kPieceBytes;
 
