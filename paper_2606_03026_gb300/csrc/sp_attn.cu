@@ -15,11 +15,12 @@
 // (which only the device knows); a CTA's run of tiles within a unit is a
 // segment, which leaves its sum over V, its maximum and its sums of
 // exponentials in a slot of the workspace.  Per CTA (192 threads):
-//   warp 4      one thread issues copies (TMA): the query rows of a segment (a box of G heads x T tokens,
-//               for the prefix x as many sequences as 128 rows hold), K tiles and V
-//               tiles into rings, each as soon as its place is free.
-//   warp 5      one thread issues S = Q K^T one tile ahead of O += P V (tcgen05,
-//               M = 128, P from tensor memory, V as an N-major operand).
+//   warp 4      one thread issues copies (TMA): the query rows of a segment (a
+//               box of G heads x T tokens, for the prefix x as many sequences as
+//               128 rows hold), K tiles and V tiles into rings, each as soon as
+//               its place is free.
+//   warp 5      S = Q K^T one tile ahead of O += P V (tcgen05, M = 128, P from
+//               tensor memory, V as an N-major operand).
 //   warps 0-3   the softmax, thread = row = tensor-memory lane: per tile they
 //               read the 64 scores of their row, keep the running maximum and
 //               sums, and put the probabilities, rounded to the type, back over
@@ -35,9 +36,27 @@
 // entries, of which the query tokens see 0, 1, .. T - 1, are left to
 // combine_kernel, so that no masked probability ever meets a value.
 //
-// combine_kernel: one or eight warps per query row merge its partial results and
-// these last entries.  weights_kernel: the weights, from the scores of the own
-// entries that attend_kernel left in the workspace and the rows' lse.
+// What bounds it: K and V from memory where few rows share an entry, the tensor
+// cores where 128 do (their rate at N = 64, where Q is read from shared memory
+// again for every tile, is 5/8 of the peak for 128-wide heads), and in between a
+// tile's way from S through the softmax to P, of which two CTAs have one each on
+// their way per SM: about 1500 cycles a tile and CTA, of which the softmax's
+// arithmetic is 370 at full rate.  Tiles of 64 entries with the scores one tile
+// ahead, because tensor memory holds no more for 128-wide heads and two CTAs (128
+// entries without: 128 drafting sequences 291 us, with 64: 212 at that state).
+// Measured (a call, its three kernels together): 128 sequences of 5 tokens, 16 query
+// heads on 4 of 128, prefix 16384, own 512 to 2048, with weights: 143 us, the floor of
+// its bytes 56, of its operations 48, tensor pipe busy 73 % in attend_kernel (113 us);
+// 16 sequences over a document of 131072: 54 us, 5.1 TB/s; 64 chats over 2048 with own
+// caches of up to 1024: 26.6 us (floor 10.7), the kernel itself 21; 32 drafting sequences
+// with 64-wide heads over 8191: 48 us (floor 13); one sequence of 60 entries over 512:
+// 10.2 us, two launches' latency.
+//
+// combine_kernel: one to eight warps per query row merge its partial results and
+// these last entries; latency, and for many rows the instructions of a row (10240
+// rows 14 us).  weights_kernel: the weights, from the scores of the own entries that
+// attend_kernel left in the workspace and the rows' lse; 4 bytes written and read
+// per own entry and query row (128 drafting sequences: 52 MB, 13 us).
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cudaTypedefs.h>

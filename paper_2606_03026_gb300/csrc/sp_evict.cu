@@ -20,9 +20,9 @@
 // kernel, whose CTAs take 64 moves each, whatever head they are of.
 //
 // Weights and pos have to be read once (8 bytes an entry), and what moves copied
-// once.  Cutting 16 prompts of 3000 to 16384 entries, 8 heads each, to 4096 moves
-// 75 MB in 41.6 us: about 24 us in move_kernel, at what a copy of scattered rows of
-// 128 bytes gets from memory, before it the selection, in a CTA a chain of
+// once.  Cutting 16 prompts of 3000 to 16384 entries, 8 heads each, to 4096 reads and
+// writes 150 MB, 22 us of memory, in 41.6 us: about 24 us in move_kernel, whose rows
+// of 128 bytes lie scattered, and before it the selection, in a CTA a chain of
 // latencies (keys 5 us, digits 3.5, kept words and list 4).  64 sequences of 2048 to
 // 2056 entries take 7.3 us, one of 1029 4.8: start, keys, one digit, one ranking.
 #include <math.h>
