@@ -399,15 +399,17 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
 }
 
 // One tile of entries into shared memory, 64 elements of all of them after 64
-// elements (`block` bytes on): in one copy where rows are made of whole blocks.
+// elements: in one copy where rows are made of whole blocks.  The whole warp
+// executes it, the lane with `issue` copies.
 template <int DK>
-__device__ __forceinline__ void load_tile(uint8_t* to, int block, const CUtensorMap* map, uint64_t* full, bool whole, int entry,
-                                          int head, int batch, uint64_t policy) {
+__device__ __forceinline__ void load_tile(uint32_t issue, uint8_t* to, const CUtensorMap* map, uint64_t* full, bool whole,
+                                          int entry, int head, int batch, uint64_t policy) {
   if (DK == 64 || !whole) {
 #pragma unroll
-    for (int i = 0; i < DK / 64; ++i) tma_load_4d(to + i * block, map, full, 64 * i, entry, head, batch, policy);
+    for (int i = 0; i < DK / 64; ++i)
+      tma_load_4d_if(issue, to + i * kBlock, map, full, 64 * i, entry, head, batch, policy);
   } else {
-    tma_load_5d(to, map, full, 0, entry, 0, head, batch, policy);
+    tma_load_5d_if(issue, to, map, full, 0, entry, 0, head, batch, policy);
   }
 }
 
@@ -490,90 +492,115 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   const uint32_t tmem = *s_tmem;
   const Line line = line_of(p, s_off[kGroups], gridDim.x);
   const int cta = blockIdx.x;
-  const int x0 = cta < line.ctas ? line.first(cta) : 0, x1 = cta < line.ctas ? line.first(cta + 1) : 0;
+  // (the same in every thread; taken from one, the compiler knows it)
+  const int x0 = __shfl_sync(0xffffffffu, cta < line.ctas ? line.first(cta) : 0, 0);
+  const int x1 = __shfl_sync(0xffffffffu, cta < line.ctas ? line.first(cta + 1) : 0, 0);
 
   if (warp == 4) {
     // ------------------------------ TMA -----------------------------------------
-    if (lane == 0) {
-      // where the keys and where the values are: a tile of a segment
-      struct Cursor {
-        Segment s;
-        int j, it;
-      };
-      Cursor k, v;
-      const auto enter = [&](Cursor& c, int x) {
-        c.j = 0;
-        c.s.count = 0;
-        if (x < x1) c.s = segment_at(p, line, s_off, x, x1, cta);
-      };
-      enter(k, x0);
-      enter(v, x0);
-      k.it = v.it = 0;
-      // Own entries that one unit reads leave L2 to the prefix, the scores and the
-      // partial results (64 chats 33.7 -> 31.9 us, 128 drafting sequences 145.6 -> 143.1).
-      const bool once = p.rows.own_units == 1;
-      const uint64_t first = l2_evict_first(), normal = l2_evict_normal();
-      RowPlaces places;
-      bool rows = k.s.count > 0;           // the query rows of the keys' segment are to come
-      bool ok = true;
-      const auto issue = [&](Cursor& c, int n, uint8_t* ring, uint64_t* full, uint64_t* empty, const CUtensorMap* prefix,
-                             const CUtensorMap* own) {
-        const int st = c.it % n;
-        if (c.s.count <= 0 || !mbar_test(&empty[st], (c.it / n & 1) ^ 1)) return false;
-        mbar_arrive_expect_tx(&full[st], kBytes);
-        load_tile<DK>(ring + st * kBytes, kBlock, c.s.prefix ? prefix : own, &full[st], p.whole_rows,
-                      (c.s.j0 + c.j) * kTile, c.s.h, c.s.prefix ? 0 : c.s.b, once && !c.s.prefix ? first : normal);
-        ++c.it;
-        ++c.j;
-        return true;
-      };
-      long long since = clock64();
-      while (k.s.count > 0 || v.s.count > 0) {
-        bool moved = false;
-        // (a segment's keys may go ahead of its query rows, the next one's not)
-        if (k.j < k.s.count) moved = issue(k, NK, sK, k_full, k_empty, &maps.pk, &maps.k);
-        if (rows) {
-          const Segment& s = k.s;
-          const int box = s.prefix ? p.rows.prefix_rows : p.rows.own_rows, halves = places.of(box);
-          if (((halves & 1) == 0 || mbar_test(&q_empty[0], places.used & 1 ^ 1)) &&
-              ((halves & 2) == 0 || mbar_test(&q_empty[1], places.used >> 1 ^ 1))) {
-            const int head = s.h * p.G + s.m % p.rows.head_tiles * p.rows.heads;
-            const int token = s.m / p.rows.head_tiles * p.rows.tokens;
-            uint64_t* full = &q_full[halves == 2];
-            mbar_arrive_expect_tx(full, DK / 64 * 128 * box);
-            if (halves == 3) mbar_arrive(&q_full[1]);
-            for (int i = 0; i < DK / 64; ++i)
-              tma_load_4d(sQ + i * kQBlock + (halves == 2 ? kQBlock / 2 : 0), s.prefix ? &maps.pq : &maps.q, full, 64 * i,
-                          head, token, s.b);
-            places.take(halves);
-            rows = false;
-            moved = true;
-          }
-        }
-        if (k.j == k.s.count && k.s.count > 0 && !rows) {
-          enter(k, k.s.next);
-          rows = k.s.count > 0;
-        }
-        if (issue(v, NV, sV, v_full, v_empty, &maps.pv, &maps.v)) {
+    // The whole warp walks the tiles and one lane issues, by predicate (as the
+    // MMAs below: by a branch of lane 0 a tile's two copies took this warp about
+    // 1000 cycles, and everything else waited for it).
+    const uint32_t one = elect_one();
+    const auto all = [](bool x) { return __all_sync(0xffffffffu, x) != 0; };
+    const auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    // where the keys and where the values are: a tile of a segment
+    struct Cursor {
+      int count, j, entry, h, b, m, next, prefix;
+      int st, phase;                       // place in the ring, how often it has gone round
+    };
+    const auto enter = [&](Cursor& c, int x) {
+      c.j = c.count = 0;
+      if (x >= x1) return;
+      const Segment s = segment_at(p, line, s_off, x, x1, cta);
+      c.count = uniform(s.count);
+      c.entry = uniform(s.j0 * kTile);
+      c.h = uniform(s.h);
+      c.b = uniform(s.b);
+      c.m = uniform(s.m);
+      c.next = uniform(s.next);
+      c.prefix = uniform(s.prefix);
+    };
+    Cursor k, v;
+    enter(k, x0);
+    v = k;
+    k.st = v.st = k.phase = v.phase = 0;
+    // Own entries that one unit reads leave L2 to the prefix, the scores and the
+    // partial results (64 chats 33.7 -> 31.9 us, 128 drafting sequences 145.6 -> 143.1).
+    const uint64_t normal = l2_evict_normal(), own = p.rows.own_units == 1 ? l2_evict_first() : normal;
+    RowPlaces places;
+    bool rows = k.count > 0;               // the query rows of the keys' segment are to come
+    const auto issue = [&](Cursor& c, int n, uint8_t* ring, uint64_t* full, const CUtensorMap* of_prefix,
+                           const CUtensorMap* of_own) {
+      mbar_arrive_expect_tx_if(one, &full[c.st], kBytes);
+      load_tile<DK>(one, ring + c.st * kBytes, c.prefix ? of_prefix : of_own, &full[c.st], p.whole_rows, c.entry, c.h,
+                    c.prefix ? 0 : c.b, c.prefix ? normal : own);
+      c.entry += kTile;
+      ++c.j;
+      if (++c.st == n) {
+        c.st = 0;
+        ++c.phase;
+      }
+    };
+    bool ok = true;
+    int idle = 0;
+    long long since = 0;
+    while (k.count > 0 || v.count > 0) {
+      // (a segment's keys may go ahead of its query rows, the next one's not)
+      const bool k_free = mbar_test(&k_empty[k.st], k.phase & 1 ^ 1), v_free = mbar_test(&v_empty[v.st], v.phase & 1 ^ 1);
+      bool moved = false;
+      if (k.j < k.count && all(k_free)) {
+        issue(k, NK, sK, k_full, &maps.pk, &maps.k);
+        moved = true;
+      }
+      if (v.count > 0 && all(v_free)) {
+        issue(v, NV, sV, v_full, &maps.pv, &maps.v);
+        if (v.j == v.count) enter(v, v.next);
+        moved = true;
+      }
+      if (rows) {
+        const int box = k.prefix ? p.rows.prefix_rows : p.rows.own_rows, halves = places.of(box);
+        if (all(((halves & 1) == 0 || mbar_test(&q_empty[0], places.used & 1 ^ 1)) &&
+                ((halves & 2) == 0 || mbar_test(&q_empty[1], places.used >> 1 ^ 1)))) {
+          const int head = k.h * p.G + k.m % p.rows.head_tiles * p.rows.heads;
+          const int token = k.m / p.rows.head_tiles * p.rows.tokens;
+          uint64_t* full = &q_full[halves == 2];
+          mbar_arrive_expect_tx_if(one, full, DK / 64 * 128 * box);
+          if (halves == 3) mbar_arrive_expect_tx_if(one, &q_full[1], 0);
+          for (int i = 0; i < DK / 64; ++i)
+            tma_load_4d_if(one, sQ + i * kQBlock + (halves == 2 ? kQBlock / 2 : 0), k.prefix ? &maps.pq : &maps.q, full, 64 * i,
+                           head, token, k.b, normal);
+          places.take(halves);
+          rows = false;
           moved = true;
-          if (v.j == v.s.count) enter(v, v.s.next);
         }
-        if (moved) {
-          since = clock64();
-        } else if (*s_abort || clock64() - since > kWaitLimitCycles) {
+      }
+      if (k.j == k.count && k.count > 0 && !rows) {
+        enter(k, k.next);
+        rows = k.count > 0;
+      }
+      if (moved) {
+        idle = 0;
+      } else {
+        if (idle++ == 0) since = clock64();
+        if (!all(!*s_abort && clock64() - since <= kWaitLimitCycles)) {
           ok = false;
           break;
         }
       }
-      if (!ok) {
-        *s_abort = 1;
-        atomicExch(p.err, kErrMbarTimeout);
-        for (int i = 0; i < 2; ++i) wait(&q_full[i], places.used >> i & 1 ^ 1);
-      }
-      // the last copies have landed
-      for (int i = max(0, k.it - NK); i < k.it; ++i) wait(&k_full[i % NK], i / NK & 1);
-      for (int i = max(0, v.it - NV); i < v.it; ++i) wait(&v_full[i % NV], i / NV & 1);
     }
+    if (!ok) {
+      *s_abort = 1;
+      atomicExch(p.err, kErrMbarTimeout);
+      for (int i = 0; i < 2; ++i) wait(&q_full[i], places.used >> i & 1 ^ 1);
+    }
+    // the last copies have landed
+    const auto landed = [&](const Cursor& c, int n, uint64_t* full) {
+      for (int i = 0; i < n; ++i)
+        if (i < c.st || c.phase > 0) wait(&full[i], (i < c.st ? c.phase : c.phase - 1) & 1);
+    };
+    landed(k, NK, k_full);
+    landed(v, NV, v_full);
   } else if (warp == 5) {
     // ------------------------------ MMA -----------------------------------------
     // The whole warp walks the tiles and one lane issues, by predicate: operands
