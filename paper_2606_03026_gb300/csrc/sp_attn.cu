@@ -82,6 +82,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Tiles of K and of V on their way: what two CTAs of an SM have room for.
 template <int DK> constexpr int kStagesK = DK == 64 ? 5 : 3;
 template <int DK> constexpr int kStagesV = DK == 64 ? 5 : 2;
+// With 64-wide heads the product with V has 16 more columns, of ones: the sum of
+// the rounded probabilities, for which tensor memory has no room at 128.
+template <int DK> constexpr int kOnes = DK == 64 ? 16 : 0;
 template <int DK> constexpr int kQBytes = DK / 64 * kQBlock;
 template <int DK> constexpr int kTileBytes = DK / 64 * kBlock;
 
@@ -286,11 +289,11 @@ __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy
 
 // An operand whose rows run along the MMA's N: 64 elements (128 bytes,
 // swizzled) per row of K, 8 rows of K 1024 bytes apart, the next 64 elements
-// of N kBlock on.
-__device__ __forceinline__ uint64_t n_major_desc(const void* p) {
+// of N `block` bytes on.
+__device__ __forceinline__ uint64_t n_major_desc(const void* p, uint32_t block) {
   uint64_t d = smem_desc(p, 1024, kSwizzle128);
   d &= ~((uint64_t)0x3FFF << 16);
-  return d | (uint64_t)(kBlock >> 4) << 16;
+  return d | (uint64_t)(block >> 4) << 16;
 }
 
 // Bounded wait, inline (a call would cost the softmax's loop its registers);
@@ -364,7 +367,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
       if (!__all_sync(0xffffffffu, wait(pv, pv_parity))) return false;
       tc_fence_after();
 #pragma unroll 1                           // (rare, and registers are short)
-      for (int i = 0; i < DK / 16; ++i) {
+      for (int i = 0; i < (DK + kOnes<DK>) / 16; ++i) {
         uint32_t o[16];
         tmem_ld16_issue(o_buf + 16 * i, o);
         tmem_ld_wait();
@@ -387,7 +390,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
       const float2 y = make_float2(ex2(x.x), ex2(x.y));
       pk[i] = pack2<BF16>(y.x, y.y);
       sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
-      add_halves<BF16>(pk[i], rsum[i % 2 * 2], rsum[i % 2 * 2 + 1]);
+      if (kOnes<DK> == 0) add_halves<BF16>(pk[i], rsum[i % 2 * 2], rsum[i % 2 * 2 + 1]);
     }
     tmem_st16_issue(s_buf + 16 * g, pk);
   }
@@ -419,12 +422,13 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   constexpr int NK = kStagesK<DK>, NV = kStagesV<DK>, kBytes = kTileBytes<DK>;
   constexpr uint32_t kType = BF16 ? 1u << 7 | 1u << 10 : 0u;
   constexpr uint32_t kIdescS = 1u << 4 | kType | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
-  constexpr uint32_t kIdescO = 1u << 4 | kType | 1u << 16 | (uint32_t)(DK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+  constexpr uint32_t kIdescO = 1u << 4 | kType | 1u << 16 | (uint32_t)((DK + kOnes<DK>) >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* sQ = smem;
   uint8_t* sK = sQ + kQBytes<DK>;
   uint8_t* sV = sK + NK * kBytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sV + NV * kBytes);
+  uint8_t* s_ones = sV + NV * kBytes;       // as a tile of 64 elements, where there are ones
+  uint64_t* bars = reinterpret_cast<uint64_t*>(s_ones + (kOnes<DK> ? kBlock : 0));
   uint64_t *k_full = bars, *k_empty = bars + NK, *v_full = bars + 2 * NK, *v_empty = v_full + NV;
   uint64_t *s_full = v_empty + NV, *p_full = s_full + 2;   // [2]: by score buffer
   uint64_t *q_full = p_full + 2, *q_empty = q_full + 2,     // [2]: by half of the rows' place
@@ -465,6 +469,11 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     tma_prefetch_desc(&maps.v);
   }
   if (warp == 5) tmem_alloc(s_tmem, kTmemCols);
+  if (kOnes<DK>) {
+    for (int i = threadIdx.x; i < kBlock / 4; i += kAttThreads)
+      reinterpret_cast<uint32_t*>(s_ones)[i] = BF16 ? 0x3f803f80u : 0x3c003c00u;
+    fence_async_shared();
+  }
   pdl_launch_dependents();
   pdl_wait();
 
@@ -651,7 +660,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
                    wait(&p_full[it & 1], (it >> 1) & 1, s_abort));
         if (!ok) break;
         tc_fence_after();
-        const uint64_t vd = n_major_desc(sV + st * kBytes);
+        const uint64_t vd = n_major_desc(sV + st * kBytes, kOnes<DK> ? (NV - st) * kBytes : kBlock);
 #pragma unroll
         for (int k = 0; k < kTile / 16; ++k)
           mma_f16_ta_if(one, tmem + kTmemO, tmem + (it & 1) * kTile + 8 * k, vd + k * (2048 >> 4), kIdescO, j > 0 || k > 0);
@@ -725,6 +734,13 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       if (work) {
         const int64_t at = s.slot * (s.prefix ? kRows : p.rows.own_rows) + row;
         float* o = (s.prefix ? p.p_o : p.o_o) + at * DK;
+        if (kOnes<DK>) {
+          uint32_t x[16];
+          tmem_ld16_issue(lanes + kTmemO + DK, x);
+          tmem_ld_wait();
+          reg_pin(x);
+          r.rl = __uint_as_float(x[0]);
+        }
         if (mine) (s.prefix ? p.p_ml : p.o_ml)[at] = make_float4(r.ref, r.l, r.rl, 0.f);
 #pragma unroll 1
         for (int i = 0; i < DK / 32; ++i) {
@@ -1077,7 +1093,7 @@ bool encode_kv(CUtensorMap* map, bool bf16, const void* base, int D, const int64
 
 template <int DK>
 constexpr size_t attend_smem() {
-  return kQBytes<DK> + (size_t)(kStagesK<DK> + kStagesV<DK>) * kTileBytes<DK> +
+  return kQBytes<DK> + (size_t)(kStagesK<DK> + kStagesV<DK>) * kTileBytes<DK> + (kOnes<DK> ? kBlock : 0) +
          (2 * kStagesK<DK> + 2 * kStagesV<DK> + 11) * 8 + 8 + 32 + (kGroups + 1) * 4;
 }
 
