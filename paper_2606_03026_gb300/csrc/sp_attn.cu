@@ -775,17 +775,19 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
 }
 
 // ---- merging ------------------------------------------------------------------
-// A lane has DK / 32 elements of a row: lane * DK / 32 ...
-template <int DK>
-__device__ __forceinline__ void load_raw(const void* base, int64_t at, int D, int lane, uint32_t (&w)[DK / 64]) {
-  const uint16_t* p = static_cast<const uint16_t*>(base) + at + lane * (DK / 32);
+// A lane has E consecutive elements of a row, from l * E on.
+template <int E>
+__device__ __forceinline__ void load_raw(const void* base, int64_t at, int D, int l, uint32_t (&w)[E / 2]) {
+  const uint16_t* p = static_cast<const uint16_t*>(base) + at + l * E;
 #pragma unroll
-  for (int i = 0; i < DK / 64; ++i) w[i] = 0u;
-  if (lane * (DK / 32) < D) {              // (D is a multiple of 8)
-    if constexpr (DK == 128) {
+  for (int i = 0; i < E / 2; ++i) w[i] = 0u;
+  if (l * E < D) {                         // (D is a multiple of 8)
+    if constexpr (E == 8) {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+      w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else if constexpr (E == 4) {
       const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
-      w[0] = u.x;
-      w[1] = u.y;
+      w[0] = u.x, w[1] = u.y;
     } else {
       w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
     }
@@ -807,33 +809,40 @@ template <int E> struct Part {
   }
 };
 
-constexpr int kLast = 4;                   // last entries that a warp has on their way
-
-// WPR warps of a CTA of W per query row, each with its share of the row's
-// partial results and of its last entries.  Two rounds of loads: what the shares
-// are, and what they hold.
+// W warps of a CTA; per query row WPR of them, each with its share of the row's
+// partial results and of its last entries, or where there are many rows half a
+// one.  Two rounds of loads: what the shares are, and what they hold.
+template <int DK, int W, int WPR> constexpr int kCombineCtas = WPR == 1 ? 5 : (DK == 64 ? 24 : 16) / W;   // per SM
 template <int DK, bool BF16, int W, int WPR>
-__global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const __grid_constant__ AttnParams p) {
-  constexpr int E = DK / 32, kBatch = WPR > 1 ? 8 : 4;     // results on their way
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % WPR;
+__global__ void __launch_bounds__(32 * W, kCombineCtas<DK, W, WPR>) combine_kernel(const __grid_constant__ AttnParams p) {
+  constexpr int L = WPR > 1 ? 32 : 16, E = DK / L;             // lanes of a row, elements of a lane
+  constexpr int kBatch = WPR > 1 ? 8 : 16 / E, kLast = WPR > 1 ? 4 : 2;    // results and last entries on their way
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % L, sub = warp % WPR;
+  // over the lanes of a row; of the rows of a warp the larger
+  const auto row_max = [](float x) {
+#pragma unroll
+    for (int d = L / 2; d >= 1; d >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+    return x;
+  };
+  const auto row_sum = [](float x) {
+#pragma unroll
+    for (int d = L / 2; d >= 1; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    return x;
+  };
+  const auto larger = [](int x) { return L == 32 ? x : max(x, __shfl_xor_sync(0xffffffffu, x, 16)); };
   pdl_launch_dependents();
   pdl_wait();
-  const uint32_t id = blockIdx.x * (W / WPR) + warp / WPR;     // (b, h, row)
+  const uint32_t id = (blockIdx.x * (W / WPR) + warp / WPR) * (32 / L) + lane / L;     // (b, h, row)
   const bool real = id < (uint32_t)(p.c.B * p.Hkv * p.R);
   Part<E> a;
   a.m = -INFINITY;
   a.l = a.r = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) a.o[i] = 0.f;
-  int b = 0, h = 0, t = 0, hq = 0;
-  if (real) {
-    const uint32_t bh = id / (uint32_t)p.R;
-    const int rr = id - bh * p.R;
-    b = bh / (uint32_t)p.Hkv;
-    h = bh - b * p.Hkv;
-    t = (uint32_t)rr / (uint32_t)p.G;
-    const int g = rr - t * p.G;
-    hq = h * p.G + g;
+  const uint32_t bh = real ? id / (uint32_t)p.R : 0;
+  const int rr = real ? id - bh * p.R : 0, b = bh / (uint32_t)p.Hkv, h = bh - b * p.Hkv;
+  const int t = (uint32_t)rr / (uint32_t)p.G, g = rr - t * p.G, hq = h * p.G + g;
+  {
     const Rows& rw = p.rows;
     int m = 0, ro = rr;                                        // tile of the sequence, row of the tile
     if (rw.per_seq > 1) {
@@ -843,13 +852,13 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
     const int group = (uint32_t)b / (uint32_t)rw.seqs;
     const int up = h * rw.prefix_units + group * rw.per_seq + m, prefix_units = p.Hkv * rw.prefix_units;
     const int64_t uo = (int64_t)(b * p.Hkv + h) * rw.own_units + m;
-    const int n = used(p, b);
+    const int n = real ? used(p, b) : 0;
     int2 cp = make_int2(0, -1), co = make_int2(0, -1);         // CTAs of the row's prefix unit, of its own one
     const auto ctas = [&](int64_t unit) {                      // (in range also where attend_kernel gave up)
       const int2 x = __ldcg(p.unit_ctas + unit);
       return make_int2(max(x.x, 0), min(x.y, p.grid - 1));
     };
-    if (p.nt_prefix > 0) cp = ctas(up);
+    if (real && p.nt_prefix > 0) cp = ctas(up);
     if (n > p.c.T - 1) co = ctas(prefix_units + uo);
     // partial results: np of the prefix unit, no of the own one
     const int np = cp.y - cp.x + 1, no = co.y - co.x + 1;
@@ -858,66 +867,61 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
     // the last T - 1 own entries, of which this row sees the first few: j_first
     // on, this warp every WPR-th, the first kLast on their way from here
     const int far = n - (p.c.T - 1 - t), j_first = p.c.T > 1 ? max(0, n - (p.c.T - 1)) + sub : n;
-    uint32_t qw[DK / 64], kw[kLast][DK / 64], vw[kLast][DK / 64];
+    uint32_t qw[E / 2], kw[kLast][E / 2], vw[kLast][E / 2];
     const auto fetch = [&](int j0) {
 #pragma unroll
       for (int i = 0; i < kLast; ++i) {
         const int64_t j = j0 + i * WPR;
         if (j < far) {
-          load_raw<DK>(p.c.k, b * p.c.k_batch + j * p.c.k_entry + h * p.c.k_head, p.D, lane, kw[i]);
-          load_raw<DK>(p.c.v, b * p.c.v_batch + j * p.c.v_entry + h * p.c.v_head, p.D, lane, vw[i]);
+          load_raw<E>(p.c.k, b * p.c.k_batch + j * p.c.k_entry + h * p.c.k_head, p.D, l, kw[i]);
+          load_raw<E>(p.c.v, b * p.c.v_batch + j * p.c.v_entry + h * p.c.v_head, p.D, l, vw[i]);
         }
       }
     };
     if (j_first < n) {
-      load_raw<DK>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, lane, qw);
+      load_raw<E>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, l, qw);
       fetch(j_first);
     }
-    const int share = (uint32_t)(np + no + WPR - 1) / (uint32_t)WPR, end = min((sub + 1) * share, np + no);
-    for (int s0 = sub * share; s0 < end; s0 += 32) {
-      const int s = s0 + lane, some = min(32, end - s0);
+    const int share = (uint32_t)(np + no + WPR - 1) / (uint32_t)WPR, begin = sub * share, end = min(begin + share, np + no);
+    const int most = larger(end - begin);
+    for (int e0 = 0; e0 < most; e0 += L) {
+      const int s0 = begin + e0, s = s0 + l, some = min(L, end - s0);
       const auto row_of = [&](int i) {                         // of result i
         return i < np ? at_p + (int64_t)i * kRows : at_o + (int64_t)(i - np) * rw.own_rows;
       };
       float4 ml = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (lane < some) ml = __ldcg((s < np ? p.p_ml : p.o_ml) + row_of(s));
+      if (l < some) ml = __ldcg((s < np ? p.p_ml : p.o_ml) + row_of(s));
       float o[kBatch][E];
       const auto load = [&](int i0) {
 #pragma unroll
         for (int i = 0; i < kBatch; ++i)
           if (i0 + i < some) {
             const int si = s0 + i0 + i;
-            const float* from = (si < np ? p.p_o : p.o_o) + row_of(si) * DK;
-            if constexpr (E == 4) {
-              const float4 f = __ldcg(reinterpret_cast<const float4*>(from) + lane);
-              o[i][0] = f.x, o[i][1] = f.y, o[i][2] = f.z, o[i][3] = f.w;
-            } else {
-              const float2 f = __ldcg(reinterpret_cast<const float2*>(from) + lane);
+            const float* from = (si < np ? p.p_o : p.o_o) + row_of(si) * DK + l * E;
+            if constexpr (E == 2) {
+              const float2 f = __ldcg(reinterpret_cast<const float2*>(from));
               o[i][0] = f.x, o[i][1] = f.y;
+            } else {
+#pragma unroll
+              for (int e = 0; e < E; e += 4) {
+                const float4 f = __ldcg(reinterpret_cast<const float4*>(from + e));
+                o[i][e] = f.x, o[i][e + 1] = f.y, o[i][e + 2] = f.z, o[i][e + 3] = f.w;
+              }
             }
           }
       };
       load(0);
       const float mi = ml.y == 0.f ? -INFINITY : ml.x;         // (a NaN sum stays in)
-      float top = mi;
-#pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      if (top == -INFINITY) continue;
+      const float top = row_max(mi);
       if (top > a.m) a.rebase(top);
       const float w = mi == -INFINITY ? 0.f : ex2(mi - a.m);
-      float l = mi == -INFINITY ? 0.f : w * ml.y, r = mi == -INFINITY ? 0.f : w * ml.z;
-#pragma unroll
-      for (int d = 16; d >= 1; d >>= 1) {
-        l += __shfl_xor_sync(0xffffffffu, l, d);
-        r += __shfl_xor_sync(0xffffffffu, r, d);
-      }
-      a.l += l;
-      a.r += r;
-      for (int i0 = 0; i0 < some; i0 += kBatch) {
+      a.l += row_sum(mi == -INFINITY ? 0.f : w * ml.y);
+      a.r += row_sum(mi == -INFINITY ? 0.f : w * ml.z);
+      for (int i0 = 0; i0 < min(L, most - e0); i0 += kBatch) {
         if (i0 > 0) load(i0);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-          const float wi = __shfl_sync(0xffffffffu, w, i0 + i);
+          const float wi = __shfl_sync(0xffffffffu, w, lane - l + i0 + i);
           if (i0 + i < some && wi != 0.f) {
 #pragma unroll
             for (int e = 0; e < E; ++e) a.o[e] = fmaf(wi, o[i][e], a.o[e]);
@@ -925,22 +929,22 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
         }
       }
     }
-    for (int j0 = j_first; j0 < n; j0 += kLast * WPR) {
-      if (j0 > j_first) fetch(j0);
+    const int last = larger(n - j_first);
+    for (int e0 = 0; e0 < last; e0 += kLast * WPR) {
+      if (e0 > 0) fetch(j_first + e0);
 #pragma unroll
       for (int i = 0; i < kLast; ++i) {
-        const int j = j0 + i * WPR;
-        if (j >= n) break;
-        float s = -INFINITY;
+        const int j = j_first + e0 + i * WPR;
+        float s = 0.f;
         if (j < far) {
-          s = 0.f;
 #pragma unroll
           for (int e = 0; e < E / 2; ++e) {
             const float2 x = unpack2<BF16>(qw[e]), y = unpack2<BF16>(kw[i][e]);
             s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
           }
-#pragma unroll
-          for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        }
+        s = row_sum(s);
+        if (j < far) {
           const float x = s * p.c2;
           if (x > a.m) a.rebase(x);
           const float w = ex2(fmaf(s, p.c2, a.m == -INFINITY ? 0.f : -a.m));
@@ -953,8 +957,10 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
             a.o[2 * e + 1] = fmaf(w, v.y, a.o[2 * e + 1]);
           }
           if (a.m == -INFINITY && w != 0.f) a.m = 0.f;      // (a NaN score)
+        } else {
+          s = -INFINITY;
         }
-        if (p.scores && lane == 0)
+        if (p.scores && l == 0 && j < n)
           p.scores[((((int64_t)b * p.Hkv + h) * p.nt_cap + j / kTile) * p.R + rr) * kTile + j % kTile] = s;
       }
     }
@@ -984,16 +990,17 @@ __global__ void __launch_bounds__(32 * W, WPR > 1 ? 2 : 8) combine_kernel(const 
   if (!real) return;
   const bool empty = a.l == 0.f;
   const float inv = empty ? 0.f : 1.f / a.r;
-  if (lane * E < p.D) {
-    uint16_t* out = static_cast<uint16_t*>(p.c.out) + b * p.c.out_batch + t * p.c.out_token + hq * p.c.out_head + lane * E;
+  if (l * E < p.D) {
+    uint16_t* out = static_cast<uint16_t*>(p.c.out) + b * p.c.out_batch + t * p.c.out_token + hq * p.c.out_head + l * E;
     uint32_t w[E / 2];
 #pragma unroll
     for (int i = 0; i < E / 2; ++i)
       w[i] = empty ? 0u : pack2<BF16>(a.o[2 * i] * inv, a.o[2 * i + 1] * inv);
-    if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+    if constexpr (E == 8) *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
     else *reinterpret_cast<uint32_t*>(out) = w[0];
   }
-  if (lane == 0) {
+  if (l == 0) {
     const float l2 = a.m + log2f(a.l);
     if (p.c.lse) p.c.lse[((int64_t)b * p.c.T + t) * p.Hq + hq] = empty ? -INFINITY : l2 * kLn2;
     if (p.scores) p.lse2[id] = empty ? INFINITY : l2;
@@ -1114,7 +1121,9 @@ cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, 
   // own cache is full.  us a call with 8 / 2 / 1: 64 chats (768 rows of 3 results)
   // 32.2 / 27.3 / 28.1, 19 sequences of 6 tokens (1824 of 15) 119 / 110 / 113, a
   // document (192 of 71) 54 / 59 / 66, 30 sequences of one token (240 of 147) 25 / 34 /
-  // 50; 32 drafting sequences (3840 of 5) with 2 / 1 51.1 / 49.7, 128 (10240) 162 / 144.
+  // 50; 32 drafting sequences (3840 of 5) with 2 / 1 51.1 / 49.7, 128 (10240) 162 / 144;
+  // many rows with 1 / a half: 128 drafting sequences 141 / 138, 128 of 196 entries 49.6 /
+  // 47.1.
   const int64_t nt = p.nt_prefix + p.nt_cap;
   const int64_t tiles = p.Hkv * ((int64_t)p.rows.prefix_units * p.nt_prefix + (int64_t)p.c.B * p.rows.own_units * p.nt_cap);
   if (rows <= p.grid || (rows <= 2048 && p.grid * nt >= 24 * tiles))
@@ -1122,7 +1131,7 @@ cudaError_t launch_attend_t(const AttnParams& p, const AttnMaps& maps, int dev, 
   else if (rows <= 2048)
     e = launch_pdl(combine_kernel<DK, BF16, 4, 2>, dim3((unsigned)((rows + 1) / 2)), dim3(128), 0, s, p);
   else
-    e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, s, p);
+    e = launch_pdl(combine_kernel<DK, BF16, 4, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(128), 0, s, p);
   if (e != cudaSuccess || !p.c.weights) return e;
   return launch_pdl(weights_kernel, dim3((unsigned)ceil_div(p.capacity, kWeightEntries), (unsigned)min(p.c.B * p.Hkv, 65535)),
                     dim3(kWeightThreads), 0, s, p);
