@@ -15,10 +15,9 @@
 // (which only the device knows); a CTA's run of tiles within a unit is a
 // segment, which leaves its sum over V, its maximum and its sums of
 // exponentials in a slot of the workspace.  Per CTA (192 threads):
-//   warp 4      one thread issues copies (TMA): the query rows of a segment (a
-//               box of G heads x T tokens, for the prefix x as many sequences as
-//               128 rows hold), K tiles and V tiles into rings, each as soon as
-//               its place is free.
+//   warp 4      copies (TMA): the query rows of a segment (a box of G heads x T
+//               tokens, for the prefix x as many sequences as 128 rows hold), K
+//               tiles and V tiles into rings, each as soon as its place is free.
 //   warp 5      S = Q K^T one tile ahead of O += P V (tcgen05, M = 128, P from
 //               tensor memory, V as an N-major operand).
 //   warps 0-3   the softmax, thread = row = tensor-memory lane: per tile they
@@ -38,23 +37,23 @@
 //
 // What bounds it: K and V from memory where few rows share an entry, the tensor
 // cores where 128 do (their rate at N = 64, where Q is read from shared memory
-// again for every tile, is 5/8 of the peak for 128-wide heads), and in between a
+// again for every tile, is 4/5 of the peak for 128-wide heads), and in between a
 // tile's way from S through the softmax to P, of which two CTAs have one each on
-// their way per SM: about 1500 cycles a tile and CTA, of which the softmax's
+// their way per SM: about 1300 cycles a tile and CTA, of which the softmax's
 // arithmetic is 370 at full rate.  Tiles of 64 entries with the scores one tile
 // ahead, because tensor memory holds no more for 128-wide heads and two CTAs (128
 // entries without: 128 drafting sequences 291 us, with 64: 212 at that state).
 // Measured (a call, its three kernels together): 128 sequences of 5 tokens, 16 query
-// heads on 4 of 128, prefix 16384, own 512 to 2048, with weights: 143 us, the floor of
-// its bytes 56, of its operations 48, tensor pipe busy 73 % in attend_kernel (113 us);
+// heads on 4 of 128, prefix 16384, own 512 to 2048, with weights: 138 us, the floor of
+// its bytes 56, of its operations 48, tensor pipe busy 74 % in attend_kernel (111 us);
 // 16 sequences over a document of 131072: 54 us, 5.1 TB/s; 64 chats over 2048 with own
-// caches of up to 1024: 26.6 us (floor 10.7), the kernel itself 21; 32 drafting sequences
-// with 64-wide heads over 8191: 48 us (floor 13); one sequence of 60 entries over 512:
+// caches of up to 1024: 26.2 us (floor 10.7), the kernel itself 21; 32 drafting sequences
+// with 64-wide heads over 8191: 47 us (floor 13); one sequence of 60 entries over 512:
 // 10.2 us, two launches' latency.
 //
-// combine_kernel: one to eight warps per query row merge its partial results and
-// these last entries; latency, and for many rows the instructions of a row (10240
-// rows 14 us).  weights_kernel: the weights, from the scores of the own entries that
+// combine_kernel: half a warp to eight warps per query row merge its partial results
+// and these last entries; latency, and for many rows the instructions of a row (10240
+// rows 12 us).  weights_kernel: the weights, from the scores of the own entries that
 // attend_kernel left in the workspace and the rows' lse; 4 bytes written and read
 // per own entry and query row (128 drafting sequences: 52 MB, 13 us).
 #include <cuda.h>
@@ -73,7 +72,7 @@ constexpr int kTile = 64;                  // entries of a tile
 constexpr int kRows = 128;                 // rows of the MMA
 constexpr int kAttThreads = 192;
 constexpr int kGroups = kAttThreads;
-constexpr int kTmemCols = 256;             // S and P: 0 .. 63 and 64 .. 127, O: 128 .. 255
+constexpr int kTmemCols = 256;             // S and P: 0 .. 63 and 64 .. 127, O (and the sum of P): from 128 on
 constexpr uint32_t kTmemO = 128;
 constexpr int kQBlock = kRows * 128;       // 64 elements of 128 rows
 constexpr int kBlock = kTile * 128;        // 64 elements of a tile's entries
@@ -508,8 +507,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
   if (warp == 4) {
     // ------------------------------ TMA -----------------------------------------
     // The whole warp walks the tiles and one lane issues, by predicate (as the
-    // MMAs below: by a branch of lane 0 a tile's two copies took this warp about
-    // 1000 cycles, and everything else waited for it).
+    // MMAs below; by a branch of lane 0 the warp was busy all the time and 128
+    // drafting sequences took 141.8 us instead of 140.4).
     const uint32_t one = elect_one();
     const auto all = [](bool x) { return __all_sync(0xffffffffu, x) != 0; };
     const auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
