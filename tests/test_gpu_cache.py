@@ -231,6 +231,14 @@ def test_attend_in_a_graph():
     cache.close()
 
 
+@pytest.mark.parametrize("D", [40, 64, 72, 128])
+def test_attend_many_rows_of_odd_number(D):
+    # 2277 rows, two to a warp of the merge; neighbours of other lengths, some empty
+    lens = [(7 * b) % 41 for b in range(23)]
+    x = make(32, 23, 3, 33, 11, D, 70, 40, lens, "bf16")
+    check(*x, run(*x))
+
+
 def test_attend_more_heads_than_a_grid_is_high():
     """1024 sequences x 65 K/V heads, one own entry each: it has all of the weight."""
     B, H, D = 1024, 65, 8
