@@ -852,17 +852,16 @@ __global__ void __launch_bounds__(32 * W, kCombineCtas<DK, W, WPR>) combine_kern
     const int up = h * rw.prefix_units + group * rw.per_seq + m, prefix_units = p.Hkv * rw.prefix_units;
     const int64_t uo = (int64_t)(b * p.Hkv + h) * rw.own_units + m;
     const int n = real ? used(p, b) : 0;
-    int2 cp = make_int2(0, -1), co = make_int2(0, -1);         // CTAs of the row's prefix unit, of its own one
-    const auto ctas = [&](int64_t unit) {                      // (in range also where attend_kernel gave up)
+    Results cp = {0, -1}, co = {0, -1};                        // of the row's prefix unit, of its own one
+    const auto noted = [&](int64_t unit) {
       const int2 x = __ldcg(p.unit_ctas + unit);
-      return make_int2(max(x.x, 0), min(x.y, p.grid - 1));
+      return noted_results(x.x, x.y, p.grid);
     };
-    if (real && p.nt_prefix > 0) cp = ctas(up);
-    if (n > p.c.T - 1) co = ctas(prefix_units + uo);
-    // partial results: np of the prefix unit, no of the own one
-    const int np = cp.y - cp.x + 1, no = co.y - co.x + 1;
-    const int64_t at_p = (int64_t)(cp.x + up) * kRows + (b - group * rw.seqs) * p.R + ro;
-    const int64_t at_o = (co.x + uo) * rw.own_rows + ro;
+    if (real && p.nt_prefix > 0) cp = noted(up);
+    if (n > p.c.T - 1) co = noted(prefix_units + uo);
+    const int np = cp.count(), no = co.count();
+    const int64_t at_p = (int64_t)(cp.first + up) * kRows + (b - group * rw.seqs) * p.R + ro;
+    const int64_t at_o = (co.first + uo) * rw.own_rows + ro;
     // the last T - 1 own entries, of which this row sees the first few: j_first
     // on, this warp every WPR-th, the first kLast on their way from here
     const int far = n - (p.c.T - 1 - t), j_first = p.c.T > 1 ? max(0, n - (p.c.T - 1)) + sub : n;
@@ -881,7 +880,7 @@ __global__ void __launch_bounds__(32 * W, kCombineCtas<DK, W, WPR>) combine_kern
       load_raw<E>(p.c.q, b * p.c.q_batch + t * p.c.q_token + hq * p.c.q_head, p.D, l, qw);
       fetch(j_first);
     }
-    const int share = (uint32_t)(np + no + WPR - 1) / (uint32_t)WPR, begin = sub * share, end = min(begin + share, np + no);
+    const auto [begin, end] = share_of(np + no, sub, WPR);
     const int most = larger(end - begin);
     for (int e0 = 0; e0 < most; e0 += L) {
       const int s0 = begin + e0, s = s0 + l, some = min(L, end - s0);

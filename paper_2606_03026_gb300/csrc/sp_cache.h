@@ -22,6 +22,27 @@ struct CacheWorkspace {
 };
 CacheWorkspace cache_workspace(const CacheShape& s, int sms);
 
+// The partial results of a unit of query rows, as the merge finds them: one of each
+// of the CTAs first .. last that the attention kernel noted down.  Where it gave
+// up on a wait the note may be anything, so that both are taken into 0 .. grid - 1
+// and a reversed pair holds none.
+struct Results {
+  int32_t first, last;
+  __host__ __device__ int32_t count() const { return last < first ? 0 : last - first + 1; }
+};
+inline __host__ __device__ int32_t within(int32_t cta, int32_t grid) { return cta < 0 ? 0 : cta < grid ? cta : grid - 1; }
+inline __host__ __device__ Results noted_results(int32_t first, int32_t last, int32_t grid) {
+  return Results{within(first, grid), within(last, grid)};
+}
+// Part `sub` of `parts` of n >= 0 things: begin .. end (none where end <= begin).
+struct Share {
+  int32_t begin, end;
+};
+inline __host__ __device__ Share share_of(int32_t n, int32_t sub, int32_t parts) {
+  const int32_t each = (int32_t)((uint32_t)(n + parts - 1) / (uint32_t)parts), begin = sub * each;
+  return Share{begin, begin + each < n ? begin + each : n};
+}
+
 // Tiles of entries that a call has at most (its launch counts them in 32 bits).
 int64_t attend_tiles(const CacheShape& s, const sp_attend& c);
 cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err,

@@ -1,0 +1,52 @@
+"""What the cache kernels read and write, as far as arithmetic that they share
+with the host decides it, and what their entry points refuse besides.  No GPU."""
+import ctypes
+import itertools
+import subprocess
+from pathlib import Path
+
+import pytest
+
+from paper_2606_03026_gb300 import _build
+
+HERE = Path(__file__).resolve().parent
+
+
+@pytest.fixture(scope="module")
+def arith(tmp_path_factory):
+    out = tmp_path_factory.mktemp("arith") / "libcache_arith.so"
+    cuda = Path(_build.nvcc()).resolve().parent.parent / "include"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{cuda}", f"-I{_build.INCLUDE}", f"-I{_build.CSRC}",
+                    str(HERE / "cache_arith.cpp"), "-o", str(out)], check=True)
+    return ctypes.CDLL(str(out))
+
+
+def two(f, *args):
+    a, b = ctypes.c_int32(), ctypes.c_int32()
+    f(*args, ctypes.byref(a), ctypes.byref(b))
+    return a.value, b.value
+
+
+ANY = [-2 ** 31, -2 ** 31 + 1, -305, -194, -8, -2, -1, 0, 1, 2, 7, 150, 302, 303, 304, 305, 2 ** 30, 2 ** 31 - 1]
+
+
+@pytest.mark.parametrize("grid", [1, 304])
+def test_partial_results_are_within_the_workspace_whatever_was_noted(arith, grid):
+    """After a wait that ran out a unit's CTAs are what an earlier call or
+    nobody wrote: reversed, negative, huge."""
+    for first, last in itertools.product(ANY, ANY):
+        at, count = two(arith.arith_results, first, last, grid)
+        assert 0 <= at < grid and 0 <= count and at + count <= grid, (first, last)
+        if 0 <= first <= last < grid:
+            assert (at, count) == (first, last - first + 1)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 8])
+def test_shares_of_the_results_are_all_of_them_once(arith, parts):
+    for n in (0, 1, 2, 7, 8, 9, 71, 304, 608):
+        have = []
+        for sub in range(parts):
+            begin, end = two(arith.arith_share, n, sub, parts)
+            assert end <= n and begin >= 0
+            have += range(begin, end)
+        assert have == list(range(n))
