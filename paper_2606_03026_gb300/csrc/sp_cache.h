@@ -43,6 +43,36 @@ inline __host__ __device__ Share share_of(int32_t n, int32_t sub, int32_t parts)
   return Share{begin, begin + each < n ? begin + each : n};
 }
 
+// Pieces of a row through a ring of RING places, one warp.  it: pieces that have
+// gone through the ring before; copies: every copy so far has arrived in time.
+// fetch(i, place) copies piece i there, arrived(place, parity) waits (within a
+// limit) for it, use(i, place, here) takes it from there, or from the row itself
+// where a copy has not come, then(i, x) is given what use returned after the
+// place has its next copy.  Returns `copies`.  When a wait has run out, all that
+// is still on its way is waited for once more, as nothing may land in the memory
+// of a CTA that has left.
+#ifdef __CUDACC__
+#define SP_WARP __device__ __forceinline__
+#else
+#define SP_WARP inline                     // (a test's simulation)
+#endif
+template <int RING, typename Fetch, typename Arrived, typename Use, typename Then>
+SP_WARP bool walk_ring(int it, int pieces, bool copies, Fetch fetch, Arrived arrived, Use use, Then then) {
+  if (copies)
+    for (int i = 0; i < RING && i < pieces; ++i) fetch(i, (it + i) % RING);
+  for (int i = 0; i < pieces; ++i) {
+    const int place = (it + i) % RING;
+    if (copies && !arrived(place, (uint32_t)((it + i) / RING & 1))) {
+      copies = false;
+      for (int j = i; j < i + RING && j < pieces; ++j) arrived((it + j) % RING, (uint32_t)((it + j) / RING & 1));
+    }
+    const auto x = use(i, place, copies);
+    if (copies && i + RING < pieces) fetch(i + RING, place);
+    then(i, x);
+  }
+  return copies;
+}
+
 // Tiles of entries that a call has at most (its launch counts them in 32 bits).
 int64_t attend_tiles(const CacheShape& s, const sp_attend& c);
 cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err,

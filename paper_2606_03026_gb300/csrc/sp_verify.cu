@@ -72,25 +72,23 @@ __device__ __forceinline__ unsigned long long sum_span(const float* pr, const fl
                                                        unsigned long long* groups) {
   const int lane = threadIdx.x & 31;
   const int pieces = ceil_div(max(v1 - v0, 0), kPiece);
-  const int it0 = it;
-  const auto fetch = [&](int i) {
-    const int st = (it0 + i) % kRing, v = v0 + i * kPiece, n = min(kPiece, v1 - v);
+  const auto fetch = [&](int i, int st) {
+    if (lane != 0) return;
+    const int v = v0 + i * kPiece, n = min(kPiece, v1 - v);
     uint8_t* to = ring + st * 2 * kPieceBytes;
     mbar_arrive_expect_tx(&full[st], piece_bytes(pr + v, n) + (qr ? piece_bytes(qr + v, n) : 0u));
     bulk_load(to, piece_base(pr + v), piece_bytes(pr + v, n), &full[st]);
     if (qr) bulk_load(to + kPieceBytes, piece_base(qr + v), piece_bytes(qr + v, n), &full[st]);
   };
-  if (lane == 0 && copies)
-    for (int i = 0; i < min(kRing, pieces); ++i) fetch(i);
-  unsigned long long all = 0, group = 0;
-  for (int i = 0; i < pieces; ++i, ++it) {
-    const int st = it % kRing, v = v0 + i * kPiece, n = min(kPiece, v1 - v);
+  const auto arrived = [&](int st, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_try_wait(&full[st], parity) || mbar_wait(&full[st], parity)) != 0;
+  };
+  const auto use = [&](int i, int st, bool here) {
+    const int v = v0 + i * kPiece, n = min(kPiece, v1 - v);
     const float* x = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes) + piece_skip(pr + v);
     const float* y = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes + kPieceBytes) + (qr ? piece_skip(qr + v) : 0);
     // (once a copy has not arrived in time, the rows are read themselves)
-    const uint32_t parity = it / kRing & 1;
-    copies = copies && __all_sync(0xffffffffu, mbar_try_wait(&full[st], parity) || mbar_wait(&full[st], parity));
-    if (!copies) {
+    if (!here) {
       x = pr + v;
       y = qr + v;
     }
@@ -112,7 +110,10 @@ __device__ __forceinline__ unsigned long long sum_span(const float* pr, const fl
       for (int e = lane; e < n; e += 32) sum += whole(x[e] - (qr ? y[e] : 0.f));
     }
     __syncwarp();
-    if (lane == 0 && i + kRing < pieces && copies) fetch(i + kRing);
+    return sum;
+  };
+  unsigned long long all = 0, group = 0;
+  const auto then = [&](int i, unsigned long long sum) {
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
     all += sum;
@@ -121,7 +122,9 @@ __device__ __forceinline__ unsigned long long sum_span(const float* pr, const fl
       if (lane == 0) groups[i / per_group] = group;
       group = 0;
     }
-  }
+  };
+  copies = walk_ring<kRing>(it, pieces, copies, fetch, arrived, use, then);
+  it += pieces;
   return all;
 }
 

@@ -50,3 +50,14 @@ def test_shares_of_the_results_are_all_of_them_once(arith, parts):
             assert end <= n and begin >= 0
             have += range(begin, end)
         assert have == list(range(n))
+
+
+@pytest.mark.parametrize("pieces", [(0,), (1,), (2, 1), (3, 5), (5, 4), (7, 0, 3)])
+def test_no_copy_of_a_verification_is_left_on_its_way(arith, pieces):
+    """Rows of so many pieces, one after another through one ring, whatever one
+    copy does: late ones are waited for before the CTA may leave."""
+    total = sum(pieces)
+    rows = (ctypes.c_int * len(pieces))(*pieces)
+    for at, what, rest in itertools.product(range(total + 1), (1, 2), (0, 1)):
+        how = [0] * at + [what] + [rest] * total
+        assert arith.arith_ring(len(pieces), rows, (ctypes.c_int * len(how))(*how)) == 0, (at, what, rest)
