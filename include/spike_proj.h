@@ -624,8 +624,9 @@ sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend *call,
  * (attention itself does not depend on it).  K and V move in place, reading
  * slots >= budget and writing slots < budget only; weight and pos of slot j of
  * the result go to weights_out and pos_out (j < min(n, budget); the rest of
- * them is left alone), min(n, budget) to lens_out[b].  The outputs must not
- * overlap the inputs (SP_EINVAL where the pointers are equal).
+ * them is left alone), min(n, budget) to lens_out[b].  weights_out, pos_out and
+ * lens_out must overlap neither an input (SP_EINVAL where the pointers are equal)
+ * nor each other.
  *
  *   weights, pos           FP32 / int32, entry j of (b, h) at
  *                          b*in_batch + h*in_head + j

@@ -1265,7 +1265,9 @@ sp_status spike_proj_cache_evict(sp_cache_t cache, const sp_evict* c, sp_stream_
   const CacheShape& sh = cache->shape;
   if (c->budget != 0 && (!c->weights_out || !c->pos_out)) return SP_EINVAL;
   if (c->B < 1 || c->budget < 0 || c->recent < 0 || c->recent > c->budget) return SP_EINVAL;
-  if (c->weights == c->weights_out || c->pos == c->pos_out || c->lens == c->lens_out) return SP_EINVAL;
+  for (const void* out : {(const void*)c->weights_out, (const void*)c->pos_out, (const void*)c->lens_out})
+    for (const void* in : {(const void*)c->weights, (const void*)c->pos, (const void*)c->lens, (const void*)c->now})
+      if (out == in) return SP_EINVAL;
   if (c->B > sh.max_batch) return SP_ERANGE;
   const auto kv = [](int64_t n, int64_t stride) { return n == 1 || (stride % 8 == 0 && stride > 0); };
   if (!aligned(c->k, 16) || !aligned(c->v, 16) || !kv(c->B, c->k_batch) || !kv(sh.capacity, c->k_entry) ||

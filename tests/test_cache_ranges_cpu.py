@@ -7,7 +7,9 @@ from pathlib import Path
 
 import pytest
 
-from paper_2606_03026_gb300 import _build
+from paper_2606_03026_gb300 import _build, spikeproj as sp
+from test_cache_cpu import cache, evict_call                     # noqa: F401  (a fixture)
+from test_host_cpu import FAKE, lib                              # noqa: F401  (a fixture)
 
 HERE = Path(__file__).resolve().parent
 
@@ -61,3 +63,22 @@ def test_no_copy_of_a_verification_is_left_on_its_way(arith, pieces):
     for at, what, rest in itertools.product(range(total + 1), (1, 2), (0, 1)):
         how = [0] * at + [what] + [rest] * total
         assert arith.arith_ring(len(pieces), rows, (ctypes.c_int * len(how))(*how)) == 0, (at, what, rest)
+
+
+OWN = {name: (i + 1) * FAKE for i, name in enumerate(("weights", "pos", "lens", "now", "weights_out", "pos_out", "lens_out"))}
+
+
+@pytest.mark.parametrize("out", ["weights_out", "pos_out", "lens_out"])
+@pytest.mark.parametrize("given", ["weights", "pos", "lens", "now"])
+def test_an_eviction_whose_output_is_an_input_is_refused(lib, cache, out, given):      # noqa: F811
+    """`now` in the place of lens_out, for one: head 0 writes the lengths while
+    the other heads may not have read the time yet."""
+    assert lib.spike_proj_cache_evict(cache, ctypes.byref(evict_call(**OWN)), None) == sp.SP_OK
+    lib.fake_launches()
+    assert lib.spike_proj_cache_evict(cache, ctypes.byref(evict_call(**{**OWN, out: OWN[given]})), None) == sp.SP_EINVAL
+    assert lib.fake_launches() == 0
+
+
+def test_an_eviction_of_everything_needs_no_outputs_of_entries(lib, cache):     # noqa: F811
+    call = evict_call(**{**OWN, "weights_out": None, "pos_out": None, "budget": 0, "recent": 0})
+    assert lib.spike_proj_cache_evict(cache, ctypes.byref(call), None) == sp.SP_OK
