@@ -681,6 +681,8 @@ sp_status spike_proj_cache_evict(sp_cache_t cache, const sp_evict *call,
  *   n_accept   int32 [B]: n
  *   tokens     int32 [B], row stride ld_tokens >= T+1: the n kept drafts, the
  *              token after them, -1 from there on
+ *   The outputs must not overlap the inputs, except that n_accept may be n_draft
+ *   and tokens may be draft with the same row stride.
  *   0 <= T <= SPIKE_PROJ_VERIFY_MAX_T, 1 <= V <= SPIKE_PROJ_VERIFY_MAX_V,
  *   1 <= B <= 65535 (SP_ERANGE); 4-byte aligned pointers (SP_EALIGN).
  * Of p and q only the entries at the drafts and the one row of each that the

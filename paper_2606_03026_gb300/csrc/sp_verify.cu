@@ -154,26 +154,21 @@ __global__ void __launch_bounds__(kVerThreads, kVerPerSm) verify_kernel(const __
   // the first draft that is not kept
   const float us = unit(__ldg(c.u_sample + b));
   const int nd = c.n_draft ? min(max(__ldg(c.n_draft + b), 0), c.T) : c.T;
+  int x = -1;
   if (warp < 2) {
     const int t = threadIdx.x;
     bool ok = false;
     if (t < c.T) {
-      const int x = __ldg(c.draft + b * c.ld_draft + t);
+      x = __ldg(c.draft + b * c.ld_draft + t);
       const float u = unit(__ldg(c.u + b * c.ld_u + t));
       if (x >= 0 && x < c.V)
         ok = __fmul_rn(u, __ldg(c.q + b * c.q_batch + t * c.q_row + x)) < __ldg(c.p + b * c.p_batch + t * c.p_row + x);
-      if (rank == 0) c.tokens[b * c.ld_tokens + t] = x;     // (those that are not kept go below)
     }
     const uint32_t bad = __ballot_sync(0xffffffffu, !ok);
     if (lane == 0) s_bad[warp] = bad ? 32 * warp + __ffs(bad) - 1 : 64;
   }
   __syncthreads();
   const int n = min(min(s_bad[0], s_bad[1]), nd);
-  if (rank == 0 && threadIdx.x <= c.T) {
-    if (threadIdx.x > n) c.tokens[b * c.ld_tokens + threadIdx.x] = -1;
-    if (threadIdx.x == 0) c.n_accept[b] = n;
-  }
-
   const float* pr = c.p + b * c.p_batch + n * c.p_row;
   const float* qr = n < nd ? c.q + b * c.q_batch + n * c.q_row : nullptr;
   const int v0 = min((int)rank * p.slice + warp * p.span, c.V);
@@ -192,6 +187,11 @@ __global__ void __launch_bounds__(kVerThreads, kVerPerSm) verify_kernel(const __
                    : "memory");
     }
     cluster_sync();
+    // (every CTA has read the drafts and their number, whose places these may be)
+    if (pass == 0 && rank == 0 && threadIdx.x <= c.T) {
+      if ((int)threadIdx.x != n) c.tokens[b * c.ld_tokens + threadIdx.x] = (int)threadIdx.x < n ? x : -1;
+      if (threadIdx.x == 0) c.n_accept[b] = n;
+    }
     unsigned long long before = 0, S = 0;
     for (uint32_t r = 0; r < ranks; ++r) {
       if (r < rank) before += s_cta[pass][r];
