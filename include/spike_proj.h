@@ -569,8 +569,9 @@ sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream);
  *
  * A row that sees no entry (or scores of minus infinity alone) gives out = 0,
  * lse = -infinity and no weight.  Entries that no row sees are never used,
- * whatever they hold; a NaN that a row sees makes that row NaN.  The
- * probabilities are rounded to the type before they meet V, and out is divided
+ * whatever they hold; a NaN key that a row sees makes that row NaN and a NaN
+ * value its element of it, however little weight the entry has (0 too; an
+ * infinite value then gives NaN as well).  The probabilities are rounded to the type before they meet V, and out is divided
  * by the sum of the rounded ones; lse and weights take them unrounded.  Scores,
  * the running maximum and sums, and the sums over V are FP32.  Results do not
  * depend on the order in which blocks run.

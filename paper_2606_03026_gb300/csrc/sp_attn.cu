@@ -919,8 +919,9 @@ __global__ void __launch_bounds__(32 * W, kCombineCtas<DK, W, WPR>) combine_kern
         if (i0 > 0) load(i0);
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
+          // (a result without weight too: what it has of NaN stays)
           const float wi = __shfl_sync(0xffffffffu, w, lane - l + i0 + i);
-          if (i0 + i < some && wi != 0.f) {
+          if (i0 + i < some) {
 #pragma unroll
             for (int e = 0; e < E; ++e) a.o[e] = fmaf(wi, o[i][e], a.o[e]);
           }
@@ -976,9 +977,8 @@ __global__ void __launch_bounds__(32 * W, kCombineCtas<DK, W, WPR>) combine_kern
     if (sub != 0) return;
     for (int w = 1; w < WPR; ++w) {
       const float m = s_ml[warp + w][0];
-      if (m == -INFINITY) continue;
       if (m > a.m) a.rebase(m);
-      const float x = ex2(m - a.m);
+      const float x = m == -INFINITY ? 0.f : ex2(m - a.m);
       a.l = fmaf(x, s_ml[warp + w][1], a.l);
       a.r = fmaf(x, s_ml[warp + w][2], a.r);
 #pragma unroll

@@ -1,5 +1,7 @@
 """Attention, eviction and verification where sums vanish, offsets are long and
 rows are wide."""
+import math
+
 import pytest
 import torch
 
@@ -7,6 +9,37 @@ from paper_2606_03026_gb300 import spikeproj as sp
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("B,G,P", [(1, 1, 40000), (40, 60, 700), (3, 3, 700)], ids=["long", "rows", "few"])
+@pytest.mark.parametrize("score", [0.0, -math.inf], ids=["vanishing", "zero"])
+def test_a_value_that_is_nan_stays_where_its_weight_vanishes(dtype, B, G, P, score):
+    """One prefix value is NaN; its weight beside the last entry's, 128 nats above,
+    is nothing in 32 bits, or it has none at all.  Its column of every row that
+    sees it is NaN all the same, however the entries are cut up."""
+    D, C = 64, 70
+    q = torch.ones(B, 1, G, D, dtype=dtype, device=DEV)
+    pk, pv = torch.full((P, 1, D), score, dtype=dtype, device=DEV), torch.ones(P, 1, D, dtype=dtype, device=DEV)
+    pk[-1] = 16.0
+    pk[64:] = pk[64:].nan_to_num(neginf=0.0)                 # only the first tile's are without weight
+    k, v = torch.zeros(B, C, 1, D, dtype=dtype, device=DEV), torch.ones(B, C, 1, D, dtype=dtype, device=DEV)
+    lens = torch.full((B,), C, dtype=torch.int32, device=DEV)
+    cache = sp.Cache(B, G, 1, D, C, dtype="bf16" if dtype == torch.bfloat16 else "fp16")
+    out = torch.zeros_like(q)
+    cache.attend(q, k, v, lens, out, pk, pv)
+    assert (out == 1).all()
+    pv[5, 0, 7] = math.nan
+    cache.attend(q, k, v, lens, out, pk, pv)
+    assert out[..., 7].isnan().all() and (out[..., :7] == 1).all() and (out[..., 8:] == 1).all()
+    # the same in an own cache
+    pv[5, 0, 7] = 1.0
+    k[0, 0], v[0, 0, 0, 3] = score, math.nan
+    cache.attend(q, k, v, lens, out, pk, pv)
+    assert out[0, ..., 3].isnan().all() and (out[0, ..., :3] == 1).all() and (out[0, ..., 4:] == 1).all()
+    assert (out[1:] == 1).all()
+    assert cache.status() == sp.SP_OK
+    cache.close()
 
 
 @pytest.mark.parametrize("B,T,V", [(1, 4, 57344), (40, 4, 57344), (400, 7, 999), (3, 64, 5000)])
