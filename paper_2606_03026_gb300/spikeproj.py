@@ -569,7 +569,7 @@ def _packer(struct_type):
 _pack_attend, _pack_evict, _pack_verify = map(_packer, (SpAttend, SpEvict, SpVerify))
 
 
-def _reject(x, name, shape, dtype):
+def _reject(x, name, shape, dtype, device):
     """Says what is wrong with a tensor that a call does not take as it is."""
     if x.shape != shape:
         raise ValueError(f"{name}: shape {tuple(x.shape)}, expected {tuple(shape)}")
@@ -577,15 +577,18 @@ def _reject(x, name, shape, dtype):
         raise ValueError(f"{name}: {x.dtype}, expected {dtype}")
     if not x.is_cuda:
         raise ValueError(f"{name}: not a CUDA tensor")
+    if x.get_device() != device:
+        raise ValueError(f"{name}: on CUDA device {x.get_device()}, expected {device}")
     if x.shape and x.shape[-1] > 1 and x.stride(-1) != 1:
         raise ValueError(f"{name}: the last dimension is not contiguous")
 
 
-def _want(x, name, shape, dtype):
-    """The strides of a tensor of the shape and type that a call needs, rows contiguous."""
+def _want(x, name, shape, dtype, device):
+    """The strides of a tensor of the shape and type that a call needs, rows
+    contiguous, on the CUDA device of that number."""
     st = x.stride()
-    if x.shape != shape or x.dtype is not dtype or not x.is_cuda or st[-1] != 1:
-        _reject(x, name, shape, dtype)
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != device or st[-1] != 1:
+        _reject(x, name, shape, dtype, device)
     return st
 
 
@@ -603,6 +606,7 @@ class Cache:
         self._scale = D ** -0.5
         self.handle = spike_proj_cache_create(max_batch, max_T, Hq, Hkv, D, capacity, dtype,
                                               SP_CACHE_WEIGHTS if weights else 0, stream)
+        self._device = torch.cuda.current_device()             # the handle's
 
     def attend(self, q, k, v, lens, out, prefix_k=None, prefix_v=None, weights=None, lse=None,
                scale=None, stream=None):
@@ -610,23 +614,23 @@ class Cache:
         own caches already hold the T tokens' entries, which lens (int32 [B])
         counts.  weights (float32 [B, Hkv, capacity]) gains the attention that
         the own entries get; lse (float32 [B, T, Hq]) is optional."""
-        t = self.dtype
+        t, dev = self.dtype, self._device
         B, T = q.shape[0], q.shape[1]
         rows, own = (B, T, self.Hq, self.D), (B, self.capacity, self.Hkv, self.D)
-        qs, os = _want(q, "q", rows, t), _want(out, "out", rows, t)
-        ks, vs = _want(k, "k", own, t), _want(v, "v", own, t)
-        _want(lens, "lens", (B,), self._i32)
+        qs, os = _want(q, "q", rows, t, dev), _want(out, "out", rows, t, dev)
+        ks, vs = _want(k, "k", own, t, dev), _want(v, "v", own, t, dev)
+        _want(lens, "lens", (B,), self._i32, dev)
         P, pk, pv, pks, pvs = 0, 0, 0, (0, 0), (0, 0)
         if prefix_k is not None and prefix_k.shape[0]:
             P = prefix_k.shape[0]
-            pks = _want(prefix_k, "prefix_k", (P, self.Hkv, self.D), t)
-            pvs = _want(prefix_v, "prefix_v", (P, self.Hkv, self.D), t)
+            pks = _want(prefix_k, "prefix_k", (P, self.Hkv, self.D), t, dev)
+            pvs = _want(prefix_v, "prefix_v", (P, self.Hkv, self.D), t, dev)
             pk, pv = prefix_k.data_ptr(), prefix_v.data_ptr()
         w, ws, l = 0, (0, 0), 0
         if weights is not None:
-            ws, w = _want(weights, "weights", own[:1] + (self.Hkv, self.capacity), self._f32), weights.data_ptr()
+            ws, w = _want(weights, "weights", own[:1] + (self.Hkv, self.capacity), self._f32, dev), weights.data_ptr()
         if lse is not None:
-            _want(lse, "lse", rows[:3], self._f32)
+            _want(lse, "lse", rows[:3], self._f32, dev)
             if not lse.is_contiguous():
                 raise ValueError("lse: not contiguous")
             l = lse.data_ptr()
@@ -643,22 +647,22 @@ class Cache:
         now - recent) and then those of the most weight; K and V [B, capacity,
         Hkv, D] in place, weights and pos [B, Hkv, capacity] into weights_out
         and pos_out [B, Hkv, >= min(budget, capacity)]."""
-        t, B = self.dtype, k.shape[0]
+        t, B, dev = self.dtype, k.shape[0], self._device
         own = (B, self.capacity, self.Hkv, self.D)
-        ks, vs = _want(k, "k", own, t), _want(v, "v", own, t)
+        ks, vs = _want(k, "k", own, t, dev), _want(v, "v", own, t, dev)
         have = (B, self.Hkv, self.capacity)
-        ws, ps = _want(weights, "weights", have, self._f32), _want(pos, "pos", have, self._i32)
+        ws, ps = _want(weights, "weights", have, self._f32, dev), _want(pos, "pos", have, self._i32, dev)
         room = weights_out.shape[-1]
         if room < min(budget, self.capacity):
             raise ValueError("weights_out: no room for the budget")
         left = (B, self.Hkv, room)
-        wos, pos_s = _want(weights_out, "weights_out", left, self._f32), _want(pos_out, "pos_out", left, self._i32)
+        wos, pos_s = _want(weights_out, "weights_out", left, self._f32, dev), _want(pos_out, "pos_out", left, self._i32, dev)
         if ps[:2] != ws[:2] or pos_s[:2] != wos[:2]:
             raise ValueError("pos: other strides than weights")
         one = (B,)
-        _want(lens, "lens", one, self._i32)
-        _want(now, "now", one, self._i32)
-        _want(lens_out, "lens_out", one, self._i32)
+        _want(lens, "lens", one, self._i32, dev)
+        _want(now, "now", one, self._i32, dev)
+        _want(lens_out, "lens_out", one, self._i32, dev)
         call = _pack_evict(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
                            weights.data_ptr(), pos.data_ptr(), ws[0], ws[1], weights_out.data_ptr(),
                            pos_out.data_ptr(), wos[0], wos[1], lens.data_ptr(), now.data_ptr(),
@@ -688,20 +692,21 @@ def verify(p, q, draft, u, u_sample, n_accept, tokens, n_draft=None, stream=None
     import torch
     f32, i32 = torch.float32, torch.int32
     B, rows, V = p.shape
-    T = rows - 1
-    ps = _want(p, "p", (B, rows, V), f32)
+    T, dev = rows - 1, torch.cuda.current_device()
+    ps = _want(p, "p", (B, rows, V), f32, dev)
     qa, qs, da, ds, ua, us = 0, (0, 0), 0, (0,), 0, (0,)
     if T:
         drafts = (B, T)
-        qs, ds, us = _want(q, "q", (B, T, V), f32), _want(draft, "draft", drafts, i32), _want(u, "u", drafts, f32)
+        qs = _want(q, "q", (B, T, V), f32, dev)
+        ds, us = _want(draft, "draft", drafts, i32, dev), _want(u, "u", drafts, f32, dev)
         qa, da, ua = q.data_ptr(), draft.data_ptr(), u.data_ptr()
     one = (B,)
-    _want(u_sample, "u_sample", one, f32)
-    _want(n_accept, "n_accept", one, i32)
-    ts = _want(tokens, "tokens", (B, rows), i32)
+    _want(u_sample, "u_sample", one, f32, dev)
+    _want(n_accept, "n_accept", one, i32, dev)
+    ts = _want(tokens, "tokens", (B, rows), i32, dev)
     nd = 0
     if n_draft is not None:
-        _want(n_draft, "n_draft", one, i32)
+        _want(n_draft, "n_draft", one, i32, dev)
         nd = n_draft.data_ptr()
     # (the stride of a dimension of size 1 says nothing)
     ld_draft, ld_u, ld_tokens = (ds[0], us[0], ts[0]) if B > 1 else (T, T, rows)
