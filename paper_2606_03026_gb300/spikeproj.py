@@ -586,6 +586,8 @@ def _reject(x, name, shape, dtype, device):
 def _want(x, name, shape, dtype, device):
     """The strides of a tensor of the shape and type that a call needs, rows
     contiguous, on the CUDA device of that number."""
+    if x is None:
+        raise ValueError(f"{name}: missing")
     st = x.stride()
     if x.shape != shape or x.dtype is not dtype or x.get_device() != device or st[-1] != 1:
         _reject(x, name, shape, dtype, device)
@@ -615,12 +617,16 @@ class Cache:
         counts.  weights (float32 [B, Hkv, capacity]) gains the attention that
         the own entries get; lse (float32 [B, T, Hq]) is optional."""
         t, dev = self.dtype, self._device
+        if q is None:
+            raise ValueError("q: missing")
         B, T = q.shape[0], q.shape[1]
         rows, own = (B, T, self.Hq, self.D), (B, self.capacity, self.Hkv, self.D)
         qs, os = _want(q, "q", rows, t, dev), _want(out, "out", rows, t, dev)
         ks, vs = _want(k, "k", own, t, dev), _want(v, "v", own, t, dev)
         _want(lens, "lens", (B,), self._i32, dev)
         P, pk, pv, pks, pvs = 0, 0, 0, (0, 0), (0, 0)
+        if (prefix_k is None) != (prefix_v is None):
+            raise ValueError("prefix_k, prefix_v: one without the other")
         if prefix_k is not None and prefix_k.shape[0]:
             P = prefix_k.shape[0]
             pks = _want(prefix_k, "prefix_k", (P, self.Hkv, self.D), t, dev)
@@ -647,6 +653,8 @@ class Cache:
         now - recent) and then those of the most weight; K and V [B, capacity,
         Hkv, D] in place, weights and pos [B, Hkv, capacity] into weights_out
         and pos_out [B, Hkv, >= min(budget, capacity)]."""
+        if k is None or weights_out is None:
+            raise ValueError("k, weights_out: missing")
         t, B, dev = self.dtype, k.shape[0], self._device
         own = (B, self.capacity, self.Hkv, self.D)
         ks, vs = _want(k, "k", own, t, dev), _want(v, "v", own, t, dev)
@@ -691,6 +699,8 @@ def verify(p, q, draft, u, u_sample, n_accept, tokens, n_draft=None, stream=None
     n_draft int32 [B] or None; n_accept int32 [B], tokens int32 [B, T+1]."""
     import torch
     f32, i32 = torch.float32, torch.int32
+    if p is None:
+        raise ValueError("p: missing")
     B, rows, V = p.shape
     T, dev = rows - 1, torch.cuda.current_device()
     ps = _want(p, "p", (B, rows, V), f32, dev)

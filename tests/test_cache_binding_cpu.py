@@ -102,3 +102,23 @@ def test_a_tensor_elsewhere_is_refused(library, cache, call, name, device):
     with pytest.raises(ValueError, match=name):
         run(cache, call, args)
     assert not library.calls
+
+
+OPTIONAL = {("attend", "weights"), ("attend", "lse"), ("verify", "n_draft")}
+
+
+@pytest.mark.parametrize("call, name", TENSORS)
+def test_a_missing_tensor_is_refused(library, cache, call, name):
+    """Also one half of a prefix, and drafts without what goes with them."""
+    args = {**MAKE[call](), name: None}
+    if (call, name) in OPTIONAL:
+        return run(cache, call, args)
+    with pytest.raises(ValueError, match=name):
+        run(cache, call, args)
+    assert not library.calls
+
+
+def test_what_a_call_can_do_without(library, cache):
+    run(cache, "attend", attend_args(prefix_k=None, prefix_v=None, weights=None, lse=None))
+    run(cache, "verify", verify_args(p=Tensor((B, 1, V), F32), tokens=Tensor((B, 1), I32), q=None, draft=None, u=None))
+    assert len(library.calls) == 2
