@@ -665,8 +665,9 @@ class Cache:
             raise ValueError("weights_out: no room for the budget")
         left = (B, self.Hkv, room)
         wos, pos_s = _want(weights_out, "weights_out", left, self._f32, dev), _want(pos_out, "pos_out", left, self._i32, dev)
-        if ps[:2] != ws[:2] or pos_s[:2] != wos[:2]:
-            raise ValueError("pos: other strides than weights")
+        for i, n in ((0, B), (1, self.Hkv)):                   # (a dimension of size 1 has no stride)
+            if n > 1 and (ps[i] != ws[i] or pos_s[i] != wos[i]):
+                raise ValueError("pos: other strides than weights")
         one = (B,)
         _want(lens, "lens", one, self._i32, dev)
         _want(now, "now", one, self._i32, dev)

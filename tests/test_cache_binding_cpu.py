@@ -122,3 +122,21 @@ def test_what_a_call_can_do_without(library, cache):
     run(cache, "attend", attend_args(prefix_k=None, prefix_v=None, weights=None, lse=None))
     run(cache, "verify", verify_args(p=Tensor((B, 1, V), F32), tokens=Tensor((B, 1), I32), q=None, draft=None, u=None))
     assert len(library.calls) == 2
+
+
+def test_positions_have_the_weights_strides(library, cache):
+    """Where a dimension has more than one element."""
+    for name, dtype in (("pos", I32), ("pos_out", I32)):
+        for stride in ((HKV * C + 1, C, 1), (HKV * C, C + 1, 1)):
+            with pytest.raises(ValueError, match="strides"):
+                run(cache, "evict", evict_args(**{name: Tensor((B, HKV, C), dtype, stride)}))
+        # one sequence: cut out of a cache whose heads come before its sequences
+        run(cache, "evict", evict_args(batch=1, **{name: Tensor((1, HKV, C), dtype, (C, C, 1))}))
+        # one head
+        one = sp.Cache(B, 2, 1, D, C)
+        one.handle = 1
+        kv = {x: Tensor((B, C, 1, D), BF16) for x in ("k", "v")}
+        entries = {x: Tensor((B, 1, C), F32) for x in ("weights", "weights_out")} | {x: Tensor((B, 1, C), I32) for x in ("pos", "pos_out")}
+        run(one, "evict", evict_args(**kv, **{**entries, name: Tensor((B, 1, C), dtype, (C, 7 * C, 1))}))
+        one.handle = None
+    assert [n for n, _ in library.calls].count("spike_proj_cache_evict") == 4
