@@ -73,6 +73,32 @@ SP_WARP bool walk_ring(int it, int pieces, bool copies, Fetch fetch, Arrived arr
   return copies;
 }
 
+// A row of V 32-bit entries (V < 2^26) that begins `skip` bytes (0, 4, 8 or 12) into
+// 16 is copied in whole 16-byte pieces that lie within it: all but up to three
+// entries at each end.  A bulk copy of entries v .. v + n - 1 and what lies around
+// them up to these boundaries, in bytes from where the row's first 16 begin: `bytes`
+// (<= 0: nothing) from `from` on, for a place that begins with the 16 bytes at `base`.
+struct RowCopy {
+  int32_t base, from, bytes;
+};
+inline __host__ __device__ RowCopy row_copy(int32_t skip, int32_t V, int32_t v, int32_t n) {
+  const int32_t base = (skip + 4 * v) & ~15, from = base == 0 && skip ? 16 : base;
+  const int32_t to = (skip + 4 * (v + n) + 15) & ~15, last = (skip + 4 * V) & ~15;
+  return RowCopy{base, from, (to < last ? to : last) - from};
+}
+// Entries at the ends of two rows that are not copied in one of them at least (of
+// one row: give it twice); lead + trail <= V.
+struct RowEnds {
+  int32_t lead, trail;
+};
+inline __host__ __device__ RowEnds row_ends(int32_t skip_p, int32_t skip_q, int32_t V) {
+  const int32_t lead_p = (16 - skip_p) / 4 & 3, lead_q = (16 - skip_q) / 4 & 3;
+  const int32_t trail_p = (skip_p / 4 + V) & 3, trail_q = (skip_q / 4 + V) & 3;
+  int32_t lead = lead_p > lead_q ? lead_p : lead_q, trail = trail_p > trail_q ? trail_p : trail_q;
+  lead = lead < V ? lead : V;
+  return RowEnds{lead, trail < V - lead ? trail : V - lead};
+}
+
 // Tiles of entries that a call has at most (its launch counts them in 32 bits).
 int64_t attend_tiles(const CacheShape& s, const sp_attend& c);
 cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err,

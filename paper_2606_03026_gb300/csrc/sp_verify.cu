@@ -10,7 +10,9 @@
 // row, their warps contiguous spans of the slice.  A warp streams its span of
 // both rows through a ring in shared memory of its own, in pieces of 512 entries
 // (bulk copies: all that the ring holds is on its way, 64 KB per CTA), and keeps
-// the sums of up to kGroups groups of pieces.  The spans' sums meet in shared
+// the sums of up to kGroups groups of pieces.  Copies are of whole 16 bytes within
+// the row; up to three entries at either end of it are read by themselves, so that
+// nothing beside a row is touched.  The spans' sums meet in shared
 // memory, the slices' in every CTA's (distributed shared memory).  The CTA whose
 // slice the running sum passes c in reads the one group where it does again,
 // every thread a few entries of it.
@@ -18,9 +20,9 @@
 // The row of p and the row of q that the token is drawn from have to be read once
 // (8 V bytes a sequence; the drafts' own entries are a few sectors), which is what
 // bounds it for many sequences: 64 of 57344 entries (25 MB, 3.6 us of memory) take
-// 9.1 us, 200 of 50001 (65 MB, 9.6 us) 19, of which about 5 are the start, the two
+// 9.5 us, 200 of 50001 (65 MB, 9.6 us) 19.5, of which about 5 are the start, the two
 // dependent reads that find the row, and the end; 200 CTAs also leave SMs with one
-// where others have two.  One sequence takes 5.2 us, all of it latency, in a
+// where others have two.  One sequence takes 5.5 us, all of it latency, in a
 // cluster of 16 CTAs.  Rings: 1 row piece of 1024 entries, 6 of 256 and 3 of 512 were
 // measured slower (200 sequences 26, 28 and 19.4 us).
 #include <math.h>
@@ -52,48 +54,67 @@ __device__ __forceinline__ unsigned long long whole(float r) {
   return r > 0.f ? __float2ull_rn(fminf(r, 1.f) * 0x1p36f) : 0ull;
 }
 
-// `count` entries of a row, in the 16-byte pieces that hold them.
-__device__ __forceinline__ uint32_t piece_bytes(const float* from, int count) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(from);
-  return (uint32_t)(((a + 4 * (uintptr_t)count + 15) & ~(uintptr_t)15) - (a & ~(uintptr_t)15));
-}
-__device__ __forceinline__ const float* piece_base(const float* from) {
-  return reinterpret_cast<const float*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15);
-}
-__device__ __forceinline__ int piece_skip(const float* from) {
-  return (int)(reinterpret_cast<uintptr_t>(from) & 15) / 4;
-}
-
 // Sum of the whole numbers of entries v0 .. v1 of a warp, the groups' into
 // `groups`.  it: pieces that have gone through the ring before; copies: every
 // copy so far has arrived.
-__device__ __forceinline__ unsigned long long sum_span(const float* pr, const float* qr, int v0, int v1, int per_group,
-                                                       uint8_t* ring, uint64_t* full, int& it, bool& copies,
+__device__ __forceinline__ unsigned long long sum_span(const float* pr, const float* qr, int V, int v0, int v1,
+                                                       int per_group, uint8_t* ring, uint64_t* full, int& it, bool& copies,
                                                        unsigned long long* groups) {
   const int lane = threadIdx.x & 31;
   const int pieces = ceil_div(max(v1 - v0, 0), kPiece);
+  // where the rows begin in their first 16 bytes, and those
+  const int p_skip = (int)(reinterpret_cast<uintptr_t>(pr) & 15), q_skip = qr ? (int)(reinterpret_cast<uintptr_t>(qr) & 15) : p_skip;
+  const uint8_t *p16 = reinterpret_cast<const uint8_t*>(pr) - p_skip, *q16 = reinterpret_cast<const uint8_t*>(qr) - q_skip;
+  // the first piece's 16 bytes, and what a whole one takes
+  const int p_base = (p_skip + 4 * v0) & ~15, q_base = (q_skip + 4 * v0) & ~15;
+  const int p_bytes = 4 * kPiece + ((p_skip + 4 * v0) & 15 ? 16 : 0), q_bytes = 4 * kPiece + ((q_skip + 4 * v0) & 15 ? 16 : 0);
   const auto fetch = [&](int i, int st) {
     if (lane != 0) return;
     const int v = v0 + i * kPiece, n = min(kPiece, v1 - v);
     uint8_t* to = ring + st * 2 * kPieceBytes;
-    mbar_arrive_expect_tx(&full[st], piece_bytes(pr + v, n) + (qr ? piece_bytes(qr + v, n) : 0u));
-    bulk_load(to, piece_base(pr + v), piece_bytes(pr + v, n), &full[st]);
-    if (qr) bulk_load(to + kPieceBytes, piece_base(qr + v), piece_bytes(qr + v, n), &full[st]);
+    if (n == kPiece && v >= 4 && v + kPiece <= V - 4) {
+      mbar_arrive_expect_tx(&full[st], p_bytes + (qr ? q_bytes : 0));
+      bulk_load(to, p16 + p_base + 4 * kPiece * i, p_bytes, &full[st]);
+      if (qr) bulk_load(to + kPieceBytes, q16 + q_base + 4 * kPiece * i, q_bytes, &full[st]);
+      return;
+    }
+    const RowCopy x = row_copy(p_skip, V, v, n);
+    RowCopy y = row_copy(q_skip, V, v, n);
+    if (!qr) y.bytes = 0;
+    mbar_arrive_expect_tx(&full[st], max(x.bytes, 0) + max(y.bytes, 0));
+    if (x.bytes > 0) bulk_load(to + (x.from - x.base), p16 + x.from, x.bytes, &full[st]);
+    if (y.bytes > 0) bulk_load(to + kPieceBytes + (y.from - y.base), q16 + y.from, y.bytes, &full[st]);
   };
   const auto arrived = [&](int st, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_try_wait(&full[st], parity) || mbar_wait(&full[st], parity)) != 0;
   };
+  // The entries at the rows' ends that are not copied: a lane each, read here and
+  // put where the copy would have left them.
+  const RowEnds ends = row_ends(p_skip, q_skip, V);
+  const int end = lane < ends.lead ? lane : lane >= 32 - ends.trail ? V - 32 + lane : -1;
+  float p_end = 0.f, q_end = 0.f;
+  if (end >= v0 && end < v1) {
+    p_end = __ldg(pr + end);
+    if (qr) q_end = __ldg(qr + end);
+  }
   const auto use = [&](int i, int st, bool here) {
     const int v = v0 + i * kPiece, n = min(kPiece, v1 - v);
-    const float* x = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes) + piece_skip(pr + v);
-    const float* y = reinterpret_cast<const float*>(ring + st * 2 * kPieceBytes + kPieceBytes) + (qr ? piece_skip(qr + v) : 0);
-    // (once a copy has not arrived in time, the rows are read themselves)
-    if (!here) {
-      x = pr + v;
-      y = qr + v;
+    float* x = reinterpret_cast<float*>(ring + st * 2 * kPieceBytes + ((p_skip + 4 * v) & 15));
+    float* y = reinterpret_cast<float*>(ring + st * 2 * kPieceBytes + kPieceBytes + ((q_skip + 4 * v) & 15));
+    unsigned long long sum = 0;
+    if (!here) {                           // a copy has not arrived in time: the rows themselves
+      for (int e = lane; e < n; e += 32) sum += whole(qr ? __ldg(pr + v + e) - __ldg(qr + v + e) : __ldg(pr + v + e));
+      return sum;
+    }
+    if (v < ends.lead || v + n > V - ends.trail) {
+      if (end >= v && end < v + n) {
+        x[end - v] = p_end;
+        y[end - v] = q_end;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // (before another copy there)
+      }
+      __syncwarp();
     }
     // nearly every number fits 32 bits, whose conversion is several times faster
-    unsigned long long sum = 0;
     float most = 0.f;
     if (n == kPiece) {
 #pragma unroll
@@ -176,7 +197,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerPerSm) verify_kernel(const __
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");   // every CTA of the cluster is running
   for (int pass = 0;; ++pass) {
     const unsigned long long sum =
-        sum_span(pr, qr, v0, v1, p.per_group, s_ring + (size_t)warp * kRing * 2 * kPieceBytes, s_full[warp], it, copies,
+        sum_span(pr, qr, c.V, v0, v1, p.per_group, s_ring + (size_t)warp * kRing * 2 * kPieceBytes, s_full[warp], it, copies,
                  s_group[warp]);
     if (lane == 0) s_warp[warp] = sum;
     __syncthreads();

@@ -17,6 +17,18 @@ void arith_share(int32_t n, int32_t sub, int32_t parts, int32_t* begin, int32_t*
   *end = s.end;
 }
 
+void arith_row_copy(int32_t skip, int32_t V, int32_t v, int32_t n, int32_t* copy) {
+  const sp::RowCopy c = sp::row_copy(skip, V, v, n);
+  copy[0] = c.base;
+  copy[1] = c.from;
+  copy[2] = c.bytes;
+}
+void arith_row_ends(int32_t skip_p, int32_t skip_q, int32_t V, int32_t* lead, int32_t* trail) {
+  const sp::RowEnds e = sp::row_ends(skip_p, skip_q, V);
+  *lead = e.lead;
+  *trail = e.trail;
+}
+
 // The walk of rows of pieces[0 .. rows - 1] pieces through a ring of two places
 // whose copies behave as how[] says, one after another: 0 it arrives at once, 1
 // after the time of a wait that runs out, 2 never.  Returns 0 where every piece was

@@ -65,6 +65,29 @@ def test_no_copy_of_a_verification_is_left_on_its_way(arith, pieces):
         assert arith.arith_ring(len(pieces), rows, (ctypes.c_int * len(how))(*how)) == 0, (at, what, rest)
 
 
+@pytest.mark.parametrize("V", [*range(1, 24), 511, 512, 513, 1030, (1 << 24) - 1])
+def test_a_verification_copies_nothing_outside_its_rows(arith, V):
+    """Copies are of whole 16-byte pieces of a row, and with the entries read by
+    themselves at its ends they are all of it, wherever both rows begin and
+    however they are cut."""
+    copy = (ctypes.c_int32 * 3)()
+    for p, q in itertools.product((0, 4, 8, 12), repeat=2):
+        lead, trail = two(arith.arith_row_ends, p, q, V)
+        assert 0 <= lead <= 3 and 0 <= trail <= 3 and lead + trail <= V
+        for skip, cut in itertools.product({p, q}, (1, 2, 3, 5, 64, 512)):
+            for v in range(0, V, cut) if V < 2000 else [0, cut, (V - 1) // cut * cut - cut, (V - 1) // cut * cut]:
+                n = min(cut, V - v)
+                arith.arith_row_copy(skip, V, v, n, copy)
+                base, start, size = copy
+                end = start + max(size, 0)
+                if size > 0:
+                    assert start % 16 == 0 and size % 16 == 0 and skip <= start and end <= skip + 4 * V
+                # the place in the ring: from the 16 bytes on that hold the piece's first entry
+                assert base == (skip + 4 * v) // 16 * 16 and start >= base and end - base <= 4 * n + 32
+                for e in range(max(v, lead), min(v + n, V - trail)):
+                    assert start <= skip + 4 * e and skip + 4 * e + 4 <= end
+
+
 OWN = {name: (i + 1) * FAKE for i, name in enumerate(("weights", "pos", "lens", "now", "weights_out", "pos_out", "lens_out"))}
 
 

@@ -1,5 +1,6 @@
 """Attention, eviction and verification where sums vanish, offsets are long and
 rows are wide."""
+import itertools
 import math
 
 import pytest
@@ -58,3 +59,23 @@ def test_a_verification_in_the_place_of_its_drafts(B, T, V):
         both, row = count.clone(), torch.cat([draft, draft[:, :1]], 1)
         sp.verify(p, q, row[:, :T], u, us, both, row, n_draft=both)
         assert torch.equal(both, n) and torch.equal(row, tokens)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 4, 5, 6, 7, 9, 66, 511, 512, 514, 1025, 4097, 30002])
+def test_a_verification_of_rows_that_begin_anywhere(V):
+    """p and q off 16 bytes by 0 to 12, all of the residual at either end of the
+    row; what lies beside the rows would be drawn if it were read."""
+    for shift_p, shift_q, end in itertools.product(range(4), range(4), (0, 1)):
+        some = min(V, 3)
+        at = torch.arange(some) if end == 0 else torch.arange(V - some, V)
+        p, q = (torch.full((V + 8,), math.inf, device=DEV) for _ in range(2))
+        p, q = p[shift_p:shift_p + V], q[shift_q:shift_q + V]
+        p.zero_(), q.zero_()
+        p[at.to(DEV)] = 0.5
+        q[at[0]] = 0.5                       # (its residual is 0)
+        first, second = (at[1], at[-1]) if some > 1 else (at[0], at[0])
+        for u, want in ((0.0, first), (0.999, second)):
+            n, token = torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1, 2, dtype=torch.int32, device=DEV)
+            sp.verify(p.expand(1, 2, V), q.view(1, 1, V), torch.full((1, 1), -1, dtype=torch.int32, device=DEV),
+                      torch.zeros(1, 1, device=DEV), torch.tensor([u], device=DEV), n, token)
+            assert token.tolist() == [[int(want), -1]] and int(n) == 0, (shift_p, shift_q, end, u)
