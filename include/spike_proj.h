@@ -736,9 +736,16 @@ sp_status spike_proj_verify(const sp_verify *call, sp_stream_t stream);
  *                   comes last, and the results are exact, with no error.
  *                   Other kernels ignore it (it is still disarmed by their
  *                   launch).
+ *                   A cache's next attend call: no CTA copies its first tile
+ *                   of keys, and the waits for these, bounded by about 2 ms,
+ *                   run out: the kernel raises the error word, drains its
+ *                   copies and frees its tensor memory, and what the call
+ *                   leaves in out, lse and weights is not to be used.  (The
+ *                   only fault of a cache; its evict calls do not wait.)
  * No fault traps, faults the GPU or spins without bound.  spike_proj_plan_status
- * / spike_proj_group_status then return SP_EKERNEL, clear the error word and
- * re-zero the workspace, and the next call is exact again.
+ * / spike_proj_group_status / spike_proj_cache_status then return SP_EKERNEL,
+ * clear the error word and (the first two) re-zero the workspace, and the next
+ * call is exact again.
  * Errors: SP_EINVAL (NULL, unknown fault).
  * ------------------------------------------------------------------------- */
 typedef enum sp_fault {
@@ -748,6 +755,7 @@ typedef enum sp_fault {
 } sp_fault;
 sp_status spike_proj_plan_inject_fault(sp_plan_t plan, int32_t fault);
 sp_status spike_proj_group_inject_fault(sp_group_t group, int32_t fault);
+sp_status spike_proj_cache_inject_fault(sp_cache_t cache, int32_t fault);
 
 /* ---------------------------------------------------------------------------
  * spike_proj_probe_gather -- MEASUREMENT AID, not part of the method (the

@@ -10,6 +10,7 @@
 #include <mutex>
 #include <new>
 #include <thread>
+#include <utility>
 
 #include "sp_cache.h"
 #include "sp_gemm.h"
@@ -85,6 +86,7 @@ struct sp_cache_s {
   CacheShape shape;
   uint8_t* ws = nullptr;          // cache_workspace(shape).bytes
   int* err = nullptr;             // device error word
+  int32_t fault = SP_FAULT_NONE;  // armed for the next attend call
 };
 
 struct sp_group_s {
@@ -1047,6 +1049,12 @@ sp_status spike_proj_group_inject_fault(sp_group_t group, int32_t fault) {
   return SP_OK;
 }
 
+sp_status spike_proj_cache_inject_fault(sp_cache_t cache, int32_t fault) {
+  if (!cache || (fault != SP_FAULT_NONE && fault != SP_FAULT_STALL)) return SP_EINVAL;
+  cache->fault = fault;
+  return SP_OK;
+}
+
 sp_status spike_proj_probe_gather(const void* base, const uint32_t* offsets16, int32_t count,
                                   int32_t piece_bytes, uint32_t* sink, sp_stream_t stream) {
   if (!base || !sink || count < 0 || (count > 0 && !offsets16)) return SP_EINVAL;
@@ -1255,7 +1263,7 @@ sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend* c, sp_strea
     return SP_EALIGN;
   const sp_status st = on_device(cache->device);
   if (st != SP_OK) return st;
-  SP_CUDA(launch_attend(sh, *c, cache->ws, cache->err, as_stream(stream)));
+  SP_CUDA(launch_attend(sh, *c, cache->ws, cache->err, std::exchange(cache->fault, SP_FAULT_NONE), as_stream(stream)));
   return SP_OK;
 }
 

@@ -115,6 +115,8 @@ struct AttnParams {
   bool whole_rows;          // D is DK = 128: a tile of K or V is one copy
   float c2;                 // scale * log2 e
   int* err;
+  int fault;                // kFaultStall: first copies are left out (tests of the error path)
+  long long limit;          // cycles that a wait takes at most
   int2* unit_ctas;          // first and last CTA of each prefix unit, of each own unit that has tiles
   float4* p_ml;             // prefix slots: [slot][128] reference, sum, sum of the rounded
   float* p_o;               //               [slot][128][DK]
@@ -297,12 +299,12 @@ __device__ __forceinline__ uint64_t n_major_desc(const void* p, uint32_t block) 
 
 // Bounded wait, inline (a call would cost the softmax's loop its registers);
 // false too when another warp of the CTA has given up (`stop`, where given).
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, const volatile int* stop = nullptr) {
+__device__ __forceinline__ bool wait(const AttnParams& p, uint64_t* bar, uint32_t parity, const volatile int* stop = nullptr) {
   if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   do {
     if (mbar_try_wait(bar, parity)) return true;
-  } while (!(stop && *stop) && clock64() - t0 < kWaitLimitCycles);
+  } while (!(stop && *stop) && clock64() - t0 < p.limit);
   return false;
 }
 
@@ -363,7 +365,7 @@ __device__ __forceinline__ bool softmax_tile(const AttnParams& p, RowState& r, u
     r.l *= a;
     r.rl *= a;
     if (!first) {
-      if (!__all_sync(0xffffffffu, wait(pv, pv_parity))) return false;
+      if (!__all_sync(0xffffffffu, wait(p, pv, pv_parity))) return false;
       tc_fence_after();
 #pragma unroll 1                           // (rare, and registers are short)
       for (int i = 0; i < (DK + kOnes<DK>) / 16; ++i) {
@@ -538,10 +540,10 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     const uint64_t normal = l2_evict_normal(), own = p.rows.own_units == 1 ? l2_evict_first() : normal;
     RowPlaces places;
     bool rows = k.count > 0;               // the query rows of the keys' segment are to come
-    const auto issue = [&](Cursor& c, int n, uint8_t* ring, uint64_t* full, const CUtensorMap* of_prefix,
+    const auto issue = [&](Cursor& c, uint32_t copy, int n, uint8_t* ring, uint64_t* full, const CUtensorMap* of_prefix,
                            const CUtensorMap* of_own) {
       mbar_arrive_expect_tx_if(one, &full[c.st], kBytes);
-      load_tile<DK>(one, ring + c.st * kBytes, c.prefix ? of_prefix : of_own, &full[c.st], p.whole_rows, c.entry, c.h,
+      load_tile<DK>(copy, ring + c.st * kBytes, c.prefix ? of_prefix : of_own, &full[c.st], p.whole_rows, c.entry, c.h,
                     c.prefix ? 0 : c.b, c.prefix ? normal : own);
       c.entry += kTile;
       ++c.j;
@@ -550,6 +552,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         ++c.phase;
       }
     };
+    uint32_t copy = p.fault == kFaultStall ? 0u : one;       // (a test's fault leaves the first keys out)
     bool ok = true;
     int idle = 0;
     long long since = 0;
@@ -558,11 +561,12 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       const bool k_free = mbar_test(&k_empty[k.st], k.phase & 1 ^ 1), v_free = mbar_test(&v_empty[v.st], v.phase & 1 ^ 1);
       bool moved = false;
       if (k.j < k.count && all(k_free)) {
-        issue(k, NK, sK, k_full, &maps.pk, &maps.k);
+        issue(k, copy, NK, sK, k_full, &maps.pk, &maps.k);
+        copy = one;
         moved = true;
       }
       if (v.count > 0 && all(v_free)) {
-        issue(v, NV, sV, v_full, &maps.pv, &maps.v);
+        issue(v, one, NV, sV, v_full, &maps.pv, &maps.v);
         if (v.j == v.count) enter(v, v.next);
         moved = true;
       }
@@ -591,7 +595,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         idle = 0;
       } else {
         if (idle++ == 0) since = clock64();
-        if (!all(!*s_abort && clock64() - since <= kWaitLimitCycles)) {
+        if (!all(!*s_abort && clock64() - since <= p.limit)) {
           ok = false;
           break;
         }
@@ -600,12 +604,12 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     if (!ok) {
       *s_abort = 1;
       atomicExch(p.err, kErrMbarTimeout);
-      for (int i = 0; i < 2; ++i) wait(&q_full[i], places.used >> i & 1 ^ 1);
+      for (int i = 0; i < 2; ++i) wait(p, &q_full[i], places.used >> i & 1 ^ 1);
     }
     // the last copies have landed
     const auto landed = [&](const Cursor& c, int n, uint64_t* full) {
       for (int i = 0; i < n; ++i)
-        if (i < c.st || c.phase > 0) wait(&full[i], (i < c.st ? c.phase : c.phase - 1) & 1);
+        if (i < c.st || c.phase > 0) wait(p, &full[i], (i < c.st ? c.phase : c.phase - 1) & 1);
     };
     landed(k, NK, k_full);
     landed(v, NV, v_full);
@@ -621,7 +625,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
     const auto all = [](bool x) { return __all_sync(0xffffffffu, x) != 0; };
     const auto scores = [&](int i, int halves, bool last) {
       const int st = i % NK;
-      if (!all(wait(&k_full[st], (i / NK) & 1, s_abort))) return false;
+      if (!all(wait(p, &k_full[st], (i / NK) & 1, s_abort))) return false;
       tc_fence_after();
       // (half a place on the MMA's later rows read what is there: nobody reads theirs)
       const uint64_t qd = smem_desc(sQ + (halves == 2 ? kQBlock / 2 : 0), 1024, kSwizzle128);
@@ -644,8 +648,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       const int halves = __shfl_sync(0xffffffffu, places.of(next.prefix ? p.rows.prefix_rows : p.rows.own_rows), 0);
       // (the buffer of tile i + 1 is that of tile i - 1, whose product with V,
       // issued before, reads the probabilities there first)
-      ok = all(((halves & 1) == 0 || wait(&q_full[0], places.used & 1, s_abort)) &&
-               ((halves & 2) == 0 || wait(&q_full[1], places.used >> 1, s_abort))) &&
+      ok = all(((halves & 1) == 0 || wait(p, &q_full[0], places.used & 1, s_abort)) &&
+               ((halves & 2) == 0 || wait(p, &q_full[1], places.used >> 1, s_abort))) &&
            scores(it, halves, count == 1);
       places.take(halves);
       const int x = next.next;             // (the next segment, while the first softmax runs)
@@ -655,8 +659,8 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         const int st = it % NV;
         if (j + 1 < count) ok = scores(it + 1, halves, j + 2 == count);
         if (ok)
-          ok = all(wait(&v_full[st], (it / NV) & 1, s_abort) && (j > 0 || wait(o_empty, (seg & 1) ^ 1u, s_abort)) &&
-                   wait(&p_full[it & 1], (it >> 1) & 1, s_abort));
+          ok = all(wait(p, &v_full[st], (it / NV) & 1, s_abort) && (j > 0 || wait(p, o_empty, (seg & 1) ^ 1u, s_abort)) &&
+                   wait(p, &p_full[it & 1], (it >> 1) & 1, s_abort));
         if (!ok) break;
         tc_fence_after();
         const uint64_t vd = n_major_desc(sV + st * kBytes, kOnes<DK> ? (NV - st) * kBytes : kBlock);
@@ -672,7 +676,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       atomicExch(p.err, kErrMbarTimeout);
     }
     mma_commit_if(one, done);              // every MMA has retired
-    wait(done, 0);
+    wait(p, done, 0);
   } else {
     // ------------------------------ softmax -------------------------------------
     const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
@@ -689,7 +693,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       RowState r = {-INFINITY, 0.f, 0.f, 0.f};
       for (int j = 0; j < s.count; ++j, ++it) {
         const int nv = min(kTile, s.seen - (s.j0 + j) * kTile);
-        ok = __all_sync(0xffffffffu, wait(&s_full[it & 1], (it >> 1) & 1, s_abort));
+        ok = __all_sync(0xffffffffu, wait(p, &s_full[it & 1], (it >> 1) & 1, s_abort));
         if (!ok) break;
         tc_fence_after();
         uint32_t v[2][32];
@@ -702,7 +706,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
         if (!s.prefix && nv < kTile) {
           // entries past those in use hold anything: their values become 0
           const int st = it % NV;
-          ok = __all_sync(0xffffffffu, wait(&v_full[st], (it / NV) & 1, s_abort));
+          ok = __all_sync(0xffffffffu, wait(p, &v_full[st], (it / NV) & 1, s_abort));
           if (!ok) break;
           if (threadIdx.x >= nv && threadIdx.x < kTile) {
 #pragma unroll
@@ -727,7 +731,7 @@ attend_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ Att
       if (!ok) break;
       next.count = 0;                      // (the next segment, while the last product is computed)
       if (s.next < x1) next = segment_at(p, line, s_off, s.next, x1, cta);
-      ok = __all_sync(0xffffffffu, wait(o_full, seg & 1, s_abort));
+      ok = __all_sync(0xffffffffu, wait(p, o_full, seg & 1, s_abort));
       if (!ok) break;
       tc_fence_after();
       if (work) {
@@ -1191,7 +1195,8 @@ int64_t attend_tiles(const CacheShape& s, const sp_attend& c) {
                   (int64_t)c.B * r.own_units * ceil_div(s.capacity, kTile));
 }
 
-cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err, cudaStream_t stream) {
+cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err, int fault,
+                          cudaStream_t stream) {
   int dev = 0, sms = 0;
   const cudaError_t e = current_device(&dev, &sms);
   if (e != cudaSuccess) return e;
@@ -1215,6 +1220,8 @@ cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, 
   p.c2 = c.scale * kLog2e;
   p.whole_rows = s.D == 128;
   p.err = err;
+  p.fault = fault;
+  p.limit = fault == kFaultStall ? kStallWaitCycles : kWaitLimitCycles;
   p.grid = 2 * sms;
   const Parts w = parts_of(s, c.B, c.T, p.grid);
   p.unit_ctas = reinterpret_cast<int2*>(ws + w.units);

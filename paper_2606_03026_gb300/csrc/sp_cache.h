@@ -101,7 +101,7 @@ inline __host__ __device__ RowEnds row_ends(int32_t skip_p, int32_t skip_q, int3
 
 // Tiles of entries that a call has at most (its launch counts them in 32 bits).
 int64_t attend_tiles(const CacheShape& s, const sp_attend& c);
-cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err,
+cudaError_t launch_attend(const CacheShape& s, const sp_attend& c, uint8_t* ws, int* err, int fault,
                           cudaStream_t stream);
 cudaError_t launch_evict(const CacheShape& s, const sp_evict& c, uint8_t* ws, cudaStream_t stream);
 cudaError_t launch_verify(const sp_verify& c, cudaStream_t stream);

@@ -83,6 +83,7 @@ _SIGNATURES = {
     "spike_proj_probe_gather": ([_P, _P, _I32, _I32, _P, _P], ctypes.c_int),
     "spike_proj_plan_inject_fault": ([_P, _I32], ctypes.c_int),
     "spike_proj_group_inject_fault": ([_P, _I32], ctypes.c_int),
+    "spike_proj_cache_inject_fault": ([_P, _I32], ctypes.c_int),
     "spike_proj_strerror": ([ctypes.c_int], ctypes.c_char_p),
     "spike_proj_last_cuda_error": ([], ctypes.c_int),
     "spike_proj_abi_version": ([], ctypes.c_int),
@@ -336,6 +337,11 @@ def spike_proj_plan_inject_fault(plan, fault):
 def spike_proj_group_inject_fault(group, fault):
     """Tests of the error path only: arm a fault for the group's next launch."""
     _check(lib().spike_proj_group_inject_fault(group, fault), "spike_proj_group_inject_fault")
+
+
+def spike_proj_cache_inject_fault(cache, fault):
+    """Tests of the error path only: arm a fault for the cache's next attend call."""
+    _check(lib().spike_proj_cache_inject_fault(cache, fault), "spike_proj_cache_inject_fault")
 
 
 def spike_proj_strerror(status) -> str:
@@ -680,6 +686,10 @@ class Cache:
 
     def status(self, stream=None) -> int:
         return spike_proj_cache_status(self.handle, stream)
+
+    def inject_fault(self, fault):
+        """Tests of the error path only (SP_FAULT_STALL)."""
+        spike_proj_cache_inject_fault(self.handle, fault)
 
     def close(self):
         if self.handle:

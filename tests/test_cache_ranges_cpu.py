@@ -105,3 +105,10 @@ def test_an_eviction_whose_output_is_an_input_is_refused(lib, cache, out, given)
 def test_an_eviction_of_everything_needs_no_outputs_of_entries(lib, cache):     # noqa: F811
     call = evict_call(**{**OWN, "weights_out": None, "pos_out": None, "budget": 0, "recent": 0})
     assert lib.spike_proj_cache_evict(cache, ctypes.byref(call), None) == sp.SP_OK
+
+
+def test_a_fault_of_a_cache_is_a_stall(lib, cache):                             # noqa: F811
+    for fault, want in ((sp.SP_FAULT_STALL, sp.SP_OK), (sp.SP_FAULT_NONE, sp.SP_OK), (sp.SP_FAULT_ABORT, sp.SP_EINVAL),
+                        (3, sp.SP_EINVAL), (-1, sp.SP_EINVAL)):
+        assert lib.spike_proj_cache_inject_fault(cache, fault) == want
+    assert lib.spike_proj_cache_inject_fault(None, sp.SP_FAULT_STALL) == sp.SP_EINVAL
