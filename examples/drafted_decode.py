@@ -7,7 +7,8 @@ embeddings.  Every step of the batch
            attention (projection by sp.dense, drawing by sp.verify without drafts)
   appends  the entries of the last token and the drafts to the own caches
   attends  with all of them to the prompt and the own entries, whose attention
-           weight adds up over the steps (Cache.attend)
+           weight adds up over the steps (Cache.attend; the queries of drafts
+           that are refused afterwards have counted too)
   verifies the drafts against the decoder's probabilities (sp.verify); the
            entries of those that were not kept are dropped
   evicts   when a cache has come near its capacity: the entries of the most

@@ -567,6 +567,9 @@ sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream);
  *     weights[b][h][j] += sum over query tokens t and the query heads of K/V
  *                         head h of exp(s_j - lse)      (own entries, FP32)
  *
+ * weights takes all T query tokens, also drafts that a verification refuses
+ * afterwards: what their queries gave to entries that stay remains there.
+ *
  * A row that sees no entry (or scores of minus infinity alone) gives out = 0,
  * lse = -infinity and no weight.  Entries that no row sees are never used,
  * whatever they hold; a NaN key that a row sees makes that row NaN and a NaN

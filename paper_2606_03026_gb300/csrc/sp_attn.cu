@@ -43,19 +43,23 @@
 // arithmetic is 370 at full rate.  Tiles of 64 entries with the scores one tile
 // ahead, because tensor memory holds no more for 128-wide heads and two CTAs (128
 // entries without: 128 drafting sequences 291 us, with 64: 212 at that state).
-// Measured (a call, its three kernels together): 128 sequences of 5 tokens, 16 query
-// heads on 4 of 128, prefix 16384, own 512 to 2048, with weights: 138 us, the floor of
-// its bytes 56, of its operations 48, tensor pipe busy 74 % in attend_kernel (111 us);
-// 16 sequences over a document of 131072: 54 us, 5.1 TB/s; 64 chats over 2048 with own
-// caches of up to 1024: 26.2 us (floor 10.7), the kernel itself 21; 32 drafting sequences
-// with 64-wide heads over 8191: 47 us (floor 13); one sequence of 60 entries over 512:
-// 10.2 us, two launches' latency.
+// Measured (a call, its three kernels together, replayed from a graph on three sets of
+// inputs in turn; by itself a call takes about 1 us more, and the largest at the power
+// limit's clock 145): 128 sequences of 5 tokens, 16 query heads on 4 of 128, prefix
+// 16384, own 512 to 2048, with weights: 141 us, the floor of its bytes 56, of its
+// operations 48, tensor pipe busy 67 to 74 % in attend_kernel (111 us); 16 sequences over
+// a document of 131072: 53.4 us, 5.2 TB/s; 64 chats over 2048 with own caches of up to
+// 1024: 26.6 us (floor 10.7), the kernel itself 21; 32 drafting sequences with 64-wide
+// heads over 8191: 47.5 us (floor 13); one sequence of 60 entries over 512: 10.0 us, two
+// launches' latency.
 //
 // combine_kernel: half a warp to eight warps per query row merge its partial results
-// and these last entries; latency, and for many rows the instructions of a row (10240
-// rows 12 us).  weights_kernel: the weights, from the scores of the own entries that
-// attend_kernel left in the workspace and the rows' lse; 4 bytes written and read
-// per own entry and query row (128 drafting sequences: 52 MB, 13 us).
+// and these last entries, row by row (right for any T, meant for a few drafts: 16
+// sequences with 1 / 8 / 16 / 32 tokens 16 / 23 / 27 / 41 us a call); latency, and for
+// many rows the instructions of a row (10240 rows 12 us).  weights_kernel: the weights,
+// from the scores of the own entries that attend_kernel left in the workspace and the
+// rows' lse; 4 bytes written and read per own entry and query row (128 drafting
+// sequences: 52 MB, 13 us).
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cudaTypedefs.h>

@@ -21,10 +21,13 @@
 //
 // Weights and pos have to be read once (8 bytes an entry), and what moves copied
 // once.  Cutting 16 prompts of 3000 to 16384 entries, 8 heads each, to 4096 reads and
-// writes 150 MB, 22 us of memory, in 41.6 us: about 24 us in move_kernel, whose rows
-// of 128 bytes lie scattered, and before it the selection, in a CTA a chain of
-// latencies (keys 5 us, digits 3.5, kept words and list 4).  64 sequences of 2048 to
-// 2056 entries take 7.3 us, one of 1029 4.8: start, keys, one digit, one ranking.
+// writes 150 MB, 22 us of memory, in 40 us (replayed from a graph): about 24 us in
+// move_kernel, whose rows of 128 bytes lie scattered, and before it the selection, in a
+// CTA a chain of latencies (keys 5 us, digits 3.5, kept words and list 4).  64 sequences
+// of 2048 to 2056 entries take 7.1 us, one of 1029 4.8: start, keys, one digit, one
+// ranking.  The second kernel's grid goes by the moves that budget and capacity allow: up
+// to 8 of 8200 entries of 512 heads leave in 26 us where the capacity is 8200, and in 102
+// where it is 16384.
 #include <math.h>
 
 #include "sp_cache.h"

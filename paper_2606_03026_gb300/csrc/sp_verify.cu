@@ -20,7 +20,7 @@
 // The row of p and the row of q that the token is drawn from have to be read once
 // (8 V bytes a sequence; the drafts' own entries are a few sectors), which is what
 // bounds it for many sequences: 64 of 57344 entries (25 MB, 3.6 us of memory) take
-// 9.5 us, 200 of 50001 (65 MB, 9.6 us) 19.5, of which about 5 are the start, the two
+// 9.6 us (replayed from a graph), 200 of 50001 (65 MB, 9.6 us) 19.7, of which about 5 are the start, the two
 // dependent reads that find the row, and the end; 200 CTAs also leave SMs with one
 // where others have two.  One sequence takes 5.5 us, all of it latency, in a
 // cluster of 16 CTAs.  Rings: 1 row piece of 1024 entries, 6 of 256 and 3 of 512 were

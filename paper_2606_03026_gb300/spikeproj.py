@@ -621,7 +621,8 @@ class Cache:
         """T query tokens per sequence, q [B, T, Hq, D] -> out [B, T, Hq, D]; the
         own caches already hold the T tokens' entries, which lens (int32 [B])
         counts.  weights (float32 [B, Hkv, capacity]) gains the attention that
-        the own entries get; lse (float32 [B, T, Hq]) is optional."""
+        the own entries get from all T tokens (of drafts that are refused later
+        too); lse (float32 [B, T, Hq]) is optional."""
         t, dev = self.dtype, self._device
         if q is None:
             raise ValueError("q: missing")
