@@ -79,3 +79,40 @@ def test_a_verification_of_rows_that_begin_anywhere(V):
             sp.verify(p.expand(1, 2, V), q.view(1, 1, V), torch.full((1, 1), -1, dtype=torch.int32, device=DEV),
                       torch.zeros(1, 1, device=DEV), torch.tensor([u], device=DEV), n, token)
             assert token.tolist() == [[int(want), -1]] and int(n) == 0, (shift_p, shift_q, end, u)
+
+
+@pytest.mark.parametrize("B,Hkv,C,budget", [(16, 8, 12000, 3000), (3, 2, 300, 250), (64, 4, 2056, 2048)])
+def test_calls_back_to_back_see_each_others_results(B, Hkv, C, budget):
+    """attend, evict, attend, evict, .. on two sets of buffers in turn, each launched
+    while the one before may still run: as with the device waited for in between."""
+    D, T = 64, 2
+
+    def run(wait):
+        g = torch.Generator(device=DEV).manual_seed(6)
+        k, v = (torch.randn(B, C, Hkv, D, generator=g, device=DEV).bfloat16() for _ in range(2))
+        q = torch.randn(B, T, 2 * Hkv, D, generator=g, device=DEV).bfloat16()
+        pk, pv = (torch.randn(100, Hkv, D, generator=g, device=DEV).bfloat16() for _ in range(2))
+        lens = torch.zeros(2, B, dtype=torch.int32, device=DEV)             # (both in one sector for few sequences)
+        lens[0] = torch.randint(C // 2, C + 1, (B,), generator=g, device=DEV)
+        now, w = lens[0].clone(), torch.zeros(2, B, Hkv, C, device=DEV)
+        pos = torch.arange(C, dtype=torch.int32, device=DEV).expand(2, B, Hkv, C).contiguous()
+        outs = [torch.zeros_like(q) for _ in range(6)]
+        torch.cuda.synchronize()
+        for i in range(6):
+            a, b = i % 2, 1 - i % 2
+            cache.attend(q, k, v, lens[a], outs[i], pk, pv, w[a])
+            if wait:
+                torch.cuda.synchronize()
+            cache.evict(k, v, w[a], pos[a], lens[a], now, budget - 10 * i, 16, w[b], pos[b], lens[b])
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return [*outs, k, v, w, pos, lens]
+
+    cache = sp.Cache(B, 2 * Hkv, Hkv, D, C, max_T=T, weights=True)
+    want = run(True)
+    for _ in range(10):
+        for x, y in zip(run(False), want):
+            assert torch.equal(x, y)
+    assert cache.status() == sp.SP_OK
+    cache.close()
