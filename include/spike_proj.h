@@ -29,7 +29,10 @@
  * a KV cache: attention of a batch that shares a long prefix
  * (spike_proj_cache_attend), eviction by accumulated attention weight
  * (spike_proj_cache_evict) and verification of the drafts
- * (spike_proj_verify).  Each is documented at its declaration below.
+ * (spike_proj_verify); and for caches held in 4 bits the writing and reading of
+ * entries (spike_proj_cache4_write, spike_proj_cache4_read) and attention over
+ * them as they are (spike_proj_cache4_attend).  Each is documented at its
+ * declaration below.
  *
  * Conventions for every call
  *   - Pointers named d_* or documented as "device" are CUDA device pointers
@@ -77,6 +80,7 @@ typedef struct sp_plan_s *sp_plan_t;
 typedef struct sp_group_s *sp_group_t;
 typedef struct sp_head_s *sp_head_t;
 typedef struct sp_cache_s *sp_cache_t;
+typedef struct sp_cache4_s *sp_cache4_t;
 typedef void *sp_stream_t;             /* a cudaStream_t */
 
 typedef enum sp_status {
@@ -711,6 +715,156 @@ typedef struct sp_verify {
 } sp_verify;
 
 sp_status spike_proj_verify(const sp_verify *call, sp_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * A KV cache held in 4 bits (the paper does not describe one: the weight rule of
+ * Section 2.3, a scale from the largest magnitude, at 4 bits).  An entry is one key
+ * and one value per K/V head, and each of these a row of D codes of 4 bits and
+ * D / 16 scales of 8 bits, 4.5 bits an element.  For each 16 elements x of a row:
+ *
+ *   a     = max |x|
+ *   s     = a / 6 to the nearest number of 3 mantissa bits (ties to even), below
+ *           2^-14 to the nearest multiple of 2^-17; at most 10240.  The scale's
+ *           byte is that of s in half precision from its exponent down to the third
+ *           mantissa bit (half precision's bits >> 7).
+ *   code  = the nearest to |x| / s of 0 0.5 1 1.5 2 3 4 6 (codes 0 .. 7, ties to the
+ *           even one), + 8 where x has its sign set; 0 where s is 0
+ *   value = s * (that number), exact in bf16 and in half precision
+ *
+ * A NaN or an infinity among the 16 makes the scale's byte 255, which is a NaN, and
+ * the codes 0: all 16 values are NaN then.  Every rounding here is exact, so that
+ * codes and scales are the definition's bit for bit.
+ *
+ * sp_kv4 is a cache of keys or of values: entry j of K/V head h of sequence b has
+ * its codes at codes + b*batch + j*entry + h*head (bytes; element 2i in the lower
+ * half of byte i) and its scales at scales + b*scales_batch + j*scales_entry +
+ * h*scales_head.  The D / 2 and D / 16 bytes of a row are contiguous.  Pointers and
+ * strides (of dimensions longer than 1) are multiples of the largest power of two
+ * that divides D / 2, at most 16, for codes, and D / 16 for scales (SP_EALIGN):
+ * rows without gaps are.  Storing the heads before the entries (head strides above
+ * entry strides) keeps what one head reads together.
+ *
+ * spike_proj_cache4_create: the handle owns workspace (40 MB at most) and no entry of
+ *   any cache.  1 <= max_T <= SPIKE_PROJ_CACHE_MAX_T, 1 <= Hq <=
+ *   SPIKE_PROJ_CACHE_MAX_HEADS, 16 <= D <= SPIKE_PROJ_CACHE_MAX_D, 1 <= capacity <=
+ *   SPIKE_PROJ_CACHE_MAX_LEN (else SP_ERANGE); Hq % Hkv == 0 (SP_EINVAL); D % 16 == 0
+ *   (SP_EALIGN); dtype (sp_dtype) is the type of all 16-bit tensors.  A handle serves
+ *   one stream at a time, on the device that was current when it was made
+ *   (SP_EDEVICE on another).  Its calls take up to SPIKE_PROJ_CACHE_MAX_B sequences
+ *   (SP_ERANGE).
+ * ------------------------------------------------------------------------- */
+typedef struct sp_kv4 {
+    uint8_t *codes;                       /* [B][capacity][Hkv][D / 2] */
+    int64_t batch, entry, head;
+    uint8_t *scales;                      /* [B][capacity][Hkv][D / 16] */
+    int64_t scales_batch, scales_entry, scales_head;
+} sp_kv4;
+
+sp_status spike_proj_cache4_create(sp_cache4_t *cache, int32_t max_T, int32_t Hq,
+                                   int32_t Hkv, int32_t D, int32_t capacity,
+                                   int32_t dtype, sp_stream_t stream);
+sp_status spike_proj_cache4_destroy(sp_cache4_t cache);
+
+/* spike_proj_cache4_write: token t < n[b] of sequence b goes to slot at[b] + t of its
+ * cache, where that is in 0 .. capacity - 1 (what is not there is dropped; no other
+ * slot is written).
+ *
+ *   k, v          [B][T][Hkv][D], strides in elements
+ *   at            device int32 [B]; NULL: 0
+ *   n             device int32 [B], taken into 0 .. T; NULL: T
+ *   k_out, v_out  [B][T][Hkv][D], or both NULL: the values that the codes stand for,
+ *                 of the tokens t < n[b] (the others are left alone).  They may be k
+ *                 and v themselves, with the same strides.
+ * 16-bit tensors: 16-byte aligned, strides of dimensions longer than 1 multiples of 8
+ * (outputs: rows must not overlap), else SP_EALIGN.  Outputs (codes, scales, values)
+ * must not overlap the inputs, except as said, nor each other.  T * Hkv * D < 2^34
+ * (SP_ERANGE).
+ * Errors: SP_EINVAL, SP_EALIGN, SP_ERANGE, SP_EDEVICE, SP_ECUDA. */
+typedef struct sp_write4 {
+    const void *k, *v;                    /* [B][T][Hkv][D] */
+    int64_t k_batch, k_token, k_head, v_batch, v_token, v_head;
+    sp_kv4 k4, v4;
+    const int32_t *at, *n;
+    void *k_out, *v_out;                  /* [B][T][Hkv][D] */
+    int64_t k_out_batch, k_out_token, k_out_head;
+    int64_t v_out_batch, v_out_token, v_out_head;
+    int32_t B, T;
+} sp_write4;
+
+sp_status spike_proj_cache4_write(sp_cache4_t cache, const sp_write4 *call,
+                                  sp_stream_t stream);
+
+/* spike_proj_cache4_read: the values of slot at[b] + t go to token t < n[b] of k_out
+ * and v_out, where that is in 0 .. capacity - 1; all others are left alone.  Arguments
+ * and errors as for spike_proj_cache4_write. */
+typedef struct sp_read4 {
+    sp_kv4 k4, v4;
+    const int32_t *at, *n;
+    void *k_out, *v_out;                  /* [B][T][Hkv][D] */
+    int64_t k_out_batch, k_out_token, k_out_head;
+    int64_t v_out_batch, v_out_token, v_out_head;
+    int32_t B, T;
+} sp_read4;
+
+sp_status spike_proj_cache4_read(sp_cache4_t cache, const sp_read4 *call,
+                                 sp_stream_t stream);
+
+/* spike_proj_cache4_attend: T query tokens of each of B sequences over the first
+ * lens[b] entries of its cache.  Query t sees the entries j < lens[b] - (T - 1 - t)
+ * where `causal` is not 0 (the cache holds the T tokens as its last entries), else
+ * all of them:
+ *
+ *     s_j = scale * sum_d q_d k_jd             FP32
+ *     lse = ln sum_j exp(s_j)
+ *     out = sum_j exp(s_j - lse) v_j           rounded once to the type
+ *
+ * with the values k_jd, v_jd that the codes stand for.  With other_out and other_lse,
+ * the out and lse that attention of the same queries over other entries gave (a
+ * shared prefix, newer entries in 16 bits: spike_proj_cache_attend), the result is
+ * that over both:
+ *
+ *     lse' = ln(exp(lse) + exp(other_lse))
+ *     out' = exp(lse - lse') out + exp(other_lse - lse') other_out
+ *
+ * A row that sees no entry (or scores of minus infinity alone), and whose other_lse,
+ * if any, is minus infinity, gives out = 0 and lse = -infinity; other_out of such an
+ * other_lse is not used, whatever it holds.  Entries that no row sees are never used,
+ * whatever they hold, nor is what a row does not see by it; a NaN key that a row sees
+ * makes that row NaN, and NaN values the elements of it that they are of, however
+ * little weight the entry has.  Codes times scales are exact; each query row
+ * is brought to half precision by a power of two (what that loses is below 2^-38 of
+ * the row's largest element), probabilities are rounded to half precision before they
+ * meet V, and out is divided by the sum of the rounded ones; lse takes them unrounded.
+ * Scores, maxima and sums are FP32.  Results do not depend on the order in which
+ * blocks run.
+ *
+ *   lens       device int32 [B]; values outside 0 .. capacity are taken as
+ *              the nearest end.
+ *   lse        FP32 [B][T][Hq] contiguous, or NULL.
+ *   other_out  [B][T][Hq][D] of the type, other_lse FP32 [B][T][Hq] contiguous, or
+ *              both NULL (SP_EINVAL).  They may be out (with the same strides) and
+ *              lse; nothing else may overlap the outputs.
+ *   scale      finite and > 0 (SP_EINVAL).
+ * q, out and other_out: as 16-bit tensors of spike_proj_cache4_write.  A T above
+ * max_T: SP_ERANGE.
+ * Errors: SP_EINVAL, SP_EALIGN, SP_ERANGE, SP_EDEVICE, SP_ECUDA. */
+typedef struct sp_attend4 {
+    const void *q;                        /* [B][T][Hq][D] */
+    int64_t q_batch, q_token, q_head;
+    sp_kv4 k4, v4;
+    const int32_t *lens;
+    void *out;                            /* [B][T][Hq][D] */
+    int64_t out_batch, out_token, out_head;
+    float *lse;
+    const void *other_out;                /* [B][T][Hq][D] */
+    int64_t other_batch, other_token, other_head;
+    const float *other_lse;
+    int32_t B, T, causal;
+    float scale;
+} sp_attend4;
+
+sp_status spike_proj_cache4_attend(sp_cache4_t cache, const sp_attend4 *call,
+                                   sp_stream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Test faults -- FOR TESTS OF THE ERROR PATH ONLY (the paper has no

@@ -13,6 +13,7 @@
 #include <utility>
 
 #include "sp_cache.h"
+#include "sp_cache4.cuh"
 #include "sp_gemm.h"
 #include "sp_internal.h"
 
@@ -89,6 +90,12 @@ struct sp_cache_s {
   int32_t fault = SP_FAULT_NONE;  // armed for the next attend call
 };
 
+struct sp_cache4_s {
+  int device = 0;
+  Cache4Shape shape;
+  uint8_t* ws = nullptr;          // cache4_workspace(shape).bytes
+};
+
 struct sp_group_s {
   int32_t count = 0;
   int32_t maxN = 0, maxK = 0;
@@ -158,6 +165,29 @@ sp_status on_device(int device) {
   int dev = 0;
   SP_CUDA(cudaGetDevice(&dev));
   return dev == device ? SP_OK : SP_EDEVICE;
+}
+
+// A 4-bit cache of keys or values.
+bool kv4_aligned(const Cache4Shape& s, const sp_kv4& x, int B) {
+  const int codes = std::min(s.D / 2 & -(s.D / 2), 16), scales = s.D / 16 & -(s.D / 16);
+  const auto ok = [&](int64_t n, int64_t stride, int a) { return n == 1 || stride % a == 0; };
+  return aligned(x.codes, codes) && aligned(x.scales, scales) && ok(B, x.batch, codes) && ok(s.capacity, x.entry, codes) &&
+         ok(s.Hkv, x.head, codes) && ok(B, x.scales_batch, scales) && ok(s.capacity, x.scales_entry, scales) &&
+         ok(s.Hkv, x.scales_head, scales);
+}
+// Rows of it that a call writes lie apart.
+bool kv4_apart(const Cache4Shape& s, const sp_kv4& x, int B) {
+  const auto ok = [&](int64_t n, int64_t stride, int row) { return n == 1 || stride >= row || stride <= -row; };
+  const int c = s.D / 2, r = s.D / 16;
+  return ok(B, x.batch, c) && ok(s.capacity, x.entry, c) && ok(s.Hkv, x.head, c) && ok(B, x.scales_batch, r) &&
+         ok(s.capacity, x.scales_entry, r) && ok(s.Hkv, x.scales_head, r);
+}
+// A 16-bit tensor of rows of D elements over B, T and H; `row`: 0, or D where it is written.
+bool rows_aligned(const void* x, int B, int64_t batch, int T, int64_t token, int H, int64_t head, int row) {
+  const auto ok = [&](int64_t n, int64_t stride) {
+    return n == 1 || (stride % 8 == 0 && (row == 0 || stride >= row || stride <= -row));
+  };
+  return aligned(x, 16) && ok(B, batch) && ok(T, token) && ok(H, head);
 }
 
 template <typename T>
@@ -1287,6 +1317,114 @@ sp_status spike_proj_cache_evict(sp_cache_t cache, const sp_evict* c, sp_stream_
   const sp_status st = on_device(cache->device);
   if (st != SP_OK) return st;
   SP_CUDA(launch_evict(sh, *c, cache->ws, as_stream(stream)));
+  return SP_OK;
+}
+
+sp_status spike_proj_cache4_create(sp_cache4_t* cache, int32_t max_T, int32_t Hq, int32_t Hkv, int32_t D,
+                                   int32_t capacity, int32_t dtype, sp_stream_t stream) {
+  if (!cache || (dtype != SP_BF16 && dtype != SP_FP16)) return SP_EINVAL;
+  if (max_T < 1 || max_T > SPIKE_PROJ_CACHE_MAX_T || Hq < 1 || Hq > SPIKE_PROJ_CACHE_MAX_HEADS || D < 16 ||
+      D > SPIKE_PROJ_CACHE_MAX_D || capacity < 1 || capacity > SPIKE_PROJ_CACHE_MAX_LEN)
+    return SP_ERANGE;
+  if (Hkv < 1 || Hq % Hkv != 0) return SP_EINVAL;
+  if (D % 16 != 0) return SP_EALIGN;
+  int dev = 0, sms = 0;
+  sp_status st = check_device(&dev);
+  if (st != SP_OK) return st;
+  SP_CUDA(current_device(&dev, &sms));
+  sp_cache4_s* ca = new (std::nothrow) sp_cache4_s();
+  if (!ca) return SP_ENOMEM;
+  ca->device = dev;
+  ca->shape = Cache4Shape{max_T, Hq, Hkv, D, capacity, dtype};
+  cudaStream_t s = as_stream(stream);
+  st = dev_alloc_zero(&ca->ws, cache4_workspace(ca->shape, sms).bytes, s);
+  cudaError_t e;
+  if (st == SP_OK && (e = cudaStreamSynchronize(s)) != cudaSuccess) st = cuda_fail(e);
+  if (st != SP_OK) {
+    cudaFree(ca->ws);
+    delete ca;
+    return st;
+  }
+  *cache = ca;
+  return SP_OK;
+}
+
+sp_status spike_proj_cache4_destroy(sp_cache4_t cache) {
+  if (!cache) return SP_OK;
+  cudaError_t e = cudaDeviceSynchronize();
+  cudaFree(cache->ws);
+  delete cache;
+  return e == cudaSuccess ? SP_OK : cuda_fail(e);
+}
+
+sp_status spike_proj_cache4_write(sp_cache4_t cache, const sp_write4* c, sp_stream_t stream) {
+  if (!cache || !c || !c->k || !c->v || !c->k4.codes || !c->k4.scales || !c->v4.codes || !c->v4.scales) return SP_EINVAL;
+  if (c->B < 1 || c->T < 1 || !c->k_out != !c->v_out) return SP_EINVAL;
+  if (c->k4.codes == c->v4.codes || c->k4.scales == c->v4.scales) return SP_EINVAL;
+  if (c->k_out) {
+    const auto same = [](int64_t a, int64_t b, int64_t n) { return n == 1 || a == b; };
+    const int64_t B = c->B, T = c->T, H = cache->shape.Hkv;
+    if (c->k_out == c->v_out || c->k_out == c->v || c->v_out == c->k) return SP_EINVAL;
+    if (c->k_out == c->k && !(same(c->k_batch, c->k_out_batch, B) && same(c->k_token, c->k_out_token, T) &&
+                              same(c->k_head, c->k_out_head, H)))
+      return SP_EINVAL;
+    if (c->v_out == c->v && !(same(c->v_batch, c->v_out_batch, B) && same(c->v_token, c->v_out_token, T) &&
+                              same(c->v_head, c->v_out_head, H)))
+      return SP_EINVAL;
+  }
+  const Cache4Shape& sh = cache->shape;
+  if (c->B > SPIKE_PROJ_CACHE_MAX_B || (int64_t)c->T * sh.Hkv * sh.D >= (int64_t)1 << 34) return SP_ERANGE;
+  if (!rows_aligned(c->k, c->B, c->k_batch, c->T, c->k_token, sh.Hkv, c->k_head, 0) ||
+      !rows_aligned(c->v, c->B, c->v_batch, c->T, c->v_token, sh.Hkv, c->v_head, 0) || !kv4_aligned(sh, c->k4, c->B) ||
+      !kv4_aligned(sh, c->v4, c->B) || !kv4_apart(sh, c->k4, c->B) || !kv4_apart(sh, c->v4, c->B) || !aligned(c->at, 4) ||
+      !aligned(c->n, 4))
+    return SP_EALIGN;
+  if (c->k_out && (!rows_aligned(c->k_out, c->B, c->k_out_batch, c->T, c->k_out_token, sh.Hkv, c->k_out_head, sh.D) ||
+                   !rows_aligned(c->v_out, c->B, c->v_out_batch, c->T, c->v_out_token, sh.Hkv, c->v_out_head, sh.D)))
+    return SP_EALIGN;
+  const sp_status st = on_device(cache->device);
+  if (st != SP_OK) return st;
+  SP_CUDA(launch_write4(sh, *c, as_stream(stream)));
+  return SP_OK;
+}
+
+sp_status spike_proj_cache4_read(sp_cache4_t cache, const sp_read4* c, sp_stream_t stream) {
+  if (!cache || !c || !c->k_out || !c->v_out || !c->k4.codes || !c->k4.scales || !c->v4.codes || !c->v4.scales)
+    return SP_EINVAL;
+  if (c->B < 1 || c->T < 1 || c->k_out == c->v_out) return SP_EINVAL;
+  const Cache4Shape& sh = cache->shape;
+  if (c->B > SPIKE_PROJ_CACHE_MAX_B || (int64_t)c->T * sh.Hkv * sh.D >= (int64_t)1 << 34) return SP_ERANGE;
+  if (!rows_aligned(c->k_out, c->B, c->k_out_batch, c->T, c->k_out_token, sh.Hkv, c->k_out_head, sh.D) ||
+      !rows_aligned(c->v_out, c->B, c->v_out_batch, c->T, c->v_out_token, sh.Hkv, c->v_out_head, sh.D) ||
+      !kv4_aligned(sh, c->k4, c->B) || !kv4_aligned(sh, c->v4, c->B) || !aligned(c->at, 4) || !aligned(c->n, 4))
+    return SP_EALIGN;
+  const sp_status st = on_device(cache->device);
+  if (st != SP_OK) return st;
+  SP_CUDA(launch_read4(sh, *c, as_stream(stream)));
+  return SP_OK;
+}
+
+sp_status spike_proj_cache4_attend(sp_cache4_t cache, const sp_attend4* c, sp_stream_t stream) {
+  if (!cache || !c || !c->q || !c->k4.codes || !c->k4.scales || !c->v4.codes || !c->v4.scales || !c->lens || !c->out)
+    return SP_EINVAL;
+  if (c->B < 1 || c->T < 1 || !c->other_out != !c->other_lse || !(c->scale > 0.f) || !std::isfinite(c->scale))
+    return SP_EINVAL;
+  const Cache4Shape& sh = cache->shape;
+  if (c->out == c->q) return SP_EINVAL;
+  if (c->other_out == c->out && !((c->B == 1 || c->other_batch == c->out_batch) && (c->T == 1 || c->other_token == c->out_token) &&
+                                  (sh.Hq == 1 || c->other_head == c->out_head)))
+    return SP_EINVAL;
+  if (c->B > SPIKE_PROJ_CACHE_MAX_B || c->T > sh.max_T) return SP_ERANGE;
+  if (!rows_aligned(c->q, c->B, c->q_batch, c->T, c->q_token, sh.Hq, c->q_head, 0) ||
+      !rows_aligned(c->out, c->B, c->out_batch, c->T, c->out_token, sh.Hq, c->out_head, sh.D) ||
+      !kv4_aligned(sh, c->k4, c->B) || !kv4_aligned(sh, c->v4, c->B) || !aligned(c->lens, 4) || !aligned(c->lse, 4) ||
+      !aligned(c->other_lse, 4))
+    return SP_EALIGN;
+  if (c->other_out && !rows_aligned(c->other_out, c->B, c->other_batch, c->T, c->other_token, sh.Hq, c->other_head, 0))
+    return SP_EALIGN;
+  const sp_status st = on_device(cache->device);
+  if (st != SP_OK) return st;
+  SP_CUDA(launch_attend4(sh, *c, cache->ws, as_stream(stream)));
   return SP_OK;
 }
 

@@ -1,0 +1,53 @@
+// sp_cache4.cuh -- the form of a KV cache held in 4 bits: codes e2m1 (sign, 2
+// exponent and 1 mantissa bits: 0 0.5 1 1.5 2 3 4 6), and per 16 elements a scale of
+// 8 bits, which are those of a half-precision number from its exponent down to
+// three mantissa bits.  A value, code times scale, has at most six significant bits
+// and lies within half precision (the largest scale is 10240), so that products of
+// the two in half precision are exact.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "sp_cache.h"
+
+namespace sp {
+
+struct Cache4Shape {
+  int32_t max_T, Hq, Hkv, D, capacity, dtype;
+};
+
+constexpr int kGroup4 = 16;                // elements of a scale
+constexpr uint32_t kNaNScale4 = 0xff;      // scale of a group with a NaN or an infinity
+constexpr float kMaxScale4 = 10240.f;
+
+struct Cache4Workspace {
+  size_t tickets, slots, bytes;            // the tickets are zero between calls
+};
+Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms);
+// Query rows of a K/V head: as many units as it takes for 32 rows each at most.
+inline __host__ __device__ int row_blocks4(int R) { return (R + 31) / 32; }
+
+cudaError_t launch_write4(const Cache4Shape& s, const sp_write4& c, cudaStream_t stream);
+cudaError_t launch_read4(const Cache4Shape& s, const sp_read4& c, cudaStream_t stream);
+cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// Four code pairs of a word, in half precision (without their scale).
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// A scale byte as two equal half-precision numbers.
+__device__ __forceinline__ uint32_t scale_half2(uint32_t byte) { return byte * 0x00800080u; }
+#endif
+
+}  // namespace sp

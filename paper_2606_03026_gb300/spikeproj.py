@@ -79,6 +79,11 @@ _SIGNATURES = {
     "spike_proj_cache_status": ([_P, _P], ctypes.c_int),
     "spike_proj_cache_attend": ([_P, _P, _P], ctypes.c_int),
     "spike_proj_cache_evict": ([_P, _P, _P], ctypes.c_int),
+    "spike_proj_cache4_create": ([_P, _I32, _I32, _I32, _I32, _I32, _I32, _P], ctypes.c_int),
+    "spike_proj_cache4_destroy": ([_P], ctypes.c_int),
+    "spike_proj_cache4_write": ([_P, _P, _P], ctypes.c_int),
+    "spike_proj_cache4_read": ([_P, _P, _P], ctypes.c_int),
+    "spike_proj_cache4_attend": ([_P, _P, _P], ctypes.c_int),
     "spike_proj_verify": ([_P, _P], ctypes.c_int),
     "spike_proj_probe_gather": ([_P, _P, _I32, _I32, _P, _P], ctypes.c_int),
     "spike_proj_plan_inject_fault": ([_P, _I32], ctypes.c_int),
@@ -519,6 +524,37 @@ class SpEvict(ctypes.Structure):
                 ("B", _I32), ("budget", _I32), ("recent", _I32)]
 
 
+def _kv4_fields(name):
+    """The fields of a struct sp_kv4 within another."""
+    return [(name + "_codes", _P), (name + "_batch", _I64), (name + "_entry", _I64), (name + "_head", _I64),
+            (name + "_scales", _P), (name + "_scales_batch", _I64), (name + "_scales_entry", _I64),
+            (name + "_scales_head", _I64)]
+
+
+def _row_fields(name):
+    return [(name + "_batch", _I64), (name + "_token", _I64), (name + "_head", _I64)]
+
+
+class SpWrite4(ctypes.Structure):
+    """struct sp_write4 of spike_proj.h."""
+    _fields_ = [("k", _P), ("v", _P), *_row_fields("k"), *_row_fields("v"), *_kv4_fields("k4"), *_kv4_fields("v4"),
+                ("at", _P), ("n", _P), ("k_out", _P), ("v_out", _P), *_row_fields("k_out"), *_row_fields("v_out"),
+                ("B", _I32), ("T", _I32)]
+
+
+class SpRead4(ctypes.Structure):
+    """struct sp_read4 of spike_proj.h."""
+    _fields_ = [*_kv4_fields("k4"), *_kv4_fields("v4"), ("at", _P), ("n", _P), ("k_out", _P), ("v_out", _P),
+                *_row_fields("k_out"), *_row_fields("v_out"), ("B", _I32), ("T", _I32)]
+
+
+class SpAttend4(ctypes.Structure):
+    """struct sp_attend4 of spike_proj.h."""
+    _fields_ = [("q", _P), *_row_fields("q"), *_kv4_fields("k4"), *_kv4_fields("v4"), ("lens", _P), ("out", _P),
+                *_row_fields("out"), ("lse", _P), ("other_out", _P), *_row_fields("other"), ("other_lse", _P),
+                ("B", _I32), ("T", _I32), ("causal", _I32), ("scale", ctypes.c_float)]
+
+
 class SpVerify(ctypes.Structure):
     """struct sp_verify of spike_proj.h."""
     _fields_ = [("p", _P), ("p_batch", _I64), ("p_row", _I64),
@@ -557,6 +593,33 @@ def spike_proj_cache_evict(cache, call, stream=None):
            "spike_proj_cache_evict")
 
 
+def spike_proj_cache4_create(max_T, Hq, Hkv, D, capacity, dtype, stream=None) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().spike_proj_cache4_create(ctypes.byref(h), max_T, Hq, Hkv, D, capacity,
+                                          DTYPES[dtype] if isinstance(dtype, str) else int(dtype),
+                                          _stream(stream)), "spike_proj_cache4_create")
+    return h.value
+
+
+def spike_proj_cache4_destroy(cache):
+    _check(lib().spike_proj_cache4_destroy(cache), "spike_proj_cache4_destroy")
+
+
+def spike_proj_cache4_write(cache, call, stream=None):
+    """call: an SpWrite4."""
+    _check(lib().spike_proj_cache4_write(cache, ctypes.addressof(call), _stream(stream)), "spike_proj_cache4_write")
+
+
+def spike_proj_cache4_read(cache, call, stream=None):
+    """call: an SpRead4."""
+    _check(lib().spike_proj_cache4_read(cache, ctypes.addressof(call), _stream(stream)), "spike_proj_cache4_read")
+
+
+def spike_proj_cache4_attend(cache, call, stream=None):
+    """call: an SpAttend4."""
+    _check(lib().spike_proj_cache4_attend(cache, ctypes.addressof(call), _stream(stream)), "spike_proj_cache4_attend")
+
+
 def spike_proj_verify(call, stream=None):
     """call: an SpVerify."""
     _check(lib().spike_proj_verify(ctypes.addressof(call), _stream(stream)), "spike_proj_verify")
@@ -573,6 +636,7 @@ def _packer(struct_type):
 
 
 _pack_attend, _pack_evict, _pack_verify = map(_packer, (SpAttend, SpEvict, SpVerify))
+_pack_write4, _pack_read4, _pack_attend4 = map(_packer, (SpWrite4, SpRead4, SpAttend4))
 
 
 def _reject(x, name, shape, dtype, device):
@@ -695,6 +759,123 @@ class Cache:
     def close(self):
         if self.handle:
             spike_proj_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Cache4:
+    """Own caches held in 4 bits: writing and reading of entries, and attention
+    over them.  The keys and the values of a batch are a pair of uint8 tensors
+    each, codes [B, capacity, Hkv, D / 2] and scales [B, capacity, Hkv, D / 16];
+    they are the caller's (new() makes a pair of pairs)."""
+
+    def __init__(self, Hq, Hkv, D, capacity, max_T=1, dtype="bf16", stream=None):
+        import torch
+        self.Hq, self.Hkv, self.D, self.capacity, self.max_T = Hq, Hkv, D, capacity, max_T
+        self.dtype = {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
+        self._f32, self._i32, self._u8 = torch.float32, torch.int32, torch.uint8
+        self._scale = D ** -0.5
+        self.handle = spike_proj_cache4_create(max_T, Hq, Hkv, D, capacity, dtype, stream)
+        self._device = torch.cuda.current_device()             # the handle's
+
+    def new(self, batch):
+        """Empty caches k4, v4 of a batch, stored with the heads before the entries."""
+        import torch
+        return tuple(tuple(torch.zeros(batch, self.Hkv, self.capacity, self.D // x, dtype=torch.uint8,
+                                       device=f"cuda:{self._device}").transpose(1, 2) for x in (2, 16)) for _ in range(2))
+
+    def _held(self, x, name, B):
+        """One of k4 and v4 as the fields of a struct sp_kv4."""
+        if x is None:
+            raise ValueError(f"{name}: missing")
+        codes, scales = x
+        own, u8, dev = (B, self.capacity, self.Hkv), self._u8, self._device
+        cs = _want(codes, name + "[0]", own + (self.D // 2,), u8, dev)
+        ss = _want(scales, name + "[1]", own + (self.D // 16,), u8, dev)
+        return codes.data_ptr(), cs[0], cs[1], cs[2], scales.data_ptr(), ss[0], ss[1], ss[2]
+
+    def _each(self, x, name, B):
+        if x is None:
+            return 0
+        _want(x, name, (B,), self._i32, self._device)
+        return x.data_ptr()
+
+    def write(self, k, v, k4, v4, at=None, n=None, k_out=None, v_out=None, stream=None):
+        """Tokens t < n[b] of k and v [B, T, Hkv, D] into the slots at[b] + t of the
+        caches (at, n: int32 [B]; 0 and T where they are None); k_out and v_out, of
+        k's shape, take the values that the codes stand for, and may be k and v."""
+        if k is None:
+            raise ValueError("k: missing")
+        t, dev = self.dtype, self._device
+        B, T = k.shape[0], k.shape[1]
+        rows = (B, T, self.Hkv, self.D)
+        ks, vs = _want(k, "k", rows, t, dev), _want(v, "v", rows, t, dev)
+        ka, va, kos, vos = 0, 0, (0, 0, 0), (0, 0, 0)
+        if (k_out is None) != (v_out is None):
+            raise ValueError("k_out, v_out: one without the other")
+        if k_out is not None:
+            kos, vos = _want(k_out, "k_out", rows, t, dev), _want(v_out, "v_out", rows, t, dev)
+            ka, va = k_out.data_ptr(), v_out.data_ptr()
+        call = _pack_write4(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                            *self._held(k4, "k4", B), *self._held(v4, "v4", B), self._each(at, "at", B),
+                            self._each(n, "n", B), ka, va, kos[0], kos[1], kos[2], vos[0], vos[1], vos[2], B, T)
+        _check(lib().spike_proj_cache4_write(self.handle, call, _stream(stream)), "spike_proj_cache4_write")
+
+    def read(self, k4, v4, k_out, v_out, at=None, n=None, stream=None):
+        """The values of the slots at[b] + t into the tokens t < n[b] of k_out and
+        v_out [B, T, Hkv, D] (at, n: int32 [B]; 0 and T where they are None)."""
+        if k_out is None:
+            raise ValueError("k_out: missing")
+        t, dev = self.dtype, self._device
+        B, T = k_out.shape[0], k_out.shape[1]
+        rows = (B, T, self.Hkv, self.D)
+        kos, vos = _want(k_out, "k_out", rows, t, dev), _want(v_out, "v_out", rows, t, dev)
+        call = _pack_read4(*self._held(k4, "k4", B), *self._held(v4, "v4", B), self._each(at, "at", B),
+                           self._each(n, "n", B), k_out.data_ptr(), v_out.data_ptr(), kos[0], kos[1], kos[2],
+                           vos[0], vos[1], vos[2], B, T)
+        _check(lib().spike_proj_cache4_read(self.handle, call, _stream(stream)), "spike_proj_cache4_read")
+
+    def attend(self, q, k4, v4, lens, out, lse=None, other_out=None, other_lse=None, causal=True, scale=None,
+               stream=None):
+        """T query tokens per sequence, q [B, T, Hq, D] -> out [B, T, Hq, D], over the
+        first lens[b] (int32 [B]) entries; causal: the T tokens are the last of
+        these, and none sees a later one.  other_out and other_lse (float32
+        [B, T, Hq]), what attention of the same queries over other entries gave
+        (Cache.attend), are joined in; lse (float32 [B, T, Hq]) is optional."""
+        if q is None:
+            raise ValueError("q: missing")
+        t, dev = self.dtype, self._device
+        B, T = q.shape[0], q.shape[1]
+        rows = (B, T, self.Hq, self.D)
+        qs, os = _want(q, "q", rows, t, dev), _want(out, "out", rows, t, dev)
+        _want(lens, "lens", (B,), self._i32, dev)
+        la, oa, ola, oos = 0, 0, 0, (0, 0, 0)
+        if lse is not None:
+            la = self._sums(lse, "lse", rows)
+        if (other_out is None) != (other_lse is None):
+            raise ValueError("other_out, other_lse: one without the other")
+        if other_out is not None:
+            oos, oa = _want(other_out, "other_out", rows, t, dev), other_out.data_ptr()
+            ola = self._sums(other_lse, "other_lse", rows)
+        call = _pack_attend4(q.data_ptr(), qs[0], qs[1], qs[2], *self._held(k4, "k4", B), *self._held(v4, "v4", B),
+                             lens.data_ptr(), out.data_ptr(), os[0], os[1], os[2], la, oa, oos[0], oos[1], oos[2], ola,
+                             B, T, 1 if causal else 0, self._scale if scale is None else scale)
+        _check(lib().spike_proj_cache4_attend(self.handle, call, _stream(stream)), "spike_proj_cache4_attend")
+
+    def _sums(self, x, name, rows):
+        _want(x, name, rows[:3], self._f32, self._device)
+        if not x.is_contiguous():
+            raise ValueError(f"{name}: not contiguous")
+        return x.data_ptr()
+
+    def close(self):
+        if self.handle:
+            spike_proj_cache4_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

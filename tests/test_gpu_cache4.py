@@ -1,0 +1,472 @@
+"""A KV cache held in 4 bits: writing, reading and attention against plain 64-bit
+implementations."""
+import math
+
+import pytest
+import torch
+
+import cache4_ref as ref
+import serving_ref
+from paper_2606_03026_gb300 import spikeproj as sp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def place(x, layout):
+    """The values of [B, C or T, H, W] on the GPU: as they are, heads before entries, or in a wider buffer."""
+    if layout == "heads":
+        return x.to(DEV).transpose(1, 2).contiguous().transpose(1, 2)
+    if layout == "padded":
+        room = 32 if x.dtype == torch.uint8 else 16
+        wide = torch.full((*x.shape[:-1], x.shape[-1] + 2 * room), 77, dtype=x.dtype, device=DEV)
+        wide[..., room:room + x.shape[-1]] = x.to(DEV)
+        return wide[..., room:room + x.shape[-1]]
+    return x.to(DEV)
+
+
+def activations(g, *shape, dtype):
+    x = torch.randn(*shape, generator=g) * torch.exp2(torch.randint(-6, 7, (*shape[:-1], 1), generator=g).float())
+    return x.to(TYPES[dtype])
+
+
+# ---------------------------------------------------------------------------
+def check_codes(x, layout="entries"):
+    """x [rows, D]: one token each of a batch of one sequence with one head."""
+    D = x.shape[1]
+    rows = x.view(1, -1, 1, D)
+    name = "bf16" if x.dtype == torch.bfloat16 else "fp16"
+    cache = sp.Cache4(1, 1, D, rows.shape[1], dtype=name)
+    k4, v4 = cache.new(1)
+    k_out, v_out = (torch.zeros_like(rows, device=DEV) for _ in range(2))
+    cache.write(rows.to(DEV), rows.flip(1).to(DEV), k4, v4, k_out=k_out, v_out=v_out)
+    codes, scales, values = ref.quantise(x)
+    for held, out, order in ((k4, k_out, 1), (v4, v_out, -1)):
+        assert torch.equal(held[0].cpu()[0, ::1, 0], codes if order > 0 else codes.flip(0))
+        assert torch.equal(held[1].cpu()[0, :, 0], scales if order > 0 else scales.flip(0))
+        want = (values if order > 0 else values.flip(0)).to(x.dtype)
+        assert torch.equal(want.double().nan_to_num(9e9), (values if order > 0 else values.flip(0)).nan_to_num(9e9)), "not exact in the type"
+        got = out.cpu()[0, :, 0]
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(0), want.nan_to_num(0))
+    back_k, back_v = (torch.zeros_like(rows, device=DEV) for _ in range(2))
+    cache.read(k4, v4, back_k, back_v)
+    assert torch.equal(back_k.view(torch.int16), k_out.view(torch.int16))
+    assert torch.equal(back_v.view(torch.int16), v_out.view(torch.int16))
+    cache.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_every_largest_element(dtype):
+    """All 2^16 bit patterns as a group's largest element (NaN and infinities too)."""
+    top = torch.arange(-2 ** 15, 2 ** 15).to(torch.int16).view(TYPES[dtype])
+    g = torch.Generator().manual_seed(1)
+    x = (top.double().unsqueeze(1) * (2 * torch.rand(2 ** 16, 16, generator=g) - 1)).to(TYPES[dtype])
+    x[torch.arange(2 ** 16), torch.randint(0, 16, (2 ** 16,), generator=g)] = top
+    check_codes(x)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_elements_on_and_beside_the_borders(dtype):
+    """Every scale times every border between two codes, and the numbers of the type beside it."""
+    borders = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], dtype=torch.float64)
+    scales = ref.SCALES[1:]
+    x = (scales.unsqueeze(1) * borders).to(TYPES[dtype])
+    rows = []
+    for step in (-1, 0, 1):
+        y = (x.view(torch.int16) + step).view(TYPES[dtype])
+        rows.append(torch.cat([y, -y, torch.zeros_like(y[:, :1]), (6 * scales).unsqueeze(1).to(TYPES[dtype])], 1))
+    check_codes(torch.cat(rows))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_scales_on_and_beside_their_borders(dtype):
+    """Largest elements six times what lies halfway between two scales, and the numbers beside them."""
+    half = 6 * (ref.SCALES[1:] + ref.SCALES[:-1]) / 2
+    x = half.to(TYPES[dtype]).view(torch.int16)
+    x = torch.cat([(x + i).view(TYPES[dtype]) for i in range(-3, 4)])
+    check_codes(x.unsqueeze(1) * torch.linspace(-1, 1, 16).to(TYPES[dtype]))
+
+
+def test_special_groups():
+    x = torch.randn(9, 128, generator=torch.Generator().manual_seed(2)).bfloat16()
+    x[0], x[1], x[2] = 0.0, -0.0, 1e-30
+    x[3, 17], x[4, 127], x[5, 0] = math.nan, math.inf, -math.inf
+    x[6], x[7, 5] = 3e38, 3e38
+    x[8] = torch.where(torch.arange(128) % 2 == 0, -1e-6, 2e-5).bfloat16()
+    check_codes(x)
+    check_codes(x.half())
+
+
+# ---------------------------------------------------------------------------
+def written(B, T, Hkv, D, C, at, n, dtype, layout, out, seed=3):
+    g = torch.Generator().manual_seed(seed)
+    k, v = (activations(g, B, T, Hkv, D, dtype=dtype) for _ in range(2))
+    held = [torch.randint(0, top, (B, C, Hkv, w), generator=g).to(torch.uint8) for w, top in ((D // 2, 256), (D // 16, 227)) * 2]
+    outs = [torch.full_like(k, 5.0) for _ in range(2)]
+    cache = sp.Cache4(Hkv, Hkv, D, C, dtype=dtype)
+    gk4 = tuple(place(x, layout) for x in held[:2])
+    gv4 = tuple(place(x, layout) for x in held[2:])
+    gouts = [place(x, layout) for x in outs] if out else [None, None]
+    ints = [None if x is None else torch.tensor(x, dtype=torch.int32) for x in (at, n)]
+    cache.write(place(k, layout), place(v, layout), gk4, gv4, *(None if x is None else x.to(DEV) for x in ints),
+                *gouts)
+    for b in range(B):
+        a = 0 if at is None else at[b]
+        for t in range(T if n is None else min(max(n[b], 0), T)):
+            for i, x in enumerate((k, v)):
+                codes, scales, values = ref.quantise(x[b, t])
+                if 0 <= a + t < C:
+                    held[2 * i][b, a + t], held[2 * i + 1][b, a + t] = codes, scales
+                outs[i][b, t] = values.to(x.dtype)
+    for got, want in zip(gk4 + gv4, held):
+        assert torch.equal(got.cpu(), want)
+    if out:
+        for got, want in zip(gouts, outs):
+            assert torch.equal(got.cpu(), want)
+    # and back: slots from one before the first on, one token more
+    reads = [torch.full((B, T + 1, Hkv, D), 3.0, dtype=TYPES[dtype]) for _ in range(2)]
+    greads = [place(x, layout) for x in reads]
+    before = None if at is None else torch.tensor([x - 1 for x in at], dtype=torch.int32, device=DEV)
+    cache.read(gk4, gv4, *greads, before, None if n is None else ints[1].to(DEV))
+    for b in range(B):
+        a = 0 if at is None else at[b] - 1
+        for t in range(T + 1 if n is None else min(max(n[b], 0), T + 1)):
+            if 0 <= a + t < C:
+                for i in range(2):
+                    reads[i][b, t] = ref.values(held[2 * i][b, a + t], held[2 * i + 1][b, a + t]).to(TYPES[dtype])
+    for got, want in zip(greads, reads):
+        got = got.cpu()
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(0, 1e4, -1e4), want.nan_to_num(0, 1e4, -1e4))
+    # a padded buffer's bytes beside the rows are as they were
+    if layout == "padded":
+        for x in gk4 + gv4 + tuple(gouts if out else ()) + tuple(greads):
+            room = 32 if x.dtype == torch.uint8 else 16
+            wide = x.as_strided((*x.shape[:-1], x.shape[-1] + 2 * room), x.stride(), x.storage_offset() - room)
+            assert (wide[..., :room] == 77).all() and (wide[..., -room:] == 77).all()
+    cache.close()
+
+
+@pytest.mark.parametrize("layout", ["entries", "heads", "padded"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", [
+    # B, T, Hkv, D, C, at, n
+    (1, 1, 1, 16, 1, [0], None),
+    (1, 1, 4, 128, 5, [4], [1]),
+    (3, 5, 2, 64, 9, [0, 4, 7], [5, 0, 3]),                    # the last runs past the end
+    (3, 5, 2, 80, 9, [-2, 9, 2 ** 31 - 1], [5, 5, 5]),         # slots before the first, past the last
+    (2, 7, 3, 96, 30, [3, 11], [-5, 900]),                     # counts outside 0 .. T
+    (2, 65, 8, 112, 70, [2, 5], None),
+    (2, 130, 5, 32, 131, None, None),
+    (33, 2, 7, 48, 4, [i % 4 for i in range(33)], [i % 3 for i in range(33)]),
+], ids=lambda c: "-".join(map(str, c[:5])))
+def test_write_and_read(case, dtype, layout):
+    written(*case, dtype, layout, True)
+
+
+def test_write_without_values():
+    written(2, 3, 2, 128, 8, [1, 5], [3, 2], "bf16", "heads", False)
+
+
+def test_values_in_the_place_of_the_tokens():
+    g = torch.Generator().manual_seed(4)
+    k, v = (activations(g, 2, 40, 3, 64, dtype="fp16").to(DEV) for _ in range(2))
+    want = [ref.quantise(x.cpu())[2].half() for x in (k, v)]
+    cache = sp.Cache4(3, 3, 64, 40, dtype="fp16")
+    k4, v4 = cache.new(2)
+    cache.write(k, v, k4, v4, k_out=k, v_out=v)
+    assert torch.equal(k.cpu(), want[0]) and torch.equal(v.cpu(), want[1])
+    assert torch.equal(ref.values(*(x.cpu() for x in k4)).half(), want[0])
+    # written once more they are the same
+    codes = k4[0].clone()
+    cache.write(k, v, k4, v4, k_out=k, v_out=v)
+    assert torch.equal(k.cpu(), want[0]) and torch.equal(ref.values(*(x.cpu() for x in k4)).half(), want[0]) and codes.shape
+    cache.close()
+
+
+# ---------------------------------------------------------------------------
+def held_entries(g, B, C, Hkv, D):
+    """Codes and scales of what normal numbers of different size give."""
+    x = torch.randn(B, C, Hkv, D, generator=g) * (0.5 + 2 * torch.rand(1, 1, Hkv, 1, generator=g))
+    codes, scales, _ = ref.quantise(x.bfloat16())
+    return codes, scales
+
+
+def make(seed, B, T, Hq, Hkv, D, C, lens, dtype, garbage=True):
+    """CPU tensors; slots that are not in use hold NaN scales."""
+    g = torch.Generator().manual_seed(seed)
+    q = (1.5 * torch.randn(B, T, Hq, D, generator=g)).to(TYPES[dtype])
+    k4, v4 = held_entries(g, B, C, Hkv, D), held_entries(g, B, C, Hkv, D)
+    if garbage:
+        for b in range(B):
+            for x in (k4, v4):
+                x[1][b, max(0, lens[b]):] = 255
+    return q, k4, v4, torch.tensor(lens, dtype=torch.int32)
+
+
+def run(q, k4, v4, lens, layout="entries", causal=True, scale=None, other=None, stream=None, cache=None):
+    B, T, Hq, D = q.shape
+    C, Hkv = k4[0].shape[1:3]
+    name = "bf16" if q.dtype == torch.bfloat16 else "fp16"
+    own = cache or sp.Cache4(Hq, Hkv, D, C, max_T=T, dtype=name)
+    out, lse = place(torch.full_like(q, 7.0), layout), torch.full((B, T, Hq), 7.0, device=DEV)
+    more = {} if other is None else dict(other_out=place(other[0], layout), other_lse=other[1].to(DEV))
+    own.attend(place(q, layout), tuple(place(x, layout) for x in k4), tuple(place(x, layout) for x in v4), lens.to(DEV), out,
+               lse=lse, causal=causal, scale=scale, **more)
+    torch.cuda.synchronize()
+    if cache is None:
+        own.close()
+    return out.cpu(), lse.cpu()
+
+
+def check(q, k4, v4, lens, got, causal=True, scale=None, other=None):
+    want, wlse, tol, lse_tol = ref.attend(q, ref.values(*k4), ref.values(*v4), lens, causal, scale, other)
+    out, lse = got[0].double(), got[1].double()
+    empty = wlse == -math.inf
+    assert torch.equal(lse.isneginf(), empty) and (out[empty] == 0).all()
+    err = (out - want).abs()
+    assert (err <= tol).all(), f"out: {(err / tol).max()} of its bound"
+    err = (lse - wlse).abs()[~empty]
+    assert (err <= lse_tol[~empty]).all(), f"lse: {(err / lse_tol[~empty]).max()} of its bound"
+
+
+CASES = [
+    # B, T, Hq, Hkv, D, C, lens
+    (1, 1, 1, 1, 16, 1, [1]),
+    (1, 1, 4, 2, 128, 5, [3]),
+    (2, 1, 12, 4, 128, 300, [300, 1]),
+    (4, 1, 3, 1, 64, 128, [128, 127, 0, 17]),
+    (3, 1, 8, 1, 128, 700, [700, 16, 15]),
+    (5, 2, 8, 2, 128, 257, [257, 256, 130, 2, 1]),
+    (4, 5, 6, 2, 64, 140, [140, 133, 3, 0]),                      # fewer entries than tokens
+    (2, 8, 16, 2, 128, 200, [200, 131]),                          # 64 rows of a head
+    (3, 3, 4, 4, 80, 90, [90, 41, 3]),
+    (2, 4, 8, 8, 96, 64, [64, 7]),
+    (2, 2, 5, 5, 32, 20, [20, 19]),
+    (2, 3, 12, 3, 112, 150, [129, 150]),
+    (2, 3, 15, 3, 48, 150, [-3, 1000]),                           # lengths outside the cache
+    (40, 1, 6, 2, 128, 33, [i % 34 for i in range(40)]),
+    (16, 6, 24, 3, 64, 150, [9 * i + 6 for i in range(16)]),      # 48 rows
+    (3, 7, 9, 3, 128, 99, [99, 98, 6]),                           # 21 rows
+    (2, 3, 9, 1, 64, 400, [400, 33]),                             # 27 rows
+    (1, 32, 16, 2, 128, 64, [40]),                                # 256 rows of one head
+    (2, 1, 200, 1, 64, 140, [140, 3]),                            # 200 query heads on one
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c[:6])))
+def test_attend_matches_the_definition(case, dtype):
+    x = make(11, *case, dtype)
+    check(*x, run(*x))
+
+
+@pytest.mark.parametrize("layout", ["heads", "padded"])
+@pytest.mark.parametrize("D", [64, 80, 112, 128])
+def test_attend_on_other_layouts(layout, D):
+    x = make(12, 3, 2, 6, 3, D, 70, [70, 33, 2], "bf16")
+    check(*x, run(*x, layout=layout))
+
+
+@pytest.mark.parametrize("G", [1, 5, 8, 9, 16, 17, 24, 25, 32, 33])
+def test_every_number_of_query_heads(G):
+    x = make(13, 2, 1, 2 * G, 2, 128, 260, [260, 31], "bf16")
+    check(*x, run(*x))
+
+
+def test_all_entries_seen():
+    x = make(14, 3, 4, 8, 2, 128, 90, [90, 17, 0], "bf16")
+    check(*x, run(*x, causal=False), causal=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_joined_with_other_attention(dtype):
+    q, k4, v4, lens = make(15, 4, 3, 8, 2, 64, 150, [150, 2, 0, 77], dtype)
+    g = torch.Generator().manual_seed(16)
+    other = torch.randn(4, 3, 8, 64, generator=g).to(q.dtype), 4 * torch.randn(4, 3, 8, generator=g)
+    other[1][0, 0, :3], other[1][2, :, 5] = -math.inf, -math.inf
+    other[0][0, 0, :3], other[0][2, :, 5] = math.nan, math.inf        # of no weight
+    other[1][3, 1, 0], other[1][3, 1, 1] = 300.0, -300.0
+    check(q, k4, v4, lens, run(q, k4, v4, lens, other=other), other=other)
+
+
+def test_joined_in_place():
+    q, k4, v4, lens = make(17, 3, 1, 6, 2, 128, 90, [90, 5, 0], "bf16")
+    g = torch.Generator().manual_seed(18)
+    other = torch.randn(3, 1, 6, 128, generator=g).bfloat16(), torch.randn(3, 1, 6, generator=g)
+    cache = sp.Cache4(6, 2, 128, 90)
+    out, lse = other[0].to(DEV), other[1].to(DEV)
+    on = [tuple(y.to(DEV) for y in x) for x in (k4, v4)]
+    cache.attend(q.to(DEV), *on, lens.to(DEV), out, lse=lse, other_out=out, other_lse=lse)
+    check(q, k4, v4, lens, (out.cpu(), lse.cpu()), other=other)
+    cache.close()
+
+
+@pytest.mark.parametrize("D,B,n", [(128, 1, 200_003), (64, 2, 70_001)])
+def test_long_caches(D, B, n):
+    x = make(19, B, 2, 3, 1, D, n, [n - 5] * B, "bf16", garbage=False)
+    check(*x, run(*x))
+
+
+def test_more_units_than_the_gpu_holds():
+    lens = [(7 * b) % 40 for b in range(1024)]
+    x = make(20, 1024, 1, 4, 4, 32, 40, lens, "fp16")
+    check(*x, run(*x))
+
+
+def test_one_entry_with_all_of_the_weight_comes_out_exactly():
+    q, k4, v4, lens = make(21, 2, 1, 4, 2, 128, 500, [500, 333], "fp16")
+    k4[1][:, 250] = 120                    # a scale of 2, above all others
+    k4[0][:, 250] = 0x77                   # all 6
+    q[:] = 4.0
+    out, _ = run(q, k4, v4, lens, scale=1.0)
+    want = ref.values(*v4)[:, 250].half().repeat_interleave(2, 1)
+    assert torch.equal(out[:, 0], want)
+
+
+def test_large_and_small_queries():
+    """Rows of bf16 queries beyond half precision's range, and far below it."""
+    q, k4, v4, lens = make(22, 2, 1, 6, 2, 128, 100, [100, 64], "bf16")
+    for i, f in enumerate((1e30, 1e-30, 1.0, 1e36, 1e-36, 0.0)):
+        q[:, :, i] *= f
+    q[1, 0, 2, 5] = 3e30                   # one element far above its row
+    for scale in (1e-30, 1e28, 1.0):
+        s = scale * (q.double().unsqueeze(3) * ref.values(*k4)[:, None, :, [0, 0, 0, 1, 1, 1]].transpose(2, 3)).sum(-1)
+        fine = s.abs().amax((1, 3)) < 1e3  # (others are one entry's, by a wide margin or a narrow one)
+        want, wlse, tol, lse_tol = ref.attend(q, ref.values(*k4), ref.values(*v4), lens, True, scale)
+        out, lse = run(q, k4, v4, lens, scale=scale)
+        assert ((out.double() - want).abs() <= tol)[:, 0][fine].all()
+        assert ((lse.double() - wlse).abs() <= lse_tol)[:, 0][fine].all()
+        assert fine.any()
+
+
+def test_nan_entries():
+    """A NaN is that of the rows that see it, and of its 16 elements in a value."""
+    T, n = 4, 60
+    q, k4, v4, lens = make(23, 3, T, 4, 2, 64, 64, [n, n, n], "bf16")
+    k4[1][0, n - 2, 1, 3] = 255            # seen by the last two tokens
+    v4[1][1, n - 3, 0, 2] = 255            # by the last three
+    v4[1][2, 7, 1] = 255                   # by all
+    out, lse = run(q, k4, v4, lens)
+    nan = torch.zeros(out.shape, dtype=torch.bool)
+    nan[0, T - 2:, 2:] = True
+    nan[1, T - 3:, :2, 32:48] = True
+    nan[2, :, 2:] = True
+    assert torch.equal(out.isnan(), nan)
+    assert torch.equal(lse.isnan(), nan.all(-1) & (torch.arange(3) == 0).view(3, 1, 1))
+    clean = [tuple(torch.where(y == 255, 56, y) if i else y for i, y in enumerate(x)) for x in (k4, v4)]
+    want, _, tol, _ = ref.attend(q, *(ref.values(*x) for x in clean), lens)
+    mixed = nan | (torch.arange(3) == 0).view(3, 1, 1, 1) & nan
+    assert ((out.double() - want).abs() <= tol)[~mixed].all()
+
+
+def test_nan_and_infinite_queries():
+    q, k4, v4, lens = make(24, 1, 1, 4, 2, 128, 40, [40], "bf16")
+    q[0, 0, 1, 9], q[0, 0, 2, 100] = math.nan, math.inf
+    out, lse = run(q, k4, v4, lens)
+    assert out[0, 0, 1:3].isnan().all() and lse[0, 0, 1:3].isnan().all()
+    q[0, 0, 1:3] = 0
+    check(*(x[:, :, [0, 3]] if i == 0 else x for i, x in enumerate((q, k4, v4, lens))), (out[:, :, [0, 3]], lse[:, :, [0, 3]]))
+
+
+def test_results_repeat():
+    """Bit for bit, whichever block comes last."""
+    x = make(25, 3, 1, 8, 2, 128, 5000, [5000, 100, 3333], "bf16", garbage=False)
+    cache = sp.Cache4(8, 2, 128, 5000)
+    first = run(*x, cache=cache)
+    for _ in range(20):
+        again = run(*x, cache=cache)
+        assert torch.equal(first[0].view(torch.int16), again[0].view(torch.int16)) and torch.equal(first[1], again[1])
+    cache.close()
+
+
+# ---------------------------------------------------------------------------
+def test_a_decode_as_it_is_used():
+    """A shared prompt in 16 bits, entries of each step written and attended to in 4
+    bits, joined; then all of them back in 16 bits for the other operators."""
+    B, T, Hq, Hkv, D, C, P = 3, 2, 8, 2, 64, 40, 90
+    g = torch.Generator(device=DEV).manual_seed(26)
+    new = lambda *s: torch.randn(*s, generator=g, device=DEV).bfloat16()     # noqa: E731
+    pk, pv = new(P, Hkv, D), new(P, Hkv, D)
+    prefix, cache = sp.Cache(B, Hq, Hkv, D, 1, max_T=T), sp.Cache4(Hq, Hkv, D, C, max_T=T)
+    none, unused = torch.zeros(B, dtype=torch.int32, device=DEV), new(B, 1, Hkv, D)
+    k4, v4 = cache.new(B)
+    lens = torch.tensor([0, 3, 1], dtype=torch.int32, device=DEV)
+    k, v = (torch.zeros(B, C, Hkv, D, dtype=torch.bfloat16) for _ in range(2))     # what the caches stand for
+    for step in range(5):
+        q, nk, nv = new(B, T, Hq, D), new(B, T, Hkv, D), new(B, T, Hkv, D)
+        n = torch.randint(1, T + 1, (B,), generator=g, device=DEV, dtype=torch.int32)
+        cache.write(nk, nv, k4, v4, at=lens, n=n)
+        for b in range(B):
+            for held, x in ((k, nk), (v, nv)):
+                at = int(lens[b])
+                held[b, at:at + int(n[b])] = ref.quantise(x[b, :int(n[b])].cpu())[2].bfloat16()
+        lens += n
+        out, lse = torch.empty_like(q), torch.empty(B, T, Hq, device=DEV)
+        prefix.attend(q, unused, unused, none, out, prefix_k=pk, prefix_v=pv, lse=lse)
+        other = out.cpu(), lse.cpu()
+        cache.attend(q, k4, v4, lens, out, lse=lse, other_out=out, other_lse=lse)
+        want, wlse, tol, lse_tol = ref.attend(q.cpu(), k.double(), v.double(), lens.cpu(), other=other)
+        assert ((out.cpu().double() - want).abs() <= tol).all() and ((lse.cpu().double() - wlse).abs() <= lse_tol).all()
+        # the same attention in one piece, but for the rounding of the part over the prompt
+        whole, _, _, mass, size = serving_ref.attend(q.cpu(), k, v, lens.cpu(), pk.cpu(), pv.cpu())
+        assert ((out.cpu().double() - whole).abs() <= tol + 2.0 ** -7 * mass).all()
+    back_k, back_v = (torch.full((B, C, Hkv, D), 9.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    cache.read(k4, v4, back_k, back_v, n=lens)
+    for b in range(B):
+        n = int(lens[b])
+        assert torch.equal(back_k[b, :n].cpu(), k[b, :n]) and torch.equal(back_v[b, :n].cpu(), v[b, :n])
+        assert (back_k[b, n:] == 9).all()
+    cache.close()
+    prefix.close()
+
+
+def test_replayed_from_graphs_on_another_stream():
+    """Two graphs on one handle, replayed in turn on new inputs."""
+    x = [make(27 + i, 2, 1, 4, 2, 128, 3000, [3000, 40 + i], "bf16") for i in range(3)]
+    cache = sp.Cache4(4, 2, 128, 3000)
+    stream = torch.cuda.Stream()
+    on = [t.clone() for t in (x[0][0].to(DEV), *(y.to(DEV) for y in x[0][1] + x[0][2]), x[0][3].to(DEV))]
+    out, lse = torch.zeros(2, 1, 4, 128, dtype=torch.bfloat16, device=DEV), torch.zeros(2, 1, 4, device=DEV)
+    out2 = torch.zeros_like(out)
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    torch.cuda.synchronize()
+    for graph, o in zip(graphs, (out, out2)):
+        with torch.cuda.graph(graph, stream=stream):
+            cache.attend(on[0], (on[1], on[2]), (on[3], on[4]), on[5], o, lse=lse)
+    for i in (1, 2, 0):
+        for to, new in zip(on, (x[i][0], *x[i][1], *x[i][2], x[i][3])):
+            to.copy_(new)
+        with torch.cuda.stream(stream):
+            stream.wait_stream(torch.cuda.default_stream())
+            graphs[0].replay()
+            graphs[1].replay()
+        torch.cuda.synchronize()
+        check(*x[i], (out.cpu(), lse.cpu()))
+        assert torch.equal(out, out2)
+    cache.close()
+
+
+def test_refusals():
+    cache = sp.Cache4(4, 2, 64, 8, max_T=2)
+    k4, v4 = cache.new(2)
+    q = torch.zeros(2, 2, 4, 64, dtype=torch.bfloat16, device=DEV)
+    k = torch.zeros(2, 3, 2, 64, dtype=torch.bfloat16, device=DEV)
+    lens, out = torch.zeros(2, dtype=torch.int32, device=DEV), torch.empty_like(q)
+    with pytest.raises(ValueError, match="k4"):
+        cache.attend(q, None, v4, lens, out)
+    with pytest.raises(ValueError, match="shape"):
+        cache.attend(q, (k4[0], v4[0]), v4, lens, out)
+    with pytest.raises(ValueError, match="one without"):
+        cache.attend(q, k4, v4, lens, out, other_out=out)
+    with pytest.raises(sp.SpikeProjError) as e:
+        cache.attend(q.repeat(1, 2, 1, 1), k4, v4, lens, out.repeat(1, 2, 1, 1))
+    assert e.value.status == sp.SP_ERANGE
+    with pytest.raises(sp.SpikeProjError) as e:
+        cache.write(k, k.clone(), k4, k4)
+    assert e.value.status == sp.SP_EINVAL
+    with pytest.raises(ValueError, match="expected"):
+        cache.write(k.half(), k, k4, v4)
+    with pytest.raises(ValueError, match="k_out"):
+        cache.read(k4, v4, None, k)
+    cache.close()
