@@ -744,7 +744,7 @@ sp_status spike_proj_verify(const sp_verify *call, sp_stream_t stream);
  * rows without gaps are.  Storing the heads before the entries (head strides above
  * entry strides) keeps what one head reads together.
  *
- * spike_proj_cache4_create: the handle owns workspace (40 MB at most) and no entry of
+ * spike_proj_cache4_create: the handle owns workspace (50 MB at most) and no entry of
  *   any cache.  1 <= max_T <= SPIKE_PROJ_CACHE_MAX_T, 1 <= Hq <=
  *   SPIKE_PROJ_CACHE_MAX_HEADS, 16 <= D <= SPIKE_PROJ_CACHE_MAX_D, 1 <= capacity <=
  *   SPIKE_PROJ_CACHE_MAX_LEN (else SP_ERANGE); Hq % Hkv == 0 (SP_EINVAL); D % 16 == 0

@@ -19,13 +19,13 @@
 //                 t, t + 4, t + 8, t + 12
 // P^T comes from S^T by transposing 8 x 8 blocks between the threads.
 //
-// Work: the entries of all (sequence, K/V head, up to 32 rows) are one line of
-// tiles of 16, which the CTAs share out evenly, whatever the lengths (which only
-// the device knows).  A warp takes every eighth tile of its CTA's, through a ring
-// of its own in shared memory (cp.async), with its own running maximum and sums;
-// the warps' results are merged at the end of a CTA's tiles of a unit.  Where a
-// unit is of several CTAs, each leaves its result in the workspace, and the one
-// that comes last merges them, in the order of the tiles.
+// Work: the entries of all units (sequence, K/V head, up to 32 rows) are one line of
+// tiles of 32, which all warps share out evenly, whatever the lengths (which only
+// the device knows).  A warp works by itself: its tiles come through a ring of its
+// own in shared memory (cp.async), unit after unit without a pause, and it keeps
+// its own maximum and sums.  A unit that one warp has the whole of is written out
+// by it; of others each warp leaves its part in the workspace, and merge4_kernel
+// adds them up, in the order of the tiles.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -37,41 +37,41 @@
 namespace sp {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kTile = 16;                  // entries of a tile
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kTile = 32, kSubs = kTile / 16;   // entries of a tile, instructions that they are the rows of
 constexpr int kMaxRows = 32;               // of a unit
-constexpr int kMaxSeqs = SPIKE_PROJ_CACHE_MAX_B;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The reference of the exponentials follows the running maximum only when that has
 // grown by more than 2^kLag; it lies kLift below, so that half precision's
 // subnormals are 2^-34 of the largest probability.
 constexpr float kLag = 4.f, kLift = 10.f;
-constexpr int kStart = 8;                  // cost of a unit beside its tiles
+constexpr int kStart = 2;                  // cost of a unit beside its tiles
+constexpr int kLeast = 4;                  // cost that is worth a warp
 constexpr uint32_t kOnes = 0x3c003c00u;
 
+// CTAs of an SM, by the registers that NT x 8 rows take.
+constexpr int ctas_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
 template <int DK> constexpr int kRowBytes = DK / 2;
 template <int DK> constexpr int kStageBytes = 2 * kTile * kRowBytes<DK> + 2 * kTile * 8;
-// Rings take what a warp's result does in the merge, at the least.
-template <int DK, int NT> constexpr int kStages = NT <= 2 ? 4 : DK == 128 ? 8 : 8;
-template <int DK, int NT> constexpr int kWarpBytes = kStages<DK, NT> * kStageBytes<DK> > 8 * NT * DK * 4
-                                                         ? kStages<DK, NT> * kStageBytes<DK>
-                                                         : 8 * NT * DK * 4;
+template <int DK, int NT> constexpr int kStages = DK == 64 || NT > 2 ? 4 : 3;
+template <int DK, int NT> constexpr int kQueryBytes = NT > 1 ? NT * (DK / 16) * 32 * 8 : 0;
+template <int DK, int NT> constexpr int kWarpBytes = kStages<DK, NT> * kStageBytes<DK> + kQueryBytes<DK, NT>;
+static_assert(ctas_per_sm(1) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
+              ctas_per_sm(2) * (kWarps * kWarpBytes<128, 2> + 1280) <= 228 * 1024 &&
+              ctas_per_sm(4) * (kWarps * kWarpBytes<128, 4> + 1280) <= 228 * 1024, "shared memory of an SM");
+static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 8, "room for the costs before each sequence");
 
 struct Params {
   sp_attend4 c;
   int32_t Hkv, G, D, capacity, R;
   int32_t blocks, block_rows;              // units of a (sequence, K/V head); rows of one
+  int32_t slot_rows;                       // rows of a slot
   int32_t bf16;
   float c2;                                // scale * log2 e
-  uint32_t* tickets;                       // [grid], zero between calls
-  float4* slot_ml;                         // [2 grid][32]: reference, sum, sum of the rounded
-  float* slot_o;                           // [2 grid][32][DK]
+  int2* units;                             // [B][Hkv][blocks]: slot of the first part, warp of the last
+  float4* slot_ml;                         // [2 warps][slot_rows]: reference, sum, sum of the rounded
+  float* slot_o;                           // [2 warps][slot_rows][DK]
 };
-
-// Dynamic shared memory: the warps' rings, and what the merge keeps of them.
-template <int DK, int NT> constexpr size_t smem_bytes() {
-  return (size_t)kWarps * kWarpBytes<DK, NT> + (NT > 1 ? NT * (DK / 16) * 32 * 8 : 0);
-}
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -103,6 +103,29 @@ __device__ __forceinline__ void copy_async(uint32_t to, const uint8_t* from) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// Two floats in one 64-bit register, for the packed FP32 instructions.
+using f32x2 = unsigned long long;
+__device__ __forceinline__ f32x2 pair(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 halves(f32x2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 __device__ __forceinline__ float2 to_float(bool bf16, uint32_t x) {
   if (bf16) return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
   return __half22float2(*reinterpret_cast<const __half2*>(&x));
@@ -133,37 +156,103 @@ template <int DK> __device__ __forceinline__ int place_of(int entry, int byte) {
 // ---- the line of tiles --------------------------------------------------------
 struct Line {
   int64_t all;
-  int ctas;
-  __device__ __forceinline__ int64_t first(int c) const { return c * all / ctas; }
-  __device__ __forceinline__ int owner(int64_t at) const { return (int)(((at + 1) * ctas - 1) / all); }
+  int warps;
+  __device__ __forceinline__ int64_t first(int w) const { return w * all / warps; }
+  __device__ __forceinline__ int owner(int64_t at) const { return (int)(((at + 1) * warps - 1) / all); }
 };
 __device__ __forceinline__ int used(const Params& p, int b) { return min(max(__ldg(p.c.lens + b), 0), p.capacity); }
 
-// A row's results of several parts, as they are merged.
-struct RowSum {
-  float m, l, r;                           // reference, sum, sum of the rounded probabilities
+// A warp's way along the line: unit (b, u), its entries, its tiles j .. j1 of the
+// warp's.  A unit takes kStart + nt on the line from `at` on; tile j is at + kStart + j,
+// and belongs to the warp whose part of the line that is in (a unit without tiles to
+// the one that `at` is in).
+struct Cursor {
+  int b, u, n, nt, j, j1;
+  int64_t at;
+  __device__ __forceinline__ void enter(const Params& p, int64_t begin, int64_t end) {
+    n = used(p, b);
+    nt = ceil_div(n, kTile);
+    j = (int)max((int64_t)0, begin - at - kStart);
+    j1 = (int)min((int64_t)nt, max((int64_t)0, end - at - kStart));
+  }
+  __device__ __forceinline__ void next(const Params& p, int64_t begin, int64_t end) {
+    at += kStart + nt;
+    if (++u == p.Hkv * p.blocks) {
+      u = 0;
+      ++b;
+    }
+    if (at < end) enter(p, begin, end);
+    else j = j1 = 0;
+  }
 };
 
+// N values of a row from element d on, out of the sums o with reference `base`, sums l
+// and r: joined with other attention, divided, rounded, stored.
+template <int N>
+__device__ __forceinline__ void finish(const Params& p, int b, int h, int r, int d, float base, float l, float r_sum,
+                                       float (&o)[N], bool first) {
+  const int tok = r / p.G, hq = h * p.G + r - tok * p.G;
+  const int64_t row = ((int64_t)b * p.c.T + tok) * p.Hkv * p.G + hq;
+  if (p.c.other_out) {
+    const float other = p.c.other_lse[row] * kLog2e;
+    if (!(other == -INFINITY)) {
+      const float to = fmaxf(base, other);
+      const float f = base == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to);
+      const uint16_t* from = static_cast<const uint16_t*>(p.c.other_out) + b * p.c.other_batch + tok * p.c.other_token +
+                             hq * p.c.other_head + d;
+#pragma unroll
+      for (int i = 0; i < N; i += 4)
+        if (d + i < p.D) {
+          const uint2 raw = *reinterpret_cast<const uint2*>(from + i);
+          const float2 lo = to_float(p.bf16, raw.x), hi = to_float(p.bf16, raw.y);
+          o[i] = fmaf(fo, lo.x, f * o[i]), o[i + 1] = fmaf(fo, lo.y, f * o[i + 1]);
+          o[i + 2] = fmaf(fo, hi.x, f * o[i + 2]), o[i + 3] = fmaf(fo, hi.y, f * o[i + 3]);
+        }
+      l = fmaf(l, f, fo);
+      r_sum = fmaf(r_sum, f, fo);
+      base = to;
+    }
+  }
+  const bool empty = l == 0.f;
+  const float inv = empty ? 0.f : 1.f / r_sum;
+  uint16_t* out = static_cast<uint16_t*>(p.c.out) + b * p.c.out_batch + tok * p.c.out_token + hq * p.c.out_head + d;
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) w[i] = empty ? 0u : from_float(p.bf16, o[2 * i] * inv, o[2 * i + 1] * inv);
+  if constexpr (N % 8 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+      if (d + i < p.D) *reinterpret_cast<uint4*>(out + i) = make_uint4(w[i / 2], w[i / 2 + 1], w[i / 2 + 2], w[i / 2 + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      if (d + i < p.D) *reinterpret_cast<uint2*>(out + i) = make_uint2(w[i / 2], w[i / 2 + 1]);
+  }
+  if (first && p.c.lse) p.c.lse[row] = empty ? -INFINITY : (base + log2f(l)) * kLn2;
+}
+
 template <int DK, int NT>
-__global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(const __grid_constant__ Params p) {
   constexpr int KS = DK / 16;              // steps of S's sum, m-tiles of O
   constexpr int RB = kRowBytes<DK>, NS = kStages<DK, NT>;
+  constexpr int SB = NT == 1 ? kSubs : 1;  // instructions' entries between two looks at the maximum
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int64_t s_before[kMaxSeqs + 1];
   __shared__ int64_t s_scan[kWarps];
-  __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT], s_r[kWarps][8 * NT];
-  __shared__ uint32_t s_poison[8 * NT];
-  __shared__ int s_last;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * kWarpBytes<DK, NT>;
-  uint2* s_q = reinterpret_cast<uint2*>(smem + kWarps * kWarpBytes<DK, NT>);     // [NT][KS][32]
+  uint2* s_q = reinterpret_cast<uint2*>(ring + NS * kStageBytes<DK>);            // [NT][KS][32]
   pdl_launch_dependents();
   pdl_wait();
 
-  // cost of the units of all sequences before each
-  const int per_seq = p.Hkv * p.blocks;
+  // Where the warp's part of the line begins (the costs before each sequence lie in
+  // the rings for that).
+  Line line;
+  Cursor cur;
+  const int me = blockIdx.x * kWarps + warp;
+  int64_t begin, end;
   {
-    const int per = (p.c.B + kThreads - 1) / kThreads;
+    int64_t* before = reinterpret_cast<int64_t*>(smem);
+    const int per_seq = p.Hkv * p.blocks, per = (p.c.B + kThreads - 1) / kThreads;
     int64_t sum = 0;
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
@@ -177,49 +266,150 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
     }
     if (lane == 31) s_scan[warp] = up;
     __syncthreads();
-    int64_t before = up - sum;
-    for (int w = 0; w < warp; ++w) before += s_scan[w];
+    int64_t x = up - sum;
+    for (int w = 0; w < warp; ++w) x += s_scan[w];
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b < p.c.B) {
-        s_before[b] = before;
-        before += (int64_t)per_seq * (kStart + ceil_div(used(p, b), kTile));
-        if (b == p.c.B - 1) s_before[p.c.B] = before;
+        before[b] = x;
+        x += (int64_t)per_seq * (kStart + ceil_div(used(p, b), kTile));
+        if (b == p.c.B - 1) before[p.c.B] = x;
       }
     }
     __syncthreads();
-  }
-  Line line;
-  line.all = s_before[p.c.B];
-  // (a tile for each warp at least)
-  line.ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, line.all / (kStart + kWarps)));
-  const int cta = blockIdx.x;
-  if (cta >= line.ctas) return;
-  const int64_t begin = line.first(cta), end = line.first(cta + 1);
-
-  for (int64_t x = begin; x < end;) {
-    int b = 0;
-    for (int hi = p.c.B; hi - b > 1;) {
-      const int mid = (b + hi) >> 1;
-      if (s_before[mid] <= x) b = mid; else hi = mid;
+    line.all = before[p.c.B];
+    line.warps = (int)min((int64_t)gridDim.x * kWarps, max((int64_t)1, line.all / kLeast));
+    begin = line.first(min(me, line.warps));
+    end = line.first(min(me + 1, line.warps));
+    int lo = 0;
+    for (int hi = p.c.B; hi - lo > 1;) {
+      const int mid = (lo + hi) >> 1;
+      if (before[mid] <= begin) lo = mid; else hi = mid;
     }
-    const int n = used(p, b), nt = ceil_div(n, kTile), cost = kStart + nt;
-    const int u = (int)((x - s_before[b]) / cost);
-    const int64_t at = s_before[b] + (int64_t)u * cost, next = at + cost;
-    const int h = u / p.blocks, block = u - h * p.blocks;
-    const int j0 = (int)max((int64_t)0, x - at - kStart);
-    const int j1 = (int)max((int64_t)0, min(end, next) - at - kStart);
-    const bool initial = x == begin;
-    x = next;
-    if (j1 <= j0 && (nt > 0 || j0 > 0 || (initial && at != begin))) continue;
+    cur.b = lo;
+    const int cost = kStart + ceil_div(used(p, lo), kTile);
+    cur.u = (int)((begin - before[lo]) / cost);
+    cur.at = before[lo] + (int64_t)cur.u * cost;
+    __syncthreads();
+    if (begin >= end) return;
+    cur.enter(p, begin, end);
+  }
+
+  // ---- tiles on their way ---------------------------------------------------------
+  const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
+  const int nbytes = p.D / 2, groups = p.D / 16;
+  Cursor f = cur;                          // of the tile to be fetched
+  // A lane copies 16 bytes of every kCopyRows-th entry of a tile, from copy_row on.
+  // Scales: lane l has those of entry l.
+  constexpr int C = RB / 16, kCopyRows = 32 / C;
+  const int copy_row = lane / C, copy_byte = lane % C * 16;
+  const uint32_t ring_u32 = smem_u32(ring), copy_to = ring_u32 + place_of<DK>(copy_row, copy_byte);
+  const uint8_t *kp, *vp, *ks, *vs;
+  const auto enter_unit = [&]() {
+    while (f.j >= f.j1 && f.at < end) f.next(p, begin, end);
+    if (f.at >= end) return;
+    const int h = f.u / p.blocks;
+    const int64_t e = (int64_t)f.j * kTile;
+    kp = k4.codes + f.b * k4.batch + h * k4.head + (e + copy_row) * k4.entry + copy_byte;
+    vp = v4.codes + f.b * v4.batch + h * v4.head + (e + copy_row) * v4.entry + copy_byte;
+    ks = k4.scales + f.b * k4.scales_batch + h * k4.scales_head + (e + lane) * k4.scales_entry;
+    vs = v4.scales + f.b * v4.scales_batch + h * v4.scales_head + (e + lane) * v4.scales_entry;
+  };
+  const auto row_scales = [&](const uint8_t* from) {
+    uint2 x = make_uint2(0, 0);
+    if (groups == 8) x = __ldg(reinterpret_cast<const uint2*>(from));
+    else if (groups == 4) x.x = __ldg(reinterpret_cast<const uint32_t*>(from));
+    else
+      for (int i = 0; i < groups; ++i) {
+        const uint32_t y = __ldg(from + i);
+        if (i < 4) x.x |= y << (8 * i); else x.y |= y << (8 * i - 32);
+      }
+    return x;
+  };
+  uint2 k_scales, v_scales;                // of the tile fetched last
+  const auto fetch = [&](int stage) {
+    if (f.j < f.j1) {
+      const uint32_t to = copy_to + stage * kStageBytes<DK>;
+      const int left = f.n - f.j * kTile;  // entries from the tile's first on
+      if (nbytes % 16 == 0) {
+        const uint8_t *kr = kp, *vr = vp;
+        if (left >= kTile && nbytes == RB) {
+#pragma unroll
+          for (int i = 0; i < kTile / kCopyRows; ++i) {
+            copy_async<16>(to + i * kCopyRows * RB, kr);
+            copy_async<16>(to + (kTile + i * kCopyRows) * RB, vr);
+            kr += kCopyRows * k4.entry;
+            vr += kCopyRows * v4.entry;
+          }
+        } else if (copy_byte < nbytes) {
+#pragma unroll
+          for (int i = 0; i < kTile / kCopyRows; ++i) {
+            if (copy_row + i * kCopyRows < left) {
+              copy_async<16>(to + i * kCopyRows * RB, kr);
+              copy_async<16>(to + (kTile + i * kCopyRows) * RB, vr);
+            }
+            kr += kCopyRows * k4.entry;
+            vr += kCopyRows * v4.entry;
+          }
+        }
+      } else {
+        constexpr int C8 = RB / 8;
+        const uint8_t* kc = kp - copy_row * k4.entry - copy_byte;
+        const uint8_t* vc = vp - copy_row * v4.entry - copy_byte;
+        const uint32_t to8 = ring_u32 + stage * kStageBytes<DK>;
+#pragma unroll 2
+        for (int i = 0; i < kTile * C8 / 32; ++i) {
+          const int e = (i * 32 + lane) / C8, byte = (i * 32 + lane) % C8 * 8;
+          if (e < left && byte < nbytes) {
+            copy_async<8>(to8 + place_of<DK>(e, byte), kc + e * k4.entry + byte);
+            copy_async<8>(to8 + kTile * RB + place_of<DK>(e, byte), vc + e * v4.entry + byte);
+          }
+        }
+      }
+      k_scales = v_scales = make_uint2(0, 0);
+      if (lane < left) {
+        k_scales = row_scales(ks);
+        v_scales = row_scales(vs);
+      }
+      if (++f.j < f.j1) {
+        kp += kTile * k4.entry;
+        vp += kTile * v4.entry;
+        ks += kTile * k4.scales_entry;
+        vs += kTile * v4.scales_entry;
+      } else {
+        enter_unit();
+      }
+    }
+    copy_commit();
+  };
+  const auto store_scales = [&](int stage, uint2 k, uint2 v) {
+    uint8_t* to = ring + stage * kStageBytes<DK> + 2 * kTile * RB + lane * 8;
+    *reinterpret_cast<uint2*>(to) = k;
+    *reinterpret_cast<uint2*>(to + kTile * 8) = v;
+  };
+  k_scales = v_scales = make_uint2(0, 0);
+  enter_unit();
+  {
+    uint2 k[NS - 1], v[NS - 1];
+#pragma unroll
+    for (int i = 0; i < NS - 1; ++i) {
+      fetch(i);
+      k[i] = k_scales, v[i] = v_scales;
+    }
+#pragma unroll
+    for (int i = 0; i < NS - 2; ++i) store_scales(i, k[i], v[i]);
+  }
+  int stage = 0, ahead = NS - 1;           // places in the ring: of the tile, of the tile to be fetched
+
+  for (; cur.at < end; cur.next(p, begin, end)) {
+    const int b = cur.b, n = cur.n, nt = cur.nt, h = cur.u / p.blocks, block = cur.u - h * p.blocks;
+    if (cur.j >= cur.j1 && (nt > 0 || cur.at < begin)) continue;
     const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0);
 
     // ---- the query rows ---------------------------------------------------------
-    if (tid < 8 * NT) s_poison[tid] = 0;
     uint2 q[KS];                           // of one n-tile
     float c2[NT][2];                       // of the rows 2t, 2t + 1 of each n-tile
     int far[NT][2];                        // entries that they see
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int r = i * 8 + g;
@@ -234,9 +424,12 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
         for (int j = 0; j < KS; ++j) {
           const int d = t * (DK / 4) + 4 * j;
           if (d < p.D) raw[j] = __ldg(reinterpret_cast<const uint2*>(from + d));
-          // (the largest that is finite)
+        }
+        // (the largest that is finite)
+        const uint32_t inf = p.bf16 ? 0x7f807f80u : 0x7c007c00u;
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
           const uint32_t w[2] = {raw[j].x & 0x7fff7fffu, raw[j].y & 0x7fff7fffu};
-          const uint32_t inf = p.bf16 ? 0x7f807f80u : 0x7c007c00u;
 #pragma unroll
           for (int e = 0; e < 2; ++e) top = __vmaxu2(top, w[e] & ~__vcmpgeu2(w[e], inf));
         }
@@ -253,10 +446,10 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
         const float2 lo = to_float(p.bf16, raw[j].x), hi = to_float(p.bf16, raw[j].y);
         const uint2 x = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
         if (NT == 1) q[j] = x;
-        else if (warp == 0) s_q[(i * KS + j) * 32 + lane] = x;
+        else s_q[(i * KS + j) * 32 + lane] = x;
       }
-      // (lane 4 r has row r's)
-      const float down = p.c2 * __int_as_float((127 - e) << 23);
+      // (lane 4 r has row r's; not 0, so that masked scores stay -infinity)
+      const float down = fmaxf(p.c2 * __int_as_float((127 - e) << 23), 0x1p-126f);
 #pragma unroll
       for (int e2 = 0; e2 < 2; ++e2) {
         c2[i][e2] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + e2));
@@ -264,79 +457,14 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
         far[i][e2] = r2 < rows ? n - (p.c.causal ? p.c.T - 1 - (row0 + r2) / p.G : 0) : n;
       }
     }
-    if (NT > 1) __syncthreads();
     const int all_see = n - (p.c.causal ? p.c.T - 1 : 0);
+    const int my_far = lane < rows ? n - (p.c.causal ? p.c.T - 1 - (row0 + lane) / p.G : 0) : 0;
+    uint32_t poison = 0;                   // lane r: groups of which row r sees a NaN value
 
-    // ---- a warp's tiles ---------------------------------------------------------
-    const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
-    const uint8_t* kc = k4.codes + b * k4.batch + h * k4.head;
-    const uint8_t* vc = v4.codes + b * v4.batch + h * v4.head;
-    // scales: lane l has those of entry l of a tile's keys, l - 16 of its values
-    const sp_kv4& mine4 = lane < 16 ? k4 : v4;
-    const uint8_t* sc = mine4.scales + b * mine4.scales_batch + h * mine4.scales_head;
-    const int64_t sc_entry = mine4.scales_entry;
-    const int groups = p.D / 16;
-    const auto fetch_codes = [&](int tile, int stage) {
-      const uint32_t to = smem_u32(ring) + stage * kStageBytes<DK>;
-      const int nbytes = p.D / 2;
-      if (nbytes % 16 == 0) {
-        constexpr int C = RB / 16;         // of a row
-#pragma unroll
-        for (int i = 0; i < kTile * C / 32; ++i) {
-          const int e = (i * 32 + lane) / C, byte = (i * 32 + lane) % C * 16;
-          const int64_t entry = (int64_t)tile * kTile + e;
-          if (entry < n && byte < nbytes) {
-            copy_async<16>(to + place_of<DK>(e, byte), kc + entry * k4.entry + byte);
-            copy_async<16>(to + kTile * RB + place_of<DK>(e, byte), vc + entry * v4.entry + byte);
-          }
-        }
-      } else {
-        constexpr int C = RB / 8;
-#pragma unroll
-        for (int i = 0; i < kTile * C / 32; ++i) {
-          const int e = (i * 32 + lane) / C, byte = (i * 32 + lane) % C * 8;
-          const int64_t entry = (int64_t)tile * kTile + e;
-          if (entry < n && byte < nbytes) {
-            copy_async<8>(to + place_of<DK>(e, byte), kc + entry * k4.entry + byte);
-            copy_async<8>(to + kTile * RB + place_of<DK>(e, byte), vc + entry * v4.entry + byte);
-          }
-        }
-      }
-    };
-    const auto fetch_scales = [&](int tile) {
-      uint2 s = make_uint2(0, 0);
-      const int64_t entry = (int64_t)tile * kTile + (lane & 15);
-      if (tile < j1 && entry < n) {
-        const uint8_t* from = sc + entry * sc_entry;
-        if (groups == 8) s = __ldg(reinterpret_cast<const uint2*>(from));
-        else if (groups == 4) s.x = __ldg(reinterpret_cast<const uint32_t*>(from));
-        else
-          for (int i = 0; i < groups; ++i) {
-            const uint32_t x = __ldg(from + i);
-            if (i < 4) s.x |= x << (8 * i); else s.y |= x << (8 * i - 32);
-          }
-      }
-      return s;
-    };
-    // A NaN scale of a value must not meet a probability of 0 of a row that does not
-    // see its entry: it becomes 0, and the rows that do see it remember the group.
-    const auto store_scales = [&](int tile, int stage, uint2 s) {
-      if (lane >= 16) {
-        const uint32_t bad[2] = {__vcmpgeu4(s.x, 0xf9f9f9f9u), __vcmpgeu4(s.y, 0xf9f9f9f9u)};
-        if (bad[0] | bad[1]) {
-          s.x &= ~bad[0];
-          s.y &= ~bad[1];
-          uint32_t mask = 0;
-          for (int i = 0; i < 8; ++i) mask |= (bad[i / 4] >> (8 * (i % 4)) & 1u) << i;
-          const int entry = tile * kTile + (lane & 15);
-          for (int r = 0; r < rows; ++r)
-            if (entry < n - (p.c.causal ? p.c.T - 1 - (row0 + r) / p.G : 0)) atomicOr(&s_poison[r], mask);
-        }
-      }
-      *reinterpret_cast<uint2*>(ring + stage * kStageBytes<DK> + 2 * kTile * RB + lane * 8) = s;
-    };
-
-    float o[NT][KS][4], sum_r[NT][4], m[NT][2], l[NT][2];
+    // ---- the unit's tiles -------------------------------------------------------
+    float o[NT][KS][4], sum_r[NT][4];
+    f32x2 l[NT], base[NT];                 // of the rows 2t, 2t + 1: sums, references (negative)
+    float lim[NT][2];                      // from where on the reference follows the maximum
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
 #pragma unroll
@@ -345,51 +473,67 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
         for (int e = 0; e < 4; ++e) o[i][j][e] = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum_r[i][e] = 0.f;
-      m[i][0] = m[i][1] = -INFINITY;
-      l[i][0] = l[i][1] = 0.f;
+      lim[i][0] = lim[i][1] = -INFINITY;
+      l[i] = base[i] = pair(0.f, 0.f);
     }
-    const int mine = max(0, ceil_div(j1 - j0 - warp, kWarps));
-    uint2 scales = fetch_scales(j0 + warp);
-#pragma unroll
-    for (int i = 0; i < NS - 1; ++i) {
-      if (i < mine) fetch_codes(j0 + warp + i * kWarps, i);
-      copy_commit();
-    }
-    for (int it = 0; it < mine; ++it) {
-      const int tile = j0 + warp + it * kWarps, stage = it % NS;
-      store_scales(tile, stage, scales);
-      scales = fetch_scales(tile + kWarps);
+#pragma unroll 1
+    for (int tile = cur.j; tile < cur.j1; ++tile) {
+      // (the place before this one's that is to be fetched to)
+      store_scales(ahead == 0 ? NS - 1 : ahead - 1, k_scales, v_scales);
       copy_wait<NS - 2>();
       __syncwarp();
       // (the place of the tile before, which every lane has left)
-      if (it + NS - 1 < mine) fetch_codes(tile + (NS - 1) * kWarps, (it + NS - 1) % NS);
-      copy_commit();
-      const uint8_t* place = ring + stage * kStageBytes<DK>;
-      const uint8_t* place_s = place + 2 * kTile * RB;
-
-      // S^T = K Q^T
-      float s[NT][4];
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+      fetch(ahead);
+      uint8_t* place = ring + stage * kStageBytes<DK>;
+      uint8_t* place_s = place + 2 * kTile * RB;
+      stage = stage + 1 == NS ? 0 : stage + 1;
+      ahead = ahead + 1 == NS ? 0 : ahead + 1;
+      // A NaN scale (exponent 31) of a value must not meet a probability of 0 of a row
+      // that does not see its entry: it becomes 0, and the rows that do see it
+      // remember the group.
       {
+        uint2* at = reinterpret_cast<uint2*>(place_s + (kTile + lane) * 8);
+        const uint2 x = *at;
+        const auto nan = [](uint32_t x) { return ((x & 0x78787878u) + 0x08080808u) & x & 0x80808080u; };
+        const uint32_t bad[2] = {nan(x.x), nan(x.y)};
+        if (__any_sync(0xffffffffu, bad[0] | bad[1])) {
+          *at = make_uint2(x.x & ~(bad[0] / 128 * 255), x.y & ~(bad[1] / 128 * 255));
+          uint32_t mask = 0;
+          for (int i = 0; i < 8; ++i) mask |= (bad[i / 4] >> (8 * (i % 4) + 7) & 1u) << i;
+          for (int e = 0; e < kTile; ++e) {
+            const uint32_t m = __shfl_sync(0xffffffffu, mask, e);
+            if (tile * kTile + e < my_far) poison |= m;
+          }
+          __syncwarp();
+        }
+      }
+#pragma unroll 1
+      for (int sub0 = 0; sub0 < kSubs; sub0 += SB) {
+      // S^T = K Q^T
+      float s[SB][NT][4];
+#pragma unroll
+      for (int sub = 0; sub < SB; ++sub) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[sub][i][e] = 0.f;
         constexpr int W = DK / 32;         // words of an entry: four code pairs each
         uint32_t w[2][W], sc2[2][W / 2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const int e = entry_of(g + 8 * half);
-          const uint8_t* from = place + place_of<DK>(e, t * (RB / 4));
+          const int e = entry_of(g) + 8 * half;
+          const uint8_t* from = place + place_of<DK>(entry_of(g), t * (RB / 4)) + (16 * (sub0 + sub) + 8 * half) * RB;
+          const uint8_t* from_s = place_s + (16 * (sub0 + sub) + e) * 8;
           if constexpr (DK == 128) {
             const uint4 x = *reinterpret_cast<const uint4*>(from);
             w[half][0] = x.x, w[half][1] = x.y, w[half][2] = x.z, w[half][3] = x.w;
-            const uint32_t y = *reinterpret_cast<const uint16_t*>(place_s + e * 8 + 2 * t);
+            const uint32_t y = *reinterpret_cast<const uint16_t*>(from_s + 2 * t);
             sc2[half][0] = scale_half2(y & 0xffu);
             sc2[half][1] = scale_half2(y >> 8);
           } else {
             const uint2 x = *reinterpret_cast<const uint2*>(from);
             w[half][0] = x.x, w[half][1] = x.y;
-            sc2[half][0] = scale_half2(place_s[e * 8 + t]);
+            sc2[half][0] = scale_half2(from_s[t]);
           }
         }
 #pragma unroll
@@ -408,50 +552,52 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
               const uint2 qq = NT == 1 ? q[2 * i + k] : s_q[(c * KS + 2 * i + k) * 32 + lane];
-              mma(s[c], a, qq.x, qq.y);
+              mma(s[sub][c], a, qq.x, qq.y);
             }
           }
         }
       }
       // probabilities
+      if (tile * kTile + 16 * (sub0 + SB) > all_see) {
+        const int e0 = tile * kTile + entry_of(g);               // of s[0][.][0 .. 1]; e0 + 8 of the others
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
+        for (int sub = 0; sub < SB; ++sub)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] *= c2[i][e & 1];
-      const int e0 = tile * kTile + entry_of(g);                 // of s[.][0 .. 1]; e0 + 8 of the others
-      if (tile * kTile + kTile > all_see) {
+          for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e0 + (e >> 1) * 8 >= far[i][e & 1]) s[i][e] = -INFINITY;
+            for (int e = 0; e < 4; ++e)
+              if (e0 + 16 * (sub0 + sub) + (e >> 1) * 8 >= far[i][e & 1]) s[sub][i][e] = -INFINITY;
       }
-      uint32_t pb[NT][2];
       bool grow = false;
       float top[NT][2];
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          top[i][e] = fmaxf(s[i][e], s[i][e + 2]);
-          grow |= top[i][e] > m[i][e] + kLag;
+          top[i][e] = fmaxf(s[0][i][e], s[0][i][e + 2]);
+#pragma unroll
+          for (int sub = 1; sub < SB; ++sub) top[i][e] = fmaxf(top[i][e], fmaxf(s[sub][i][e], s[sub][i][e + 2]));
+          top[i][e] *= c2[i][e];
+          grow |= top[i][e] > lim[i][e];
         }
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          float a[2];
+          float a[2], nb[2] = {halves(base[i]).x, halves(base[i]).y};
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float x = top[i][e];
 #pragma unroll
             for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             a[e] = 1.f;
-            if (x > m[i][e] + kLag) {
-              a[e] = ex2(m[i][e] - x);     // 0 at the first
-              m[i][e] = x;
+            if (x > lim[i][e]) {
+              a[e] = lim[i][e] == -INFINITY ? 0.f : ex2((kLift - x) - nb[e]);
+              lim[i][e] = x + kLag;
+              nb[e] = kLift - x;
             }
-            l[i][e] *= a[e];
           }
+          base[i] = pair(nb[0], nb[1]);
+          l[i] = fma2(l[i], pair(a[0], a[1]), pair(0.f, 0.f));
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum_r[i][e] *= a[e & 1];
 #pragma unroll
@@ -460,244 +606,240 @@ __global__ void __launch_bounds__(kThreads, NT <= 2 ? 2 : 1) attend4_kernel(cons
             for (int e = 0; e < 4; ++e) o[i][j][e] *= a[e & 1];
         }
       }
+      uint32_t pb[SB][NT][2];
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
+        const f32x2 by = pair(c2[i][0], c2[i][1]);
+        f32x2 sum[2 * SB];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float base = m[i][e] == -INFINITY ? 0.f : m[i][e] - kLift;
-          s[i][e] = ex2(s[i][e] - base);
-          s[i][e + 2] = ex2(s[i][e + 2] - base);
-          l[i][e] += s[i][e] + s[i][e + 2];
-        }
-        pb[i][0] = transpose8(pack_half2(s[i][0], s[i][1]));
-        pb[i][1] = transpose8(pack_half2(s[i][2], s[i][3]));
+        for (int sub = 0; sub < SB; ++sub)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const float2 x = halves(fma2(pair(s[sub][i][2 * half], s[sub][i][2 * half + 1]), by, base[i]));
+            const float2 y = make_float2(ex2(x.x), ex2(x.y));
+            sum[2 * sub + half] = pair(y.x, y.y);
+            pb[sub][i][half] = transpose8(pack_half2(y.x, y.y));
+          }
+#pragma unroll
+        for (int d = SB; d > 0; d /= 2)
+#pragma unroll
+          for (int j = 0; j < d; ++j) sum[j] = add2(sum[j], sum[j + d]);
+        l[i] = add2(l[i], sum[0]);
       }
       // O^T += V^T P^T
-      {
+#pragma unroll
+      for (int sub = 0; sub < SB; ++sub) {
         uint32_t w[4][KS / 4], sb[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int e = t + 4 * i;
-          const uint8_t* from = place + kTile * RB + place_of<DK>(e, g * (RB / 8));
+          // (entries t, t + 4: their places differ by more than the rows between)
+          const uint8_t* from = place + place_of<DK>(t + 4 * (i & 1), g * (RB / 8)) + (kTile + 16 * (sub0 + sub) + 8 * (i >> 1)) * RB;
+          const uint8_t* from_s = place_s + (kTile + 16 * (sub0 + sub) + t + 4 * i) * 8;
           if constexpr (DK == 128) {
             const uint2 x = *reinterpret_cast<const uint2*>(from);
             w[i][0] = x.x, w[i][1] = x.y;
-            sb[i] = place_s[(16 + e) * 8 + g];
+            sb[i] = from_s[g];
           } else {
             w[i][0] = *reinterpret_cast<const uint32_t*>(from);
-            sb[i] = place_s[(16 + e) * 8 + g / 2];
+            sb[i] = from_s[g / 2];
           }
         }
         const uint32_t s01 = sb[0] << 7 | sb[1] << 23, s23 = sb[2] << 7 | sb[3] << 23;
 #pragma unroll
         for (int i = 0; i < KS / 4; ++i) {
+          // pairs of entries instead of pairs of elements: even elements, odd ones
           uint32_t y[4][4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) codes_to_half(w[k][i], y[k]);
+          constexpr uint32_t low = 0x0f0f0f0fu;
+          codes_to_half((w[0][i] & low) | (w[1][i] << 4 & ~low), y[0]);
+          codes_to_half((w[0][i] >> 4 & low) | (w[1][i] & ~low), y[1]);
+          codes_to_half((w[2][i] & low) | (w[3][i] << 4 & ~low), y[2]);
+          codes_to_half((w[2][i] >> 4 & low) | (w[3][i] & ~low), y[3]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t a[4] = {mul_half2(__byte_perm(y[0][k], y[1][k], 0x5410), s01),
-                                   mul_half2(__byte_perm(y[0][k], y[1][k], 0x7632), s01),
-                                   mul_half2(__byte_perm(y[2][k], y[3][k], 0x5410), s23),
-                                   mul_half2(__byte_perm(y[2][k], y[3][k], 0x7632), s23)};
+            const uint32_t a[4] = {mul_half2(y[0][k], s01), mul_half2(y[1][k], s01), mul_half2(y[2][k], s23),
+                                   mul_half2(y[3][k], s23)};
 #pragma unroll
-            for (int c = 0; c < NT; ++c) mma(o[c][4 * i + k], a, pb[c][0], pb[c][1]);
+            for (int c = 0; c < NT; ++c) mma(o[c][4 * i + k], a, pb[sub][c][0], pb[sub][c][1]);
           }
         }
         const uint32_t ones[4] = {kOnes, kOnes, kOnes, kOnes};
 #pragma unroll
-        for (int c = 0; c < NT; ++c) mma(sum_r[c], ones, pb[c][0], pb[c][1]);
+        for (int c = 0; c < NT; ++c) mma(sum_r[c], ones, pb[sub][c][0], pb[sub][c][1]);
+      }
       }
       __syncwarp();
     }
-    copy_wait<0>();
-    __syncwarp();
 
-    // ---- the warps' results, one after the other --------------------------------
-    float* ow = reinterpret_cast<float*>(ring);                  // [8 NT][DK]
+    // ---- what the warp has of the unit ------------------------------------------
+    const int w_first = nt > 0 ? line.owner(cur.at + kStart) : me, w_last = nt > 0 ? line.owner(cur.at + kStart + nt - 1) : me;
+    const bool whole = w_first == w_last;
+    const int64_t slot = 2 * (int64_t)me + (cur.at >= begin ? 1 : 0);            // (begun before, or here)
+    if (lane == 0 && me == w_first) p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] = make_int2(whole ? -1 : (int)slot, w_last);
+    const bool poisoned = __any_sync(0xffffffffu, poison != 0);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float x = l[i][e];
+        float x = e ? halves(l[i]).y : halves(l[i]).x;
 #pragma unroll
         for (int d = 4; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
         const int r = i * 8 + 2 * t + e;
-        if (g == 0) {
-          s_m[warp][r] = m[i][e];
-          s_l[warp][r] = x;
-          s_r[warp][r] = sum_r[i][e];
-        }
+        float v[DK / 8];
 #pragma unroll
-        for (int j = 0; j < KS; ++j)
-          *reinterpret_cast<float2*>(ow + r * DK + g * (DK / 8) + 2 * j) = make_float2(o[i][j][e], o[i][j][e + 2]);
+        for (int j = 0; j < KS; ++j) v[2 * j] = o[i][j][e], v[2 * j + 1] = o[i][j][e + 2];
+        if (poisoned) {
+          const uint32_t bits = __shfl_sync(0xffffffffu, poison, r);
+          if (bits >> (g * (DK / 8) / 16) & 1u)
+#pragma unroll
+            for (int j = 0; j < DK / 8; ++j) v[j] = NAN;
+        }
+        const float ref = lim[i][e] == -INFINITY ? -INFINITY : -(e ? halves(base[i]).y : halves(base[i]).x);
+        if (r < rows) {
+          if (whole) {
+            finish<DK / 8>(p, b, h, row0 + r, g * (DK / 8), ref, x, sum_r[i][e], v, g == 0);
+          } else {
+            if (g == 0) p.slot_ml[slot * p.slot_rows + r] = make_float4(ref, x, sum_r[i][e], 0.f);
+            float* to = p.slot_o + (slot * p.slot_rows + r) * DK + g * (DK / 8);
+#pragma unroll
+            for (int j = 0; j < DK / 8; j += 4) *reinterpret_cast<float4*>(to + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          }
+        }
       }
     }
-    __syncthreads();
+    __syncwarp();                          // (the queries' place)
+  }
+  copy_wait<0>();
+}
 
-    const int c_first = nt > 0 ? line.owner(at + kStart) : cta, c_last = nt > 0 ? line.owner(at + kStart + nt - 1) : cta;
-    // The sum over the warps: thread = (row, 4 elements).  (A NaN stays.)
-    const auto over_warps = [&](int r, int d, RowSum& a) {
-      a.m = -INFINITY;
+// Rows of units that several warps have parts of: WPR warps a row.
+template <int DK, int WPR>
+__global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant__ Params p) {
+  constexpr int kBatch = 8, E = DK / 32;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int64_t id = blockIdx.x;           // (sequence, K/V head, row)
+  const int64_t bh = id / p.R;
+  const int r = (int)(id - bh * p.R), block = r / p.block_rows, in = r - block * p.block_rows;
+  const int2 unit = __ldcg(p.units + bh * p.blocks + block);
+  if (unit.x < 0) return;
+  const int first = unit.x >> 1, count = unit.y - first + 1;
+  const auto slot_of = [&](int i) { return i == 0 ? (int64_t)unit.x : 2 * (int64_t)(first + i); };
+  float m = -INFINITY, l = 0.f, rs = 0.f, o[E] = {};
+  for (int i0 = warp; i0 < count; i0 += 32 * WPR) {
+    // lane j: part i0 + j WPR
+    const int mine = i0 + lane * WPR, some = min(32, (count - i0 + WPR - 1) / WPR);
+    float4 ml = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    if (mine < count) ml = __ldcg(p.slot_ml + slot_of(mine) * p.slot_rows + in);
+    float top = ml.x;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) a.m = fmaxf(a.m, s_m[w][r]);
-      a.l = a.r = 0.f;
-      float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
-      const float base = a.m == -INFINITY ? 0.f : a.m;
+    for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const float to = fmaxf(m, top), base = to == -INFINITY ? 0.f : to, f = ex2(m - base), w = ex2(ml.x - base);
+    float ls = w * ml.y, rr = w * ml.z;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = ex2(s_m[w][r] - base);
-        const float4 x = *reinterpret_cast<const float4*>(smem + w * kWarpBytes<DK, NT> + (r * DK + d) * 4);
-        a.l = fmaf(f, s_l[w][r], a.l);
-        a.r = fmaf(f, s_r[w][r], a.r);
-        o4.x = fmaf(f, x.x, o4.x), o4.y = fmaf(f, x.y, o4.y), o4.z = fmaf(f, x.z, o4.z), o4.w = fmaf(f, x.w, o4.w);
-      }
-      return o4;
-    };
-    const auto finish = [&](int r, int d, RowSum a, float4 o4) {
-      const int tok = (row0 + r) / p.G, hq = h * p.G + (row0 + r) - tok * p.G;
-      const int64_t row = ((int64_t)b * p.c.T + tok) * p.Hkv * p.G + hq;
-      float base = a.m - kLift;
-      if (p.c.other_out) {
-        const float other = p.c.other_lse[row] * kLog2e;
-        if (!(other == -INFINITY)) {
-          const float to = fmaxf(base, other);
-          const float f = a.m == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to);
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (d < p.D) {
-            const uint2 raw = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.c.other_out) + b * p.c.other_batch +
-                                                              tok * p.c.other_token + hq * p.c.other_head + d);
-            const float2 lo = to_float(p.bf16, raw.x), hi = to_float(p.bf16, raw.y);
-            x = make_float4(lo.x, lo.y, hi.x, hi.y);
-          }
-          o4.x = fmaf(fo, x.x, f * o4.x), o4.y = fmaf(fo, x.y, f * o4.y);
-          o4.z = fmaf(fo, x.z, f * o4.z), o4.w = fmaf(fo, x.w, f * o4.w);
-          a.l = fmaf(a.l, f, fo);
-          a.r = fmaf(a.r, f, fo);
-          a.m = 0.f;
-          base = to;
-        }
-      }
-      const bool empty = a.l == 0.f;
-      const float inv = empty ? 0.f : 1.f / a.r;
-      if (d < p.D) {
-        uint2 w = make_uint2(0u, 0u);
-        if (!empty) w = make_uint2(from_float(p.bf16, o4.x * inv, o4.y * inv), from_float(p.bf16, o4.z * inv, o4.w * inv));
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.c.out) + b * p.c.out_batch + tok * p.c.out_token +
-                                  hq * p.c.out_head + d) = w;
-      }
-      if (d == 0 && p.c.lse) p.c.lse[row] = empty ? -INFINITY : (base + log2f(a.l)) * kLn2;
-    };
-    const auto poison = [&](int r, int d, float4& o4) {
-      if (s_poison[r] >> (d / 16) & 1u) o4 = make_float4(NAN, NAN, NAN, NAN);
-    };
-    if (c_first == c_last) {
-      for (int i = tid; i < rows * (DK / 4); i += kThreads) {
-        const int r = i / (DK / 4), d = i % (DK / 4) * 4;
-        RowSum a;
-        float4 o4 = over_warps(r, d, a);
-        poison(r, d, o4);
-        finish(r, d, a, o4);
-      }
-      __syncthreads();
-      continue;
+    for (int d = 1; d < 32; d *= 2) {
+      ls += __shfl_xor_sync(0xffffffffu, ls, d);
+      rr += __shfl_xor_sync(0xffffffffu, rr, d);
     }
-    {
-      const int64_t slot = 2 * (int64_t)cta + (initial ? 0 : 1);
-      for (int i = tid; i < rows * (DK / 4); i += kThreads) {
-        const int r = i / (DK / 4), d = i % (DK / 4) * 4;
-        RowSum a;
-        float4 o4 = over_warps(r, d, a);
-        poison(r, d, o4);
-        if (d == 0) p.slot_ml[slot * kMaxRows + r] = make_float4(a.m, a.l, a.r, 0.f);
-        *reinterpret_cast<float4*>(p.slot_o + (slot * kMaxRows + r) * DK + d) = o4;
-      }
-    }
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) {
-      const uint32_t before = atomicAdd(p.tickets + c_first, 1u);
-      s_last = before == (uint32_t)(c_last - c_first);
-      if (s_last) p.tickets[c_first] = 0;
-    }
-    __syncthreads();
-    if (!s_last) continue;
-    __threadfence();
-    // Warp w sums every eighth of the unit's results, row by row; the warps' sums are
-    // then merged as those of their tiles were.
-    const int first_slot = line.first(c_first) >= at ? 2 * c_first : 2 * c_first + 1;
-    for (int r = 0; r < rows; ++r) {
-      RowSum a{-INFINITY, 0.f, 0.f};
-      float4 o4 = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int c0 = c_first + warp; c0 <= c_last; c0 += kWarps * 4) {
-        float4 ml[4], x[4];
+    m = to;
+    l = fmaf(l, f, ls);
+    rs = fmaf(rs, f, rr);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int c = c0 + i * kWarps;
-          ml[i] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-          x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (c <= c_last) {
-            const int64_t slot = c == c_first ? first_slot : 2 * (int64_t)c;
-            ml[i] = __ldcg(p.slot_ml + slot * kMaxRows + r);
-            if (lane < DK / 4) x[i] = __ldcg(reinterpret_cast<const float4*>(p.slot_o + (slot * kMaxRows + r) * DK + 4 * lane));
+    for (int e = 0; e < E; ++e) o[e] *= f;
+    for (int j0 = 0; j0 < some; j0 += kBatch) {
+      float x[kBatch][E];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (j0 + j < some) {
+          const float* from = p.slot_o + (slot_of(i0 + (j0 + j) * WPR) * p.slot_rows + in) * DK + lane * E;
+          if constexpr (E == 4) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
+            x[j][0] = y.x, x[j][1] = y.y, x[j][2] = y.z, x[j][3] = y.w;
+          } else {
+            const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
+            x[j][0] = y.x, x[j][1] = y.y;
           }
         }
-        float to = a.m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to = fmaxf(to, ml[i].x);
-        const float base = to == -INFINITY ? 0.f : to, f0 = ex2(a.m - base);
-        a.m = to;
-        a.l *= f0, a.r *= f0;
-        o4.x *= f0, o4.y *= f0, o4.z *= f0, o4.w *= f0;
+      for (int j = 0; j < kBatch; ++j) {
+        // (a part without weight too: what it has of NaN stays)
+        const float wj = __shfl_sync(0xffffffffu, w, j0 + j);
+        if (j0 + j < some)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float f = ex2(ml[i].x - base);
-          a.l = fmaf(f, ml[i].y, a.l);
-          a.r = fmaf(f, ml[i].z, a.r);
-          o4.x = fmaf(f, x[i].x, o4.x), o4.y = fmaf(f, x[i].y, o4.y), o4.z = fmaf(f, x[i].z, o4.z), o4.w = fmaf(f, x[i].w, o4.w);
-        }
-      }
-      if (lane < DK / 4) *reinterpret_cast<float4*>(ow + r * DK + 4 * lane) = o4;
-      if (lane == 0) {
-        s_m[warp][r] = a.m;
-        s_l[warp][r] = a.l;
-        s_r[warp][r] = a.r;
+          for (int e = 0; e < E; ++e) o[e] = fmaf(wj, x[j][e], o[e]);
       }
     }
-    __syncthreads();
-    for (int i = tid; i < rows * (DK / 4); i += kThreads) {
-      const int r = i / (DK / 4), d = i % (DK / 4) * 4;
-      RowSum a;
-      const float4 o4 = over_warps(r, d, a);
-      finish(r, d, a, o4);
+  }
+  if constexpr (WPR > 1) {
+    __shared__ float s_ml[WPR][3], s_o[WPR][DK];
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_o[warp][lane * E + e] = o[e];
+    if (lane == 0) {
+      s_ml[warp][0] = m;
+      s_ml[warp][1] = l;
+      s_ml[warp][2] = rs;
     }
     __syncthreads();
+    if (warp > 0) return;
+    float to = m;
+    for (int w = 1; w < WPR; ++w) to = fmaxf(to, s_ml[w][0]);
+    const float base = to == -INFINITY ? 0.f : to, f = ex2(m - base);
+    l *= f, rs *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+    for (int w = 1; w < WPR; ++w) {
+      const float x = ex2(s_ml[w][0] - base);
+      l = fmaf(x, s_ml[w][1], l);
+      rs = fmaf(x, s_ml[w][2], rs);
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(x, s_o[w][lane * E + e], o[e]);
+    }
+    m = to;
+  }
+  const int b = (int)(bh / p.Hkv), h = (int)(bh - (int64_t)b * p.Hkv);
+  if constexpr (E == 4) {
+    finish<4>(p, b, h, r, lane * 4, m, l, rs, o, lane == 0);
+  } else {
+    // two lanes' elements in one of them
+    float v[4] = {o[0], o[1], __shfl_down_sync(0xffffffffu, o[0], 1), __shfl_down_sync(0xffffffffu, o[1], 1)};
+    if (lane % 2 == 0) finish<4>(p, b, h, r, lane * 2, m, l, rs, v, lane == 0);
   }
 }
 
 // ---- host ---------------------------------------------------------------------
-int ctas_per_sm(int NT) { return NT <= 2 ? 2 : 1; }
 int n_tiles(int rows) { return (rows + 7) / 8; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <int DK, int NT>
 cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   static PerDevice attr;
-  const cudaError_t e = attr.once(dev, []() {
-    return cudaFuncSetAttribute(attend4_kernel<DK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<DK, NT>());
+  constexpr size_t bytes = (size_t)kWarps * kWarpBytes<DK, NT>;
+  cudaError_t e = attr.once(dev, []() {
+    return cudaFuncSetAttribute(attend4_kernel<DK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   });
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)(sms * ctas_per_sm(NT))), dim3(kThreads), smem_bytes<DK, NT>(), s, p);
+  const int grid = sms * ctas_per_sm(NT);
+  e = launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)grid), dim3(kThreads), bytes, s, p);
+  if (e != cudaSuccess) return e;
+  const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
+  // a warp of its own for every few parts of a unit
+  if ((int64_t)grid * kWarps >= 16 * (int64_t)p.c.B * p.Hkv * p.blocks)
+    return launch_pdl(merge4_kernel<DK, 16>, dim3((unsigned)rows), dim3(512), 0, s, p);
+  return launch_pdl(merge4_kernel<DK, 1>, dim3((unsigned)rows), dim3(32), 0, s, p);
 }
 
 }  // namespace
 
 Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
-  const size_t grid = 2 * (size_t)sms, DK = s.D <= 64 ? 64 : 128;
+  const int R = s.max_T * (s.Hq / s.Hkv);
+  const size_t DK = s.D <= 64 ? 64 : 128;
   Cache4Workspace w;
-  w.tickets = 0;
-  w.slots = round256(grid * 4);
-  w.bytes = w.slots + 2 * grid * kMaxRows * (16 + DK * 4);
+  w.slots = round256((size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * row_blocks4(R) * 8);
+  // (most for the most rows of a unit: fewer warps, but by less)
+  size_t most = 0;
+  for (int NT = 1; NT <= n_tiles(min(R, kMaxRows)); ++NT)
+    most = max(most, 2 * (size_t)sms * ctas_per_sm(NT) * kWarps * 8 * NT * (16 + DK * 4));
+  w.bytes = w.slots + most;
   return w;
 }
 
@@ -717,10 +859,11 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.bf16 = s.dtype == SP_BF16;
   p.c2 = c.scale * kLog2e;
   const Cache4Workspace w = cache4_workspace(s, sms);
-  p.tickets = reinterpret_cast<uint32_t*>(ws + w.tickets);
-  p.slot_ml = reinterpret_cast<float4*>(ws + w.slots);
-  p.slot_o = reinterpret_cast<float*>(ws + w.slots + 4 * (size_t)sms * kMaxRows * 16);
   const int NT = n_tiles(p.block_rows);
+  p.slot_rows = 8 * NT;
+  p.units = reinterpret_cast<int2*>(ws);
+  p.slot_ml = reinterpret_cast<float4*>(ws + w.slots);
+  p.slot_o = reinterpret_cast<float*>(ws + w.slots + 2 * (size_t)sms * ctas_per_sm(NT) * kWarps * p.slot_rows * 16);
   if (s.D <= 64) {
     switch (NT) {
       case 1: return launch_t<64, 1>(p, dev, sms, stream);

@@ -22,7 +22,7 @@ constexpr uint32_t kNaNScale4 = 0xff;      // scale of a group with a NaN or an 
 constexpr float kMaxScale4 = 10240.f;
 
 struct Cache4Workspace {
-  size_t tickets, slots, bytes;            // the tickets are zero between calls
+  size_t slots, bytes;                     // parts of units; notes on the units lie before them
 };
 Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms);
 // Query rows of a K/V head: as many units as it takes for 32 rows each at most.
