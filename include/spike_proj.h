@@ -846,7 +846,8 @@ sp_status spike_proj_cache4_read(sp_cache4_t cache, const sp_read4 *call,
  *              lse; nothing else may overlap the outputs.
  *   scale      finite and > 0 (SP_EINVAL).
  * q, out and other_out: as 16-bit tensors of spike_proj_cache4_write.  A T above
- * max_T: SP_ERANGE.
+ * max_T, or a call of 2^31 tiles (32 entries for up to 32 query rows of one K/V head)
+ * and more, were all caches full: SP_ERANGE.
  * Errors: SP_EINVAL, SP_EALIGN, SP_ERANGE, SP_EDEVICE, SP_ECUDA. */
 typedef struct sp_attend4 {
     const void *q;                        /* [B][T][Hq][D] */

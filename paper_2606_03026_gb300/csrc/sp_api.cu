@@ -1414,7 +1414,7 @@ sp_status spike_proj_cache4_attend(sp_cache4_t cache, const sp_attend4* c, sp_st
   if (c->other_out == c->out && !((c->B == 1 || c->other_batch == c->out_batch) && (c->T == 1 || c->other_token == c->out_token) &&
                                   (sh.Hq == 1 || c->other_head == c->out_head)))
     return SP_EINVAL;
-  if (c->B > SPIKE_PROJ_CACHE_MAX_B || c->T > sh.max_T) return SP_ERANGE;
+  if (c->B > SPIKE_PROJ_CACHE_MAX_B || c->T > sh.max_T || attend4_tiles(sh, *c) >= (int64_t)1 << 31) return SP_ERANGE;
   if (!rows_aligned(c->q, c->B, c->q_batch, c->T, c->q_token, sh.Hq, c->q_head, 0) ||
       !rows_aligned(c->out, c->B, c->out_batch, c->T, c->out_token, sh.Hq, c->out_head, sh.D) ||
       !kv4_aligned(sh, c->k4, c->B) || !kv4_aligned(sh, c->v4, c->B) || !aligned(c->lens, 4) || !aligned(c->lse, 4) ||

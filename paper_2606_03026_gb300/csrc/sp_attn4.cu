@@ -59,12 +59,13 @@ template <int DK, int NT> constexpr int kWarpBytes = kStages<DK, NT> * kStageByt
 static_assert(ctas_per_sm(1) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
               ctas_per_sm(2) * (kWarps * kWarpBytes<128, 2> + 1280) <= 228 * 1024 &&
               ctas_per_sm(4) * (kWarps * kWarpBytes<128, 4> + 1280) <= 228 * 1024, "shared memory of an SM");
-static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 8, "room for the costs before each sequence");
+static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
 struct Params {
   sp_attend4 c;
   int32_t Hkv, G, D, capacity, R;
   int32_t blocks, block_rows;              // units of a (sequence, K/V head); rows of one
+  Divide by_blocks, by_G;
   int32_t slot_rows;                       // rows of a slot
   int32_t bf16;
   float c2;                                // scale * log2 e
@@ -155,10 +156,17 @@ template <int DK> __device__ __forceinline__ int place_of(int entry, int byte) {
 
 // ---- the line of tiles --------------------------------------------------------
 struct Line {
-  int64_t all;
-  int warps;
-  __device__ __forceinline__ int64_t first(int w) const { return w * all / warps; }
-  __device__ __forceinline__ int owner(int64_t at) const { return (int)(((at + 1) * warps - 1) / all); }
+  uint32_t all, warps, each, more;         // the first `more` warps have each + 1 of it, the others each
+  __device__ __forceinline__ Line(uint32_t all, uint32_t most) : all(all) {
+    warps = min(most, max(1u, all / kLeast));
+    each = all / warps;
+    more = all - each * warps;
+  }
+  __device__ __forceinline__ uint32_t first(uint32_t w) const { return w * each + min(w, more); }
+  __device__ __forceinline__ int owner(uint32_t at) const {
+    const uint32_t long_ones = more * (each + 1);
+    return (int)(at < long_ones ? at / (each + 1) : more + (at - long_ones) / each);
+  }
 };
 __device__ __forceinline__ int used(const Params& p, int b) { return min(max(__ldg(p.c.lens + b), 0), p.capacity); }
 
@@ -168,14 +176,14 @@ __device__ __forceinline__ int used(const Params& p, int b) { return min(max(__l
 // the one that `at` is in).
 struct Cursor {
   int b, u, n, nt, j, j1;
-  int64_t at;
-  __device__ __forceinline__ void enter(const Params& p, int64_t begin, int64_t end) {
+  uint32_t at;
+  __device__ __forceinline__ void enter(const Params& p, uint32_t begin, uint32_t end) {
     n = used(p, b);
     nt = ceil_div(n, kTile);
-    j = (int)max((int64_t)0, begin - at - kStart);
-    j1 = (int)min((int64_t)nt, max((int64_t)0, end - at - kStart));
+    j = begin > at + kStart ? (int)(begin - at - kStart) : 0;
+    j1 = end > at + kStart ? min(nt, (int)(end - at - kStart)) : 0;
   }
-  __device__ __forceinline__ void next(const Params& p, int64_t begin, int64_t end) {
+  __device__ __forceinline__ void next(const Params& p, uint32_t begin, uint32_t end) {
     at += kStart + nt;
     if (++u == p.Hkv * p.blocks) {
       u = 0;
@@ -191,7 +199,8 @@ struct Cursor {
 template <int N>
 __device__ __forceinline__ void finish(const Params& p, int b, int h, int r, int d, float base, float l, float r_sum,
                                        float (&o)[N], bool first) {
-  const int tok = r / p.G, hq = h * p.G + r - tok * p.G;
+  uint32_t in_head;
+  const int tok = p.by_G(r, &in_head), hq = h * p.G + in_head;
   const int64_t row = ((int64_t)b * p.c.T + tok) * p.Hkv * p.G + hq;
   if (p.c.other_out) {
     const float other = p.c.other_lse[row] * kLog2e;
@@ -237,7 +246,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
   constexpr int RB = kRowBytes<DK>, NS = kStages<DK, NT>;
   constexpr int SB = NT == 1 ? kSubs : 1;  // instructions' entries between two looks at the maximum
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int64_t s_scan[kWarps];
+  __shared__ uint32_t s_scan[kWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * kWarpBytes<DK, NT>;
   uint2* s_q = reinterpret_cast<uint2*>(ring + NS * kStageBytes<DK>);            // [NT][KS][32]
@@ -246,54 +255,52 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
 
   // Where the warp's part of the line begins (the costs before each sequence lie in
   // the rings for that).
-  Line line;
   Cursor cur;
   const int me = blockIdx.x * kWarps + warp;
-  int64_t begin, end;
+  uint32_t* before = reinterpret_cast<uint32_t*>(smem);
   {
-    int64_t* before = reinterpret_cast<int64_t*>(smem);
-    const int per_seq = p.Hkv * p.blocks, per = (p.c.B + kThreads - 1) / kThreads;
-    int64_t sum = 0;
-    for (int i = 0; i < per; ++i) {
+    const uint32_t per_seq = p.Hkv * p.blocks, per = (p.c.B + kThreads - 1) / kThreads;
+    uint32_t sum = 0;
+    for (uint32_t i = 0; i < per; ++i) {
       const int b = tid * per + i;
-      if (b < p.c.B) sum += (int64_t)per_seq * (kStart + ceil_div(used(p, b), kTile));
+      if (b < p.c.B) sum += per_seq * (kStart + ceil_div(used(p, b), kTile));
     }
-    int64_t up = sum;
+    uint32_t up = sum;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, up, d);
+      const uint32_t x = __shfl_up_sync(0xffffffffu, up, d);
       if (lane >= d) up += x;
     }
     if (lane == 31) s_scan[warp] = up;
     __syncthreads();
-    int64_t x = up - sum;
+    uint32_t x = up - sum;
     for (int w = 0; w < warp; ++w) x += s_scan[w];
-    for (int i = 0; i < per; ++i) {
+    for (uint32_t i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b < p.c.B) {
         before[b] = x;
-        x += (int64_t)per_seq * (kStart + ceil_div(used(p, b), kTile));
+        x += per_seq * (kStart + ceil_div(used(p, b), kTile));
         if (b == p.c.B - 1) before[p.c.B] = x;
       }
     }
     __syncthreads();
-    line.all = before[p.c.B];
-    line.warps = (int)min((int64_t)gridDim.x * kWarps, max((int64_t)1, line.all / kLeast));
-    begin = line.first(min(me, line.warps));
-    end = line.first(min(me + 1, line.warps));
+  }
+  const Line line(before[p.c.B], gridDim.x * kWarps);
+  const uint32_t begin = line.first(min((uint32_t)me, line.warps)), end = line.first(min((uint32_t)me + 1, line.warps));
+  {
     int lo = 0;
     for (int hi = p.c.B; hi - lo > 1;) {
       const int mid = (lo + hi) >> 1;
       if (before[mid] <= begin) lo = mid; else hi = mid;
     }
     cur.b = lo;
-    const int cost = kStart + ceil_div(used(p, lo), kTile);
-    cur.u = (int)((begin - before[lo]) / cost);
-    cur.at = before[lo] + (int64_t)cur.u * cost;
-    __syncthreads();
-    if (begin >= end) return;
-    cur.enter(p, begin, end);
+    const uint32_t start = before[lo], cost = kStart + ceil_div(used(p, lo), kTile);
+    cur.u = (int)((begin - start) / cost);
+    cur.at = start + cur.u * cost;
   }
+  __syncthreads();
+  if (begin >= end) return;
+  cur.enter(p, begin, end);
 
   // ---- tiles on their way ---------------------------------------------------------
   const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
@@ -308,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
   const auto enter_unit = [&]() {
     while (f.j >= f.j1 && f.at < end) f.next(p, begin, end);
     if (f.at >= end) return;
-    const int h = f.u / p.blocks;
+    const int h = p.by_blocks(f.u);
     const int64_t e = (int64_t)f.j * kTile;
     kp = k4.codes + f.b * k4.batch + h * k4.head + (e + copy_row) * k4.entry + copy_byte;
     vp = v4.codes + f.b * v4.batch + h * v4.head + (e + copy_row) * v4.entry + copy_byte;
@@ -389,20 +396,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
   };
   k_scales = v_scales = make_uint2(0, 0);
   enter_unit();
-  {
-    uint2 k[NS - 1], v[NS - 1];
+  uint2 k_first[NS - 1], v_first[NS - 1];  // (stored when the queries are there)
 #pragma unroll
-    for (int i = 0; i < NS - 1; ++i) {
-      fetch(i);
-      k[i] = k_scales, v[i] = v_scales;
-    }
-#pragma unroll
-    for (int i = 0; i < NS - 2; ++i) store_scales(i, k[i], v[i]);
+  for (int i = 0; i < NS - 1; ++i) {
+    fetch(i);
+    k_first[i] = k_scales, v_first[i] = v_scales;
   }
+  bool first_unit = true;
   int stage = 0, ahead = NS - 1;           // places in the ring: of the tile, of the tile to be fetched
 
   for (; cur.at < end; cur.next(p, begin, end)) {
-    const int b = cur.b, n = cur.n, nt = cur.nt, h = cur.u / p.blocks, block = cur.u - h * p.blocks;
+    const int b = cur.b, n = cur.n, nt = cur.nt, h = p.by_blocks(cur.u), block = cur.u - h * p.blocks;
     if (cur.j >= cur.j1 && (nt > 0 || cur.at < begin)) continue;
     const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0);
 
@@ -414,37 +418,48 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     for (int i = 0; i < NT; ++i) {
       const int r = i * 8 + g;
       uint2 raw[KS];
-      uint32_t top = 0;
 #pragma unroll
       for (int j = 0; j < KS; ++j) raw[j] = make_uint2(0, 0);
       if (r < rows) {
-        const int tok = (row0 + r) / p.G, hq = h * p.G + (row0 + r) - tok * p.G;
-        const uint16_t* from = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token + hq * p.c.q_head;
+        uint32_t in_head;
+        const int tok = p.by_G(row0 + r, &in_head);
+        const uint16_t* from = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token +
+                               (int64_t)(h * p.G + in_head) * p.c.q_head + t * (DK / 4);
 #pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          const int d = t * (DK / 4) + 4 * j;
-          if (d < p.D) raw[j] = __ldg(reinterpret_cast<const uint2*>(from + d));
-        }
-        // (the largest that is finite)
-        const uint32_t inf = p.bf16 ? 0x7f807f80u : 0x7c007c00u;
-#pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          const uint32_t w[2] = {raw[j].x & 0x7fff7fffu, raw[j].y & 0x7fff7fffu};
-#pragma unroll
-          for (int e = 0; e < 2; ++e) top = __vmaxu2(top, w[e] & ~__vcmpgeu2(w[e], inf));
-        }
+        for (int j = 0; j < KS; ++j)
+          if (t * (DK / 4) + 4 * j < p.D) raw[j] = __ldg(reinterpret_cast<const uint2*>(from + 4 * j));
       }
-      top = max(top & 0xffffu, top >> 16);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      // 2^e that brings the largest to 2^14 .. 2^15 (bf16 only)
       int e = 0;
-      if (p.bf16) e = min(14 - ((int)(top >> 7) - 127), 100);
+      if (p.bf16) {
+        // 2^e that brings the largest that is finite to 2^14 .. 2^15
+        const auto largest = [&](uint32_t keep) {
+          uint32_t top = 0;
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            const uint32_t x = raw[j].x & 0x7fff7fffu, y = raw[j].y & 0x7fff7fffu;
+            if (keep) {
+              top = __vmaxu2(top, __vmaxu2(x, y));
+            } else {
+              top = __vmaxu2(top, x & ~__vcmpgeu2(x, 0x7f807f80u));
+              top = __vmaxu2(top, y & ~__vcmpgeu2(y, 0x7f807f80u));
+            }
+          }
+          top = max(top & 0xffffu, top >> 16);
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          return max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        };
+        uint32_t top = largest(1);
+        if (__any_sync(0xffffffffu, top >= 0x7f80u)) top = largest(0);
+        e = min(14 - ((int)(top >> 7) - 127), 100);
+      }
       const float up = __int_as_float((e + 127) << 23);
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        const float2 lo = to_float(p.bf16, raw[j].x), hi = to_float(p.bf16, raw[j].y);
-        const uint2 x = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
+        uint2 x = raw[j];
+        if (p.bf16) {
+          const float2 lo = to_float(true, x.x), hi = to_float(true, x.y);
+          x = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
+        }
         if (NT == 1) q[j] = x;
         else s_q[(i * KS + j) * 32 + lane] = x;
       }
@@ -454,11 +469,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
       for (int e2 = 0; e2 < 2; ++e2) {
         c2[i][e2] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + e2));
         const int r2 = i * 8 + 2 * t + e2;
-        far[i][e2] = r2 < rows ? n - (p.c.causal ? p.c.T - 1 - (row0 + r2) / p.G : 0) : n;
+        far[i][e2] = r2 < rows && p.c.causal ? n - (p.c.T - 1 - (int)p.by_G(row0 + r2)) : n;
       }
     }
     const int all_see = n - (p.c.causal ? p.c.T - 1 : 0);
-    const int my_far = lane < rows ? n - (p.c.causal ? p.c.T - 1 - (row0 + lane) / p.G : 0) : 0;
+    if (first_unit) {
+#pragma unroll
+      for (int i = 0; i < NS - 2; ++i) store_scales(i, k_first[i], v_first[i]);
+      first_unit = false;
+    }
     uint32_t poison = 0;                   // lane r: groups of which row r sees a NaN value
 
     // ---- the unit's tiles -------------------------------------------------------
@@ -498,6 +517,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
         const uint32_t bad[2] = {nan(x.x), nan(x.y)};
         if (__any_sync(0xffffffffu, bad[0] | bad[1])) {
           *at = make_uint2(x.x & ~(bad[0] / 128 * 255), x.y & ~(bad[1] / 128 * 255));
+          const int my_far = lane >= rows ? 0 : p.c.causal ? n - (p.c.T - 1 - (int)p.by_G(row0 + lane)) : n;
           uint32_t mask = 0;
           for (int i = 0; i < 8; ++i) mask |= (bad[i / 4] >> (8 * (i % 4) + 7) & 1u) << i;
           for (int e = 0; e < kTile; ++e) {
@@ -671,10 +691,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     }
 
     // ---- what the warp has of the unit ------------------------------------------
-    const int w_first = nt > 0 ? line.owner(cur.at + kStart) : me, w_last = nt > 0 ? line.owner(cur.at + kStart + nt - 1) : me;
-    const bool whole = w_first == w_last;
+    const bool begins = cur.j == 0, whole = begins && cur.j1 == nt;
     const int64_t slot = 2 * (int64_t)me + (cur.at >= begin ? 1 : 0);            // (begun before, or here)
-    if (lane == 0 && me == w_first) p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] = make_int2(whole ? -1 : (int)slot, w_last);
+    if (lane == 0 && begins)
+      p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] = make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kStart + nt - 1));
     const bool poisoned = __any_sync(0xffffffffu, poison != 0);
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -716,7 +736,6 @@ template <int DK, int WPR>
 __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant__ Params p) {
   constexpr int kBatch = 8, E = DK / 32;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_launch_dependents();
   pdl_wait();
   const int64_t id = blockIdx.x;           // (sequence, K/V head, row)
   const int64_t bh = id / p.R;
@@ -731,6 +750,22 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
     const int mine = i0 + lane * WPR, some = min(32, (count - i0 + WPR - 1) / WPR);
     float4 ml = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     if (mine < count) ml = __ldcg(p.slot_ml + slot_of(mine) * p.slot_rows + in);
+    float x[kBatch][E];
+    const auto load = [&](int j0) {
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (j0 + j < some) {
+          const float* from = p.slot_o + (slot_of(i0 + (j0 + j) * WPR) * p.slot_rows + in) * DK + lane * E;
+          if constexpr (E == 4) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
+            x[j][0] = y.x, x[j][1] = y.y, x[j][2] = y.z, x[j][3] = y.w;
+          } else {
+            const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
+            x[j][0] = y.x, x[j][1] = y.y;
+          }
+        }
+    };
+    load(0);
     float top = ml.x;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -747,19 +782,7 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] *= f;
     for (int j0 = 0; j0 < some; j0 += kBatch) {
-      float x[kBatch][E];
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j)
-        if (j0 + j < some) {
-          const float* from = p.slot_o + (slot_of(i0 + (j0 + j) * WPR) * p.slot_rows + in) * DK + lane * E;
-          if constexpr (E == 4) {
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(from));
-            x[j][0] = y.x, x[j][1] = y.y, x[j][2] = y.z, x[j][3] = y.w;
-          } else {
-            const float2 y = __ldcg(reinterpret_cast<const float2*>(from));
-            x[j][0] = y.x, x[j][1] = y.y;
-          }
-        }
+      if (j0 > 0) load(j0);
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         // (a part without weight too: what it has of NaN stays)
@@ -810,6 +833,18 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
 int n_tiles(int rows) { return (rows + 7) / 8; }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
+// (the SMs' shared memory stays divided as attend4_kernel needs it: otherwise some of
+// its CTAs find no place beside those of a merge before, and begin when others end)
+template <int DK, int WPR>
+cudaError_t launch_merge(const Params& p, int dev, cudaStream_t s) {
+  static PerDevice attr;
+  const cudaError_t e = attr.once(dev, []() {
+    return cudaFuncSetAttribute(merge4_kernel<DK, WPR>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  });
+  if (e != cudaSuccess) return e;
+  return launch_pdl(merge4_kernel<DK, WPR>, dim3((unsigned)((int64_t)p.c.B * p.Hkv * p.R)), dim3(32 * WPR), 0, s, p);
+}
+
 template <int DK, int NT>
 cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   static PerDevice attr;
@@ -821,11 +856,9 @@ cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   const int grid = sms * ctas_per_sm(NT);
   e = launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)grid), dim3(kThreads), bytes, s, p);
   if (e != cudaSuccess) return e;
-  const int64_t rows = (int64_t)p.c.B * p.Hkv * p.R;
   // a warp of its own for every few parts of a unit
-  if ((int64_t)grid * kWarps >= 16 * (int64_t)p.c.B * p.Hkv * p.blocks)
-    return launch_pdl(merge4_kernel<DK, 16>, dim3((unsigned)rows), dim3(512), 0, s, p);
-  return launch_pdl(merge4_kernel<DK, 1>, dim3((unsigned)rows), dim3(32), 0, s, p);
+  if ((int64_t)grid * kWarps >= 16 * (int64_t)p.c.B * p.Hkv * p.blocks) return launch_merge<DK, 32>(p, dev, s);
+  return launch_merge<DK, 1>(p, dev, s);
 }
 
 }  // namespace
@@ -843,6 +876,10 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
   return w;
 }
 
+int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c) {
+  return (int64_t)c.B * s.Hkv * row_blocks4(c.T * (s.Hq / s.Hkv)) * (kStart + ceil_div(s.capacity, kTile));
+}
+
 cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, cudaStream_t stream) {
   int dev = 0, sms = 0;
   const cudaError_t e = current_device(&dev, &sms);
@@ -856,6 +893,8 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.R = c.T * p.G;
   p.blocks = row_blocks4(p.R);
   p.block_rows = ceil_div(p.R, p.blocks);
+  p.by_blocks = Divide(p.blocks);
+  p.by_G = Divide(p.G);
   p.bf16 = s.dtype == SP_BF16;
   p.c2 = c.scale * kLog2e;
   const Cache4Workspace w = cache4_workspace(s, sms);

@@ -22,21 +22,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kItems = 4;                  // of 8 elements, of a thread
 
-// n / d and n % d for n < 2^31, d < 2^31.
-struct Divide {
-  uint32_t mul, shift, d;
-  explicit Divide(uint32_t by) : d(by) {
-    shift = 0;
-    while ((1ull << shift) < by) ++shift;
-    mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
-  }
-  __device__ __forceinline__ uint32_t operator()(uint32_t n, uint32_t* rest) const {
-    const uint32_t q = (uint32_t)(((uint64_t)__umulhi(n, mul) + n) >> shift);
-    *rest = n - q * d;
-    return q;
-  }
-};
-
 struct Strides {
   int64_t batch, token, head;
 };

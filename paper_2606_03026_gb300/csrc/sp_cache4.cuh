@@ -28,9 +28,31 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms);
 // Query rows of a K/V head: as many units as it takes for 32 rows each at most.
 inline __host__ __device__ int row_blocks4(int R) { return (R + 31) / 32; }
 
+// Tiles of entries that an attend call has at most (its kernels count them in 32 bits).
+int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c);
 cudaError_t launch_write4(const Cache4Shape& s, const sp_write4& c, cudaStream_t stream);
 cudaError_t launch_read4(const Cache4Shape& s, const sp_read4& c, cudaStream_t stream);
 cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, cudaStream_t stream);
+
+// n / d and n % d for n < 2^31, d < 2^31.
+struct Divide {
+  uint32_t mul = 0, shift = 0, d = 0;
+  Divide() = default;
+  explicit Divide(uint32_t by) : d(by) {
+    while ((1ull << shift) < by) ++shift;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
+  }
+#ifdef __CUDACC__
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const {
+    return (uint32_t)(((uint64_t)__umulhi(n, mul) + n) >> shift);
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t n, uint32_t* rest) const {
+    const uint32_t q = (*this)(n);
+    *rest = n - q * d;
+    return q;
+  }
+#endif
+};
 
 #ifdef __CUDACC__
 // Four code pairs of a word, in half precision (without their scale).
