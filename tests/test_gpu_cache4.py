@@ -89,7 +89,8 @@ def test_scales_on_and_beside_their_borders(dtype):
 
 
 def test_special_groups():
-    x = torch.randn(9, 128, generator=torch.Generator().manual_seed(2)).bfloat16()
+    x = torch.randn(10, 128, generator=torch.Generator().manual_seed(2)).bfloat16()
+    x[9, ::3], x[9, 1::3] = -0.0, 0.0
     x[0], x[1], x[2] = 0.0, -0.0, 1e-30
     x[3, 17], x[4, 127], x[5, 0] = math.nan, math.inf, -math.inf
     x[6], x[7, 5] = 3e38, 3e38
