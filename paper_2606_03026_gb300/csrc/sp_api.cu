@@ -93,7 +93,8 @@ struct sp_cache_s {
 struct sp_cache4_s {
   int device = 0;
   Cache4Shape shape;
-  uint8_t* ws = nullptr;          // cache4_workspace(shape).bytes
+  Cache4Workspace parts;
+  uint8_t* ws = nullptr;          // parts.bytes
 };
 
 struct sp_group_s {
@@ -1337,7 +1338,8 @@ sp_status spike_proj_cache4_create(sp_cache4_t* cache, int32_t max_T, int32_t Hq
   ca->device = dev;
   ca->shape = Cache4Shape{max_T, Hq, Hkv, D, capacity, dtype};
   cudaStream_t s = as_stream(stream);
-  st = dev_alloc_zero(&ca->ws, cache4_workspace(ca->shape, sms).bytes, s);
+  ca->parts = cache4_workspace(ca->shape, sms);
+  st = dev_alloc_zero(&ca->ws, ca->parts.bytes, s);
   cudaError_t e;
   if (st == SP_OK && (e = cudaStreamSynchronize(s)) != cudaSuccess) st = cuda_fail(e);
   if (st != SP_OK) {
@@ -1424,7 +1426,7 @@ sp_status spike_proj_cache4_attend(sp_cache4_t cache, const sp_attend4* c, sp_st
     return SP_EALIGN;
   const sp_status st = on_device(cache->device);
   if (st != SP_OK) return st;
-  SP_CUDA(launch_attend4(sh, *c, cache->ws, as_stream(stream)));
+  SP_CUDA(launch_attend4(sh, *c, cache->ws, cache->parts.slots, as_stream(stream)));
   return SP_OK;
 }
 

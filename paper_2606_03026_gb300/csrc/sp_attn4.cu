@@ -26,32 +26,16 @@
 // its own maximum and sums.  A unit that one warp has the whole of is written out
 // by it; of others each warp leaves its part in the workspace, and merge4_kernel
 // adds them up, in the order of the tiles.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include <math.h>
-
-#include "sp_cache4.cuh"
-#include "sp_ptx.cuh"
+#include "sp_attn4.cuh"
 
 namespace sp {
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+using Params = Attend4Params;
 constexpr int kTile = 32, kSubs = kTile / 16;   // entries of a tile, instructions that they are the rows of
-constexpr int kMaxRows = 32;               // of a unit
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// The reference of the exponentials follows the running maximum only when that has
-// grown by more than 2^kLag; it lies kLift below, so that half precision's
-// subnormals are 2^-34 of the largest probability.
-constexpr float kLag = 4.f, kLift = 10.f;
-constexpr int kStart = 2;                  // cost of a unit beside its tiles
-constexpr int kLeast = 4;                  // cost that is worth a warp
-constexpr uint32_t kOnes = 0x3c003c00u;
 
 // CTAs of an SM, by the registers that NT x 8 rows take.
 constexpr int ctas_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
-template <int DK> constexpr int kRowBytes = DK / 2;
 template <int DK> constexpr int kStageBytes = 2 * kTile * kRowBytes<DK> + 2 * kTile * 8;
 template <int DK, int NT> constexpr int kStages = DK == 64 || NT > 2 ? 4 : 3;
 template <int DK, int NT> constexpr int kQueryBytes = NT > 1 ? NT * (DK / 16) * 32 * 8 : 0;
@@ -61,228 +45,30 @@ static_assert(ctas_per_sm(1) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 102
               ctas_per_sm(4) * (kWarps * kWarpBytes<128, 4> + 1280) <= 228 * 1024, "shared memory of an SM");
 static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
-struct Params {
-  sp_attend4 c;
-  int32_t Hkv, G, D, capacity, R;
-  int32_t blocks, block_rows;              // units of a (sequence, K/V head); rows of one
-  Divide by_blocks, by_G;
-  int32_t slot_rows;                       // rows of a slot
-  int32_t bf16;
-  float c2;                                // scale * log2 e
-  int2* units;                             // [B][Hkv][blocks]: slot of the first part, warp of the last
-  float4* slot_ml;                         // [2 warps][slot_rows]: reference, sum, sum of the rounded
-  float* slot_o;                           // [2 warps][slot_rows][DK]
-};
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t to, const uint8_t* from) {
-  if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-__device__ __forceinline__ float2 to_float(bool bf16, uint32_t x) {
-  if (bf16) return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
-  return __half22float2(*reinterpret_cast<const __half2*>(&x));
-}
-__device__ __forceinline__ uint32_t from_float(bool bf16, float lo, float hi) {
-  uint32_t r;
-  if (bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  else r = pack_half2(lo, hi);
-  return r;
-}
-
-// Entry of row i < 16 of an instruction's K operand, and with it of element i of
-// the sum over entries: thread t's elements 2t, 2t + 1, 2t + 8, 2t + 9 are the
-// entries t, t + 4, t + 8, t + 12.
-__device__ __forceinline__ int entry_of(int i) { return (i & 8) | (i & 1) << 2 | (i & 7) >> 1; }
-// Where 16 bytes (8 where rows are 32 bytes) of an entry lie in a tile of the ring,
-// so that neither operand's loads meet in a bank.
-template <int DK> __device__ __forceinline__ int place_of(int entry, int byte) {
-  if constexpr (DK == 128) {
-    const int row = entry ^ (entry >> 2 & 1);
-    return row * 64 + (byte ^ (row >> 1 & 1) << 5);
-  } else {
-    const int row = entry ^ (entry & 4) >> 1;
-    return row * 32 + byte;
-  }
-}
-
-// ---- the line of tiles --------------------------------------------------------
-struct Line {
-  uint32_t all, warps, each, more;         // the first `more` warps have each + 1 of it, the others each
-  __device__ __forceinline__ Line(uint32_t all, uint32_t most) : all(all) {
-    warps = min(most, max(1u, all / kLeast));
-    each = all / warps;
-    more = all - each * warps;
-  }
-  __device__ __forceinline__ uint32_t first(uint32_t w) const { return w * each + min(w, more); }
-  __device__ __forceinline__ int owner(uint32_t at) const {
-    const uint32_t long_ones = more * (each + 1);
-    return (int)(at < long_ones ? at / (each + 1) : more + (at - long_ones) / each);
-  }
-};
-__device__ __forceinline__ int used(const Params& p, int b) { return min(max(__ldg(p.c.lens + b), 0), p.capacity); }
-
-// A warp's way along the line: unit (b, u), its entries, its tiles j .. j1 of the
-// warp's.  A unit takes kStart + nt on the line from `at` on; tile j is at + kStart + j,
-// and belongs to the warp whose part of the line that is in (a unit without tiles to
-// the one that `at` is in).
-struct Cursor {
-  int b, u, n, nt, j, j1;
-  uint32_t at;
-  __device__ __forceinline__ void enter(const Params& p, uint32_t begin, uint32_t end) {
-    n = used(p, b);
-    nt = ceil_div(n, kTile);
-    j = begin > at + kStart ? (int)(begin - at - kStart) : 0;
-    j1 = end > at + kStart ? min(nt, (int)(end - at - kStart)) : 0;
-  }
-  __device__ __forceinline__ void next(const Params& p, uint32_t begin, uint32_t end) {
-    at += kStart + nt;
-    if (++u == p.Hkv * p.blocks) {
-      u = 0;
-      ++b;
-    }
-    if (at < end) enter(p, begin, end);
-    else j = j1 = 0;
-  }
-};
-
-// N values of a row from element d on, out of the sums o with reference `base`, sums l
-// and r: joined with other attention, divided, rounded, stored.
-template <int N>
-__device__ __forceinline__ void finish(const Params& p, int b, int h, int r, int d, float base, float l, float r_sum,
-                                       float (&o)[N], bool first) {
-  uint32_t in_head;
-  const int tok = p.by_G(r, &in_head), hq = h * p.G + in_head;
-  const int64_t row = ((int64_t)b * p.c.T + tok) * p.Hkv * p.G + hq;
-  if (p.c.other_out) {
-    const float other = p.c.other_lse[row] * kLog2e;
-    if (!(other == -INFINITY)) {
-      const float to = fmaxf(base, other);
-      const float f = base == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to);
-      const uint16_t* from = static_cast<const uint16_t*>(p.c.other_out) + b * p.c.other_batch + tok * p.c.other_token +
-                             hq * p.c.other_head + d;
-#pragma unroll
-      for (int i = 0; i < N; i += 4)
-        if (d + i < p.D) {
-          const uint2 raw = *reinterpret_cast<const uint2*>(from + i);
-          const float2 lo = to_float(p.bf16, raw.x), hi = to_float(p.bf16, raw.y);
-          o[i] = fmaf(fo, lo.x, f * o[i]), o[i + 1] = fmaf(fo, lo.y, f * o[i + 1]);
-          o[i + 2] = fmaf(fo, hi.x, f * o[i + 2]), o[i + 3] = fmaf(fo, hi.y, f * o[i + 3]);
-        }
-      l = fmaf(l, f, fo);
-      r_sum = fmaf(r_sum, f, fo);
-      base = to;
-    }
-  }
-  const bool empty = l == 0.f;
-  const float inv = empty ? 0.f : 1.f / r_sum;
-  uint16_t* out = static_cast<uint16_t*>(p.c.out) + b * p.c.out_batch + tok * p.c.out_token + hq * p.c.out_head + d;
-  uint32_t w[N / 2];
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) w[i] = empty ? 0u : from_float(p.bf16, o[2 * i] * inv, o[2 * i + 1] * inv);
-  if constexpr (N % 8 == 0) {
-#pragma unroll
-    for (int i = 0; i < N; i += 8)
-      if (d + i < p.D) *reinterpret_cast<uint4*>(out + i) = make_uint4(w[i / 2], w[i / 2 + 1], w[i / 2 + 2], w[i / 2 + 3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4)
-      if (d + i < p.D) *reinterpret_cast<uint2*>(out + i) = make_uint2(w[i / 2], w[i / 2 + 1]);
-  }
-  if (first && p.c.lse) p.c.lse[row] = empty ? -INFINITY : (base + log2f(l)) * kLn2;
-}
-
 template <int DK, int NT>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(const __grid_constant__ Params p) {
   constexpr int KS = DK / 16;              // steps of S's sum, m-tiles of O
   constexpr int RB = kRowBytes<DK>, NS = kStages<DK, NT>;
   constexpr int SB = NT == 1 ? kSubs : 1;  // instructions' entries between two looks at the maximum
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ uint32_t s_scan[kWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * kWarpBytes<DK, NT>;
   uint2* s_q = reinterpret_cast<uint2*>(ring + NS * kStageBytes<DK>);            // [NT][KS][32]
   pdl_launch_dependents();
   pdl_wait();
 
-  // Where the warp's part of the line begins (the costs before each sequence lie in
-  // the rings for that).
-  Cursor cur;
   const int me = blockIdx.x * kWarps + warp;
-  uint32_t* before = reinterpret_cast<uint32_t*>(smem);
-  {
-    const uint32_t per_seq = p.Hkv * p.blocks, per = (p.c.B + kThreads - 1) / kThreads;
-    uint32_t sum = 0;
-    for (uint32_t i = 0; i < per; ++i) {
-      const int b = tid * per + i;
-      if (b < p.c.B) sum += per_seq * (kStart + ceil_div(used(p, b), kTile));
-    }
-    uint32_t up = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const uint32_t x = __shfl_up_sync(0xffffffffu, up, d);
-      if (lane >= d) up += x;
-    }
-    if (lane == 31) s_scan[warp] = up;
-    __syncthreads();
-    uint32_t x = up - sum;
-    for (int w = 0; w < warp; ++w) x += s_scan[w];
-    for (uint32_t i = 0; i < per; ++i) {
-      const int b = tid * per + i;
-      if (b < p.c.B) {
-        before[b] = x;
-        x += per_seq * (kStart + ceil_div(used(p, b), kTile));
-        if (b == p.c.B - 1) before[p.c.B] = x;
-      }
-    }
-    __syncthreads();
-  }
-  const Line line(before[p.c.B], gridDim.x * kWarps);
-  const uint32_t begin = line.first(min((uint32_t)me, line.warps)), end = line.first(min((uint32_t)me + 1, line.warps));
-  {
-    int lo = 0;
-    for (int hi = p.c.B; hi - lo > 1;) {
-      const int mid = (lo + hi) >> 1;
-      if (before[mid] <= begin) lo = mid; else hi = mid;
-    }
-    cur.b = lo;
-    const uint32_t start = before[lo], cost = kStart + ceil_div(used(p, lo), kTile);
-    cur.u = (int)((begin - start) / cost);
-    cur.at = start + cur.u * cost;
-  }
+  const Start<kTile> start = start_of<kTile>(p, reinterpret_cast<uint32_t*>(smem), me, gridDim.x * kWarps);
+  const Line line = start.line;
+  const uint32_t begin = start.begin, end = start.end;
   __syncthreads();
   if (begin >= end) return;
-  cur.enter(p, begin, end);
+  Cursor<kTile> cur = start.cur;
 
   // ---- tiles on their way ---------------------------------------------------------
   const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
   const int nbytes = p.D / 2, groups = p.D / 16;
-  Cursor f = cur;                          // of the tile to be fetched
+  Cursor<kTile> f = cur;                          // of the tile to be fetched
   // A lane copies 16 bytes of every kCopyRows-th entry of a tile, from copy_row on.
   // Scales: lane l has those of entry l.
   constexpr int C = RB / 16, kCopyRows = 32 / C;
@@ -298,17 +84,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     vp = v4.codes + f.b * v4.batch + h * v4.head + (e + copy_row) * v4.entry + copy_byte;
     ks = k4.scales + f.b * k4.scales_batch + h * k4.scales_head + (e + lane) * k4.scales_entry;
     vs = v4.scales + f.b * v4.scales_batch + h * v4.scales_head + (e + lane) * v4.scales_entry;
-  };
-  const auto row_scales = [&](const uint8_t* from) {
-    uint2 x = make_uint2(0, 0);
-    if (groups == 8) x = __ldg(reinterpret_cast<const uint2*>(from));
-    else if (groups == 4) x.x = __ldg(reinterpret_cast<const uint32_t*>(from));
-    else
-      for (int i = 0; i < groups; ++i) {
-        const uint32_t y = __ldg(from + i);
-        if (i < 4) x.x |= y << (8 * i); else x.y |= y << (8 * i - 32);
-      }
-    return x;
   };
   uint2 k_scales, v_scales;                // of the tile fetched last
   const auto fetch = [&](int stage) {
@@ -352,8 +127,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
       }
       k_scales = v_scales = make_uint2(0, 0);
       if (lane < left) {
-        k_scales = row_scales(ks);
-        v_scales = row_scales(vs);
+        k_scales = row_scales(ks, groups);
+        v_scales = row_scales(vs, groups);
       }
       if (++f.j < f.j1) {
         kp += kTile * k4.entry;
@@ -393,55 +168,14 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     int far[NT][2];                        // entries that they see
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const int r = i * 8 + g;
-      uint2 raw[KS];
-#pragma unroll
-      for (int j = 0; j < KS; ++j) raw[j] = make_uint2(0, 0);
-      if (r < rows) {
-        uint32_t in_head;
-        const int tok = p.by_G(row0 + r, &in_head);
-        const uint16_t* from = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token +
-                               (int64_t)(h * p.G + in_head) * p.c.q_head + t * (DK / 4);
-#pragma unroll
-        for (int j = 0; j < KS; ++j)
-          if (t * (DK / 4) + 4 * j < p.D) raw[j] = __ldg(reinterpret_cast<const uint2*>(from + 4 * j));
-      }
-      int e = 0;
-      if (p.bf16) {
-        // 2^e that brings the largest that is finite to 2^14 .. 2^15
-        const auto largest = [&](uint32_t keep) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int j = 0; j < KS; ++j) {
-            const uint32_t x = raw[j].x & 0x7fff7fffu, y = raw[j].y & 0x7fff7fffu;
-            if (keep) {
-              top = __vmaxu2(top, __vmaxu2(x, y));
-            } else {
-              top = __vmaxu2(top, x & ~__vcmpgeu2(x, 0x7f807f80u));
-              top = __vmaxu2(top, y & ~__vcmpgeu2(y, 0x7f807f80u));
-            }
-          }
-          top = max(top & 0xffffu, top >> 16);
-          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          return max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        };
-        uint32_t top = largest(1);
-        if (__any_sync(0xffffffffu, top >= 0x7f80u)) top = largest(0);
-        e = min(14 - ((int)(top >> 7) - 127), 100);
-      }
-      const float up = __int_as_float((e + 127) << 23);
+      uint2 x[KS];
+      const float down = load_query<DK>(p, b, h, row0 + i * 8 + g, i * 8 + g < rows, t, x);
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        uint2 x = raw[j];
-        if (p.bf16) {
-          const float2 lo = to_float(true, x.x), hi = to_float(true, x.y);
-          x = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
-        }
-        if (NT == 1) q[j] = x;
-        else s_q[(i * KS + j) * 32 + lane] = x;
+        if (NT == 1) q[j] = x[j];
+        else s_q[(i * KS + j) * 32 + lane] = x[j];
       }
-      // (lane 4 r has row r's; not 0, so that masked scores stay -infinity)
-      const float down = fmaxf(p.c2 * __int_as_float((127 - e) << 23), 0x1p-126f);
+      // (lane 4 r has row r's)
 #pragma unroll
       for (int e2 = 0; e2 < 2; ++e2) {
         c2[i][e2] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + e2));
@@ -490,13 +224,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
       {
         uint2* at = reinterpret_cast<uint2*>(place_s + (kTile + lane) * 8);
         const uint2 x = *at;
-        const auto nan = [](uint32_t x) { return ((x & 0x78787878u) + 0x08080808u) & x & 0x80808080u; };
-        const uint32_t bad[2] = {nan(x.x), nan(x.y)};
+        const uint32_t bad[2] = {nan_scales(x.x), nan_scales(x.y)};
         if (__any_sync(0xffffffffu, bad[0] | bad[1])) {
           *at = make_uint2(x.x & ~(bad[0] / 128 * 255), x.y & ~(bad[1] / 128 * 255));
           const int my_far = lane >= rows ? 0 : p.c.causal ? n - (p.c.T - 1 - (int)p.by_G(row0 + lane)) : n;
-          uint32_t mask = 0;
-          for (int i = 0; i < 8; ++i) mask |= (bad[i / 4] >> (8 * (i % 4) + 7) & 1u) << i;
+          const uint32_t mask = groups_of(bad);
           for (int e = 0; e < kTile; ++e) {
             const uint32_t m = __shfl_sync(0xffffffffu, mask, e);
             if (tile * kTile + e < my_far) poison |= m;
@@ -807,7 +539,7 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
 }
 
 // ---- host ---------------------------------------------------------------------
-int n_tiles(int rows) { return (rows + 7) / 8; }
+constexpr int kWarpRows = 16;              // most rows of a unit that a warp takes
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 // (the SMs' shared memory stays divided as attend4_kernel needs it: otherwise some of
@@ -826,40 +558,53 @@ template <int DK, int NT>
 cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   static PerDevice attr;
   constexpr size_t bytes = (size_t)kWarps * kWarpBytes<DK, NT>;
-  cudaError_t e = attr.once(dev, []() {
+  const cudaError_t e = attr.once(dev, []() {
     return cudaFuncSetAttribute(attend4_kernel<DK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   });
   if (e != cudaSuccess) return e;
-  const int grid = sms * ctas_per_sm(NT);
-  e = launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)grid), dim3(kThreads), bytes, s, p);
-  if (e != cudaSuccess) return e;
-  // a warp of its own for every few parts of a unit
-  if ((int64_t)grid * kWarps >= 16 * (int64_t)p.c.B * p.Hkv * p.blocks) return launch_merge<DK, 32>(p, dev, s);
-  return launch_merge<DK, 1>(p, dev, s);
+  return launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)(sms * ctas_per_sm(NT))), dim3(kThreads), bytes, s, p);
+}
+
+// How the R query rows of a K/V head are taken: by warps or by CTAs, in units of as
+// many rows, workers.
+struct Plan {
+  bool by_ctas;
+  int blocks, rows, NT, workers;
+};
+Plan plan_of(int R, int sms) {
+  Plan x;
+  x.by_ctas = R > kWarpRows;
+  x.blocks = ceil_div(R, x.by_ctas ? kRowsMost4 : kWarpRows);
+  x.rows = ceil_div(R, x.blocks);
+  x.NT = ceil_div(x.rows, 8);
+  if (x.by_ctas) x.NT += x.NT & 1;
+  x.workers = x.by_ctas ? rows4_workers(x.NT, sms) : sms * ctas_per_sm(x.NT) * kWarps;
+  return x;
 }
 
 }  // namespace
 
 Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
-  const int R = s.max_T * (s.Hq / s.Hkv);
   const size_t DK = s.D <= 64 ? 64 : 128;
-  Cache4Workspace w;
-  w.slots = round256((size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * row_blocks4(R) * 8);
-  // (most for the most rows of a unit: fewer warps, but by less)
-  size_t most = 0;
-  for (int NT = 1; NT <= n_tiles(min(R, kMaxRows)); ++NT)
-    most = max(most, 2 * (size_t)sms * ctas_per_sm(NT) * kWarps * 8 * NT * (16 + DK * 4));
+  Cache4Workspace w{};
+  size_t units = 0, most = 0;
+  for (int T = 1; T <= s.max_T; ++T) {
+    const Plan x = plan_of(T * (s.Hq / s.Hkv), sms);
+    units = max(units, (size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * x.blocks * 8);
+    most = max(most, 2 * (size_t)x.workers * 8 * x.NT * (16 + DK * 4));
+  }
+  w.slots = round256(units);
   w.bytes = w.slots + most;
   return w;
 }
 
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c) {
-  return (int64_t)c.B * s.Hkv * row_blocks4(c.T * (s.Hq / s.Hkv)) * (kStart + ceil_div(s.capacity, kTile));
+  return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), 1).blocks * (kStart + ceil_div(s.capacity, kTile));
 }
 
-cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, cudaStream_t stream) {
+cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, cudaStream_t stream) {
   int dev = 0, sms = 0;
-  const cudaError_t e = current_device(&dev, &sms);
+  cudaError_t e = current_device(&dev, &sms);
   if (e != cudaSuccess) return e;
   Params p;
   p.c = c;
@@ -868,32 +613,26 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.D = s.D;
   p.capacity = s.capacity;
   p.R = c.T * p.G;
-  p.blocks = row_blocks4(p.R);
-  p.block_rows = ceil_div(p.R, p.blocks);
+  const Plan plan = plan_of(p.R, sms);
+  p.blocks = plan.blocks;
+  p.block_rows = plan.rows;
   p.by_blocks = Divide(p.blocks);
   p.by_G = Divide(p.G);
   p.bf16 = s.dtype == SP_BF16;
   p.c2 = c.scale * kLog2e;
-  const Cache4Workspace w = cache4_workspace(s, sms);
-  const int NT = n_tiles(p.block_rows);
-  p.slot_rows = 8 * NT;
+  p.slot_rows = 8 * plan.NT;
   p.units = reinterpret_cast<int2*>(ws);
-  p.slot_ml = reinterpret_cast<float4*>(ws + w.slots);
-  p.slot_o = reinterpret_cast<float*>(ws + w.slots + 2 * (size_t)sms * ctas_per_sm(NT) * kWarps * p.slot_rows * 16);
-  if (s.D <= 64) {
-    switch (NT) {
-      case 1: return launch_t<64, 1>(p, dev, sms, stream);
-      case 2: return launch_t<64, 2>(p, dev, sms, stream);
-      case 3: return launch_t<64, 3>(p, dev, sms, stream);
-      default: return launch_t<64, 4>(p, dev, sms, stream);
-    }
-  }
-  switch (NT) {
-    case 1: return launch_t<128, 1>(p, dev, sms, stream);
-    case 2: return launch_t<128, 2>(p, dev, sms, stream);
-    case 3: return launch_t<128, 3>(p, dev, sms, stream);
-    default: return launch_t<128, 4>(p, dev, sms, stream);
-  }
+  p.slot_ml = reinterpret_cast<float4*>(ws + slots);
+  p.slot_o = reinterpret_cast<float*>(ws + slots + 2 * (size_t)plan.workers * p.slot_rows * 16);
+  const bool wide = s.D > 64;
+  e = plan.by_ctas     ? launch_attend4_rows(p, dev, sms, stream)
+      : plan.NT == 1 ? (wide ? launch_t<128, 1>(p, dev, sms, stream) : launch_t<64, 1>(p, dev, sms, stream))
+                     : (wide ? launch_t<128, 2>(p, dev, sms, stream) : launch_t<64, 2>(p, dev, sms, stream));
+  if (e != cudaSuccess) return e;
+  // many warps a row where it has many parts
+  if (plan.workers >= 16 * (int64_t)c.B * s.Hkv * plan.blocks)
+    return wide ? launch_merge<128, 32>(p, dev, stream) : launch_merge<64, 32>(p, dev, stream);
+  return wide ? launch_merge<128, 1>(p, dev, stream) : launch_merge<64, 1>(p, dev, stream);
 }
 
 }  // namespace sp

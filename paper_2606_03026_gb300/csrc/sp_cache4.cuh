@@ -25,14 +25,12 @@ struct Cache4Workspace {
   size_t slots, bytes;                     // parts of units; notes on the units lie before them
 };
 Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms);
-// Query rows of a K/V head: as many units as it takes for 32 rows each at most.
-inline __host__ __device__ int row_blocks4(int R) { return (R + 31) / 32; }
 
 // Tiles of entries that an attend call has at most (its kernels count them in 32 bits).
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c);
 cudaError_t launch_write4(const Cache4Shape& s, const sp_write4& c, cudaStream_t stream);
 cudaError_t launch_read4(const Cache4Shape& s, const sp_read4& c, cudaStream_t stream);
-cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, cudaStream_t stream);
+cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, cudaStream_t stream);
 
 // n / d and n % d for n < 2^31, d < 2^31.
 struct Divide {

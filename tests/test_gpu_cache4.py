@@ -269,9 +269,10 @@ def test_attend_on_other_layouts(layout, D):
     check(*x, run(*x, layout=layout))
 
 
-@pytest.mark.parametrize("G", [1, 5, 8, 9, 16, 17, 24, 25, 32, 33])
-def test_every_number_of_query_heads(G):
-    x = make(13, 2, 1, 2 * G, 2, 128, 260, [260, 31], "bf16")
+@pytest.mark.parametrize("G", [1, 5, 8, 9, 16, 17, 24, 25, 32, 33, 40, 48, 50, 64, 65])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_number_of_query_heads(G, D):
+    x = make(13, 2, 1, 2 * G, 2, D, 260, [260, 31], "bf16")
     check(*x, run(*x))
 
 
