@@ -539,7 +539,6 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
 }
 
 // ---- host ---------------------------------------------------------------------
-constexpr int kWarpRows = 16;              // most rows of a unit that a warp takes
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 // (the SMs' shared memory stays divided as attend4_kernel needs it: otherwise some of
@@ -565,16 +564,17 @@ cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   return launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)(sms * ctas_per_sm(NT))), dim3(kThreads), bytes, s, p);
 }
 
-// How the R query rows of a K/V head are taken: by warps or by CTAs, in units of as
+// How the R query rows of a K/V head are taken: by warps or by CTAs (a warp's
+// registers hold O of 8 rows of 128-wide heads, of 16 of 64-wide ones), in units of as
 // many rows, workers.
 struct Plan {
   bool by_ctas;
   int blocks, rows, NT, workers;
 };
-Plan plan_of(int R, int sms) {
+Plan plan_of(int R, bool wide, int sms) {
   Plan x;
-  x.by_ctas = R > kWarpRows;
-  x.blocks = ceil_div(R, x.by_ctas ? kRowsMost4 : kWarpRows);
+  x.by_ctas = R > (wide ? 8 : 16);
+  x.blocks = x.by_ctas ? ceil_div(R, kRowsMost4) : 1;
   x.rows = ceil_div(R, x.blocks);
   x.NT = ceil_div(x.rows, 8);
   if (x.by_ctas) x.NT += x.NT & 1;
@@ -589,7 +589,7 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
   Cache4Workspace w{};
   size_t units = 0, most = 0;
   for (int T = 1; T <= s.max_T; ++T) {
-    const Plan x = plan_of(T * (s.Hq / s.Hkv), sms);
+    const Plan x = plan_of(T * (s.Hq / s.Hkv), s.D > 64, sms);
     units = max(units, (size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * x.blocks * 8);
     most = max(most, 2 * (size_t)x.workers * 8 * x.NT * (16 + DK * 4));
   }
@@ -599,7 +599,7 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
 }
 
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c) {
-  return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), 1).blocks * (kStart + ceil_div(s.capacity, kTile));
+  return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), s.D > 64, 1).blocks * (kStart + ceil_div(s.capacity, kTile));
 }
 
 cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, cudaStream_t stream) {
@@ -613,7 +613,7 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.D = s.D;
   p.capacity = s.capacity;
   p.R = c.T * p.G;
-  const Plan plan = plan_of(p.R, sms);
+  const Plan plan = plan_of(p.R, s.D > 64, sms);
   p.blocks = plan.blocks;
   p.block_rows = plan.rows;
   p.by_blocks = Divide(p.blocks);
@@ -627,7 +627,7 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   const bool wide = s.D > 64;
   e = plan.by_ctas     ? launch_attend4_rows(p, dev, sms, stream)
       : plan.NT == 1 ? (wide ? launch_t<128, 1>(p, dev, sms, stream) : launch_t<64, 1>(p, dev, sms, stream))
-                     : (wide ? launch_t<128, 2>(p, dev, sms, stream) : launch_t<64, 2>(p, dev, sms, stream));
+                     : launch_t<64, 2>(p, dev, sms, stream);
   if (e != cudaSuccess) return e;
   // many warps a row where it has many parts
   if (plan.workers >= 16 * (int64_t)c.B * s.Hkv * plan.blocks)

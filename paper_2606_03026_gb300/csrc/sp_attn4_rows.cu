@@ -259,20 +259,18 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_rows_kernel
       }
       f32x2 sum[NT];
       const auto make = [&](int i, uint32_t (&pb)[2], f32x2 by, f32x2 nb) {
-        float most = -INFINITY;
         f32x2 y[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const float2 x = halves(fma2(pair(s[i][2 * half], s[i][2 * half + 1]), by, nb));
-          most = fmaxf(most, fmaxf(x.x, x.y));
           const float2 z = make_float2(ex2(x.x), ex2(x.y));
           y[half] = pair(z.x, z.y);
           pb[half] = transpose8(pack_half2(z.x, z.y));
         }
         sum[i] = add2(y[0], y[1]);
-        return most;
+        return fmaxf(halves(sum[i]).x, halves(sum[i]).y);
       };
-      float most = -INFINITY;
+      float most = 0.f;                    // (of two probabilities: none of them above is too large for half precision)
 #pragma unroll
       for (int i = 0; i < NT; i += 2) {
         const float4 r0 = s_row[i][t], r1 = s_row[i + 1][t];
@@ -281,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_rows_kernel
         most = fmaxf(most, make(i + 1, c, pair(r1.x, r1.y), pair(r1.z, r1.w)));
         s_p[(warp * (NT / 2) + i / 2) * 32 + lane] = make_uint4(a[0], a[1], c[0], c[1]);
       }
-      if (__syncthreads_or(most > kLift + kLag)) {
+      if (__syncthreads_or(most > 16384.f)) {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
           const float4 row = s_row[i][t];
@@ -305,7 +303,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_rows_kernel
             const float x = fmaxf(fmaxf(s_top[0][r], s_top[1][r]), fmaxf(s_top[2][r], s_top[3][r])), had = e ? row.w : row.z;
             nb[i][e] = had;
             a[e] = 1.f;
-            if (x + had > kLift + kLag) {
+            if (x + had > kLift + kLag - 1.f) {
               nb[i][e] = kLift - x;
               a[e] = ex2(nb[i][e] - had);  // 0 at the first
             }
