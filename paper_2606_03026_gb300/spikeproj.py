@@ -639,6 +639,17 @@ _pack_attend, _pack_evict, _pack_verify = map(_packer, (SpAttend, SpEvict, SpVer
 _pack_write4, _pack_read4, _pack_attend4 = map(_packer, (SpWrite4, SpRead4, SpAttend4))
 
 
+def _not_held(x, name, codes, scales, device):
+    """Says what is wrong with a pair of tensors that is not a cache held in 4 bits."""
+    if x is None:
+        raise ValueError(f"{name}: missing")
+    for i, shape in enumerate((codes, scales)):
+        if x[i] is None:
+            raise ValueError(f"{name}[{i}]: missing")
+        import torch
+        _reject(x[i], f"{name}[{i}]", shape, torch.uint8, device)
+
+
 def _reject(x, name, shape, dtype, device):
     """Says what is wrong with a tensor that a call does not take as it is."""
     if x.shape != shape:
@@ -779,6 +790,7 @@ class Cache4:
         self.Hq, self.Hkv, self.D, self.capacity, self.max_T = Hq, Hkv, D, capacity, max_T
         self.dtype = {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype]
         self._f32, self._i32, self._u8 = torch.float32, torch.int32, torch.uint8
+        self._shapes = {}                                      # of the caches of a batch, by its size
         self._scale = D ** -0.5
         self.handle = spike_proj_cache4_create(max_T, Hq, Hkv, D, capacity, dtype, stream)
         self._device = torch.cuda.current_device()             # the handle's
@@ -789,15 +801,29 @@ class Cache4:
         return tuple(tuple(torch.zeros(batch, self.Hkv, self.capacity, self.D // x, dtype=torch.uint8,
                                        device=f"cuda:{self._device}").transpose(1, 2) for x in (2, 16)) for _ in range(2))
 
-    def _held(self, x, name, B):
-        """One of k4 and v4 as the fields of a struct sp_kv4."""
-        if x is None:
-            raise ValueError(f"{name}: missing")
-        codes, scales = x
-        own, u8, dev = (B, self.capacity, self.Hkv), self._u8, self._device
-        cs = _want(codes, name + "[0]", own + (self.D // 2,), u8, dev)
-        ss = _want(scales, name + "[1]", own + (self.D // 16,), u8, dev)
-        return codes.data_ptr(), cs[0], cs[1], cs[2], scales.data_ptr(), ss[0], ss[1], ss[2]
+    def _held(self, k4, v4, B):
+        """k4 and v4 as the fields of two structs sp_kv4.  (The checks of _want, for
+        four tensors in one place: these calls are short, and half of a call's time
+        on the host is the reading of its tensors' attributes.)"""
+        codes, scales = self._shapes.get(B) or self._shapes.setdefault(
+            B, ((B, self.capacity, self.Hkv, self.D // 2), (B, self.capacity, self.Hkv, self.D // 16)))
+        u8, dev = self._u8, self._device
+        if k4 is None or v4 is None:
+            _not_held(k4, "k4", codes, scales, dev)
+            _not_held(v4, "v4", codes, scales, dev)
+        (kc, ks), (vc, vs) = k4, v4
+        if kc is None or ks is None or vc is None or vs is None:
+            _not_held(k4, "k4", codes, scales, dev)
+            _not_held(v4, "v4", codes, scales, dev)
+        a, b, c, d = kc.stride(), ks.stride(), vc.stride(), vs.stride()
+        if (kc.shape != codes or kc.dtype is not u8 or kc.get_device() != dev or a[3] != 1
+                or ks.shape != scales or ks.dtype is not u8 or ks.get_device() != dev or b[3] != 1):
+            _not_held(k4, "k4", codes, scales, dev)
+        if (vc.shape != codes or vc.dtype is not u8 or vc.get_device() != dev or c[3] != 1
+                or vs.shape != scales or vs.dtype is not u8 or vs.get_device() != dev or d[3] != 1):
+            _not_held(v4, "v4", codes, scales, dev)
+        return (kc.data_ptr(), a[0], a[1], a[2], ks.data_ptr(), b[0], b[1], b[2],
+                vc.data_ptr(), c[0], c[1], c[2], vs.data_ptr(), d[0], d[1], d[2])
 
     def _each(self, x, name, B):
         if x is None:
@@ -822,7 +848,7 @@ class Cache4:
             kos, vos = _want(k_out, "k_out", rows, t, dev), _want(v_out, "v_out", rows, t, dev)
             ka, va = k_out.data_ptr(), v_out.data_ptr()
         call = _pack_write4(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                            *self._held(k4, "k4", B), *self._held(v4, "v4", B), self._each(at, "at", B),
+                            *self._held(k4, v4, B), self._each(at, "at", B),
                             self._each(n, "n", B), ka, va, kos[0], kos[1], kos[2], vos[0], vos[1], vos[2], B, T)
         _check(lib().spike_proj_cache4_write(self.handle, call, _stream(stream)), "spike_proj_cache4_write")
 
@@ -835,7 +861,7 @@ class Cache4:
         B, T = k_out.shape[0], k_out.shape[1]
         rows = (B, T, self.Hkv, self.D)
         kos, vos = _want(k_out, "k_out", rows, t, dev), _want(v_out, "v_out", rows, t, dev)
-        call = _pack_read4(*self._held(k4, "k4", B), *self._held(v4, "v4", B), self._each(at, "at", B),
+        call = _pack_read4(*self._held(k4, v4, B), self._each(at, "at", B),
                            self._each(n, "n", B), k_out.data_ptr(), v_out.data_ptr(), kos[0], kos[1], kos[2],
                            vos[0], vos[1], vos[2], B, T)
         _check(lib().spike_proj_cache4_read(self.handle, call, _stream(stream)), "spike_proj_cache4_read")
@@ -862,7 +888,7 @@ class Cache4:
         if other_out is not None:
             oos, oa = _want(other_out, "other_out", rows, t, dev), other_out.data_ptr()
             ola = self._sums(other_lse, "other_lse", rows)
-        call = _pack_attend4(q.data_ptr(), qs[0], qs[1], qs[2], *self._held(k4, "k4", B), *self._held(v4, "v4", B),
+        call = _pack_attend4(q.data_ptr(), qs[0], qs[1], qs[2], *self._held(k4, v4, B),
                              lens.data_ptr(), out.data_ptr(), os[0], os[1], os[2], la, oa, oos[0], oos[1], oos[2], ola,
                              B, T, 1 if causal else 0, self._scale if scale is None else scale)
         _check(lib().spike_proj_cache4_attend(self.handle, call, _stream(stream)), "spike_proj_cache4_attend")
