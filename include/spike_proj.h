@@ -765,6 +765,11 @@ sp_status spike_proj_cache4_create(sp_cache4_t *cache, int32_t max_T, int32_t Hq
                                    int32_t dtype, sp_stream_t stream);
 sp_status spike_proj_cache4_destroy(sp_cache4_t cache);
 
+/* Synchronises the stream and returns SP_EKERNEL, once, when a kernel of the
+ * handle gave up on a wait since the last call (attend calls of many query rows
+ * wait; others do not). */
+sp_status spike_proj_cache4_status(sp_cache4_t cache, sp_stream_t stream);
+
 /* spike_proj_cache4_write: token t < n[b] of sequence b goes to slot at[b] + t of its
  * cache, where that is in 0 .. capacity - 1 (what is not there is dropped; no other
  * slot is written).
@@ -900,8 +905,11 @@ sp_status spike_proj_cache4_attend(sp_cache4_t cache, const sp_attend4 *call,
  *                   copies and frees its tensor memory, and what the call
  *                   leaves in out, lse and weights is not to be used.  (The
  *                   only fault of a cache; its evict calls do not wait.)
+ *                   A 4-bit cache's next attend call, where its query rows of a
+ *                   K/V head are more than 16: the first keys that each CTA
+ *                   decodes are not handed over, with the same consequences.
  * No fault traps, faults the GPU or spins without bound.  spike_proj_plan_status
- * / spike_proj_group_status / spike_proj_cache_status then return SP_EKERNEL,
+ * / spike_proj_group_status / spike_proj_cache_status (cache4) then return SP_EKERNEL,
  * clear the error word and (the first two) re-zero the workspace, and the next
  * call is exact again.
  * Errors: SP_EINVAL (NULL, unknown fault).
@@ -914,6 +922,7 @@ typedef enum sp_fault {
 sp_status spike_proj_plan_inject_fault(sp_plan_t plan, int32_t fault);
 sp_status spike_proj_group_inject_fault(sp_group_t group, int32_t fault);
 sp_status spike_proj_cache_inject_fault(sp_cache_t cache, int32_t fault);
+sp_status spike_proj_cache4_inject_fault(sp_cache4_t cache, int32_t fault);
 
 /* ---------------------------------------------------------------------------
  * spike_proj_probe_gather -- MEASUREMENT AID, not part of the method (the

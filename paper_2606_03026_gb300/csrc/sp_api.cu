@@ -95,6 +95,8 @@ struct sp_cache4_s {
   Cache4Shape shape;
   Cache4Workspace parts;
   uint8_t* ws = nullptr;          // parts.bytes
+  int* err = nullptr;             // device error word
+  int32_t fault = SP_FAULT_NONE;  // armed for the next attend call
 };
 
 struct sp_group_s {
@@ -166,6 +168,17 @@ sp_status on_device(int device) {
   int dev = 0;
   SP_CUDA(cudaGetDevice(&dev));
   return dev == device ? SP_OK : SP_EDEVICE;
+}
+
+// Whether a cache's kernel has raised its error word, which is cleared.
+sp_status take_error(int* word, cudaStream_t s) {
+  int err = 0;
+  SP_CUDA(cudaMemcpyAsync(&err, word, sizeof(err), cudaMemcpyDeviceToHost, s));
+  SP_CUDA(cudaStreamSynchronize(s));
+  if (err == 0) return SP_OK;
+  SP_CUDA(cudaMemsetAsync(word, 0, sizeof(err), s));
+  SP_CUDA(cudaStreamSynchronize(s));
+  return SP_EKERNEL;
 }
 
 // A 4-bit cache of keys or values.
@@ -1086,6 +1099,12 @@ sp_status spike_proj_cache_inject_fault(sp_cache_t cache, int32_t fault) {
   return SP_OK;
 }
 
+sp_status spike_proj_cache4_inject_fault(sp_cache4_t cache, int32_t fault) {
+  if (!cache || (fault != SP_FAULT_NONE && fault != SP_FAULT_STALL)) return SP_EINVAL;
+  cache->fault = fault;
+  return SP_OK;
+}
+
 sp_status spike_proj_probe_gather(const void* base, const uint32_t* offsets16, int32_t count,
                                   int32_t piece_bytes, uint32_t* sink, sp_stream_t stream) {
   if (!base || !sink || count < 0 || (count > 0 && !offsets16)) return SP_EINVAL;
@@ -1259,14 +1278,7 @@ sp_status spike_proj_cache_destroy(sp_cache_t cache) {
 
 sp_status spike_proj_cache_status(sp_cache_t cache, sp_stream_t stream) {
   if (!cache) return SP_EINVAL;
-  cudaStream_t s = as_stream(stream);
-  int err = 0;
-  SP_CUDA(cudaMemcpyAsync(&err, cache->err, sizeof(err), cudaMemcpyDeviceToHost, s));
-  SP_CUDA(cudaStreamSynchronize(s));
-  if (err == 0) return SP_OK;
-  SP_CUDA(cudaMemsetAsync(cache->err, 0, sizeof(err), s));
-  SP_CUDA(cudaStreamSynchronize(s));
-  return SP_EKERNEL;
+  return take_error(cache->err, as_stream(stream));
 }
 
 sp_status spike_proj_cache_attend(sp_cache_t cache, const sp_attend* c, sp_stream_t stream) {
@@ -1340,10 +1352,12 @@ sp_status spike_proj_cache4_create(sp_cache4_t* cache, int32_t max_T, int32_t Hq
   cudaStream_t s = as_stream(stream);
   ca->parts = cache4_workspace(ca->shape, sms);
   st = dev_alloc_zero(&ca->ws, ca->parts.bytes, s);
+  if (st == SP_OK) st = dev_alloc_zero(&ca->err, 1, s);
   cudaError_t e;
   if (st == SP_OK && (e = cudaStreamSynchronize(s)) != cudaSuccess) st = cuda_fail(e);
   if (st != SP_OK) {
     cudaFree(ca->ws);
+    cudaFree(ca->err);
     delete ca;
     return st;
   }
@@ -1355,8 +1369,14 @@ sp_status spike_proj_cache4_destroy(sp_cache4_t cache) {
   if (!cache) return SP_OK;
   cudaError_t e = cudaDeviceSynchronize();
   cudaFree(cache->ws);
+  cudaFree(cache->err);
   delete cache;
   return e == cudaSuccess ? SP_OK : cuda_fail(e);
+}
+
+sp_status spike_proj_cache4_status(sp_cache4_t cache, sp_stream_t stream) {
+  if (!cache) return SP_EINVAL;
+  return take_error(cache->err, as_stream(stream));
 }
 
 sp_status spike_proj_cache4_write(sp_cache4_t cache, const sp_write4* c, sp_stream_t stream) {
@@ -1426,7 +1446,8 @@ sp_status spike_proj_cache4_attend(sp_cache4_t cache, const sp_attend4* c, sp_st
     return SP_EALIGN;
   const sp_status st = on_device(cache->device);
   if (st != SP_OK) return st;
-  SP_CUDA(launch_attend4(sh, *c, cache->ws, cache->parts.slots, as_stream(stream)));
+  SP_CUDA(launch_attend4(sh, *c, cache->ws, cache->parts.slots, cache->err,
+                         std::exchange(cache->fault, SP_FAULT_NONE), as_stream(stream)));
   return SP_OK;
 }
 

@@ -290,16 +290,6 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// An operand whose rows run along the MMA's N: 64 elements (128 bytes,
-// swizzled) per row of K, 8 rows of K 1024 bytes apart, the next 64 elements
-// of N `block` bytes on.
-__device__ __forceinline__ uint64_t n_major_desc(const void* p, uint32_t block) {
-  uint64_t d = smem_desc(p, 1024, kSwizzle128);
-  d &= ~((uint64_t)0x3FFF << 16);
-  return d | (uint64_t)(block >> 4) << 16;
-}
 
 // Bounded wait, inline (a call would cost the softmax's loop its registers);
 // false too when another warp of the CTA has given up (`stop`, where given).

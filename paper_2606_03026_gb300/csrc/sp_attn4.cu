@@ -33,6 +33,7 @@ namespace {
 
 using Params = Attend4Params;
 constexpr int kTile = 32, kSubs = kTile / 16;   // entries of a tile, instructions that they are the rows of
+constexpr int kStart = 2;                  // cost of a unit beside its tiles
 
 // CTAs of an SM, by the registers that NT x 8 rows take.
 constexpr int ctas_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
@@ -58,17 +59,17 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
   pdl_wait();
 
   const int me = blockIdx.x * kWarps + warp;
-  const Start<kTile> start = start_of<kTile>(p, reinterpret_cast<uint32_t*>(smem), me, gridDim.x * kWarps);
+  const Start<kTile, kStart> start = start_of<kTile, kStart, kThreads>(p, reinterpret_cast<uint32_t*>(smem), me, gridDim.x * kWarps);
   const Line line = start.line;
   const uint32_t begin = start.begin, end = start.end;
   __syncthreads();
   if (begin >= end) return;
-  Cursor<kTile> cur = start.cur;
+  Cursor<kTile, kStart> cur = start.cur;
 
   // ---- tiles on their way ---------------------------------------------------------
   const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
   const int nbytes = p.D / 2, groups = p.D / 16;
-  Cursor<kTile> f = cur;                          // of the tile to be fetched
+  Cursor<kTile, kStart> f = cur;                          // of the tile to be fetched
   // A lane copies 16 bytes of every kCopyRows-th entry of a tile, from copy_row on.
   // Scales: lane l has those of entry l.
   constexpr int C = RB / 16, kCopyRows = 32 / C;
@@ -577,8 +578,7 @@ Plan plan_of(int R, bool wide, int sms) {
   x.blocks = x.by_ctas ? ceil_div(R, kRowsMost4) : 1;
   x.rows = ceil_div(R, x.blocks);
   x.NT = ceil_div(x.rows, 8);
-  if (x.by_ctas) x.NT += x.NT & 1;
-  x.workers = x.by_ctas ? rows4_workers(x.NT, sms) : sms * ctas_per_sm(x.NT) * kWarps;
+  x.workers = x.by_ctas ? rows4_workers(sms) : sms * ctas_per_sm(x.NT) * kWarps;
   return x;
 }
 
@@ -602,7 +602,8 @@ int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c) {
   return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), s.D > 64, 1).blocks * (kStart + ceil_div(s.capacity, kTile));
 }
 
-cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, cudaStream_t stream) {
+cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, int* err, int fault,
+                           cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = current_device(&dev, &sms);
   if (e != cudaSuccess) return e;
@@ -620,6 +621,9 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.by_G = Divide(p.G);
   p.bf16 = s.dtype == SP_BF16;
   p.c2 = c.scale * kLog2e;
+  p.err = err;
+  p.fault = fault;
+  p.limit = fault == kFaultStall ? kStallWaitCycles : kWaitLimitCycles;
   p.slot_rows = 8 * plan.NT;
   p.units = reinterpret_cast<int2*>(ws);
   p.slot_ml = reinterpret_cast<float4*>(ws + slots);

@@ -20,14 +20,17 @@ struct Attend4Params {
   int32_t slot_rows;                       // rows of a slot
   int32_t bf16;
   float c2;                                // scale * log2 e
+  int* err;
+  int fault;                               // kFaultStall: the first keys are never there (tests of the error path)
+  long long limit;                         // cycles that a wait takes at most
   int2* units;                             // [B][Hkv][blocks]: slot of the first part (-1: whole), worker of the last
   float4* slot_ml;                         // [2 workers][slot_rows]: reference, sum, sum of the rounded
   float* slot_o;                           // [2 workers][slot_rows][DK]
 };
 
 // Units of more rows than one warp takes, a CTA each (sp_attn4_rows.cu).
-constexpr int kRowsMost4 = 64;
-int rows4_workers(int NT, int sms);
+constexpr int kRowsMost4 = 96;
+int rows4_workers(int sms);
 cudaError_t launch_attend4_rows(const Attend4Params& p, int dev, int sms, cudaStream_t s);
 
 namespace {
@@ -38,7 +41,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // grown by more than 2^kLag; it lies kLift below, so that half precision's
 // subnormals are 2^-34 of the largest probability.
 constexpr float kLag = 4.f, kLift = 10.f;
-constexpr int kStart = 2;                  // cost of a unit beside its tiles
 constexpr int kLeast = 4;                  // cost that is worth a worker
 constexpr uint32_t kOnes = 0x3c003c00u;
 template <int DK> constexpr int kRowBytes = DK / 2;
@@ -67,8 +69,10 @@ template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t to, const uint8_t* from) {
   if constexpr (BYTES == 16)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-  else
+  else if constexpr (BYTES == 8)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -118,21 +122,21 @@ struct Line {
 __device__ __forceinline__ int used(const Attend4Params& p, int b) { return min(max(__ldg(p.c.lens + b), 0), p.capacity); }
 
 // A worker's (a warp, or a CTA) way along the line: unit (b, u), its entries, its tiles j .. j1 of the
-// worker's.  A unit takes kStart + nt on the line from `at` on; tile j is at + kStart + j,
+// worker's.  A unit takes START + nt on the line from `at` on; tile j is at + START + j,
 // and belongs to the worker whose part of the line that is in (a unit without tiles to
 // the one that `at` is in).
-template <int TILE>
+template <int TILE, int START>
 struct Cursor {
   int b, u, n, nt, j, j1;
   uint32_t at;
   __device__ __forceinline__ void enter(const Attend4Params& p, uint32_t begin, uint32_t end) {
     n = used(p, b);
     nt = ceil_div(n, TILE);
-    j = begin > at + kStart ? (int)(begin - at - kStart) : 0;
-    j1 = end > at + kStart ? min(nt, (int)(end - at - kStart)) : 0;
+    j = begin > at + START ? (int)(begin - at - START) : 0;
+    j1 = end > at + START ? min(nt, (int)(end - at - START)) : 0;
   }
   __device__ __forceinline__ void next(const Attend4Params& p, uint32_t begin, uint32_t end) {
-    at += kStart + nt;
+    at += START + nt;
     if (++u == p.Hkv * p.blocks) {
       u = 0;
       ++b;
@@ -145,21 +149,21 @@ struct Cursor {
 // Where worker `me` of at most `most` begins; all threads of a CTA take part.  before:
 // room in shared memory for SPIKE_PROJ_CACHE_MAX_B + 1 words, which may be used for
 // something else behind the caller's next barrier.
-template <int TILE>
+template <int TILE, int START>
 struct Start {
   Line line;
   uint32_t begin, end;
-  Cursor<TILE> cur;
+  Cursor<TILE, START> cur;
 };
-template <int TILE>
-__device__ __forceinline__ Start<TILE> start_of(const Attend4Params& p, uint32_t* before, int me, uint32_t most) {
-  __shared__ uint32_t s_scan[kWarps];
+template <int TILE, int START, int THREADS>
+__device__ __forceinline__ Start<TILE, START> start_of(const Attend4Params& p, uint32_t* before, int me, uint32_t most) {
+  __shared__ uint32_t s_scan[THREADS / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t per_seq = p.Hkv * p.blocks, per = (p.c.B + kThreads - 1) / kThreads;
+  const uint32_t per_seq = p.Hkv * p.blocks, per = (p.c.B + THREADS - 1) / THREADS;
   uint32_t sum = 0;
   for (uint32_t i = 0; i < per; ++i) {
     const int b = tid * per + i;
-    if (b < p.c.B) sum += per_seq * (kStart + ceil_div(used(p, b), TILE));
+    if (b < p.c.B) sum += per_seq * (START + ceil_div(used(p, b), TILE));
   }
   uint32_t up = sum;
 #pragma unroll
@@ -175,12 +179,12 @@ __device__ __forceinline__ Start<TILE> start_of(const Attend4Params& p, uint32_t
     const int b = tid * per + i;
     if (b < p.c.B) {
       before[b] = x;
-      x += per_seq * (kStart + ceil_div(used(p, b), TILE));
+      x += per_seq * (START + ceil_div(used(p, b), TILE));
       if (b == p.c.B - 1) before[p.c.B] = x;
     }
   }
   __syncthreads();
-  Start<TILE> s;
+  Start<TILE, START> s;
   s.line = Line(before[p.c.B], most);
   s.begin = s.line.first(min((uint32_t)me, s.line.workers));
   s.end = s.line.first(min((uint32_t)me + 1, s.line.workers));
@@ -189,7 +193,7 @@ __device__ __forceinline__ Start<TILE> start_of(const Attend4Params& p, uint32_t
     const int mid = (lo + hi) >> 1;
     if (before[mid] <= s.begin) lo = mid; else hi = mid;
   }
-  const uint32_t start = before[lo], cost = kStart + ceil_div(used(p, lo), TILE);
+  const uint32_t start = before[lo], cost = START + ceil_div(used(p, lo), TILE);
   s.cur.b = lo;
   s.cur.u = (int)((s.begin - start) / cost);
   s.cur.at = start + s.cur.u * cost;

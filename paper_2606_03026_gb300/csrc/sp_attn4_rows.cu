@@ -1,481 +1,508 @@
 // sp_attn4_rows.cu -- attention over a cache held in 4 bits for units of many query
-// rows (see sp_attn4.cu for the operands and for the line that the work is on): what
-// codes cost to be made half precision is shared by up to 64 rows, so the four warps
-// of a CTA work on one unit together, in tiles of 64 entries.
+// rows (see sp_attn4.cu for the form of the cache, and for the line that the work is
+// on).  What codes cost to be made half precision is shared by up to 96 rows, and the
+// products are tcgen05's (M = 128, query rows are the lanes of tensor memory).
 //
-//   S^T = K Q^T   warp w: entries 16 w .. 16 w + 15, all rows
-//   P^T           from each warp's registers through shared memory to all warps
-//   O^T = V^T P^T warp w: the w-th quarter of the elements, all entries
-//
-// so that no code is decoded twice, and a warp holds O of a quarter of the elements
-// only.  The reference of a row's exponentials is the CTA's; it is looked at after
-// the probabilities are made, at the barrier that hands them over, and they are made
-// again in the few tiles where it has to change.
+// A CTA (256 threads, two per SM) walks its tiles of 64 entries:
+//   warps 4-7   decode, two the keys and two the values: a thread makes an entry half
+//               precision, into rings in shared memory; the codes of the next two tiles
+//               are on their way meanwhile (cp.async, each warp its own)
+//   warps 0-2   the softmax, thread = row: per tile they read the 64 scores of their
+//               row, keep the running maximum and sums, and put the probabilities,
+//               rounded to half precision, back over the scores; at the end of a
+//               unit's tiles they read O.  At its beginning they make its queries.
+//   warp 3      S = Q K^T one tile ahead of O += P V (P from tensor memory, V as an
+//               N-major operand)
+// (96 rows, not the 128 of the MMA, so that 8 warps do, with 128 registers a thread:
+// with a ninth and 96 the loops spilled and a tile took twice as long.)
+// A row's queries are times a power of two, and its scores are masked, by its thread.
 #include "sp_attn4.cuh"
 
 namespace sp {
 namespace {
 
 using Params = Attend4Params;
-constexpr int kTile = 64;
-constexpr float kNone = 1.7e38f;           // negative reference of a row without a score yet: any score is above it
+constexpr int kTile = 64, kUnitStart = 6;
+constexpr int kRows = 128, kRowWarps = kRowsMost4 / 32;        // of the MMA; warps that query rows are the lanes of
+constexpr int kRowThreads = 256;
+constexpr int kRing = 2;                   // tiles of K in half precision
+template <int DK> constexpr int kRingV = DK == 128 ? 1 : 2;    // and of V: what there is room for
+constexpr int kRaw = 3;                    // tiles of codes and scales, as they are held
+constexpr int kTmemCols = 256;             // S and P: 0 .. 63 and 64 .. 127, O from 128 on
+constexpr uint32_t kTmemO = 128;
+constexpr int kQBlock = kRows * 128;       // 64 elements of 128 rows
+constexpr int kBlock = kTile * 128;        // 64 elements of a tile's entries
+template <int DK> constexpr int kQBytes = DK / 64 * kQBlock;
+template <int DK> constexpr int kTileBytes = DK / 64 * kBlock;
+template <int DK> constexpr int kRawBytes = 32 * (kRowBytes<DK> + 8);   // of a warp: 32 entries
+template <int DK> constexpr int kSmem = 1024 + kQBytes<DK> + (kRing + kRingV<DK>) * kTileBytes<DK> + 4 * kRaw * kRawBytes<DK>;
+static_assert(2 * (kSmem<128> + 4 * 1024) <= 228 * 1024, "two CTAs per SM");
+static_assert(kRing * kTileBytes<64> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
-constexpr int ctas_per_sm(int NT) { return NT <= 4 ? 4 : 3; }
-template <int DK> constexpr int kStageBytes = 2 * kTile * kRowBytes<DK> + 2 * kTile * 8;
-constexpr int kStages = 3;
-template <int DK, int NT> constexpr int kQueryBytes = NT * (DK / 32) * 32 * 16;
-template <int NT> constexpr int kProbBytes = kWarps * (NT / 2) * 32 * 16;
-template <int DK, int NT> constexpr int kSmem = kStages * kStageBytes<DK> + kQueryBytes<DK, NT> + kProbBytes<NT>;
-static_assert(3 * (kSmem<128, 8> + 5 * 1024) <= 228 * 1024 && 4 * (kSmem<128, 4> + 3 * 1024) <= 228 * 1024, "shared memory of an SM");
-static_assert(kSmem<64, 2> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
+// Bounded wait; false too when another warp of the CTA has given up.
+__device__ __forceinline__ bool wait(const Params& p, uint64_t* bar, uint32_t parity, const volatile int* stop) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  do {
+    if (mbar_try_wait(bar, parity)) return true;
+  } while (!*stop && clock64() - t0 < p.limit);
+  return false;
+}
+__device__ __forceinline__ bool all(bool x) { return __all_sync(0xffffffffu, x) != 0; }
+// a += the lower half of x, b += the upper one.
+__device__ __forceinline__ void add_halves(uint32_t x, float& a, float& b) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %0;\n\tadd.rn.f32.f16 %1, h, %1;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "r"(x));
+}
 
-template <int DK, int NT>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_rows_kernel(const __grid_constant__ Params p) {
-  constexpr int KS = DK / 16, RB = kRowBytes<DK>, NS = kStages;
-  constexpr int MT = DK / 64;              // m-tiles of O of a warp
-  constexpr int OWN = (NT + 3) / 4;        // n-tiles whose rounded probabilities a warp adds up: warp, warp + 4
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float4 s_row[NT][4];          // rows 2t, 2t + 1 of n-tile i: factors of scores, negative references
-  __shared__ int2 s_far[NT][4];            // entries that they see
-  __shared__ float s_top[kWarps][8 * NT], s_sum[8 * NT];       // (tops of a tile, sums of a unit)
-  __shared__ uint32_t s_poison[8 * NT];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  uint4* s_q = reinterpret_cast<uint4*>(smem + NS * kStageBytes<DK>);            // [NT][KS / 2][32]
-  uint4* s_p = reinterpret_cast<uint4*>(smem + NS * kStageBytes<DK> + kQueryBytes<DK, NT>);      // [4][NT / 2][32]
+struct Bars {
+  uint64_t k_full[kRing], k_empty[kRing], v_full[2], v_empty[2], s_full[2], p_full[2];
+  uint64_t q_full, o_full, o_empty, done;
+};
+
+template <int DK>
+__global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __grid_constant__ Params p) {
+  constexpr uint32_t kIdescS = 1u << 4 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+  constexpr uint32_t kIdescO = 1u << 4 | 1u << 16 | (uint32_t)(DK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+  extern __shared__ uint8_t smem_base[];
+  uint8_t* smem = smem_base + (-smem_u32(smem_base) & 1023u);  // (swizzled operands begin on 1024 bytes)
+  __shared__ Bars bars;
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  // groups of which a row sees a NaN value, by unit (values are decoded up to two
+  // units ahead of the one whose O is read)
+  __shared__ uint32_t s_poison[4][kRows];
+  uint8_t* sQ = smem;
+  uint8_t* sK = sQ + kQBytes<DK>;
+  uint8_t* sV = sK + kRing * kTileBytes<DK>;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars.k_full[i], 2);
+      mbar_init(&bars.k_empty[i], 1);
+      mbar_init(&bars.v_full[i], 2);
+      mbar_init(&bars.v_empty[i], 1);
+      mbar_init(&bars.s_full[i], 1);
+      mbar_init(&bars.p_full[i], kRowWarps);
+    }
+    mbar_init(&bars.q_full, kRowWarps);
+    mbar_init(&bars.o_full, 1);
+    mbar_init(&bars.o_empty, kRowWarps);
+    mbar_init(&bars.done, 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = tid; i < 4 * kRows; i += kRowThreads) s_poison[i / kRows][i % kRows] = 0;
+  if (warp == 0) tmem_alloc(&s_tmem, kTmemCols);
   pdl_launch_dependents();
   pdl_wait();
 
   const int me = blockIdx.x;
-  const Start<kTile> start = start_of<kTile>(p, reinterpret_cast<uint32_t*>(smem), me, gridDim.x);
-  const Line line = start.line;
-  const uint32_t begin = start.begin, end = start.end;
+  tc_fence_before();
+  const Start<kTile, kUnitStart> start =
+      start_of<kTile, kUnitStart, kRowThreads>(p, reinterpret_cast<uint32_t*>(sK), me, gridDim.x);
   __syncthreads();
-  if (begin >= end) return;
-  Cursor<kTile> cur = start.cur;
+  tc_fence_after();
+  const Line line = start.line;
+  const uint32_t begin = start.begin, end = start.end, tmem = s_tmem;
+  Cursor<kTile, kUnitStart> cur = start.cur;
+  const volatile int* stop = &s_abort;
+  bool ok = true;
+  // A unit that the CTA has no tile of: of no concern, but for one without entries,
+  // whose rows warps 0 to 3 write out.
+  const auto skip = [&]() { return cur.j >= cur.j1; };
 
-  // ---- tiles on their way ---------------------------------------------------------
-  const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
-  const int nbytes = p.D / 2, groups = p.D / 16;
-  Cursor<kTile> f = cur;                   // of the tile to be fetched
-  // A thread copies 16 bytes of every kCopyRows-th entry of a tile, from copy_row on.
-  // Scales: thread i has those of key i, i - 64 of its values.
-  constexpr int C = RB / 16, kCopyRows = kThreads / C;
-  const int copy_row = tid / C, copy_byte = tid % C * 16;
-  const uint32_t ring_u32 = smem_u32(smem), copy_to = ring_u32 + place_of<DK>(copy_row, copy_byte);
-  const sp_kv4& scale4 = tid < kTile ? k4 : v4;
-  const uint8_t *kp = nullptr, *vp = nullptr, *sc = nullptr;
-  const auto enter_unit = [&]() {
-    while (f.j >= f.j1 && f.at < end) f.next(p, begin, end);
-    if (f.at >= end) return;
-    const int h = p.by_blocks(f.u);
-    const int64_t e = (int64_t)f.j * kTile;
-    kp = k4.codes + f.b * k4.batch + h * k4.head + (e + copy_row) * k4.entry + copy_byte;
-    vp = v4.codes + f.b * v4.batch + h * v4.head + (e + copy_row) * v4.entry + copy_byte;
-    sc = scale4.scales + f.b * scale4.scales_batch + h * scale4.scales_head + (e + tid % kTile) * scale4.scales_entry;
-  };
-  uint2 scales = make_uint2(0, 0);         // of the tile fetched last
-  const auto fetch = [&](int stage) {
-    if (f.j < f.j1) {
-      const uint32_t to = copy_to + stage * kStageBytes<DK>;
-      const int left = f.n - f.j * kTile;  // entries from the tile's first on
-      if (nbytes % 16 == 0) {
-        const uint8_t *kr = kp, *vr = vp;
-        if (copy_byte < nbytes) {
+  if (warp >= 4) {
+    // ------------------------------ decode ------------------------------------------
+    // Warps 4 and 5 have the keys of a tile's entries 0 .. 31 and 32 .. 63, warps 6 and
+    // 7 the values; thread = entry, but for the copies.
+    constexpr int RB = kRowBytes<DK>, C = RB / 16, kCopyRows = 32 / C;
+    const bool keys = warp < 6;
+    const int e0 = (warp & 1) * 32, e = e0 + lane, nbytes = p.D / 2, groups = p.D / 16;
+    const sp_kv4 held = keys ? p.c.k4 : p.c.v4;
+    const uint32_t raw_u32 = smem_u32(sV + kRingV<DK> * kTileBytes<DK>) + (warp - 4) * (kRaw * kRawBytes<DK>);
+    // 16 bytes of a row: so that neither the copies' rows nor a row's reads meet in a bank
+    const auto raw_at = [&](int row, int chunk) { return row * RB + (chunk ^ (DK == 128 ? row >> 1 & 3 : row >> 2 & 1)) * 16; };
+    const int copy_row = lane / C, copy_byte = lane % C * 16;
+    // f: the tile that is copied, kRaw - 1 before cur, the one that is decoded
+    Cursor<kTile, kUnitStart> f = cur;
+    const uint8_t *code = nullptr, *scale = nullptr;
+    const auto settle = [&](Cursor<kTile, kUnitStart>& c) {    // at a tile, or at the end
+      while (c.at < end && c.j >= c.j1) c.next(p, begin, end);
+    };
+    const auto enter = [&]() {
+      settle(f);
+      if (f.at >= end) return;
+      const int h = p.by_blocks(f.u);
+      const int64_t entry = (int64_t)f.j * kTile + e0;
+      code = held.codes + f.b * held.batch + (entry + copy_row) * held.entry + h * held.head + copy_byte;
+      scale = held.scales + f.b * held.scales_batch + (entry + lane) * held.scales_entry + h * held.scales_head;
+    };
+    uint2 scales = make_uint2(0, 0);       // of the tile copied last
+    const auto fetch = [&](int stage) {    // and on
+      if (f.at < end) {
+        const uint32_t to = raw_u32 + stage * kRawBytes<DK>;
+        const int left = f.n - f.j * kTile - e0;
+        if (nbytes % 16 == 0) {
+          const uint8_t* from = code;
 #pragma unroll
-          for (int i = 0; i < kTile / kCopyRows; ++i) {
-            if (copy_row + i * kCopyRows < left) {
-              copy_async<16>(to + i * kCopyRows * RB, kr);
-              copy_async<16>(to + (kTile + i * kCopyRows) * RB, vr);
-            }
-            kr += kCopyRows * k4.entry;
-            vr += kCopyRows * v4.entry;
+          for (int i = 0; i < 32 / kCopyRows; ++i) {
+            const int row = copy_row + i * kCopyRows;
+            if (row < left && copy_byte < nbytes) copy_async<16>(to + raw_at(row, lane % C), from);
+            from += kCopyRows * held.entry;
           }
-        }
-      } else {
-        constexpr int C8 = RB / 8;
-        const uint8_t* kc = kp - copy_row * k4.entry - copy_byte;
-        const uint8_t* vc = vp - copy_row * v4.entry - copy_byte;
-        const uint32_t to8 = ring_u32 + stage * kStageBytes<DK>;
+        } else {
+          const uint8_t* from = code - copy_row * held.entry - copy_byte;
 #pragma unroll 2
-        for (int i = 0; i < kTile * C8 / kThreads; ++i) {
-          const int e = (i * kThreads + tid) / C8, byte = (i * kThreads + tid) % C8 * 8;
-          if (e < left && byte < nbytes) {
-            copy_async<8>(to8 + place_of<DK>(e, byte), kc + e * k4.entry + byte);
-            copy_async<8>(to8 + kTile * RB + place_of<DK>(e, byte), vc + e * v4.entry + byte);
+          for (int i = 0; i < RB / 8; ++i) {
+            const int row = (i * 32 + lane) / (RB / 8), byte = (i * 32 + lane) % (RB / 8) * 8;
+            if (row < left && byte < nbytes) copy_async<8>(to + raw_at(row, byte >> 4) + (byte & 8), from + row * held.entry + byte);
           }
         }
+        scales = make_uint2(0, 0);
+        if (lane < left) scales = row_scales(scale, groups);
+        code += kTile * held.entry;
+        scale += kTile * held.scales_entry;
+        if (++f.j >= f.j1) enter();
       }
-      scales = make_uint2(0, 0);
-      if (tid % kTile < left) scales = row_scales(sc, groups);
-      if (++f.j < f.j1) {
-        kp += kTile * k4.entry;
-        vp += kTile * v4.entry;
-        sc += kTile * scale4.scales_entry;
-      } else {
-        enter_unit();
+      copy_commit();
+    };
+    const auto store_scales = [&](int stage, uint2 x) {
+      asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(raw_u32 + stage * kRawBytes<DK> + 32 * RB + lane * 8), "r"(x.x), "r"(x.y)
+                   : "memory");
+    };
+    // A thread's entry to its row of a tile, 16 bytes at a time (swizzled as the MMA reads
+    // them).  (Codes of entries that are not there are anything, their scales 0.)
+    const auto decode = [&](int stage, uint2 x, uint8_t* tile) {
+      const uint32_t to = smem_u32(tile) + e * 128 + (e & 7) * 16;
+      uint32_t w[C][4];                    // (all loads before the stores: these are not moved past each other)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[c][0]), "=r"(w[c][1]), "=r"(w[c][2]), "=r"(w[c][3])
+                     : "r"(raw_u32 + stage * kRawBytes<DK> + raw_at(lane, c)));
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const uint32_t of_chunk = c < 2 ? x.x : x.y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t s = scale_half2(of_chunk >> (c % 2 * 16 + i / 2 * 8) & 0xffu);
+          uint32_t h[4];
+          codes_to_half(w[c][i], h);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((to ^ (c % 2 * 4 + i) * 16) + c / 2 * kBlock),
+                       "r"(mul_half2(h[0], s)), "r"(mul_half2(h[1], s)), "r"(mul_half2(h[2], s)), "r"(mul_half2(h[3], s)));
+        }
       }
-    }
-    copy_commit();
-  };
-  const auto store_scales = [&](int stage, uint2 x) {
-    *reinterpret_cast<uint2*>(smem + stage * kStageBytes<DK> + 2 * kTile * RB + tid * 8) = x;
-  };
-  enter_unit();
-  uint2 first_scales[NS - 1];              // (stored when the queries are there)
+    };
+    settle(cur);
+    enter();
+    {
+      uint2 x[kRaw - 1];
 #pragma unroll
-  for (int i = 0; i < NS - 1; ++i) {
-    fetch(i);
-    first_scales[i] = scales;
-  }
-  bool first_unit = true;
-  int stage = 0, ahead = NS - 1;           // places in the ring: of the tile, of the tile to be fetched
-
-  for (; cur.at < end; cur.next(p, begin, end)) {
-    const int b = cur.b, n = cur.n, nt = cur.nt, h = p.by_blocks(cur.u), block = cur.u - h * p.blocks;
-    if (cur.j >= cur.j1 && (nt > 0 || cur.at < begin)) continue;
-    const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0);
-
-    // ---- the query rows ---------------------------------------------------------
-    __syncthreads();                       // (the unit before has left its place)
-    if (tid < 8 * NT) s_poison[tid] = 0;
-    for (int i = warp; i < NT; i += kWarps) {
-      const int r = i * 8 + g;
-      uint2 x[KS];
-      const float down = load_query<DK>(p, b, h, row0 + r, r < rows, t, x);
-#pragma unroll
-      for (int j = 0; j < KS / 2; ++j)
-        s_q[(i * (KS / 2) + j) * 32 + lane] = make_uint4(x[2 * j].x, x[2 * j].y, x[2 * j + 1].x, x[2 * j + 1].y);
-      if (t == 0) {
-        float* row = reinterpret_cast<float*>(&s_row[i][g >> 1]) + (g & 1);
-        row[0] = down;
-        row[2] = kNone;
-        reinterpret_cast<int*>(&s_far[i][g >> 1])[g & 1] = r < rows && p.c.causal ? n - (p.c.T - 1 - (int)p.by_G(row0 + r)) : n;
+      for (int i = 0; i < kRaw - 1; ++i) {
+        fetch(i);
+        x[i] = scales;
       }
+#pragma unroll
+      for (int i = 0; i < kRaw - 2; ++i) store_scales(i, x[i]);
     }
-    if (first_unit) {
-#pragma unroll
-      for (int i = 0; i < NS - 2; ++i) store_scales(i, first_scales[i]);
-      first_unit = false;
-    }
-    const int all_see = n - (p.c.causal ? p.c.T - 1 : 0);
-
-    // ---- the unit's tiles -------------------------------------------------------
-    float o[MT][NT][4], sum_r[OWN][4];
-    f32x2 l[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-#pragma unroll
-      for (int j = 0; j < MT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][i][e] = 0.f;
-      l[i] = pair(0.f, 0.f);
-    }
-#pragma unroll
-    for (int i = 0; i < OWN; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum_r[i][e] = 0.f;
-#pragma unroll 1
-    for (int tile = cur.j; tile < cur.j1; ++tile) {
-      // (the place before this one's that is to be fetched to)
-      store_scales(ahead == 0 ? NS - 1 : ahead - 1, scales);
-      copy_wait<NS - 2>();
-      __syncthreads();
-      // (the place of the tile before, which every warp has left)
-      fetch(ahead);
-      uint8_t* place = smem + stage * kStageBytes<DK>;
-      uint8_t* place_s = place + 2 * kTile * RB;
-      stage = stage + 1 == NS ? 0 : stage + 1;
-      ahead = ahead + 1 == NS ? 0 : ahead + 1;
+    uint64_t *full = keys ? bars.k_full : bars.v_full, *empty = keys ? bars.k_empty : bars.v_empty;
+    uint8_t* tiles = keys ? sK : sV;
+    const int ring = keys ? kRing : kRingV<DK>;
+    int seg = 0, raw = 0, st = 0;
+    uint32_t free = 1;                     // parity of a place's release
+    for (int it = 0; cur.at < end; ++it) {
+      const int ahead = raw == 0 ? kRaw - 1 : raw - 1;
+      store_scales(ahead == 0 ? kRaw - 1 : ahead - 1, scales);
+      copy_wait<kRaw - 2>();
+      __syncwarp();
+      fetch(ahead);                        // (the place of the tile before, which every lane has left)
+      uint2 x;
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
+                   : "=r"(x.x), "=r"(x.y)
+                   : "r"(raw_u32 + raw * kRawBytes<DK> + 32 * RB + lane * 8));
       // A NaN scale of a value must not meet a probability of 0 of a row that does not
-      // see its entry: it becomes 0 (before the next barrier, behind which it is read),
-      // and the rows that do see it remember the group.
-      if (tid >= kTile) {
-        uint2* at = reinterpret_cast<uint2*>(place_s + tid * 8);
-        const uint2 x = *at;
-        const uint32_t bad[2] = {nan_scales(x.x), nan_scales(x.y)};
-        if (bad[0] | bad[1]) {
-          *at = make_uint2(x.x & ~(bad[0] / 128 * 255), x.y & ~(bad[1] / 128 * 255));
-          const uint32_t mask = groups_of(bad);
-          for (int r = 0; r < rows; ++r)
-            if (tile * kTile + tid - kTile < reinterpret_cast<const int*>(&s_far[r >> 3][(r & 7) >> 1])[r & 1])
-              atomicOr(&s_poison[r], mask);
-        }
+      // see its entry: it becomes 0, and the rows that do see it remember the group.
+      const uint32_t bad[2] = {keys ? 0u : nan_scales(x.x), keys ? 0u : nan_scales(x.y)};
+      if (bad[0] | bad[1]) {
+        x.x &= ~(bad[0] / 128 * 255);
+        x.y &= ~(bad[1] / 128 * 255);
+        const uint32_t mask = groups_of(bad);
+        const int row0 = (cur.u - p.by_blocks(cur.u) * p.blocks) * p.block_rows, rows = min(p.block_rows, p.R - row0);
+        for (int r = 0; r < rows; ++r)
+          if (cur.j * kTile + e < (p.c.causal ? cur.n - (p.c.T - 1 - (int)p.by_G(row0 + r)) : cur.n))
+            atomicOr(&s_poison[seg & 3][r], mask);
       }
-
-      // S^T = K Q^T
-      float s[NT][4];
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
-      {
-        constexpr int W = DK / 32;         // words of an entry: four code pairs each
-        uint32_t w[2][W], sc2[2][W / 2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint8_t* from = place + place_of<DK>(entry_of(g), t * (RB / 4)) + (16 * warp + 8 * half) * RB;
-          const uint8_t* from_s = place_s + (16 * warp + entry_of(g) + 8 * half) * 8;
-          if constexpr (DK == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(from);
-            w[half][0] = x.x, w[half][1] = x.y, w[half][2] = x.z, w[half][3] = x.w;
-            const uint32_t y = *reinterpret_cast<const uint16_t*>(from_s + 2 * t);
-            sc2[half][0] = scale_half2(y & 0xffu);
-            sc2[half][1] = scale_half2(y >> 8);
-          } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(from);
-            w[half][0] = x.x, w[half][1] = x.y;
-            sc2[half][0] = scale_half2(from_s[t]);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          uint32_t lo[4], hi[4];
-          codes_to_half(w[0][i], lo);
-          codes_to_half(w[1][i], hi);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            lo[k] = mul_half2(lo[k], sc2[0][i / 2]);
-            hi[k] = mul_half2(hi[k], sc2[1][i / 2]);
-          }
-          const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-#pragma unroll
-          for (int c = 0; c < NT; ++c) {
-            const uint4 qq = s_q[(c * (KS / 2) + i) * 32 + lane];
-            mma(s[c], a0, qq.x, qq.y);
-            mma(s[c], a1, qq.z, qq.w);
-          }
-        }
+      ok = all(wait(p, &empty[st], free, stop));
+      if (!ok) break;
+      decode(raw, x, tiles + st * kTileBytes<DK>);
+      fence_async_shared();
+      __syncwarp();
+      if (lane == 0 && !(p.fault == kFaultStall && it == 0 && keys)) mbar_arrive(&full[st]);
+      raw = raw + 1 == kRaw ? 0 : raw + 1;
+      if (++st == ring) {
+        st = 0;
+        free ^= 1;
       }
-      // probabilities
-      if (tile * kTile + 16 * (warp + 1) > all_see) {
-        const int e0 = tile * kTile + 16 * warp + entry_of(g);   // of s[.][0 .. 1]; e0 + 8 of the others
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const int2 far = s_far[i][t];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e0 + (e >> 1) * 8 >= (e & 1 ? far.y : far.x)) s[i][e] = -INFINITY;
-        }
+      if (++cur.j >= cur.j1) {
+        settle(cur);
+        ++seg;
       }
-      f32x2 sum[NT];
-      const auto make = [&](int i, uint32_t (&pb)[2], f32x2 by, f32x2 nb) {
-        f32x2 y[2];
+    }
+    copy_wait<0>();
+  } else if (warp == 3) {
+    // ------------------------------ products ----------------------------------------
+    int it = 0, seg = 0;
+    const uint32_t one = elect_one();
+    const auto scores = [&](int i) {
+      const int st = i % kRing;
+      if (!all(wait(p, &bars.k_full[st], i / kRing & 1, stop))) return false;
+      tc_fence_after();
+      const uint64_t qd = smem_desc(sQ, 1024, kSwizzle128), kd = smem_desc(sK + st * kTileBytes<DK>, 1024, kSwizzle128);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const float2 x = halves(fma2(pair(s[i][2 * half], s[i][2 * half + 1]), by, nb));
-          const float2 z = make_float2(ex2(x.x), ex2(x.y));
-          y[half] = pair(z.x, z.y);
-          pb[half] = transpose8(pack_half2(z.x, z.y));
+      for (int k = 0; k < DK / 16; ++k)
+        mma_f16_if(one, tmem + (i & 1) * kTile, qd + (k / 4) * (kQBlock >> 4) + (k % 4) * 2,
+                   kd + (k / 4) * (kBlock >> 4) + (k % 4) * 2, kIdescS, k > 0);
+      mma_commit_if(one, &bars.s_full[i & 1]);
+      mma_commit_if(one, &bars.k_empty[st]);
+      return true;
+    };
+    const auto values = [&](int i, bool first, bool last) {
+      const int st = i % kRingV<DK>;
+      if (!all(wait(p, &bars.p_full[i & 1], i >> 1 & 1, stop) && wait(p, &bars.v_full[st], i / kRingV<DK> & 1, stop) &&
+               (!first || wait(p, &bars.o_empty, (seg & 1) ^ 1u, stop))))
+        return false;
+      tc_fence_after();
+      const uint64_t vd = n_major_desc(sV + st * kTileBytes<DK>, kBlock);
+#pragma unroll
+      for (int k = 0; k < kTile / 16; ++k)
+        mma_f16_ta_if(one, tmem + kTmemO, tmem + (i & 1) * kTile + 8 * k, vd + k * (2048 >> 4), kIdescO, !first || k > 0);
+      mma_commit_if(one, &bars.v_empty[st]);
+      if (last) mma_commit_if(one, &bars.o_full);
+      return true;
+    };
+    for (; ok && cur.at < end; cur.next(p, begin, end)) {
+      if (cur.j >= cur.j1) continue;
+      const int count = cur.j1 - cur.j;
+      // (the buffer of tile i + 1 is that of tile i - 1, whose product with V, issued
+      // before, reads the probabilities there first)
+      ok = all(wait(p, &bars.q_full, seg & 1, stop)) && scores(it);
+      for (int j = 0; j < count && ok; ++j, ++it)
+        ok = (j + 1 == count || scores(it + 1)) && values(it, j == 0, j + 1 == count);
+      ++seg;
+    }
+    mma_commit_if(one, &bars.done);        // every MMA has retired
+    const volatile int never = 0;
+    wait(p, &bars.done, 0, &never);
+  } else {
+    // ------------------------------ softmax -----------------------------------------
+    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+    const int row = tid;
+    int it = 0, seg = 0;
+    for (; ok && cur.at < end; cur.next(p, begin, end)) {
+      const bool empty = cur.nt == 0 && cur.at >= begin;
+      if (skip() && !empty) continue;
+      const int b = cur.b, n = cur.n, h = p.by_blocks(cur.u), block = cur.u - h * p.blocks;
+      const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0), r = row0 + row;
+      const bool mine = row < rows, work = warp * 32 < rows;
+      uint32_t in_head;
+      const int tok = p.by_G(mine ? r : 0, &in_head);
+      if (empty) {
+        float none[16] = {};
+        for (int d = 0; d < DK && mine; d += 16) {
+          finish<16>(p, b, h, r, d, -INFINITY, 0.f, 0.f, none, d == 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) none[i] = 0.f;
         }
-        sum[i] = add2(y[0], y[1]);
-        return fmaxf(halves(sum[i]).x, halves(sum[i]).y);
-      };
-      float most = 0.f;                    // (of two probabilities: none of them above is too large for half precision)
-#pragma unroll
-      for (int i = 0; i < NT; i += 2) {
-        const float4 r0 = s_row[i][t], r1 = s_row[i + 1][t];
-        uint32_t a[2], c[2];
-        most = fmaxf(most, make(i, a, pair(r0.x, r0.y), pair(r0.z, r0.w)));
-        most = fmaxf(most, make(i + 1, c, pair(r1.x, r1.y), pair(r1.z, r1.w)));
-        s_p[(warp * (NT / 2) + i / 2) * 32 + lane] = make_uint4(a[0], a[1], c[0], c[1]);
+        continue;
       }
-      if (__syncthreads_or(most > 16384.f)) {
+      // the row's queries (the tiles before have been multiplied: their scores were here)
+      float c2 = 0.f;
+      if (work) {
+        const uint16_t* q = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token +
+                            (int64_t)(h * p.G + in_head) * p.c.q_head;
+        const auto chunk = [&](int i) {
+          return mine && 8 * i < p.D ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
+        };
+        int up = 0;
+        if (p.bf16) {
+          // 2^up that brings the largest that is finite to 2^14 .. 2^15
+          uint32_t most = 0;
+#pragma unroll 8
+          for (int i = 0; i < DK / 8; ++i) {
+            const uint4 x = chunk(i);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const float4 row = s_row[i][t];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float x = fmaxf(s[i][e], s[i][e + 2]) * (e ? row.y : row.x);
-#pragma unroll
-            for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-            if (g == 0) s_top[warp][i * 8 + 2 * t + e] = x;
-          }
-        }
-        __syncthreads();
-        float nb[NT][2];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const float4 row = s_row[i][t];
-          float a[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = i * 8 + 2 * t + e;
-            const float x = fmaxf(fmaxf(s_top[0][r], s_top[1][r]), fmaxf(s_top[2][r], s_top[3][r])), had = e ? row.w : row.z;
-            nb[i][e] = had;
-            a[e] = 1.f;
-            if (x + had > kLift + kLag - 1.f) {
-              nb[i][e] = kLift - x;
-              a[e] = ex2(nb[i][e] - had);  // 0 at the first
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t y = w[j] & 0x7fff7fffu;
+              most = __vmaxu2(most, y & ~__vcmpgeu2(y, 0x7f807f80u));
             }
           }
-          l[i] = mul2(l[i], pair(a[0], a[1]));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-#pragma unroll
-            for (int j = 0; j < MT; ++j) o[j][i][e] *= a[e & 1];
-            if (i % 4 == warp) sum_r[i / 4][e] *= a[e & 1];
-          }
-          uint32_t pb[2];
-          make(i, pb, pair(row.x, row.y), pair(nb[i][0], nb[i][1]));
-          *(reinterpret_cast<uint2*>(s_p + (warp * (NT / 2) + i / 2) * 32 + lane) + i % 2) = make_uint2(pb[0], pb[1]);
+          most = max(most & 0xffffu, most >> 16);
+          up = min(14 - ((int)(most >> 7) - 127), 100);
         }
-        __syncthreads();
-        // (read again behind the next tile's barrier)
+        const float by = __int_as_float((up + 127) << 23);
+        c2 = fmaxf(p.c2 * __int_as_float((127 - up) << 23), 0x1p-126f);       // (not 0: masked scores stay -infinity)
+#pragma unroll 4
+        for (int i = 0; i < DK / 8; ++i) {
+          const uint4 x = chunk(i);
+          uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          if (p.bf16) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
-          if (i % 4 == warp && g == 0) {
-            s_row[i][t].z = nb[i][0];
-            s_row[i][t].w = nb[i][1];
+            for (int j = 0; j < 4; ++j) {
+              const float2 y = to_float(true, w[j]);
+              w[j] = pack_half2(y.x * by, y.y * by);
+            }
           }
+          *reinterpret_cast<uint4*>(sQ + (i >> 3) * kQBlock + row * 128 + ((i ^ row) & 7) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        fence_async_shared();
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars.q_full);
+      const int far = p.c.causal ? n - (p.c.T - 1 - tok) : n;  // entries that the row sees
+      float lim = -INFINITY, nb = 0.f, l = 0.f, rl = 0.f;      // from where on the reference (negative) follows; sums
+      for (int j = cur.j; j < cur.j1; ++j, ++it) {
+        ok = all(wait(p, &bars.s_full[it & 1], it >> 1 & 1, stop));
+        if (!ok) break;
+        tc_fence_after();
+        if (work) {
+          const uint32_t s_buf = lanes + (it & 1) * kTile, o_buf = lanes + kTmemO;
+          uint32_t v[2][32];
+          tmem_ld32_issue(s_buf, v[0]);
+          tmem_ld32_issue(s_buf + 32, v[1]);
+          tmem_ld_wait();
+          reg_pin(v[0]);
+          reg_pin(v[1]);
+          const int nv = far - j * kTile;
+          if (__any_sync(0xffffffffu, nv < kTile)) {
 #pragma unroll
-      for (int i = 0; i < NT; ++i) l[i] = add2(l[i], sum[i]);
-      // O^T += V^T P^T: elements 32 warp + 4 g .. + 3 (16 warp + 2 g, + 1 of 64)
-      const uint32_t ones[4] = {kOnes, kOnes, kOnes, kOnes};
-      constexpr uint32_t low = 0x0f0f0f0fu;
-      const auto products = [&](int k, const uint32_t (&a)[MT][4]) {
-#pragma unroll
-        for (int i = 0; i < NT; i += 2) {
-          const uint4 pb = s_p[(k * (NT / 2) + i / 2) * 32 + lane];
-#pragma unroll
-          for (int j = 0; j < MT; ++j) {
-            mma(o[j][i], a[j], pb.x, pb.y);
-            mma(o[j][i + 1], a[j], pb.z, pb.w);
+            for (int i = 0; i < kTile; ++i)
+              if (i >= nv) v[i / 32][i % 32] = 0xff800000u;
           }
-          if (i % 4 == (warp & 2)) {       // n-tiles warp, warp + 4
-            if (warp & 1) mma(sum_r[i / 4], ones, pb.z, pb.w);
-            else mma(sum_r[i / 4], ones, pb.x, pb.y);
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < kTile; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(v[i / 32][i % 32]));
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2;
+          const bool grow = top > lim;
+          if (__any_sync(0xffffffffu, grow)) {
+            float a = 1.f;
+            if (grow) {
+              a = lim == -INFINITY ? 0.f : ex2((kLift - top) - nb);
+              lim = top + kLag;
+              nb = kLift - top;
+            }
+            l *= a;
+            rl *= a;
+            if (j > cur.j) {
+              ok = all(wait(p, &bars.v_empty[(it - 1) % kRingV<DK>], (it - 1) / kRingV<DK> & 1, stop));
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1                           // (rare, and registers are short)
+              for (int i = 0; i < DK / 16; ++i) {
+                uint32_t o[16];
+                tmem_ld16_issue(o_buf + 16 * i, o);
+                tmem_ld_wait();
+                reg_pin(o);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * a);
+                tmem_st16_issue(o_buf + 16 * i, o);
+              }
+            }
           }
+          f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+          float rsum[4] = {};
+          const f32x2 by = pair(c2, c2), ref = pair(nb, nb);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 x = halves(fma2(pair(__uint_as_float(v[g][2 * i]), __uint_as_float(v[g][2 * i + 1])), by, ref));
+              const float2 y = make_float2(ex2(x.x), ex2(x.y));
+              pk[i] = pack_half2(y.x, y.y);
+              sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
+              add_halves(pk[i], rsum[i % 2 * 2], rsum[i % 2 * 2 + 1]);
+            }
+            tmem_st16_issue(s_buf + 16 * g, pk);
+          }
+          const float2 ls = halves(add2(sum[0], sum[1]));
+          l += ls.x + ls.y;
+          rl += (rsum[0] + rsum[1]) + (rsum[2] + rsum[3]);
+          tmem_st_wait();
         }
-      };
-      if constexpr (DK == 128) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t w[4], sb[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i] = *reinterpret_cast<const uint16_t*>(place + place_of<DK>(t + 4 * (i & 1), 16 * warp + 2 * g) +
-                                                      (kTile + 16 * k + 8 * (i >> 1)) * RB);
-            sb[i] = place_s[(kTile + 16 * k + t + 4 * i) * 8 + 2 * warp + (g >> 2)];
-          }
-          const uint32_t s01 = sb[0] << 7 | sb[1] << 23, s23 = sb[2] << 7 | sb[3] << 23;
-          // entries t and t + 8 in one word, t + 4 and t + 12 in the other; pairs of entries
-          const uint32_t x = w[0] | w[2] << 16, z = w[1] | w[3] << 16;
-          uint32_t even[4], odd[4];        // elements 0, 2 (and 1, 3) of t, t + 4; of t + 8, t + 12
-          codes_to_half((x & low) | (z << 4 & ~low), even);
-          codes_to_half((x >> 4 & low) | (z & ~low), odd);
-          uint32_t a[MT][4];
-#pragma unroll
-          for (int j = 0; j < MT; ++j) {
-            a[j][0] = mul_half2(even[j], s01);
-            a[j][1] = mul_half2(odd[j], s01);
-            a[j][2] = mul_half2(even[2 + j], s23);
-            a[j][3] = mul_half2(odd[2 + j], s23);
-          }
-          products(k, a);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; k += 2) {
-          uint32_t x = 0, z = 0, sb[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t w = place[place_of<DK>(t + 4 * (i & 1), 8 * warp + g) + (kTile + 16 * k + 8 * (i >> 1)) * RB];
-            if (i & 1) z |= w << (8 * (i >> 1)); else x |= w << (8 * (i >> 1));
-            sb[i] = place_s[(kTile + 16 * k + t + 4 * i) * 8 + warp];
-          }
-          uint32_t even[4], odd[4];
-          codes_to_half((x & low) | (z << 4 & ~low), even);
-          codes_to_half((x >> 4 & low) | (z & ~low), odd);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t s01 = sb[4 * i] << 7 | sb[4 * i + 1] << 23, s23 = sb[4 * i + 2] << 7 | sb[4 * i + 3] << 23;
-            const uint32_t a[MT][4] = {{mul_half2(even[2 * i], s01), mul_half2(odd[2 * i], s01),
-                                        mul_half2(even[2 * i + 1], s23), mul_half2(odd[2 * i + 1], s23)}};
-            products(k + i, a);
-          }
-        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.p_full[it & 1]);
       }
-    }
-
-    // ---- what the CTA has of the unit -------------------------------------------
-    const bool begins = cur.j == 0, whole = begins && cur.j1 == nt;
-    const int64_t slot = 2 * (int64_t)me + (cur.at >= begin ? 1 : 0);            // (begun before, or here)
-    if (tid == 0 && begins)
-      p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] =
-          make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kStart + nt - 1));
-    __syncthreads();                       // (tops were read, references written)
+      if (!ok) break;
+      const bool begins = cur.j == 0, whole = begins && cur.j1 == cur.nt;
+      const int64_t slot = 2 * (int64_t)me + (cur.at >= begin ? 1 : 0);          // (begun before, or here)
+      if (row == 0 && begins)
+        p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] =
+            make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kUnitStart + cur.nt - 1));
+      ok = all(wait(p, &bars.o_full, seg & 1, stop));
+      if (!ok) break;
+      tc_fence_after();
+      if (work) {
+        const uint32_t poison = s_poison[seg & 3][row];
+        s_poison[seg & 3][row] = 0;
+        const float base = lim == -INFINITY ? -INFINITY : -nb;
+        const int64_t at = slot * p.slot_rows + row;
+        if (mine && !whole) p.slot_ml[at] = make_float4(base, l, rl, 0.f);
+#pragma unroll 1
+        for (int i = 0; i < DK / 16; ++i) {
+          uint32_t raw[16];
+          tmem_ld16_issue(lanes + kTmemO + 16 * i, raw);
+          tmem_ld_wait();
+          reg_pin(raw);
+          float o[16];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
+          for (int x = 0; x < 16; ++x) o[x] = poison >> i & 1u ? NAN : __uint_as_float(raw[x]);
+          if (mine) {
+            if (whole) {
+              finish<16>(p, b, h, r, 16 * i, base, l, rl, o, i == 0);
+            } else {
+              float* to = p.slot_o + at * DK + 16 * i;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float x = e ? halves(l[i]).y : halves(l[i]).x;
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
-        if (g == 0) {
-          s_top[warp][i * 8 + 2 * t + e] = x;
-          if (i % 4 == warp) s_sum[i * 8 + 2 * t + e] = sum_r[i / 4][e];
-        }
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = i * 8 + 2 * t + e;
-        const float had = e ? s_row[i][t].w : s_row[i][t].z, ref = had == kNone ? -INFINITY : -had;
-        const float sum = (s_top[0][r] + s_top[1][r]) + (s_top[2][r] + s_top[3][r]), rounded = s_sum[r];
-        float v[4];
-        int d;
-        if constexpr (DK == 128) {
-          d = 32 * warp + 4 * g;
-          v[0] = o[0][i][e], v[1] = o[0][i][e + 2], v[2] = o[MT - 1][i][e], v[3] = o[MT - 1][i][e + 2];
-        } else {                           // two lanes' elements in one of them
-          d = 16 * warp + 2 * g;
-          v[0] = o[0][i][e], v[1] = o[0][i][e + 2];
-          v[2] = __shfl_down_sync(0xffffffffu, v[0], 4);
-          v[3] = __shfl_down_sync(0xffffffffu, v[1], 4);
-        }
-        if (s_poison[r] >> (d / 16) & 1u) v[0] = v[1] = v[2] = v[3] = NAN;
-        if (r < rows && (DK == 128 || g % 2 == 0)) {
-          if (whole) {
-            finish<4>(p, b, h, row0 + r, d, ref, sum, rounded, v, d == 0);
-          } else {
-            if (d == 0) p.slot_ml[slot * p.slot_rows + r] = make_float4(ref, sum, rounded, 0.f);
-            *reinterpret_cast<float4*>(p.slot_o + (slot * p.slot_rows + r) * DK + d) = make_float4(v[0], v[1], v[2], v[3]);
+              for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(to + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+            }
           }
         }
       }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars.o_empty);
+      ++seg;
     }
   }
-  copy_wait<0>();
+  if (!ok) {
+    s_abort = 1;
+    if (lane == 0) atomicExch(p.err, kErrMbarTimeout);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) tmem_dealloc(tmem, kTmemCols);
 }
 
-template <int DK, int NT>
+template <int DK>
 cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   static PerDevice attr;
   const cudaError_t e = attr.once(dev, []() {
-    return cudaFuncSetAttribute(attend4_rows_kernel<DK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DK, NT>);
+    return cudaFuncSetAttribute(attend4_rows_kernel<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DK>);
   });
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend4_rows_kernel<DK, NT>, dim3((unsigned)rows4_workers(NT, sms)), dim3(kThreads), kSmem<DK, NT>, s, p);
+  return launch_pdl(attend4_rows_kernel<DK>, dim3((unsigned)rows4_workers(sms)), dim3(kRowThreads), kSmem<DK>, s, p);
 }
 
 }  // namespace
 
-int rows4_workers(int NT, int sms) { return sms * ctas_per_sm(NT); }
+int rows4_workers(int sms) { return 2 * sms; }
 
 cudaError_t launch_attend4_rows(const Attend4Params& p, int dev, int sms, cudaStream_t s) {
-  const int NT = p.slot_rows / 8;
-  if (p.D <= 64) return NT == 2   ? launch_t<64, 2>(p, dev, sms, s)
-                        : NT == 4 ? launch_t<64, 4>(p, dev, sms, s)
-                        : NT == 6 ? launch_t<64, 6>(p, dev, sms, s)
-                                  : launch_t<64, 8>(p, dev, sms, s);
-  return NT == 2   ? launch_t<128, 2>(p, dev, sms, s)
-         : NT == 4 ? launch_t<128, 4>(p, dev, sms, s)
-         : NT == 6 ? launch_t<128, 6>(p, dev, sms, s)
-                   : launch_t<128, 8>(p, dev, sms, s);
+  return p.D <= 64 ? launch_t<64>(p, dev, sms, s) : launch_t<128>(p, dev, sms, s);
 }
 
 }  // namespace sp

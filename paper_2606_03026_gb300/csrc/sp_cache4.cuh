@@ -30,7 +30,8 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms);
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c);
 cudaError_t launch_write4(const Cache4Shape& s, const sp_write4& c, cudaStream_t stream);
 cudaError_t launch_read4(const Cache4Shape& s, const sp_read4& c, cudaStream_t stream);
-cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, cudaStream_t stream);
+cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, int* err, int fault,
+                           cudaStream_t stream);
 
 // n / d and n % d for n < 2^31, d < 2^31.
 struct Divide {

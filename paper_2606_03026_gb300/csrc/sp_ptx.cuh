@@ -188,6 +188,16 @@ __device__ __forceinline__ uint64_t smem_desc(const void* p, uint32_t group_byte
   return d;
 }
 constexpr uint64_t kSwizzle128 = 2, kSwizzle64 = 4;
+// An operand whose rows run along the MMA's N: 64 elements (128 bytes,
+// swizzled) per row of K, 8 rows of K 1024 bytes apart, the next 64 elements
+// of N `block` bytes on.
+__device__ __forceinline__ uint64_t n_major_desc(const void* p, uint32_t block) {
+  uint64_t d = smem_desc(p, 1024, kSwizzle128);
+  d &= ~((uint64_t)0x3FFF << 16);
+  return d | (uint64_t)(block >> 4) << 16;
+}
+// Shared-memory writes of this thread are seen by the tensor cores and bulk copies after it.
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;

@@ -81,6 +81,8 @@ _SIGNATURES = {
     "spike_proj_cache_evict": ([_P, _P, _P], ctypes.c_int),
     "spike_proj_cache4_create": ([_P, _I32, _I32, _I32, _I32, _I32, _I32, _P], ctypes.c_int),
     "spike_proj_cache4_destroy": ([_P], ctypes.c_int),
+    "spike_proj_cache4_status": ([_P, _P], ctypes.c_int),
+    "spike_proj_cache4_inject_fault": ([_P, _I32], ctypes.c_int),
     "spike_proj_cache4_write": ([_P, _P, _P], ctypes.c_int),
     "spike_proj_cache4_read": ([_P, _P, _P], ctypes.c_int),
     "spike_proj_cache4_attend": ([_P, _P, _P], ctypes.c_int),
@@ -349,6 +351,10 @@ def spike_proj_cache_inject_fault(cache, fault):
     _check(lib().spike_proj_cache_inject_fault(cache, fault), "spike_proj_cache_inject_fault")
 
 
+def spike_proj_cache4_inject_fault(cache, fault):
+    _check(lib().spike_proj_cache4_inject_fault(cache, fault), "spike_proj_cache4_inject_fault")
+
+
 def spike_proj_strerror(status) -> str:
     return lib().spike_proj_strerror(status).decode()
 
@@ -603,6 +609,10 @@ def spike_proj_cache4_create(max_T, Hq, Hkv, D, capacity, dtype, stream=None) ->
 
 def spike_proj_cache4_destroy(cache):
     _check(lib().spike_proj_cache4_destroy(cache), "spike_proj_cache4_destroy")
+
+
+def spike_proj_cache4_status(cache, stream=None) -> int:
+    return lib().spike_proj_cache4_status(cache, _stream(stream))
 
 
 def spike_proj_cache4_write(cache, call, stream=None):
@@ -898,6 +908,13 @@ class Cache4:
         if not x.is_contiguous():
             raise ValueError(f"{name}: not contiguous")
         return x.data_ptr()
+
+    def status(self, stream=None) -> int:
+        return spike_proj_cache4_status(self.handle, stream)
+
+    def inject_fault(self, fault):
+        """Tests of the error path only (SP_FAULT_STALL)."""
+        spike_proj_cache4_inject_fault(self.handle, fault)
 
     def close(self):
         if self.handle:

@@ -215,6 +215,7 @@ def run(q, k4, v4, lens, layout="entries", causal=True, scale=None, other=None, 
     own.attend(place(q, layout), tuple(place(x, layout) for x in k4), tuple(place(x, layout) for x in v4), lens.to(DEV), out,
                lse=lse, causal=causal, scale=scale, **more)
     torch.cuda.synchronize()
+    assert own.status() == sp.SP_OK
     if cache is None:
         own.close()
     return out.cpu(), lse.cpu()
