@@ -406,6 +406,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     if (lane == 0 && begins)
       p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] = make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kStart + nt - 1));
     const bool poisoned = __any_sync(0xffffffffu, poison != 0);
+    float other[NT][2];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = i * 8 + 2 * t + e;
+        other[i][e] = whole && r < rows ? other_of(p, b, h, row0 + r) : -INFINITY;
+      }
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
 #pragma unroll
@@ -426,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
         const float ref = lim[i][e] == -INFINITY ? -INFINITY : -(e ? halves(base[i]).y : halves(base[i]).x);
         if (r < rows) {
           if (whole) {
-            finish<DK / 8>(p, b, h, row0 + r, g * (DK / 8), ref, x, sum_r[i][e], v, g == 0);
+            finish<DK / 8>(p, b, h, row0 + r, g * (DK / 8), ref, x, sum_r[i][e], v, other[i][e], g == 0);
           } else {
             if (g == 0) p.slot_ml[slot * p.slot_rows + r] = make_float4(ref, x, sum_r[i][e], 0.f);
             float* to = p.slot_o + (slot * p.slot_rows + r) * DK + g * (DK / 8);
@@ -450,8 +459,10 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
   const int64_t id = blockIdx.x;           // (sequence, K/V head, row)
   const int64_t bh = id / p.R;
   const int r = (int)(id - bh * p.R), block = r / p.block_rows, in = r - block * p.block_rows;
+  const int b = (int)(bh / p.Hkv), h = (int)(bh - (int64_t)b * p.Hkv);
   const int2 unit = __ldcg(p.units + bh * p.blocks + block);
   if (unit.x < 0) return;
+  const float other = other_of(p, b, h, r);
   const int first = unit.x >> 1, count = unit.y - first + 1;
   const auto slot_of = [&](int i) { return i == 0 ? (int64_t)unit.x : 2 * (int64_t)(first + i); };
   float m = -INFINITY, l = 0.f, rs = 0.f, o[E] = {};
@@ -529,13 +540,13 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
     }
     m = to;
   }
-  const int b = (int)(bh / p.Hkv), h = (int)(bh - (int64_t)b * p.Hkv);
   if constexpr (E == 4) {
-    finish<4>(p, b, h, r, lane * 4, m, l, rs, o, lane == 0);
+    __syncwarp();
+    finish<4>(p, b, h, r, lane * 4, m, l, rs, o, other, lane == 0);
   } else {
     // two lanes' elements in one of them
     float v[4] = {o[0], o[1], __shfl_down_sync(0xffffffffu, o[0], 1), __shfl_down_sync(0xffffffffu, o[1], 1)};
-    if (lane % 2 == 0) finish<4>(p, b, h, r, lane * 2, m, l, rs, v, lane == 0);
+    if (lane % 2 == 0) finish<4>(p, b, h, r, lane * 2, m, l, rs, v, other, lane == 0);
   }
 }
 

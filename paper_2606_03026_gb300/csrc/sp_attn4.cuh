@@ -269,33 +269,38 @@ __device__ __forceinline__ uint32_t groups_of(const uint32_t (&bad)[2]) {
   return mask;
 }
 
+// The lse (base 2) of the attention over other entries that row r of a K/V head is
+// joined with.  It may lie where the row's lse goes, so that all of a row's threads
+// have it before one of them stores that.
+__device__ __forceinline__ float other_of(const Attend4Params& p, int b, int h, int r) {
+  if (!p.c.other_out) return -INFINITY;
+  uint32_t in_head;
+  const int tok = p.by_G(r, &in_head);
+  return p.c.other_lse[((int64_t)b * p.c.T + tok) * p.Hkv * p.G + h * p.G + in_head] * kLog2e;
+}
 // N values of a row from element d on, out of the sums o with reference `base`, sums l
 // and r: joined with other attention, divided, rounded, stored.
 template <int N>
 __device__ __forceinline__ void finish(const Attend4Params& p, int b, int h, int r, int d, float base, float l, float r_sum,
-                                       float (&o)[N], bool first) {
+                                       float (&o)[N], float other, bool first) {
   uint32_t in_head;
   const int tok = p.by_G(r, &in_head), hq = h * p.G + in_head;
-  const int64_t row = ((int64_t)b * p.c.T + tok) * p.Hkv * p.G + hq;
-  if (p.c.other_out) {
-    const float other = p.c.other_lse[row] * kLog2e;
-    if (!(other == -INFINITY)) {
-      const float to = fmaxf(base, other);
-      const float f = base == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to);
-      const uint16_t* from = static_cast<const uint16_t*>(p.c.other_out) + b * p.c.other_batch + tok * p.c.other_token +
-                             hq * p.c.other_head + d;
+  if (!(other == -INFINITY)) {
+    const float to = fmaxf(base, other);
+    const float f = base == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to);
+    const uint16_t* from = static_cast<const uint16_t*>(p.c.other_out) + b * p.c.other_batch + tok * p.c.other_token +
+                           hq * p.c.other_head + d;
 #pragma unroll
-      for (int i = 0; i < N; i += 4)
-        if (d + i < p.D) {
-          const uint2 raw = *reinterpret_cast<const uint2*>(from + i);
-          const float2 lo = to_float(p.bf16, raw.x), hi = to_float(p.bf16, raw.y);
-          o[i] = fmaf(fo, lo.x, f * o[i]), o[i + 1] = fmaf(fo, lo.y, f * o[i + 1]);
-          o[i + 2] = fmaf(fo, hi.x, f * o[i + 2]), o[i + 3] = fmaf(fo, hi.y, f * o[i + 3]);
-        }
-      l = fmaf(l, f, fo);
-      r_sum = fmaf(r_sum, f, fo);
-      base = to;
-    }
+    for (int i = 0; i < N; i += 4)
+      if (d + i < p.D) {
+        const uint2 raw = *reinterpret_cast<const uint2*>(from + i);
+        const float2 lo = to_float(p.bf16, raw.x), hi = to_float(p.bf16, raw.y);
+        o[i] = fmaf(fo, lo.x, f * o[i]), o[i + 1] = fmaf(fo, lo.y, f * o[i + 1]);
+        o[i + 2] = fmaf(fo, hi.x, f * o[i + 2]), o[i + 3] = fmaf(fo, hi.y, f * o[i + 3]);
+      }
+    l = fmaf(l, f, fo);
+    r_sum = fmaf(r_sum, f, fo);
+    base = to;
   }
   const bool empty = l == 0.f;
   const float inv = empty ? 0.f : 1.f / r_sum;
@@ -312,7 +317,7 @@ __device__ __forceinline__ void finish(const Attend4Params& p, int b, int h, int
     for (int i = 0; i < N; i += 4)
       if (d + i < p.D) *reinterpret_cast<uint2*>(out + i) = make_uint2(w[i / 2], w[i / 2 + 1]);
   }
-  if (first && p.c.lse) p.c.lse[row] = empty ? -INFINITY : (base + log2f(l)) * kLn2;
+  if (first && p.c.lse) p.c.lse[((int64_t)b * p.c.T + tok) * p.Hkv * p.G + hq] = empty ? -INFINITY : (base + log2f(l)) * kLn2;
 }
 
 }  // namespace

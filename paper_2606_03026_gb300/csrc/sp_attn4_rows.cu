@@ -308,12 +308,13 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       const bool mine = row < rows, work = warp * 32 < rows;
       uint32_t in_head;
       const int tok = p.by_G(mine ? r : 0, &in_head);
+      int2* const unit = p.units + (int64_t)b * p.Hkv * p.blocks + cur.u;
       if (empty) {
-        float none[16] = {};
+        if (row == 0) *unit = make_int2(-1, me);
+        const float other = mine ? other_of(p, b, h, r) : 0.f;
         for (int d = 0; d < DK && mine; d += 16) {
-          finish<16>(p, b, h, r, d, -INFINITY, 0.f, 0.f, none, d == 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) none[i] = 0.f;
+          float none[16] = {};
+          finish<16>(p, b, h, r, d, -INFINITY, 0.f, 0.f, none, other, d == 0);
         }
         continue;
       }
@@ -440,8 +441,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       const bool begins = cur.j == 0, whole = begins && cur.j1 == cur.nt;
       const int64_t slot = 2 * (int64_t)me + (cur.at >= begin ? 1 : 0);          // (begun before, or here)
       if (row == 0 && begins)
-        p.units[(int64_t)b * p.Hkv * p.blocks + cur.u] =
-            make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kUnitStart + cur.nt - 1));
+        *unit = make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kUnitStart + cur.nt - 1));
       ok = all(wait(p, &bars.o_full, seg & 1, stop));
       if (!ok) break;
       tc_fence_after();
@@ -449,6 +449,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
         const uint32_t poison = s_poison[seg & 3][row];
         s_poison[seg & 3][row] = 0;
         const float base = lim == -INFINITY ? -INFINITY : -nb;
+        const float other = mine && whole ? other_of(p, b, h, r) : -INFINITY;
         const int64_t at = slot * p.slot_rows + row;
         if (mine && !whole) p.slot_ml[at] = make_float4(base, l, rl, 0.f);
 #pragma unroll 1
@@ -462,7 +463,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
           for (int x = 0; x < 16; ++x) o[x] = poison >> i & 1u ? NAN : __uint_as_float(raw[x]);
           if (mine) {
             if (whole) {
-              finish<16>(p, b, h, r, 16 * i, base, l, rl, o, i == 0);
+              finish<16>(p, b, h, r, 16 * i, base, l, rl, o, other, i == 0);
             } else {
               float* to = p.slot_o + at * DK + 16 * i;
 #pragma unroll

@@ -293,16 +293,40 @@ def test_joined_with_other_attention(dtype):
     check(q, k4, v4, lens, run(q, k4, v4, lens, other=other), other=other)
 
 
-def test_joined_in_place():
-    q, k4, v4, lens = make(17, 3, 1, 6, 2, 128, 90, [90, 5, 0], "bf16")
-    g = torch.Generator().manual_seed(18)
-    other = torch.randn(3, 1, 6, 128, generator=g).bfloat16(), torch.randn(3, 1, 6, generator=g)
-    cache = sp.Cache4(6, 2, 128, 90)
-    out, lse = other[0].to(DEV), other[1].to(DEV)
-    on = [tuple(y.to(DEV) for y in x) for x in (k4, v4)]
-    cache.attend(q.to(DEV), *on, lens.to(DEV), out, lse=lse, other_out=out, other_lse=lse)
-    check(q, k4, v4, lens, (out.cpu(), lse.cpu()), other=other)
+@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (5, 10, 64), (1, 6, 64), (4, 40, 128), (9, 42, 64)], ids=str)
+def test_joined_in_place(T, Hq, D):
+    """Into the tensors of what is joined, by calls of other lengths one after the other:
+    sequences without entries beside some that are cut up between the workers."""
+    cache = sp.Cache4(Hq, 2, D, 900, max_T=T)
+    for i, lens in enumerate(([900, 5, 0], [0, 900, 70], [40, 0, 0], [0, 0, 0], [700, 900, 800])):
+        q, k4, v4, lens = make(17 + i, 3, T, Hq, 2, D, 900, lens, "bf16")
+        g = torch.Generator().manual_seed(18 + i)
+        other = torch.randn(3, T, Hq, D, generator=g).bfloat16(), torch.randn(3, T, Hq, generator=g)
+        out, lse = other[0].to(DEV), other[1].to(DEV)
+        on = [tuple(y.to(DEV) for y in x) for x in (k4, v4)]
+        cache.attend(q.to(DEV), *on, lens.to(DEV), out, lse=lse, other_out=out, other_lse=lse)
+        check(q, k4, v4, lens, (out.cpu(), lse.cpu()), other=other)
+        check(q, k4, v4, lens, run(q, k4, v4, lens, cache=cache))
     cache.close()
+
+
+@pytest.mark.parametrize("T,Hq", [(1, 4), (2, 8), (4, 16), (7, 50)], ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_nan_value_stays_where_its_weight_vanishes(T, Hq, D):
+    """A value's group is NaN; its weight beside another entry's, 128 nats above, is
+    nothing in 32 bits, whatever workers have the two."""
+    C = 5000
+    q = torch.ones(2, T, Hq, D, dtype=torch.float16)
+    k4 = torch.zeros(2, C, 2, D // 2, dtype=torch.uint8), torch.full((2, C, 2, D // 16), 120, dtype=torch.uint8)
+    v4 = torch.full((2, C, 2, D // 2), 0x22, dtype=torch.uint8), torch.full((2, C, 2, D // 16), 120, dtype=torch.uint8)
+    k4[0][:, C - T - 1] = 0x77
+    k4[1][:, C - T - 1] = 144              # 6 * 16 an element
+    v4[1][0, 3, 0, 1] = 255
+    lens = torch.tensor([C, C], dtype=torch.int32)
+    out, lse = run(q, k4, v4, lens, scale=1.0)
+    assert out[0, :, :Hq // 2, 16:32].isnan().all()
+    out[0, :, :Hq // 2, 16:32] = 1.0       # (code 2, as all values)
+    assert (out == 1).all() and lse.isfinite().all()
 
 
 @pytest.mark.parametrize("D,B,n", [(128, 1, 200_003), (64, 2, 70_001)])
