@@ -87,13 +87,22 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     vs = v4.scales + f.b * v4.scales_batch + h * v4.scales_head + (e + lane) * v4.scales_entry;
   };
   uint2 k_scales, v_scales;                // of the tile fetched last
+  // Rows of the width that the kernel is made for; of a head one after the other.
+  const bool plain = p.D == DK, lined = plain && k4.entry == RB && v4.entry == RB;
   const auto fetch = [&](int stage) {
     if (f.j < f.j1) {
       const uint32_t to = copy_to + stage * kStageBytes<DK>;
       const int left = f.n - f.j * kTile;  // entries from the tile's first on
-      if (nbytes % 16 == 0) {
-        const uint8_t *kr = kp, *vr = vp;
-        if (left >= kTile && nbytes == RB) {
+      k_scales = v_scales = make_uint2(0, 0);
+      if (plain && left >= kTile) {
+        if (lined) {
+#pragma unroll
+          for (int i = 0; i < kTile / kCopyRows; ++i) {
+            copy_async<16>(to + i * kCopyRows * RB, kp + i * kCopyRows * RB);
+            copy_async<16>(to + (kTile + i * kCopyRows) * RB, vp + i * kCopyRows * RB);
+          }
+        } else {
+          const uint8_t *kr = kp, *vr = vp;
 #pragma unroll
           for (int i = 0; i < kTile / kCopyRows; ++i) {
             copy_async<16>(to + i * kCopyRows * RB, kr);
@@ -101,35 +110,44 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
             kr += kCopyRows * k4.entry;
             vr += kCopyRows * v4.entry;
           }
-        } else if (copy_byte < nbytes) {
-#pragma unroll
+        }
+        if constexpr (DK == 128) {
+          k_scales = __ldg(reinterpret_cast<const uint2*>(ks));
+          v_scales = __ldg(reinterpret_cast<const uint2*>(vs));
+        } else {
+          k_scales.x = __ldg(reinterpret_cast<const uint32_t*>(ks));
+          v_scales.x = __ldg(reinterpret_cast<const uint32_t*>(vs));
+        }
+      } else {
+        if (nbytes % 16 == 0) {
+          const uint8_t *kr = kp, *vr = vp;
+#pragma unroll 2
           for (int i = 0; i < kTile / kCopyRows; ++i) {
-            if (copy_row + i * kCopyRows < left) {
+            if (copy_row + i * kCopyRows < left && copy_byte < nbytes) {
               copy_async<16>(to + i * kCopyRows * RB, kr);
               copy_async<16>(to + (kTile + i * kCopyRows) * RB, vr);
             }
             kr += kCopyRows * k4.entry;
             vr += kCopyRows * v4.entry;
           }
-        }
-      } else {
-        constexpr int C8 = RB / 8;
-        const uint8_t* kc = kp - copy_row * k4.entry - copy_byte;
-        const uint8_t* vc = vp - copy_row * v4.entry - copy_byte;
-        const uint32_t to8 = ring_u32 + stage * kStageBytes<DK>;
+        } else {
+          constexpr int C8 = RB / 8;
+          const uint8_t* kc = kp - copy_row * k4.entry - copy_byte;
+          const uint8_t* vc = vp - copy_row * v4.entry - copy_byte;
+          const uint32_t to8 = ring_u32 + stage * kStageBytes<DK>;
 #pragma unroll 2
-        for (int i = 0; i < kTile * C8 / 32; ++i) {
-          const int e = (i * 32 + lane) / C8, byte = (i * 32 + lane) % C8 * 8;
-          if (e < left && byte < nbytes) {
-            copy_async<8>(to8 + place_of<DK>(e, byte), kc + e * k4.entry + byte);
-            copy_async<8>(to8 + kTile * RB + place_of<DK>(e, byte), vc + e * v4.entry + byte);
+          for (int i = 0; i < kTile * C8 / 32; ++i) {
+            const int e = (i * 32 + lane) / C8, byte = (i * 32 + lane) % C8 * 8;
+            if (e < left && byte < nbytes) {
+              copy_async<8>(to8 + place_of<DK>(e, byte), kc + e * k4.entry + byte);
+              copy_async<8>(to8 + kTile * RB + place_of<DK>(e, byte), vc + e * v4.entry + byte);
+            }
           }
         }
-      }
-      k_scales = v_scales = make_uint2(0, 0);
-      if (lane < left) {
-        k_scales = row_scales(ks, groups);
-        v_scales = row_scales(vs, groups);
+        if (lane < left) {
+          k_scales = row_scales(ks, groups);
+          v_scales = row_scales(vs, groups);
+        }
       }
       if (++f.j < f.j1) {
         kp += kTile * k4.entry;
@@ -148,6 +166,16 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     *reinterpret_cast<uint2*>(to + kTile * 8) = v;
   };
   k_scales = v_scales = make_uint2(0, 0);
+  // the first unit's queries before its tiles, which would hold them up
+  const auto skipped = [&]() { return cur.j >= cur.j1 && (cur.nt > 0 || cur.at < begin); };
+  uint2 x[NT][KS];
+  const auto load_queries = [&]() {
+    const int h = p.by_blocks(cur.u), row0 = (cur.u - h * p.blocks) * p.block_rows, rows = min(p.block_rows, p.R - row0);
+#pragma unroll
+    for (int i = 0; i < NT; ++i) load_query<DK>(p, cur.b, h, row0 + i * 8 + g, i * 8 + g < rows, t, x[i]);
+  };
+  while (cur.at < end && skipped()) cur.next(p, begin, end);
+  if (cur.at < end) load_queries();
   enter_unit();
   uint2 k_first[NS - 1], v_first[NS - 1];  // (stored when the queries are there)
 #pragma unroll
@@ -160,7 +188,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
 
   for (; cur.at < end; cur.next(p, begin, end)) {
     const int b = cur.b, n = cur.n, nt = cur.nt, h = p.by_blocks(cur.u), block = cur.u - h * p.blocks;
-    if (cur.j >= cur.j1 && (nt > 0 || cur.at < begin)) continue;
+    if (skipped()) continue;
+    if (!first_unit) load_queries();
     const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0);
 
     // ---- the query rows ---------------------------------------------------------
@@ -169,12 +198,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     int far[NT][2];                        // entries that they see
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      uint2 x[KS];
-      const float down = load_query<DK>(p, b, h, row0 + i * 8 + g, i * 8 + g < rows, t, x);
+      const float down = make_query<DK>(p, x[i]);
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        if (NT == 1) q[j] = x[j];
-        else s_q[(i * KS + j) * 32 + lane] = x[j];
+        if (NT == 1) q[j] = x[i][j];
+        else s_q[(i * KS + j) * 32 + lane] = x[i][j];
       }
       // (lane 4 r has row r's)
 #pragma unroll
@@ -221,8 +249,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
       ahead = ahead + 1 == NS ? 0 : ahead + 1;
       // A NaN scale (exponent 31) of a value must not meet a probability of 0 of a row
       // that does not see its entry: it becomes 0, and the rows that do see it
-      // remember the group.
-      {
+      // remember the group.  (Where all rows see all entries it makes them NaN itself.)
+      if (tile * kTile + kTile > all_see) {
         uint2* at = reinterpret_cast<uint2*>(place_s + (kTile + lane) * 8);
         const uint2 x = *at;
         const uint32_t bad[2] = {nan_scales(x.x), nan_scales(x.y)};
@@ -248,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[sub][i][e] = 0.f;
         constexpr int W = DK / 32;         // words of an entry: four code pairs each
-        uint32_t w[2][W], sc2[2][W / 2];
+        uint32_t w[2][W], sc2[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           const int e = entry_of(g) + 8 * half;
@@ -257,13 +285,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
           if constexpr (DK == 128) {
             const uint4 x = *reinterpret_cast<const uint4*>(from);
             w[half][0] = x.x, w[half][1] = x.y, w[half][2] = x.z, w[half][3] = x.w;
-            const uint32_t y = *reinterpret_cast<const uint16_t*>(from_s + 2 * t);
-            sc2[half][0] = scale_half2(y & 0xffu);
-            sc2[half][1] = scale_half2(y >> 8);
+            sc2[half] = scales_half2(*reinterpret_cast<const uint16_t*>(from_s + 2 * t));
           } else {
             const uint2 x = *reinterpret_cast<const uint2*>(from);
             w[half][0] = x.x, w[half][1] = x.y;
-            sc2[half][0] = scale_half2(from_s[t]);
+            sc2[half] = from_s[t] << 7;
           }
         }
 #pragma unroll
@@ -273,8 +299,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
           codes_to_half(w[1][i], hi);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            lo[k] = mul_half2(lo[k], sc2[0][i / 2]);
-            hi[k] = mul_half2(hi[k], sc2[1][i / 2]);
+            lo[k] = i < 2 ? mul_half2_by<0>(lo[k], sc2[0]) : mul_half2_by<1>(lo[k], sc2[0]);
+            hi[k] = i < 2 ? mul_half2_by<0>(hi[k], sc2[1]) : mul_half2_by<1>(hi[k], sc2[1]);
           }
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
@@ -380,10 +406,10 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
           // pairs of entries instead of pairs of elements: even elements, odd ones
           uint32_t y[4][4];
           constexpr uint32_t low = 0x0f0f0f0fu;
-          codes_to_half((w[0][i] & low) | (w[1][i] << 4 & ~low), y[0]);
-          codes_to_half((w[0][i] >> 4 & low) | (w[1][i] & ~low), y[1]);
-          codes_to_half((w[2][i] & low) | (w[3][i] << 4 & ~low), y[2]);
-          codes_to_half((w[2][i] >> 4 & low) | (w[3][i] & ~low), y[3]);
+          codes_to_half(select_bits<low>(w[0][i], w[1][i] << 4), y[0]);
+          codes_to_half(select_bits<low>(w[0][i] >> 4, w[1][i]), y[1]);
+          codes_to_half(select_bits<low>(w[2][i], w[3][i] << 4), y[2]);
+          codes_to_half(select_bits<low>(w[2][i] >> 4, w[3][i]), y[3]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const uint32_t a[4] = {mul_half2(y[0][k], s01), mul_half2(y[1][k], s01), mul_half2(y[2][k], s23),

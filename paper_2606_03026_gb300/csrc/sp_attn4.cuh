@@ -202,25 +202,28 @@ __device__ __forceinline__ Start<TILE, START> start_of(const Attend4Params& p, u
 }
 
 // ---- query rows -----------------------------------------------------------------
-// A row (`there`: of the K/V head's row number r) as the instructions take it: elements
-// t DK/4 .. (t + 1) DK/4 in half precision, for the four lanes t of the row together.
-// Returns what its scores are to be multiplied by (not 0, so that masked ones stay
-// -infinity).
+// Elements t DK/4 .. (t + 1) DK/4 of row r of a K/V head (`there`: there is one), for the
+// four lanes t of the row together.
 template <int DK>
-__device__ __forceinline__ float load_query(const Attend4Params& p, int b, int h, int r, bool there, int t,
-                                            uint2 (&x)[DK / 16]) {
-  constexpr int KS = DK / 16;
+__device__ __forceinline__ void load_query(const Attend4Params& p, int b, int h, int r, bool there, int t,
+                                           uint2 (&x)[DK / 16]) {
 #pragma unroll
-  for (int j = 0; j < KS; ++j) x[j] = make_uint2(0, 0);
+  for (int j = 0; j < DK / 16; ++j) x[j] = make_uint2(0, 0);
   if (there) {
     uint32_t in_head;
     const int tok = p.by_G(r, &in_head);
     const uint16_t* from = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token +
                            (int64_t)(h * p.G + in_head) * p.c.q_head + t * (DK / 4);
 #pragma unroll
-    for (int j = 0; j < KS; ++j)
+    for (int j = 0; j < DK / 16; ++j)
       if (t * (DK / 4) + 4 * j < p.D) x[j] = __ldg(reinterpret_cast<const uint2*>(from + 4 * j));
   }
+}
+// These as the instructions take them, in half precision.  Returns what the row's scores
+// are to be multiplied by (not 0, so that masked ones stay -infinity).
+template <int DK>
+__device__ __forceinline__ float make_query(const Attend4Params& p, uint2 (&x)[DK / 16]) {
+  constexpr int KS = DK / 16;
   int e = 0;
   if (p.bf16) {
     // 2^e that brings the largest that is finite to 2^14 .. 2^15

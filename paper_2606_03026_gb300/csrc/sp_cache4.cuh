@@ -6,6 +6,7 @@
 // the two in half precision are exact.
 #pragma once
 
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -66,6 +67,22 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
+}
+// The bits of a where the mask is 1, those of b where it is 0.
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t select_bits(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xe4;" : "=r"(r) : "r"(a), "r"(b), "n"(MASK));
+  return r;
+}
+// Two scale bytes (the lower ones of x) in half precision; a product of both halves of x
+// with one of them (an operand of the instruction that takes it twice).
+__device__ __forceinline__ uint32_t scales_half2(uint32_t x) { return __byte_perm(x, 0, 0x4140) << 7; }
+template <int WHICH>
+__device__ __forceinline__ uint32_t mul_half2_by(uint32_t x, uint32_t scales) {
+  const __half2 s = *reinterpret_cast<const __half2*>(&scales), a = *reinterpret_cast<const __half2*>(&x);
+  const __half2 r = __hmul2_rn(a, WHICH ? __high2half2(s) : __low2half2(s));
+  return *reinterpret_cast<const uint32_t*>(&r);
 }
 // A scale byte as two equal half-precision numbers.
 __device__ __forceinline__ uint32_t scale_half2(uint32_t byte) { return byte * 0x00800080u; }
