@@ -46,6 +46,33 @@ static_assert(ctas_per_sm(1) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 102
               ctas_per_sm(4) * (kWarps * kWarpBytes<128, 4> + 1280) <= 228 * 1024, "shared memory of an SM");
 static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
+// From shared memory, in order with the waits for its copies.
+__device__ __forceinline__ uint4 shared16(uint32_t at) {
+  uint4 x;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint2 shared8(uint32_t at) {
+  uint2 x;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint32_t shared4(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint32_t shared2(uint32_t at) {
+  uint32_t x;
+  asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(x) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint32_t shared1(uint32_t at) {
+  uint32_t x;
+  asm volatile("{\n\t.reg .u16 h;\n\tld.shared.u8 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(x) : "r"(at));
+  return x;
+}
+
 template <int DK, int NT>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(const __grid_constant__ Params p) {
   constexpr int KS = DK / 16;              // steps of S's sum, m-tiles of O
@@ -184,6 +211,12 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     k_first[i] = k_scales, v_first[i] = v_scales;
   }
   bool first_unit = true;
+  // Where a lane's operands and scales lie in a tile.  (Kept: the compiler would rather
+  // make them anew for every tile.)
+  uint32_t k_off = place_of<DK>(entry_of(g), t * (RB / 4)), ks_off = 2 * kTile * RB + entry_of(g) * 8 + t * (DK / 64);
+  uint32_t v_off = kTile * RB + place_of<DK>(t, g * (RB / 8)), v4_off = kTile * RB + place_of<DK>(t + 4, g * (RB / 8));
+  uint32_t vs_off = 2 * kTile * RB + (kTile + t) * 8 + (DK == 128 ? g : g / 2);
+  asm volatile("" : "+r"(k_off), "+r"(ks_off), "+r"(v_off), "+r"(v4_off), "+r"(vs_off));
   int stage = 0, ahead = NS - 1;           // places in the ring: of the tile, of the tile to be fetched
 
   for (; cur.at < end; cur.next(p, begin, end)) {
@@ -243,8 +276,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
       __syncwarp();
       // (the place of the tile before, which every lane has left)
       fetch(ahead);
-      uint8_t* place = ring + stage * kStageBytes<DK>;
-      uint8_t* place_s = place + 2 * kTile * RB;
+      const uint32_t place = ring_u32 + stage * kStageBytes<DK>;
+      uint8_t* place_s = ring + stage * kStageBytes<DK> + 2 * kTile * RB;
       stage = stage + 1 == NS ? 0 : stage + 1;
       ahead = ahead + 1 == NS ? 0 : ahead + 1;
       // A NaN scale (exponent 31) of a value must not meet a probability of 0 of a row
@@ -279,17 +312,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
         uint32_t w[2][W], sc2[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const int e = entry_of(g) + 8 * half;
-          const uint8_t* from = place + place_of<DK>(entry_of(g), t * (RB / 4)) + (16 * (sub0 + sub) + 8 * half) * RB;
-          const uint8_t* from_s = place_s + (16 * (sub0 + sub) + e) * 8;
+          const int below = 16 * (sub0 + sub) + 8 * half;
           if constexpr (DK == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(from);
+            const uint4 x = shared16(place + k_off + below * RB);
             w[half][0] = x.x, w[half][1] = x.y, w[half][2] = x.z, w[half][3] = x.w;
-            sc2[half] = scales_half2(*reinterpret_cast<const uint16_t*>(from_s + 2 * t));
+            sc2[half] = scales_half2(shared2(place + ks_off + below * 8));
           } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(from);
+            const uint2 x = shared8(place + k_off + below * RB);
             w[half][0] = x.x, w[half][1] = x.y;
-            sc2[half] = from_s[t] << 7;
+            sc2[half] = shared1(place + ks_off + below * 8) << 7;
           }
         }
 #pragma unroll
@@ -388,17 +419,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
         uint32_t w[4][KS / 4], sb[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          // (entries t, t + 4: their places differ by more than the rows between)
-          const uint8_t* from = place + place_of<DK>(t + 4 * (i & 1), g * (RB / 8)) + (kTile + 16 * (sub0 + sub) + 8 * (i >> 1)) * RB;
-          const uint8_t* from_s = place_s + (kTile + 16 * (sub0 + sub) + t + 4 * i) * 8;
+          const int below = 16 * (sub0 + sub) + 8 * (i >> 1);
+          const uint32_t from = place + (i & 1 ? v4_off : v_off) + below * RB;
           if constexpr (DK == 128) {
-            const uint2 x = *reinterpret_cast<const uint2*>(from);
+            const uint2 x = shared8(from);
             w[i][0] = x.x, w[i][1] = x.y;
-            sb[i] = from_s[g];
           } else {
-            w[i][0] = *reinterpret_cast<const uint32_t*>(from);
-            sb[i] = from_s[g / 2];
+            w[i][0] = shared4(from);
           }
+          sb[i] = shared1(place + vs_off + (16 * (sub0 + sub) + 4 * i) * 8);
         }
         const uint32_t s01 = sb[0] << 7 | sb[1] << 23, s23 = sb[2] << 7 | sb[3] << 23;
 #pragma unroll
