@@ -140,11 +140,23 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       scale = held.scales + f.b * held.scales_batch + (entry + lane) * held.scales_entry + h * held.scales_head;
     };
     uint2 scales = make_uint2(0, 0);       // of the tile copied last
+    // Rows of the width that the kernel is made for; of a head one after the other.
+    const bool plain = p.D == DK, lined = plain && held.entry == RB;
     const auto fetch = [&](int stage) {    // and on
       if (f.at < end) {
         const uint32_t to = raw_u32 + stage * kRawBytes<DK>;
         const int left = f.n - f.j * kTile - e0;
-        if (nbytes % 16 == 0) {
+        scales = make_uint2(0, 0);
+        if (plain && left >= 32) {
+          const uint8_t* from = code;
+#pragma unroll
+          for (int i = 0; i < 32 / kCopyRows; ++i) {
+            copy_async<16>(to + raw_at(copy_row + i * kCopyRows, lane % C), lined ? code + i * kCopyRows * RB : from);
+            from += kCopyRows * held.entry;
+          }
+          if constexpr (DK == 128) scales = __ldg(reinterpret_cast<const uint2*>(scale));
+          else scales.x = __ldg(reinterpret_cast<const uint32_t*>(scale));
+        } else if (nbytes % 16 == 0) {
           const uint8_t* from = code;
 #pragma unroll
           for (int i = 0; i < 32 / kCopyRows; ++i) {
@@ -160,8 +172,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
             if (row < left && byte < nbytes) copy_async<8>(to + raw_at(row, byte >> 4) + (byte & 8), from + row * held.entry + byte);
           }
         }
-        scales = make_uint2(0, 0);
-        if (lane < left) scales = row_scales(scale, groups);
+        if (!(plain && left >= 32) && lane < left) scales = row_scales(scale, groups);
         code += kTile * held.entry;
         scale += kTile * held.scales_entry;
         if (++f.j >= f.j1) enter();
@@ -184,14 +195,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
                      : "r"(raw_u32 + stage * kRawBytes<DK> + raw_at(lane, c)));
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const uint32_t of_chunk = c < 2 ? x.x : x.y;
+        const uint32_t s = scales_half2((c < 2 ? x.x : x.y) >> c % 2 * 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t s = scale_half2(of_chunk >> (c % 2 * 16 + i / 2 * 8) & 0xffu);
           uint32_t h[4];
           codes_to_half(w[c][i], h);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = i < 2 ? mul_half2_by<0>(h[k], s) : mul_half2_by<1>(h[k], s);
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"((to ^ (c % 2 * 4 + i) * 16) + c / 2 * kBlock),
-                       "r"(mul_half2(h[0], s)), "r"(mul_half2(h[1], s)), "r"(mul_half2(h[2], s)), "r"(mul_half2(h[3], s)));
+                       "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]));
         }
       }
     };
