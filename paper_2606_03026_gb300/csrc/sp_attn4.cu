@@ -36,14 +36,13 @@ constexpr int kTile = 32, kSubs = kTile / 16;   // entries of a tile, instructio
 constexpr int kStart = 2;                  // cost of a unit beside its tiles
 
 // CTAs of an SM, by the registers that NT x 8 rows take.
-constexpr int ctas_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
+constexpr int ctas_per_sm(int NT) { return NT == 1 ? 4 : 3; }
 template <int DK> constexpr int kStageBytes = 2 * kTile * kRowBytes<DK> + 2 * kTile * 8;
-template <int DK, int NT> constexpr int kStages = DK == 64 || NT > 2 ? 4 : 3;
+template <int DK> constexpr int kStages = DK == 64 ? 4 : 3;
 template <int DK, int NT> constexpr int kQueryBytes = NT > 1 ? NT * (DK / 16) * 32 * 8 : 0;
-template <int DK, int NT> constexpr int kWarpBytes = kStages<DK, NT> * kStageBytes<DK> + kQueryBytes<DK, NT>;
+template <int DK, int NT> constexpr int kWarpBytes = kStages<DK> * kStageBytes<DK> + kQueryBytes<DK, NT>;
 static_assert(ctas_per_sm(1) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
-              ctas_per_sm(2) * (kWarps * kWarpBytes<128, 2> + 1280) <= 228 * 1024 &&
-              ctas_per_sm(4) * (kWarps * kWarpBytes<128, 4> + 1280) <= 228 * 1024, "shared memory of an SM");
+              ctas_per_sm(2) * (kWarps * kWarpBytes<64, 2> + 1280) <= 228 * 1024, "shared memory of an SM");
 static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
 // From shared memory, in order with the waits for its copies.
@@ -76,7 +75,7 @@ __device__ __forceinline__ uint32_t shared1(uint32_t at) {
 template <int DK, int NT>
 __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(const __grid_constant__ Params p) {
   constexpr int KS = DK / 16;              // steps of S's sum, m-tiles of O
-  constexpr int RB = kRowBytes<DK>, NS = kStages<DK, NT>;
+  constexpr int RB = kRowBytes<DK>, NS = kStages<DK>;
   constexpr int SB = NT == 1 ? kSubs : 1;  // instructions' entries between two looks at the maximum
   extern __shared__ __align__(128) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -505,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
   copy_wait<0>();
 }
 
-// Rows of units that several warps have parts of: WPR warps a row.
+// Rows of units that several workers have parts of: WPR warps a row.
 template <int DK, int WPR>
 __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant__ Params p) {
   constexpr int kBatch = 8, E = DK / 32;

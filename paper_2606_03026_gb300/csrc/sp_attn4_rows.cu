@@ -318,8 +318,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       const int b = cur.b, n = cur.n, h = p.by_blocks(cur.u), block = cur.u - h * p.blocks;
       const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0), r = row0 + row;
       const bool mine = row < rows, work = warp * 32 < rows;
-      uint32_t in_head;
-      const int tok = p.by_G(mine ? r : 0, &in_head);
+      const int tok = p.by_G(mine ? r : 0);
       int2* const unit = p.units + (int64_t)b * p.Hkv * p.blocks + cur.u;
       if (empty) {
         if (row == 0) *unit = make_int2(-1, me);
@@ -330,45 +329,65 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
         }
         continue;
       }
-      // the row's queries (the tiles before have been multiplied: their scores were here)
+      // The warp's rows of queries (the tiles before have been multiplied: their scores
+      // were here), `per` lanes a row.
       float c2 = 0.f;
       if (work) {
-        const uint16_t* q = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token +
-                            (int64_t)(h * p.G + in_head) * p.c.q_head;
-        const auto chunk = [&](int i) {
-          return mine && 8 * i < p.D ? __ldg(reinterpret_cast<const uint4*>(q) + i) : make_uint4(0, 0, 0, 0);
-        };
-        int up = 0;
-        if (p.bf16) {
-          // 2^up that brings the largest that is finite to 2^14 .. 2^15
-          uint32_t most = 0;
-#pragma unroll 8
-          for (int i = 0; i < DK / 8; ++i) {
-            const uint4 x = chunk(i);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        constexpr int kPer = DK / 8, kAtOnce = 32 / kPer, kBatch = 32 / kAtOnce;
+        const int chunk = lane % kPer;
+        uint4 x[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int at = warp * 32 + i * kAtOnce + lane / kPer;
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (at < rows && 8 * chunk < p.D) {
+            uint32_t in;
+            const int token = p.by_G(row0 + at, &in);
+            x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch +
+                                                        token * p.c.q_token + (int64_t)(h * p.G + in) * p.c.q_head) + chunk);
+          }
+        }
+        // 2^up brings a row's largest that is finite to 2^14 .. 2^15
+        int up[kBatch];
+        const auto largest = [&](bool all) {
+          uint32_t over = 0;
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            uint32_t most = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const uint32_t y = w[j] & 0x7fff7fffu;
-              most = __vmaxu2(most, y & ~__vcmpgeu2(y, 0x7f807f80u));
+              most = __vmaxu2(most, all ? y : y & ~__vcmpgeu2(y, 0x7f807f80u));
             }
+            most = max(most & 0xffffu, most >> 16);
+#pragma unroll
+            for (int d = 1; d < kPer; d *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+            over = max(over, most);
+            up[i] = min(14 - ((int)(most >> 7) - 127), 100);
           }
-          most = max(most & 0xffffu, most >> 16);
-          up = min(14 - ((int)(most >> 7) - 127), 100);
-        }
-        const float by = __int_as_float((up + 127) << 23);
-        c2 = fmaxf(p.c2 * __int_as_float((127 - up) << 23), 0x1p-126f);       // (not 0: masked scores stay -infinity)
-#pragma unroll 4
-        for (int i = 0; i < DK / 8; ++i) {
-          const uint4 x = chunk(i);
-          uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          return over >= 0x7f80u;
+        };
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) up[i] = 0;
+        if (p.bf16 && __any_sync(0xffffffffu, largest(true))) largest(false);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const int at = warp * 32 + i * kAtOnce + lane / kPer;
+          uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
           if (p.bf16) {
+            const float by = __int_as_float((up[i] + 127) << 23);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float2 y = to_float(true, w[j]);
               w[j] = pack_half2(y.x * by, y.y * by);
             }
           }
-          *reinterpret_cast<uint4*>(sQ + (i >> 3) * kQBlock + row * 128 + ((i ^ row) & 7) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(sQ + (chunk >> 3) * kQBlock + at * 128 + ((chunk ^ at) & 7) * 16) =
+              make_uint4(w[0], w[1], w[2], w[3]);
+          // (its thread has the row's factor; not 0, so that masked scores stay -infinity)
+          const int up_here = __shfl_sync(0xffffffffu, up[i], (lane - i * kAtOnce) * kPer & 31);
+          if (lane / kAtOnce == i) c2 = fmaxf(p.c2 * __int_as_float((127 - up_here) << 23), 0x1p-126f);
         }
         fence_async_shared();
       }
