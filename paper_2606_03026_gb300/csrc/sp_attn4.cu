@@ -35,14 +35,14 @@ using Params = Attend4Params;
 constexpr int kTile = 32, kSubs = kTile / 16;   // entries of a tile, instructions that they are the rows of
 constexpr int kStart = 2;                  // cost of a unit beside its tiles
 
-// CTAs of an SM, by the registers that NT x 8 rows take.
-constexpr int ctas_per_sm(int NT) { return NT == 1 ? 4 : 3; }
+// CTAs of an SM, by the registers that NT x 8 rows take (and scales that come in pieces).
+constexpr int ctas_per_sm(int NT, bool plain) { return NT == 1 && plain ? 4 : 3; }
 template <int DK> constexpr int kStageBytes = 2 * kTile * kRowBytes<DK> + 2 * kTile * 8;
 template <int DK> constexpr int kStages = DK == 64 ? 4 : 3;
 template <int DK, int NT> constexpr int kQueryBytes = NT > 1 ? NT * (DK / 16) * 32 * 8 : 0;
 template <int DK, int NT> constexpr int kWarpBytes = kStages<DK> * kStageBytes<DK> + kQueryBytes<DK, NT>;
-static_assert(ctas_per_sm(1) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
-              ctas_per_sm(2) * (kWarps * kWarpBytes<64, 2> + 1280) <= 228 * 1024, "shared memory of an SM");
+static_assert(ctas_per_sm(1, true) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
+              ctas_per_sm(2, true) * (kWarps * kWarpBytes<64, 2> + 1280) <= 228 * 1024, "shared memory of an SM");
 static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
 // From shared memory, in order with the waits for its copies.
@@ -72,8 +72,9 @@ __device__ __forceinline__ uint32_t shared1(uint32_t at) {
   return x;
 }
 
-template <int DK, int NT>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(const __grid_constant__ Params p) {
+// PLAIN: heads of DK elements; else of fewer, whose rows are not of whole 16 bytes.
+template <int DK, int NT, bool PLAIN>
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kernel(const __grid_constant__ Params p) {
   constexpr int KS = DK / 16;              // steps of S's sum, m-tiles of O
   constexpr int RB = kRowBytes<DK>, NS = kStages<DK>;
   constexpr int SB = NT == 1 ? kSubs : 1;  // instructions' entries between two looks at the maximum
@@ -94,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
 
   // ---- tiles on their way ---------------------------------------------------------
   const sp_kv4 &k4 = p.c.k4, &v4 = p.c.v4;
-  const int nbytes = p.D / 2, groups = p.D / 16;
+  const int nbytes = PLAIN ? RB : p.D / 2, groups = PLAIN ? DK / 16 : p.D / 16;
   Cursor<kTile, kStart> f = cur;                          // of the tile to be fetched
   // A lane copies 16 bytes of every kCopyRows-th entry of a tile, from copy_row on.
   // Scales: lane l has those of entry l.
@@ -112,69 +113,49 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     ks = k4.scales + f.b * k4.scales_batch + h * k4.scales_head + (e + lane) * k4.scales_entry;
     vs = v4.scales + f.b * v4.scales_batch + h * v4.scales_head + (e + lane) * v4.scales_entry;
   };
-  uint2 k_scales, v_scales;                // of the tile fetched last
-  // Rows of the width that the kernel is made for; of a head one after the other.
-  const bool plain = p.D == DK, lined = plain && k4.entry == RB && v4.entry == RB;
+  ScaleRow<DK, PLAIN> k_scales, v_scales;  // of the tile fetched last
+  // Rows of a head one after the other.
+  const bool lined = PLAIN && k4.entry == RB && v4.entry == RB;
   const auto fetch = [&](int stage) {
     if (f.j < f.j1) {
       const uint32_t to = copy_to + stage * kStageBytes<DK>;
       const int left = f.n - f.j * kTile;  // entries from the tile's first on
-      k_scales = v_scales = make_uint2(0, 0);
-      if (plain && left >= kTile) {
-        if (lined) {
+      if (lined && left >= kTile) {
 #pragma unroll
-          for (int i = 0; i < kTile / kCopyRows; ++i) {
-            copy_async<16>(to + i * kCopyRows * RB, kp + i * kCopyRows * RB);
-            copy_async<16>(to + (kTile + i * kCopyRows) * RB, vp + i * kCopyRows * RB);
-          }
-        } else {
-          const uint8_t *kr = kp, *vr = vp;
+        for (int i = 0; i < kTile / kCopyRows; ++i) {
+          copy_async<16>(to + i * kCopyRows * RB, kp + i * kCopyRows * RB);
+          copy_async<16>(to + (kTile + i * kCopyRows) * RB, vp + i * kCopyRows * RB);
+        }
+      } else if (PLAIN || nbytes % 16 == 0) {
+        const uint8_t *kr = kp, *vr = vp;
 #pragma unroll
-          for (int i = 0; i < kTile / kCopyRows; ++i) {
+        for (int i = 0; i < kTile / kCopyRows; ++i) {
+          if (copy_row + i * kCopyRows < left && (PLAIN || copy_byte < nbytes)) {
             copy_async<16>(to + i * kCopyRows * RB, kr);
             copy_async<16>(to + (kTile + i * kCopyRows) * RB, vr);
-            kr += kCopyRows * k4.entry;
-            vr += kCopyRows * v4.entry;
           }
-        }
-        if constexpr (DK == 128) {
-          k_scales = __ldg(reinterpret_cast<const uint2*>(ks));
-          v_scales = __ldg(reinterpret_cast<const uint2*>(vs));
-        } else {
-          k_scales.x = __ldg(reinterpret_cast<const uint32_t*>(ks));
-          v_scales.x = __ldg(reinterpret_cast<const uint32_t*>(vs));
+          kr += kCopyRows * k4.entry;
+          vr += kCopyRows * v4.entry;
         }
       } else {
-        if (nbytes % 16 == 0) {
-          const uint8_t *kr = kp, *vr = vp;
-#pragma unroll 2
-          for (int i = 0; i < kTile / kCopyRows; ++i) {
-            if (copy_row + i * kCopyRows < left && copy_byte < nbytes) {
-              copy_async<16>(to + i * kCopyRows * RB, kr);
-              copy_async<16>(to + (kTile + i * kCopyRows) * RB, vr);
-            }
-            kr += kCopyRows * k4.entry;
-            vr += kCopyRows * v4.entry;
+        // 8 bytes of every kRows8-th entry
+        constexpr int C8 = RB / 8, kRows8 = 32 / C8;
+        const int row = lane / C8, byte = lane % C8 * 8;
+        const uint8_t* kr = kp + (row - copy_row) * k4.entry + (byte - copy_byte);
+        const uint8_t* vr = vp + (row - copy_row) * v4.entry + (byte - copy_byte);
+        const uint32_t to8 = ring_u32 + stage * kStageBytes<DK>;
+#pragma unroll
+        for (int i = 0; i < kTile / kRows8; ++i) {
+          if (row + i * kRows8 < left && byte < nbytes) {
+            copy_async<8>(to8 + place_of<DK>(row + i * kRows8, byte), kr);
+            copy_async<8>(to8 + kTile * RB + place_of<DK>(row + i * kRows8, byte), vr);
           }
-        } else {
-          constexpr int C8 = RB / 8;
-          const uint8_t* kc = kp - copy_row * k4.entry - copy_byte;
-          const uint8_t* vc = vp - copy_row * v4.entry - copy_byte;
-          const uint32_t to8 = ring_u32 + stage * kStageBytes<DK>;
-#pragma unroll 2
-          for (int i = 0; i < kTile * C8 / 32; ++i) {
-            const int e = (i * 32 + lane) / C8, byte = (i * 32 + lane) % C8 * 8;
-            if (e < left && byte < nbytes) {
-              copy_async<8>(to8 + place_of<DK>(e, byte), kc + e * k4.entry + byte);
-              copy_async<8>(to8 + kTile * RB + place_of<DK>(e, byte), vc + e * v4.entry + byte);
-            }
-          }
-        }
-        if (lane < left) {
-          k_scales = row_scales(ks, groups);
-          v_scales = row_scales(vs, groups);
+          kr += kRows8 * k4.entry;
+          vr += kRows8 * v4.entry;
         }
       }
+      k_scales.load(ks, groups, lane < left);
+      v_scales.load(vs, groups, lane < left);
       if (++f.j < f.j1) {
         kp += kTile * k4.entry;
         vp += kTile * v4.entry;
@@ -186,12 +167,13 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
     }
     copy_commit();
   };
-  const auto store_scales = [&](int stage, uint2 k, uint2 v) {
+  const auto store_scales = [&](int stage, const ScaleRow<DK, PLAIN>& k, const ScaleRow<DK, PLAIN>& v) {
     uint8_t* to = ring + stage * kStageBytes<DK> + 2 * kTile * RB + lane * 8;
-    *reinterpret_cast<uint2*>(to) = k;
-    *reinterpret_cast<uint2*>(to + kTile * 8) = v;
+    *reinterpret_cast<uint2*>(to) = k.value(groups);
+    *reinterpret_cast<uint2*>(to + kTile * 8) = v.value(groups);
   };
-  k_scales = v_scales = make_uint2(0, 0);
+  k_scales.load(nullptr, groups, false);
+  v_scales = k_scales;
   // the first unit's queries before its tiles, which would hold them up
   const auto skipped = [&]() { return cur.j >= cur.j1 && (cur.nt > 0 || cur.at < begin); };
   uint2 x[NT][KS];
@@ -203,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT)) attend4_kernel(cons
   while (cur.at < end && skipped()) cur.next(p, begin, end);
   if (cur.at < end) load_queries();
   enter_unit();
-  uint2 k_first[NS - 1], v_first[NS - 1];  // (stored when the queries are there)
+  ScaleRow<DK, PLAIN> k_first[NS - 1], v_first[NS - 1];        // (stored when the queries are there)
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i) {
     fetch(i);
@@ -619,31 +601,33 @@ cudaError_t launch_merge(const Params& p, int dev, cudaStream_t s) {
   return launch_pdl(merge4_kernel<DK, WPR>, dim3((unsigned)((int64_t)p.c.B * p.Hkv * p.R)), dim3(32 * WPR), 0, s, p);
 }
 
-template <int DK, int NT>
+template <int DK, int NT, bool PLAIN>
 cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   static PerDevice attr;
   constexpr size_t bytes = (size_t)kWarps * kWarpBytes<DK, NT>;
   const cudaError_t e = attr.once(dev, []() {
-    return cudaFuncSetAttribute(attend4_kernel<DK, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    return cudaFuncSetAttribute(attend4_kernel<DK, NT, PLAIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   });
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend4_kernel<DK, NT>, dim3((unsigned)(sms * ctas_per_sm(NT))), dim3(kThreads), bytes, s, p);
+  return launch_pdl(attend4_kernel<DK, NT, PLAIN>, dim3((unsigned)(sms * ctas_per_sm(NT, PLAIN))), dim3(kThreads), bytes, s, p);
 }
 
 // How the R query rows of a K/V head are taken: by warps or by CTAs (a warp's
 // registers hold O of 8 rows of 128-wide heads, of 16 of 64-wide ones), in units of as
 // many rows, workers.
 struct Plan {
-  bool by_ctas;
+  bool wide, plain, by_ctas;
   int blocks, rows, NT, workers;
 };
-Plan plan_of(int R, bool wide, int sms) {
+Plan plan_of(int R, int D, int sms) {
   Plan x;
-  x.by_ctas = R > (wide ? 8 : 16);
+  x.wide = D > 64;
+  x.plain = D == (x.wide ? 128 : 64);
+  x.by_ctas = R > (x.wide ? 8 : 16);
   x.blocks = x.by_ctas ? ceil_div(R, kRowsMost4) : 1;
   x.rows = ceil_div(R, x.blocks);
   x.NT = ceil_div(x.rows, 8);
-  x.workers = x.by_ctas ? rows4_workers(sms) : sms * ctas_per_sm(x.NT) * kWarps;
+  x.workers = x.by_ctas ? rows4_workers(sms) : sms * ctas_per_sm(x.NT, x.plain) * kWarps;
   return x;
 }
 
@@ -654,7 +638,7 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
   Cache4Workspace w{};
   size_t units = 0, most = 0;
   for (int T = 1; T <= s.max_T; ++T) {
-    const Plan x = plan_of(T * (s.Hq / s.Hkv), s.D > 64, sms);
+    const Plan x = plan_of(T * (s.Hq / s.Hkv), s.D, sms);
     units = max(units, (size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * x.blocks * 8);
     most = max(most, 2 * (size_t)x.workers * 8 * x.NT * (16 + DK * 4));
   }
@@ -664,7 +648,7 @@ Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
 }
 
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c) {
-  return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), s.D > 64, 1).blocks * (kStart + ceil_div(s.capacity, kTile));
+  return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), s.D, 1).blocks * (kStart + ceil_div(s.capacity, kTile));
 }
 
 cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, int* err, int fault,
@@ -679,7 +663,7 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.D = s.D;
   p.capacity = s.capacity;
   p.R = c.T * p.G;
-  const Plan plan = plan_of(p.R, s.D > 64, sms);
+  const Plan plan = plan_of(p.R, s.D, sms);
   p.blocks = plan.blocks;
   p.block_rows = plan.rows;
   p.by_blocks = Divide(p.blocks);
@@ -693,10 +677,12 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.units = reinterpret_cast<int2*>(ws);
   p.slot_ml = reinterpret_cast<float4*>(ws + slots);
   p.slot_o = reinterpret_cast<float*>(ws + slots + 2 * (size_t)plan.workers * p.slot_rows * 16);
-  const bool wide = s.D > 64;
+  const bool wide = plan.wide;
   e = plan.by_ctas     ? launch_attend4_rows(p, dev, sms, stream)
-      : plan.NT == 1 ? (wide ? launch_t<128, 1>(p, dev, sms, stream) : launch_t<64, 1>(p, dev, sms, stream))
-                     : launch_t<64, 2>(p, dev, sms, stream);
+      : wide           ? (plan.plain ? launch_t<128, 1, true>(p, dev, sms, stream) : launch_t<128, 1, false>(p, dev, sms, stream))
+      : plan.NT == 1   ? (plan.plain ? launch_t<64, 1, true>(p, dev, sms, stream) : launch_t<64, 1, false>(p, dev, sms, stream))
+      : plan.plain     ? launch_t<64, 2, true>(p, dev, sms, stream)
+                       : launch_t<64, 2, false>(p, dev, sms, stream);
   if (e != cudaSuccess) return e;
   // many warps a row where it has many parts
   if (plan.workers >= 16 * (int64_t)c.B * s.Hkv * plan.blocks)

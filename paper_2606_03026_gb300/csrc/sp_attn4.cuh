@@ -252,18 +252,47 @@ __device__ __forceinline__ float make_query(const Attend4Params& p, uint2 (&x)[D
   return fmaxf(p.c2 * __int_as_float((127 - e) << 23), 0x1p-126f);
 }
 
-// A row's scales (8 at most), bytes.
-__device__ __forceinline__ uint2 row_scales(const uint8_t* from, int groups) {
-  uint2 x = make_uint2(0, 0);
-  if (groups == 8) x = __ldg(reinterpret_cast<const uint2*>(from));
-  else if (groups == 4) x.x = __ldg(reinterpret_cast<const uint32_t*>(from));
-  else
-    for (int i = 0; i < groups; ++i) {
-      const uint32_t y = __ldg(from + i);
-      if (i < 4) x.x |= y << (8 * i); else x.y |= y << (8 * i - 32);
+// A row's scales on their way: what a load brings is not looked at before value(), so
+// that nothing waits for it.  PLAIN: rows of DK elements.
+template <int DK, bool PLAIN>
+struct ScaleRow {
+  uint32_t b[PLAIN ? DK / 64 : DK / 16];
+  __device__ __forceinline__ void load(const uint8_t* from, int groups, bool there) {
+    if constexpr (PLAIN) {
+#pragma unroll
+      for (int i = 0; i < DK / 64; ++i) b[i] = 0;
+      if (!there) return;
+      if constexpr (DK == 128) {
+        const uint2 x = __ldg(reinterpret_cast<const uint2*>(from));
+        b[0] = x.x, b[DK / 64 - 1] = x.y;
+      } else {
+        b[0] = __ldg(reinterpret_cast<const uint32_t*>(from));
+      }
+    } else {
+      const bool even = groups % 2 == 0;
+#pragma unroll
+      for (int i = 0; i < DK / 16; ++i) {
+        b[i] = 0;
+        if (even) {
+          if (2 * i < groups && there) b[i] = __ldg(reinterpret_cast<const uint16_t*>(from) + i);
+        } else if (i < groups && there) {
+          b[i] = __ldg(from + i);
+        }
+      }
     }
-  return x;
-}
+  }
+  // all of them (8 at most), bytes
+  __device__ __forceinline__ uint2 value(int groups) const {
+    if constexpr (PLAIN) {
+      return make_uint2(b[0], DK == 128 ? b[DK / 64 - 1] : 0u);
+    } else if constexpr (DK == 64) {
+      return make_uint2(groups % 2 == 0 ? b[0] | b[1] << 16 : b[0] | b[1] << 8 | b[2] << 16, 0u);
+    } else {
+      if (groups % 2 == 0) return make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+      return make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16);
+    }
+  }
+};
 // The bytes of a row's scales that are NaN (exponent 31), their upper bits.
 __device__ __forceinline__ uint32_t nan_scales(uint32_t x) { return ((x & 0x78787878u) + 0x08080808u) & x & 0x80808080u; }
 __device__ __forceinline__ uint32_t groups_of(const uint32_t (&bad)[2]) {

@@ -61,7 +61,8 @@ struct Bars {
   uint64_t q_full, o_full, o_empty, done;
 };
 
-template <int DK>
+// PLAIN: heads of DK elements; else of fewer, whose rows are not of whole 16 bytes.
+template <int DK, bool PLAIN>
 __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __grid_constant__ Params p) {
   constexpr uint32_t kIdescS = 1u << 4 | (uint32_t)(kTile >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
   constexpr uint32_t kIdescO = 1u << 4 | 1u << 16 | (uint32_t)(DK >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
     // 7 the values; thread = entry, but for the copies.
     constexpr int RB = kRowBytes<DK>, C = RB / 16, kCopyRows = 32 / C;
     const bool keys = warp < 6;
-    const int e0 = (warp & 1) * 32, e = e0 + lane, nbytes = p.D / 2, groups = p.D / 16;
+    const int e0 = (warp & 1) * 32, e = e0 + lane, nbytes = PLAIN ? RB : p.D / 2, groups = PLAIN ? DK / 16 : p.D / 16;
     const sp_kv4 held = keys ? p.c.k4 : p.c.v4;
     const uint32_t raw_u32 = smem_u32(sV + kRingV<DK> * kTileBytes<DK>) + (warp - 4) * (kRaw * kRawBytes<DK>);
     // 16 bytes of a row: so that neither the copies' rows nor a row's reads meet in a bank
@@ -139,40 +140,38 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       code = held.codes + f.b * held.batch + (entry + copy_row) * held.entry + h * held.head + copy_byte;
       scale = held.scales + f.b * held.scales_batch + (entry + lane) * held.scales_entry + h * held.scales_head;
     };
-    uint2 scales = make_uint2(0, 0);       // of the tile copied last
-    // Rows of the width that the kernel is made for; of a head one after the other.
-    const bool plain = p.D == DK, lined = plain && held.entry == RB;
+    ScaleRow<DK, PLAIN> scales;            // of the tile copied last
+    scales.load(nullptr, groups, false);
+    const bool lined = PLAIN && held.entry == RB;              // rows of a head one after the other
     const auto fetch = [&](int stage) {    // and on
       if (f.at < end) {
         const uint32_t to = raw_u32 + stage * kRawBytes<DK>;
         const int left = f.n - f.j * kTile - e0;
-        scales = make_uint2(0, 0);
-        if (plain && left >= 32) {
-          const uint8_t* from = code;
+        if (lined && left >= 32) {
 #pragma unroll
-          for (int i = 0; i < 32 / kCopyRows; ++i) {
-            copy_async<16>(to + raw_at(copy_row + i * kCopyRows, lane % C), lined ? code + i * kCopyRows * RB : from);
-            from += kCopyRows * held.entry;
-          }
-          if constexpr (DK == 128) scales = __ldg(reinterpret_cast<const uint2*>(scale));
-          else scales.x = __ldg(reinterpret_cast<const uint32_t*>(scale));
-        } else if (nbytes % 16 == 0) {
+          for (int i = 0; i < 32 / kCopyRows; ++i)
+            copy_async<16>(to + raw_at(copy_row + i * kCopyRows, lane % C), code + i * kCopyRows * RB);
+        } else if (PLAIN || nbytes % 16 == 0) {
           const uint8_t* from = code;
 #pragma unroll
           for (int i = 0; i < 32 / kCopyRows; ++i) {
             const int row = copy_row + i * kCopyRows;
-            if (row < left && copy_byte < nbytes) copy_async<16>(to + raw_at(row, lane % C), from);
+            if (row < left && (PLAIN || copy_byte < nbytes)) copy_async<16>(to + raw_at(row, lane % C), from);
             from += kCopyRows * held.entry;
           }
         } else {
-          const uint8_t* from = code - copy_row * held.entry - copy_byte;
-#pragma unroll 2
-          for (int i = 0; i < RB / 8; ++i) {
-            const int row = (i * 32 + lane) / (RB / 8), byte = (i * 32 + lane) % (RB / 8) * 8;
-            if (row < left && byte < nbytes) copy_async<8>(to + raw_at(row, byte >> 4) + (byte & 8), from + row * held.entry + byte);
+          // 8 bytes of every kRows8-th entry
+          constexpr int C8 = RB / 8, kRows8 = 32 / C8;
+          const int row8 = lane / C8, byte = lane % C8 * 8;
+          const uint8_t* from = code + (row8 - copy_row) * held.entry + (byte - copy_byte);
+#pragma unroll
+          for (int i = 0; i < 32 / kRows8; ++i) {
+            const int row = row8 + i * kRows8;
+            if (row < left && byte < nbytes) copy_async<8>(to + raw_at(row, byte >> 4) + (byte & 8), from);
+            from += kRows8 * held.entry;
           }
         }
-        if (!(plain && left >= 32) && lane < left) scales = row_scales(scale, groups);
+        scales.load(scale, groups, lane < left);
         code += kTile * held.entry;
         scale += kTile * held.scales_entry;
         if (++f.j >= f.j1) enter();
@@ -210,14 +209,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
     settle(cur);
     enter();
     {
-      uint2 x[kRaw - 1];
+      ScaleRow<DK, PLAIN> x[kRaw - 1];
 #pragma unroll
       for (int i = 0; i < kRaw - 1; ++i) {
         fetch(i);
         x[i] = scales;
       }
 #pragma unroll
-      for (int i = 0; i < kRaw - 2; ++i) store_scales(i, x[i]);
+      for (int i = 0; i < kRaw - 2; ++i) store_scales(i, x[i].value(groups));
     }
     uint64_t *full = keys ? bars.k_full : bars.v_full, *empty = keys ? bars.k_empty : bars.v_empty;
     uint8_t* tiles = keys ? sK : sV;
@@ -226,7 +225,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
     uint32_t free = 1;                     // parity of a place's release
     for (int it = 0; cur.at < end; ++it) {
       const int ahead = raw == 0 ? kRaw - 1 : raw - 1;
-      store_scales(ahead == 0 ? kRaw - 1 : ahead - 1, scales);
+      store_scales(ahead == 0 ? kRaw - 1 : ahead - 1, scales.value(groups));
       copy_wait<kRaw - 2>();
       __syncwarp();
       fetch(ahead);                        // (the place of the tile before, which every lane has left)
@@ -519,14 +518,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
   if (warp == 0) tmem_dealloc(tmem, kTmemCols);
 }
 
-template <int DK>
+template <int DK, bool PLAIN>
 cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
   static PerDevice attr;
   const cudaError_t e = attr.once(dev, []() {
-    return cudaFuncSetAttribute(attend4_rows_kernel<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DK>);
+    return cudaFuncSetAttribute(attend4_rows_kernel<DK, PLAIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DK>);
   });
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend4_rows_kernel<DK>, dim3((unsigned)rows4_workers(sms)), dim3(kRowThreads), kSmem<DK>, s, p);
+  return launch_pdl(attend4_rows_kernel<DK, PLAIN>, dim3((unsigned)rows4_workers(sms)), dim3(kRowThreads), kSmem<DK>, s, p);
 }
 
 }  // namespace
@@ -534,7 +533,8 @@ cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
 int rows4_workers(int sms) { return 2 * sms; }
 
 cudaError_t launch_attend4_rows(const Attend4Params& p, int dev, int sms, cudaStream_t s) {
-  return p.D <= 64 ? launch_t<64>(p, dev, sms, s) : launch_t<128>(p, dev, sms, s);
+  if (p.D <= 64) return p.D == 64 ? launch_t<64, true>(p, dev, sms, s) : launch_t<64, false>(p, dev, sms, s);
+  return p.D == 128 ? launch_t<128, true>(p, dev, sms, s) : launch_t<128, false>(p, dev, sms, s);
 }
 
 }  // namespace sp
