@@ -789,6 +789,9 @@ class Cache:
             pass
 
 
+_NO_STRIDES = (0, 0, 0)
+
+
 class Cache4:
     """Own caches held in 4 bits: writing and reading of entries, and attention
     over them.  The keys and the values of a batch are a pair of uint8 tensors
@@ -836,44 +839,45 @@ class Cache4:
                 vc.data_ptr(), c[0], c[1], c[2], vs.data_ptr(), d[0], d[1], d[2])
 
     def _each(self, x, name, B):
-        if x is None:
-            return 0
-        _want(x, name, (B,), self._i32, self._device)
+        if x.shape != (B,) or x.dtype is not self._i32 or x.get_device() != self._device or x.stride(0) != 1:
+            _want(x, name, (B,), self._i32, self._device)
         return x.data_ptr()
 
     def write(self, k, v, k4, v4, at=None, n=None, k_out=None, v_out=None, stream=None):
         """Tokens t < n[b] of k and v [B, T, Hkv, D] into the slots at[b] + t of the
         caches (at, n: int32 [B]; 0 and T where they are None); k_out and v_out, of
         k's shape, take the values that the codes stand for, and may be k and v."""
-        if k is None:
-            raise ValueError("k: missing")
-        t, dev = self.dtype, self._device
-        B, T = k.shape[0], k.shape[1]
-        rows = (B, T, self.Hkv, self.D)
-        ks, vs = _want(k, "k", rows, t, dev), _want(v, "v", rows, t, dev)
-        ka, va, kos, vos = 0, 0, (0, 0, 0), (0, 0, 0)
+        if k is None or v is None:
+            raise ValueError("k, v: missing")
         if (k_out is None) != (v_out is None):
             raise ValueError("k_out, v_out: one without the other")
+        t, dev, shape = self.dtype, self._device, k.shape
+        B, T = shape[0], shape[1]
+        rows = (B, T, self.Hkv, self.D)
+        ks, vs = k.stride(), v.stride()
+        if (shape != rows or k.dtype is not t or k.get_device() != dev or ks[3] != 1
+                or v.shape != rows or v.dtype is not t or v.get_device() != dev or vs[3] != 1):
+            _want(k, "k", rows, t, dev)
+            _want(v, "v", rows, t, dev)
+        ka, va, kos, vos = 0, 0, _NO_STRIDES, _NO_STRIDES
         if k_out is not None:
-            kos, vos = _want(k_out, "k_out", rows, t, dev), _want(v_out, "v_out", rows, t, dev)
+            kos, vos = self._rows_out(k_out, v_out, rows)
             ka, va = k_out.data_ptr(), v_out.data_ptr()
-        call = _pack_write4(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                            *self._held(k4, v4, B), self._each(at, "at", B),
-                            self._each(n, "n", B), ka, va, kos[0], kos[1], kos[2], vos[0], vos[1], vos[2], B, T)
+        call = _pack_write4(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], *self._held(k4, v4, B),
+                            0 if at is None else self._each(at, "at", B), 0 if n is None else self._each(n, "n", B),
+                            ka, va, kos[0], kos[1], kos[2], vos[0], vos[1], vos[2], B, T)
         _check(lib().spike_proj_cache4_write(self.handle, call, _stream(stream)), "spike_proj_cache4_write")
 
     def read(self, k4, v4, k_out, v_out, at=None, n=None, stream=None):
         """The values of the slots at[b] + t into the tokens t < n[b] of k_out and
         v_out [B, T, Hkv, D] (at, n: int32 [B]; 0 and T where they are None)."""
-        if k_out is None:
-            raise ValueError("k_out: missing")
-        t, dev = self.dtype, self._device
+        if k_out is None or v_out is None:
+            raise ValueError("k_out, v_out: missing")
         B, T = k_out.shape[0], k_out.shape[1]
-        rows = (B, T, self.Hkv, self.D)
-        kos, vos = _want(k_out, "k_out", rows, t, dev), _want(v_out, "v_out", rows, t, dev)
-        call = _pack_read4(*self._held(k4, v4, B), self._each(at, "at", B),
-                           self._each(n, "n", B), k_out.data_ptr(), v_out.data_ptr(), kos[0], kos[1], kos[2],
-                           vos[0], vos[1], vos[2], B, T)
+        kos, vos = self._rows_out(k_out, v_out, (B, T, self.Hkv, self.D))
+        call = _pack_read4(*self._held(k4, v4, B), 0 if at is None else self._each(at, "at", B),
+                           0 if n is None else self._each(n, "n", B), k_out.data_ptr(), v_out.data_ptr(),
+                           kos[0], kos[1], kos[2], vos[0], vos[1], vos[2], B, T)
         _check(lib().spike_proj_cache4_read(self.handle, call, _stream(stream)), "spike_proj_cache4_read")
 
     def attend(self, q, k4, v4, lens, out, lse=None, other_out=None, other_lse=None, causal=True, scale=None,
@@ -883,14 +887,17 @@ class Cache4:
         these, and none sees a later one.  other_out and other_lse (float32
         [B, T, Hq]), what attention of the same queries over other entries gave
         (Cache.attend), are joined in; lse (float32 [B, T, Hq]) is optional."""
-        if q is None:
-            raise ValueError("q: missing")
-        t, dev = self.dtype, self._device
-        B, T = q.shape[0], q.shape[1]
+        if q is None or out is None or lens is None:
+            raise ValueError("q, out, lens: missing")
+        t, dev, shape = self.dtype, self._device, q.shape
+        B, T = shape[0], shape[1]
         rows = (B, T, self.Hq, self.D)
-        qs, os = _want(q, "q", rows, t, dev), _want(out, "out", rows, t, dev)
-        _want(lens, "lens", (B,), self._i32, dev)
-        la, oa, ola, oos = 0, 0, 0, (0, 0, 0)
+        qs, os = q.stride(), out.stride()
+        if (shape != rows or q.dtype is not t or q.get_device() != dev or qs[3] != 1
+                or out.shape != rows or out.dtype is not t or out.get_device() != dev or os[3] != 1):
+            _want(q, "q", rows, t, dev)
+            _want(out, "out", rows, t, dev)
+        la, oa, ola, oos = 0, 0, 0, _NO_STRIDES
         if lse is not None:
             la = self._sums(lse, "lse", rows)
         if (other_out is None) != (other_lse is None):
@@ -898,10 +905,18 @@ class Cache4:
         if other_out is not None:
             oos, oa = _want(other_out, "other_out", rows, t, dev), other_out.data_ptr()
             ola = self._sums(other_lse, "other_lse", rows)
-        call = _pack_attend4(q.data_ptr(), qs[0], qs[1], qs[2], *self._held(k4, v4, B),
-                             lens.data_ptr(), out.data_ptr(), os[0], os[1], os[2], la, oa, oos[0], oos[1], oos[2], ola,
+        call = _pack_attend4(q.data_ptr(), qs[0], qs[1], qs[2], *self._held(k4, v4, B), self._each(lens, "lens", B),
+                             out.data_ptr(), os[0], os[1], os[2], la, oa, oos[0], oos[1], oos[2], ola,
                              B, T, 1 if causal else 0, self._scale if scale is None else scale)
         _check(lib().spike_proj_cache4_attend(self.handle, call, _stream(stream)), "spike_proj_cache4_attend")
+
+    def _rows_out(self, k_out, v_out, rows):
+        kos, vos, t, dev = k_out.stride(), v_out.stride(), self.dtype, self._device
+        if (k_out.shape != rows or k_out.dtype is not t or k_out.get_device() != dev or kos[3] != 1
+                or v_out.shape != rows or v_out.dtype is not t or v_out.get_device() != dev or vos[3] != 1):
+            _want(k_out, "k_out", rows, t, dev)
+            _want(v_out, "v_out", rows, t, dev)
+        return kos, vos
 
     def _sums(self, x, name, rows):
         _want(x, name, rows[:3], self._f32, self._device)
