@@ -310,12 +310,54 @@ def test_joined_in_place(T, Hq, D):
     cache.close()
 
 
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c[:6])))
+def test_the_same_sequences_in_a_larger_cache(case):
+    """Where blocks share out the tiles of all sequences, not those of one."""
+    B, T, Hq, Hkv, D, _, lens = case
+    x = make(11, B, T, Hq, Hkv, D, 1100, lens, "bf16")
+    check(*x, run(*x))
+
+
+@pytest.mark.parametrize("C", [768, 769])
+@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (4, 4, 112), (1, 12, 64), (5, 6, 64), (3, 6, 32)], ids=str)
+def test_every_number_of_tiles(T, Hq, D, C):
+    """Fewer tiles than a block's warps, as many, more; joined in place."""
+    lens = [0, 1, 31, 32, 33, 64, 65, 96, 97, 128, 129, 160, 161, 224, 257, 767, 768]
+    q, k4, v4, lens = make(31, len(lens), T, Hq, 2, D, C, lens, "bf16")
+    check(q, k4, v4, lens, run(q, k4, v4, lens))
+    g = torch.Generator().manual_seed(32)
+    other = torch.randn(q.shape, generator=g).bfloat16(), 4 * torch.randn(q.shape[:3], generator=g)
+    cache = sp.Cache4(Hq, 2, D, C, max_T=T)
+    out, lse = other[0].to(DEV), other[1].to(DEV)
+    cache.attend(q.to(DEV), *(tuple(y.to(DEV) for y in x) for x in (k4, v4)), lens.to(DEV), out, lse=lse, other_out=out,
+                 other_lse=lse)
+    check(q, k4, v4, lens, (out.cpu(), lse.cpu()), other=other)
+    cache.close()
+
+
+@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (3, 6, 64), (4, 10, 64)], ids=str)
+@pytest.mark.parametrize("B", [1, 8, 20, 100])
+def test_few_and_many_parts_of_a_row(B, T, Hq, D):
+    x = make(33, B, T, Hq, 2, D, 1600, [1600 - 11 * b for b in range(B)], "bf16")
+    check(*x, run(*x))
+
+
+@pytest.mark.parametrize("T,Hq", [(1, 4), (2, 8), (7, 50)], ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_nan_value_of_no_weight_in_a_short_cache(T, Hq, D):
+    """As in a long cache, where the parts of one block meet."""
+    nan_beside_all_of_the_weight(T, Hq, D, 600)
+
+
 @pytest.mark.parametrize("T,Hq", [(1, 4), (2, 8), (4, 16), (7, 50)], ids=str)
 @pytest.mark.parametrize("D", [64, 128])
 def test_a_nan_value_stays_where_its_weight_vanishes(T, Hq, D):
     """A value's group is NaN; its weight beside another entry's, 128 nats above, is
     nothing in 32 bits, whatever workers have the two."""
-    C = 5000
+    nan_beside_all_of_the_weight(T, Hq, D, 5000)
+
+
+def nan_beside_all_of_the_weight(T, Hq, D, C):
     q = torch.ones(2, T, Hq, D, dtype=torch.float16)
     k4 = torch.zeros(2, C, 2, D // 2, dtype=torch.uint8), torch.full((2, C, 2, D // 16), 120, dtype=torch.uint8)
     v4 = torch.full((2, C, 2, D // 2), 0x22, dtype=torch.uint8), torch.full((2, C, 2, D // 16), 120, dtype=torch.uint8)
