@@ -107,6 +107,9 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
   tc_fence_after();
   const Line line = start.line;
   const uint32_t begin = start.begin, end = start.end, tmem = s_tmem;
+  // The first rows are those of warps 0 and 1, or, in the CTA that has the SM's other half of
+  // tensor memory, of warps 2 and 3: its softmax is at work where the first CTA's is not.
+  const int turn = tmem / kTmemCols % 2 * 2, lw = warp < 4 ? (warp + turn) & 3 : warp;
   Cursor<kTile, kUnitStart> cur = start.cur;
   const volatile int* stop = &s_abort;
   bool ok = true;
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       }
     }
     copy_wait<0>();
-  } else if (warp == 3) {
+  } else if (lw == 3) {
     // ------------------------------ products ----------------------------------------
     int it = 0, seg = 0;
     const uint32_t one = elect_one();
@@ -309,14 +312,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
   } else {
     // ------------------------------ softmax -----------------------------------------
     const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-    const int row = tid;
+    const int row = lw * 32 + lane;        // of the unit's; warp * 32 + lane: of the MMAs'
     int it = 0, seg = 0;
     for (; ok && cur.at < end; cur.next(p, begin, end)) {
       const bool empty = cur.nt == 0 && cur.at >= begin;
       if (skip() && !empty) continue;
       const int b = cur.b, n = cur.n, h = p.by_blocks(cur.u), block = cur.u - h * p.blocks;
       const int row0 = block * p.block_rows, rows = min(p.block_rows, p.R - row0), r = row0 + row;
-      const bool mine = row < rows, work = warp * 32 < rows;
+      const bool mine = row < rows, work = lw * 32 < rows;
       const int tok = p.by_G(mine ? r : 0);
       int2* const unit = p.units + (int64_t)b * p.Hkv * p.blocks + cur.u;
       if (empty) {
@@ -328,65 +331,54 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
         }
         continue;
       }
-      // The warp's rows of queries (the tiles before have been multiplied: their scores
-      // were here), `per` lanes a row.
-      float c2 = 0.f;
+      // The thread's row of queries (the tiles before have been multiplied: their scores
+      // were here).  A row a thread, not a row by several: the loads touch more lines, but
+      // a warp has a third of the instructions, and it has them to itself.
+      float c2 = fmaxf(p.c2, 0x1p-126f);   // (not 0, so that masked scores stay -infinity)
       if (work) {
-        constexpr int kPer = DK / 8, kAtOnce = 32 / kPer, kBatch = 32 / kAtOnce;
-        const int chunk = lane % kPer;
-        uint4 x[kBatch];
+        uint32_t in;
+        const int token = p.by_G(mine ? r : 0, &in);
+        const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch +
+                                                           token * p.c.q_token + (int64_t)(h * p.G + in) * p.c.q_head);
+        const int chunks = !mine ? 0 : PLAIN ? DK / 8 : p.D / 8, at = warp * 32 + lane;
+        uint4 x[DK / 8];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const int at = warp * 32 + i * kAtOnce + lane / kPer;
-          x[i] = make_uint4(0, 0, 0, 0);
-          if (at < rows && 8 * chunk < p.D) {
-            uint32_t in;
-            const int token = p.by_G(row0 + at, &in);
-            x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch +
-                                                        token * p.c.q_token + (int64_t)(h * p.G + in) * p.c.q_head) + chunk);
-          }
-        }
-        // 2^up brings a row's largest that is finite to 2^14 .. 2^15
-        int up[kBatch];
-        const auto largest = [&](bool all) {
-          uint32_t over = 0;
+        for (int i = 0; i < DK / 8; ++i) x[i] = i < chunks ? __ldg(from + i) : make_uint4(0, 0, 0, 0);
+        float by = 1.f;
+        if (p.bf16) {
+          const auto largest = [&](bool finite) {
+            uint32_t most[2] = {0, 0};
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            uint32_t most = 0;
+            for (int i = 0; i < DK / 8; ++i) {
+              const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t y = w[j] & 0x7fff7fffu;
-              most = __vmaxu2(most, all ? y : y & ~__vcmpgeu2(y, 0x7f807f80u));
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t y = w[j] & 0x7fff7fffu;
+                most[j % 2] = __vmaxu2(most[j % 2], finite ? y & ~__vcmpgeu2(y, 0x7f807f80u) : y);
+              }
             }
-            most = max(most & 0xffffu, most >> 16);
+            most[0] = __vmaxu2(most[0], most[1]);
+            return max(most[0] & 0xffffu, most[0] >> 16);
+          };
+          uint32_t most = largest(false);
+          if (most >= 0x7f80u) most = largest(true);
+          // 2^up brings the row's largest that is finite to 2^14 .. 2^15
+          const int up = min(14 - ((int)(most >> 7) - 127), 100);
+          by = __int_as_float((up + 127) << 23);
+          c2 = fmaxf(p.c2 * __int_as_float((127 - up) << 23), 0x1p-126f);
+        }
+        const f32x2 by2 = pair(by, by);
 #pragma unroll
-            for (int d = 1; d < kPer; d *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
-            over = max(over, most);
-            up[i] = min(14 - ((int)(most >> 7) - 127), 100);
-          }
-          return over >= 0x7f80u;
-        };
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) up[i] = 0;
-        if (p.bf16 && __any_sync(0xffffffffu, largest(true))) largest(false);
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-          const int at = warp * 32 + i * kAtOnce + lane / kPer;
+        for (int i = 0; i < DK / 8; ++i) {
           uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
           if (p.bf16) {
-            const float by = __int_as_float((up[i] + 127) << 23);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const float2 y = to_float(true, w[j]);
-              w[j] = pack_half2(y.x * by, y.y * by);
+              const float2 y = to_float(true, w[j]), z = halves(mul2(pair(y.x, y.y), by2));
+              w[j] = pack_half2(z.x, z.y);
             }
           }
-          *reinterpret_cast<uint4*>(sQ + (chunk >> 3) * kQBlock + at * 128 + ((chunk ^ at) & 7) * 16) =
-              make_uint4(w[0], w[1], w[2], w[3]);
-          // (its thread has the row's factor; not 0, so that masked scores stay -infinity)
-          const int up_here = __shfl_sync(0xffffffffu, up[i], (lane - i * kAtOnce) * kPer & 31);
-          if (lane / kAtOnce == i) c2 = fmaxf(p.c2 * __int_as_float((127 - up_here) << 23), 0x1p-126f);
+          *reinterpret_cast<uint4*>(sQ + (i >> 3) * kQBlock + at * 128 + ((i ^ at) & 7) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
         }
         fence_async_shared();
       }
@@ -480,25 +472,37 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
         s_poison[seg & 3][row] = 0;
         const float base = lim == -INFINITY ? -INFINITY : -nb;
         const float other = mine && whole ? other_of(p, b, h, r) : -INFINITY;
-        const int64_t at = slot * p.slot_rows + row;
-        if (mine && !whole) p.slot_ml[at] = make_float4(base, l, rl, 0.f);
+        float* to = p.slot_o + (slot * p.slot_rows + row) * DK;
+        if (mine && !whole) p.slot_ml[slot * p.slot_rows + row] = make_float4(base, l, rl, 0.f);
+        if (whole || __any_sync(0xffffffffu, poison != 0)) {
 #pragma unroll 1
-        for (int i = 0; i < DK / 16; ++i) {
-          uint32_t raw[16];
-          tmem_ld16_issue(lanes + kTmemO + 16 * i, raw);
-          tmem_ld_wait();
-          reg_pin(raw);
-          float o[16];
+          for (int i = 0; i < DK / 16; ++i) {
+            uint32_t raw[16];
+            tmem_ld16_issue(lanes + kTmemO + 16 * i, raw);
+            tmem_ld_wait();
+            reg_pin(raw);
+            float o[16];
 #pragma unroll
-          for (int x = 0; x < 16; ++x) o[x] = poison >> i & 1u ? NAN : __uint_as_float(raw[x]);
-          if (mine) {
-            if (whole) {
-              finish<16>(p, b, h, r, 16 * i, base, l, rl, o, other, i == 0);
-            } else {
-              float* to = p.slot_o + at * DK + 16 * i;
+            for (int x = 0; x < 16; ++x) o[x] = poison >> i & 1u ? NAN : __uint_as_float(raw[x]);
+            if (mine) {
+              if (whole) {
+                finish<16>(p, b, h, r, 16 * i, base, l, rl, o, other, i == 0);
+              } else {
 #pragma unroll
-              for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(to + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+                for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(to + 16 * i + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+              }
             }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < DK; i += 32) {
+            uint32_t o[32];
+            tmem_ld32_issue(lanes + kTmemO + i, o);
+            tmem_ld_wait();
+            reg_pin(o);
+            if (mine)
+#pragma unroll
+              for (int x = 0; x < 32; x += 4) *reinterpret_cast<uint4*>(to + i + x) = make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]);
           }
         }
       }
