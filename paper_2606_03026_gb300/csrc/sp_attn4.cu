@@ -184,7 +184,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kern
     begin = start.begin;
     end = start.end;
     cur = start.cur;
-    __syncthreads();
     if (begin >= end) return;
   }
   [[maybe_unused]] const Cursor<kTile, kStart> unit = cur;       // (SMALL)

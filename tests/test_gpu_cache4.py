@@ -383,6 +383,14 @@ def test_more_units_than_the_gpu_holds():
     check(*x, run(*x))
 
 
+@pytest.mark.parametrize("B", [5, 31, 127, 128, 129, 131])
+@pytest.mark.parametrize("T,Hq", [(1, 2), (3, 12)], ids=str)
+def test_numbers_of_sequences(B, T, Hq):
+    lens = [(37 * b) % 200 if b % 3 else 0 for b in range(B)]
+    x = make(34, B, T, Hq, 2, 64, 800, lens, "bf16")
+    check(*x, run(*x))
+
+
 def test_one_entry_with_all_of_the_weight_comes_out_exactly():
     q, k4, v4, lens = make(21, 2, 1, 4, 2, 128, 500, [500, 333], "fp16")
     k4[1][:, 250] = 120                    # a scale of 2, above all others
