@@ -17,6 +17,9 @@ struct Attend4Params {
   int32_t Hkv, G, D, capacity, R;
   int32_t blocks, block_rows;              // units of a (sequence, K/V head); rows of one
   Divide by_blocks, by_G;
+  int32_t heads;                           // that so many workers walk side by side (1, or Hkv)
+  int32_t on_line;                         // units of a sequence on the line
+  Divide by_heads, by_on_line;
   int32_t slot_rows;                       // rows of a slot
   int32_t bf16;
   float c2;                                // scale * log2 e
@@ -116,12 +119,19 @@ struct Line {
     more = all - each * workers;
   }
   __device__ __forceinline__ uint32_t first(uint32_t w) const { return w * each + min(w, more); }
-  __device__ __forceinline__ int owner(uint32_t at) const {
+  __device__ __forceinline__ uint32_t owner(uint32_t at) const {
     const uint32_t long_ones = more * (each + 1);
-    return (int)(at < long_ones ? at / (each + 1) : more + (at - long_ones) / each);
+    return at < long_ones ? at / (each + 1) : more + (at - long_ones) / each;
   }
 };
 __device__ __forceinline__ int used(const Attend4Params& p, int b) { return min(max(__ldg(p.c.lens + b), 0), p.capacity); }
+
+// The number of the worker that has place `at` of a unit's line, beside worker `me`.
+__device__ __forceinline__ int worker_of(const Attend4Params& p, const Line& line, uint32_t at, int me) {
+  uint32_t head = 0;
+  if (p.heads > 1) p.by_heads(me, &head);
+  return (int)(line.owner(at) * p.heads + head);
+}
 
 // A worker's (a warp, or a CTA) way along the line: unit (b, u), its entries, its tiles j .. j1 of the
 // worker's.  A unit takes START + nt on the line from `at` on; tile j is at + START + j,
@@ -138,8 +148,10 @@ struct Cursor {
   }
   __device__ __forceinline__ void next(const Attend4Params& p, uint32_t begin, uint32_t end) {
     at += START + nt;
-    if (++u == p.Hkv * p.blocks) {
-      u = 0;
+    uint32_t rest;
+    p.by_on_line(++u, &rest);
+    if (rest == 0) {
+      u -= p.on_line;
       ++b;
     }
     if (at < end) {
@@ -165,13 +177,20 @@ template <int TILE, int START, int THREADS>
 __device__ __forceinline__ Start<TILE, START> start_of(const Attend4Params& p, uint32_t* before, int me, uint32_t most) {
   __shared__ uint32_t s_scan[THREADS / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t per_seq = p.Hkv * p.blocks;
+  const uint32_t per_seq = p.on_line;
   Start<TILE, START> s;
+  // a worker of several walks with the others of its number's `heads`, of another head
+  uint32_t head = 0;
+  if (p.heads > 1) {
+    me = p.by_heads(me, &head);
+    most = p.by_heads(most);
+  }
   const auto set_off = [&](int b, uint32_t at, int n) {
     const uint32_t cost = START + ceil_div(n, TILE);
     s.cur.b = b;
-    s.cur.u = (int)((s.begin - at) / cost);
-    s.cur.at = at + s.cur.u * cost;
+    const uint32_t u = (s.begin - at) / cost;
+    s.cur.u = (int)(head * p.blocks + u);
+    s.cur.at = at + u * cost;
     s.cur.n = n;
     s.cur.settle(s.begin, s.end);
   };

@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       const bool begins = cur.j == 0, whole = begins && cur.j1 == cur.nt;
       const int64_t slot = 2 * (int64_t)me + (cur.at >= begin ? 1 : 0);          // (begun before, or here)
       if (row == 0 && begins)
-        *unit = make_int2(whole ? -1 : (int)slot, whole ? me : line.owner(cur.at + kUnitStart + cur.nt - 1));
+        *unit = make_int2(whole ? -1 : (int)slot, whole ? me : worker_of(p, line, cur.at + kUnitStart + cur.nt - 1, me));
       ok = all(wait(p, &bars.o_full, seg & 1, stop));
       if (!ok) break;
       tc_fence_after();

@@ -310,12 +310,24 @@ def test_joined_in_place(T, Hq, D):
     cache.close()
 
 
+@pytest.mark.parametrize("layout", ["entries", "heads"])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c[:6])))
-def test_the_same_sequences_in_a_larger_cache(case):
+def test_the_same_sequences_in_a_larger_cache(case, layout):
     """Where blocks share out the tiles of all sequences, not those of one."""
     B, T, Hq, Hkv, D, _, lens = case
     x = make(11, B, T, Hq, Hkv, D, 1100, lens, "bf16")
-    check(*x, run(*x))
+    check(*x, run(*x, layout=layout))
+
+
+@pytest.mark.parametrize("layout", ["entries", "heads"])
+@pytest.mark.parametrize("Hq,Hkv", [(7, 7), (40, 20), (150, 150), (400, 200), (480, 60), (500, 500)])
+def test_numbers_of_heads(Hq, Hkv, layout):
+    """Workers that are left over where so many walk side by side; more heads than workers."""
+    x = make(35, 3, 1, Hq, Hkv, 16, 800, [800, 33, 401], "bf16")
+    check(*x, run(*x, layout=layout))
+    if Hq < 500:
+        x = make(36, 2, 9, Hq, Hkv, 16, 80, [80, 77], "bf16")
+        check(*x, run(*x, layout=layout))
 
 
 @pytest.mark.parametrize("C", [768, 769])
