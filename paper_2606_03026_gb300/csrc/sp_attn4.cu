@@ -614,9 +614,9 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
   if (unit.x < 0) return;
   const float other = other_of(p, b, h, r);
   const int first = unit.x >> 1;
-  const int parts = (int)p.by_heads(max(0, unit.y - first)) + 1;
+  const int parts = (int)p.by_side(max(0, unit.y - first)) + 1;
   RowSum<DK> a = sum_parts<DK, WPR, 8>(p, in, warp, parts,
-                                       [&](int i) { return i == 0 ? (int64_t)unit.x : 2 * (first + (int64_t)i * p.heads); });
+                                       [&](int i) { return i == 0 ? (int64_t)unit.x : 2 * (first + (int64_t)i * p.side); });
   if constexpr (WPR > 1) {
     __shared__ float s_ml[WPR][3], s_o[WPR][DK];
 #pragma unroll
@@ -665,9 +665,14 @@ cudaError_t launch_t(const Params& p, int dev, int grid, cudaStream_t s) {
   return launch_pdl(attend4_kernel<DK, NT, PLAIN, SMALL>, dim3((unsigned)grid), dim3(kThreads), bytes, s, p);
 }
 
-// How the R query rows of a K/V head are taken: by warps or by CTAs (a warp's
-// registers hold O of 8 rows of 128-wide heads, of 16 of 64-wide ones), in units of as
-// many rows, workers.
+// How the R query rows of a K/V head are taken: by warps or by CTAs, in units of as many
+// rows, workers.  A warp's registers hold O of 8 rows of 128-wide heads, of 16 of 64-wide
+// ones, and it decodes an entry for these alone; the CTAs of attend4_rows_kernel decode it
+// for up to 96, in a pipeline that takes as long for one row as for 64.  us by warps and by CTAs:
+// 64-wide heads, 32 sequences up to 8000, 6 rows 25, 49; 15 rows 36, 50; 16 rows of 64
+// sequences up to 16384 131, 218; 32 rows (two units of 16 side by side) 248, 225.  128-wide
+// heads, 64 sequences up to 16384, 8 rows 131, 262; 12 rows (two units) 245, 264; 24 (three)
+// 364, 271; 16 sequences up to 6000, 16 rows 34, 37; 24 rows 45, 38.
 struct Plan {
   bool wide, plain, by_ctas;
   int blocks, rows, NT, workers;
@@ -676,8 +681,8 @@ Plan plan_of(int R, int D, int sms) {
   Plan x;
   x.wide = D > 64;
   x.plain = D == (x.wide ? 128 : 64);
-  x.by_ctas = R > (x.wide ? 8 : 16);
-  x.blocks = x.by_ctas ? ceil_div(R, kRowsMost4) : 1;
+  x.by_ctas = R > 16;
+  x.blocks = ceil_div(R, x.by_ctas ? kRowsMost4 : x.wide ? 8 : 16);
   x.rows = ceil_div(R, x.blocks);
   x.NT = ceil_div(x.rows, 8);
   x.workers = x.by_ctas ? rows4_workers(sms) : sms * ctas_per_sm(x.NT, x.plain) * kWarps;
@@ -721,16 +726,16 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.block_rows = plan.rows;
   p.by_blocks = Divide(p.blocks);
   p.by_G = Divide(p.G);
-  // Where an entry's heads lie side by side, as many workers read them at about the same time,
-  // while memory's 64 bytes that several heads' scales are in are in the L2 (64 sequences of
-  // 4096 to 16384 entries, 8 heads: 136 us instead of 262, 113 by bytes; 64 chats, 4 heads: 27.2
-  // instead of 29.9; not where more than a tenth of the workers would be left over).
-  const bool side_by_side = s.Hkv > 1 && c.k4.head < c.k4.entry && c.v4.head < c.v4.entry &&
-                            plan.workers % s.Hkv * 10 <= plan.workers;
-  p.heads = side_by_side ? s.Hkv : 1;
-  p.on_line = side_by_side ? p.blocks : s.Hkv * p.blocks;
-  p.by_heads = Divide(p.heads);
-  p.by_on_line = Divide(p.on_line);
+  // The units of the same entries' query rows walk side by side, and where an entry's heads lie
+  // side by side theirs too: memory's 64 bytes that several heads' scales are in are then in
+  // the L2 (64 sequences of 4096 to 16384 entries, 8 heads: 136 us instead of 262, 113 by
+  // bytes; 64 chats, 4 heads: 27.2 instead of 29.9).  Not where more than a tenth of the workers
+  // would be left over.
+  const bool adjacent = c.k4.head < c.k4.entry && c.v4.head < c.v4.entry;
+  const auto fits = [&](int side) { return plan.workers % side * 10 <= plan.workers; };
+  p.side = adjacent && fits(s.Hkv * p.blocks) ? s.Hkv * p.blocks : fits(p.blocks) ? p.blocks : 1;
+  p.on_line = s.Hkv * p.blocks / p.side;
+  p.by_side = Divide(p.side);
   p.bf16 = s.dtype == SP_BF16;
   p.c2 = c.scale * kLog2e;
   p.err = err;

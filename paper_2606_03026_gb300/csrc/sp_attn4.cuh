@@ -17,9 +17,9 @@ struct Attend4Params {
   int32_t Hkv, G, D, capacity, R;
   int32_t blocks, block_rows;              // units of a (sequence, K/V head); rows of one
   Divide by_blocks, by_G;
-  int32_t heads;                           // that so many workers walk side by side (1, or Hkv)
-  int32_t on_line;                         // units of a sequence on the line
-  Divide by_heads, by_on_line;
+  int32_t side;                            // workers that walk side by side, each in units of its own
+  int32_t on_line;                         // places of a sequence's units on the line: Hkv blocks / side
+  Divide by_side;
   int32_t slot_rows;                       // rows of a slot
   int32_t bf16;
   float c2;                                // scale * log2 e
@@ -128,9 +128,9 @@ __device__ __forceinline__ int used(const Attend4Params& p, int b) { return min(
 
 // The number of the worker that has place `at` of a unit's line, beside worker `me`.
 __device__ __forceinline__ int worker_of(const Attend4Params& p, const Line& line, uint32_t at, int me) {
-  uint32_t head = 0;
-  if (p.heads > 1) p.by_heads(me, &head);
-  return (int)(line.owner(at) * p.heads + head);
+  uint32_t which = 0;
+  if (p.side > 1) p.by_side(me, &which);
+  return (int)(line.owner(at) * p.side + which);
 }
 
 // A worker's (a warp, or a CTA) way along the line: unit (b, u), its entries, its tiles j .. j1 of the
@@ -148,10 +148,9 @@ struct Cursor {
   }
   __device__ __forceinline__ void next(const Attend4Params& p, uint32_t begin, uint32_t end) {
     at += START + nt;
-    uint32_t rest;
-    p.by_on_line(++u, &rest);
-    if (rest == 0) {
-      u -= p.on_line;
+    u += p.side;
+    if (u >= p.Hkv * p.blocks) {
+      u -= p.Hkv * p.blocks;
       ++b;
     }
     if (at < end) {
@@ -179,17 +178,16 @@ __device__ __forceinline__ Start<TILE, START> start_of(const Attend4Params& p, u
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t per_seq = p.on_line;
   Start<TILE, START> s;
-  // a worker of several walks with the others of its number's `heads`, of another head
-  uint32_t head = 0;
-  if (p.heads > 1) {
-    me = p.by_heads(me, &head);
-    most = p.by_heads(most);
+  uint32_t which = 0;                      // of those that walk side by side
+  if (p.side > 1) {
+    me = p.by_side(me, &which);
+    most = p.by_side(most);
   }
   const auto set_off = [&](int b, uint32_t at, int n) {
     const uint32_t cost = START + ceil_div(n, TILE);
     s.cur.b = b;
     const uint32_t u = (s.begin - at) / cost;
-    s.cur.u = (int)(head * p.blocks + u);
+    s.cur.u = (int)(u * p.side + which);
     s.cur.at = at + u * cost;
     s.cur.n = n;
     s.cur.settle(s.begin, s.end);

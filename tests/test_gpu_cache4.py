@@ -331,7 +331,7 @@ def test_numbers_of_heads(Hq, Hkv, layout):
 
 
 @pytest.mark.parametrize("C", [768, 769])
-@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (4, 4, 112), (1, 12, 64), (5, 6, 64), (3, 6, 32)], ids=str)
+@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (4, 4, 112), (2, 14, 128), (1, 12, 64), (5, 6, 64), (3, 6, 32)], ids=str)
 def test_every_number_of_tiles(T, Hq, D, C):
     """Fewer tiles than a block's warps, as many, more; joined in place."""
     lens = [0, 1, 31, 32, 33, 64, 65, 96, 97, 128, 129, 160, 161, 224, 257, 767, 768]
@@ -347,7 +347,7 @@ def test_every_number_of_tiles(T, Hq, D, C):
     cache.close()
 
 
-@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (3, 6, 64), (4, 10, 64)], ids=str)
+@pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (2, 12, 128), (3, 6, 64), (4, 10, 64)], ids=str)
 @pytest.mark.parametrize("B", [1, 8, 20, 100])
 def test_few_and_many_parts_of_a_row(B, T, Hq, D):
     x = make(33, B, T, Hq, 2, D, 1600, [1600 - 11 * b for b in range(B)], "bf16")
