@@ -742,7 +742,8 @@ sp_status spike_proj_verify(const sp_verify *call, sp_stream_t stream);
  * strides (of dimensions longer than 1) are multiples of the largest power of two
  * that divides D / 2, at most 16, for codes, and D / 16 for scales (SP_EALIGN):
  * rows without gaps are.  Storing the heads before the entries (head strides above
- * entry strides) keeps what one head reads together.
+ * entry strides) keeps what one head reads together; attention over the other order
+ * takes up to a tenth longer.
  *
  * spike_proj_cache4_create: the handle owns workspace (50 MB at most) and no entry of
  *   any cache.  1 <= max_T <= SPIKE_PROJ_CACHE_MAX_T, 1 <= Hq <=
@@ -766,8 +767,8 @@ sp_status spike_proj_cache4_create(sp_cache4_t *cache, int32_t max_T, int32_t Hq
 sp_status spike_proj_cache4_destroy(sp_cache4_t cache);
 
 /* Synchronises the stream and returns SP_EKERNEL, once, when a kernel of the
- * handle gave up on a wait since the last call (attend calls of many query rows
- * wait; others do not). */
+ * handle gave up on a wait since the last call (attend calls of more than 16 query
+ * rows of a K/V head wait; others do not). */
 sp_status spike_proj_cache4_status(sp_cache4_t cache, sp_stream_t stream);
 
 /* spike_proj_cache4_write: token t < n[b] of sequence b goes to slot at[b] + t of its
@@ -851,8 +852,8 @@ sp_status spike_proj_cache4_read(sp_cache4_t cache, const sp_read4 *call,
  *              lse; nothing else may overlap the outputs.
  *   scale      finite and > 0 (SP_EINVAL).
  * q, out and other_out: as 16-bit tensors of spike_proj_cache4_write.  A T above
- * max_T, or a call of 2^31 tiles (32 entries for up to 32 query rows of one K/V head)
- * and more, were all caches full: SP_ERANGE.
+ * max_T, or a call of 2^31 tiles and more, were all caches full (32 entries of one K/V
+ * head, for 8 to 96 of its query rows): SP_ERANGE.
  * Errors: SP_EINVAL, SP_EALIGN, SP_ERANGE, SP_EDEVICE, SP_ECUDA. */
 typedef struct sp_attend4 {
     const void *q;                        /* [B][T][Hq][D] */

@@ -19,13 +19,23 @@
 //                 t, t + 4, t + 8, t + 12
 // P^T comes from S^T by transposing 8 x 8 blocks between the threads.
 //
-// Work: the entries of all units (sequence, K/V head, up to 32 rows) are one line of
+// Work: the entries of all units (sequence, K/V head, up to 8 or 16 rows) are one line of
 // tiles of 32, which all warps share out evenly, whatever the lengths (which only
 // the device knows).  A warp works by itself: its tiles come through a ring of its
 // own in shared memory (cp.async), unit after unit without a pause, and it keeps
 // its own maximum and sums.  A unit that one warp has the whole of is written out
 // by it; of others each warp leaves its part in the workspace, and merge4_kernel
-// adds them up, in the order of the tiles.
+// adds them up, in the order of the tiles.  (Warps, not CTAs, so that no barrier stands
+// between a tile and the next: with tiles shared by a CTA's warps only one CTA had room
+// on an SM, and 64 chats took 59 us.)
+//
+// What bounds it: for long caches memory.  64 sequences of 4096 to 16384 entries, 32/8
+// heads of 128, 756 MB: 129 us, 5.9 TB/s (88 % of a copy's rate); at the same time 61 % of the
+// issue slots, as 16 entries of a head take about 310 warp instructions (64 conversions of
+// code pairs, 64 products with scales, 17 of the matrix unit), which is what bounds 16 rows
+// (two walks over the same entries, 245 us).  For short ones the start (places on the line
+// 1.6 us, first tiles there at 5 to 9) and the merge with its launch (4): 64 chats of 2048
+// entries on average, 76 MB, 27 us.
 #include <type_traits>
 
 #include "sp_attn4.cuh"

