@@ -124,7 +124,7 @@ struct Line {
     return at < long_ones ? at / (each + 1) : more + (at - long_ones) / each;
   }
 };
-__device__ __forceinline__ int used(const Attend4Params& p, int b) { return min(max(__ldg(p.c.lens + b), 0), p.capacity); }
+__device__ __forceinline__ int used(const Attend4Params& p, int b) { return min(max(p.c.lens[b], 0), p.capacity); }
 
 // The number of the worker that has place `at` of a unit's line, beside worker `me`.
 __device__ __forceinline__ int worker_of(const Attend4Params& p, const Line& line, uint32_t at, int me) {
@@ -280,7 +280,7 @@ __device__ __forceinline__ void load_query(const Attend4Params& p, int b, int h,
                            (int64_t)(h * p.G + in_head) * p.c.q_head + t * (DK / 4);
 #pragma unroll
     for (int j = 0; j < DK / 16; ++j)
-      if (t * (DK / 4) + 4 * j < p.D) x[j] = __ldg(reinterpret_cast<const uint2*>(from + 4 * j));
+      if (t * (DK / 4) + 4 * j < p.D) x[j] = *reinterpret_cast<const uint2*>(from + 4 * j);
   }
 }
 // These as the instructions take them, in half precision.  Returns what the row's scores
@@ -327,10 +327,10 @@ struct ScaleRow {
       for (int i = 0; i < DK / 64; ++i) b[i] = 0;
       if (!there) return;
       if constexpr (DK == 128) {
-        const uint2 x = __ldg(reinterpret_cast<const uint2*>(from));
+        const uint2 x = *reinterpret_cast<const uint2*>(from);
         b[0] = x.x, b[DK / 64 - 1] = x.y;
       } else {
-        b[0] = __ldg(reinterpret_cast<const uint32_t*>(from));
+        b[0] = *reinterpret_cast<const uint32_t*>(from);
       }
     } else {
       const bool even = groups % 2 == 0;
@@ -338,9 +338,9 @@ struct ScaleRow {
       for (int i = 0; i < DK / 16; ++i) {
         b[i] = 0;
         if (even) {
-          if (2 * i < groups && there) b[i] = __ldg(reinterpret_cast<const uint16_t*>(from) + i);
+          if (2 * i < groups && there) b[i] = reinterpret_cast<const uint16_t*>(from)[i];
         } else if (i < groups && there) {
-          b[i] = __ldg(from + i);
+          b[i] = from[i];
         }
       }
     }

@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
         const int chunks = !mine ? 0 : PLAIN ? DK / 8 : p.D / 8, at = warp * 32 + lane;
         uint4 x[DK / 8];
 #pragma unroll
-        for (int i = 0; i < DK / 8; ++i) x[i] = i < chunks ? __ldg(from + i) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < DK / 8; ++i) x[i] = i < chunks ? from[i] : make_uint4(0, 0, 0, 0);
         float by = 1.f;
         if (p.bf16) {
           const auto largest = [&](bool finite) {

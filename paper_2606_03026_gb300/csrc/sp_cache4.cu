@@ -60,8 +60,8 @@ __device__ __forceinline__ bool place_of(const Params& p, Place* x) {
   x->step = p.tokens;
   const int first = chunk * (p.tokens * kItems * kTurns);
   x->t = first + row;
-  x->end = min(p.n ? min(max(__ldg(p.n + x->b), 0), p.T) : p.T, first + p.tokens * kItems * kTurns);
-  x->at = p.at ? __ldg(p.at + x->b) : 0;
+  x->end = min(p.n ? min(max(p.n[x->b], 0), p.T) : p.T, first + p.tokens * kItems * kTurns);
+  x->at = p.at ? p.at[x->b] : 0;
   return row < p.tokens && column < p.columns && x->t < x->end;
 }
 
@@ -232,8 +232,8 @@ __global__ void __launch_bounds__(kThreads) read4_kernel(const __grid_constant__
   for (int i = 0; i < kAll; ++i) {
     there[i] = x.t + i * x.step < x.end && slot >= 0 && slot < p.capacity;
     if (there[i]) {
-      c[i] = __ldg(reinterpret_cast<const uint2*>(codes));
-      byte[i] = __ldg(scales);
+      c[i] = *reinterpret_cast<const uint2*>(codes);
+      byte[i] = *scales;
     }
     slot += x.step;
     codes += codes_step;

@@ -510,6 +510,42 @@ def test_a_decode_as_it_is_used():
     prefix.close()
 
 
+@pytest.mark.parametrize("layout", ["entries", "heads"])
+@pytest.mark.parametrize("T,Hq,C", [(1, 4, 200), (1, 4, 1000), (4, 12, 1000)], ids=str)
+def test_back_to_back_calls_see_each_others_results(T, Hq, C, layout):
+    """Writes over the same slots, attention in two parts, reads, nothing between them."""
+    B, Hkv, D, steps = 24, 2, 128, 12
+    g = torch.Generator(device=DEV).manual_seed(37)
+    new = lambda *s: torch.randn(*s, generator=g, device=DEV).bfloat16()     # noqa: E731
+    cache = sp.Cache4(Hq, Hkv, D, C, max_T=T)
+    k4, v4 = (tuple(place(y, layout) for y in held_entries(torch.Generator().manual_seed(s), B, C, Hkv, D)) for s in (38, 39))
+    lens = torch.randint(T, C + 1, (B,), generator=g, device=DEV, dtype=torch.int32)
+    at, half = lens - T, lens // 2
+    k, v, q = new(steps, B, T, Hkv, D), new(steps, B, T, Hkv, D), new(steps, B, T, Hq, D)
+
+    def calls(wait):
+        out, first = torch.zeros_like(q), torch.zeros_like(q)
+        lse, lse1 = (torch.zeros(steps, B, T, Hq, device=DEV) for _ in range(2))
+        kb, vb = torch.zeros_like(k), torch.zeros_like(v)
+        torch.cuda.synchronize()
+        for i in range(steps):
+            for call in (lambda: cache.write(k[i], v[i], k4, v4, at=at),
+                         lambda: cache.attend(q[i], k4, v4, half, first[i], lse=lse1[i], causal=False),
+                         lambda: cache.attend(q[i], k4, v4, lens, out[i], lse=lse[i], other_out=first[i], other_lse=lse1[i]),
+                         lambda: cache.read(k4, v4, kb[i], vb[i], at=at)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return [x.cpu() for x in (out, first, lse, lse1, kb, vb)]
+
+    want = calls(True)
+    for _ in range(3):
+        for x, y in zip(calls(False), want):
+            assert torch.equal(x, y)
+    cache.close()
+
+
 def test_replayed_from_graphs_on_another_stream():
     """Two graphs on one handle, replayed in turn on new inputs."""
     x = [make(27 + i, 2, 1, 4, 2, 128, 3000, [3000, 40 + i], "bf16") for i in range(3)]
