@@ -341,8 +341,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kern
 
     // ---- the unit's tiles -------------------------------------------------------
     float o[NT][KS][4], sum_r[NT][4];
-    f32x2 l[NT], base[NT];                 // of the rows 2t, 2t + 1: sums, references (negative)
-    float lim[NT][2];                      // from where on the reference follows the maximum
+    f32x2 l[NT], minus_m[NT];              // of the rows 2t, 2t + 1: sums, the maximum that the reference has
+    float lag[NT][2];                      // from how far above it on that follows: kLag, at first from anywhere
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
 #pragma unroll
@@ -351,8 +351,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kern
         for (int e = 0; e < 4; ++e) o[i][j][e] = 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum_r[i][e] = 0.f;
-      lim[i][0] = lim[i][1] = -INFINITY;
-      l[i] = base[i] = pair(0.f, 0.f);
+      lag[i][0] = lag[i][1] = -INFINITY;
+      l[i] = minus_m[i] = pair(0.f, 0.f);
     }
 #pragma unroll 1
     for (int tile = cur.j; tile < cur.j1; ++tile) {
@@ -450,26 +450,26 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kern
           top[i][e] = fmaxf(s[0][i][e], s[0][i][e + 2]);
 #pragma unroll
           for (int sub = 1; sub < SB; ++sub) top[i][e] = fmaxf(top[i][e], fmaxf(s[sub][i][e], s[sub][i][e + 2]));
-          top[i][e] *= c2[i][e];
-          grow |= top[i][e] > lim[i][e];
+          grow |= (top[i][e] + (e ? halves(minus_m[i]).y : halves(minus_m[i]).x)) * c2[i][e] > lag[i][e];
         }
       if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          float a[2], nb[2] = {halves(base[i]).x, halves(base[i]).y};
+          float a[2], m[2] = {halves(minus_m[i]).x, halves(minus_m[i]).y};
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             float x = top[i][e];
 #pragma unroll
             for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
             a[e] = 1.f;
-            if (x > lim[i][e]) {
-              a[e] = lim[i][e] == -INFINITY ? 0.f : ex2((kLift - x) - nb[e]);
-              lim[i][e] = x + kLag;
-              nb[e] = kLift - x;
+            const float by = (x + m[e]) * c2[i][e];
+            if (by > lag[i][e]) {
+              a[e] = lag[i][e] == -INFINITY ? 0.f : ex2(-by);
+              lag[i][e] = kLag;
+              m[e] = -x;
             }
           }
-          base[i] = pair(nb[0], nb[1]);
+          minus_m[i] = pair(m[0], m[1]);
           l[i] = fma2(l[i], pair(a[0], a[1]), pair(0.f, 0.f));
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum_r[i][e] *= a[e & 1];
@@ -482,13 +482,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kern
       uint32_t pb[SB][NT][2];
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
-        const f32x2 by = pair(c2[i][0], c2[i][1]);
+        const f32x2 by = pair(c2[i][0], c2[i][1]), lift = pair(kLift, kLift);
         f32x2 sum[2 * SB];
 #pragma unroll
         for (int sub = 0; sub < SB; ++sub)
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const float2 x = halves(fma2(pair(s[sub][i][2 * half], s[sub][i][2 * half + 1]), by, base[i]));
+            // (the difference first, which is exact near the maximum: of large scores the product
+            // is off by more than half precision has room for)
+            const float2 x = halves(fma2(add2(pair(s[sub][i][2 * half], s[sub][i][2 * half + 1]), minus_m[i]), by, lift));
             const float2 y = make_float2(ex2(x.x), ex2(x.y));
             sum[2 * sub + half] = pair(y.x, y.y);
             pb[sub][i][half] = transpose8(pack_half2(y.x, y.y));
@@ -573,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kern
 #pragma unroll
             for (int j = 0; j < DK / 8; ++j) v[j] = NAN;
         }
-        const float ref = lim[i][e] == -INFINITY ? -INFINITY : -(e ? halves(base[i]).y : halves(base[i]).x);
+        const float ref = lag[i][e] == -INFINITY ? -INFINITY : fmaf(-(e ? halves(minus_m[i]).y : halves(minus_m[i]).x), c2[i][e], -kLift);
         if (r < rows) {
           if (whole) {
             finish<DK / 8>(p, b, h, row0 + r, g * (DK / 8), ref, x, sum_r[i][e], v, other[i][e], g == 0);

@@ -392,7 +392,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars.q_full);
       const int far = p.c.causal ? n - (p.c.T - 1 - tok) : n;  // entries that the row sees
-      float lim = -INFINITY, nb = 0.f, l = 0.f, rl = 0.f;      // from where on the reference (negative) follows; sums
+      // how far above the maximum that the reference has it follows (at first from anywhere), that maximum; sums
+      float lag = -INFINITY, m = 0.f, l = 0.f, rl = 0.f;
       for (int j = cur.j; j < cur.j1; ++j, ++it) {
         ok = all(wait(p, &bars.s_full[it & 1], it >> 1 & 1, stop));
         if (!ok) break;
@@ -414,14 +415,14 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int i = 0; i < kTile; ++i) mx[i % 4] = fmaxf(mx[i % 4], __uint_as_float(v[i / 32][i % 32]));
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c2;
-          const bool grow = top > lim;
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), above = (top - m) * c2;
+          const bool grow = above > lag;
           if (__any_sync(0xffffffffu, grow)) {
             float a = 1.f;
             if (grow) {
-              a = lim == -INFINITY ? 0.f : ex2((kLift - top) - nb);
-              lim = top + kLag;
-              nb = kLift - top;
+              a = lag == -INFINITY ? 0.f : ex2(-above);
+              lag = kLag;
+              m = top;
             }
             l *= a;
             rl *= a;
@@ -443,13 +444,15 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
           }
           f32x2 sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
           float rsum[4] = {};
-          const f32x2 by = pair(c2, c2), ref = pair(nb, nb);
+          const f32x2 by = pair(c2, c2), minus_m = pair(-m, -m), lift = pair(kLift, kLift);
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             uint32_t pk[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float2 x = halves(fma2(pair(__uint_as_float(v[g][2 * i]), __uint_as_float(v[g][2 * i + 1])), by, ref));
+              // (the difference first: see attend4_kernel)
+              const float2 x =
+                  halves(fma2(add2(pair(__uint_as_float(v[g][2 * i]), __uint_as_float(v[g][2 * i + 1])), minus_m), by, lift));
               const float2 y = make_float2(ex2(x.x), ex2(x.y));
               pk[i] = pack_half2(y.x, y.y);
               sum[i % 2] = add2(sum[i % 2], pair(y.x, y.y));
@@ -477,7 +480,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       if (work) {
         const uint32_t poison = s_poison[seg & 3][row];
         s_poison[seg & 3][row] = 0;
-        const float base = lim == -INFINITY ? -INFINITY : -nb;
+        const float base = lag == -INFINITY ? -INFINITY : fmaf(m, c2, -kLift);
         const float other = mine && whole ? other_of(p, b, h, r) : -INFINITY;
         float* to = p.slot_o + (slot * p.slot_rows + row) * DK;
         if (mine && !whole) p.slot_ml[slot * p.slot_rows + row] = make_float4(base, l, rl, 0.f);

@@ -429,6 +429,30 @@ def test_large_and_small_queries():
         assert fine.any()
 
 
+@pytest.mark.parametrize("T,Hq,C", [(1, 4, 700), (1, 4, 3000), (5, 6, 3000), (9, 8, 3000)], ids=str)
+@pytest.mark.parametrize("power", [10, 20, 22, 26, 30, 60, 100])
+def test_scores_of_any_size(T, Hq, C, power):
+    """Equal scores of 2^power and more give the mean of the values, one score above
+    them its value, however far apart FP32 numbers of that size are."""
+    g = torch.Generator().manual_seed(41)
+    q = torch.full((2, T, Hq, 64), 2.0 ** (power - 11), dtype=torch.bfloat16)
+    k4 = torch.full((2, C, 2, 32), 0x77, dtype=torch.uint8), torch.full((2, C, 2, 4), 120, dtype=torch.uint8)  # 6 * 1
+    _, v4 = held_entries(g, 2, C, 2, 64), held_entries(g, 2, C, 2, 64)
+    lens = torch.tensor([C, C // 2], dtype=torch.int32)
+    out, lse = run(q, k4, v4, lens, causal=False, scale=1.0)
+    v = ref.values(*v4)
+    for b in range(2):
+        mean, size = v[b, :lens[b]].mean(0).repeat_interleave(Hq // 2, 0), v[b, :lens[b]].abs().mean(0).repeat_interleave(Hq // 2, 0)
+        tol = size * (2 * 2.0 ** -11 + 2.0 ** -16) + mean.abs() * 2.0 ** -8
+        assert ((out[b].double() - mean).abs() <= tol).all()
+    want = 64 * 6 * 2.0 ** (power - 11) + torch.log(lens.double())
+    assert ((lse.double() - want.view(2, 1, 1)).abs() <= 2.0 ** -22 * want.view(2, 1, 1)).all()
+    if power >= 20:                        # (others' scores are half of it, more than 2^18 less)
+        k4[1][:, 300] = 128                # twice the scale
+        out, _ = run(q, k4, v4, lens, causal=False, scale=1.0)
+        assert torch.equal(out, v[:, 300].bfloat16().repeat_interleave(Hq // 2, 1).unsqueeze(1).expand(out.shape))
+
+
 def test_nan_entries():
     """A NaN is that of the rows that see it, and of its 16 elements in a value."""
     T, n = 4, 60
