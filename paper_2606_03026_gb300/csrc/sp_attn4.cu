@@ -30,7 +30,7 @@
 // on an SM, and 64 chats took 59 us.)
 //
 // What bounds it: for long caches memory.  64 sequences of 4096 to 16384 entries, 32/8
-// heads of 128, 756 MB: 129 us, 5.9 TB/s (88 % of a copy's rate); at the same time 61 % of the
+// heads of 128, 756 MB: 130 us, 5.8 TB/s (87 % of a copy's rate); at the same time 61 % of the
 // issue slots, as 16 entries of a head take about 310 warp instructions (64 conversions of
 // code pairs, 64 products with scales, 17 of the matrix unit), which is what bounds 16 rows
 // (two walks over the same entries, 245 us).  For short ones the start (places on the line
