@@ -383,7 +383,8 @@ __device__ __forceinline__ void finish(const Attend4Params& p, int b, int h, int
   const int tok = p.by_G(r, &in_head), hq = h * p.G + in_head;
   if (!(other == -INFINITY)) {
     const float to = fmaxf(base, other);
-    const float f = base == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to);
+    // (what the rounding of probabilities did to their sum must not change the parts' weights)
+    const float f = base == -INFINITY ? 0.f : ex2(base - to), fo = ex2(other - to), fr = l == 0.f ? 0.f : f * (l / r_sum);
     const uint16_t* from = static_cast<const uint16_t*>(p.c.other_out) + b * p.c.other_batch + tok * p.c.other_token +
                            hq * p.c.other_head + d;
 #pragma unroll
@@ -391,11 +392,11 @@ __device__ __forceinline__ void finish(const Attend4Params& p, int b, int h, int
       if (d + i < p.D) {
         const uint2 raw = *reinterpret_cast<const uint2*>(from + i);
         const float2 lo = to_float(p.bf16, raw.x), hi = to_float(p.bf16, raw.y);
-        o[i] = fmaf(fo, lo.x, f * o[i]), o[i + 1] = fmaf(fo, lo.y, f * o[i + 1]);
-        o[i + 2] = fmaf(fo, hi.x, f * o[i + 2]), o[i + 3] = fmaf(fo, hi.y, f * o[i + 3]);
+        o[i] = fmaf(fo, lo.x, fr * o[i]), o[i + 1] = fmaf(fo, lo.y, fr * o[i + 1]);
+        o[i + 2] = fmaf(fo, hi.x, fr * o[i + 2]), o[i + 3] = fmaf(fo, hi.y, fr * o[i + 3]);
       }
     l = fmaf(l, f, fo);
-    r_sum = fmaf(r_sum, f, fo);
+    r_sum = l;
     base = to;
   }
   const bool empty = l == 0.f;

@@ -293,6 +293,18 @@ def test_joined_with_other_attention(dtype):
     check(q, k4, v4, lens, run(q, k4, v4, lens, other=other), other=other)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("T,Hq,C", [(1, 32, 40), (4, 40, 40), (1, 32, 2000)], ids=str)
+def test_parts_are_weighed_by_unrounded_sums(T, Hq, C, dtype):
+    """Values of nothing beside other attention of 1: what comes out is the weight."""
+    q, k4, v4, lens = make(42, 40, T, Hq, 4, 64, C, [2 + b for b in range(39)] + [C], dtype)
+    v4[0][:] = 0
+    lse = ref.attend(q, ref.values(*k4), ref.values(*v4), lens, scale=0.02)[1]
+    lse = torch.where(lse.isfinite(), lse, 0.0)
+    other = torch.ones_like(q), (lse + torch.linspace(-3, 3, Hq)).float()
+    check(q, k4, v4, lens, run(q, k4, v4, lens, scale=0.02, other=other), scale=0.02, other=other)
+
+
 @pytest.mark.parametrize("T,Hq,D", [(1, 6, 128), (5, 10, 64), (1, 6, 64), (4, 40, 128), (9, 42, 64)], ids=str)
 def test_joined_in_place(T, Hq, D):
     """Into the tensors of what is joined, by calls of other lengths one after the other:
