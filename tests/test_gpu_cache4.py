@@ -582,6 +582,32 @@ def test_back_to_back_calls_see_each_others_results(T, Hq, C, layout):
     cache.close()
 
 
+@pytest.mark.parametrize("T,Hq", [(1, 8), (5, 24)], ids=str)
+def test_handles_on_streams_at_once(T, Hq):
+    """Two 4-bit caches and one in 16 bits, each on a stream of its own."""
+    B, Hkv, D, C = 6, 2, 128, 6000
+    x = [make(43 + i, B, T, Hq, Hkv, D, C, [C - 900 * b - i for b in range(B)], "bf16", garbage=False) for i in range(2)]
+    on = [[q.to(DEV), tuple(y.to(DEV) for y in k4), tuple(y.to(DEV) for y in v4), lens.to(DEV)] for q, k4, v4, lens in x]
+    caches, streams = [sp.Cache4(Hq, Hkv, D, C, max_T=T) for _ in range(2)], [torch.cuda.Stream() for _ in range(3)]
+    outs = [[torch.zeros_like(o[0]) for _ in range(15)] for o in on]
+    own = sp.Cache(B, Hq, Hkv, D, 1000, max_T=T)
+    g = torch.Generator(device=DEV).manual_seed(45)
+    k, v = (torch.randn(B, 1000, Hkv, D, generator=g, device=DEV).bfloat16() for _ in range(2))
+    lens16, outs16 = torch.full((B,), 1000, dtype=torch.int32, device=DEV), [torch.zeros_like(on[0][0]) for _ in range(15)]
+    torch.cuda.synchronize()
+    for i in range(15):
+        for cache, o, out, stream in zip(caches, on, outs, streams):
+            cache.attend(o[0], o[1], o[2], o[3], out[i], stream=stream)
+        own.attend(on[0][0], k, v, lens16, outs16[i], stream=streams[2])
+    torch.cuda.synchronize()
+    for cache, o, out, y in zip(caches, on, outs, x):
+        alone = run(*y)[0]
+        assert cache.status() == sp.SP_OK and all(torch.equal(z.cpu(), alone) for z in out)
+        cache.close()
+    assert own.status() == sp.SP_OK and all(torch.equal(z, outs16[0]) for z in outs16)
+    own.close()
+
+
 def test_replayed_from_graphs_on_another_stream():
     """Two graphs on one handle, replayed in turn on new inputs."""
     x = [make(27 + i, 2, 1, 4, 2, 128, 3000, [3000, 40 + i], "bf16") for i in range(3)]
