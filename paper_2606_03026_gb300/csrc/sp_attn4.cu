@@ -48,14 +48,12 @@ constexpr int kTile = 32, kSubs = kTile / 16;   // entries of a tile, instructio
 constexpr int kStart = 2;                  // cost of a unit beside its tiles
 constexpr int kSmallTiles = 24;            // of a cache whose units are CTAs' by themselves
 
-// CTAs of an SM, by the registers that NT x 8 rows take (and scales that come in pieces).
-constexpr int ctas_per_sm(int NT, bool plain) { return NT == 1 && plain ? 4 : 3; }
 template <int DK> constexpr int kStageBytes = 2 * kTile * kRowBytes<DK> + 2 * kTile * 8;
 template <int DK> constexpr int kStages = DK == 64 ? 4 : 3;
 template <int DK, int NT> constexpr int kQueryBytes = NT > 1 ? NT * (DK / 16) * 32 * 8 : 0;
 template <int DK, int NT> constexpr int kWarpBytes = kStages<DK> * kStageBytes<DK> + kQueryBytes<DK, NT>;
-static_assert(ctas_per_sm(1, true) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
-              ctas_per_sm(2, true) * (kWarps * kWarpBytes<64, 2> + 1280) <= 228 * 1024, "shared memory of an SM");
+static_assert(attend4_blocks(1, true) * (kWarps * kWarpBytes<128, 1> + 1280) <= 228 * 1024 &&
+              attend4_blocks(2, true) * (kWarps * kWarpBytes<64, 2> + 1280) <= 228 * 1024, "shared memory of an SM");
 static_assert(kWarps * kWarpBytes<64, 1> >= (SPIKE_PROJ_CACHE_MAX_B + 1) * 4, "room for the costs before each sequence");
 
 // From shared memory, in order with the waits for its copies.
@@ -163,7 +161,7 @@ __device__ __forceinline__ void finish_row(const Params& p, int b, int h, int r,
 // PLAIN: heads of DK elements; else of fewer, whose rows are not of whole 16 bytes.
 // SMALL: a unit is a CTA's, whose warps share its tiles out and merge their parts.
 template <int DK, int NT, bool PLAIN, bool SMALL>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(NT, PLAIN)) attend4_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kThreads, attend4_blocks(NT, PLAIN)) attend4_kernel(const __grid_constant__ Params p) {
   constexpr int KS = DK / 16;              // steps of S's sum, m-tiles of O
   constexpr int RB = kRowBytes<DK>, NS = kStages<DK>;
   constexpr int SB = NT == 1 ? kSubs : 1;  // instructions' entries between two looks at the maximum
@@ -625,10 +623,10 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
   const int2 unit = __ldcg(p.units + bh * p.blocks + block);
   if (unit.x < 0) return;
   const float other = other_of(p, b, h, r);
-  const int first = unit.x >> 1;
-  const int parts = (int)p.by_side(max(0, unit.y - first)) + 1;
+  const Parts4 noted = noted_parts(unit.x, unit.y, p.workers);
+  const int first = noted.slot / 2, parts = (int)p.by_side(noted.rest) + 1;
   RowSum<DK> a = sum_parts<DK, WPR, 8>(p, in, warp, parts,
-                                       [&](int i) { return i == 0 ? (int64_t)unit.x : 2 * (first + (int64_t)i * p.side); });
+                                       [&](int i) { return i == 0 ? (int64_t)noted.slot : 2 * (first + (int64_t)i * p.side); });
   if constexpr (WPR > 1) {
     __shared__ float s_ml[WPR][3], s_o[WPR][DK];
 #pragma unroll
@@ -659,8 +657,6 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
 }
 
 // ---- host ---------------------------------------------------------------------
-size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-
 template <int DK, int WPR>
 cudaError_t launch_merge(const Params& p, cudaStream_t s) {
   return launch_pdl(merge4_kernel<DK, WPR>, dim3((unsigned)((int64_t)p.c.B * p.Hkv * p.R)), dim3(32 * WPR), 0, s, p);
@@ -677,48 +673,10 @@ cudaError_t launch_t(const Params& p, int dev, int grid, cudaStream_t s) {
   return launch_pdl(attend4_kernel<DK, NT, PLAIN, SMALL>, dim3((unsigned)grid), dim3(kThreads), bytes, s, p);
 }
 
-// How the R query rows of a K/V head are taken: by warps or by CTAs, in units of as many
-// rows, workers.  A warp's registers hold O of 8 rows of 128-wide heads, of 16 of 64-wide
-// ones, and it decodes an entry for these alone; the CTAs of attend4_rows_kernel decode it
-// for up to 96, in a pipeline that takes as long for one row as for 64.  us by warps and by CTAs:
-// 64-wide heads, 32 sequences up to 8000, 6 rows 25, 49; 15 rows 36, 50; 16 rows of 64
-// sequences up to 16384 131, 218; 32 rows (two units of 16 side by side) 248, 225.  128-wide
-// heads, 64 sequences up to 16384, 8 rows 131, 262; 12 rows (two units) 245, 264; 24 (three)
-// 364, 271; 16 sequences up to 6000, 16 rows 34, 37; 24 rows 45, 38.
-struct Plan {
-  bool wide, plain, by_ctas;
-  int blocks, rows, NT, workers;
-};
-Plan plan_of(int R, int D, int sms) {
-  Plan x;
-  x.wide = D > 64;
-  x.plain = D == (x.wide ? 128 : 64);
-  x.by_ctas = R > 16;
-  x.blocks = ceil_div(R, x.by_ctas ? kRowsMost4 : x.wide ? 8 : 16);
-  x.rows = ceil_div(R, x.blocks);
-  x.NT = ceil_div(x.rows, 8);
-  x.workers = x.by_ctas ? rows4_workers(sms) : sms * ctas_per_sm(x.NT, x.plain) * kWarps;
-  return x;
-}
-
 }  // namespace
 
-Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
-  const size_t DK = s.D <= 64 ? 64 : 128;
-  Cache4Workspace w{};
-  size_t units = 0, most = 0;
-  for (int T = 1; T <= s.max_T; ++T) {
-    const Plan x = plan_of(T * (s.Hq / s.Hkv), s.D, sms);
-    units = max(units, (size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * x.blocks * 8);
-    most = max(most, 2 * (size_t)x.workers * 8 * x.NT * (16 + DK * 4));
-  }
-  w.slots = round256(units);
-  w.bytes = w.slots + most;
-  return w;
-}
-
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c) {
-  return (int64_t)c.B * s.Hkv * plan_of(c.T * (s.Hq / s.Hkv), s.D, 1).blocks * (kStart + ceil_div(s.capacity, kTile));
+  return (int64_t)c.B * s.Hkv * plan4_of(c.T * (s.Hq / s.Hkv), s.D, 1).blocks * (kStart + ceil_div(s.capacity, kTile));
 }
 
 cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, int* err, int fault,
@@ -733,7 +691,7 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.D = s.D;
   p.capacity = s.capacity;
   p.R = c.T * p.G;
-  const Plan plan = plan_of(p.R, s.D, sms);
+  const Plan4 plan = plan4_of(p.R, s.D, sms);
   p.blocks = plan.blocks;
   p.block_rows = plan.rows;
   p.by_blocks = Divide(p.blocks);
@@ -753,10 +711,12 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.err = err;
   p.fault = fault;
   p.limit = fault == kFaultStall ? kStallWaitCycles : kWaitLimitCycles;
+  p.workers = plan.workers;
   p.slot_rows = 8 * plan.NT;
+  const Slots4 at = slots4_of(plan);
   p.units = reinterpret_cast<int2*>(ws);
-  p.slot_ml = reinterpret_cast<float4*>(ws + slots);
-  p.slot_o = reinterpret_cast<float*>(ws + slots + 2 * (size_t)plan.workers * p.slot_rows * 16);
+  p.slot_ml = reinterpret_cast<float4*>(ws + slots + at.ml);
+  p.slot_o = reinterpret_cast<float*>(ws + slots + at.o);
   const int64_t units = (int64_t)c.B * s.Hkv * plan.blocks;
   // Units that a CTA has by itself need neither the line nor the merge of another
   // kernel (one sequence, 4 heads, 60 of 512 entries: 4.6 us instead of 8.0).

@@ -20,7 +20,7 @@ struct Attend4Params {
   int32_t side;                            // workers that walk side by side, each in units of its own
   int32_t on_line;                         // places of a sequence's units on the line: Hkv blocks / side
   Divide by_side;
-  int32_t slot_rows;                       // rows of a slot
+  int32_t workers, slot_rows;              // two slots a worker; rows of one
   int32_t bf16;
   float c2;                                // scale * log2 e
   int* err;
@@ -32,13 +32,11 @@ struct Attend4Params {
 };
 
 // Units of more rows than one warp takes, a CTA each (sp_attn4_rows.cu).
-constexpr int kRowsMost4 = 96;
-int rows4_workers(int sms);
 cudaError_t launch_attend4_rows(const Attend4Params& p, int dev, int sms, cudaStream_t s);
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kWarps = kWarps4, kThreads = 32 * kWarps;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The reference of the exponentials follows the running maximum only when that has
 // grown by more than 2^kLag; it lies kLift below, so that half precision's

@@ -544,8 +544,6 @@ cudaError_t launch_t(const Params& p, int dev, int sms, cudaStream_t s) {
 
 }  // namespace
 
-int rows4_workers(int sms) { return 2 * sms; }
-
 cudaError_t launch_attend4_rows(const Attend4Params& p, int dev, int sms, cudaStream_t s) {
   if (p.D <= 64) return p.D == 64 ? launch_t<64, true>(p, dev, sms, s) : launch_t<64, false>(p, dev, sms, s);
   return p.D == 128 ? launch_t<128, true>(p, dev, sms, s) : launch_t<128, false>(p, dev, sms, s);

@@ -22,10 +22,71 @@ constexpr int kGroup4 = 16;                // elements of a scale
 constexpr uint32_t kNaNScale4 = 0xff;      // scale of a group with a NaN or an infinity
 constexpr float kMaxScale4 = 10240.f;
 
+// How the R query rows of a K/V head are taken: by warps or by CTAs, in units of as many
+// rows, workers.  A warp's registers hold O of 8 rows of 128-wide heads, of 16 of 64-wide
+// ones, and it decodes an entry for these alone; the CTAs of attend4_rows_kernel decode it
+// for up to 96, in a pipeline that takes as long for one row as for 64.  us by warps and by CTAs:
+// 64-wide heads, 32 sequences up to 8000, 6 rows 25, 49; 15 rows 36, 50; 16 rows of 64
+// sequences up to 16384 131, 218; 32 rows (two units of 16 side by side) 248, 225.  128-wide
+// heads, 64 sequences up to 16384, 8 rows 131, 262; 12 rows (two units) 245, 264; 24 (three)
+// 364, 271; 16 sequences up to 6000, 16 rows 34, 37; 24 rows 45, 38.
+constexpr int kWarps4 = 4;                 // of a block of attend4_kernel
+constexpr int kRowsMost4 = 96;             // of a unit of attend4_rows_kernel
+// Blocks of an SM, by the registers that NT x 8 rows take (and scales that come in pieces).
+constexpr int attend4_blocks(int NT, bool plain) { return NT == 1 && plain ? 4 : 3; }
+constexpr int rows4_workers(int sms) { return 2 * sms; }
+struct Plan4 {
+  bool wide, plain, by_ctas;
+  int blocks, rows, NT, workers;
+};
+inline Plan4 plan4_of(int R, int D, int sms) {
+  Plan4 x;
+  x.wide = D > 64;
+  x.plain = D == (x.wide ? 128 : 64);
+  x.by_ctas = R > 16;
+  x.blocks = ceil_div(R, x.by_ctas ? kRowsMost4 : x.wide ? 8 : 16);
+  x.rows = ceil_div(R, x.blocks);
+  x.NT = ceil_div(x.rows, 8);
+  x.workers = x.by_ctas ? rows4_workers(sms) : sms * attend4_blocks(x.NT, x.plain) * kWarps4;
+  return x;
+}
+
+// A handle's workspace: notes on the units, then the slots of parts, two a worker: a row's
+// reference and sums (16 bytes), and its DK elements.
+struct Slots4 {
+  size_t ml, o, end;                       // bytes from the first slot's on
+};
+inline Slots4 slots4_of(const Plan4& x) {
+  const size_t rows = 2 * (size_t)x.workers * 8 * x.NT;
+  return Slots4{0, rows * 16, rows * (16 + (x.wide ? 128 : 64) * 4)};
+}
 struct Cache4Workspace {
   size_t slots, bytes;                     // parts of units; notes on the units lie before them
 };
-Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms);
+inline Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
+  size_t units = 0, most = 0;
+  for (int T = 1; T <= s.max_T; ++T) {
+    const Plan4 x = plan4_of(T * (s.Hq / s.Hkv), s.D, sms);
+    const size_t u = (size_t)SPIKE_PROJ_CACHE_MAX_B * s.Hkv * x.blocks * 8, p = slots4_of(x).end;
+    units = u > units ? u : units;
+    most = p > most ? p : most;
+  }
+  const size_t slots = (units + 255) / 256 * 256;
+  return Cache4Workspace{slots, slots + most};
+}
+
+// The parts of a unit as merge4_kernel finds them noted: in slot `slot`, and in the first
+// slots, 2 w, of the workers w behind that one (slot / 2) that walk beside it, up to `rest` on.
+// Where attend4_rows_kernel gave up on a wait the note may be an earlier call's, of more
+// workers with fewer rows each, so that both numbers are taken into what this call has
+// (a reversed pair holds the first part alone).  slot >= 0.
+struct Parts4 {
+  int32_t slot, rest;
+};
+inline __host__ __device__ Parts4 noted_parts(int32_t slot, int32_t last, int32_t workers) {
+  const int32_t s = slot < 2 * workers ? slot : 2 * workers - 1, l = last < workers ? last : workers - 1;
+  return Parts4{s, l > s / 2 ? l - s / 2 : 0};
+}
 
 // Tiles of entries that an attend call has at most (its kernels count them in 32 bits).
 int64_t attend4_tiles(const Cache4Shape& s, const sp_attend4& c);
