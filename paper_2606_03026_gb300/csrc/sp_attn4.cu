@@ -621,12 +621,11 @@ __global__ void __launch_bounds__(32 * WPR) merge4_kernel(const __grid_constant_
   const int r = (int)(id - bh * p.R), block = r / p.block_rows, in = r - block * p.block_rows;
   const int b = (int)(bh / p.Hkv), h = (int)(bh - (int64_t)b * p.Hkv);
   const int2 unit = __ldcg(p.units + bh * p.blocks + block);
-  if (unit.x < 0) return;
+  if (unit.x < 0 || !parts_within(unit.x, unit.y, p.workers)) return;
   const float other = other_of(p, b, h, r);
-  const Parts4 noted = noted_parts(unit.x, unit.y, p.workers);
-  const int first = noted.slot / 2, parts = (int)p.by_side(noted.rest) + 1;
+  const int first = unit.x >> 1, parts = (int)p.by_side(max(0, unit.y - first)) + 1;
   RowSum<DK> a = sum_parts<DK, WPR, 8>(p, in, warp, parts,
-                                       [&](int i) { return i == 0 ? (int64_t)noted.slot : 2 * (first + (int64_t)i * p.side); });
+                                       [&](int i) { return i == 0 ? (int64_t)unit.x : 2 * (first + (int64_t)i * p.side); });
   if constexpr (WPR > 1) {
     __shared__ float s_ml[WPR][3], s_o[WPR][DK];
 #pragma unroll

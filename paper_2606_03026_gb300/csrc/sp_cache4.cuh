@@ -75,17 +75,13 @@ inline Cache4Workspace cache4_workspace(const Cache4Shape& s, int sms) {
   return Cache4Workspace{slots, slots + most};
 }
 
-// The parts of a unit as merge4_kernel finds them noted: in slot `slot`, and in the first
-// slots, 2 w, of the workers w behind that one (slot / 2) that walk beside it, up to `rest` on.
-// Where attend4_rows_kernel gave up on a wait the note may be an earlier call's, of more
-// workers with fewer rows each, so that both numbers are taken into what this call has
-// (a reversed pair holds the first part alone).  slot >= 0.
-struct Parts4 {
-  int32_t slot, rest;
-};
-inline __host__ __device__ Parts4 noted_parts(int32_t slot, int32_t last, int32_t workers) {
-  const int32_t s = slot < 2 * workers ? slot : 2 * workers - 1, l = last < workers ? last : workers - 1;
-  return Parts4{s, l > s / 2 ? l - s / 2 : 0};
+// A unit's parts, as merge4_kernel finds them noted: in slot `slot` >= 0, and in the first
+// slots, 2 w, of the workers w behind that one (slot / 2) that walk beside it, up to `last` (none:
+// last <= slot / 2).  Where attend4_rows_kernel gave up on a wait the note may be an earlier call's,
+// of more workers with fewer rows each: whether it is of slots that this call has, of
+// `workers` workers.
+inline __host__ __device__ bool parts_within(int32_t slot, int32_t last, int32_t workers) {
+  return slot < 2 * workers && last < workers;
 }
 
 // Tiles of entries that an attend call has at most (its kernels count them in 32 bits).
