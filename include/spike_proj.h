@@ -837,12 +837,13 @@ sp_status spike_proj_cache4_read(sp_cache4_t cache, const sp_read4 *call,
  * other_lse is not used, whatever it holds.  Entries that no row sees are never used,
  * whatever they hold, nor is what a row does not see by it; a NaN key that a row sees
  * makes that row NaN, and NaN values the elements of it that they are of, however
- * little weight the entry has.  Codes times scales are exact; each query row
- * is brought to half precision by a power of two (what that loses is below 2^-38 of
- * the row's largest element), probabilities are rounded to half precision before they
+ * little weight the entry has.  Codes times scales are exact; each bf16 query row is
+ * brought to half precision by a power of two, whatever its size (what that loses is
+ * below 2^-38 of its largest element); probabilities are rounded to half precision before they
  * meet V, and out is divided by the sum of the rounded ones; lse takes them unrounded.
- * Scores, maxima and sums are FP32.  Results do not depend on the order in which
- * blocks run.
+ * Scores, maxima and sums are FP32: an entry whose score lies below its range has no
+ * weight, and of a row with a score above it nothing is defined.  Results do not depend
+ * on the order in which blocks run.
  *
  *   lens       device int32 [B]; values outside 0 .. capacity are taken as
  *              the nearest end.

@@ -7,9 +7,9 @@
 // attention of the same rows over other entries where that is given.
 //
 // Codes become half precision in registers, where both products take them from:
-// a code times its scale is exact there.  Queries are half precision too, each row
-// times a power of two that brings its largest element to 2^14 .. 2^15, so that
-// bf16's range fits (what is lost lies 2^-39 below the row's largest).  Entries are
+// a code times its scale is exact there.  Queries are half precision too, each row of
+// bf16 times a power of two that brings its largest element to 2^14 .. 2^15, so that
+// its range fits (what is lost lies 2^-39 below the row's largest).  Entries are
 // the rows of the matrix instructions (m16n8k16), query rows their 8 columns: for
 // few rows an instruction is full of entries.  The order of the elements of a row
 // in an instruction's sum, and of the entries in the other's, is free, so that a
@@ -36,6 +36,7 @@
 // (two walks over the same entries, 245 us).  For short ones the start (places on the line
 // 1.6 us, first tiles there at 5 to 9) and the merge with its launch (4): 64 chats of 2048
 // entries on average, 76 MB, 27 us.
+#include <cmath>
 #include <type_traits>
 
 #include "sp_attn4.cuh"
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, attend4_blocks(NT, PLAIN)) attend4_k
     int far[NT][2];                        // entries that they see
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const float down = make_query<DK>(p, x[i]);
+      const float by = make_query<DK>(p, x[i]);
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
         if (NT == 1) q[j] = x[i][j];
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, attend4_blocks(NT, PLAIN)) attend4_k
       // (lane 4 r has row r's)
 #pragma unroll
       for (int e2 = 0; e2 < 2; ++e2) {
-        c2[i][e2] = __shfl_sync(0xffffffffu, down, 4 * (2 * t + e2));
+        c2[i][e2] = __shfl_sync(0xffffffffu, by, 4 * (2 * t + e2));
         const int r2 = i * 8 + 2 * t + e2;
         far[i][e2] = r2 < rows && p.c.causal ? n - (p.c.T - 1 - (int)p.by_G(row0 + r2)) : n;
       }
@@ -706,7 +707,9 @@ cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* w
   p.on_line = s.Hkv * p.blocks / p.side;
   p.by_side = Divide(p.side);
   p.bf16 = s.dtype == SP_BF16;
-  p.c2 = c.scale * kLog2e;
+  // (the product in 64 bits, whose range no scale leaves)
+  p.c2 = 2.f * (float)std::frexp((double)c.scale * (double)kLog2e, &p.c2_power);
+  --p.c2_power;
   p.err = err;
   p.fault = fault;
   p.limit = fault == kFaultStall ? kStallWaitCycles : kWaitLimitCycles;

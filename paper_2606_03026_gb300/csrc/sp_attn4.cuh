@@ -22,7 +22,8 @@ struct Attend4Params {
   Divide by_side;
   int32_t workers, slot_rows;              // two slots a worker; rows of one
   int32_t bf16;
-  float c2;                                // scale * log2 e
+  float c2;                                // scale * log2 e is c2 2^c2_power, 1 <= c2 <= 2
+  int32_t c2_power;
   int* err;
   int fault;                               // kFaultStall: the first keys are never there (tests of the error path)
   long long limit;                         // cycles that a wait takes at most
@@ -281,14 +282,31 @@ __device__ __forceinline__ void load_query(const Attend4Params& p, int b, int h,
       if (t * (DK / 4) + 4 * j < p.D) x[j] = *reinterpret_cast<const uint2*>(from + 4 * j);
   }
 }
-// These as the instructions take them, in half precision.  Returns what the row's scores
-// are to be multiplied by (not 0, so that masked ones stay -infinity).
+// The size of queries.  A row of bf16 is brought to half precision times 2^e, which puts its
+// largest finite element at 2^14 .. 2^15.  e is at most 126, as far as a factor of FP32 goes: of
+// a row below 2^-112 nothing is lost there, as bf16's numbers are multiples of 2^-133.
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ int lift_of(uint32_t top) { return min(14 - ((int)(top >> 7) - 127), 126); }  // bits of that element
+// What the matrix instructions' scores s of such a row are multiplied by, scale log2 e 2^-e =
+// c2 2^power: `by`, within 2^-126 .. 2^127, times `more`.  by is not 0, so that masked scores stay
+// -infinity, nor infinite, times which a difference of 0 were a NaN.  Weights do not change by these
+// limits: s is below 2^39, and a multiple of 2^-42 (2^-24 of queries, 2^-18 of keys), so that
+// where `more` is not 1 scores are equal or more than 2^83 apart.  An lse does: see finish().
+struct RowFactor {
+  float by, more;
+};
+__device__ __forceinline__ RowFactor factor_of(const Attend4Params& p, int e) {
+  const int power = p.c2_power - e, some = min(max(power, -126), 126);
+  return RowFactor{p.c2 * power_of_two(some), power_of_two(max(power - some, 0))};
+}
+
+// These as the instructions take them, in half precision.  Returns what the row's scores are to
+// be multiplied by.
 template <int DK>
 __device__ __forceinline__ float make_query(const Attend4Params& p, uint2 (&x)[DK / 16]) {
   constexpr int KS = DK / 16;
   int e = 0;
   if (p.bf16) {
-    // 2^e that brings the largest that is finite to 2^14 .. 2^15
     const auto largest = [&](bool all) {
       uint32_t top = 0;
 #pragma unroll
@@ -303,15 +321,15 @@ __device__ __forceinline__ float make_query(const Attend4Params& p, uint2 (&x)[D
     };
     uint32_t top = largest(true);
     if (__any_sync(0xffffffffu, top >= 0x7f80u)) top = largest(false);
-    e = min(14 - ((int)(top >> 7) - 127), 100);
-    const float up = __int_as_float((e + 127) << 23);
+    e = lift_of(top);
+    const float up = power_of_two(e);
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
       const float2 lo = to_float(true, x[j].x), hi = to_float(true, x[j].y);
       x[j] = make_uint2(pack_half2(lo.x * up, lo.y * up), pack_half2(hi.x * up, hi.y * up));
     }
   }
-  return fmaxf(p.c2 * __int_as_float((127 - e) << 23), 0x1p-126f);
+  return factor_of(p, e).by;
 }
 
 // A row's scales on their way: what a load brings is not looked at before value(), so
@@ -379,6 +397,17 @@ __device__ __forceinline__ void finish(const Attend4Params& p, int b, int h, int
                                        float (&o)[N], float other, bool first) {
   uint32_t in_head;
   const int tok = p.by_G(r, &in_head), hq = h * p.G + in_head;
+  if (fabsf(base) >= 0x1p64f && base != -INFINITY) {           // (where more may not be 1: at 2^83 and above)
+    const uint16_t* q = static_cast<const uint16_t*>(p.c.q) + b * p.c.q_batch + tok * p.c.q_token + hq * p.c.q_head;
+    uint32_t top = 0;
+#pragma unroll 1
+    for (int i = 0; i < p.D; ++i) {
+      const uint32_t x = q[i] & 0x7fffu;
+      if (x < 0x7f80u) top = max(top, x);
+    }
+    base *= factor_of(p, p.bf16 ? lift_of(top) : 0).more;
+    if (base == -INFINITY) l = 0.f;        // (scores below FP32's range)
+  }
   if (!(other == -INFINITY)) {
     const float to = fmaxf(base, other);
     // (what the rounding of probabilities did to their sum must not change the parts' weights)

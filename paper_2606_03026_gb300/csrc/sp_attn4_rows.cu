@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       // The thread's row of queries (the tiles before have been multiplied: their scores
       // were here).  A row a thread, not a row by several: the loads touch more lines, but
       // a warp has a third of the instructions, and it has them to itself.
-      float c2 = fmaxf(p.c2, 0x1p-126f);   // (not 0, so that masked scores stay -infinity)
+      int e = 0;                           // (see factor_of)
       if (work) {
         uint32_t in;
         const int token = p.by_G(mine ? r : 0, &in);
@@ -369,10 +369,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
           };
           uint32_t most = largest(false);
           if (most >= 0x7f80u) most = largest(true);
-          // 2^up brings the row's largest that is finite to 2^14 .. 2^15
-          const int up = min(14 - ((int)(most >> 7) - 127), 100);
-          by = __int_as_float((up + 127) << 23);
-          c2 = fmaxf(p.c2 * __int_as_float((127 - up) << 23), 0x1p-126f);
+          e = lift_of(most);
+          by = power_of_two(e);
         }
         const f32x2 by2 = pair(by, by);
 #pragma unroll
@@ -391,6 +389,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) attend4_rows_kernel(const __gr
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars.q_full);
+      const float c2 = factor_of(p, e).by;
       const int far = p.c.causal ? n - (p.c.T - 1 - tok) : n;  // entries that the row sees
       // how far above the maximum that the reference has it follows (at first from anywhere), that maximum; sums
       float lag = -INFINITY, m = 0.f, l = 0.f, rl = 0.f;
