@@ -17,12 +17,12 @@
 // with a ninth and 96 the loops spilled and a tile took twice as long.)
 // A row's queries are times a power of two, and its scores are masked, by its thread.
 //
-// What bounds it: shared memory.  A tile of 128-wide heads moves 114 KB in it (codes in and
-// out 18, half precision in 32, operands 64, of which half are the 128 rows of Q that the
-// MMA reads again for each tile): 890 cycles at 128 bytes; with two CTAs an SM a tile takes 1950,
-// for 16 rows as for 64.  16 sequences of 3500 entries, 64/8 heads, 8 tokens, 69 MB: 48 us, of
-// which 6.4 until the first scores (places 2.2, queries 3, product 1), 24 the tiles, 2 a
-// unit's end, 9 the merge of 8192 rows.
+// What bounds it: for half of its time, by the bytes that the code moves, shared memory.  A tile of
+// 128-wide heads moves 114 KB in it (codes in and out 18, half precision in 32, operands 64, of
+// which half are the 128 rows of Q that the MMA reads again for each tile): 890 cycles at 128 bytes;
+// with two CTAs an SM a tile takes 1950, for 16 rows as for 64.  16 sequences of 3500 entries, 64/8
+// heads, 8 tokens, 69 MB: 48.5 us, of which 6.4 until the first scores (places 2.2, queries 3,
+// product 1), 24 the tiles, 2 a unit's end, 9 the merge of 8192 rows.
 #include "sp_attn4.cuh"
 
 namespace sp {

@@ -91,7 +91,8 @@ cudaError_t launch_read4(const Cache4Shape& s, const sp_read4& c, cudaStream_t s
 cudaError_t launch_attend4(const Cache4Shape& s, const sp_attend4& c, uint8_t* ws, size_t slots, int* err, int fault,
                            cudaStream_t stream);
 
-// n / d and n % d for n < 2^31, d < 2^31.
+// n / d and n % d for n < 2^31, d < 2^31: a product with the reciprocal, rounded up to 33 bits
+// (Granlund and Montgomery, "Division by invariant integers using multiplication", 1994).
 struct Divide {
   uint32_t mul = 0, shift = 0, d = 0;
   Divide() = default;
